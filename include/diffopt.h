@@ -499,6 +499,226 @@ int diffopt_es_weights(const float* fvals, const float* f0,
                        int64_t num_samples, int32_t method, double sigma,
                        float* weights, void* stream);
 
+/* -------------------------------------------------------------------------
+ * Operators of a language model that an inner loop adapts.  Listing 1's inner
+ * step differentiates its loss with the graph kept and the outer loss
+ * differentiates through that gradient, so each of these has the derivative
+ * of its backward too: as an entry point of its own (..._bwd_bwd), or, for
+ * linear attention, as calls of its own forward and backward.
+ * Element types: DIFFOPT_F32, or DIFFOPT_BF16 for activations; every sum,
+ * softmax statistic, norm and state is fp32, each result is rounded once.
+ */
+#define DIFFOPT_F32 0
+#define DIFFOPT_BF16 1
+
+/* A device tensor [B][T][heads][width] of a call's element type: elements of
+ * a head are contiguous, the other axes have strides in elements (any sign;
+ * an axis of an input may be broadcast with stride 0, outputs must not
+ * overlap themselves).  Pointers need the element type's alignment only;
+ * 16-byte aligned rows are fastest, the results do not depend on it.       */
+typedef struct diffopt_heads {
+  void* data;
+  int64_t stride_b, stride_t, stride_h;
+} diffopt_heads;
+
+/* Linear attention with a decay for each head, over sequences: with
+ * g = exp(log_decay[j]) for k/v head j = h / (H / Hk) of query head h,
+ *   S_t = g S_{t-1} + k_t v_t^T          (one state per k/v head, S_{-1} = state)
+ *   out_t = scale S_t^T q_t              t = 0 .. lengths[b] - 1
+ *   state_out = S_{lengths[b]-1}         (state for a length of 0)
+ * (an unrolled inner loop in itself: the update is a decayed gradient step on
+ * -<S^T k, v>).  Tokens from lengths[b] on are not read and get out = 0.
+ *   q [B][T][H][Dk], k [B][T][Hk][Dk], v [B][T][Hk][Dv], out [B][T][H][Dv]
+ *   log_decay  DEVICE fp32 [Hk], <= 0 (0: no decay; -inf: the token alone)
+ *   lengths    DEVICE int32 [B] in [0, T] (clamped), or NULL for T
+ *   state, state_out  fp32 [B][Hk][Dk][Dv], or NULL (zeros / not wanted);
+ *              state_out may be state
+ *   1 <= Dk, Dv <= 256; H a multiple of Hk; scale finite
+ *   workspace  device scratch of diffopt_linattn_workspace(..., backward 0)
+ *              bytes (its contents do not matter, 16-byte aligned); NULL if
+ *              that is 0
+ * B, T or H == 0 is a no-op but for state_out.                             */
+int diffopt_linattn_fwd(const diffopt_heads* q, const diffopt_heads* k,
+                        const diffopt_heads* v, const float* log_decay,
+                        const int32_t* lengths, const float* state, int64_t B,
+                        int64_t T, int64_t H, int64_t Hk, int64_t Dk,
+                        int64_t Dv, int32_t dtype, double scale,
+                        const diffopt_heads* out, float* state_out,
+                        void* workspace, int64_t workspace_bytes,
+                        void* stream);
+
+/* Its vector-Jacobian product, for cotangents dout and dstate_out (NULL: 0):
+ *   dq_t = scale sum_{s<=t} g^(t-s) (dout_t . v_s) k_s + scale g^(t+1) state dout_t
+ *   dk_s = scale sum_{t>=s} g^(t-s) (v_s . dout_t) q_t + g^(L-1-s) dstate_out v_s
+ *   dv_s = scale sum_{t>=s} g^(t-s) (k_s . q_t) dout_t + g^(L-1-s) dstate_out^T k_s
+ *   dstate = scale sum_t g^(t+1) q_t dout_t^T + g^L dstate_out,  L = lengths[b]
+ * with sums over the query heads that share a k/v head in dk, dv and dstate.
+ * Each of dq, dk, dv (pointers to the struct) and dstate may be NULL: it is
+ * then not computed.  dstate must be neither dstate_out nor state.  Rows from L on get 0.  log_decay is a constant of the
+ * operator: it has no gradient.  The three results are the forward's sum on
+ * permuted operands, so a derivative of any order is made of the same calls. */
+int diffopt_linattn_bwd(const diffopt_heads* dout, const float* dstate_out,
+                        const diffopt_heads* q, const diffopt_heads* k,
+                        const diffopt_heads* v, const float* log_decay,
+                        const int32_t* lengths, const float* state, int64_t B,
+                        int64_t T, int64_t H, int64_t Hk, int64_t Dk,
+                        int64_t Dv, int32_t dtype, double scale,
+                        const diffopt_heads* dq, const diffopt_heads* dk,
+                        const diffopt_heads* dv, float* dstate,
+                        void* workspace, int64_t workspace_bytes,
+                        void* stream);
+
+/* Bytes of workspace those two calls need for these sizes (0: none); -1 for
+ * sizes that they refuse.                                                  */
+int64_t diffopt_linattn_workspace(int64_t B, int64_t T, int64_t H, int64_t Hk,
+                                  int64_t Dk, int64_t Dv, int32_t dtype,
+                                  int32_t backward);
+
+/* One token for each of B sequences, the state updated in place:
+ *   state = g state + k v^T,  out = scale state^T q
+ * as diffopt_linattn_fwd with T = 1 (the strides of the time axis are not
+ * used).                                                                   */
+int diffopt_linattn_step(const diffopt_heads* q, const diffopt_heads* k,
+                         const diffopt_heads* v, const float* log_decay,
+                         int64_t B, int64_t H, int64_t Hk, int64_t Dk,
+                         int64_t Dv, int32_t dtype, double scale, float* state,
+                         const diffopt_heads* out, void* stream);
+
+/* RMS norms of queries and keys for each head, and the position rotation:
+ *   z = w x r,  r = (mean(x^2) + eps)^(-1/2)    over a head's D elements
+ *   out: pair (a, c) of z's first `rot` elements becomes
+ *        (a cos - c sin, c cos + a sin), the others stay
+ * Pair i is elements (i, i + rot/2), or (2i, 2i+1) with interleaved != 0.
+ *   q, q_out [B][T][H][D]; k, k_out [B][T][Hk][D] (Hk may be 0)
+ *   q_weight, k_weight  fp32 [D], or NULL for ones
+ *   cos, sin   fp32 [rows][rot/2]; token t of sequence b uses row
+ *              positions[b T + t] (int32 or int64 by position_bytes), or
+ *              first + t without positions.  A position outside [0, rows)
+ *              gives that token NaN.
+ *   1 <= D <= 1024; rot even, 0 <= rot <= D; eps >= 0
+ * q_out may be q and k_out k.                                              */
+int diffopt_qknorm_rope_fwd(const diffopt_heads* q, const diffopt_heads* k,
+                            const float* q_weight, const float* k_weight,
+                            const float* cos, const float* sin, int64_t rows,
+                            const void* positions, int32_t position_bytes,
+                            int64_t first, int64_t B, int64_t T, int64_t H,
+                            int64_t Hk, int64_t D, int64_t rot,
+                            int32_t interleaved, int32_t dtype, double eps,
+                            const diffopt_heads* q_out,
+                            const diffopt_heads* k_out, void* stream);
+
+/* Its vector-Jacobian product.  With dz the cotangent rotated back, u = w dz:
+ *   dx = r u - x r^3 (x . u) / D,   dw = sum over tokens and heads of dz x r
+ * dq_weight, dk_weight: fp32 [D], or NULL (not wanted).  dq may be dq_out and
+ * dk may be dk_out.  workspace: diffopt_qknorm_rope_workspace() bytes, needed
+ * where a weight's gradient is wanted.  Sums run in a fixed order.          */
+int diffopt_qknorm_rope_bwd(const diffopt_heads* dq_out,
+                            const diffopt_heads* dk_out,
+                            const diffopt_heads* q, const diffopt_heads* k,
+                            const float* q_weight, const float* k_weight,
+                            const float* cos, const float* sin, int64_t rows,
+                            const void* positions, int32_t position_bytes,
+                            int64_t first, int64_t B, int64_t T, int64_t H,
+                            int64_t Hk, int64_t D, int64_t rot,
+                            int32_t interleaved, int32_t dtype, double eps,
+                            const diffopt_heads* dq, const diffopt_heads* dk,
+                            float* dq_weight, float* dk_weight,
+                            void* workspace, int64_t workspace_bytes,
+                            void* stream);
+
+/* The vector-Jacobian product of that backward, for cotangents ddq = a, ddk
+ * of dq, dk and ddq_weight = b, ddk_weight (NULL: 0) of the weights' gradients:
+ *   out_dq_out  the rotation of w (r a - r^3 (x . a)/D x) + r b x
+ *   out_q_weight = sum of dz (r a - r^3 (x . a)/D x)
+ *   out_q = -r^3/D (x (a . u) + u (x . a) + a (x . u) + x (b x . dz))
+ *           + 3 r^5/D^2 x (x . u)(x . a) + r b dz
+ * and the same for k.  out_q_weight and out_k_weight may be NULL.           */
+int diffopt_qknorm_rope_bwd_bwd(
+    const diffopt_heads* ddq, const diffopt_heads* ddk,
+    const float* ddq_weight, const float* ddk_weight,
+    const diffopt_heads* dq_out, const diffopt_heads* dk_out,
+    const diffopt_heads* q, const diffopt_heads* k, const float* q_weight,
+    const float* k_weight, const float* cos, const float* sin, int64_t rows,
+    const void* positions, int32_t position_bytes, int64_t first, int64_t B,
+    int64_t T, int64_t H, int64_t Hk, int64_t D, int64_t rot,
+    int32_t interleaved, int32_t dtype, double eps,
+    const diffopt_heads* out_dq_out, const diffopt_heads* out_dk_out,
+    const diffopt_heads* out_q, const diffopt_heads* out_k,
+    float* out_q_weight, float* out_k_weight, void* workspace,
+    int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace the two calls above need; -1 for sizes they refuse.    */
+int64_t diffopt_qknorm_rope_workspace(int64_t B, int64_t T, int64_t H,
+                                      int64_t Hk, int64_t D);
+
+/* Distillation from a teacher's top logits.  For each of N rows, with the
+ * student's distribution p = softmax(logits / T) over V and the teacher's
+ * q = softmax(teacher / T) over the row's entries,
+ *   l_j = log q_j - log p[ids_j],  loss = T^2 sum_j q_j l_j
+ *   logits   [N] rows of V elements, row_stride elements apart
+ *   ids      [N][K] int32 or int64 (by id_bytes): the token of each entry.
+ *            A negative id, or a teacher logit of -inf, is no entry; a row
+ *            with none has loss 0 and gradients 0.  An id >= V makes its
+ *            row's results NaN.  Entries of one token add up.
+ *   teacher  fp32 [N][K];  1 <= K <= 1024
+ *   loss     fp32 [N]
+ *   stats    fp32 [N][2]: the row's max and its sum of exp((x - max) / T),
+ *            which the backwards take
+ *   workspace  diffopt_distill_workspace() bytes, or NULL if that is 0       */
+int diffopt_distill_fwd(const void* logits, int64_t row_stride, int64_t N,
+                        int64_t V, int32_t dtype, const void* ids,
+                        int32_t id_bytes, const float* teacher, int64_t K,
+                        double temperature, float* loss, float* stats,
+                        void* workspace, int64_t workspace_bytes,
+                        void* stream);
+
+/* Its vector-Jacobian product, for the cotangent dloss [N]:
+ *   dlogits = dloss T (p - sum_j q_j e[ids_j])  (may be logits)
+ *   dteacher_j = dloss T q_j (l_j - sum_i q_i l_i), fp32 [N][K], or NULL     */
+int diffopt_distill_bwd(const float* dloss, const void* logits,
+                        int64_t row_stride, int64_t N, int64_t V,
+                        int32_t dtype, const void* ids, int32_t id_bytes,
+                        const float* teacher, int64_t K, double temperature,
+                        const float* stats, void* dlogits, int64_t drow_stride,
+                        float* dteacher, void* stream);
+
+/* Both at once, for a caller that knows dloss before the loss (the weights
+ * of a mean): the logits are read from memory once.  dlogits must not be
+ * logits.                                                                   */
+int diffopt_distill_fwd_bwd(const float* dloss, const void* logits,
+                            int64_t row_stride, int64_t N, int64_t V,
+                            int32_t dtype, const void* ids, int32_t id_bytes,
+                            const float* teacher, int64_t K,
+                            double temperature, float* loss, float* stats,
+                            void* dlogits, int64_t drow_stride,
+                            float* dteacher, void* workspace,
+                            int64_t workspace_bytes, void* stream);
+
+/* The vector-Jacobian product of the backward, for cotangents ddlogits = a of
+ * dlogits (element type, rows ddrow_stride apart) and ddteacher = c of
+ * dteacher (either NULL: 0).  With averages under q written [.], g = dloss:
+ *   out_dloss = T (sum p a - [a_ids] + cov),  cov = [(c - [c]) (l - [l])]
+ *   out_logits = g p (a - sum p a) - g sum_j q_j (c_j - [c]) e[ids_j]
+ *   out_teacher_j = g q_j ([a_ids] - a[ids_j] + c_j - [c]
+ *                          + (c_j - [c])(l_j - [l]) - cov)
+ * out_dloss [N] and out_teacher [N][K] fp32, either may be NULL; out_logits
+ * must be neither logits nor ddlogits.                                      */
+int diffopt_distill_bwd_bwd(const void* ddlogits, int64_t ddrow_stride,
+                            const float* ddteacher, const float* dloss,
+                            const void* logits, int64_t row_stride, int64_t N,
+                            int64_t V, int32_t dtype, const void* ids,
+                            int32_t id_bytes, const float* teacher, int64_t K,
+                            double temperature, const float* stats,
+                            float* out_dloss, void* out_logits,
+                            int64_t out_row_stride, float* out_teacher,
+                            void* workspace, int64_t workspace_bytes,
+                            void* stream);
+
+/* Bytes of workspace that distill_fwd, _fwd_bwd and _bwd_bwd need; -1 for
+ * sizes they refuse.                                                        */
+int64_t diffopt_distill_workspace(int64_t N, int64_t V, int32_t dtype,
+                                  int64_t K);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,62 @@
+// Shared pieces of the language-model operators (distill, qknorm, linattn):
+// element types, vectors at any alignment, reductions, argument checks.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "common.hpp"
+
+namespace diffopt {
+
+using bf16 = __bf16;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// 16 bytes of elements as memory holds them: aligned to the element only (the
+// hardware takes 128-bit accesses at any address).
+template <class E>
+struct Vec {
+  static constexpr int N = 16 / (int)sizeof(E);
+  typedef E type __attribute__((ext_vector_type(16 / sizeof(E)), aligned(alignof(E))));
+};
+
+template <class E>
+__device__ __forceinline__ typename Vec<E>::type load_vec(const E* p) {
+  return *reinterpret_cast<const typename Vec<E>::type*>(p);
+}
+
+template <class E>
+__device__ __forceinline__ void store_vec(E* p, const float* x) {
+  typename Vec<E>::type v;
+#pragma unroll
+  for (int i = 0; i < Vec<E>::N; ++i) v[i] = (E)x[i];
+  *reinterpret_cast<typename Vec<E>::type*>(p) = v;
+}
+
+constexpr float kInf = __builtin_inff();
+constexpr float kNan = __builtin_nanf("");
+
+template <int WIDTH = 64>
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int o = WIDTH / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+
+// fmaxf drops a NaN operand; a NaN logit has to reach the row's results, which
+// it does through the sum.
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
+  return x;
+}
+
+inline bool dtype_ok(int32_t dtype) { return dtype == DIFFOPT_F32 || dtype == DIFFOPT_BF16; }
+inline int64_t elem_size(int32_t dtype) { return dtype == DIFFOPT_F32 ? 4 : 2; }
+inline bool aligned_to(const void* p, int64_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
+
+}  // namespace diffopt

@@ -1,0 +1,424 @@
+// RMS norms of queries and keys for each head with the position rotation in
+// the same pass, on gfx950: forward, VJP, and the VJP's own VJP (formulas in
+// diffopt.h).
+//
+// Every direction reads its operands once and writes its results once, so all
+// are bound by memory.  One wave per head vector: a lane holds pairs of
+// elements that the rotation turns together (pair p of the rotated part, or
+// two neighbours beyond it with the rotation by zero), so nothing crosses
+// lanes but the sums over the head.  Gradients of the weights gather in
+// registers over the heads a wave walks, then over the workgroup in LDS, then
+// over workgroups in a second small launch: a fixed order, no atomics.
+#include "lm_common.hpp"
+
+namespace diffopt {
+namespace {
+
+constexpr int kQB = 256;        // threads per workgroup
+constexpr int kQWaves = kQB / 64;
+constexpr int kMaxBlocks = 2048;  // workgroups per launch (they walk the heads)
+
+struct HeadArr {
+  void* p;
+  int64_t sb, st, sh;
+};
+
+struct QkShape {
+  int64_t B, T;
+  int32_t H, Hk, D, rot, interleaved;
+  float inv_d, eps;
+  const float *cos, *sin;
+  int64_t rows, first;
+  const void* positions;
+  int32_t position_bytes;
+};
+
+// What a direction reads and writes for q (0) and k (1).
+struct QkArgs {
+  HeadArr x[2], dy[2], a[2], o0[2], o1[2];
+  const float *w[2], *b[2];
+  float* dw[2];     // results: the weights' gradients (NULL: not wanted)
+  float* partial;   // [workgroup][D] of either side, q's workgroups first
+};
+
+enum Dir { kFwd, kBwd, kSecond };
+
+template <class E>
+__device__ __forceinline__ const E* row_of(const HeadArr& h, int64_t b, int64_t t, int64_t head) {
+  return static_cast<const E*>(h.p) + b * h.sb + t * h.st + head * h.sh;
+}
+
+__device__ __forceinline__ int64_t position_of(const QkShape& s, int64_t b, int64_t t) {
+  if (!s.positions) return s.first + t;
+  const int64_t at = b * s.T + t;
+  return s.position_bytes == 4 ? (int64_t) static_cast<const int32_t*>(s.positions)[at]
+                               : static_cast<const int64_t*>(s.positions)[at];
+}
+
+// NP pairs per lane: heads of up to 128 NP elements.
+template <class E, int DIR, int NP>
+__global__ __launch_bounds__(kQB) void qknorm_kernel(QkShape s, QkArgs A, int32_t q_blocks) {
+  const int side = (int)blockIdx.x >= q_blocks;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int heads = side ? s.Hk : s.H;
+  const int64_t nrow = s.B * s.T * heads;
+  const int64_t blk = (int64_t)blockIdx.x - (side ? q_blocks : 0), nblk = side ? (int64_t)gridDim.x - q_blocks : q_blocks;
+  const HeadArr X = A.x[side], DY = A.dy[side], AA = A.a[side], O0 = A.o0[side], O1 = A.o1[side];
+  const int half = s.rot >> 1, pairs = (s.D + 1) >> 1;
+
+  // where the pairs lie, and what does not change from head to head
+  int e0[NP], e1[NP];
+  float w0[NP], w1[NP], b0[NP], b1[NP], g0[NP], g1[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int p = lane + 64 * i;
+    int u = -1, v = -1;
+    if (p < half) {
+      u = s.interleaved ? 2 * p : p;
+      v = s.interleaved ? 2 * p + 1 : p + half;
+    } else if (p < pairs) {
+      u = 2 * p;
+      v = 2 * p + 1 < s.D ? 2 * p + 1 : -1;
+    }
+    e0[i] = u;
+    e1[i] = v;
+    const float* w = A.w[side];
+    w0[i] = u >= 0 ? (w ? w[u] : 1.0f) : 0.0f;
+    w1[i] = v >= 0 ? (w ? w[v] : 1.0f) : 0.0f;
+    const float* b = DIR == kSecond ? A.b[side] : nullptr;
+    b0[i] = b && u >= 0 ? b[u] : 0.0f;
+    b1[i] = b && v >= 0 ? b[v] : 0.0f;
+    g0[i] = g1[i] = 0.0f;
+  }
+
+  for (int64_t r = blk * kQWaves + wave; r < nrow; r += nblk * kQWaves) {
+    const int64_t h = r % heads, bt = r / heads, b = bt / s.T, t = bt - b * s.T;
+    const int64_t pos = position_of(s, b, t);
+    const bool known = s.rot == 0 || (pos >= 0 && pos < s.rows);
+    const E* x = row_of<E>(X, b, t, h);
+    float x0[NP], x1[NP], c[NP], sn[NP];
+    float ss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int p = lane + 64 * i;
+      x0[i] = e0[i] >= 0 ? (float)x[e0[i]] : 0.0f;
+      x1[i] = e1[i] >= 0 ? (float)x[e1[i]] : 0.0f;
+      ss += x0[i] * x0[i] + x1[i] * x1[i];
+      c[i] = 1.0f;
+      sn[i] = 0.0f;
+      if (p < half) {
+        c[i] = known ? s.cos[pos * half + p] : kNan;
+        sn[i] = known ? s.sin[pos * half + p] : kNan;
+      } else if (!known) {
+        c[i] = sn[i] = kNan;
+      }
+    }
+    const float rr = rsqrtf(wave_sum(ss) * s.inv_d + s.eps);
+    if (DIR == kFwd) {
+      E* y = const_cast<E*>(row_of<E>(O0, b, t, h));
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const float z0 = w0[i] * (x0[i] * rr), z1 = w1[i] * (x1[i] * rr);
+        if (e0[i] >= 0) y[e0[i]] = (E)(z0 * c[i] - z1 * sn[i]);
+        if (e1[i] >= 0) y[e1[i]] = (E)(z1 * c[i] + z0 * sn[i]);
+      }
+      continue;
+    }
+    // xn = x r, dz the cotangent rotated back, u = w dz
+    const E* dy = row_of<E>(DY, b, t, h);
+    float z0[NP], z1[NP], xu = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      x0[i] *= rr;
+      x1[i] *= rr;
+      const float y0 = e0[i] >= 0 ? (float)dy[e0[i]] : 0.0f, y1 = e1[i] >= 0 ? (float)dy[e1[i]] : 0.0f;
+      z0[i] = y0 * c[i] + y1 * sn[i];
+      z1[i] = y1 * c[i] - y0 * sn[i];
+      xu += x0[i] * w0[i] * z0[i] + x1[i] * w1[i] * z1[i];
+    }
+    xu = wave_sum(xu) * s.inv_d;
+    if (DIR == kBwd) {
+      E* dx = const_cast<E*>(row_of<E>(O0, b, t, h));
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        if (e0[i] >= 0) dx[e0[i]] = (E)(rr * (w0[i] * z0[i] - x0[i] * xu));
+        if (e1[i] >= 0) dx[e1[i]] = (E)(rr * (w1[i] * z1[i] - x1[i] * xu));
+        g0[i] += z0[i] * x0[i];
+        g1[i] += z1[i] * x1[i];
+      }
+      continue;
+    }
+    const E* ap = row_of<E>(AA, b, t, h);
+    float a0[NP], a1[NP], xa = 0.0f, au = 0.0f, bz = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      a0[i] = AA.p && e0[i] >= 0 ? (float)ap[e0[i]] : 0.0f;
+      a1[i] = AA.p && e1[i] >= 0 ? (float)ap[e1[i]] : 0.0f;
+      xa += x0[i] * a0[i] + x1[i] * a1[i];
+      au += a0[i] * w0[i] * z0[i] + a1[i] * w1[i] * z1[i];
+      bz += b0[i] * x0[i] * z0[i] + b1[i] * x1[i] * z1[i];
+    }
+    xa = wave_sum(xa) * s.inv_d;
+    au = wave_sum(au) * s.inv_d;
+    bz = wave_sum(bz) * s.inv_d;
+    E* oy = const_cast<E*>(row_of<E>(O0, b, t, h));
+    E* ox = const_cast<E*>(row_of<E>(O1, b, t, h));
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const float t0 = rr * (a0[i] - x0[i] * xa), t1 = rr * (a1[i] - x1[i] * xa);  // derivative of x r along a
+      const float v0 = w0[i] * t0 + b0[i] * x0[i], v1 = w1[i] * t1 + b1[i] * x1[i];
+      const float u0 = w0[i] * z0[i], u1 = w1[i] * z1[i];
+      const float q0 = rr * (x0[i] * (3.0f * xu * xa - au) - u0 * xa - a0[i] * xu) + b0[i] * z0[i] - x0[i] * bz;
+      const float q1 = rr * (x1[i] * (3.0f * xu * xa - au) - u1 * xa - a1[i] * xu) + b1[i] * z1[i] - x1[i] * bz;
+      if (e0[i] >= 0) {
+        oy[e0[i]] = (E)(v0 * c[i] - v1 * sn[i]);
+        ox[e0[i]] = (E)(rr * q0);
+      }
+      if (e1[i] >= 0) {
+        oy[e1[i]] = (E)(v1 * c[i] + v0 * sn[i]);
+        ox[e1[i]] = (E)(rr * q1);
+      }
+      g0[i] += z0[i] * t0;
+      g1[i] += z1[i] * t1;
+    }
+  }
+  if (DIR == kFwd || !A.dw[side]) return;
+  __shared__ float sum[kQWaves][128 * NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    if (e0[i] >= 0) sum[wave][e0[i]] = g0[i];
+    if (e1[i] >= 0) sum[wave][e1[i]] = g1[i];
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < s.D; d += kQB) {
+    float v = sum[0][d];
+    for (int w = 1; w < kQWaves; ++w) v += sum[w][d];
+    A.partial[(int64_t)blockIdx.x * s.D + d] = v;
+  }
+}
+
+// dw[d] = the sum of the workgroups' parts: one workgroup per 16 elements of a side.
+constexpr int kRB = 256, kRCols = 16, kRRows = kRB / kRCols;
+__global__ __launch_bounds__(kRB) void qknorm_weights(const float* partial, int32_t q_blocks, int32_t k_blocks, int32_t D,
+                                                      float* dwq, float* dwk) {
+  __shared__ float sum[kRRows][kRCols + 1];
+  const int side = blockIdx.y, col = threadIdx.x % kRCols, row = threadIdx.x / kRCols;
+  float* dw = side ? dwk : dwq;
+  if (!dw) return;
+  const int d = blockIdx.x * kRCols + col, n = side ? k_blocks : q_blocks;
+  const float* p = partial + (side ? (int64_t)q_blocks * D : 0);
+  float v = 0.0f;
+  if (d < D)
+    for (int i = row; i < n; i += kRRows) v += p[(int64_t)i * D + d];
+  sum[row][col] = v;
+  __syncthreads();
+  if (row == 0 && d < D) {
+    for (int i = 1; i < kRRows; ++i) v += sum[i][col];
+    dw[d] = v;
+  }
+}
+
+// ---- host -------------------------------------------------------------------
+
+struct Blocks {
+  int32_t q, k;
+};
+
+// Workgroups for each side: a wave per head vector up to kMaxBlocks in all.
+Blocks blocks_of(int64_t B, int64_t T, int64_t H, int64_t Hk) {
+  const double nq = (double)B * T * H, nk = (double)B * T * Hk;
+  auto side = [&](double n) -> int32_t {
+    if (n == 0) return 0;
+    double b = std::ceil(n / kQWaves);
+    const double most = std::floor(kMaxBlocks * (n / (nq + nk)));
+    if (b > most) b = most;
+    return b < 1 ? 1 : (int32_t)b;
+  };
+  return Blocks{side(nq), side(nk)};
+}
+
+int check_heads(const char* who, const char* what, const diffopt_heads* h, int32_t dtype, HeadArr* out) {
+  if (!h || !h->data) return fail(DIFFOPT_EINVAL, "%s: null %s", who, what);
+  if (!aligned_to(h->data, elem_size(dtype))) return fail(DIFFOPT_EINVAL, "%s: %s is not aligned to its elements", who, what);
+  *out = HeadArr{h->data, h->stride_b, h->stride_t, h->stride_h};
+  return DIFFOPT_OK;
+}
+
+bool sizes_ok(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t D) {
+  return B >= 0 && T >= 0 && H >= 0 && Hk >= 0 && D >= 1 && D <= 1024 && H <= 65536 && Hk <= 65536;
+}
+
+int check_shape(const char* who, const float* cos, const float* sin, int64_t rows, const void* positions,
+                int32_t position_bytes, int64_t first, int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t D,
+                int64_t rot, int32_t interleaved, int32_t dtype, double eps, QkShape* s) {
+  if (!sizes_ok(B, T, H, Hk, D)) return fail(DIFFOPT_EINVAL, "%s: sizes must be >= 0, heads <= 65536, D in [1, 1024]", who);
+  if (rot < 0 || rot > D || (rot & 1)) return fail(DIFFOPT_EINVAL, "%s: rot must be even and in [0, D]", who);
+  if (!dtype_ok(dtype)) return fail(DIFFOPT_EINVAL, "%s: unknown element type %d", who, (int)dtype);
+  if (!(std::isfinite(eps) && eps >= 0.0)) return fail(DIFFOPT_EINVAL, "%s: eps must be finite and >= 0", who);
+  if (rot > 0 && (!cos || !sin)) return fail(DIFFOPT_EINVAL, "%s: null cos or sin", who);
+  if (rot > 0 && rows < 0) return fail(DIFFOPT_EINVAL, "%s: rows must be >= 0", who);
+  if (positions && position_bytes != 4 && position_bytes != 8)
+    return fail(DIFFOPT_EINVAL, "%s: position_bytes must be 4 or 8", who);
+  if (positions && !aligned_to(positions, position_bytes))
+    return fail(DIFFOPT_EINVAL, "%s: positions is not aligned to its elements", who);
+  if (!aligned_to(cos, 4) || !aligned_to(sin, 4)) return fail(DIFFOPT_EINVAL, "%s: cos or sin is not 4-byte aligned", who);
+  if (!positions && rot > 0 && (first < 0 || T > rows || first > rows - T))
+    return fail(DIFFOPT_EINVAL, "%s: positions %lld to %lld are outside the %lld rows of cos and sin", who, (long long)first,
+                (long long)(first + T - 1), (long long)rows);
+  *s = QkShape{B, T, (int32_t)H, (int32_t)Hk, (int32_t)D, (int32_t)rot, interleaved, (float)(1.0 / (double)D), (float)eps,
+               cos, sin, rows, first, positions, position_bytes};
+  return DIFFOPT_OK;
+}
+
+template <class E, int DIR>
+void launch_pairs(const QkShape& s, const QkArgs& A, Blocks n, hipStream_t st) {
+  const dim3 grid((unsigned)(n.q + n.k)), block(kQB);
+  if (s.D <= 128)
+    hipLaunchKernelGGL((qknorm_kernel<E, DIR, 1>), grid, block, 0, st, s, A, n.q);
+  else if (s.D <= 256)
+    hipLaunchKernelGGL((qknorm_kernel<E, DIR, 2>), grid, block, 0, st, s, A, n.q);
+  else
+    hipLaunchKernelGGL((qknorm_kernel<E, DIR, 8>), grid, block, 0, st, s, A, n.q);
+}
+
+template <int DIR>
+int launch(const char* who, const QkShape& s, const QkArgs& A, int32_t dtype, hipStream_t st) {
+  const Blocks n = blocks_of(s.B, s.T, s.H, s.Hk);
+  if (n.q + n.k > 0) {
+    if (dtype == DIFFOPT_F32)
+      launch_pairs<float, DIR>(s, A, n, st);
+    else
+      launch_pairs<bf16, DIR>(s, A, n, st);
+    const int rc = launch_status(who);
+    if (rc) return rc;
+  }
+  if (DIR != kFwd && (A.dw[0] || A.dw[1])) {
+    hipLaunchKernelGGL(qknorm_weights, dim3((unsigned)((s.D + kRCols - 1) / kRCols), 2), dim3(kRB), 0, st, A.partial, n.q, n.k,
+                       s.D, A.dw[0], A.dw[1]);
+    return launch_status(who);
+  }
+  return DIFFOPT_OK;
+}
+
+int check_workspace(const char* who, const QkShape& s, QkArgs* A, void* workspace, int64_t bytes) {
+  if (!A->dw[0] && !A->dw[1]) return DIFFOPT_OK;
+  const Blocks n = blocks_of(s.B, s.T, s.H, s.Hk);
+  const int64_t need = (int64_t)(n.q + n.k) * s.D * 4;
+  if (need > 0 && (!workspace || bytes < need))
+    return fail(DIFFOPT_EINVAL, "%s: the workspace has %lld bytes of %lld", who, (long long)(workspace ? bytes : 0), (long long)need);
+  if (!aligned_to(workspace, 4)) return fail(DIFFOPT_EINVAL, "%s: the workspace is not 4-byte aligned", who);
+  A->partial = static_cast<float*>(workspace);
+  return DIFFOPT_OK;
+}
+
+// Operands of q and, where there are k heads, of k.
+int check_both(const char* who, const char* what, const diffopt_heads* q, const diffopt_heads* k, const QkShape& s, int32_t dtype,
+               HeadArr out[2]) {
+  int rc = DIFFOPT_OK;
+  if (s.H > 0) rc = check_heads(who, what, q, dtype, &out[0]);
+  if (!rc && s.Hk > 0) rc = check_heads(who, what, k, dtype, &out[1]);
+  return rc;
+}
+
+int check_floats(const char* who, const float* const* p, int n) {
+  for (int i = 0; i < n; ++i)
+    if (!aligned_to(p[i], 4)) return fail(DIFFOPT_EINVAL, "%s: pointer %p is not 4-byte aligned", who, (const void*)p[i]);
+  return DIFFOPT_OK;
+}
+
+}  // namespace
+}  // namespace diffopt
+
+using namespace diffopt;
+
+extern "C" int64_t diffopt_qknorm_rope_workspace(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t D) {
+  if (!sizes_ok(B, T, H, Hk, D)) return -1;
+  const Blocks n = blocks_of(B, T, H, Hk);
+  return (int64_t)(n.q + n.k) * D * 4;
+}
+
+extern "C" int diffopt_qknorm_rope_fwd(const diffopt_heads* q, const diffopt_heads* k, const float* q_weight,
+                                       const float* k_weight, const float* cos, const float* sin, int64_t rows,
+                                       const void* positions, int32_t position_bytes, int64_t first, int64_t B,
+                                       int64_t T, int64_t H, int64_t Hk, int64_t D, int64_t rot, int32_t interleaved,
+                                       int32_t dtype, double eps, const diffopt_heads* q_out,
+                                       const diffopt_heads* k_out, void* stream) {
+  clear_error();
+  static const char* who = "diffopt_qknorm_rope_fwd";
+  QkShape s;
+  int rc = check_shape(who, cos, sin, rows, positions, position_bytes, first, B, T, H, Hk, D, rot, interleaved, dtype, eps, &s);
+  if (rc || B == 0 || T == 0) return rc;
+  QkArgs A{};
+  rc = check_both(who, "q or k", q, k, s, dtype, A.x);
+  if (!rc) rc = check_both(who, "q_out or k_out", q_out, k_out, s, dtype, A.o0);
+  const float* f[] = {q_weight, k_weight};
+  if (!rc) rc = check_floats(who, f, 2);
+  if (rc) return rc;
+  A.w[0] = q_weight;
+  A.w[1] = k_weight;
+  return launch<kFwd>(who, s, A, dtype, as_stream(stream));
+}
+
+extern "C" int diffopt_qknorm_rope_bwd(const diffopt_heads* dq_out, const diffopt_heads* dk_out, const diffopt_heads* q,
+                                       const diffopt_heads* k, const float* q_weight, const float* k_weight,
+                                       const float* cos, const float* sin, int64_t rows, const void* positions,
+                                       int32_t position_bytes, int64_t first, int64_t B, int64_t T, int64_t H,
+                                       int64_t Hk, int64_t D, int64_t rot, int32_t interleaved, int32_t dtype,
+                                       double eps, const diffopt_heads* dq, const diffopt_heads* dk, float* dq_weight,
+                                       float* dk_weight, void* workspace, int64_t workspace_bytes, void* stream) {
+  clear_error();
+  static const char* who = "diffopt_qknorm_rope_bwd";
+  QkShape s;
+  int rc = check_shape(who, cos, sin, rows, positions, position_bytes, first, B, T, H, Hk, D, rot, interleaved, dtype, eps, &s);
+  if (rc) return rc;
+  QkArgs A{};
+  A.dw[0] = dq_weight;
+  A.dw[1] = dk_weight;
+  if (B * T > 0) {
+    rc = check_both(who, "q or k", q, k, s, dtype, A.x);
+    if (!rc) rc = check_both(who, "dq_out or dk_out", dq_out, dk_out, s, dtype, A.dy);
+    if (!rc) rc = check_both(who, "dq or dk", dq, dk, s, dtype, A.o0);
+  }
+  const float* f[] = {q_weight, k_weight, dq_weight, dk_weight};
+  if (!rc) rc = check_floats(who, f, 4);
+  if (!rc) rc = check_workspace(who, s, &A, workspace, workspace_bytes);
+  if (rc) return rc;
+  A.w[0] = q_weight;
+  A.w[1] = k_weight;
+  return launch<kBwd>(who, s, A, dtype, as_stream(stream));
+}
+
+extern "C" int diffopt_qknorm_rope_bwd_bwd(
+    const diffopt_heads* ddq, const diffopt_heads* ddk, const float* ddq_weight, const float* ddk_weight,
+    const diffopt_heads* dq_out, const diffopt_heads* dk_out, const diffopt_heads* q, const diffopt_heads* k,
+    const float* q_weight, const float* k_weight, const float* cos, const float* sin, int64_t rows,
+    const void* positions, int32_t position_bytes, int64_t first, int64_t B, int64_t T, int64_t H, int64_t Hk,
+    int64_t D, int64_t rot, int32_t interleaved, int32_t dtype, double eps, const diffopt_heads* out_dq_out,
+    const diffopt_heads* out_dk_out, const diffopt_heads* out_q, const diffopt_heads* out_k, float* out_q_weight,
+    float* out_k_weight, void* workspace, int64_t workspace_bytes, void* stream) {
+  clear_error();
+  static const char* who = "diffopt_qknorm_rope_bwd_bwd";
+  QkShape s;
+  int rc = check_shape(who, cos, sin, rows, positions, position_bytes, first, B, T, H, Hk, D, rot, interleaved, dtype, eps, &s);
+  if (rc) return rc;
+  QkArgs A{};
+  A.dw[0] = out_q_weight;
+  A.dw[1] = out_k_weight;
+  if (B * T > 0) {
+    rc = check_both(who, "q or k", q, k, s, dtype, A.x);
+    if (!rc) rc = check_both(who, "dq_out or dk_out", dq_out, dk_out, s, dtype, A.dy);
+    if (!rc && ddq) rc = check_heads(who, "ddq", ddq, dtype, &A.a[0]);
+    if (!rc && ddk && Hk > 0) rc = check_heads(who, "ddk", ddk, dtype, &A.a[1]);
+    if (!rc) rc = check_both(who, "out_dq_out or out_dk_out", out_dq_out, out_dk_out, s, dtype, A.o0);
+    if (!rc) rc = check_both(who, "out_q or out_k", out_q, out_k, s, dtype, A.o1);
+  }
+  const float* f[] = {q_weight, k_weight, ddq_weight, ddk_weight, out_q_weight, out_k_weight};
+  if (!rc) rc = check_floats(who, f, 6);
+  if (!rc) rc = check_workspace(who, s, &A, workspace, workspace_bytes);
+  if (rc) return rc;
+  A.w[0] = q_weight;
+  A.w[1] = k_weight;
+  A.b[0] = ddq_weight;
+  A.b[1] = ddk_weight;
+  return launch<kSecond>(who, s, A, dtype, as_stream(stream));
+}
