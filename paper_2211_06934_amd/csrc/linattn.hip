@@ -21,10 +21,9 @@ struct HeadArr {
 // heads j nk .. + nk (one of nq, nk is 1).
 struct Scan {
   HeadArr q, k, v, o;
-  const float* s0;  // initial state or NULL; element (r, c) at r s_r + c s_c of its [Dk][Dv] block
-  float* s1;        // final state or NULL, laid out alike
-  int64_t s_r, s_c;
-  int32_t nq, nk, Dk, Dv;
+  const float* s0;  // initial state or NULL: [Dk][Dv] blocks, or [Dv][Dk] ones with flip
+  float* s1;        // final state or NULL: [Dk][Dv] blocks
+  int32_t flip, nq, nk, Dk, Dv;
   int32_t back;     // tokens run from the last to the first; the state meets a token undecayed
   float qs, ks;     // scale of the outputs, of the update
 };
@@ -68,7 +67,7 @@ __global__ __launch_bounds__(kTokenB) void linattn_tokens(Shape s, Scan a, int32
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const int r = rg + 16 * i;
-      S[i][c] = a.s0 && r < a.Dk && c0 + c < a.Dv ? a.s0[block + r * a.s_r + (c0 + c) * a.s_c] : 0.0f;
+      S[i][c] = a.s0 && r < a.Dk && c0 + c < a.Dv ? a.s0[block + (a.flip ? (c0 + c) * a.Dk + r : r * a.Dv + c0 + c)] : 0.0f;
     }
   for (int64_t n = 0; n < L; ++n) {
     const int64_t t = a.back ? L - 1 - n : n;
@@ -126,9 +125,529 @@ __global__ __launch_bounds__(kTokenB) void linattn_tokens(Shape s, Scan a, int32
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         const int r = rg + 16 * i;
-        if (r < a.Dk && c0 + c < a.Dv) a.s1[block + r * a.s_r + (c0 + c) * a.s_c] = S[i][c] * last;
+        if (r < a.Dk && c0 + c < a.Dv) a.s1[block + r * a.Dv + c0 + c] = S[i][c] * last;
       }
   }
+}
+
+// ---- chunks -----------------------------------------------------------------
+// C tokens at a time, all as matrix products.  With t, s counted inside a chunk
+// of L <= C tokens and S the state before it,
+//   O = W_q (Q S) + (P o M) V,  P = Q K^T,  M_ts = g^(t-s) for s <= t
+//   S = g^L S + K^T (W_k V)
+// where W_q, W_k are diagonal: g^(t+1), g^(L-1-s) forward and g^t, g^(L-s) back
+// in time (no power is ever negative).  A workgroup of four waves walks the
+// chunks of one segment of a sequence; wave w owns 16 NCT columns of the state,
+// all DK rows of them, in registers for the whole walk.
+//
+// Fragments: v_mfma 16x16 takes row (or column) lane % 16 and, of a block of 32
+// along the contraction, 8 elements per 16-lane group g = lane / 16; it returns
+// column lane % 16, rows 4 g .. + 4.  The rows of two state tiles are numbered
+// so that a lane's eight results are elements 32 b + 8 g .. + 8 of the key axis:
+// the state is an operand of Q S as it lies in the registers, Q and K are read
+// in 16-byte pieces.  Tokens are numbered 32 b + 4 g .. + 4 and + 16: P^T as it
+// is computed is an operand of P V, and V and K^T come out of LDS transposed
+// four tokens at a time (ds_read_b64_tr_b16).  The products are computed
+// transposed, so that a lane stores 4 NCT neighbouring elements of one token.
+//
+// In bf16 the scores and the state are rounded where they enter a product (the
+// outputs are bf16 too); the state itself is fp32 and its update takes W_k V in
+// SPLIT bf16 parts, exact to 2^-8 SPLIT: two where only outputs follow, three
+// where a state is handed out.  fp32 runs on the fp32 matrix instructions.
+
+template <class E>
+struct Frag;
+template <>
+struct Frag<bf16> {
+  typedef bf16x8 type;
+};
+template <>
+struct Frag<float> {
+  typedef float type __attribute__((ext_vector_type(8)));
+};
+
+__device__ __forceinline__ f32x4 mfma32(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma32(Frag<float>::type a, Frag<float>::type b, f32x4 c) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+  return c;
+}
+
+// A matrix of rows of W elements in LDS.  A row takes three 16-byte pieces more
+// than its elements, so that 16 rows at one piece fall on different banks and 8
+// rows of 4 pieces, half of each read, on the banks two or three times (two is
+// the least), and every access lies a constant from one address per lane.
+template <class E, int W>
+struct Tile {
+  static constexpr int VN = 16 / (int)sizeof(E);
+  static constexpr int ROW = W + 3 * VN;  // elements from row to row
+  typedef typename Frag<E>::type frag;
+
+  // a lane's part of the address of row(): row lane % 16, elements 8 g
+  static __device__ __forceinline__ int row_lane(int lane) { return (lane & 15) * ROW + 8 * (lane >> 4); }
+  // elements col .. + 8 (from 8 g on) of row r (from lane % 16 on)
+  static __device__ __forceinline__ frag row(const E* base, int lane_part, int r, int col) {
+    const E* p = base + lane_part + (r * ROW + col);
+    if constexpr (sizeof(E) == 2) {
+      return *reinterpret_cast<const frag*>(p);
+    } else {
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
+      return frag{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    }
+  }
+
+  // a lane's part of the address of column()
+  template <int STEP>
+  static __device__ __forceinline__ int column_lane(int lane) {
+    const int g = lane >> 4, m = lane & 15;
+    return sizeof(E) == 2 ? (4 * g + (m >> 2)) * ROW + STEP * (m & 3) : 4 * g * ROW + STEP * (m >> 2) + (m & 3);
+  }
+  // element col + (m / 4) STEP + m % 4, m = lane % 16, of rows 32 b + 4 g .. + 4 and 16 further
+  static __device__ __forceinline__ frag column(const E* base, int lane_part, int b, int col) {
+    const E* p = base + lane_part + (32 * b * ROW + col);
+    if constexpr (sizeof(E) == 2) {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef short s16x8 __attribute__((ext_vector_type(8)));
+      typedef __attribute__((address_space(3))) s16x4 lds4;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + 16 * ROW));
+      return __builtin_bit_cast(frag, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      frag f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = p[((j >> 2) * 16 + (j & 3)) * ROW];
+      return f;
+    }
+  }
+};
+
+__device__ __forceinline__ bf16x8 pack(f32x4 a, f32x4 b, bf16) {
+  return bf16x8{(bf16)a[0], (bf16)a[1], (bf16)a[2], (bf16)a[3], (bf16)b[0], (bf16)b[1], (bf16)b[2], (bf16)b[3]};
+}
+__device__ __forceinline__ Frag<float>::type pack(f32x4 a, f32x4 b, float) {
+  return Frag<float>::type{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+
+// g^n for n >= 0; lg2 = log2 g may be -inf (g = 0, g^0 = 1).
+__device__ __forceinline__ float power(float lg2, int n) { return n == 0 ? 1.0f : __builtin_amdgcn_exp2f((float)n * lg2); }
+
+// What a launch runs: up to three scans of one shape, each cut into segments of
+// whole chunks; seg[i] holds the segments' states ([state][segment][Dk][Dv]).
+struct Jobs {
+  Scan scan[3];
+  float* seg[3];
+  int32_t nseg, seg_chunks;
+};
+
+template <class E>
+struct ChunkOf {
+  static constexpr int C = sizeof(E) == 2 ? 64 : 32;
+};
+
+constexpr int kChunkB = 256;
+
+// A thread's 16-byte pieces of one staged matrix: C rows (tokens) of W elements.
+template <class E, int W, int C>
+struct Stage {
+  static constexpr int VN = 16 / (int)sizeof(E), NP = W / VN, N = C * NP / kChunkB, STEP = kChunkB / NP;
+  typename Vec<E>::type v[N];
+
+  // rows 0 .. L - 1 from `head`, st elements apart (negative: back in time),
+  // columns from col0 on; WHOLE: W of them are there, else those below `width`
+  template <bool WHOLE>
+  __device__ __forceinline__ void load(const E* head, int64_t st, int L, int col0, int width) {
+    const int r0 = threadIdx.x / NP, c = col0 + threadIdx.x % NP * VN;
+    const E* p = head + r0 * st + c;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      typename Vec<E>::type x{};
+      if (r0 + i * STEP < L) {
+        if (WHOLE) {
+          x = load_vec(p);
+        } else {
+#pragma unroll
+          for (int e = 0; e < VN; ++e) {
+            const E y = p[c + e < width ? e : -c];  // the row's first element where there is none
+            x[e] = c + e < width ? y : (E)0.0f;
+          }
+        }
+      }
+      v[i] = x;
+      p += STEP * st;
+    }
+  }
+  __device__ __forceinline__ void put(E* lds) const {
+    typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
+    E* p = lds + threadIdx.x / NP * Tile<E, W>::ROW + threadIdx.x % NP * VN;
+#pragma unroll
+    for (int i = 0; i < N; ++i) *reinterpret_cast<whole*>(p + i * STEP * Tile<E, W>::ROW) = v[i];
+  }
+};
+
+template <class E, int DK, int NCT>
+struct ChunkLds {
+  static constexpr int C = ChunkOf<E>::C;
+  static constexpr int bytes = C * (2 * Tile<E, DK>::ROW + Tile<E, 64 * NCT>::ROW) * (int)sizeof(E) + C * C * (int)sizeof(E);
+};
+
+template <class E, int DK, int NCT, int SPLIT, bool OUT, bool WHOLE>
+__global__ __launch_bounds__(kChunkB, (ChunkLds<E, DK, NCT>::bytes > 80 * 1024 ? 1 : 2)) void linattn_chunks(Shape sh, Jobs jobs,
+                                                                                                     int32_t col_tiles) {
+  constexpr int C = ChunkOf<E>::C, NT = C / 16, NB = C / 32, KB = DK / 32, CT = 64 * NCT;
+  typedef typename Frag<E>::type frag;
+  typedef Tile<E, DK> KTile;
+  typedef Tile<E, CT> VTile;
+  __shared__ __attribute__((aligned(16))) E sQ[OUT ? C * KTile::ROW : 16];
+  __shared__ __attribute__((aligned(16))) E sK[C * KTile::ROW];
+  __shared__ __attribute__((aligned(16))) E sV[C * VTile::ROW];
+  __shared__ __attribute__((aligned(16))) frag sP[OUT ? NT * NB * 64 : 1];
+
+  const Scan a = jobs.scan[blockIdx.y];
+  const int nq = OUT ? a.nq : 1;
+  int64_t x = blockIdx.x;
+  const int ct0 = (int)(x % col_tiles) * CT;
+  x /= col_tiles;
+  const int seg = (int)(x % jobs.nseg);
+  x /= jobs.nseg;
+  const int qh = (int)(x % nq);
+  const int64_t state = x / nq, b = state / sh.Hs;
+  if (b >= sh.B) return;  // the launch's scans differ in heads
+  const int j = (int)(state - b * sh.Hs);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, m = lane & 15;
+  const int at_row = KTile::row_lane(lane), at_k = KTile::template column_lane<8>(lane), at_v = VTile::template column_lane<4 * NCT>(lane);
+  const int64_t len = length_of(sh, b);
+  const double lgd = (double)sh.log_decay[j];
+  const float lg2 = (float)(lgd * 1.4426950408889634074);
+  const int back = a.back;
+  const int64_t first = (int64_t)seg * jobs.seg_chunks;
+  int64_t last = first + jobs.seg_chunks;
+  const int64_t chunks = (sh.T + C - 1) / C;
+  if (last > chunks) last = chunks;
+  const int64_t live = (len + C - 1) / C;  // chunks with tokens
+  const int64_t end = last < live ? last : live;
+
+  // the state: tile (kb, u), column tile ct; a lane holds column wave 16 NCT +
+  // (m/4) 4 NCT + 4 ct + m%4 of the tile, rows 32 kb + 8 g + 4 u + i
+  const int row0 = 8 * g, col0 = ct0 + 16 * NCT * wave + 4 * NCT * (m >> 2) + (m & 3);
+  const bool cut = jobs.nseg > 1;
+  float* segments = cut ? jobs.seg[blockIdx.y] + (state * jobs.nseg + seg) * a.Dk * a.Dv : nullptr;
+  f32x4 S[KB][2][NCT];
+  {
+    const float* s0 = !OUT ? nullptr : cut ? segments : a.s0 ? a.s0 + state * a.Dk * a.Dv : nullptr;
+    const bool flip = !cut && a.flip;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = row0 + 32 * kb + 4 * u + i, c = col0 + 4 * ct;
+            const bool in = s0 && (WHOLE || (r < a.Dk && c < a.Dv));
+            S[kb][u][ct][i] = in ? s0[flip ? c * a.Dk + r : r * a.Dv + c] : 0.0f;
+          }
+  }
+
+  // g^C rounds once; what that leaves out grows with every chunk and is made
+  // good each eighth one
+  const double gcd = exp(lgd * C);
+  const float gc = (float)gcd;
+  const double gc8 = gc > 0.0f ? gcd * exp(7.0 * log(gcd / (double)gc)) : 0.0;
+  const float g8_hi = (float)gc8, g8_lo = (float)(gc8 - (double)g8_hi);
+  const float gl = (float)exp(lgd * (double)(len % C));  // the last chunk's, where it is not whole
+
+  // weights of whole chunks: scores of a diagonal tile and of the tile before
+  // it, outputs of the state, values that enter it
+  const float ps = a.qs * a.ks;
+  float diag[4], beside[4], kw[NB][8], qw[NT];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int gap = m - 4 * g - e;
+    diag[e] = gap >= 0 ? ps * power(lg2, gap) : 0.0f;
+    beside[e] = ps * power(lg2, gap + 16);
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) qw[t] = a.qs * power(lg2, 16 * t + m + 1 - back);
+  auto key_weights = [&](int L) {
+    int g = lane >> 4;
+    asm volatile("" : "+v"(g));  // nothing of it is kept over the walk for the last chunk's weights
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int n = L - 1 + back - (32 * nb + (e >> 2) * 16 + 4 * g + (e & 3));
+        kw[nb][e] = n >= back ? a.ks * power(lg2, n) : 0.0f;
+      }
+  };
+  key_weights(C);
+
+  const int dir = back ? -1 : 1;
+  const E* q0 = OUT ? at<E>(a.q, b, back ? len - 1 : 0, (int64_t)j * a.nq + qh) : nullptr;
+  const E* k0 = at<E>(a.k, b, back ? len - 1 : 0, (int64_t)j * a.nk);
+  const E* v0 = at<E>(a.v, b, back ? len - 1 : 0, (int64_t)j * a.nk);
+  const int64_t qst = dir * a.q.st, kst = dir * a.k.st, vst = dir * a.v.st;
+  Stage<E, DK, C> pq, pk;
+  Stage<E, CT, C> pv;
+  auto valid = [&](int64_t c) { return (int)(len - c * C < C ? len - c * C : C); };
+  // item n of the walk: k/v head n % nk of chunk first + n / nk
+  int h = -1, h_next = 0;
+  int64_t c = first, c_next = first;
+  f32x4 O[NT][NCT];
+  while (true) {
+    if (h >= 0) {
+      __syncthreads();
+      if (OUT && h == 0) pq.put(sQ);
+      pk.put(sK);
+      pv.put(sV);
+      __syncthreads();
+    }
+    if (c_next < end) {
+      const int L = valid(c_next);
+      if (OUT && h_next == 0) pq.template load<WHOLE>(q0 + c_next * C * qst, qst, L, 0, a.Dk);
+      pk.template load<WHOLE>(k0 + c_next * C * kst + h_next * a.k.sh, kst, L, 0, a.Dk);
+      pv.template load<WHOLE>(v0 + c_next * C * vst + h_next * a.v.sh, vst, L, ct0, a.Dv);
+    }
+    if (h >= 0) {
+      const int L = valid(c);
+      if (L < C) key_weights(L);
+      if (OUT) {
+        // P^T of this wave's tiles, masked and decayed, as operands of P V
+        constexpr int PER = NT * NT / 4;  // tiles, of one query tile, that a wave computes
+        const int tq = wave * PER / NT, tk0 = wave * PER % NT;
+        f32x4 P[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          const int apart = tq - tk0 - i;
+          P[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+          if (apart >= 0) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+              P[i] = mfma32(KTile::row(sK + 16 * tk0 * KTile::ROW, at_row, 16 * i, 32 * kb), KTile::row(sQ + 16 * tq * KTile::ROW, at_row, 0, 32 * kb), P[i]);
+            if (apart == 0) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) P[i][e] = m >= 4 * g + e ? P[i][e] * diag[e] : 0.0f;
+            } else {
+              const float w = power(lg2, 16 * (apart - 1));
+#pragma unroll
+              for (int e = 0; e < 4; ++e) P[i][e] *= beside[e] * w;
+            }
+          }
+        }
+        if constexpr (PER >= 2) {
+#pragma unroll
+          for (int kb = 0; kb < PER / 2; ++kb) sP[(tq * NB + kb) * 64 + lane] = pack(P[2 * kb], P[2 * kb + 1], E());
+        } else {  // half a block: four of a lane's eight elements
+          reinterpret_cast<f32x4*>(&sP[(tq * NB) * 64 + lane])[tk0] = P[0];
+        }
+      }
+
+      frag V[NB][NCT];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct) V[nb][ct] = VTile::column(sV + 16 * NCT * wave, at_v, nb, 4 * ct);
+
+      if (OUT) {
+        // zeros times the values: zero unless one is infinite or NaN
+        f32x4 odd{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int ct = 0; ct < NCT; ++ct) {
+            if constexpr (sizeof(E) == 2) {
+              odd = mfma32(V[nb][ct], frag{}, odd);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) odd[e & 3] = fmaf(V[nb][ct][e], 0.0f, odd[e & 3]);
+            }
+          }
+        if (h == 0) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) O[t][ct] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb) {
+            frag s[NCT];
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) s[ct] = pack(S[kb][0][ct], S[kb][1][ct], E());
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+              const frag q = KTile::row(sQ, at_row, 16 * t, 32 * kb);
+#pragma unroll
+              for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(s[ct], q, O[t][ct]);
+            }
+          }
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) O[t][ct] *= qw[t];
+        }
+        __syncthreads();
+        if (__all(odd[0] + odd[1] + odd[2] + odd[3] == 0.0f)) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int nb = 0; nb <= t / 2; ++nb) {
+              const frag p = sP[(t * NB + nb) * 64 + lane];
+#pragma unroll
+              for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(V[nb][ct], p, O[t][ct]);
+            }
+        } else {
+          // a product with the zeros of the mask would carry an infinity or NaN
+          // to earlier tokens, so the sum stops at the token
+#pragma unroll 1
+          for (int s = 0; s < L; ++s) {
+            const E* p = reinterpret_cast<const E*>(&sP[(s >> 5) * 64 + ((s >> 2) & 3) * 16 + m]) + ((s >> 4) & 1) * 4 + (s & 3);
+            const E* v = sV + s * VTile::ROW + 16 * NCT * wave + 4 * NCT * g;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+              if (s <= 16 * t + m) {
+#pragma unroll
+                for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) O[t][ct][i] = fmaf((float)p[t * NB * 64 * 8], (float)v[4 * ct + i], O[t][ct][i]);
+              }
+          }
+        }
+        if (h + 1 == a.nk && a.o.p) {
+          E* o = at<E>(a.o, b, back ? len - 1 : 0, (int64_t)j * a.nq + qh) + c * C * dir * a.o.st;
+          const int col = ct0 + 16 * NCT * wave + 4 * NCT * g;
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            E* p = o + (16 * t + m) * dir * a.o.st + col;
+            if (16 * t + m < L) {
+              if (WHOLE) {
+                typedef E out_vec __attribute__((ext_vector_type(4 * NCT), aligned(alignof(E))));
+                out_vec z;
+#pragma unroll
+                for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) z[4 * ct + i] = (E)O[t][ct][i];
+                *reinterpret_cast<out_vec*>(p) = z;
+              } else {
+#pragma unroll
+                for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+                  for (int i = 0; i < 4; ++i)
+                    if (col + 4 * ct + i < a.Dv) p[4 * ct + i] = (E)O[t][ct][i];
+              }
+            }
+          }
+        }
+      }
+
+      if (h == 0) {
+        if (L == C && ((c - first) & 7) == 7) {
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) S[kb][u][ct][i] = fmaf(S[kb][u][ct][i], g8_hi, S[kb][u][ct][i] * g8_lo);
+        } else {
+          const float d = L < C ? gl : gc;
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int ct = 0; ct < NCT; ++ct) S[kb][u][ct] *= d;
+        }
+      }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        frag part[SPLIT][NCT];
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            float y = (float)V[nb][ct][e] * kw[nb][e];
+#pragma unroll
+            for (int p = 0; p < SPLIT; ++p) {
+              part[p][ct][e] = (E)y;
+              y -= (float)part[p][ct][e];
+            }
+          }
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const frag k = KTile::column(sK, at_k, nb, 32 * kb + 4 * u);
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+              for (int p = 0; p < SPLIT; ++p) S[kb][u][ct] = mfma32(k, part[p][ct], S[kb][u][ct]);
+          }
+      }
+    }
+    if (c_next >= end) break;
+    c = c_next;
+    h = h_next;
+    if (++h_next == a.nk) {
+      h_next = 0;
+      ++c_next;
+    }
+  }
+
+  if (OUT && a.o.p) {  // tokens past the sequence's length
+    E* o = at<E>(a.o, b, 0, (int64_t)j * a.nq + qh);
+    const int64_t from = len > first * C ? len : first * C, to = last * C < sh.T ? last * C : sh.T;
+    for (int64_t t = from + wave; t < to; t += kChunkB / 64)
+      for (int col = ct0 + lane; col < ct0 + CT && col < a.Dv; col += 64) o[t * a.o.st + col] = (E)0.0f;
+  }
+  float* s1 = !OUT ? segments : !cut && a.s1 && qh == 0 ? a.s1 + state * a.Dk * a.Dv : nullptr;
+  if (s1) {
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));  // addresses anew: those of the initial state are not kept over the walk
+    const int r0 = 8 * ((tid & 63) >> 4), c0 = ct0 + 16 * NCT * (tid >> 6) + 4 * NCT * ((tid & 15) >> 2) + (tid & 3);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = r0 + 32 * kb + 4 * u + i, col = c0 + 4 * ct;
+            if (WHOLE || (r < a.Dk && col < a.Dv)) s1[r * a.Dv + col] = S[kb][u][ct][i];
+          }
+  }
+}
+
+// The segments' own states to the states before them, in place, and the last:
+//   before_0 = s0, before_{i+1} = g^(tokens of i) before_i + own_i
+constexpr int kJoinB = 256, kJoinAhead = 8;
+__global__ __launch_bounds__(kJoinB) void linattn_join(Shape sh, Jobs jobs, int32_t chunk) {
+  const Scan& a = jobs.scan[blockIdx.y];
+  const int n = a.Dk * a.Dv, blocks = (n + kJoinB - 1) / kJoinB;
+  const int64_t state = blockIdx.x / blocks, b = state / sh.Hs;
+  const int e = (int)(blockIdx.x % blocks) * kJoinB + threadIdx.x;
+  if (b >= sh.B || e >= n) return;
+  const int64_t len = length_of(sh, b), per = (int64_t)jobs.seg_chunks * chunk;
+  const double lgd = (double)sh.log_decay[state - b * sh.Hs];
+  const float whole = (float)exp(lgd * (double)per);
+  float* buf = jobs.seg[blockIdx.y] + state * jobs.nseg * n + e;
+  float S = a.s0 ? a.s0[state * n + (a.flip ? e % a.Dv * a.Dk + e / a.Dv : e)] : 0.0f;
+  for (int i0 = 0; i0 < jobs.nseg; i0 += kJoinAhead) {
+    float own[kJoinAhead];
+#pragma unroll
+    for (int i = 0; i < kJoinAhead; ++i) own[i] = i0 + i < jobs.nseg - (a.s1 ? 0 : 1) ? buf[(int64_t)(i0 + i) * n] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < kJoinAhead; ++i)
+      if (i0 + i < jobs.nseg) {
+        const int64_t left = len - (i0 + i) * per;
+        buf[(int64_t)(i0 + i) * n] = S;
+        if (left >= per) S = fmaf(S, whole, own[i]);
+        else if (left > 0) S = fmaf(S, (float)exp(lgd * (double)left), own[i]);
+      }
+  }
+  if (a.s1) a.s1[state * n + e] = S;
 }
 
 // ---- host -------------------------------------------------------------------
@@ -147,11 +666,182 @@ void launch_tokens(const Shape& s, const Scan& a, hipStream_t st) {
     hipLaunchKernelGGL((linattn_tokens<E, 16>), grid, block, 0, st, s, a, tiles);
 }
 
-int run_scan(const char* who, const Shape& s, const Scan& a, int32_t dtype, hipStream_t st) {
-  if (dtype == DIFFOPT_F32)
-    launch_tokens<float>(s, a, st);
+// Which chunk kernel a scan takes: key rows, column tiles of a wave.
+struct Class {
+  int dk, nct;
+  bool whole;
+};
+
+Class class_of(const Scan& a) {
+  Class c;
+  c.dk = a.Dk <= 32 ? 32 : a.Dk <= 64 ? 64 : a.Dk <= 128 ? 128 : 256;
+  c.nct = c.dk == 128 ? 2 : 1;
+  c.whole = a.Dk == c.dk && a.Dv % (64 * c.nct) == 0;
+  return c;
+}
+
+// Segments of a call's scans.  A workgroup walks its chunks one after another,
+// so with few heads a sequence is cut until the workgroups fill the card twice
+// over (two share a compute unit); a cut costs one more read of k and v and the
+// segments' states, so there is none from half of that on, and no segment is
+// shorter than kMinChunks.
+constexpr int kFill = 512, kMinChunks = 4;
+
+struct Plan {
+  int32_t nseg, seg_chunks;
+};
+
+Plan plan_of(int64_t workgroups, int64_t T, int chunk) {
+  const int64_t chunks = (T + chunk - 1) / chunk;
+  int64_t n = workgroups > 0 ? kFill / workgroups : 1;
+  if (n > chunks / kMinChunks) n = chunks / kMinChunks;
+  if (n < 1) n = 1;
+  const int64_t per = chunks > 0 ? (chunks + n - 1) / n : 1;
+  return Plan{(int32_t)((chunks + per - 1) / per > 1 ? (chunks + per - 1) / per : 1), (int32_t)per};
+}
+
+int64_t col_tiles(const Scan& a) {
+  const int ct = 64 * class_of(a).nct;
+  return (a.Dv + ct - 1) / ct;
+}
+
+int64_t main_groups(const Shape& s, const Scan& a) { return s.B * s.Hs * a.nq * col_tiles(a); }
+
+int64_t segment_bytes(const Shape& s, const Scan& a, const Plan& p) {
+  return p.nseg > 1 ? (s.B * s.Hs * p.nseg * a.Dk * a.Dv * 4 + 255) / 256 * 256 : 0;
+}
+
+Plan plan_of(const Shape& s, const Scan* a, int n, int32_t dtype) {
+  int64_t w = 0;
+  for (int i = 0; i < n; ++i) w += main_groups(s, a[i]);
+  return plan_of(w, s.T, dtype == DIFFOPT_F32 ? ChunkOf<float>::C : ChunkOf<bf16>::C);
+}
+
+// The scans of a call, as the sizes alone make them.
+int forward_scans(int64_t H, int64_t Hk, int64_t Dk, int64_t Dv, Scan* a) {
+  a[0] = Scan{};
+  a[0].nq = (int32_t)(H / Hk);
+  a[0].nk = 1;
+  a[0].Dk = (int32_t)Dk;
+  a[0].Dv = (int32_t)Dv;
+  return 1;
+}
+
+// dq, dk, dv
+int backward_scans(int64_t H, int64_t Hk, int64_t Dk, int64_t Dv, Scan* a) {
+  for (int i = 0; i < 3; ++i) {
+    a[i] = Scan{};
+    a[i].nq = i == 0 ? (int32_t)(H / Hk) : 1;
+    a[i].nk = i == 0 ? 1 : (int32_t)(H / Hk);
+    a[i].Dk = (int32_t)(i == 2 ? Dk : Dv);
+    a[i].Dv = (int32_t)(i == 2 ? Dv : Dk);
+    a[i].back = i > 0;
+    a[i].flip = i < 2;
+  }
+  return 3;
+}
+
+int64_t workspace_of(const Shape& s, const Scan* a, int n, int32_t dtype) {
+  const Plan p = plan_of(s, a, n, dtype);
+  int64_t bytes = 0;
+  for (int i = 0; i < n; ++i) bytes += segment_bytes(s, a[i], p);
+  return bytes;
+}
+
+template <class E, int DK, int NCT, bool WHOLE>
+void launch_class(const Shape& s, const Jobs& jobs, int n, bool states, hipStream_t st) {
+  constexpr int SPLIT = sizeof(E) == 2 ? 3 : 1;
+  int64_t tiles = 0, main = 0, own = 0;
+  bool keep = false;
+  for (int i = 0; i < n; ++i) {
+    const int64_t c = col_tiles(jobs.scan[i]);
+    tiles = c > tiles ? c : tiles;
+    keep |= jobs.scan[i].s1 != nullptr && jobs.nseg == 1;
+  }
+  for (int i = 0; i < n; ++i) {
+    const int64_t w = s.B * s.Hs * jobs.nseg * tiles;
+    own = w > own ? w : own;
+    main = w * jobs.scan[i].nq > main ? w * jobs.scan[i].nq : main;
+  }
+  if (states)
+    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, SPLIT, false, WHOLE>), dim3((unsigned)own, n), dim3(kChunkB), 0, st, s, jobs, (int32_t)tiles);
+  else if (keep || !WHOLE || sizeof(E) == 4)
+    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, SPLIT, true, WHOLE>), dim3((unsigned)main, n), dim3(kChunkB), 0, st, s, jobs, (int32_t)tiles);
   else
-    launch_tokens<bf16>(s, a, st);
+    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, sizeof(E) == 2 ? 2 : 1, true, WHOLE>), dim3((unsigned)main, n), dim3(kChunkB), 0, st, s, jobs,
+                       (int32_t)tiles);
+}
+
+template <class E>
+void launch_chunks(const Shape& s, const Jobs& jobs, int n, bool states, hipStream_t st) {
+  // scans of one class share a launch
+  bool done[3] = {false, false, false};
+  for (int i = 0; i < n; ++i) {
+    if (done[i]) continue;
+    const Class c = class_of(jobs.scan[i]);
+    Jobs part = jobs;
+    int k = 0;
+    for (int l = i; l < n; ++l) {
+      const Class d = class_of(jobs.scan[l]);
+      if (done[l] || d.dk != c.dk || d.nct != c.nct || d.whole != c.whole || col_tiles(jobs.scan[l]) != col_tiles(jobs.scan[i])) continue;
+      done[l] = true;
+      part.scan[k] = jobs.scan[l];
+      part.seg[k++] = jobs.seg[l];
+    }
+#define DIFFOPT_CLASS(DK, NCT)                                        \
+  if (c.dk == DK && c.whole) launch_class<E, DK, NCT, true>(s, part, k, states, st); \
+  if (c.dk == DK && !c.whole) launch_class<E, DK, NCT, false>(s, part, k, states, st);
+    DIFFOPT_CLASS(32, 1)
+    DIFFOPT_CLASS(64, 1)
+    DIFFOPT_CLASS(128, 2)
+    DIFFOPT_CLASS(256, 1)
+#undef DIFFOPT_CLASS
+  }
+}
+
+// Sequences of up to this many tokens go token after token.
+constexpr int kFewTokens = 4;
+
+// Runs the scans whose `run` is set; `a` holds all the call's scans, by which
+// the plan goes.
+int run_scans(const char* who, const Shape& s, const Scan* a, const bool* run, int n, int32_t dtype, void* workspace, int64_t bytes, hipStream_t st) {
+  if (s.T <= kFewTokens) {
+    for (int i = 0; i < n; ++i)
+      if (run[i]) {
+        if (dtype == DIFFOPT_F32)
+          launch_tokens<float>(s, a[i], st);
+        else
+          launch_tokens<bf16>(s, a[i], st);
+      }
+    return launch_status(who);
+  }
+  const Plan p = plan_of(s, a, n, dtype);
+  const int64_t need = workspace_of(s, a, n, dtype);
+  if (need > 0 && (!workspace || bytes < need))
+    return fail(DIFFOPT_EINVAL, "%s: the workspace has %lld bytes of %lld", who, (long long)(workspace ? bytes : 0), (long long)need);
+  if (!aligned_to(workspace, 16)) return fail(DIFFOPT_EINVAL, "%s: the workspace is not 16-byte aligned", who);
+  Jobs jobs{};
+  jobs.nseg = p.nseg;
+  jobs.seg_chunks = p.seg_chunks;
+  char* at = static_cast<char*>(workspace);
+  int k = 0, block = 0;
+  for (int i = 0; i < n; ++i) {
+    const int64_t b = segment_bytes(s, a[i], p);
+    if (run[i]) {
+      jobs.scan[k] = a[i];
+      jobs.seg[k++] = reinterpret_cast<float*>(at);
+    }
+    at += b;
+    block = a[i].Dk * a[i].Dv;
+  }
+  if (k == 0) return DIFFOPT_OK;
+  const bool f32 = dtype == DIFFOPT_F32;
+  if (p.nseg > 1) {
+    f32 ? launch_chunks<float>(s, jobs, k, true, st) : launch_chunks<bf16>(s, jobs, k, true, st);
+    const int64_t groups = s.B * s.Hs * ((block + kJoinB - 1) / kJoinB);
+    hipLaunchKernelGGL(linattn_join, dim3((unsigned)groups, k), dim3(kJoinB), 0, st, s, jobs, f32 ? ChunkOf<float>::C : ChunkOf<bf16>::C);
+  }
+  f32 ? launch_chunks<float>(s, jobs, k, false, st) : launch_chunks<bf16>(s, jobs, k, false, st);
   return launch_status(who);
 }
 
@@ -190,8 +880,11 @@ using namespace diffopt;
 
 extern "C" int64_t diffopt_linattn_workspace(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t Dk, int64_t Dv,
                                              int32_t dtype, int32_t backward) {
-  (void)backward;
-  return sizes_wrong(B, T, H, Hk, Dk, Dv, dtype) ? -1 : 0;
+  if (sizes_wrong(B, T, H, Hk, Dk, Dv, dtype)) return -1;
+  if (B == 0 || Hk == 0 || T <= kFewTokens) return 0;
+  Scan a[3];
+  const int n = backward ? backward_scans(H, Hk, Dk, Dv, a) : forward_scans(H, Hk, Dk, Dv, a);
+  return workspace_of(Shape{B, T, (int32_t)Hk, nullptr, nullptr}, a, n, dtype);
 }
 
 extern "C" int diffopt_linattn_fwd(const diffopt_heads* q, const diffopt_heads* k, const diffopt_heads* v,
@@ -203,30 +896,23 @@ extern "C" int diffopt_linattn_fwd(const diffopt_heads* q, const diffopt_heads* 
   static const char* who = "diffopt_linattn_fwd";
   int rc = check_call(who, B, T, H, Hk, Dk, Dv, dtype, scale, log_decay, lengths, {state, state_out});
   if (rc || B == 0 || Hk == 0) return rc;
-  Scan a{};
+  Scan a[1];
+  forward_scans(H, Hk, Dk, Dv, a);
   if (T > 0) {
-    rc = check_heads(who, "q", q, dtype, &a.q);
-    if (!rc) rc = check_heads(who, "k", k, dtype, &a.k);
-    if (!rc) rc = check_heads(who, "v", v, dtype, &a.v);
-    if (!rc) rc = check_heads(who, "out", out, dtype, &a.o);
+    rc = check_heads(who, "q", q, dtype, &a[0].q);
+    if (!rc) rc = check_heads(who, "k", k, dtype, &a[0].k);
+    if (!rc) rc = check_heads(who, "v", v, dtype, &a[0].v);
+    if (!rc) rc = check_heads(who, "out", out, dtype, &a[0].o);
     if (rc) return rc;
   } else if (!state_out) {
     return DIFFOPT_OK;
   }
-  (void)workspace;
-  (void)workspace_bytes;
-  a.s0 = state;
-  a.s1 = state_out;
-  a.s_r = Dv;
-  a.s_c = 1;
-  a.nq = (int32_t)(H / Hk);
-  a.nk = 1;
-  a.Dk = (int32_t)Dk;
-  a.Dv = (int32_t)Dv;
-  a.qs = (float)scale;
-  a.ks = 1.0f;
-  const Shape s{B, T, (int32_t)Hk, log_decay, lengths};
-  return run_scan(who, s, a, dtype, as_stream(stream));
+  a[0].s0 = state;
+  a[0].s1 = state_out;
+  a[0].qs = (float)scale;
+  a[0].ks = 1.0f;
+  const bool run[1] = {true};
+  return run_scans(who, Shape{B, T, (int32_t)Hk, log_decay, lengths}, a, run, 1, dtype, workspace, workspace_bytes, as_stream(stream));
 }
 
 extern "C" int diffopt_linattn_bwd(const diffopt_heads* dout, const float* dstate_out, const diffopt_heads* q,
@@ -239,36 +925,33 @@ extern "C" int diffopt_linattn_bwd(const diffopt_heads* dout, const float* dstat
   static const char* who = "diffopt_linattn_bwd";
   int rc = check_call(who, B, T, H, Hk, Dk, Dv, dtype, scale, log_decay, lengths, {state, dstate_out, dstate});
   if (rc || B == 0 || Hk == 0) return rc;
-  HeadArr Q{}, K{}, V{}, DO{}, DQ{}, DK{}, DV{};
+  if (dstate && (dstate == dstate_out || dstate == state))
+    return fail(DIFFOPT_EINVAL, "%s: dstate must be neither dstate_out nor state", who);
+  HeadArr Q{}, K{}, V{}, DO{};
+  Scan a[3];
+  backward_scans(H, Hk, Dk, Dv, a);
   if (T > 0) {
     rc = check_heads(who, "q", q, dtype, &Q);
     if (!rc) rc = check_heads(who, "k", k, dtype, &K);
     if (!rc) rc = check_heads(who, "v", v, dtype, &V);
     if (!rc) rc = check_heads(who, "dout", dout, dtype, &DO);
-    if (!rc && dq) rc = check_heads(who, "dq", dq, dtype, &DQ);
-    if (!rc && dk) rc = check_heads(who, "dk", dk, dtype, &DK);
-    if (!rc && dv) rc = check_heads(who, "dv", dv, dtype, &DV);
+    if (!rc && dq) rc = check_heads(who, "dq", dq, dtype, &a[0].o);
+    if (!rc && dk) rc = check_heads(who, "dk", dk, dtype, &a[1].o);
+    if (!rc && dv) rc = check_heads(who, "dv", dv, dtype, &a[2].o);
     if (rc) return rc;
   }
-  if (dstate && (dstate == dstate_out || dstate == state))
-    return fail(DIFFOPT_EINVAL, "%s: dstate must be neither dstate_out nor state", who);
-  (void)workspace;
-  (void)workspace_bytes;
-  const Shape s{B, T, (int32_t)Hk, log_decay, lengths};
-  const int32_t G = (int32_t)(H / Hk), dk_ = (int32_t)Dk, dv_ = (int32_t)Dv;
-  const float sc = (float)scale;
-  hipStream_t st = as_stream(stream);
-  if (DQ.p) {
-    rc = run_scan(who, s, Scan{DO, V, K, DQ, state, nullptr, 1, Dv, G, 1, dv_, dk_, 0, sc, 1.0f}, dtype, st);
-    if (rc) return rc;
+  const HeadArr in[3][3] = {{DO, V, K}, {V, DO, Q}, {K, Q, DO}};
+  for (int i = 0; i < 3; ++i) {
+    a[i].q = in[i][0];
+    a[i].k = in[i][1];
+    a[i].v = in[i][2];
+    a[i].s0 = i == 0 ? state : dstate_out;
+    a[i].qs = i == 0 ? (float)scale : 1.0f;
+    a[i].ks = i == 0 ? 1.0f : (float)scale;
   }
-  // dv's scan holds the state's gradient as [Dk][Dv], dk's its transpose
-  if (DV.p || dstate) {
-    rc = run_scan(who, s, Scan{K, Q, DO, DV, dstate_out, dstate, Dv, 1, 1, G, dk_, dv_, 1, 1.0f, sc}, dtype, st);
-    if (rc) return rc;
-  }
-  if (DK.p) rc = run_scan(who, s, Scan{V, DO, Q, DK, dstate_out, nullptr, 1, Dv, 1, G, dv_, dk_, 1, 1.0f, sc}, dtype, st);
-  return rc;
+  a[2].s1 = dstate;
+  const bool run[3] = {a[0].o.p != nullptr, a[1].o.p != nullptr, a[2].o.p != nullptr || dstate != nullptr};
+  return run_scans(who, Shape{B, T, (int32_t)Hk, log_decay, lengths}, a, run, 3, dtype, workspace, workspace_bytes, as_stream(stream));
 }
 
 extern "C" int diffopt_linattn_step(const diffopt_heads* q, const diffopt_heads* k, const diffopt_heads* v,
@@ -279,22 +962,17 @@ extern "C" int diffopt_linattn_step(const diffopt_heads* q, const diffopt_heads*
   int rc = check_call(who, B, 1, H, Hk, Dk, Dv, dtype, scale, log_decay, nullptr, {state});
   if (rc || B == 0 || Hk == 0) return rc;
   if (!state) return fail(DIFFOPT_EINVAL, "%s: null state", who);
-  Scan a{};
-  rc = check_heads(who, "q", q, dtype, &a.q);
-  if (!rc) rc = check_heads(who, "k", k, dtype, &a.k);
-  if (!rc) rc = check_heads(who, "v", v, dtype, &a.v);
-  if (!rc) rc = check_heads(who, "out", out, dtype, &a.o);
+  Scan a[1];
+  forward_scans(H, Hk, Dk, Dv, a);
+  rc = check_heads(who, "q", q, dtype, &a[0].q);
+  if (!rc) rc = check_heads(who, "k", k, dtype, &a[0].k);
+  if (!rc) rc = check_heads(who, "v", v, dtype, &a[0].v);
+  if (!rc) rc = check_heads(who, "out", out, dtype, &a[0].o);
   if (rc) return rc;
-  a.s0 = state;
-  a.s1 = state;
-  a.s_r = Dv;
-  a.s_c = 1;
-  a.nq = (int32_t)(H / Hk);
-  a.nk = 1;
-  a.Dk = (int32_t)Dk;
-  a.Dv = (int32_t)Dv;
-  a.qs = (float)scale;
-  a.ks = 1.0f;
-  const Shape s{B, 1, (int32_t)Hk, log_decay, nullptr};
-  return run_scan(who, s, a, dtype, as_stream(stream));
+  a[0].s0 = state;
+  a[0].s1 = state;
+  a[0].qs = (float)scale;
+  a[0].ks = 1.0f;
+  const bool run[1] = {true};
+  return run_scans(who, Shape{B, 1, (int32_t)Hk, log_decay, nullptr}, a, run, 1, dtype, nullptr, 0, as_stream(stream));
 }

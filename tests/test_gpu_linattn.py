@@ -116,6 +116,19 @@ def test_long_sequences(T, Dk, Dv, dtype):
     _check(*_inputs(1, T, 1, 1, Dk, Dv, dtype, seed=T))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_decay_is_not_rounded_along_the_way(dtype):
+    # a state carried over 20,000 tokens that add nothing: g^20000 to fp32's accuracy, not 20,000 roundings of g
+    import paper_2211_06934_amd as P
+    T, lg = 20000, torch.tensor([-1.0 / 8000, -1e-5], dtype=torch.float32)
+    z = torch.zeros(1, T, 2, 32, dtype=dtype, device="cuda")
+    s0 = torch.randn(1, 2, 32, 32, generator=torch.Generator().manual_seed(1))
+    so, o = torch.empty(1, 2, 32, 32, device="cuda"), torch.empty_like(z)
+    P.linattn_fwd(z, z, z, lg.cuda(), o, state=s0.cuda(), state_out=so)
+    ref = s0.double() * torch.exp(lg.double() * T)[None, :, None, None]
+    assert float((so.double().cpu() - ref).norm() / ref.norm()) < 2e-6
+
+
 def _strided(kind):
     def wrap(x):
         B, T, H, D = x.shape
