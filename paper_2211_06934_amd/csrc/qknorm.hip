@@ -3,12 +3,16 @@
 // diffopt.h).
 //
 // Every direction reads its operands once and writes its results once, so all
-// are bound by memory.  One wave per head vector: a lane holds pairs of
-// elements that the rotation turns together (pair p of the rotated part, or
-// two neighbours beyond it with the rotation by zero), so nothing crosses
-// lanes but the sums over the head.  Gradients of the weights gather in
-// registers over the heads a wave walks, then over the workgroup in LDS, then
-// over workgroups in a second small launch: a fixed order, no atomics.
+// are bound by memory.  A lane holds pairs of elements that the rotation turns
+// together (of the rotated part, or two neighbours beyond it with the rotation
+// by zero), so nothing crosses lanes but the sums over the head.  Gradients of
+// the weights gather in registers over the heads a wave walks, then over the
+// workgroup in LDS, then over workgroups in a second small launch: a fixed
+// order, no atomics.
+// Widths that fall into pairs of 16-byte pieces take qknorm_pieces, others
+// qknorm_any, a wave per head with single elements.
+#include <algorithm>
+
 #include "lm_common.hpp"
 
 namespace diffopt {
@@ -57,7 +61,7 @@ __device__ __forceinline__ int64_t position_of(const QkShape& s, int64_t b, int6
 
 // NP pairs per lane: heads of up to 128 NP elements.
 template <class E, int DIR, int NP>
-__global__ __launch_bounds__(kQB) void qknorm_kernel(QkShape s, QkArgs A, int32_t q_blocks) {
+__global__ __launch_bounds__(kQB) void qknorm_any(QkShape s, QkArgs A, int32_t q_blocks) {
   const int side = (int)blockIdx.x >= q_blocks;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int heads = side ? s.Hk : s.H;
@@ -197,8 +201,213 @@ __global__ __launch_bounds__(kQB) void qknorm_kernel(QkShape s, QkArgs A, int32_
   }
 }
 
-// dw[d] = the sum of the workgroups' parts: one workgroup per 16 elements of a side.
-constexpr int kRB = 256, kRCols = 16, kRRows = kRB / kRCols;
+// Heads in 16-byte pieces: a lane holds two of them, VN pairs, a head takes L
+// lanes of a group of LPG and a wave 64 / LPG heads at a time.  A wave takes a
+// token (or one of the `per` parts of its heads, where there are few tokens) and
+// walks its heads, so that the rotation's row is read once and the weights stay
+// in registers.  The launch covers the card with kPieceBlocks workgroups, which
+// walk the tokens.
+constexpr int kPieceBlocks = 1024;
+
+template <class E, int DIR, int LPG, bool INTER>
+__global__ __launch_bounds__(kQB) void qknorm_pieces(QkShape s, QkArgs A, int32_t per) {
+  constexpr int VN = Vec<E>::N, HPW = 64 / LPG;  // pairs of a lane, heads of a wave
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l = lane % LPG, sub = lane / LPG;
+  const int turned = s.rot / (2 * VN);  // lanes with rotated pairs
+  const bool on = l < s.D / (2 * VN), rotated = l < turned;
+  const int half = s.rot >> 1;
+  // first elements of the lane's two pieces
+  const int u = rotated && !INTER ? VN * l : 2 * VN * l, v = rotated && !INTER ? half + VN * l : u + VN;
+
+  // pairs (a[i], c[i]) of the lane's 2 VN elements
+  auto get = [&](const E* p, float* a, float* c) {
+    typename Vec<E>::type x{}, y{};
+    if (on) {
+      x = load_vec(p + u);
+      y = load_vec(p + v);
+    }
+#pragma unroll
+    for (int i = 0; i < VN; ++i) {
+      a[i] = INTER ? (float)(2 * i < VN ? x[2 * i % VN] : y[2 * i % VN]) : (float)x[i];
+      c[i] = INTER ? (float)(2 * i < VN ? x[(2 * i + 1) % VN] : y[(2 * i + 1) % VN]) : (float)y[i];
+    }
+  };
+  auto put = [&](E* p, const float* a, const float* c) {
+    float x[VN], y[VN];
+#pragma unroll
+    for (int i = 0; i < VN; ++i) {
+      x[i] = INTER ? (i & 1 ? c[i / 2] : a[i / 2]) : a[i];
+      y[i] = INTER ? (i & 1 ? c[(VN + i) / 2] : a[(VN + i) / 2]) : c[i];
+    }
+    if (on) {
+      store_vec(p + u, x);
+      store_vec(p + v, y);
+    }
+  };
+  auto get_weights = [&](const float* w, float none, float* a, float* c) {
+#pragma unroll
+    for (int i = 0; i < VN; ++i) {
+      const int first = INTER ? u + 2 * i : u + i, second = INTER ? u + 2 * i + 1 : v + i;
+      a[i] = on ? (w ? w[first] : none) : 0.0f;
+      c[i] = on ? (w ? w[second] : none) : 0.0f;
+    }
+  };
+  auto group_sum = [](float x) {
+#pragma unroll
+    for (int o = 1; o < LPG; o <<= 1) x += __shfl_xor(x, o, 64);
+    return x;
+  };
+
+  float wa[2][VN], wc[2][VN], ba[2][VN], bc[2][VN], ga[2][VN], gc[2][VN];
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    get_weights(A.w[side], 1.0f, wa[side], wc[side]);
+    if (DIR == kSecond) get_weights(A.b[side], 0.0f, ba[side], bc[side]);
+#pragma unroll
+    for (int i = 0; i < VN; ++i) ga[side][i] = gc[side][i] = 0.0f;
+  }
+
+  const int64_t items = s.B * s.T * per, step = (int64_t)gridDim.x * kQWaves;
+  for (int64_t item = (int64_t)blockIdx.x * kQWaves + wave; item < items; item += step) {
+    const uint32_t tok = (uint32_t)item / (uint32_t)per, part = (uint32_t)item - tok * (uint32_t)per;
+    const uint32_t b = tok / (uint32_t)s.T, t = tok - b * (uint32_t)s.T;
+    const int64_t pos = position_of(s, b, t);
+    const bool known = s.rot == 0 || (pos >= 0 && pos < s.rows);
+    float cs[VN], sn[VN];
+#pragma unroll
+    for (int i = 0; i < VN; ++i) {
+      cs[i] = known ? 1.0f : kNan;
+      sn[i] = known ? 0.0f : kNan;
+    }
+    if (known && rotated) {
+      const float *pc = s.cos + pos * half + VN * l, *psn = s.sin + pos * half + VN * l;
+#pragma unroll
+      for (int q = 0; q < VN; q += 4) {
+        const auto x = load_vec(pc + q), y = load_vec(psn + q);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          cs[q + i] = x[i];
+          sn[q + i] = y[i];
+        }
+      }
+    }
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+      const int heads = side ? s.Hk : s.H;
+      for (int h0 = (int)part * HPW; h0 < heads; h0 += (int)per * HPW) {
+        const int h = h0 + sub < heads ? h0 + sub : heads - 1;  // the last groups repeat the last head, and store nothing
+        const bool own = h0 + sub < heads;
+        const E* x = row_of<E>(A.x[side], b, t, h);
+        float xa[VN], xc[VN], ss = 0.0f;
+        get(x, xa, xc);
+        float ya[VN], yc[VN], aa[VN], ac[VN];
+        if (DIR != kFwd) get(row_of<E>(A.dy[side], b, t, h), ya, yc);
+        if (DIR == kSecond) {
+          if (A.a[side].p) {
+            get(row_of<E>(A.a[side], b, t, h), aa, ac);
+          } else {
+#pragma unroll
+            for (int i = 0; i < VN; ++i) aa[i] = ac[i] = 0.0f;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < VN; ++i) ss += xa[i] * xa[i] + xc[i] * xc[i];
+        const float rr = rsqrtf(group_sum(ss) * s.inv_d + s.eps);
+        if (DIR == kFwd) {
+          float oa[VN], oc[VN];
+#pragma unroll
+          for (int i = 0; i < VN; ++i) {
+            const float z0 = wa[side][i] * (xa[i] * rr), z1 = wc[side][i] * (xc[i] * rr);
+            oa[i] = z0 * cs[i] - z1 * sn[i];
+            oc[i] = z1 * cs[i] + z0 * sn[i];
+          }
+          if (own) put(const_cast<E*>(row_of<E>(A.o0[side], b, t, h)), oa, oc);
+          continue;
+        }
+        // x r, the cotangent turned back, u = w dz
+        float za[VN], zc[VN], xu = 0.0f;
+#pragma unroll
+        for (int i = 0; i < VN; ++i) {
+          xa[i] *= rr;
+          xc[i] *= rr;
+          za[i] = ya[i] * cs[i] + yc[i] * sn[i];
+          zc[i] = yc[i] * cs[i] - ya[i] * sn[i];
+          xu += xa[i] * wa[side][i] * za[i] + xc[i] * wc[side][i] * zc[i];
+        }
+        if (DIR == kBwd) {
+          xu = group_sum(xu) * s.inv_d;
+          float oa[VN], oc[VN];
+#pragma unroll
+          for (int i = 0; i < VN; ++i) {
+            oa[i] = rr * (wa[side][i] * za[i] - xa[i] * xu);
+            oc[i] = rr * (wc[side][i] * zc[i] - xc[i] * xu);
+            ga[side][i] += own ? za[i] * xa[i] : 0.0f;
+            gc[side][i] += own ? zc[i] * xc[i] : 0.0f;
+          }
+          if (own) put(const_cast<E*>(row_of<E>(A.o0[side], b, t, h)), oa, oc);
+          continue;
+        }
+        float xa_ = 0.0f, au = 0.0f, bz = 0.0f;
+#pragma unroll
+        for (int i = 0; i < VN; ++i) {
+          xa_ += xa[i] * aa[i] + xc[i] * ac[i];
+          au += aa[i] * wa[side][i] * za[i] + ac[i] * wc[side][i] * zc[i];
+          bz += ba[side][i] * xa[i] * za[i] + bc[side][i] * xc[i] * zc[i];
+        }
+        xu = group_sum(xu) * s.inv_d;
+        xa_ = group_sum(xa_) * s.inv_d;
+        au = group_sum(au) * s.inv_d;
+        bz = group_sum(bz) * s.inv_d;
+        float oa[VN], oc[VN], pa[VN], pc[VN];
+#pragma unroll
+        for (int i = 0; i < VN; ++i) {
+          const float t0 = rr * (aa[i] - xa[i] * xa_), t1 = rr * (ac[i] - xc[i] * xa_);  // derivative of x r along a
+          const float v0 = wa[side][i] * t0 + ba[side][i] * xa[i], v1 = wc[side][i] * t1 + bc[side][i] * xc[i];
+          oa[i] = v0 * cs[i] - v1 * sn[i];
+          oc[i] = v1 * cs[i] + v0 * sn[i];
+          const float k = 3.0f * xu * xa_ - au;
+          pa[i] = rr * (rr * (xa[i] * k - wa[side][i] * za[i] * xa_ - aa[i] * xu) + ba[side][i] * za[i] - xa[i] * bz);
+          pc[i] = rr * (rr * (xc[i] * k - wc[side][i] * zc[i] * xa_ - ac[i] * xu) + bc[side][i] * zc[i] - xc[i] * bz);
+          ga[side][i] += own ? za[i] * t0 : 0.0f;
+          gc[side][i] += own ? zc[i] * t1 : 0.0f;
+        }
+        if (own) {
+          put(const_cast<E*>(row_of<E>(A.o0[side], b, t, h)), oa, oc);
+          put(const_cast<E*>(row_of<E>(A.o1[side], b, t, h)), pa, pc);
+        }
+      }
+    }
+  }
+  if (DIR == kFwd || (!A.dw[0] && !A.dw[1])) return;
+  __shared__ float sum[kQWaves][2][2 * VN * LPG];
+#pragma unroll
+  for (int side = 0; side < 2; ++side)
+#pragma unroll
+    for (int i = 0; i < VN; ++i) {
+      float x = ga[side][i], y = gc[side][i];
+#pragma unroll
+      for (int o = LPG; o < 64; o <<= 1) {
+        x += __shfl_xor(x, o, 64);
+        y += __shfl_xor(y, o, 64);
+      }
+      if (sub == 0 && on) {
+        sum[wave][side][INTER ? u + 2 * i : u + i] = x;
+        sum[wave][side][INTER ? u + 2 * i + 1 : v + i] = y;
+      }
+    }
+  __syncthreads();
+  for (int d = threadIdx.x; d < 2 * s.D; d += kQB) {
+    const int side = d >= s.D, e = side ? d - s.D : d;
+    float x = sum[0][side][e];
+#pragma unroll
+    for (int w = 1; w < kQWaves; ++w) x += sum[w][side][e];
+    A.partial[((int64_t)side * gridDim.x + blockIdx.x) * s.D + e] = x;
+  }
+}
+
+// dw[d] = the sum of the workgroups' parts: one workgroup per 8 elements of a side.
+constexpr int kRB = 256, kRCols = 8, kRRows = kRB / kRCols;
 __global__ __launch_bounds__(kRB) void qknorm_weights(const float* partial, int32_t q_blocks, int32_t k_blocks, int32_t D,
                                                       float* dwq, float* dwk) {
   __shared__ float sum[kRRows][kRCols + 1];
@@ -208,8 +417,10 @@ __global__ __launch_bounds__(kRB) void qknorm_weights(const float* partial, int3
   const int d = blockIdx.x * kRCols + col, n = side ? k_blocks : q_blocks;
   const float* p = partial + (side ? (int64_t)q_blocks * D : 0);
   float v = 0.0f;
-  if (d < D)
+  if (d < D) {
+#pragma unroll 8
     for (int i = row; i < n; i += kRRows) v += p[(int64_t)i * D + d];
+  }
   sum[row][col] = v;
   __syncthreads();
   if (row == 0 && d < D) {
@@ -220,21 +431,51 @@ __global__ __launch_bounds__(kRB) void qknorm_weights(const float* partial, int3
 
 // ---- host -------------------------------------------------------------------
 
+// The workgroups of each side's partial sums.
 struct Blocks {
   int32_t q, k;
 };
 
-// Workgroups for each side: a wave per head vector up to kMaxBlocks in all.
-Blocks blocks_of(int64_t B, int64_t T, int64_t H, int64_t Hk) {
+// How a call is launched, by its sizes alone.
+struct Plan {
+  bool pieces;
+  int32_t lpg, per;  // pieces: lanes of a head's group, waves of a token
+  int32_t grid;
+  Blocks blocks;
+};
+
+// Widths that fall into pairs of pieces, with up to 32 lanes a head, and counts
+// of tokens that 32 bits index.
+Plan plan_of(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t D, int64_t rot, int32_t dtype) {
+  Plan p{};
+  const int two = dtype == DIFFOPT_F32 ? 8 : 16;  // elements of a lane
+  const int64_t lanes = D / two;
+  if (D % two == 0 && rot % two == 0 && lanes <= (dtype == DIFFOPT_F32 ? 32 : 16) && (double)B * T * 256.0 < 2147483648.0 && B * T > 0) {
+    p.pieces = true;
+    for (p.lpg = 4; p.lpg < lanes;) p.lpg *= 2;
+    // a token's heads are split until the card has waves enough
+    const int64_t hpw = 64 / p.lpg, parts = std::max((H + hpw - 1) / hpw, (Hk + hpw - 1) / hpw);
+    int64_t per = (int64_t)kPieceBlocks * kQWaves / (B * T);
+    per = per < 1 ? 1 : per > parts ? parts : per;
+    if (per > 256) per = 256;
+    if (per < 1) per = 1;
+    p.per = (int32_t)per;
+    const int64_t need = (B * T * per + kQWaves - 1) / kQWaves;
+    p.grid = (int32_t)(need < kPieceBlocks ? need : kPieceBlocks);
+    p.blocks = Blocks{p.grid, p.grid};
+    return p;
+  }
   const double nq = (double)B * T * H, nk = (double)B * T * Hk;
-  auto side = [&](double n) -> int32_t {
+  auto side = [&](double n) -> int32_t {  // a wave per head up to kMaxBlocks workgroups in all
     if (n == 0) return 0;
     double b = std::ceil(n / kQWaves);
     const double most = std::floor(kMaxBlocks * (n / (nq + nk)));
     if (b > most) b = most;
     return b < 1 ? 1 : (int32_t)b;
   };
-  return Blocks{side(nq), side(nk)};
+  p.blocks = Blocks{side(nq), side(nk)};
+  p.grid = p.blocks.q + p.blocks.k;
+  return p;
 }
 
 int check_heads(const char* who, const char* what, const diffopt_heads* h, int32_t dtype, HeadArr* out) {
@@ -271,39 +512,70 @@ int check_shape(const char* who, const float* cos, const float* sin, int64_t row
 }
 
 template <class E, int DIR>
-void launch_pairs(const QkShape& s, const QkArgs& A, Blocks n, hipStream_t st) {
-  const dim3 grid((unsigned)(n.q + n.k)), block(kQB);
+void launch_any(const QkShape& s, const QkArgs& A, const Plan& p, hipStream_t st) {
+  const dim3 grid((unsigned)p.grid), block(kQB);
   if (s.D <= 128)
-    hipLaunchKernelGGL((qknorm_kernel<E, DIR, 1>), grid, block, 0, st, s, A, n.q);
+    hipLaunchKernelGGL((qknorm_any<E, DIR, 1>), grid, block, 0, st, s, A, p.blocks.q);
   else if (s.D <= 256)
-    hipLaunchKernelGGL((qknorm_kernel<E, DIR, 2>), grid, block, 0, st, s, A, n.q);
+    hipLaunchKernelGGL((qknorm_any<E, DIR, 2>), grid, block, 0, st, s, A, p.blocks.q);
   else
-    hipLaunchKernelGGL((qknorm_kernel<E, DIR, 8>), grid, block, 0, st, s, A, n.q);
+    hipLaunchKernelGGL((qknorm_any<E, DIR, 8>), grid, block, 0, st, s, A, p.blocks.q);
+}
+
+template <class E, int DIR, bool INTER>
+void launch_pieces(const QkShape& s, const QkArgs& A, const Plan& p, hipStream_t st) {
+  const dim3 grid((unsigned)p.grid), block(kQB);
+  if (p.lpg == 4) hipLaunchKernelGGL((qknorm_pieces<E, DIR, 4, INTER>), grid, block, 0, st, s, A, p.per);
+  if (p.lpg == 8) hipLaunchKernelGGL((qknorm_pieces<E, DIR, 8, INTER>), grid, block, 0, st, s, A, p.per);
+  if (p.lpg == 16) hipLaunchKernelGGL((qknorm_pieces<E, DIR, 16, INTER>), grid, block, 0, st, s, A, p.per);
+  if constexpr (sizeof(E) == 4)
+    if (p.lpg == 32) hipLaunchKernelGGL((qknorm_pieces<E, DIR, 32, INTER>), grid, block, 0, st, s, A, p.per);
+}
+
+template <class E, int DIR>
+void launch_dir(const QkShape& s, const QkArgs& A, const Plan& p, hipStream_t st) {
+  if (!p.pieces)
+    launch_any<E, DIR>(s, A, p, st);
+  else if (s.interleaved)
+    launch_pieces<E, DIR, true>(s, A, p, st);
+  else
+    launch_pieces<E, DIR, false>(s, A, p, st);
 }
 
 template <int DIR>
 int launch(const char* who, const QkShape& s, const QkArgs& A, int32_t dtype, hipStream_t st) {
-  const Blocks n = blocks_of(s.B, s.T, s.H, s.Hk);
-  if (n.q + n.k > 0) {
+  const Plan p = plan_of(s.B, s.T, s.H, s.Hk, s.D, s.rot, dtype);
+  if (p.grid > 0) {
     if (dtype == DIFFOPT_F32)
-      launch_pairs<float, DIR>(s, A, n, st);
+      launch_dir<float, DIR>(s, A, p, st);
     else
-      launch_pairs<bf16, DIR>(s, A, n, st);
+      launch_dir<bf16, DIR>(s, A, p, st);
     const int rc = launch_status(who);
     if (rc) return rc;
   }
   if (DIR != kFwd && (A.dw[0] || A.dw[1])) {
-    hipLaunchKernelGGL(qknorm_weights, dim3((unsigned)((s.D + kRCols - 1) / kRCols), 2), dim3(kRB), 0, st, A.partial, n.q, n.k,
-                       s.D, A.dw[0], A.dw[1]);
+    hipLaunchKernelGGL(qknorm_weights, dim3((unsigned)((s.D + kRCols - 1) / kRCols), 2), dim3(kRB), 0, st, A.partial, p.blocks.q,
+                       p.blocks.k, s.D, A.dw[0], A.dw[1]);
     return launch_status(who);
   }
   return DIFFOPT_OK;
 }
 
+// Partial sums of any call of these sizes, whatever its element type.
+int64_t workspace_of(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t D) {
+  int64_t most = 0;
+  for (int32_t dtype : {DIFFOPT_F32, DIFFOPT_BF16})
+    for (int64_t rot : {(int64_t)0, (int64_t)1}) {  // 1: a rotated part that does not fall into pieces
+      const Plan p = plan_of(B, T, H, Hk, D, rot, dtype);
+      const int64_t n = ((int64_t)p.blocks.q + p.blocks.k) * D * 4;
+      most = n > most ? n : most;
+    }
+  return most;
+}
+
 int check_workspace(const char* who, const QkShape& s, QkArgs* A, void* workspace, int64_t bytes) {
   if (!A->dw[0] && !A->dw[1]) return DIFFOPT_OK;
-  const Blocks n = blocks_of(s.B, s.T, s.H, s.Hk);
-  const int64_t need = (int64_t)(n.q + n.k) * s.D * 4;
+  const int64_t need = workspace_of(s.B, s.T, s.H, s.Hk, s.D);
   if (need > 0 && (!workspace || bytes < need))
     return fail(DIFFOPT_EINVAL, "%s: the workspace has %lld bytes of %lld", who, (long long)(workspace ? bytes : 0), (long long)need);
   if (!aligned_to(workspace, 4)) return fail(DIFFOPT_EINVAL, "%s: the workspace is not 4-byte aligned", who);
@@ -333,8 +605,7 @@ using namespace diffopt;
 
 extern "C" int64_t diffopt_qknorm_rope_workspace(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t D) {
   if (!sizes_ok(B, T, H, Hk, D)) return -1;
-  const Blocks n = blocks_of(B, T, H, Hk);
-  return (int64_t)(n.q + n.k) * D * 4;
+  return workspace_of(B, T, H, Hk, D);
 }
 
 extern "C" int diffopt_qknorm_rope_fwd(const diffopt_heads* q, const diffopt_heads* k, const float* q_weight,
