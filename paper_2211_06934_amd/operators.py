@@ -18,7 +18,7 @@ from typing import Optional
 
 import torch
 
-from .diffopt import _check, _lib, _stream
+from .diffopt import _check, _done, _lib, _native, _stream
 
 F32, BF16 = 0, 1
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
@@ -116,10 +116,22 @@ def _type_of(x, what: str) -> int:
     return _DTYPES[x.dtype]
 
 
-def _scratch(given, need: int, device):
-    """(tensor kept alive, address, bytes) of a call's workspace."""
-    if given is None:
-        given = torch.empty(need, dtype=torch.uint8, device=device) if need > 0 else None
+def _here(workspace, stream) -> bool:
+    """Whether scratch memory that the call allocates may be allocated on the current stream."""
+    return stream is None or workspace is not None
+
+
+def _scratch(given, need: int, device, stream):
+    """(tensor kept alive, address, bytes) of a call's workspace, allocated on the call's stream: it returns to that stream's
+    pool, so nothing enqueued elsewhere takes it while the call still uses it."""
+    if given is None and need > 0:
+        if stream is None:
+            given = torch.empty(need, dtype=torch.uint8, device=device)
+        else:
+            with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=device)):
+                given = torch.empty(need, dtype=torch.uint8, device=device)
+    elif given is None:
+        pass
     elif not isinstance(given, torch.Tensor) or given.dtype != torch.uint8 or not given.is_cuda or not given.is_contiguous():
         raise ValueError("workspace: expected a contiguous uint8 tensor in device memory")
     elif given.numel() < need:
@@ -151,6 +163,9 @@ def linattn_fwd(q, k, v, log_decay, out, state=None, state_out=None, lengths=Non
 
     q [B, T, H, Dk], k [B, T, Hk, Dk], v [B, T, Hk, Dv] -> out [B, T, H, Dv]; log_decay [Hk]; state, state_out
     [B, Hk, Dk, Dv]; lengths int32 [B] (tokens from there on are padding)."""
+    if _here(workspace, stream) and _done(_native.linattn_fwd(
+            q, k, v, log_decay, out, state, state_out, lengths, scale, workspace, _stream(stream))):
+        return
     dt = _type_of(q, "q")
     H, Hk, Dk, Dv = _dims(q, k, v, 4)
     B, T = q.shape[:2]
@@ -159,7 +174,7 @@ def linattn_fwd(q, k, v, log_decay, out, state=None, state_out=None, lengths=Non
     _apart(out, "out")
     lg, ln = _flat(log_decay, "log_decay", q, (Hk,)), _flat(lengths, "lengths", q, (B,), True, torch.int32)
     s0, s1 = _flat(state, "state", q, (B, Hk, Dk, Dv), True), _flat(state_out, "state_out", q, (B, Hk, Dk, Dv), True)
-    keep, ws, nws = _scratch(workspace, _lib.diffopt_linattn_workspace(B, T, H, Hk, Dk, Dv, dt, 0), q.device)
+    keep, ws, nws = _scratch(workspace, _lib.diffopt_linattn_workspace(B, T, H, Hk, Dk, Dv, dt, 0), q.device, stream)
     _check(_lib.diffopt_linattn_fwd(_ref(cq), _ref(ck), _ref(cv), lg, ln, s0, B, T, H, Hk, Dk, Dv, dt, float(scale), _ref(co), s1,
                                     ws, nws, _stream(stream)))
 
@@ -168,6 +183,9 @@ def linattn_bwd(dout, q, k, v, log_decay, dq, dk, dv, state=None, dstate_out=Non
                 workspace=None, stream=None) -> None:
     """diffopt_linattn_bwd: gradients of linattn_fwd for the cotangents dout and dstate_out; any of dq, dk, dv, dstate may be
     None."""
+    if _here(workspace, stream) and _done(_native.linattn_bwd(
+            dout, q, k, v, log_decay, dq, dk, dv, state, dstate_out, dstate, lengths, scale, workspace, _stream(stream))):
+        return
     dt = _type_of(q, "q")
     H, Hk, Dk, Dv = _dims(q, k, v, 4)
     B, T = q.shape[:2]
@@ -181,7 +199,7 @@ def linattn_bwd(dout, q, k, v, log_decay, dq, dk, dv, state=None, dstate_out=Non
     lg, ln = _flat(log_decay, "log_decay", q, (Hk,)), _flat(lengths, "lengths", q, (B,), True, torch.int32)
     s0, ds1, ds0 = (_flat(x, w, q, (B, Hk, Dk, Dv), True) for x, w in ((state, "state"), (dstate_out, "dstate_out"),
                                                                        (dstate, "dstate")))
-    keep, ws, nws = _scratch(workspace, _lib.diffopt_linattn_workspace(B, T, H, Hk, Dk, Dv, dt, 1), q.device)
+    keep, ws, nws = _scratch(workspace, _lib.diffopt_linattn_workspace(B, T, H, Hk, Dk, Dv, dt, 1), q.device, stream)
     _check(_lib.diffopt_linattn_bwd(_ref(cdo), ds1, _ref(cq), _ref(ck), _ref(cv), lg, ln, s0, B, T, H, Hk, Dk, Dv, dt, float(scale),
                                     _ref(cdq), _ref(cdk), _ref(cdv), ds0, ws, nws, _stream(stream)))
 
@@ -189,6 +207,8 @@ def linattn_bwd(dout, q, k, v, log_decay, dq, dk, dv, state=None, dstate_out=Non
 def linattn_step(q, k, v, log_decay, state, out, scale: float = 1.0, stream=None) -> None:
     """diffopt_linattn_step: one token per sequence, q [B, H, Dk], k [B, Hk, Dk], v [B, Hk, Dv] -> out [B, H, Dv]; state
     [B, Hk, Dk, Dv] is updated in place."""
+    if _done(_native.linattn_step(q, k, v, log_decay, state, out, scale, _stream(stream))):
+        return
     dt = _type_of(q, "q")
     H, Hk, Dk, Dv = _dims(q, k, v, 3)
     B = q.shape[0]
@@ -256,6 +276,9 @@ def qknorm_rope_fwd(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions=
                     interleaved: bool = False, stream=None) -> None:
     """diffopt_qknorm_rope_fwd: q [B, T, H, D] and k [B, T, Hk, D] (or None) normed for each head, scaled by the weights [D]
     (None: ones) and rotated by row positions[b, t] (None: first + t) of cos and sin [rows, rot/2] (None: no rotation)."""
+    if _done(_native.qknorm_rope_fwd(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions, first, eps, bool(interleaved),
+                                     _stream(stream))):
+        return
     sq, sk, args = _qk_shape(q, k, q_weight, k_weight, cos, sin, positions, first, eps, interleaved)
     x = _qk_pair(q, k, "%s", q, sq, sk)
     y = _qk_pair(q_out, k_out, "%s_out", q, sq, sk, result=True)
@@ -265,12 +288,16 @@ def qknorm_rope_fwd(q, k, q_weight, k_weight, cos, sin, q_out, k_out, positions=
 def qknorm_rope_bwd(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq, dk, dq_weight=None, dk_weight=None, positions=None,
                     first: int = 0, eps: float = 1e-6, interleaved: bool = False, workspace=None, stream=None) -> None:
     """diffopt_qknorm_rope_bwd: gradients of qknorm_rope_fwd; the weights' may be None."""
+    if _here(workspace, stream) and _done(_native.qknorm_rope_bwd(
+            dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, dq, dk, dq_weight, dk_weight, positions, first, eps,
+            bool(interleaved), workspace, _stream(stream))):
+        return
     sq, sk, args = _qk_shape(q, k, q_weight, k_weight, cos, sin, positions, first, eps, interleaved)
     x, dy = _qk_pair(q, k, "%s", q, sq, sk), _qk_pair(dq_out, dk_out, "d%s_out", q, sq, sk)
     dx = _qk_pair(dq, dk, "d%s", q, sq, sk, result=True)
     wq, wk = _flat(dq_weight, "dq_weight", q, sq[3:], True), _flat(dk_weight, "dk_weight", q, sq[3:], True)
     need = _lib.diffopt_qknorm_rope_workspace(*sq[:3], sk[2], sq[3]) if wq or wk else 0
-    keep, ws, nws = _scratch(workspace, need, q.device)
+    keep, ws, nws = _scratch(workspace, need, q.device, stream)
     _check(_lib.diffopt_qknorm_rope_bwd(_ref(dy[0]), _ref(dy[1]), _ref(x[0]), _ref(x[1]), *args, _ref(dx[0]), _ref(dx[1]), wq, wk, ws,
                                         nws, _stream(stream)))
 
@@ -279,6 +306,10 @@ def qknorm_rope_bwd_bwd(ddq, ddk, ddq_weight, ddk_weight, dq_out, dk_out, q, k, 
                         out_q, out_k, out_q_weight=None, out_k_weight=None, positions=None, first: int = 0, eps: float = 1e-6,
                         interleaved: bool = False, workspace=None, stream=None) -> None:
     """diffopt_qknorm_rope_bwd_bwd: gradients of qknorm_rope_bwd for cotangents of its results (None: zero)."""
+    if _here(workspace, stream) and _done(_native.qknorm_rope_bwd_bwd(
+            ddq, ddk, ddq_weight, ddk_weight, dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, out_dq_out, out_dk_out, out_q, out_k,
+            out_q_weight, out_k_weight, positions, first, eps, bool(interleaved), workspace, _stream(stream))):
+        return
     sq, sk, args = _qk_shape(q, k, q_weight, k_weight, cos, sin, positions, first, eps, interleaved)
     x, dy = _qk_pair(q, k, "%s", q, sq, sk), _qk_pair(dq_out, dk_out, "d%s_out", q, sq, sk)
     a = _qk_pair(ddq, ddk, "dd%s", q, sq, sk, optional=True)
@@ -287,7 +318,7 @@ def qknorm_rope_bwd_bwd(ddq, ddk, ddq_weight, ddk_weight, dq_out, dk_out, q, k, 
     b = [_flat(w, n, q, sq[3:], True) for w, n in ((ddq_weight, "ddq_weight"), (ddk_weight, "ddk_weight"))]
     wq, wk = _flat(out_q_weight, "out_q_weight", q, sq[3:], True), _flat(out_k_weight, "out_k_weight", q, sq[3:], True)
     need = _lib.diffopt_qknorm_rope_workspace(*sq[:3], sk[2], sq[3]) if wq or wk else 0
-    keep, ws, nws = _scratch(workspace, need, q.device)
+    keep, ws, nws = _scratch(workspace, need, q.device, stream)
     _check(_lib.diffopt_qknorm_rope_bwd_bwd(_ref(a[0]), _ref(a[1]), *b, _ref(dy[0]), _ref(dy[1]), _ref(x[0]), _ref(x[1]), *args,
                                             _ref(oy[0]), _ref(oy[1]), _ref(ox[0]), _ref(ox[1]), wq, wk, ws, nws, _stream(stream)))
 
@@ -329,14 +360,19 @@ def _logits(logits, ids, teacher, temperature):
 def distill_fwd(logits, ids, teacher, loss, stats, temperature: float = 1.0, workspace=None, stream=None) -> None:
     """diffopt_distill_fwd: loss [N] of logits [N, V] against the teacher's logits [N, K] at tokens ids [N, K]; stats [N, 2] is
     what the backwards take."""
+    if _here(workspace, stream) and _done(_native.distill_fwd(
+            logits, ids, teacher, loss, stats, temperature, workspace, _stream(stream))):
+        return
     N, V, K, dt, args = _logits(logits, ids, teacher, temperature)
     pl, ps = _flat(loss, "loss", logits, (N,)), _flat(stats, "stats", logits, (N, 2))
-    keep, ws, nws = _scratch(workspace, _lib.diffopt_distill_workspace(N, V, dt, K), logits.device)
+    keep, ws, nws = _scratch(workspace, _lib.diffopt_distill_workspace(N, V, dt, K), logits.device, stream)
     _check(_lib.diffopt_distill_fwd(*args, pl, ps, ws, nws, _stream(stream)))
 
 
 def distill_bwd(dloss, logits, ids, teacher, stats, dlogits, dteacher=None, temperature: float = 1.0, stream=None) -> None:
     """diffopt_distill_bwd: gradients of distill_fwd for the cotangent dloss [N]; dlogits may be logits."""
+    if _done(_native.distill_bwd(dloss, logits, ids, teacher, stats, dlogits, dteacher, temperature, _stream(stream))):
+        return
     N, V, K, dt, args = _logits(logits, ids, teacher, temperature)
     pg, ps = _flat(dloss, "dloss", logits, (N,)), _flat(stats, "stats", logits, (N, 2))
     pd, dstride = _rows(dlogits, "dlogits", logits, (N, V), True)
@@ -346,10 +382,13 @@ def distill_bwd(dloss, logits, ids, teacher, stats, dlogits, dteacher=None, temp
 def distill_fwd_bwd(dloss, logits, ids, teacher, loss, stats, dlogits, dteacher=None, temperature: float = 1.0, workspace=None,
                     stream=None) -> None:
     """diffopt_distill_fwd_bwd: the loss and its gradients for a dloss known beforehand, the logits read once."""
+    if _here(workspace, stream) and _done(_native.distill_fwd_bwd(
+            dloss, logits, ids, teacher, loss, stats, dlogits, dteacher, temperature, workspace, _stream(stream))):
+        return
     N, V, K, dt, args = _logits(logits, ids, teacher, temperature)
     pg, pl, ps = _flat(dloss, "dloss", logits, (N,)), _flat(loss, "loss", logits, (N,)), _flat(stats, "stats", logits, (N, 2))
     pd, dstride = _rows(dlogits, "dlogits", logits, (N, V), True)
-    keep, ws, nws = _scratch(workspace, _lib.diffopt_distill_workspace(N, V, dt, K), logits.device)
+    keep, ws, nws = _scratch(workspace, _lib.diffopt_distill_workspace(N, V, dt, K), logits.device, stream)
     _check(_lib.diffopt_distill_fwd_bwd(pg, *args, pl, ps, pd, dstride, _flat(dteacher, "dteacher", logits, (N, K), True), ws, nws,
                                         _stream(stream)))
 
@@ -358,11 +397,15 @@ def distill_bwd_bwd(ddlogits, ddteacher, dloss, logits, ids, teacher, stats, out
                     temperature: float = 1.0, workspace=None, stream=None) -> None:
     """diffopt_distill_bwd_bwd: gradients of distill_bwd for cotangents of dlogits and dteacher (None: zero); out_dloss and
     out_teacher may be None."""
+    if _here(workspace, stream) and _done(_native.distill_bwd_bwd(
+            ddlogits, ddteacher, dloss, logits, ids, teacher, stats, out_dloss, out_logits, out_teacher, temperature, workspace,
+            _stream(stream))):
+        return
     N, V, K, dt, args = _logits(logits, ids, teacher, temperature)
     pa, astride = (None, 0) if ddlogits is None else _rows(ddlogits, "ddlogits", logits, (N, V))
     po, ostride = _rows(out_logits, "out_logits", logits, (N, V), True)
     pg, ps = _flat(dloss, "dloss", logits, (N,)), _flat(stats, "stats", logits, (N, 2))
-    keep, ws, nws = _scratch(workspace, _lib.diffopt_distill_workspace(N, V, dt, K), logits.device)
+    keep, ws, nws = _scratch(workspace, _lib.diffopt_distill_workspace(N, V, dt, K), logits.device, stream)
     _check(_lib.diffopt_distill_bwd_bwd(pa, astride, _flat(ddteacher, "ddteacher", logits, (N, K), True), pg, *args, ps,
                                         _flat(out_dloss, "out_dloss", logits, (N,), True), po, ostride,
                                         _flat(out_teacher, "out_teacher", logits, (N, K), True), ws, nws, _stream(stream)))
