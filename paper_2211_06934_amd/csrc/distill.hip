@@ -1,13 +1,15 @@
 // Distillation from a teacher's top logits on gfx950: the loss, its gradient,
 // and the gradient's own vector-Jacobian product (formulas in diffopt.h).
 //
-// One workgroup per row.  The row's max m and sum s = sum exp((x - m)/T) come
-// from one pass with a running max (a lane rescales its sum once per 16 bytes);
-// wave 0 forms the teacher's softmax over the K entries meanwhile.  The
-// gradient's dense part g T p is one more pass over the row; the K entries are
-// then written once more by the same workgroup after a barrier, each with the
-// sum of q over the entries of its token, so nothing is added atomically and
-// equal ids need no order.  A few exponentials per element: bound by memory.
+// One workgroup per row, or per slice of one where there are few rows.  The
+// row's max m and sum s = sum exp((x - m)/T) come from one pass with a running
+// max (a lane rescales its sum once per 16 bytes); wave 0 forms the teacher's
+// softmax over the K entries meanwhile.  The gradient's dense part g T p takes
+// the row again: where the same call has just read it, from registers (rows of
+// up to 512 KiB), else from memory.  The K entries are then written once more
+// by the same workgroup after a barrier, each with the sum of q over the entries
+// of its token, so nothing is added atomically and equal ids need no order.
+// A few exponentials per element: bound by memory.
 #include <initializer_list>
 
 #include "lm_common.hpp"
@@ -113,64 +115,142 @@ __device__ float entry_terms(const Rows& r, Entries& E, float m, float s, int la
   return wave_sum(mean);
 }
 
-// f(first element, 16 bytes of x from there) over a row's aligned vectors,
-// g(element) over the elements before and after them.
-template <class E_, class F, class G>
-__device__ __forceinline__ void over_row(const E_* x, int64_t n, F f, G g) {
-  constexpr int NV = Vec<E_>::N;
+// Elements before the first 16-byte boundary of x, at most n.
+template <class E_>
+__device__ __forceinline__ int64_t head_of(const E_* x, int64_t n) {
   const int64_t off = (int64_t)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (int)sizeof(E_);
-  const int64_t head = off < n ? off : n;
-  const int64_t nv = (n - head) / NV;
-  for (int64_t i = threadIdx.x; i < nv; i += blockDim.x) f(head + i * NV);
-  const int64_t rest = n - nv * NV;  // head and tail elements
-  if ((int64_t)threadIdx.x < rest) g((int64_t)threadIdx.x < head ? (int64_t)threadIdx.x : threadIdx.x + nv * NV);
+  return off < n ? off : n;
 }
 
+// f(first element) over the aligned 16-byte pieces of elements [c0, c1) of a
+// row, g(element) over the elements before and after them.
+template <class E_, class F, class G>
+__device__ __forceinline__ void over_row(const E_* x, int64_t c0, int64_t c1, F f, G g) {
+  constexpr int NV = Vec<E_>::N;
+  const int64_t n = c1 - c0, head = head_of(x + c0, n), nv = (n - head) / NV;
+  for (int64_t i = threadIdx.x; i < nv; i += blockDim.x) f(c0 + head + i * NV);
+  const int64_t rest = n - nv * NV;  // head and tail elements
+  if ((int64_t)threadIdx.x < rest) g(c0 + ((int64_t)threadIdx.x < head ? (int64_t)threadIdx.x : threadIdx.x + nv * NV));
+}
+
+constexpr int kMaxWaves = 16;
 struct Reduce {
-  float m[kDB / 64], s[kDB / 64];
+  float m[kMaxWaves], s[kMaxWaves];
+};
+
+// One lane's running max and sum.
+struct Running {
+  float m = -kInf, s = 0.0f;
+  template <int N>
+  __device__ __forceinline__ void piece(const float* e, float c) {
+    float vm = e[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) vm = fmaxf(vm, e[i]);
+    if (vm > m) {
+      s *= exp2_fast((m - vm) * c);
+      m = vm;
+    }
+    const float b = safe_max(m);
+#pragma unroll
+    for (int i = 0; i < N; ++i) s += exp2_fast((e[i] - b) * c);
+  }
+  __device__ __forceinline__ void one(float e, float c) { join(m, s, e, e == -kInf ? 0.0f : (e - e == 0.0f ? 1.0f : kNan), c); }
+  // over the workgroup
+  __device__ __forceinline__ void all(Reduce& R, float c) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const float m2 = __shfl_xor(m, o, 64), s2 = __shfl_xor(s, o, 64);
+      join(m, s, m2, s2, c);
+    }
+    const int wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) {
+      R.m[wave] = m;
+      R.s[wave] = s;
+    }
+    __syncthreads();
+    m = R.m[0];
+    s = R.s[0];
+    for (int w = 1; w < nw; ++w) join(m, s, R.m[w], R.s[w], c);
+  }
 };
 
 template <class E_>
-__device__ void row_stats(const E_* x, int64_t V, float c, Reduce& R, float& m, float& s) {
-  m = -kInf;
-  s = 0.0f;
+__device__ __forceinline__ void row_stats(const E_* x, int64_t c0, int64_t c1, float c, Running& run) {
   over_row(
-      x, V,
+      x, c0, c1,
       [&](int64_t at) {
         const auto v = load_vec(x + at);
-        float e[Vec<E_>::N], vm = -kInf;
+        float e[Vec<E_>::N];
 #pragma unroll
-        for (int i = 0; i < Vec<E_>::N; ++i) {
-          e[i] = (float)v[i];
-          vm = fmaxf(vm, e[i]);
-        }
-        if (vm > m) {
-          s *= exp2_fast((m - vm) * c);
-          m = vm;
-        }
-        const float b = safe_max(m);
-#pragma unroll
-        for (int i = 0; i < Vec<E_>::N; ++i) s += exp2_fast((e[i] - b) * c);
+        for (int i = 0; i < Vec<E_>::N; ++i) e[i] = (float)v[i];
+        run.template piece<Vec<E_>::N>(e, c);
       },
-      [&](int64_t at) {
-        const float e = (float)x[at];
-        join(m, s, e, e == -kInf ? 0.0f : (e - e == 0.0f ? 1.0f : kNan), c);
-      });
+      [&](int64_t at) { run.one((float)x[at], c); });
+}
+
+// Elements [c0, c1) of a row in registers: NV pieces of every lane of a
+// workgroup of B, and one of the elements around them.
+template <class E_, int B, int NV>
+struct Kept {
+  static constexpr int N = Vec<E_>::N;
+  typename Vec<E_>::type v[NV];
+  E_ single;
+  int64_t first, nv, at_single;
+  bool has_single;
+
+  // where the pieces lie goes by x; another array's are taken at the same elements
+  __device__ __forceinline__ void place(const E_* x, int64_t c0, int64_t c1) {
+    const int64_t n = c1 - c0, head = head_of(x + c0, n), rest = n - (n - head) / N * N;
+    nv = (n - head) / N;
+    first = c0 + head;
+    has_single = (int64_t)threadIdx.x < rest;
+    at_single = c0 + ((int64_t)threadIdx.x < head ? (int64_t)threadIdx.x : threadIdx.x + nv * N);
+  }
+  __device__ __forceinline__ bool has(int i) const { return threadIdx.x + i * B < nv; }
+  __device__ __forceinline__ int64_t at(int i) const { return first + (int64_t)(threadIdx.x + i * B) * N; }
+  __device__ __forceinline__ void load(const E_* x) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const float m2 = __shfl_xor(m, o, 64), s2 = __shfl_xor(s, o, 64);
-    join(m, s, m2, s2, c);
+    for (int i = 0; i < NV; ++i)
+      if (has(i)) v[i] = load_vec(x + at(i));
+    if (has_single) single = x[at_single];
   }
-  const int wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) {
-    R.m[wave] = m;
-    R.s[wave] = s;
+};
+
+// What a workgroup takes of a launch of `slices` per row.
+struct Slice {
+  int64_t row, c0, c1;
+  int32_t index;
+};
+
+__device__ __forceinline__ Slice slice_of(const Rows& r, int64_t block, int32_t slices, int64_t per) {
+  Slice s;
+  s.row = block / slices;
+  s.index = (int32_t)(block - s.row * slices);
+  s.c0 = s.index * per;
+  s.c1 = s.c0 + per < r.V ? s.c0 + per : r.V;
+  return s;
+}
+
+// A slice's max and sum, for rows that several workgroups share.
+template <class E_>
+__global__ __launch_bounds__(kDB) void distill_parts(Rows r, float* parts, int32_t slices, int64_t per) {
+  __shared__ Reduce R;
+  const Slice sl = slice_of(r, blockIdx.x, slices, per);
+  const float c = r.invT * kLog2e;
+  Running run;
+  row_stats(static_cast<const E_*>(r.logits) + sl.row * r.row_stride, sl.c0, sl.c1, c, run);
+  run.all(R, c);
+  if (threadIdx.x == 0) {
+    parts[2 * (int64_t)blockIdx.x] = run.m;
+    parts[2 * (int64_t)blockIdx.x + 1] = run.s;
   }
-  __syncthreads();
-  m = R.m[0];
-  s = R.s[0];
-  for (int w = 1; w < nw; ++w) join(m, s, R.m[w], R.s[w], c);
+}
+
+// The row's max and sum from its slices'.
+__device__ __forceinline__ void join_parts(const float* parts, int64_t row, int32_t slices, float c, Running& run, Reduce& R) {
+  for (int i = threadIdx.x; i < slices; i += blockDim.x) join(run.m, run.s, parts[2 * (row * slices + i)], parts[2 * (row * slices + i) + 1], c);
+  run.all(R, c);
 }
 
 // The sum of q over the entries that name the token of entry j.
@@ -180,153 +260,230 @@ __device__ __forceinline__ float same_token(const float* w, const Entries& E, in
   return sum;
 }
 
-// The row's results from its statistics on: loss, gradients.
-template <class E_, bool FWD, bool BWD>
-__global__ __launch_bounds__(kDB) void distill_row(Rows r, const float* dloss, float* loss, float* stats, E_* dlogits,
-                                                   int64_t drow_stride, float* dteacher) {
+// Where a row's max and sum come from.
+enum Stats {
+  kGiven,  // the caller
+  kRead,   // this workgroup's pass over the row
+  kKept,   // the same, the row staying in registers
+  kParts   // slices of the row
+};
+
+template <class E_, int STATS, bool BWD, int B = kDB, int NV = 1>
+__global__ __launch_bounds__(B) void distill_row(Rows r, const float* dloss, float* loss, float* stats, E_* dlogits, int64_t drow_stride,
+                                                 float* dteacher, const float* parts, int32_t slices, int64_t per) {
+  constexpr bool FWD = STATS != kGiven;
   __shared__ Entries E;
   __shared__ Reduce R;
   const int lane = threadIdx.x & 63;
   const float c = r.invT * kLog2e;
-  for (int64_t row = blockIdx.x; row < r.N; row += gridDim.x) {
-    const E_* x = static_cast<const E_*>(r.logits) + row * r.row_stride;
-    __syncthreads();
-    if (threadIdx.x < 64) {
-      teacher_softmax(r, row, E, lane);
-      gather(x, E, r.K, E.x, lane);  // before dlogits, which may be logits, is written
-    }
-    float m, s;
-    if (FWD) {
-      row_stats(x, r.V, c, R, m, s);
-      if (threadIdx.x == 0) {
-        stats[2 * row] = m;
-        stats[2 * row + 1] = s;
-      }
-    } else {
-      m = stats[2 * row];
-      s = stats[2 * row + 1];
-    }
-    __syncthreads();
-    const bool some = E.some, bad = E.bad;
-    const float g = BWD ? (bad ? kNan : dloss[row]) : 0.0f, gT = g * r.T;
-    if (threadIdx.x < 64 && (FWD || dteacher)) {
-      const float mean = entry_terms(r, E, m, s, lane);
-      if (FWD && lane == 0) loss[row] = bad ? kNan : some ? r.T * mean : 0.0f;
-      if (BWD && dteacher)
-        for (int j = lane; j < r.K; j += 64)
-          dteacher[row * r.K + j] = E.q[j] != 0.0f ? g * E.q[j] * (E.lq[j] - mean) : bad ? kNan : 0.0f;
-    }
-    if (!BWD) continue;
-    E_* dx = dlogits + row * drow_stride;
-    const float w = some ? gT / s : 0.0f;
-    over_row(
-        x, r.V,
-        [&](int64_t at) {
-          float y[Vec<E_>::N];
-          const auto v = load_vec(x + at);
-#pragma unroll
-          for (int i = 0; i < Vec<E_>::N; ++i) y[i] = some ? w * exp2_fast(((float)v[i] - m) * c) : 0.0f;
-          store_vec(dx + at, y);
-        },
-        [&](int64_t at) { dx[at] = (E_)(some ? w * exp2_fast(((float)x[at] - m) * c) : 0.0f); });
-    __syncthreads();  // the entries' elements are written after the dense part's
-    for (int j = threadIdx.x; j < r.K; j += kDB)
-      if (E.id[j] >= 0)
-        dx[E.id[j]] = (E_)(w * exp2_fast((E.x[j] - m) * c) - gT * same_token(E.q, E, r.K, E.id[j]));
+  const Slice sl = slice_of(r, blockIdx.x, BWD ? slices : 1, BWD ? per : r.V);
+  const int64_t row = sl.row;
+  const E_* x = static_cast<const E_*>(r.logits) + row * r.row_stride;
+  Kept<E_, B, NV> kept;
+  if (STATS == kKept) {
+    kept.place(x, 0, r.V);
+    kept.load(x);
   }
+  if (threadIdx.x < 64) {
+    teacher_softmax(r, row, E, lane);
+    gather(x, E, r.K, E.x, lane);  // before dlogits, which may be logits, is written
+  }
+  Running run;
+  if (STATS == kRead) row_stats(x, 0, r.V, c, run);
+  if (STATS == kKept) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (kept.has(i)) {
+        float e[Vec<E_>::N];
+#pragma unroll
+        for (int k = 0; k < Vec<E_>::N; ++k) e[k] = (float)kept.v[i][k];
+        run.template piece<Vec<E_>::N>(e, c);
+      }
+    if (kept.has_single) run.one((float)kept.single, c);
+  }
+  if (STATS == kRead || STATS == kKept) run.all(R, c);
+  if (STATS == kParts) join_parts(parts, row, slices, c, run, R);
+  if (STATS == kGiven) {
+    run.m = stats[2 * row];
+    run.s = stats[2 * row + 1];
+  } else if (threadIdx.x == 0 && sl.index == 0) {
+    stats[2 * row] = run.m;
+    stats[2 * row + 1] = run.s;
+  }
+  const float m = run.m, s = run.s;
+  __syncthreads();
+  const bool some = E.some, bad = E.bad;
+  const float g = BWD ? (bad ? kNan : dloss[row]) : 0.0f, gT = g * r.T;
+  if (threadIdx.x < 64 && sl.index == 0 && (FWD || dteacher)) {
+    const float mean = entry_terms(r, E, m, s, lane);
+    if (FWD && lane == 0) loss[row] = bad ? kNan : some ? r.T * mean : 0.0f;
+    if (BWD && dteacher)
+      for (int j = lane; j < r.K; j += 64)
+        dteacher[row * r.K + j] = E.q[j] != 0.0f ? g * E.q[j] * (E.lq[j] - mean) : bad ? kNan : 0.0f;
+  }
+  if (!BWD) return;
+  E_* dx = dlogits + row * drow_stride;
+  const float w = some ? gT / s : 0.0f;
+  auto piece = [&](int64_t at, typename Vec<E_>::type v) {
+    float y[Vec<E_>::N];
+#pragma unroll
+    for (int i = 0; i < Vec<E_>::N; ++i) y[i] = some ? w * exp2_fast(((float)v[i] - m) * c) : 0.0f;
+    store_vec(dx + at, y);
+  };
+  auto one = [&](int64_t at, float e) { dx[at] = (E_)(some ? w * exp2_fast((e - m) * c) : 0.0f); };
+  if (STATS == kKept) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (kept.has(i)) piece(kept.at(i), kept.v[i]);
+    if (kept.has_single) one(kept.at_single, (float)kept.single);
+  } else {
+    over_row(x, sl.c0, sl.c1, [&](int64_t at) { piece(at, load_vec(x + at)); }, [&](int64_t at) { one(at, (float)x[at]); });
+  }
+  __syncthreads();  // the entries' elements are written after the dense part's
+  for (int j = threadIdx.x; j < r.K; j += blockDim.x)
+    if (E.id[j] >= sl.c0 && E.id[j] < sl.c1)
+      dx[E.id[j]] = (E_)(w * exp2_fast((E.x[j] - m) * c) - gT * same_token(E.q, E, r.K, E.id[j]));
+}
+
+// ---- the gradient's vector-Jacobian product ---------------------------------
+
+struct Second {
+  const void* a;  // cotangent of dlogits or NULL
+  int64_t a_stride;
+  const float *c, *dloss, *stats;
+  float *out_dloss, *out_teacher;
+  void* out;
+  int64_t out_stride;
+};
+
+// A lane's sum of p a (times s), over elements [c0, c1).
+template <class E_>
+__device__ __forceinline__ float weighted(const E_* x, const E_* a, int64_t c0, int64_t c1, float m, float c) {
+  float pa = 0.0f;
+  over_row(
+      x, c0, c1,
+      [&](int64_t at) {
+        const auto v = load_vec(x + at);
+        const auto u = load_vec(a + at);
+#pragma unroll
+        for (int i = 0; i < Vec<E_>::N; ++i) pa += exp2_fast(((float)v[i] - m) * c) * (float)u[i];
+      },
+      [&](int64_t at) { pa += exp2_fast(((float)x[at] - m) * c) * (float)a[at]; });
+  return pa;
+}
+
+// The sum over the workgroup, the same in every lane.
+__device__ __forceinline__ float block_sum(float x, Reduce& R) {
+  x = wave_sum(x);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) R.s[threadIdx.x >> 6] = x;
+  __syncthreads();
+  x = 0.0f;
+  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) x += R.s[w];
+  return x;
 }
 
 template <class E_>
-__global__ __launch_bounds__(kDB) void distill_second(Rows r, const E_* dd, int64_t ddrow_stride, const float* ddteacher,
-                                                      const float* dloss, const float* stats, float* out_dloss,
-                                                      E_* out, int64_t out_stride, float* out_teacher) {
+__global__ __launch_bounds__(kDB) void distill_second_parts(Rows r, Second t, float* parts, int32_t slices, int64_t per) {
+  __shared__ Reduce R;
+  const Slice sl = slice_of(r, blockIdx.x, slices, per);
+  const float pa = block_sum(weighted(static_cast<const E_*>(r.logits) + sl.row * r.row_stride, static_cast<const E_*>(t.a) + sl.row * t.a_stride,
+                                      sl.c0, sl.c1, t.stats[2 * sl.row], r.invT * kLog2e), R);
+  if (threadIdx.x == 0) parts[blockIdx.x] = pa;
+}
+
+template <class E_, int STATS, int B = kDB, int NV = 1>
+__global__ __launch_bounds__(B) void distill_second(Rows r, Second t, const float* parts, int32_t slices, int64_t per) {
   __shared__ Entries E;
   __shared__ float aj[kMaxK], cj[kMaxK];
-  __shared__ float part[kDB / 64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ Reduce R;
+  const int lane = threadIdx.x & 63;
   const float c = r.invT * kLog2e;
-  for (int64_t row = blockIdx.x; row < r.N; row += gridDim.x) {
-    const E_* x = static_cast<const E_*>(r.logits) + row * r.row_stride;
-    const E_* a = dd ? dd + row * ddrow_stride : nullptr;
-    E_* y = out + row * out_stride;
-    const float m = stats[2 * row], s = stats[2 * row + 1], inv = 1.0f / s;
-    __syncthreads();
-    if (threadIdx.x < 64) {
-      teacher_softmax(r, row, E, lane);
-      gather(x, E, r.K, E.x, lane);
-      for (int j = lane; j < r.K; j += 64) {
-        aj[j] = a && E.id[j] >= 0 ? (float)a[E.id[j]] : 0.0f;
-        cj[j] = ddteacher && E.q[j] != 0.0f ? ddteacher[row * r.K + j] : 0.0f;
-      }
-    }
-    float pa = 0.0f;
-    if (a)
-      over_row(
-          x, r.V,
-          [&](int64_t at) {
-            const auto v = load_vec(x + at);
-            const auto u = load_vec(a + at);
-#pragma unroll
-            for (int i = 0; i < Vec<E_>::N; ++i) pa += exp2_fast(((float)v[i] - m) * c) * (float)u[i];
-          },
-          [&](int64_t at) { pa += exp2_fast(((float)x[at] - m) * c) * (float)a[at]; });
-    pa = wave_sum(pa);
-    if (lane == 0) part[wave] = pa;
-    __syncthreads();
-    pa = 0.0f;
-    for (int w = 0; w < kDB / 64; ++w) pa += part[w];
-    pa *= inv;
-    const bool some = E.some, bad = E.bad;
-    const float g = bad ? kNan : dloss[row];
-    if (threadIdx.x < 64) {
-      const float mean = entry_terms(r, E, m, s, lane);
-      float abar = 0.0f, cbar = 0.0f, cov = 0.0f;  // means of a and c, covariance of c and T l under q
-      for (int j = lane; j < r.K; j += 64) {
-        const float q = E.q[j];
-        if (q == 0.0f) continue;
-        abar += q * aj[j];
-        cbar += q * cj[j];
-      }
-      abar = wave_sum(abar);
-      cbar = wave_sum(cbar);
-      for (int j = lane; j < r.K; j += 64) cov += E.q[j] * (cj[j] - cbar) * (E.lq[j] - mean);
-      cov = wave_sum(cov);
-      if (out_dloss && lane == 0) out_dloss[row] = bad ? kNan : some ? r.T * (pa - abar) + cov : 0.0f;
-      for (int j = lane; j < r.K; j += 64) {
-        const float q = E.q[j], cc = cj[j], l = E.lq[j];
-        if (out_teacher)
-          out_teacher[row * r.K + j] =
-              q != 0.0f ? g * q * ((abar - aj[j]) + (cc - cbar) + r.invT * ((cc - cbar) * (l - mean) - cov))
-                        : bad ? kNan : 0.0f;
-        E.q[j] = q * (cc - cbar);  // what the entry takes from its token's element
-      }
-    }
-    const float w = some ? g * inv : 0.0f;
-    over_row(
-        x, r.V,
-        [&](int64_t at) {
-          float z[Vec<E_>::N];
-          if (a && some) {
-            const auto v = load_vec(x + at);
-            const auto u = load_vec(a + at);
-#pragma unroll
-            for (int i = 0; i < Vec<E_>::N; ++i) z[i] = w * exp2_fast(((float)v[i] - m) * c) * ((float)u[i] - pa);
-          } else {
-#pragma unroll
-            for (int i = 0; i < Vec<E_>::N; ++i) z[i] = 0.0f;
-          }
-          store_vec(y + at, z);
-        },
-        [&](int64_t at) {
-          y[at] = (E_)(a && some ? w * exp2_fast(((float)x[at] - m) * c) * ((float)a[at] - pa) : 0.0f);
-        });
-    __syncthreads();
-    for (int j = threadIdx.x; j < r.K; j += kDB)
-      if (E.id[j] >= 0) {
-        const float dense = a ? w * exp2_fast((E.x[j] - m) * c) * (aj[j] - pa) : 0.0f;
-        y[E.id[j]] = (E_)(dense - g * same_token(E.q, E, r.K, E.id[j]));
-      }
+  const Slice sl = slice_of(r, blockIdx.x, slices, per);
+  const int64_t row = sl.row;
+  const E_* x = static_cast<const E_*>(r.logits) + row * r.row_stride;
+  const E_* a = t.a ? static_cast<const E_*>(t.a) + row * t.a_stride : nullptr;
+  E_* y = static_cast<E_*>(t.out) + row * t.out_stride;
+  Kept<E_, B, NV> kx, ka;
+  if (STATS == kKept && a) {
+    kx.place(x, 0, r.V);
+    ka.place(x, 0, r.V);
+    kx.load(x);
+    ka.load(a);
   }
+  const float m = t.stats[2 * row], s = t.stats[2 * row + 1], inv = 1.0f / s;
+  if (threadIdx.x < 64) {
+    teacher_softmax(r, row, E, lane);
+    gather(x, E, r.K, E.x, lane);
+    for (int j = lane; j < r.K; j += 64) {
+      aj[j] = a && E.id[j] >= 0 ? (float)a[E.id[j]] : 0.0f;
+      cj[j] = t.c && E.q[j] != 0.0f ? t.c[row * r.K + j] : 0.0f;
+    }
+  }
+  float pa = 0.0f;
+  if (STATS == kKept && a) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (kx.has(i)) {
+#pragma unroll
+        for (int k = 0; k < Vec<E_>::N; ++k) pa += exp2_fast(((float)kx.v[i][k] - m) * c) * (float)ka.v[i][k];
+      }
+    if (kx.has_single) pa += exp2_fast(((float)kx.single - m) * c) * (float)ka.single;
+  } else if (STATS == kRead && a) {
+    pa = weighted(x, a, 0, r.V, m, c);
+  } else if (STATS == kParts && a) {
+    for (int i = threadIdx.x; i < slices; i += blockDim.x) pa += parts[row * slices + i];
+  }
+  pa = block_sum(pa, R) * inv;
+  const bool some = E.some, bad = E.bad;
+  const float g = bad ? kNan : t.dloss[row];
+  if (threadIdx.x < 64) {
+    const float mean = entry_terms(r, E, m, s, lane);
+    float abar = 0.0f, cbar = 0.0f, cov = 0.0f;  // means of a and c, covariance of c and T l under q
+    for (int j = lane; j < r.K; j += 64) {
+      const float q = E.q[j];
+      if (q == 0.0f) continue;
+      abar += q * aj[j];
+      cbar += q * cj[j];
+    }
+    abar = wave_sum(abar);
+    cbar = wave_sum(cbar);
+    for (int j = lane; j < r.K; j += 64) cov += E.q[j] * (cj[j] - cbar) * (E.lq[j] - mean);
+    cov = wave_sum(cov);
+    if (t.out_dloss && sl.index == 0 && lane == 0) t.out_dloss[row] = bad ? kNan : some ? r.T * (pa - abar) + cov : 0.0f;
+    for (int j = lane; j < r.K; j += 64) {
+      const float q = E.q[j], cc = cj[j], l = E.lq[j];
+      if (t.out_teacher && sl.index == 0)
+        t.out_teacher[row * r.K + j] =
+            q != 0.0f ? g * q * ((abar - aj[j]) + (cc - cbar) + r.invT * ((cc - cbar) * (l - mean) - cov)) : bad ? kNan : 0.0f;
+      E.q[j] = q * (cc - cbar);  // what the entry takes from its token's element
+    }
+  }
+  const float w = some ? g * inv : 0.0f;
+  const bool dense = a && some;
+  auto piece = [&](int64_t at, typename Vec<E_>::type v, typename Vec<E_>::type u) {
+    float z[Vec<E_>::N];
+#pragma unroll
+    for (int i = 0; i < Vec<E_>::N; ++i) z[i] = dense ? w * exp2_fast(((float)v[i] - m) * c) * ((float)u[i] - pa) : 0.0f;
+    store_vec(y + at, z);
+  };
+  auto one = [&](int64_t at, float v, float u) { y[at] = (E_)(dense ? w * exp2_fast((v - m) * c) * (u - pa) : 0.0f); };
+  if (STATS == kKept && a) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (kx.has(i)) piece(kx.at(i), kx.v[i], ka.v[i]);
+    if (kx.has_single) one(kx.at_single, (float)kx.single, (float)ka.single);
+  } else {
+    const E_* b = a ? a : x;
+    over_row(x, sl.c0, sl.c1, [&](int64_t at) { piece(at, load_vec(x + at), load_vec(b + at)); },
+             [&](int64_t at) { one(at, (float)x[at], (float)b[at]); });
+  }
+  __syncthreads();
+  for (int j = threadIdx.x; j < r.K; j += blockDim.x)
+    if (E.id[j] >= sl.c0 && E.id[j] < sl.c1) {
+      const float d = a ? w * exp2_fast((E.x[j] - m) * c) * (aj[j] - pa) : 0.0f;
+      y[E.id[j]] = (E_)(d - g * same_token(E.q, E, r.K, E.id[j]));
+    }
 }
 
 // ---- host -------------------------------------------------------------------
@@ -334,7 +491,8 @@ __global__ __launch_bounds__(kDB) void distill_second(Rows r, const E_* dd, int6
 int check_rows(const char* who, const void* logits, int64_t row_stride, int64_t N, int64_t V, int32_t dtype,
                const void* ids, int32_t id_bytes, const float* teacher, int64_t K, double temperature, Rows* r) {
   if (N < 0) return fail(DIFFOPT_EINVAL, "%s: N must be >= 0", who);
-  if (V < 1) return fail(DIFFOPT_EINVAL, "%s: V must be >= 1", who);
+  if (N > 0x7fffffff) return fail(DIFFOPT_EINVAL, "%s: N must be below 2^31", who);
+  if (V < 1 || V > 0x7fffffff) return fail(DIFFOPT_EINVAL, "%s: V must be in [1, 2^31)", who);
   if (!dtype_ok(dtype)) return fail(DIFFOPT_EINVAL, "%s: unknown element type %d", who, (int)dtype);
   if (id_bytes != 4 && id_bytes != 8) return fail(DIFFOPT_EINVAL, "%s: id_bytes must be 4 or 8", who);
   if (K < 1 || K > kMaxK) return fail(DIFFOPT_EINVAL, "%s: K must be in [1, %d]", who, kMaxK);
@@ -362,18 +520,111 @@ int check_out_rows(const char* who, const void* out, int64_t stride, int64_t V, 
   return DIFFOPT_OK;
 }
 
-dim3 row_grid(int64_t N) { return dim3((unsigned)(N < 0x7fffffff ? N : 0x7fffffff)); }
+// Workgroups of a row: with fewer rows than kFewRows each is cut into slices of
+// at least kSliceBytes until kFillRows workgroups run.
+constexpr int64_t kFewRows = 256, kFillRows = 1024, kSliceBytes = 8192;
 
-template <bool FWD, bool BWD>
-int launch_rows(const char* who, const Rows& r, int32_t dtype, const float* dloss, float* loss, float* stats,
-                void* dlogits, int64_t drow_stride, float* dteacher, hipStream_t st) {
-  if (dtype == DIFFOPT_F32)
-    hipLaunchKernelGGL((distill_row<float, FWD, BWD>), row_grid(r.N), dim3(kDB), 0, st, r, dloss, loss, stats,
-                       static_cast<float*>(dlogits), drow_stride, dteacher);
-  else
-    hipLaunchKernelGGL((distill_row<bf16, FWD, BWD>), row_grid(r.N), dim3(kDB), 0, st, r, dloss, loss, stats,
-                       static_cast<bf16*>(dlogits), drow_stride, dteacher);
+struct Cut {
+  int32_t slices;
+  int64_t per;
+};
+
+Cut cut_of(int64_t N, int64_t V, int32_t dtype) {
+  if (N >= kFewRows || N == 0) return Cut{1, V};
+  int64_t n = kFillRows / N;
+  const int64_t most = V * elem_size(dtype) / kSliceBytes;
+  n = n > most ? most : n;
+  if (n < 2) return Cut{1, V};
+  int64_t per = (V + n - 1) / n;
+  per = (per + 63) / 64 * 64;
+  return Cut{(int32_t)((V + per - 1) / per), per};
+}
+
+#define DIFFOPT_LAUNCH(kernel, grid, block, ...) hipLaunchKernelGGL((kernel), dim3((unsigned)(grid)), dim3(block), 0, st, __VA_ARGS__)
+
+template <class E_>
+int fwd_rows(const char* who, const Rows& r, int32_t dtype, float* loss, float* stats, float* parts, hipStream_t st) {
+  const Cut c = cut_of(r.N, r.V, dtype);
+  E_* none = nullptr;
+  if (c.slices > 1) {
+    DIFFOPT_LAUNCH(distill_parts<E_>, r.N * c.slices, kDB, r, parts, c.slices, c.per);
+    DIFFOPT_LAUNCH((distill_row<E_, kParts, false, 64>), r.N, 64, r, nullptr, loss, stats, none, 0, nullptr, parts, c.slices, c.per);
+  } else {
+    DIFFOPT_LAUNCH((distill_row<E_, kRead, false>), r.N, kDB, r, nullptr, loss, stats, none, 0, nullptr, nullptr, 1, r.V);
+  }
   return launch_status(who);
+}
+
+template <class E_>
+int bwd_rows(const char* who, const Rows& r, int32_t dtype, const float* dloss, const float* stats, void* dx, int64_t dstride, float* dt,
+             hipStream_t st) {
+  // over the logits in place, a row's workgroups would overwrite one another's entries
+  const Cut c = dx == r.logits ? Cut{1, r.V} : cut_of(r.N, r.V, dtype);
+  DIFFOPT_LAUNCH((distill_row<E_, kGiven, true>), r.N * c.slices, kDB, r, dloss, nullptr, const_cast<float*>(stats), static_cast<E_*>(dx), dstride,
+                 dt, nullptr, c.slices, c.per);
+  return launch_status(who);
+}
+
+template <class E_>
+int both_rows(const char* who, const Rows& r, int32_t dtype, const float* dloss, float* loss, float* stats, void* dlogits, int64_t dstride,
+              float* dt, float* parts, hipStream_t st) {
+  const Cut c = cut_of(r.N, r.V, dtype);
+  E_* dx = static_cast<E_*>(dlogits);
+  if (c.slices > 1) {
+    DIFFOPT_LAUNCH(distill_parts<E_>, r.N * c.slices, kDB, r, parts, c.slices, c.per);
+    DIFFOPT_LAUNCH((distill_row<E_, kParts, true>), r.N * c.slices, kDB, r, dloss, loss, stats, dx, dstride, dt, parts, c.slices, c.per);
+    return launch_status(who);
+  }
+  const int64_t bytes = r.V * elem_size(dtype);
+#define DIFFOPT_KEPT(B, NV)                                                                                                       \
+  if (bytes <= (int64_t)B * NV * 16) {                                                                                            \
+    DIFFOPT_LAUNCH((distill_row<E_, kKept, true, B, NV>), r.N, B, r, dloss, loss, stats, dx, dstride, dt, nullptr, 1, r.V);       \
+    return launch_status(who);                                                                                                    \
+  }
+  DIFFOPT_KEPT(256, 2)
+  DIFFOPT_KEPT(256, 4)
+  DIFFOPT_KEPT(256, 8)
+  DIFFOPT_KEPT(512, 8)
+  DIFFOPT_KEPT(512, 13)
+  DIFFOPT_KEPT(512, 16)
+  DIFFOPT_KEPT(1024, 16)
+  DIFFOPT_KEPT(1024, 32)
+#undef DIFFOPT_KEPT
+  DIFFOPT_LAUNCH((distill_row<E_, kRead, true>), r.N, kDB, r, dloss, loss, stats, dx, dstride, dt, nullptr, 1, r.V);
+  return launch_status(who);
+}
+
+template <class E_>
+int second_rows(const char* who, const Rows& r, int32_t dtype, const Second& t, float* parts, hipStream_t st) {
+  const Cut c = cut_of(r.N, r.V, dtype);
+  if (c.slices > 1) {
+    if (t.a) DIFFOPT_LAUNCH(distill_second_parts<E_>, r.N * c.slices, kDB, r, t, parts, c.slices, c.per);
+    DIFFOPT_LAUNCH((distill_second<E_, kParts>), r.N * c.slices, kDB, r, t, parts, c.slices, c.per);
+    return launch_status(who);
+  }
+  const int64_t bytes = r.V * elem_size(dtype);
+#define DIFFOPT_KEPT(B, NV)                                                                  \
+  if (bytes <= (int64_t)B * NV * 16) {                                                       \
+    DIFFOPT_LAUNCH((distill_second<E_, kKept, B, NV>), r.N, B, r, t, nullptr, 1, r.V);       \
+    return launch_status(who);                                                               \
+  }
+  DIFFOPT_KEPT(256, 4)
+  DIFFOPT_KEPT(512, 4)
+  DIFFOPT_KEPT(512, 8)
+  DIFFOPT_KEPT(1024, 8)
+  DIFFOPT_KEPT(1024, 16)
+#undef DIFFOPT_KEPT
+  DIFFOPT_LAUNCH((distill_second<E_, kRead>), r.N, kDB, r, t, nullptr, 1, r.V);
+  return launch_status(who);
+}
+
+int check_workspace(const char* who, const Rows& r, int32_t dtype, void* workspace, int64_t bytes) {
+  const Cut c = cut_of(r.N, r.V, dtype);
+  const int64_t need = c.slices > 1 ? r.N * c.slices * 8 : 0;
+  if (need > 0 && (!workspace || bytes < need))
+    return fail(DIFFOPT_EINVAL, "%s: the workspace has %lld bytes of %lld", who, (long long)(workspace ? bytes : 0), (long long)need);
+  if (!aligned_to(workspace, 4)) return fail(DIFFOPT_EINVAL, "%s: the workspace is not 4-byte aligned", who);
+  return DIFFOPT_OK;
 }
 
 }  // namespace
@@ -382,8 +633,9 @@ int launch_rows(const char* who, const Rows& r, int32_t dtype, const float* dlos
 using namespace diffopt;
 
 extern "C" int64_t diffopt_distill_workspace(int64_t N, int64_t V, int32_t dtype, int64_t K) {
-  if (N < 0 || V < 1 || !dtype_ok(dtype) || K < 1 || K > kMaxK) return -1;
-  return 0;
+  if (N < 0 || N > 0x7fffffff || V < 1 || V > 0x7fffffff || !dtype_ok(dtype) || K < 1 || K > kMaxK) return -1;
+  const Cut c = cut_of(N, V, dtype);
+  return c.slices > 1 ? N * c.slices * 8 : 0;
 }
 
 extern "C" int diffopt_distill_fwd(const void* logits, int64_t row_stride, int64_t N, int64_t V, int32_t dtype,
@@ -398,9 +650,11 @@ extern "C" int diffopt_distill_fwd(const void* logits, int64_t row_stride, int64
   if (!loss || !stats) return fail(DIFFOPT_EINVAL, "%s: null required pointer", who);
   rc = check_aligned(who, {loss, stats});
   if (rc) return rc;
-  (void)workspace;
-  (void)workspace_bytes;
-  return launch_rows<true, false>(who, r, dtype, nullptr, loss, stats, nullptr, 0, nullptr, as_stream(stream));
+  rc = check_workspace(who, r, dtype, workspace, workspace_bytes);
+  if (rc) return rc;
+  float* parts = static_cast<float*>(workspace);
+  return dtype == DIFFOPT_F32 ? fwd_rows<float>(who, r, dtype, loss, stats, parts, as_stream(stream))
+                              : fwd_rows<bf16>(who, r, dtype, loss, stats, parts, as_stream(stream));
 }
 
 extern "C" int diffopt_distill_bwd(const float* dloss, const void* logits, int64_t row_stride, int64_t N, int64_t V,
@@ -416,8 +670,8 @@ extern "C" int diffopt_distill_bwd(const float* dloss, const void* logits, int64
   rc = check_aligned(who, {dloss, stats, dteacher});
   if (!rc) rc = check_out_rows(who, dlogits, drow_stride, V, N, dtype);
   if (rc) return rc;
-  return launch_rows<false, true>(who, r, dtype, dloss, nullptr, const_cast<float*>(stats), dlogits, drow_stride,
-                                  dteacher, as_stream(stream));
+  return dtype == DIFFOPT_F32 ? bwd_rows<float>(who, r, dtype, dloss, stats, dlogits, drow_stride, dteacher, as_stream(stream))
+                              : bwd_rows<bf16>(who, r, dtype, dloss, stats, dlogits, drow_stride, dteacher, as_stream(stream));
 }
 
 extern "C" int diffopt_distill_fwd_bwd(const float* dloss, const void* logits, int64_t row_stride, int64_t N, int64_t V,
@@ -435,9 +689,12 @@ extern "C" int diffopt_distill_fwd_bwd(const float* dloss, const void* logits, i
   if (!rc) rc = check_out_rows(who, dlogits, drow_stride, V, N, dtype);
   if (rc) return rc;
   if (dlogits == logits) return fail(DIFFOPT_EINVAL, "%s: dlogits must not be logits", who);
-  (void)workspace;
-  (void)workspace_bytes;
-  return launch_rows<true, true>(who, r, dtype, dloss, loss, stats, dlogits, drow_stride, dteacher, as_stream(stream));
+  rc = check_workspace(who, r, dtype, workspace, workspace_bytes);
+  if (rc) return rc;
+  float* parts = static_cast<float*>(workspace);
+  return dtype == DIFFOPT_F32
+             ? both_rows<float>(who, r, dtype, dloss, loss, stats, dlogits, drow_stride, dteacher, parts, as_stream(stream))
+             : both_rows<bf16>(who, r, dtype, dloss, loss, stats, dlogits, drow_stride, dteacher, parts, as_stream(stream));
 }
 
 extern "C" int diffopt_distill_bwd_bwd(const void* ddlogits, int64_t ddrow_stride, const float* ddteacher,
@@ -459,16 +716,10 @@ extern "C" int diffopt_distill_bwd_bwd(const void* ddlogits, int64_t ddrow_strid
   if (rc) return rc;
   if (out_logits == logits || out_logits == ddlogits)
     return fail(DIFFOPT_EINVAL, "%s: out_logits must be neither logits nor ddlogits", who);
-  (void)workspace;
-  (void)workspace_bytes;
-  hipStream_t st = as_stream(stream);
-  if (dtype == DIFFOPT_F32)
-    hipLaunchKernelGGL((distill_second<float>), row_grid(N), dim3(kDB), 0, st, r, static_cast<const float*>(ddlogits),
-                       ddrow_stride, ddteacher, dloss, stats, out_dloss, static_cast<float*>(out_logits),
-                       out_row_stride, out_teacher);
-  else
-    hipLaunchKernelGGL((distill_second<bf16>), row_grid(N), dim3(kDB), 0, st, r, static_cast<const bf16*>(ddlogits),
-                       ddrow_stride, ddteacher, dloss, stats, out_dloss, static_cast<bf16*>(out_logits),
-                       out_row_stride, out_teacher);
-  return launch_status(who);
+  rc = check_workspace(who, r, dtype, workspace, workspace_bytes);
+  if (rc) return rc;
+  const Second t{ddlogits, ddrow_stride, ddteacher, dloss, stats, out_dloss, out_teacher, out_logits, out_row_stride};
+  float* parts = static_cast<float*>(workspace);
+  return dtype == DIFFOPT_F32 ? second_rows<float>(who, r, dtype, t, parts, as_stream(stream))
+                              : second_rows<bf16>(who, r, dtype, t, parts, as_stream(stream));
 }

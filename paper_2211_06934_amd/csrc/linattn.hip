@@ -130,6 +130,79 @@ __global__ __launch_bounds__(kTokenB) void linattn_tokens(Shape s, Scan a, int32
   }
 }
 
+// One token: the state is read and written once, which is nearly all there is
+// to move, in 16-byte pieces.  A workgroup takes 4 CG columns of one state and
+// all its rows; a lane holds 4 columns of R rows, so that every load of a call
+// is in flight at once and the product with q is joined over lanes and waves.
+// Few columns a workgroup (32) put a single sequence's states on many compute
+// units; whole lines of 128 bytes a row are enough for the memory as well.
+constexpr int kStepB = 256, kStepCG = 8, kStepGroup = 8;
+
+template <class E, int R>
+__global__ __launch_bounds__(kStepB) void linattn_one(Shape s, Scan a, int32_t col_tiles) {
+  constexpr int RG = kStepB / kStepCG;  // row groups of a workgroup
+  __shared__ float part[kStepB / 64][kStepGroup][4 * kStepCG];
+  const int cg = threadIdx.x % kStepCG, rg = threadIdx.x / kStepCG, wave = threadIdx.x >> 6;
+  const int64_t state = blockIdx.x / (uint32_t)col_tiles;
+  const int64_t b = state / s.Hs;
+  const int j = (int)(state - b * s.Hs), c0 = ((int)(blockIdx.x % (uint32_t)col_tiles) * kStepCG + cg) * 4;
+  const bool in = c0 < a.Dv;
+  const float* s0 = a.s0 + state * a.Dk * a.Dv + (in ? c0 : 0);
+  f32x4 S[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int r = rg + i * RG;
+    S[i] = r < a.Dk ? *reinterpret_cast<const f32x4*>(s0 + r * a.Dv) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  const E *k = at<E>(a.k, b, 0, j), *v = at<E>(a.v, b, 0, j);
+  float kk[R];
+  f32x4 vv;
+#pragma unroll
+  for (int i = 0; i < R; ++i) kk[i] = rg + i * RG < a.Dk ? (float)k[rg + i * RG] : 0.0f;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) vv[c] = in ? (float)v[c0 + c] : 0.0f;
+  // the decay to 48 bits: one rounding of it would grow with every token
+  const double gd = exp((double)s.log_decay[j]);
+  const float g = (float)gd, g_lo = (float)(gd - (double)g);
+  float* s1 = a.s1 + state * a.Dk * a.Dv + c0;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) S[i][c] = fmaf(S[i][c], g, fmaf(S[i][c], g_lo, kk[i] * vv[c]));
+    const int r = rg + i * RG;
+    if (in && r < a.Dk) *reinterpret_cast<f32x4*>(s1 + r * a.Dv) = S[i];
+  }
+  for (int h0 = 0; h0 < a.nq; h0 += kStepGroup) {
+    const int n = a.nq - h0 < kStepGroup ? a.nq - h0 : kStepGroup;
+    for (int h = 0; h < n; ++h) {
+      const E* q = at<E>(a.q, b, 0, (int64_t)j * a.nq + h0 + h);
+      f32x4 o{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const float qq = rg + i * RG < a.Dk ? (float)q[rg + i * RG] : 0.0f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] = fmaf(qq, S[i][c], o[c]);
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int m = kStepCG; m < 64; m <<= 1) o[c] += __shfl_xor(o[c], m, 64);
+      if ((threadIdx.x & 63) < kStepCG)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) part[wave][h][4 * cg + c] = o[c];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n * 4 * kStepCG; i += kStepB) {
+      const int h = i / (4 * kStepCG), c = i % (4 * kStepCG), col = c0 - 4 * cg + c;
+      float o = part[0][h][c];
+#pragma unroll
+      for (int w = 1; w < kStepB / 64; ++w) o += part[w][h][c];
+      if (col < a.Dv) at<E>(a.o, b, 0, (int64_t)j * a.nq + h0 + h)[col] = (E)(o * a.qs);
+    }
+    __syncthreads();
+  }
+}
+
 // ---- chunks -----------------------------------------------------------------
 // C tokens at a time, all as matrix products.  With t, s counted inside a chunk
 // of L <= C tokens and S the state before it,
@@ -666,6 +739,20 @@ void launch_tokens(const Shape& s, const Scan& a, hipStream_t st) {
     hipLaunchKernelGGL((linattn_tokens<E, 16>), grid, block, 0, st, s, a, tiles);
 }
 
+template <class E>
+void launch_one(const Shape& s, const Scan& a, hipStream_t st) {
+  const int tiles = (a.Dv + 4 * kStepCG - 1) / (4 * kStepCG);
+  const dim3 grid((unsigned)(s.B * s.Hs * tiles)), block(kStepB);
+  if (a.Dk <= 32)
+    hipLaunchKernelGGL((linattn_one<E, 1>), grid, block, 0, st, s, a, tiles);
+  else if (a.Dk <= 64)
+    hipLaunchKernelGGL((linattn_one<E, 2>), grid, block, 0, st, s, a, tiles);
+  else if (a.Dk <= 128)
+    hipLaunchKernelGGL((linattn_one<E, 4>), grid, block, 0, st, s, a, tiles);
+  else
+    hipLaunchKernelGGL((linattn_one<E, 8>), grid, block, 0, st, s, a, tiles);
+}
+
 // Which chunk kernel a scan takes: key rows, column tiles of a wave.
 struct Class {
   int dk, nct;
@@ -973,6 +1060,12 @@ extern "C" int diffopt_linattn_step(const diffopt_heads* q, const diffopt_heads*
   a[0].s1 = state;
   a[0].qs = (float)scale;
   a[0].ks = 1.0f;
-  const bool run[1] = {true};
-  return run_scans(who, Shape{B, 1, (int32_t)Hk, log_decay, nullptr}, a, run, 1, dtype, nullptr, 0, as_stream(stream));
+  const Shape s{B, 1, (int32_t)Hk, log_decay, nullptr};
+  hipStream_t st = as_stream(stream);
+  const bool pieces = Dv % 4 == 0 && aligned_to(state, 16);  // rows of whole 16-byte pieces
+  if (dtype == DIFFOPT_F32)
+    pieces ? launch_one<float>(s, a[0], st) : launch_tokens<float>(s, a[0], st);
+  else
+    pieces ? launch_one<bf16>(s, a[0], st) : launch_tokens<bf16>(s, a[0], st);
+  return launch_status(who);
 }
