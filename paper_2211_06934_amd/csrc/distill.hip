@@ -6,11 +6,12 @@
 // max (a lane rescales its sum once per 16 bytes); wave 0 forms the teacher's
 // softmax over the K entries meanwhile.  The gradient's dense part g T p takes
 // the row again: where the same call has just read it, from registers (rows of
-// up to 512 KiB), else from memory.  The K entries are then written once more
+// up to 256 KiB), else from memory.  The K entries are then written once more
 // by the same workgroup after a barrier, each with the sum of q over the entries
 // of its token, so nothing is added atomically and equal ids need no order.
 // A few exponentials per element: bound by memory.
 #include <initializer_list>
+#include <type_traits>
 
 #include "lm_common.hpp"
 
@@ -45,6 +46,20 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 
 // (x - m) / T in units of log 2; a row of -inf alone keeps m = -inf, s = 0.
 __device__ __forceinline__ float safe_max(float m) { return m == -kInf ? 0.0f : m; }
+
+// exp((x - b) / T) for many x and one b: 2^(x c - b c) by one multiply-add, with
+// what the rounding of b c leaves out as a factor of its own.  Where b c
+// overflows, `wide` takes the difference first.
+struct Shift {
+  float b, c, bc;
+  bool wide;
+  __device__ __forceinline__ Shift(float b_, float c_) : b(b_), c(c_), bc(b_ * c_), wide(!(__builtin_fabsf(bc) < 1e30f)) {}
+  __device__ __forceinline__ float factor() const { return wide ? 1.0f : exp2_fast(-__builtin_fmaf(b, c, -bc)); }
+  template <bool WIDE>
+  __device__ __forceinline__ float part(float x) const {
+    return exp2_fast(WIDE ? (x - b) * c : __builtin_fmaf(x, c, -bc));
+  }
+};
 
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2, float c) {
   const float M = fmaxf(m, m2), b = safe_max(M);
@@ -189,31 +204,55 @@ __device__ __forceinline__ void row_stats(const E_* x, int64_t c0, int64_t c1, f
       [&](int64_t at) { run.one((float)x[at], c); });
 }
 
-// Elements [c0, c1) of a row in registers: NV pieces of every lane of a
-// workgroup of B, and one of the elements around them.
+// A row in registers: NV pieces of every lane of a workgroup of B, and one of
+// the elements around them.  Where the pieces lie goes by one array's alignment,
+// another array's are taken at the same elements.  Offsets are 32 bits from the
+// row, which a wave's registers hold once.
 template <class E_, int B, int NV>
 struct Kept {
   static constexpr int N = Vec<E_>::N;
-  typename Vec<E_>::type v[NV];
+  uint32_t v[NV][4];  // the pieces as memory holds them
   E_ single;
-  int64_t first, nv, at_single;
+  uint32_t first, nv, at_single;
   bool has_single;
 
-  // where the pieces lie goes by x; another array's are taken at the same elements
-  __device__ __forceinline__ void place(const E_* x, int64_t c0, int64_t c1) {
-    const int64_t n = c1 - c0, head = head_of(x + c0, n), rest = n - (n - head) / N * N;
+  __device__ __forceinline__ void place(const E_* x, uint32_t n) {
+    const uint32_t head = (uint32_t)head_of(x, n), rest = n - (n - head) / N * N;
     nv = (n - head) / N;
-    first = c0 + head;
-    has_single = (int64_t)threadIdx.x < rest;
-    at_single = c0 + ((int64_t)threadIdx.x < head ? (int64_t)threadIdx.x : threadIdx.x + nv * N);
+    first = head + threadIdx.x * N;
+    has_single = threadIdx.x < rest;
+    at_single = threadIdx.x < head ? threadIdx.x : threadIdx.x + nv * N;
   }
   __device__ __forceinline__ bool has(int i) const { return threadIdx.x + i * B < nv; }
-  __device__ __forceinline__ int64_t at(int i) const { return first + (int64_t)(threadIdx.x + i * B) * N; }
-  __device__ __forceinline__ void load(const E_* x) {
+  __device__ __forceinline__ uint32_t at(int i) const { return first + i * (B * N); }
+  // pieces that are not there hold `none`
+  __device__ __forceinline__ void load(const E_* x, E_ none) {
+    typename Vec<E_>::type fill;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (has(i)) v[i] = load_vec(x + at(i));
+    for (int k = 0; k < N; ++k) fill[k] = none;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      typename Vec<E_>::type y = fill;
+      if (has(i)) y = load_vec(x + at(i));
+      __builtin_memcpy(v[i], &y, 16);
+    }
+    single = none;
     if (has_single) single = x[at_single];
+  }
+  // A piece's values.  The compiler would keep what one pass unpacked for the
+  // next, twice the registers of the row itself: it is made to unpack anew.
+  __device__ __forceinline__ void get(int i, float* e) const {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint32_t x = v[i][k];
+      asm volatile("" : "+v"(x));
+      if constexpr (sizeof(E_) == 2) {
+        e[2 * k] = __builtin_bit_cast(float, x << 16);
+        e[2 * k + 1] = __builtin_bit_cast(float, x & 0xffff0000u);
+      } else {
+        e[k] = __builtin_bit_cast(float, x);
+      }
+    }
   }
 };
 
@@ -260,6 +299,12 @@ __device__ __forceinline__ float same_token(const float* w, const Entries& E, in
   return sum;
 }
 
+// Waves of a SIMD that the compiler has to leave room for where rows stay in
+// registers: rows of 104 KiB at three workgroups a compute unit (80 registers, 52
+// of them the row's) took 175 us for 4096 rows of 50,021 bf16 logits, at two 186,
+// at four (with spills) 199; elsewhere its own choice is as good.
+constexpr int kept_waves(int B, int NV) { return B == 512 && NV == 13 ? 6 : 1; }
+
 // Where a row's max and sum come from.
 enum Stats {
   kGiven,  // the caller
@@ -269,7 +314,7 @@ enum Stats {
 };
 
 template <class E_, int STATS, bool BWD, int B = kDB, int NV = 1>
-__global__ __launch_bounds__(B) void distill_row(Rows r, const float* dloss, float* loss, float* stats, E_* dlogits, int64_t drow_stride,
+__global__ __launch_bounds__(B, (STATS == kKept ? kept_waves(B, NV) : 1)) void distill_row(Rows r, const float* dloss, float* loss, float* stats, E_* dlogits, int64_t drow_stride,
                                                  float* dteacher, const float* parts, int32_t slices, int64_t per) {
   constexpr bool FWD = STATS != kGiven;
   __shared__ Entries E;
@@ -281,8 +326,8 @@ __global__ __launch_bounds__(B) void distill_row(Rows r, const float* dloss, flo
   const E_* x = static_cast<const E_*>(r.logits) + row * r.row_stride;
   Kept<E_, B, NV> kept;
   if (STATS == kKept) {
-    kept.place(x, 0, r.V);
-    kept.load(x);
+    kept.place(x, (uint32_t)r.V);
+    kept.load(x, (E_)-kInf);
   }
   if (threadIdx.x < 64) {
     teacher_softmax(r, row, E, lane);
@@ -291,15 +336,32 @@ __global__ __launch_bounds__(B) void distill_row(Rows r, const float* dloss, flo
   Running run;
   if (STATS == kRead) row_stats(x, 0, r.V, c, run);
   if (STATS == kKept) {
+    constexpr int N = Vec<E_>::N;
+    float top = (float)kept.single;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (kept.has(i)) {
-        float e[Vec<E_>::N];
+    for (int i = 0; i < NV; ++i) {
+      float e[N];
+      kept.get(i, e);
 #pragma unroll
-        for (int k = 0; k < Vec<E_>::N; ++k) e[k] = (float)kept.v[i][k];
-        run.template piece<Vec<E_>::N>(e, c);
+      for (int k = 0; k < N; k += 2) top = fmaxf(fmaxf(top, e[k]), e[k + 1]);
+    }
+    run.m = top;
+    const Shift sh(safe_max(top), c);
+    auto sum = [&](auto wide) {
+      run.s = sh.part<wide.value>((float)kept.single);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        float e[N];
+        kept.get(i, e);
+#pragma unroll
+        for (int k = 0; k < N; ++k) run.s += sh.part<wide.value>(e[k]);
       }
-    if (kept.has_single) run.one((float)kept.single, c);
+      run.s *= sh.factor();
+    };
+    if (__any(sh.wide))
+      sum(std::true_type{});
+    else
+      sum(std::false_type{});
   }
   if (STATS == kRead || STATS == kKept) run.all(R, c);
   if (STATS == kParts) join_parts(parts, row, slices, c, run, R);
@@ -324,20 +386,43 @@ __global__ __launch_bounds__(B) void distill_row(Rows r, const float* dloss, flo
   if (!BWD) return;
   E_* dx = dlogits + row * drow_stride;
   const float w = some ? gT / s : 0.0f;
-  auto piece = [&](int64_t at, typename Vec<E_>::type v) {
+  auto piece = [&](int64_t at, const float* e) {
     float y[Vec<E_>::N];
 #pragma unroll
-    for (int i = 0; i < Vec<E_>::N; ++i) y[i] = some ? w * exp2_fast(((float)v[i] - m) * c) : 0.0f;
+    for (int i = 0; i < Vec<E_>::N; ++i) y[i] = some ? w * exp2_fast((e[i] - m) * c) : 0.0f;
     store_vec(dx + at, y);
   };
   auto one = [&](int64_t at, float e) { dx[at] = (E_)(some ? w * exp2_fast((e - m) * c) : 0.0f); };
   if (STATS == kKept) {
+    const Shift sh(m, c);
+    const float f = w * sh.factor();
+    auto write = [&](auto value) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (kept.has(i)) piece(kept.at(i), kept.v[i]);
-    if (kept.has_single) one(kept.at_single, (float)kept.single);
+      for (int i = 0; i < NV; ++i)
+        if (kept.has(i)) {
+          float e[Vec<E_>::N];
+          kept.get(i, e);
+#pragma unroll
+          for (int k = 0; k < Vec<E_>::N; ++k) e[k] = value(e[k]);
+          store_vec(dx + kept.at(i), e);
+        }
+      if (kept.has_single) dx[kept.at_single] = (E_)value((float)kept.single);
+    };
+    if (!some)
+      write([](float) { return 0.0f; });
+    else if (sh.wide)
+      write([&](float e) { return f * sh.part<true>(e); });
+    else
+      write([&](float e) { return f * sh.part<false>(e); });
   } else {
-    over_row(x, sl.c0, sl.c1, [&](int64_t at) { piece(at, load_vec(x + at)); }, [&](int64_t at) { one(at, (float)x[at]); });
+    over_row(
+        x, sl.c0, sl.c1,
+        [&](int64_t at) {
+          float e[Vec<E_>::N];
+          load_floats(x + at, e);
+          piece(at, e);
+        },
+        [&](int64_t at) { one(at, (float)x[at]); });
   }
   __syncthreads();  // the entries' elements are written after the dense part's
   for (int j = threadIdx.x; j < r.K; j += blockDim.x)
@@ -406,10 +491,10 @@ __global__ __launch_bounds__(B) void distill_second(Rows r, Second t, const floa
   E_* y = static_cast<E_*>(t.out) + row * t.out_stride;
   Kept<E_, B, NV> kx, ka;
   if (STATS == kKept && a) {
-    kx.place(x, 0, r.V);
-    ka.place(x, 0, r.V);
-    kx.load(x);
-    ka.load(a);
+    kx.place(x, (uint32_t)r.V);
+    ka.place(x, (uint32_t)r.V);
+    kx.load(x, (E_)-kInf);
+    ka.load(a, (E_)0.0f);
   }
   const float m = t.stats[2 * row], s = t.stats[2 * row + 1], inv = 1.0f / s;
   if (threadIdx.x < 64) {
@@ -421,14 +506,24 @@ __global__ __launch_bounds__(B) void distill_second(Rows r, Second t, const floa
     }
   }
   float pa = 0.0f;
+  const Shift sh(m, c);
   if (STATS == kKept && a) {
+    auto sum = [&](auto wide) {
+      pa = sh.part<wide.value>((float)kx.single) * (float)ka.single;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (kx.has(i)) {
+      for (int i = 0; i < NV; ++i) {
+        float e[Vec<E_>::N], u[Vec<E_>::N];
+        kx.get(i, e);
+        ka.get(i, u);
 #pragma unroll
-        for (int k = 0; k < Vec<E_>::N; ++k) pa += exp2_fast(((float)kx.v[i][k] - m) * c) * (float)ka.v[i][k];
+        for (int k = 0; k < Vec<E_>::N; ++k) pa += sh.part<wide.value>(e[k]) * u[k];
       }
-    if (kx.has_single) pa += exp2_fast(((float)kx.single - m) * c) * (float)ka.single;
+      pa *= sh.factor();
+    };
+    if (sh.wide)
+      sum(std::true_type{});
+    else
+      sum(std::false_type{});
   } else if (STATS == kRead && a) {
     pa = weighted(x, a, 0, r.V, m, c);
   } else if (STATS == kParts && a) {
@@ -461,22 +556,45 @@ __global__ __launch_bounds__(B) void distill_second(Rows r, Second t, const floa
   }
   const float w = some ? g * inv : 0.0f;
   const bool dense = a && some;
-  auto piece = [&](int64_t at, typename Vec<E_>::type v, typename Vec<E_>::type u) {
+  auto piece = [&](int64_t at, const float* e, const float* u) {
     float z[Vec<E_>::N];
 #pragma unroll
-    for (int i = 0; i < Vec<E_>::N; ++i) z[i] = dense ? w * exp2_fast(((float)v[i] - m) * c) * ((float)u[i] - pa) : 0.0f;
+    for (int i = 0; i < Vec<E_>::N; ++i) z[i] = dense ? w * exp2_fast((e[i] - m) * c) * (u[i] - pa) : 0.0f;
     store_vec(y + at, z);
   };
   auto one = [&](int64_t at, float v, float u) { y[at] = (E_)(dense ? w * exp2_fast((v - m) * c) * (u - pa) : 0.0f); };
   if (STATS == kKept && a) {
+    const float f = w * sh.factor();
+    auto write = [&](auto value) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (kx.has(i)) piece(kx.at(i), kx.v[i], ka.v[i]);
-    if (kx.has_single) one(kx.at_single, (float)kx.single, (float)ka.single);
+      for (int i = 0; i < NV; ++i)
+        if (kx.has(i)) {
+          float e[Vec<E_>::N], u[Vec<E_>::N];
+          kx.get(i, e);
+          ka.get(i, u);
+#pragma unroll
+          for (int k = 0; k < Vec<E_>::N; ++k) e[k] = value(e[k], u[k]);
+          store_vec(y + kx.at(i), e);
+        }
+      if (kx.has_single) y[kx.at_single] = (E_)value((float)kx.single, (float)ka.single);
+    };
+    if (!some)
+      write([](float, float) { return 0.0f; });
+    else if (sh.wide)
+      write([&](float e, float u) { return f * sh.part<true>(e) * (u - pa); });
+    else
+      write([&](float e, float u) { return f * sh.part<false>(e) * (u - pa); });
   } else {
     const E_* b = a ? a : x;
-    over_row(x, sl.c0, sl.c1, [&](int64_t at) { piece(at, load_vec(x + at), load_vec(b + at)); },
-             [&](int64_t at) { one(at, (float)x[at], (float)b[at]); });
+    over_row(
+        x, sl.c0, sl.c1,
+        [&](int64_t at) {
+          float e[Vec<E_>::N], u[Vec<E_>::N];
+          load_floats(x + at, e);
+          load_floats(b + at, u);
+          piece(at, e, u);
+        },
+        [&](int64_t at) { one(at, (float)x[at], (float)b[at]); });
   }
   __syncthreads();
   for (int j = threadIdx.x; j < r.K; j += blockDim.x)
@@ -588,7 +706,6 @@ int both_rows(const char* who, const Rows& r, int32_t dtype, const float* dloss,
   DIFFOPT_KEPT(512, 13)
   DIFFOPT_KEPT(512, 16)
   DIFFOPT_KEPT(1024, 16)
-  DIFFOPT_KEPT(1024, 32)
 #undef DIFFOPT_KEPT
   DIFFOPT_LAUNCH((distill_row<E_, kRead, true>), r.N, kDB, r, dloss, loss, stats, dx, dstride, dt, nullptr, 1, r.V);
   return launch_status(who);
@@ -612,7 +729,6 @@ int second_rows(const char* who, const Rows& r, int32_t dtype, const Second& t, 
   DIFFOPT_KEPT(512, 4)
   DIFFOPT_KEPT(512, 8)
   DIFFOPT_KEPT(1024, 8)
-  DIFFOPT_KEPT(1024, 16)
 #undef DIFFOPT_KEPT
   DIFFOPT_LAUNCH((distill_second<E_, kRead>), r.N, kDB, r, t, nullptr, 1, r.V);
   return launch_status(who);

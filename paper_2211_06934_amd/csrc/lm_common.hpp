@@ -30,11 +30,20 @@ __device__ __forceinline__ typename Vec<E>::type load_vec(const E* p) {
 }
 
 template <class E>
-__device__ __forceinline__ void store_vec(E* p, const float* x) {
-  typename Vec<E>::type v;
+__device__ __forceinline__ void load_floats(const E* p, float* x) {
+  const typename Vec<E>::type v = load_vec(p);
 #pragma unroll
-  for (int i = 0; i < Vec<E>::N; ++i) v[i] = (E)x[i];
-  *reinterpret_cast<typename Vec<E>::type*>(p) = v;
+  for (int i = 0; i < Vec<E>::N; ++i) x[i] = (float)v[i];
+}
+
+template <class E>
+__device__ __forceinline__ void store_vec(E* p, const float* x) {
+  typedef float wide __attribute__((ext_vector_type(16 / sizeof(E))));
+  typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
+  wide w;
+#pragma unroll
+  for (int i = 0; i < Vec<E>::N; ++i) w[i] = x[i];
+  *reinterpret_cast<typename Vec<E>::type*>(p) = __builtin_convertvector(w, whole);  // pairs in one instruction
 }
 
 constexpr float kInf = __builtin_inff();
