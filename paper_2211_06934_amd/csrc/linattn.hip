@@ -209,9 +209,9 @@ __global__ __launch_bounds__(kStepB) void linattn_one(Shape s, Scan a, int32_t c
 //   O = W_q (Q S) + (P o M) V,  P = Q K^T,  M_ts = g^(t-s) for s <= t
 //   S = g^L S + K^T (W_k V)
 // where W_q, W_k are diagonal: g^(t+1), g^(L-1-s) forward and g^t, g^(L-s) back
-// in time (no power is ever negative).  A workgroup of four waves walks the
-// chunks of one segment of a sequence; wave w owns 16 NCT columns of the state,
-// all DK rows of them, in registers for the whole walk.
+// in time (no power is ever negative).  A workgroup of NW waves walks the
+// chunks of one segment of a sequence; wave w owns 16 columns of the state, all
+// DK rows of them, in registers for the whole walk.
 //
 // Fragments: v_mfma 16x16 takes row (or column) lane % 16 and, of a block of 32
 // along the contraction, 8 elements per 16-lane group g = lane / 16; it returns
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(kStepB) void linattn_one(Shape s, Scan a, int32_t c
 // in 16-byte pieces.  Tokens are numbered 32 b + 4 g .. + 4 and + 16: P^T as it
 // is computed is an operand of P V, and V and K^T come out of LDS transposed
 // four tokens at a time (ds_read_b64_tr_b16).  The products are computed
-// transposed, so that a lane stores 4 NCT neighbouring elements of one token.
+// transposed, so that a lane stores 4 neighbouring elements of one token.
 //
 // In bf16 the scores and the state are rounded where they enter a product (the
 // outputs are bf16 too); the state itself is fp32 and its update takes W_k V in
@@ -248,21 +248,27 @@ __device__ __forceinline__ f32x4 mfma32(Frag<float>::type a, Frag<float>::type b
   return c;
 }
 
-// A matrix of rows of W elements in LDS.  A row takes three 16-byte pieces more
-// than its elements, so that 16 rows at one piece fall on different banks and 8
-// rows of 4 pieces, half of each read, on the banks two or three times (two is
-// the least), and every access lies a constant from one address per lane.
+// A matrix of C rows of W elements in LDS, as loads that go there directly write
+// it: a wave's 64 pieces of 16 bytes in the order of its lanes make a block of RB
+// rows, one piece more separates blocks, and within its row a piece lies at its
+// number xor mix(row).  Then 16 rows at one piece fall on 16 different pieces of
+// the banks, and 8 rows of 4 pieces, half of each read, on each of them twice (the
+// least).
 template <class E, int W>
 struct Tile {
-  static constexpr int VN = 16 / (int)sizeof(E);
-  static constexpr int ROW = W + 3 * VN;  // elements from row to row
+  static constexpr int VN = 16 / (int)sizeof(E), NP = W / VN, RB = 64 / NP, BLOCK = 65 * VN;
+  static_assert(NP >= 4 && NP <= 64 && RB * NP == 64, "rows of 64 bytes to 1 KiB");
+  static constexpr int elements(int rows) { return rows / RB * BLOCK; }
   typedef typename Frag<E>::type frag;
 
-  // a lane's part of the address of row(): row lane % 16, elements 8 g
-  static __device__ __forceinline__ int row_lane(int lane) { return (lane & 15) * ROW + 8 * (lane >> 4); }
-  // elements col .. + 8 (from 8 g on) of row r (from lane % 16 on)
-  static __device__ __forceinline__ frag row(const E* base, int lane_part, int r, int col) {
-    const E* p = base + lane_part + (r * ROW + col);
+  static __device__ __forceinline__ constexpr int mix(int r) {
+    return NP == 64 ? 0 : NP == 32 ? (r & 1) << 3 : NP == 16 ? (r & 3) << 2 : NP == 8 ? (r & 6) : (r >> 2) & 3;
+  }
+  static __device__ __forceinline__ constexpr int at(int r, int piece) { return r / RB * BLOCK + (r % RB * NP + (piece ^ mix(r))) * VN; }
+
+  // elements col .. + 8 (col a multiple of 8) of row r
+  static __device__ __forceinline__ frag row(const E* base, int r, int col) {
+    const E* p = base + at(r, col / VN);
     if constexpr (sizeof(E) == 2) {
       return *reinterpret_cast<const frag*>(p);
     } else {
@@ -271,30 +277,45 @@ struct Tile {
     }
   }
 
-  // a lane's part of the address of column()
-  template <int STEP>
-  static __device__ __forceinline__ int column_lane(int lane) {
-    const int g = lane >> 4, m = lane & 15;
-    return sizeof(E) == 2 ? (4 * g + (m >> 2)) * ROW + STEP * (m & 3) : 4 * g * ROW + STEP * (m >> 2) + (m & 3);
-  }
   // element col + (m / 4) STEP + m % 4, m = lane % 16, of rows 32 b + 4 g .. + 4 and 16 further
-  static __device__ __forceinline__ frag column(const E* base, int lane_part, int b, int col) {
-    const E* p = base + lane_part + (32 * b * ROW + col);
+  template <int STEP>
+  static __device__ __forceinline__ frag column(const E* base, int b, int col, int g, int m) {
     if constexpr (sizeof(E) == 2) {
       typedef short s16x4 __attribute__((ext_vector_type(4)));
       typedef short s16x8 __attribute__((ext_vector_type(8)));
       typedef __attribute__((address_space(3))) s16x4 lds4;
+      const int r = 32 * b + 4 * g + (m >> 2), c = col + STEP * (m & 3);
+      const E *p = base + at(r, c / VN) + c % VN, *q = base + at(r + 16, c / VN) + c % VN;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + 16 * ROW));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(q));
       return __builtin_bit_cast(frag, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
+      const int c = col + STEP * (m >> 2) + (m & 3);
       frag f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = p[((j >> 2) * 16 + (j & 3)) * ROW];
+      for (int j = 0; j < 8; ++j) f[j] = base[at(32 * b + (j >> 2) * 16 + 4 * g + (j & 3), c / VN) + c % VN];
       return f;
     }
   }
 };
+
+// 16 bytes a lane from memory to LDS: the lanes' pieces follow one another from
+// LDS address `to` (the same in every lane) on.  Counted with the wave's other loads; the
+// caller waits for all of them before the workgroup's barrier.  (Of the builtin
+// the compiler takes every transposing read to depend, and waits for the next
+// chunk before this one is used.  The instruction has no result register, and
+// nothing else here uses m0, which it takes its address from.)
+template <class E>
+__device__ __forceinline__ void load_to_lds(const E* from, uint32_t to) {
+  const uint32_t base = __builtin_amdgcn_readfirstlane(to);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(base), "v"(from) : "memory");
+}
+
+// The address of a shared object in LDS.
+template <class E>
+__device__ __forceinline__ uint32_t lds_address(E* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) E*)p;
+}
 
 __device__ __forceinline__ bf16x8 pack(f32x4 a, f32x4 b, bf16) {
   return bf16x8{(bf16)a[0], (bf16)a[1], (bf16)a[2], (bf16)a[3], (bf16)b[0], (bf16)b[1], (bf16)b[2], (bf16)b[3]};
@@ -306,76 +327,92 @@ __device__ __forceinline__ Frag<float>::type pack(f32x4 a, f32x4 b, float) {
 // g^n for n >= 0; lg2 = log2 g may be -inf (g = 0, g^0 = 1).
 __device__ __forceinline__ float power(float lg2, int n) { return n == 0 ? 1.0f : __builtin_amdgcn_exp2f((float)n * lg2); }
 
+// A value that all lanes hold, in a scalar register.
+__device__ __forceinline__ float uniform(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
+
 // What a launch runs: up to three scans of one shape, each cut into segments of
 // whole chunks; seg[i] holds the segments' states ([state][segment][Dk][Dv]).
 struct Jobs {
   Scan scan[3];
   float* seg[3];
-  int32_t nseg, seg_chunks;
+  int32_t nseg;
+  int64_t seg_tokens;  // whole chunks
 };
 
-template <class E>
+// Tokens of a chunk.
+template <class E, int DK>
 struct ChunkOf {
-  static constexpr int C = sizeof(E) == 2 ? 64 : 32;
+  static constexpr int C = sizeof(E) == 2 && DK <= 128 ? 64 : 32;
 };
 
-constexpr int kChunkB = 256;
+#ifndef FILL
+#define FILL 512
+#endif
+#ifndef MINC
+#define MINC 4
+#endif
 
-// A thread's 16-byte pieces of one staged matrix: C rows (tokens) of W elements.
-template <class E, int W, int C>
-struct Stage {
-  static constexpr int VN = 16 / (int)sizeof(E), NP = W / VN, N = C * NP / kChunkB, STEP = kChunkB / NP;
-  typename Vec<E>::type v[N];
-
-  // rows 0 .. L - 1 from `head`, st elements apart (negative: back in time),
-  // columns from col0 on; WHOLE: W of them are there, else those below `width`
-  template <bool WHOLE>
-  __device__ __forceinline__ void load(const E* head, int64_t st, int L, int col0, int width) {
-    const int r0 = threadIdx.x / NP, c = col0 + threadIdx.x % NP * VN;
-    const E* p = head + r0 * st + c;
+// One matrix of a chunk on its way to LDS (element `at` of what begins at `lds`,
+// LDS address `address`), by a workgroup of NW waves: rows
+// 0 .. L - 1 from `head`, st elements apart (negative: back in time), columns
+// col0 .. + W of `width`; rows from L on become zero, columns past the width stay
+// zero from before.  PIECES: the width is whole pieces; else through registers,
+// element by element.
+template <class E, int W, int C, int NW, bool PIECES>
+__device__ __forceinline__ void stage(E* lds, uint32_t address, int at, const E* head, int64_t st, int L, int col0, int width, int lane, int wave) {
+  typedef Tile<E, W> T;
+  constexpr int N = C / T::RB / NW;  // blocks of a wave
+  static_assert(N * NW * T::RB == C, "whole blocks for every wave");
+  typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      typename Vec<E>::type x{};
-      if (r0 + i * STEP < L) {
-        if (WHOLE) {
-          x = load_vec(p);
-        } else {
+  for (int i = 0; i < N; ++i) {
+    const int block = wave + NW * i, r = block * T::RB + lane / T::NP, c = col0 + ((lane % T::NP) ^ T::mix(r)) * T::VN;
+    const int to = at + block * T::BLOCK;
+    if (PIECES) {
+      if (c < width) {
+        if (r < L)
+          load_to_lds(head + r * st + c, address + to * (int)sizeof(E));
+        else
+          *reinterpret_cast<whole*>(lds + to + lane * T::VN) = whole{};
+      }
+    } else {
+      whole x{};
+      if (r < L) {
+        const E* p = head + r * st;
 #pragma unroll
-          for (int e = 0; e < VN; ++e) {
-            const E y = p[c + e < width ? e : -c];  // the row's first element where there is none
-            x[e] = c + e < width ? y : (E)0.0f;
-          }
+        for (int e = 0; e < T::VN; ++e) {
+          const E y = p[c + e < width ? c + e : 0];
+          x[e] = c + e < width ? y : (E)0.0f;
         }
       }
-      v[i] = x;
-      p += STEP * st;
+      *reinterpret_cast<whole*>(lds + to + lane * T::VN) = x;
     }
   }
-  __device__ __forceinline__ void put(E* lds) const {
-    typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
-    E* p = lds + threadIdx.x / NP * Tile<E, W>::ROW + threadIdx.x % NP * VN;
-#pragma unroll
-    for (int i = 0; i < N; ++i) *reinterpret_cast<whole*>(p + i * STEP * Tile<E, W>::ROW) = v[i];
-  }
-};
+}
 
-template <class E, int DK, int NCT>
+// What a chunk kernel keeps in LDS: two buffers of Q, K and V (one is read while
+// the next chunk arrives in the other), the scores' operands, the outputs.
+template <class E, int DK, int NW, bool OUT>
 struct ChunkLds {
-  static constexpr int C = ChunkOf<E>::C;
-  static constexpr int bytes = C * (2 * Tile<E, DK>::ROW + Tile<E, 64 * NCT>::ROW) * (int)sizeof(E) + C * C * (int)sizeof(E);
+  static constexpr int C = ChunkOf<E, DK>::C, NT = C / 16, NB = C / 32, CT = 16 * NW;
+  static constexpr int kq = Tile<E, DK>::elements(C), kv = Tile<E, CT>::elements(C);
+  static constexpr int buffer = (OUT ? 2 : 1) * kq + kv;  // K, V, then Q
+  static constexpr int orow = CT + 16 / (int)sizeof(E);   // elements from an output's row to the next
+  E in[2][buffer];
+  typename Frag<E>::type P[OUT ? NT * NB * 64 : 1];
+  E out[OUT ? C * orow : 1];
 };
 
-template <class E, int DK, int NCT, int SPLIT, bool OUT, bool WHOLE>
-__global__ __launch_bounds__(kChunkB, (ChunkLds<E, DK, NCT>::bytes > 80 * 1024 ? 1 : 2)) void linattn_chunks(Shape sh, Jobs jobs,
-                                                                                                     int32_t col_tiles) {
-  constexpr int C = ChunkOf<E>::C, NT = C / 16, NB = C / 32, KB = DK / 32, CT = 64 * NCT;
+template <class E, int DK, int NW, int SPLIT, bool OUT, bool PIECES>
+__global__ __launch_bounds__(64 * NW, (OUT || DK > 128 ? 1 : NW / 2)) void linattn_chunks(Shape sh, Jobs jobs, int32_t col_tiles) {
+  typedef ChunkLds<E, DK, NW, OUT> Lds;
+  constexpr int C = Lds::C, NT = Lds::NT, NB = Lds::NB, KB = DK / 32, CT = Lds::CT, B = 64 * NW;
   typedef typename Frag<E>::type frag;
   typedef Tile<E, DK> KTile;
   typedef Tile<E, CT> VTile;
-  __shared__ __attribute__((aligned(16))) E sQ[OUT ? C * KTile::ROW : 16];
-  __shared__ __attribute__((aligned(16))) E sK[C * KTile::ROW];
-  __shared__ __attribute__((aligned(16))) E sV[C * VTile::ROW];
-  __shared__ __attribute__((aligned(16))) frag sP[OUT ? NT * NB * 64 : 1];
+  __shared__ __attribute__((aligned(16))) Lds lds;
 
   const Scan a = jobs.scan[blockIdx.y];
   const int nq = OUT ? a.nq : 1;
@@ -389,225 +426,215 @@ __global__ __launch_bounds__(kChunkB, (ChunkLds<E, DK, NCT>::bytes > 80 * 1024 ?
   if (b >= sh.B) return;  // the launch's scans differ in heads
   const int j = (int)(state - b * sh.Hs);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, m = lane & 15;
-  const int at_row = KTile::row_lane(lane), at_k = KTile::template column_lane<8>(lane), at_v = VTile::template column_lane<4 * NCT>(lane);
   const int64_t len = length_of(sh, b);
   const double lgd = (double)sh.log_decay[j];
   const float lg2 = (float)(lgd * 1.4426950408889634074);
   const int back = a.back;
-  const int64_t first = (int64_t)seg * jobs.seg_chunks;
-  int64_t last = first + jobs.seg_chunks;
+  const int64_t first = seg * (jobs.seg_tokens / C);
+  int64_t last = first + jobs.seg_tokens / C;
   const int64_t chunks = (sh.T + C - 1) / C;
   if (last > chunks) last = chunks;
   const int64_t live = (len + C - 1) / C;  // chunks with tokens
   const int64_t end = last < live ? last : live;
 
-  // the state: tile (kb, u), column tile ct; a lane holds column wave 16 NCT +
-  // (m/4) 4 NCT + 4 ct + m%4 of the tile, rows 32 kb + 8 g + 4 u + i
-  const int row0 = 8 * g, col0 = ct0 + 16 * NCT * wave + 4 * NCT * (m >> 2) + (m & 3);
+  // the state: tile (kb, u); a lane holds column 16 wave + m of the tile, rows
+  // 32 kb + 8 g + 4 u + i
   const bool cut = jobs.nseg > 1;
   float* segments = cut ? jobs.seg[blockIdx.y] + (state * jobs.nseg + seg) * a.Dk * a.Dv : nullptr;
-  f32x4 S[KB][2][NCT];
+  f32x4 S[KB][2];
   {
     const float* s0 = !OUT ? nullptr : cut ? segments : a.s0 ? a.s0 + state * a.Dk * a.Dv : nullptr;
     const bool flip = !cut && a.flip;
+    const int c = ct0 + 16 * wave + m;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = row0 + 32 * kb + 4 * u + i, c = col0 + 4 * ct;
-            const bool in = s0 && (WHOLE || (r < a.Dk && c < a.Dv));
-            S[kb][u][ct][i] = in ? s0[flip ? c * a.Dk + r : r * a.Dv + c] : 0.0f;
-          }
+        for (int i = 0; i < 4; ++i) {
+          const int r = 8 * g + 32 * kb + 4 * u + i;
+          const bool in = s0 && r < a.Dk && c < a.Dv;
+          S[kb][u][i] = in ? s0[flip ? c * a.Dk + r : r * a.Dv + c] : 0.0f;
+        }
   }
 
   // g^C rounds once; what that leaves out grows with every chunk and is made
   // good each eighth one
   const double gcd = exp(lgd * C);
-  const float gc = (float)gcd;
+  const float gc = uniform((float)gcd);
   const double gc8 = gc > 0.0f ? gcd * exp(7.0 * log(gcd / (double)gc)) : 0.0;
-  const float g8_hi = (float)gc8, g8_lo = (float)(gc8 - (double)g8_hi);
-  const float gl = (float)exp(lgd * (double)(len % C));  // the last chunk's, where it is not whole
+  const float g8_hi = uniform((float)gc8), g8_lo = uniform((float)(gc8 - (double)g8_hi));
+  const float gl = uniform((float)exp(lgd * (double)(len % C)));  // the last chunk's, where it is not whole
 
-  // weights of whole chunks: scores of a diagonal tile and of the tile before
-  // it, outputs of the state, values that enter it
+  // The powers of a chunk's tokens are products of one per lane and one for all
+  // lanes (scalar registers): of the outputs of the state, qw g^(16 t), and of the
+  // values that enter it, kw g^(...) (whole chunks).
   const float ps = a.qs * a.ks;
-  float diag[4], beside[4], kw[NB][8], qw[NT];
+  const float qw = a.qs * power(lg2, m + 1 - back), kw = a.ks * power(lg2, 12 - 4 * g);
+  float qt[NT], ks[NB][8];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int gap = m - 4 * g - e;
-    diag[e] = gap >= 0 ? ps * power(lg2, gap) : 0.0f;
-    beside[e] = ps * power(lg2, gap + 16);
-  }
+  for (int t = 0; t < NT; ++t) qt[t] = uniform(power(lg2, 16 * t));
 #pragma unroll
-  for (int t = 0; t < NT; ++t) qw[t] = a.qs * power(lg2, 16 * t + m + 1 - back);
-  auto key_weights = [&](int L) {
-    int g = lane >> 4;
-    asm volatile("" : "+v"(g));  // nothing of it is kept over the walk for the last chunk's weights
+  for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int n = L - 1 + back - (32 * nb + (e >> 2) * 16 + 4 * g + (e & 3));
-        kw[nb][e] = n >= back ? a.ks * power(lg2, n) : 0.0f;
-      }
-  };
-  key_weights(C);
+    for (int e = 0; e < 8; ++e) ks[nb][e] = uniform(power(lg2, C - 13 + back - 32 * nb - 16 * (e >> 2) - (e & 3)));
 
   const int dir = back ? -1 : 1;
   const E* q0 = OUT ? at<E>(a.q, b, back ? len - 1 : 0, (int64_t)j * a.nq + qh) : nullptr;
   const E* k0 = at<E>(a.k, b, back ? len - 1 : 0, (int64_t)j * a.nk);
   const E* v0 = at<E>(a.v, b, back ? len - 1 : 0, (int64_t)j * a.nk);
   const int64_t qst = dir * a.q.st, kst = dir * a.k.st, vst = dir * a.v.st;
-  Stage<E, DK, C> pq, pk;
-  Stage<E, CT, C> pv;
   auto valid = [&](int64_t c) { return (int)(len - c * C < C ? len - c * C : C); };
-  // item n of the walk: k/v head n % nk of chunk first + n / nk
-  int h = -1, h_next = 0;
-  int64_t c = first, c_next = first;
-  f32x4 O[NT][NCT];
-  while (true) {
-    if (h >= 0) {
-      __syncthreads();
-      if (OUT && h == 0) pq.put(sQ);
-      pk.put(sK);
-      pv.put(sV);
-      __syncthreads();
+  if (PIECES && (a.Dk < DK || a.Dv - ct0 < CT)) {  // columns past the widths
+    typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
+    for (int i = threadIdx.x; i < 2 * Lds::buffer / KTile::VN; i += B) reinterpret_cast<whole*>(&lds.in[0][0])[i] = whole{};
+    __syncthreads();
+  }
+
+  // a finished chunk's outputs, from LDS in whole pieces of a token's row
+  auto store_outputs = [&](int64_t c) {
+    const int L = valid(c);
+    E* o = at<E>(a.o, b, back ? len - 1 : 0, (int64_t)j * a.nq + qh) + c * C * dir * a.o.st;
+    constexpr int NP = CT / VTile::VN;
+#pragma unroll
+    for (int i = 0; i < C * NP / B; ++i) {
+      const int item = threadIdx.x + i * B, r = item / NP, col = item % NP * VTile::VN;
+      if (r < L && ct0 + col < a.Dv) {
+        typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
+        *reinterpret_cast<typename Vec<E>::type*>(o + r * dir * a.o.st + ct0 + col) = *reinterpret_cast<const whole*>(lds.out + r * Lds::orow + col);
+      }
     }
+  };
+
+  // item n of the walk: k/v head n % nk of chunk first + n / nk
+  int h = -1, h_next = 0, turn = 0;
+  int64_t c = first, c_next = first, pending = -1;
+  f32x4 O[NT];
+  while (true) {
+    // the item has arrived, and every wave is done with the one before it
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    __syncthreads();
     if (c_next < end) {
       const int L = valid(c_next);
-      if (OUT && h_next == 0) pq.template load<WHOLE>(q0 + c_next * C * qst, qst, L, 0, a.Dk);
-      pk.template load<WHOLE>(k0 + c_next * C * kst + h_next * a.k.sh, kst, L, 0, a.Dk);
-      pv.template load<WHOLE>(v0 + c_next * C * vst + h_next * a.v.sh, vst, L, ct0, a.Dv);
+      E* in = &lds.in[0][0];
+      const uint32_t address = lds_address(in);
+      const int to = (turn ^ (h >= 0)) * Lds::buffer;
+      stage<E, DK, C, NW, PIECES>(in, address, to, k0 + c_next * C * kst + h_next * a.k.sh, kst, L, 0, a.Dk, lane, wave);
+      stage<E, CT, C, NW, PIECES>(in, address, to + Lds::kq, v0 + c_next * C * vst + h_next * a.v.sh, vst, L, ct0, a.Dv, lane, wave);
+      if (OUT) stage<E, DK, C, NW, PIECES>(in, address, to + Lds::kq + Lds::kv, q0 + c_next * C * qst, qst, L, 0, a.Dk, lane, wave);
+    }
+    if (OUT && PIECES && pending >= 0) {
+      store_outputs(pending);
+      pending = -1;
     }
     if (h >= 0) {
+      const E *sK = &lds.in[0][0] + turn * Lds::buffer, *sV = sK + Lds::kq, *sQ = sV + Lds::kv;
+      frag* sP = lds.P;
       const int L = valid(c);
-      if (L < C) key_weights(L);
+      // what follows from these is made anew in every chunk: kept over the walk,
+      // it would cost the registers of a second workgroup
+      int gap0 = m - 4 * g, g4 = 4 * g;
+      float kwc = kw, qwc = qw;
+      asm volatile("" : "+v"(gap0), "+v"(g4), "+v"(kwc), "+v"(qwc));
       if (OUT) {
         // P^T of this wave's tiles, masked and decayed, as operands of P V
-        constexpr int PER = NT * NT / 4;  // tiles, of one query tile, that a wave computes
+        constexpr int PER = NT * NT / NW > 0 ? NT * NT / NW : 1;  // tiles, of one query tile, that a wave computes
         const int tq = wave * PER / NT, tk0 = wave * PER % NT;
         f32x4 P[PER];
+        if (tq < NT) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          const int apart = tq - tk0 - i;
-          P[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-          if (apart >= 0) {
+          for (int i = 0; i < PER; ++i) {
+            const int apart = tq - tk0 - i;
+            P[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (apart >= 0) {
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-              P[i] = mfma32(KTile::row(sK + 16 * tk0 * KTile::ROW, at_row, 16 * i, 32 * kb), KTile::row(sQ + 16 * tq * KTile::ROW, at_row, 0, 32 * kb), P[i]);
-            if (apart == 0) {
+              for (int kb = 0; kb < KB; ++kb)
+                P[i] = mfma32(KTile::row(sK + KTile::elements(16) * tk0, 16 * i + m, 32 * kb + 8 * g),
+                              KTile::row(sQ + KTile::elements(16) * tq, m, 32 * kb + 8 * g), P[i]);
+              if (apart == 0) {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) P[i][e] = m >= 4 * g + e ? P[i][e] * diag[e] : 0.0f;
-            } else {
-              const float w = power(lg2, 16 * (apart - 1));
+                for (int e = 0; e < 4; ++e) P[i][e] = gap0 >= e ? P[i][e] * (ps * power(lg2, gap0 - e)) : 0.0f;
+              } else {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) P[i][e] *= beside[e] * w;
+                for (int e = 0; e < 4; ++e) P[i][e] *= ps * power(lg2, gap0 + 16 * apart - e);
+              }
             }
           }
-        }
-        if constexpr (PER >= 2) {
+          if constexpr (PER >= 2) {
 #pragma unroll
-          for (int kb = 0; kb < PER / 2; ++kb) sP[(tq * NB + kb) * 64 + lane] = pack(P[2 * kb], P[2 * kb + 1], E());
-        } else {  // half a block: four of a lane's eight elements
-          reinterpret_cast<f32x4*>(&sP[(tq * NB) * 64 + lane])[tk0] = P[0];
+            for (int kb = 0; kb < PER / 2; ++kb) sP[(tq * NB + tk0 / 2 + kb) * 64 + lane] = pack(P[2 * kb], P[2 * kb + 1], E());
+          } else {  // half a block: four of a lane's eight elements
+            typedef E four __attribute__((ext_vector_type(4)));
+            reinterpret_cast<four*>(&sP[(tq * NB + tk0 / 2) * 64 + lane])[tk0 & 1] = __builtin_convertvector(P[0], four);
+          }
         }
       }
 
-      frag V[NB][NCT];
+      frag V[NB];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int ct = 0; ct < NCT; ++ct) V[nb][ct] = VTile::column(sV + 16 * NCT * wave, at_v, nb, 4 * ct);
+      for (int nb = 0; nb < NB; ++nb) V[nb] = VTile::template column<4>(sV, nb, 16 * wave, g, m);
 
       if (OUT) {
         // zeros times the values: zero unless one is infinite or NaN
         f32x4 odd{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+        for (int nb = 0; nb < NB; ++nb) {
+          if constexpr (sizeof(E) == 2) {
+            odd = mfma32(V[nb], frag{}, odd);
+          } else {
 #pragma unroll
-          for (int ct = 0; ct < NCT; ++ct) {
-            if constexpr (sizeof(E) == 2) {
-              odd = mfma32(V[nb][ct], frag{}, odd);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) odd[e & 3] = fmaf(V[nb][ct][e], 0.0f, odd[e & 3]);
-            }
+            for (int e = 0; e < 8; ++e) odd[e & 3] = fmaf(V[nb][e], 0.0f, odd[e & 3]);
           }
+        }
         if (h == 0) {
 #pragma unroll
-          for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int ct = 0; ct < NCT; ++ct) O[t][ct] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+          for (int t = 0; t < NT; ++t) O[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb) {
-            frag s[NCT];
+            const frag s = pack(S[kb][0], S[kb][1], E());
 #pragma unroll
-            for (int ct = 0; ct < NCT; ++ct) s[ct] = pack(S[kb][0][ct], S[kb][1][ct], E());
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              const frag q = KTile::row(sQ, at_row, 16 * t, 32 * kb);
-#pragma unroll
-              for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(s[ct], q, O[t][ct]);
-            }
+            for (int t = 0; t < NT; ++t) O[t] = mfma32(s, KTile::row(sQ, 16 * t + m, 32 * kb + 8 * g), O[t]);
           }
 #pragma unroll
-          for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int ct = 0; ct < NCT; ++ct) O[t][ct] *= qw[t];
+          for (int t = 0; t < NT; ++t) O[t] *= qwc * qt[t];
         }
         __syncthreads();
         if (__all(odd[0] + odd[1] + odd[2] + odd[3] == 0.0f)) {
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int nb = 0; nb <= t / 2; ++nb) {
-              const frag p = sP[(t * NB + nb) * 64 + lane];
-#pragma unroll
-              for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(V[nb][ct], p, O[t][ct]);
-            }
+            for (int nb = 0; nb <= t / 2; ++nb) O[t] = mfma32(V[nb], sP[(t * NB + nb) * 64 + lane], O[t]);
         } else {
           // a product with the zeros of the mask would carry an infinity or NaN
           // to earlier tokens, so the sum stops at the token
 #pragma unroll 1
           for (int s = 0; s < L; ++s) {
             const E* p = reinterpret_cast<const E*>(&sP[(s >> 5) * 64 + ((s >> 2) & 3) * 16 + m]) + ((s >> 4) & 1) * 4 + (s & 3);
-            const E* v = sV + s * VTile::ROW + 16 * NCT * wave + 4 * NCT * g;
+            const E* v = sV + VTile::at(s, (16 * wave + 4 * g) / VTile::VN) + (16 * wave + 4 * g) % VTile::VN;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
               if (s <= 16 * t + m) {
 #pragma unroll
-                for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-                  for (int i = 0; i < 4; ++i) O[t][ct][i] = fmaf((float)p[t * NB * 64 * 8], (float)v[4 * ct + i], O[t][ct][i]);
+                for (int i = 0; i < 4; ++i) O[t][i] = fmaf((float)p[t * NB * 64 * 8], (float)v[i], O[t][i]);
               }
           }
         }
         if (h + 1 == a.nk && a.o.p) {
-          E* o = at<E>(a.o, b, back ? len - 1 : 0, (int64_t)j * a.nq + qh) + c * C * dir * a.o.st;
-          const int col = ct0 + 16 * NCT * wave + 4 * NCT * g;
+          if (PIECES) {
+            typedef E four __attribute__((ext_vector_type(4)));
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            E* p = o + (16 * t + m) * dir * a.o.st + col;
-            if (16 * t + m < L) {
-              if (WHOLE) {
-                typedef E out_vec __attribute__((ext_vector_type(4 * NCT), aligned(alignof(E))));
-                out_vec z;
+            for (int t = 0; t < NT; ++t)
+              *reinterpret_cast<four*>(lds.out + (16 * t + m) * Lds::orow + 16 * wave + 4 * g) = __builtin_convertvector(O[t], four);
+            pending = c;
+          } else {
+            const int col = ct0 + 16 * wave + 4 * g;
+            E* p = at<E>(a.o, b, back ? len - 1 : 0, (int64_t)j * a.nq + qh) + (c * C + m) * dir * a.o.st + col;
 #pragma unroll
-                for (int ct = 0; ct < NCT; ++ct)
+            for (int t = 0; t < NT; ++t) {
 #pragma unroll
-                  for (int i = 0; i < 4; ++i) z[4 * ct + i] = (E)O[t][ct][i];
-                *reinterpret_cast<out_vec*>(p) = z;
-              } else {
-#pragma unroll
-                for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-                  for (int i = 0; i < 4; ++i)
-                    if (col + 4 * ct + i < a.Dv) p[4 * ct + i] = (E)O[t][ct][i];
-              }
+              for (int i = 0; i < 4; ++i)
+                if (16 * t + m < L && col + i < a.Dv) p[i] = (E)O[t][i];
+              p += 16 * dir * a.o.st;
             }
           }
         }
@@ -620,46 +647,50 @@ __global__ __launch_bounds__(kChunkB, (ChunkLds<E, DK, NCT>::bytes > 80 * 1024 ?
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-              for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) S[kb][u][ct][i] = fmaf(S[kb][u][ct][i], g8_hi, S[kb][u][ct][i] * g8_lo);
+              for (int i = 0; i < 4; ++i) S[kb][u][i] = fmaf(S[kb][u][i], g8_hi, S[kb][u][i] * g8_lo);
         } else {
           const float d = L < C ? gl : gc;
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-              for (int ct = 0; ct < NCT; ++ct) S[kb][u][ct] *= d;
+            for (int u = 0; u < 2; ++u) S[kb][u] *= d;
         }
       }
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        frag part[SPLIT][NCT];
+        float w[8];
 #pragma unroll
-        for (int ct = 0; ct < NCT; ++ct)
+        for (int e = 0; e < 8; ++e) w[e] = kwc * ks[nb][e];
+        if (L < C) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            float y = (float)V[nb][ct][e] * kw[nb][e];
-#pragma unroll
-            for (int p = 0; p < SPLIT; ++p) {
-              part[p][ct][e] = (E)y;
-              y -= (float)part[p][ct][e];
-            }
+            const int n = L - 1 + back - g4 - (32 * nb + (e >> 2) * 16 + (e & 3));
+            w[e] = n >= back ? a.ks * power(lg2, n) : 0.0f;
           }
+        }
+        // the weighted values in SPLIT parts, each the rounding of what is left
+        frag part[SPLIT];
+        typename Frag<float>::type y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = (float)V[nb][e] * w[e];
+#pragma unroll
+        for (int p = 0; p < SPLIT; ++p) {
+          part[p] = __builtin_convertvector(y, frag);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] -= (float)part[p][e];
+        }
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const frag k = KTile::column(sK, at_k, nb, 32 * kb + 4 * u);
+            const frag k = KTile::template column<8>(sK, nb, 32 * kb + 4 * u, g, m);
 #pragma unroll
-            for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-              for (int p = 0; p < SPLIT; ++p) S[kb][u][ct] = mfma32(k, part[p][ct], S[kb][u][ct]);
+            for (int p = 0; p < SPLIT; ++p) S[kb][u] = mfma32(k, part[p], S[kb][u]);
           }
       }
     }
     if (c_next >= end) break;
+    turn ^= h >= 0;
     c = c_next;
     h = h_next;
     if (++h_next == a.nk) {
@@ -668,41 +699,44 @@ __global__ __launch_bounds__(kChunkB, (ChunkLds<E, DK, NCT>::bytes > 80 * 1024 ?
     }
   }
 
+  if (OUT && PIECES && pending >= 0) {
+    __syncthreads();
+    store_outputs(pending);
+  }
+
   if (OUT && a.o.p) {  // tokens past the sequence's length
     E* o = at<E>(a.o, b, 0, (int64_t)j * a.nq + qh);
     const int64_t from = len > first * C ? len : first * C, to = last * C < sh.T ? last * C : sh.T;
-    for (int64_t t = from + wave; t < to; t += kChunkB / 64)
+    for (int64_t t = from + wave; t < to; t += NW)
       for (int col = ct0 + lane; col < ct0 + CT && col < a.Dv; col += 64) o[t * a.o.st + col] = (E)0.0f;
   }
   float* s1 = !OUT ? segments : !cut && a.s1 && qh == 0 ? a.s1 + state * a.Dk * a.Dv : nullptr;
   if (s1) {
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));  // addresses anew: those of the initial state are not kept over the walk
-    const int r0 = 8 * ((tid & 63) >> 4), c0 = ct0 + 16 * NCT * (tid >> 6) + 4 * NCT * ((tid & 15) >> 2) + (tid & 3);
+    const int r0 = 8 * ((tid & 63) >> 4), col = ct0 + 16 * (tid >> 6) + (tid & 15);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = r0 + 32 * kb + 4 * u + i, col = c0 + 4 * ct;
-            if (WHOLE || (r < a.Dk && col < a.Dv)) s1[r * a.Dv + col] = S[kb][u][ct][i];
-          }
+        for (int i = 0; i < 4; ++i) {
+          const int r = r0 + 32 * kb + 4 * u + i;
+          if (r < a.Dk && col < a.Dv) s1[r * a.Dv + col] = S[kb][u][i];
+        }
   }
 }
 
 // The segments' own states to the states before them, in place, and the last:
 //   before_0 = s0, before_{i+1} = g^(tokens of i) before_i + own_i
 constexpr int kJoinB = 256, kJoinAhead = 8;
-__global__ __launch_bounds__(kJoinB) void linattn_join(Shape sh, Jobs jobs, int32_t chunk) {
+__global__ __launch_bounds__(kJoinB) void linattn_join(Shape sh, Jobs jobs) {
   const Scan& a = jobs.scan[blockIdx.y];
   const int n = a.Dk * a.Dv, blocks = (n + kJoinB - 1) / kJoinB;
   const int64_t state = blockIdx.x / blocks, b = state / sh.Hs;
   const int e = (int)(blockIdx.x % blocks) * kJoinB + threadIdx.x;
   if (b >= sh.B || e >= n) return;
-  const int64_t len = length_of(sh, b), per = (int64_t)jobs.seg_chunks * chunk;
+  const int64_t len = length_of(sh, b), per = jobs.seg_tokens;
   const double lgd = (double)sh.log_decay[state - b * sh.Hs];
   const float whole = (float)exp(lgd * (double)per);
   float* buf = jobs.seg[blockIdx.y] + state * jobs.nseg * n + e;
@@ -753,17 +787,18 @@ void launch_one(const Shape& s, const Scan& a, hipStream_t st) {
     hipLaunchKernelGGL((linattn_one<E, 8>), grid, block, 0, st, s, a, tiles);
 }
 
-// Which chunk kernel a scan takes: key rows, column tiles of a wave.
+// Which chunk kernel a scan takes: key rows, waves (16 columns each).
 struct Class {
-  int dk, nct;
-  bool whole;
+  int dk, nw;
+  bool pieces;
 };
 
-Class class_of(const Scan& a) {
+Class class_of(const Scan& a, int32_t dtype) {
   Class c;
   c.dk = a.Dk <= 32 ? 32 : a.Dk <= 64 ? 64 : a.Dk <= 128 ? 128 : 256;
-  c.nct = c.dk == 128 ? 2 : 1;
-  c.whole = a.Dk == c.dk && a.Dv % (64 * c.nct) == 0;
+  c.nw = c.dk == 128 || (c.dk == 256 && dtype == DIFFOPT_BF16) ? 8 : 4;
+  const int vn = dtype == DIFFOPT_F32 ? 4 : 8;
+  c.pieces = a.Dk % vn == 0 && a.Dv % vn == 0;
   return c;
 }
 
@@ -772,27 +807,31 @@ Class class_of(const Scan& a) {
 // over (two share a compute unit); a cut costs one more read of k and v and the
 // segments' states, so there is none from half of that on, and no segment is
 // shorter than kMinChunks.
-constexpr int kFill = 512, kMinChunks = 4;
+constexpr int kFill = FILL, kMinChunks = MINC;
 
 struct Plan {
-  int32_t nseg, seg_chunks;
+  int32_t nseg;
+  int64_t seg_tokens;  // a multiple of kUnit
 };
 
-Plan plan_of(int64_t workgroups, int64_t T, int chunk) {
-  const int64_t chunks = (T + chunk - 1) / chunk;
+constexpr int kUnit = 64;  // whole chunks of every kernel
+
+Plan plan_of(int64_t workgroups, int64_t T) {
+  const int64_t units = (T + kUnit - 1) / kUnit;
   int64_t n = workgroups > 0 ? kFill / workgroups : 1;
-  if (n > chunks / kMinChunks) n = chunks / kMinChunks;
+  if (n > units / kMinChunks) n = units / kMinChunks;
   if (n < 1) n = 1;
-  const int64_t per = chunks > 0 ? (chunks + n - 1) / n : 1;
-  return Plan{(int32_t)((chunks + per - 1) / per > 1 ? (chunks + per - 1) / per : 1), (int32_t)per};
+  const int64_t per = units > 0 ? (units + n - 1) / n : 1;
+  n = (units + per - 1) / per;
+  return Plan{(int32_t)(n > 1 ? n : 1), per * kUnit};
 }
 
-int64_t col_tiles(const Scan& a) {
-  const int ct = 64 * class_of(a).nct;
+int64_t col_tiles(const Scan& a, int32_t dtype) {
+  const int ct = 16 * class_of(a, dtype).nw;
   return (a.Dv + ct - 1) / ct;
 }
 
-int64_t main_groups(const Shape& s, const Scan& a) { return s.B * s.Hs * a.nq * col_tiles(a); }
+int64_t main_groups(const Shape& s, const Scan& a, int32_t dtype) { return s.B * s.Hs * a.nq * col_tiles(a, dtype); }
 
 int64_t segment_bytes(const Shape& s, const Scan& a, const Plan& p) {
   return p.nseg > 1 ? (s.B * s.Hs * p.nseg * a.Dk * a.Dv * 4 + 255) / 256 * 256 : 0;
@@ -800,8 +839,8 @@ int64_t segment_bytes(const Shape& s, const Scan& a, const Plan& p) {
 
 Plan plan_of(const Shape& s, const Scan* a, int n, int32_t dtype) {
   int64_t w = 0;
-  for (int i = 0; i < n; ++i) w += main_groups(s, a[i]);
-  return plan_of(w, s.T, dtype == DIFFOPT_F32 ? ChunkOf<float>::C : ChunkOf<bf16>::C);
+  for (int i = 0; i < n; ++i) w += main_groups(s, a[i], dtype);
+  return plan_of(w, s.T);
 }
 
 // The scans of a call, as the sizes alone make them.
@@ -835,13 +874,13 @@ int64_t workspace_of(const Shape& s, const Scan* a, int n, int32_t dtype) {
   return bytes;
 }
 
-template <class E, int DK, int NCT, bool WHOLE>
+template <class E, int DK, int NW, bool PIECES>
 void launch_class(const Shape& s, const Jobs& jobs, int n, bool states, hipStream_t st) {
   constexpr int SPLIT = sizeof(E) == 2 ? 3 : 1;
   int64_t tiles = 0, main = 0, own = 0;
   bool keep = false;
   for (int i = 0; i < n; ++i) {
-    const int64_t c = col_tiles(jobs.scan[i]);
+    const int64_t c = col_tiles(jobs.scan[i], sizeof(E) == 4 ? DIFFOPT_F32 : DIFFOPT_BF16);
     tiles = c > tiles ? c : tiles;
     keep |= jobs.scan[i].s1 != nullptr && jobs.nseg == 1;
   }
@@ -851,11 +890,11 @@ void launch_class(const Shape& s, const Jobs& jobs, int n, bool states, hipStrea
     main = w * jobs.scan[i].nq > main ? w * jobs.scan[i].nq : main;
   }
   if (states)
-    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, SPLIT, false, WHOLE>), dim3((unsigned)own, n), dim3(kChunkB), 0, st, s, jobs, (int32_t)tiles);
-  else if (keep || !WHOLE || sizeof(E) == 4)
-    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, SPLIT, true, WHOLE>), dim3((unsigned)main, n), dim3(kChunkB), 0, st, s, jobs, (int32_t)tiles);
+    hipLaunchKernelGGL((linattn_chunks<E, DK, NW, SPLIT, false, PIECES>), dim3((unsigned)own, n), dim3(64 * NW), 0, st, s, jobs, (int32_t)tiles);
+  else if (keep || !PIECES || sizeof(E) == 4)
+    hipLaunchKernelGGL((linattn_chunks<E, DK, NW, SPLIT, true, PIECES>), dim3((unsigned)main, n), dim3(64 * NW), 0, st, s, jobs, (int32_t)tiles);
   else
-    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, sizeof(E) == 2 ? 2 : 1, true, WHOLE>), dim3((unsigned)main, n), dim3(kChunkB), 0, st, s, jobs,
+    hipLaunchKernelGGL((linattn_chunks<E, DK, NW, sizeof(E) == 2 ? 2 : 1, true, PIECES>), dim3((unsigned)main, n), dim3(64 * NW), 0, st, s, jobs,
                        (int32_t)tiles);
 }
 
@@ -863,25 +902,30 @@ template <class E>
 void launch_chunks(const Shape& s, const Jobs& jobs, int n, bool states, hipStream_t st) {
   // scans of one class share a launch
   bool done[3] = {false, false, false};
+  const int32_t dtype = sizeof(E) == 4 ? DIFFOPT_F32 : DIFFOPT_BF16;
   for (int i = 0; i < n; ++i) {
     if (done[i]) continue;
-    const Class c = class_of(jobs.scan[i]);
+    const Class c = class_of(jobs.scan[i], dtype);
     Jobs part = jobs;
     int k = 0;
     for (int l = i; l < n; ++l) {
-      const Class d = class_of(jobs.scan[l]);
-      if (done[l] || d.dk != c.dk || d.nct != c.nct || d.whole != c.whole || col_tiles(jobs.scan[l]) != col_tiles(jobs.scan[i])) continue;
+      const Class d = class_of(jobs.scan[l], dtype);
+      if (done[l] || d.dk != c.dk || d.pieces != c.pieces || col_tiles(jobs.scan[l], dtype) != col_tiles(jobs.scan[i], dtype)) continue;
       done[l] = true;
       part.scan[k] = jobs.scan[l];
       part.seg[k++] = jobs.seg[l];
     }
-#define DIFFOPT_CLASS(DK, NCT)                                        \
-  if (c.dk == DK && c.whole) launch_class<E, DK, NCT, true>(s, part, k, states, st); \
-  if (c.dk == DK && !c.whole) launch_class<E, DK, NCT, false>(s, part, k, states, st);
-    DIFFOPT_CLASS(32, 1)
-    DIFFOPT_CLASS(64, 1)
-    DIFFOPT_CLASS(128, 2)
-    DIFFOPT_CLASS(256, 1)
+#define DIFFOPT_CLASS(DK, NW)                                        \
+  if (c.dk == DK && c.pieces) launch_class<E, DK, NW, true>(s, part, k, states, st); \
+  if (c.dk == DK && !c.pieces) launch_class<E, DK, NW, false>(s, part, k, states, st);
+    DIFFOPT_CLASS(32, 4)
+    DIFFOPT_CLASS(64, 4)
+    DIFFOPT_CLASS(128, 8)
+    if constexpr (sizeof(E) == 2) {
+      DIFFOPT_CLASS(256, 8)
+    } else {
+      DIFFOPT_CLASS(256, 4)
+    }
 #undef DIFFOPT_CLASS
   }
 }
@@ -909,7 +953,7 @@ int run_scans(const char* who, const Shape& s, const Scan* a, const bool* run, i
   if (!aligned_to(workspace, 16)) return fail(DIFFOPT_EINVAL, "%s: the workspace is not 16-byte aligned", who);
   Jobs jobs{};
   jobs.nseg = p.nseg;
-  jobs.seg_chunks = p.seg_chunks;
+  jobs.seg_tokens = p.seg_tokens;
   char* at = static_cast<char*>(workspace);
   int k = 0, block = 0;
   for (int i = 0; i < n; ++i) {
@@ -926,7 +970,7 @@ int run_scans(const char* who, const Shape& s, const Scan* a, const bool* run, i
   if (p.nseg > 1) {
     f32 ? launch_chunks<float>(s, jobs, k, true, st) : launch_chunks<bf16>(s, jobs, k, true, st);
     const int64_t groups = s.B * s.Hs * ((block + kJoinB - 1) / kJoinB);
-    hipLaunchKernelGGL(linattn_join, dim3((unsigned)groups, k), dim3(kJoinB), 0, st, s, jobs, f32 ? ChunkOf<float>::C : ChunkOf<bf16>::C);
+    hipLaunchKernelGGL(linattn_join, dim3((unsigned)groups, k), dim3(kJoinB), 0, st, s, jobs);
   }
   f32 ? launch_chunks<float>(s, jobs, k, false, st) : launch_chunks<bf16>(s, jobs, k, false, st);
   return launch_status(who);
