@@ -209,19 +209,18 @@ __global__ __launch_bounds__(kStepB) void linattn_one(Shape s, Scan a, int32_t c
 //   O = W_q (Q S) + (P o M) V,  P = Q K^T,  M_ts = g^(t-s) for s <= t
 //   S = g^L S + K^T (W_k V)
 // where W_q, W_k are diagonal: g^(t+1), g^(L-1-s) forward and g^t, g^(L-s) back
-// in time (no power is ever negative).  A workgroup of NW waves walks the
-// chunks of one segment of a sequence; wave w owns 16 columns of the state, all
-// DK rows of them, in registers for the whole walk.
+// in time (no power is ever negative).  A workgroup of four waves walks the
+// chunks of one segment of a sequence; wave w owns 16 NCT columns of the state,
+// all DK rows of them, in registers for the whole walk.
 //
 // Fragments: v_mfma 16x16 takes row (or column) lane % 16 and, of a block of 32
 // along the contraction, 8 elements per 16-lane group g = lane / 16; it returns
-// column lane % 16, rows 4 g .. + 4.  The rows of two state tiles are numbered
-// so that a lane's eight results are elements 32 b + 8 g .. + 8 of the key axis:
-// the state is an operand of Q S as it lies in the registers, Q and K are read
-// in 16-byte pieces.  Tokens are numbered 32 b + 4 g .. + 4 and + 16: P^T as it
-// is computed is an operand of P V, and V and K^T come out of LDS transposed
-// four tokens at a time (ds_read_b64_tr_b16).  The products are computed
-// transposed, so that a lane stores 4 neighbouring elements of one token.
+// column lane % 16, rows 4 g .. + 4.  Along tokens and along the state's rows a
+// block of 32 is numbered 4 g .. + 4 and 16 + 4 g .. + 4, so that two results are
+// an operand as they lie in the registers: P^T as computed for P V, the state for
+// Q S.  V and K^T come out of LDS transposed, four tokens at a time
+// (ds_read_b64_tr_b16).  The products are computed transposed, so that a lane
+// holds 4 neighbouring elements of one token's output.
 //
 // In bf16 the scores and the state are rounded where they enter a product (the
 // outputs are bf16 too); the state itself is fp32 and its update takes W_k V in
@@ -248,52 +247,56 @@ __device__ __forceinline__ f32x4 mfma32(Frag<float>::type a, Frag<float>::type b
   return c;
 }
 
-// A matrix of C rows of W elements in LDS, as loads that go there directly write
-// it: a wave's 64 pieces of 16 bytes in the order of its lanes make a block of RB
-// rows, one piece more separates blocks, and within its row a piece lies at its
-// number xor mix(row).  Then 16 rows at one piece fall on 16 different pieces of
-// the banks, and 8 rows of 4 pieces, half of each read, on each of them twice (the
-// least).
+// A matrix of rows of W elements in LDS, as loads that go there directly write it:
+// a wave's 64 pieces of 16 bytes follow one another in the order of its lanes.
+// Within its row a piece lies at its number xor mix(row), so that 16 rows at one
+// piece, and the rows that a transposing read takes together, fall on different
+// banks.
 template <class E, int W>
 struct Tile {
-  static constexpr int VN = 16 / (int)sizeof(E), NP = W / VN, RB = 64 / NP, BLOCK = 65 * VN;
+  static constexpr int VN = 16 / (int)sizeof(E), NP = W / VN, RB = 64 / NP, BLOCK = 64 * VN;
   static_assert(NP >= 4 && NP <= 64 && RB * NP == 64, "rows of 64 bytes to 1 KiB");
-  static constexpr int elements(int rows) { return rows / RB * BLOCK; }
+  static constexpr int elements(int rows) { return rows * W; }
   typedef typename Frag<E>::type frag;
 
   static __device__ __forceinline__ constexpr int mix(int r) {
-    return NP == 64 ? 0 : NP == 32 ? (r & 1) << 3 : NP == 16 ? (r & 3) << 2 : NP == 8 ? (r & 6) : (r >> 2) & 3;
+    if (sizeof(E) == 4) return NP >= 16 ? (r & 12) | (r & 3) : NP == 8 ? (r >> 1) & 7 : (r >> 2) & 3;
+    return NP >= 16 ? ((r & 3) << 2) | ((r >> 1) & 2) | ((r >> 3) & 1) : NP == 8 ? (r & 6) | ((r >> 3) & 1) : ((r >> 1) & 2) | ((r >> 3) & 1);
   }
-  static __device__ __forceinline__ constexpr int at(int r, int piece) { return r / RB * BLOCK + (r % RB * NP + (piece ^ mix(r))) * VN; }
+  static __device__ __forceinline__ constexpr int at(int r, int piece) { return r * W + (piece ^ mix(r)) * VN; }
+  // element c of row r
+  static __device__ __forceinline__ constexpr int element(int r, int c) { return at(r, c / VN) + c % VN; }
 
-  // elements col .. + 8 (col a multiple of 8) of row r
-  static __device__ __forceinline__ frag row(const E* base, int r, int col) {
-    const E* p = base + at(r, col / VN);
+  // elements 32 b + 8 g .. + 8 of row r
+  static __device__ __forceinline__ frag row(const E* base, int r, int b, int g) {
     if constexpr (sizeof(E) == 2) {
-      return *reinterpret_cast<const frag*>(p);
+      return *reinterpret_cast<const frag*>(base + at(r, 4 * b + g));
     } else {
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(base + at(r, 8 * b + 2 * g)), hi = *reinterpret_cast<const f32x4*>(base + at(r, 8 * b + 2 * g + 1));
       return frag{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     }
   }
-
-  // element col + (m / 4) STEP + m % 4, m = lane % 16, of rows 32 b + 4 g .. + 4 and 16 further
-  template <int STEP>
+  // elements 32 b + 4 g .. + 4 and 16 further of row r
+  static __device__ __forceinline__ frag halves(const E* base, int r, int b, int g) {
+    typedef E four __attribute__((ext_vector_type(4)));
+    const four lo = *reinterpret_cast<const four*>(base + element(r, 32 * b + 4 * g));
+    const four hi = *reinterpret_cast<const four*>(base + element(r, 32 * b + 16 + 4 * g));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  // element col + m, m = lane % 16, of rows 32 b + 4 g .. + 4 and 16 further
   static __device__ __forceinline__ frag column(const E* base, int b, int col, int g, int m) {
     if constexpr (sizeof(E) == 2) {
       typedef short s16x4 __attribute__((ext_vector_type(4)));
       typedef short s16x8 __attribute__((ext_vector_type(8)));
       typedef __attribute__((address_space(3))) s16x4 lds4;
-      const int r = 32 * b + 4 * g + (m >> 2), c = col + STEP * (m & 3);
-      const E *p = base + at(r, c / VN) + c % VN, *q = base + at(r + 16, c / VN) + c % VN;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(q));
+      const int r = 32 * b + 4 * g + (m >> 2), c = col + 4 * (m & 3);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(base + element(r, c)));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(base + element(r + 16, c)));
       return __builtin_bit_cast(frag, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-      const int c = col + STEP * (m >> 2) + (m & 3);
       frag f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = base[at(32 * b + (j >> 2) * 16 + 4 * g + (j & 3), c / VN) + c % VN];
+      for (int j = 0; j < 8; ++j) f[j] = base[element(32 * b + (j >> 2) * 16 + 4 * g + (j & 3), col + m)];
       return f;
     }
   }
@@ -354,33 +357,35 @@ struct ChunkOf {
 #define MINC 4
 #endif
 
+constexpr int kWaves = 4, kChunkB = 64 * kWaves;
+
 // One matrix of a chunk on its way to LDS (element `at` of what begins at `lds`,
-// LDS address `address`), by a workgroup of NW waves: rows
+// LDS address `address`), by a workgroup of four waves: rows
 // 0 .. L - 1 from `head`, st elements apart (negative: back in time), columns
 // col0 .. + W of `width`; rows from L on become zero, columns past the width stay
 // zero from before.  PIECES: the width is whole pieces; else through registers,
 // element by element.
-template <class E, int W, int C, int NW, bool PIECES>
+template <class E, int W, int C, bool PIECES>
 __device__ __forceinline__ void stage(E* lds, uint32_t address, int at, const E* head, int64_t st, int L, int col0, int width, int lane, int wave) {
   typedef Tile<E, W> T;
-  constexpr int N = C / T::RB / NW;  // blocks of a wave
-  static_assert(N * NW * T::RB == C, "whole blocks for every wave");
+  constexpr int N = C / T::RB / kWaves;  // blocks of a wave
+  static_assert(N * kWaves * T::RB == C, "whole blocks for every wave");
   typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
+  const int r0 = wave * T::RB + lane / T::NP;
+  const E* p = head + r0 * st;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int block = wave + NW * i, r = block * T::RB + lane / T::NP, c = col0 + ((lane % T::NP) ^ T::mix(r)) * T::VN;
-    const int to = at + block * T::BLOCK;
+    const int r = r0 + i * (kWaves * T::RB), c = col0 + ((lane % T::NP) ^ T::mix(r)) * T::VN, to = at + (wave + kWaves * i) * T::BLOCK;
     if (PIECES) {
       if (c < width) {
         if (r < L)
-          load_to_lds(head + r * st + c, address + to * (int)sizeof(E));
+          load_to_lds(p + c, address + to * (int)sizeof(E));
         else
           *reinterpret_cast<whole*>(lds + to + lane * T::VN) = whole{};
       }
     } else {
       whole x{};
       if (r < L) {
-        const E* p = head + r * st;
 #pragma unroll
         for (int e = 0; e < T::VN; ++e) {
           const E y = p[c + e < width ? c + e : 0];
@@ -389,26 +394,28 @@ __device__ __forceinline__ void stage(E* lds, uint32_t address, int at, const E*
       }
       *reinterpret_cast<whole*>(lds + to + lane * T::VN) = x;
     }
+    p += (kWaves * T::RB) * st;
   }
 }
 
-// What a chunk kernel keeps in LDS: two buffers of Q, K and V (one is read while
-// the next chunk arrives in the other), the scores' operands, the outputs.
-template <class E, int DK, int NW, bool OUT>
+// What a chunk kernel keeps in LDS: K, V, Q of a chunk, the scores' operands, the
+// outputs.
+template <class E, int DK, int NCT, bool OUT>
 struct ChunkLds {
-  static constexpr int C = ChunkOf<E, DK>::C, NT = C / 16, NB = C / 32, CT = 16 * NW;
+  static constexpr int C = ChunkOf<E, DK>::C, NT = C / 16, NB = C / 32, CT = 64 * NCT;
   static constexpr int kq = Tile<E, DK>::elements(C), kv = Tile<E, CT>::elements(C);
-  static constexpr int buffer = (OUT ? 2 : 1) * kq + kv;  // K, V, then Q
-  static constexpr int orow = CT + 16 / (int)sizeof(E);   // elements from an output's row to the next
-  E in[2][buffer];
+  static constexpr int all = (OUT ? 2 : 1) * kq + kv;
+  static constexpr int orow = CT + 16 / (int)sizeof(E);  // elements from an output's row to the next
+  E in[all];
   typename Frag<E>::type P[OUT ? NT * NB * 64 : 1];
   E out[OUT ? C * orow : 1];
 };
 
-template <class E, int DK, int NW, int SPLIT, bool OUT, bool PIECES>
-__global__ __launch_bounds__(64 * NW, (OUT || DK > 128 ? 1 : NW / 2)) void linattn_chunks(Shape sh, Jobs jobs, int32_t col_tiles) {
-  typedef ChunkLds<E, DK, NW, OUT> Lds;
-  constexpr int C = Lds::C, NT = Lds::NT, NB = Lds::NB, KB = DK / 32, CT = Lds::CT, B = 64 * NW;
+template <class E, int DK, int NCT, int SPLIT, bool OUT, bool PIECES>
+__global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 1024 ? 1 : 2)) void linattn_chunks(Shape sh, Jobs jobs,
+                                                                                                               int32_t col_tiles) {
+  typedef ChunkLds<E, DK, NCT, OUT> Lds;
+  constexpr int C = Lds::C, NT = Lds::NT, NB = Lds::NB, KB = DK / 32, CT = Lds::CT, B = kChunkB;
   typedef typename Frag<E>::type frag;
   typedef Tile<E, DK> KTile;
   typedef Tile<E, CT> VTile;
@@ -425,7 +432,7 @@ __global__ __launch_bounds__(64 * NW, (OUT || DK > 128 ? 1 : NW / 2)) void linat
   const int64_t state = x / nq, b = state / sh.Hs;
   if (b >= sh.B) return;  // the launch's scans differ in heads
   const int j = (int)(state - b * sh.Hs);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, m = lane & 15;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g_ = lane >> 4, m_ = lane & 15;
   const int64_t len = length_of(sh, b);
   const double lgd = (double)sh.log_decay[j];
   const float lg2 = (float)(lgd * 1.4426950408889634074);
@@ -437,25 +444,27 @@ __global__ __launch_bounds__(64 * NW, (OUT || DK > 128 ? 1 : NW / 2)) void linat
   const int64_t live = (len + C - 1) / C;  // chunks with tokens
   const int64_t end = last < live ? last : live;
 
-  // the state: tile (kb, u); a lane holds column 16 wave + m of the tile, rows
-  // 32 kb + 8 g + 4 u + i
+  // the state: tile (kb, u), column tile ct; a lane holds column 16 (NCT wave + ct)
+  // + m, rows 32 kb + 16 u + 4 g + i
   const bool cut = jobs.nseg > 1;
   float* segments = cut ? jobs.seg[blockIdx.y] + (state * jobs.nseg + seg) * a.Dk * a.Dv : nullptr;
-  f32x4 S[KB][2];
+  const int wcol = 16 * NCT * wave;
+  f32x4 S[KB][2][NCT];
   {
     const float* s0 = !OUT ? nullptr : cut ? segments : a.s0 ? a.s0 + state * a.Dk * a.Dv : nullptr;
     const bool flip = !cut && a.flip;
-    const int c = ct0 + 16 * wave + m;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 8 * g + 32 * kb + 4 * u + i;
-          const bool in = s0 && r < a.Dk && c < a.Dv;
-          S[kb][u][i] = in ? s0[flip ? c * a.Dk + r : r * a.Dv + c] : 0.0f;
-        }
+        for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = 32 * kb + 16 * u + 4 * g_ + i, c = ct0 + wcol + 16 * ct + m_;
+            const bool in = s0 && r < a.Dk && c < a.Dv;
+            S[kb][u][ct][i] = in ? s0[flip ? c * a.Dk + r : r * a.Dv + c] : 0.0f;
+          }
   }
 
   // g^C rounds once; what that leaves out grows with every chunk and is made
@@ -470,7 +479,7 @@ __global__ __launch_bounds__(64 * NW, (OUT || DK > 128 ? 1 : NW / 2)) void linat
   // lanes (scalar registers): of the outputs of the state, qw g^(16 t), and of the
   // values that enter it, kw g^(...) (whole chunks).
   const float ps = a.qs * a.ks;
-  const float qw = a.qs * power(lg2, m + 1 - back), kw = a.ks * power(lg2, 12 - 4 * g);
+  const float qw = a.qs * power(lg2, m_ + 1 - back), kw = a.ks * power(lg2, 12 - 4 * g_);
   float qt[NT], ks[NB][8];
 #pragma unroll
   for (int t = 0; t < NT; ++t) qt[t] = uniform(power(lg2, 16 * t));
@@ -487,7 +496,7 @@ __global__ __launch_bounds__(64 * NW, (OUT || DK > 128 ? 1 : NW / 2)) void linat
   auto valid = [&](int64_t c) { return (int)(len - c * C < C ? len - c * C : C); };
   if (PIECES && (a.Dk < DK || a.Dv - ct0 < CT)) {  // columns past the widths
     typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
-    for (int i = threadIdx.x; i < 2 * Lds::buffer / KTile::VN; i += B) reinterpret_cast<whole*>(&lds.in[0][0])[i] = whole{};
+    for (int i = threadIdx.x; i < Lds::all / KTile::VN; i += B) reinterpret_cast<whole*>(lds.in)[i] = whole{};
     __syncthreads();
   }
 
@@ -506,197 +515,240 @@ __global__ __launch_bounds__(64 * NW, (OUT || DK > 128 ? 1 : NW / 2)) void linat
     }
   };
 
-  // item n of the walk: k/v head n % nk of chunk first + n / nk
-  int h = -1, h_next = 0, turn = 0;
-  int64_t c = first, c_next = first, pending = -1;
-  f32x4 O[NT];
-  while (true) {
-    // the item has arrived, and every wave is done with the one before it
+  E *sK = lds.in, *sV = sK + Lds::kq, *sQ = sV + Lds::kv;
+  frag* sP = lds.P;
+  const uint32_t address = lds_address(sK);
+  auto stage_k = [&](int64_t c, int h) {
+    stage<E, DK, C, PIECES>(sK, address, 0, k0 + c * C * kst + h * a.k.sh, kst, valid(c), 0, a.Dk, lane, wave);
+  };
+  auto stage_vq = [&](int64_t c, int h) {
+    stage<E, CT, C, PIECES>(sK, address, Lds::kq, v0 + c * C * vst + h * a.v.sh, vst, valid(c), ct0, a.Dv, lane, wave);
+    if (OUT && h == 0) stage<E, DK, C, PIECES>(sK, address, Lds::kq + Lds::kv, q0 + c * C * qst, qst, valid(c), 0, a.Dk, lane, wave);
+  };
+
+  // item n of the walk: k/v head n % nk of chunk first + n / nk.  V and Q of the
+  // next item are on their way from the second barrier of this one on, K from its
+  // end on; the other workgroup of the compute unit works meanwhile.
+  int64_t pending = -1;
+  f32x4 O[NT][NCT];
+  if (first < end) stage_vq(first, 0);
+  int h = 0;
+  for (int64_t c = first; c < end;) {
+    const int L = valid(c);
+    __syncthreads();
+    stage_k(c, h);
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
     __syncthreads();
-    if (c_next < end) {
-      const int L = valid(c_next);
-      E* in = &lds.in[0][0];
-      const uint32_t address = lds_address(in);
-      const int to = (turn ^ (h >= 0)) * Lds::buffer;
-      stage<E, DK, C, NW, PIECES>(in, address, to, k0 + c_next * C * kst + h_next * a.k.sh, kst, L, 0, a.Dk, lane, wave);
-      stage<E, CT, C, NW, PIECES>(in, address, to + Lds::kq, v0 + c_next * C * vst + h_next * a.v.sh, vst, L, ct0, a.Dv, lane, wave);
-      if (OUT) stage<E, DK, C, NW, PIECES>(in, address, to + Lds::kq + Lds::kv, q0 + c_next * C * qst, qst, L, 0, a.Dk, lane, wave);
-    }
     if (OUT && PIECES && pending >= 0) {
       store_outputs(pending);
       pending = -1;
     }
-    if (h >= 0) {
-      const E *sK = &lds.in[0][0] + turn * Lds::buffer, *sV = sK + Lds::kq, *sQ = sV + Lds::kv;
-      frag* sP = lds.P;
-      const int L = valid(c);
-      // what follows from these is made anew in every chunk: kept over the walk,
-      // it would cost the registers of a second workgroup
-      int gap0 = m - 4 * g, g4 = 4 * g;
-      float kwc = kw, qwc = qw;
-      asm volatile("" : "+v"(gap0), "+v"(g4), "+v"(kwc), "+v"(qwc));
-      if (OUT) {
-        // P^T of this wave's tiles, masked and decayed, as operands of P V
-        constexpr int PER = NT * NT / NW > 0 ? NT * NT / NW : 1;  // tiles, of one query tile, that a wave computes
-        const int tq = wave * PER / NT, tk0 = wave * PER % NT;
-        f32x4 P[PER];
-        if (tq < NT) {
+    // what follows from these is made anew in every chunk: kept over the walk, it
+    // would cost the registers of a second workgroup
+    int m = m_, g = g_;
+    float kwc = kw, qwc = qw;
+    asm volatile("" : "+v"(m), "+v"(g), "+v"(kwc), "+v"(qwc));
+    const int gap0 = m - 4 * g;
+    if (OUT) {
+      // P^T by blocks of 16 queries and 32 keys, masked and decayed, as operands of
+      // P V; of the six of 64 tokens two waves take three tiles each, two take two
+#pragma unroll 1
+      for (int n = 0; n < (NT == 4 && wave < 2 ? 2 : 1); ++n) {
+        const int tq = NT == 2 ? wave : wave == 0 ? n : wave == 1 ? 2 : 3, nb = NT == 2 || wave == 0 ? 0 : wave == 1 ? n : wave - 2;
+        if (NT == 2 && wave >= 2) break;
+        f32x4 P[2];
 #pragma unroll
-          for (int i = 0; i < PER; ++i) {
-            const int apart = tq - tk0 - i;
-            P[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            if (apart >= 0) {
+        for (int i = 0; i < 2; ++i) {
+          const int apart = tq - 2 * nb - i;
+          P[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+          if (apart >= 0) {
 #pragma unroll
-              for (int kb = 0; kb < KB; ++kb)
-                P[i] = mfma32(KTile::row(sK + KTile::elements(16) * tk0, 16 * i + m, 32 * kb + 8 * g),
-                              KTile::row(sQ + KTile::elements(16) * tq, m, 32 * kb + 8 * g), P[i]);
-              if (apart == 0) {
+            for (int kb = 0; kb < KB; ++kb)
+              P[i] = mfma32(KTile::row(sK + KTile::elements(32) * nb, 16 * i + m, kb, g), KTile::row(sQ + KTile::elements(16) * tq, m, kb, g), P[i]);
+            if (apart == 0) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) P[i][e] = gap0 >= e ? P[i][e] * (ps * power(lg2, gap0 - e)) : 0.0f;
-              } else {
+              for (int e = 0; e < 4; ++e) P[i][e] = gap0 >= e ? P[i][e] * (ps * power(lg2, gap0 - e)) : 0.0f;
+            } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) P[i][e] *= ps * power(lg2, gap0 + 16 * apart - e);
-              }
+              for (int e = 0; e < 4; ++e) P[i][e] *= ps * power(lg2, gap0 + 16 * apart - e);
             }
           }
-          if constexpr (PER >= 2) {
-#pragma unroll
-            for (int kb = 0; kb < PER / 2; ++kb) sP[(tq * NB + tk0 / 2 + kb) * 64 + lane] = pack(P[2 * kb], P[2 * kb + 1], E());
-          } else {  // half a block: four of a lane's eight elements
-            typedef E four __attribute__((ext_vector_type(4)));
-            reinterpret_cast<four*>(&sP[(tq * NB + tk0 / 2) * 64 + lane])[tk0 & 1] = __builtin_convertvector(P[0], four);
-          }
         }
+        sP[(tq * NB + nb) * 64 + lane] = pack(P[0], P[1], E());
       }
+    }
 
-      frag V[NB];
+    asm volatile("" : "+v"(m), "+v"(g));
+    frag V[NB][NCT];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) V[nb] = VTile::template column<4>(sV, nb, 16 * wave, g, m);
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct) V[nb][ct] = VTile::column(sV, nb, wcol + 16 * ct, g, m);
 
-      if (OUT) {
-        // zeros times the values: zero unless one is infinite or NaN
-        f32x4 odd{0.0f, 0.0f, 0.0f, 0.0f};
+    bool odd = false;
+    if (OUT) {
+      // zeros times the values: zero unless one is infinite or NaN
+      f32x4 z{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct) {
           if constexpr (sizeof(E) == 2) {
-            odd = mfma32(V[nb], frag{}, odd);
+            z = mfma32(V[nb][ct], frag{}, z);
           } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) odd[e & 3] = fmaf(V[nb][e], 0.0f, odd[e & 3]);
+            for (int e = 0; e < 8; ++e) z[e & 3] = fmaf(V[nb][ct][e], 0.0f, z[e & 3]);
           }
         }
-        if (h == 0) {
+      odd = !__all(z[0] + z[1] + z[2] + z[3] == 0.0f);
+      if (h == 0) {
 #pragma unroll
-          for (int t = 0; t < NT; ++t) O[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int kb = 0; kb < KB; ++kb) {
-            const frag s = pack(S[kb][0], S[kb][1], E());
+          for (int ct = 0; ct < NCT; ++ct) O[t][ct] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int t = 0; t < NT; ++t) O[t] = mfma32(s, KTile::row(sQ, 16 * t + m, 32 * kb + 8 * g), O[t]);
+        for (int kb = 0; kb < KB; ++kb) {
+          frag s[NCT];
+#pragma unroll
+          for (int ct = 0; ct < NCT; ++ct) s[ct] = pack(S[kb][0][ct], S[kb][1][ct], E());
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const frag q = KTile::halves(sQ, 16 * t + m, kb, g);
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(s[ct], q, O[t][ct]);
           }
-#pragma unroll
-          for (int t = 0; t < NT; ++t) O[t] *= qwc * qt[t];
         }
-        __syncthreads();
-        if (__all(odd[0] + odd[1] + odd[2] + odd[3] == 0.0f)) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int ct = 0; ct < NCT; ++ct) O[t][ct] *= qwc * qt[t];
+      }
+    }
+    const bool decay = h == 0;
+    const bool last_head = h + 1 == a.nk;
+    const int h_next = last_head ? 0 : h + 1;
+    const int64_t c_next = last_head ? c + 1 : c;
+    __syncthreads();
+    if (c_next < end) stage_vq(c_next, h_next);
+    if (OUT) {
+      if (!odd) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int nb = 0; nb <= t / 2; ++nb) {
+            const frag p = sP[(t * NB + nb) * 64 + lane];
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(V[nb][ct], p, O[t][ct]);
+          }
+      } else {
+        // a product with the zeros of the mask would carry an infinity or NaN to
+        // earlier tokens, so the sum stops at the token
+        asm volatile("" : "+v"(m), "+v"(g));
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+#pragma unroll 1
+            for (int sg = 0; sg < 4; ++sg) {
+              const int s = 32 * nb + (e >> 2) * 16 + 4 * sg + (e & 3);
+#pragma unroll
+              for (int t = 0; t < NT; ++t) {
+                const float p = s <= 16 * t + m ? (float)reinterpret_cast<const E*>(&sP[(t * NB + nb) * 64 + sg * 16 + m])[e] : 0.0f;
+#pragma unroll
+                for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) {
+                    const float v = __shfl((float)V[nb][ct][e], sg * 16 + 4 * g + i, 64);
+                    if (s <= 16 * t + m) O[t][ct][i] = fmaf(p, v, O[t][ct][i]);
+                  }
+              }
+            }
+      }
+      if (last_head && a.o.p) {
+        if (PIECES) {
+          typedef E four __attribute__((ext_vector_type(4)));
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int nb = 0; nb <= t / 2; ++nb) O[t] = mfma32(V[nb], sP[(t * NB + nb) * 64 + lane], O[t]);
+            for (int ct = 0; ct < NCT; ++ct)
+              *reinterpret_cast<four*>(lds.out + (16 * t + m) * Lds::orow + wcol + 16 * ct + 4 * g) = __builtin_convertvector(O[t][ct], four);
+          pending = c;
         } else {
-          // a product with the zeros of the mask would carry an infinity or NaN
-          // to earlier tokens, so the sum stops at the token
-#pragma unroll 1
-          for (int s = 0; s < L; ++s) {
-            const E* p = reinterpret_cast<const E*>(&sP[(s >> 5) * 64 + ((s >> 2) & 3) * 16 + m]) + ((s >> 4) & 1) * 4 + (s & 3);
-            const E* v = sV + VTile::at(s, (16 * wave + 4 * g) / VTile::VN) + (16 * wave + 4 * g) % VTile::VN;
+          const int col = ct0 + wcol + 4 * g;
+          E* p = at<E>(a.o, b, back ? len - 1 : 0, (int64_t)j * a.nq + qh) + (c * C + m) * dir * a.o.st + col;
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-              if (s <= 16 * t + m) {
+          for (int t = 0; t < NT; ++t) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) O[t][i] = fmaf((float)p[t * NB * 64 * 8], (float)v[i], O[t][i]);
-              }
-          }
-        }
-        if (h + 1 == a.nk && a.o.p) {
-          if (PIECES) {
-            typedef E four __attribute__((ext_vector_type(4)));
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-              *reinterpret_cast<four*>(lds.out + (16 * t + m) * Lds::orow + 16 * wave + 4 * g) = __builtin_convertvector(O[t], four);
-            pending = c;
-          } else {
-            const int col = ct0 + 16 * wave + 4 * g;
-            E* p = at<E>(a.o, b, back ? len - 1 : 0, (int64_t)j * a.nq + qh) + (c * C + m) * dir * a.o.st + col;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
+            for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
               for (int i = 0; i < 4; ++i)
-                if (16 * t + m < L && col + i < a.Dv) p[i] = (E)O[t][i];
-              p += 16 * dir * a.o.st;
-            }
+                if (16 * t + m < L && col + 16 * ct + i < a.Dv) p[16 * ct + i] = (E)O[t][ct][i];
+            p += 16 * dir * a.o.st;
           }
         }
       }
+    }
 
-      if (h == 0) {
-        if (L == C && ((c - first) & 7) == 7) {
-#pragma unroll
-          for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) S[kb][u][i] = fmaf(S[kb][u][i], g8_hi, S[kb][u][i] * g8_lo);
-        } else {
-          const float d = L < C ? gl : gc;
-#pragma unroll
-          for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) S[kb][u] *= d;
-        }
-      }
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        float w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = kwc * ks[nb][e];
-        if (L < C) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int n = L - 1 + back - g4 - (32 * nb + (e >> 2) * 16 + (e & 3));
-            w[e] = n >= back ? a.ks * power(lg2, n) : 0.0f;
-          }
-        }
-        // the weighted values in SPLIT parts, each the rounding of what is left
-        frag part[SPLIT];
-        typename Frag<float>::type y;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = (float)V[nb][e] * w[e];
-#pragma unroll
-        for (int p = 0; p < SPLIT; ++p) {
-          part[p] = __builtin_convertvector(y, frag);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] -= (float)part[p][e];
-        }
+    asm volatile("" : "+v"(m), "+v"(g));
+    if (decay) {
+      if (L == C && ((c - first) & 7) == 7) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const frag k = KTile::template column<8>(sK, nb, 32 * kb + 4 * u, g, m);
+          for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int p = 0; p < SPLIT; ++p) S[kb][u] = mfma32(k, part[p], S[kb][u]);
-          }
+            for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) S[kb][u][ct][i] = fmaf(S[kb][u][ct][i], g8_hi, S[kb][u][ct][i] * g8_lo);
+      } else {
+        const float d = L < C ? gl : gc;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) S[kb][u][ct] *= d;
       }
     }
-    if (c_next >= end) break;
-    turn ^= h >= 0;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      float w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = kwc * ks[nb][e];
+      if (L < C) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int n = L - 1 + back - 4 * g - (32 * nb + (e >> 2) * 16 + (e & 3));
+          w[e] = n >= back ? a.ks * power(lg2, n) : 0.0f;
+        }
+      }
+      // the weighted values in SPLIT parts, each the rounding of what is left
+      frag part[SPLIT][NCT];
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct) {
+        typename Frag<float>::type y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = (float)V[nb][ct][e] * w[e];
+#pragma unroll
+        for (int p = 0; p < SPLIT; ++p) {
+          part[p][ct] = __builtin_convertvector(y, frag);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] -= (float)part[p][ct][e];
+        }
+      }
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const frag k = KTile::column(sK, nb, 32 * kb + 16 * u, g, m);
+#pragma unroll
+          for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+            for (int p = 0; p < SPLIT; ++p) S[kb][u][ct] = mfma32(k, part[p][ct], S[kb][u][ct]);
+        }
+    }
     c = c_next;
     h = h_next;
-    if (++h_next == a.nk) {
-      h_next = 0;
-      ++c_next;
-    }
   }
 
   if (OUT && PIECES && pending >= 0) {
@@ -707,23 +759,25 @@ __global__ __launch_bounds__(64 * NW, (OUT || DK > 128 ? 1 : NW / 2)) void linat
   if (OUT && a.o.p) {  // tokens past the sequence's length
     E* o = at<E>(a.o, b, 0, (int64_t)j * a.nq + qh);
     const int64_t from = len > first * C ? len : first * C, to = last * C < sh.T ? last * C : sh.T;
-    for (int64_t t = from + wave; t < to; t += NW)
+    for (int64_t t = from + wave; t < to; t += kWaves)
       for (int col = ct0 + lane; col < ct0 + CT && col < a.Dv; col += 64) o[t * a.o.st + col] = (E)0.0f;
   }
   float* s1 = !OUT ? segments : !cut && a.s1 && qh == 0 ? a.s1 + state * a.Dk * a.Dv : nullptr;
   if (s1) {
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));  // addresses anew: those of the initial state are not kept over the walk
-    const int r0 = 8 * ((tid & 63) >> 4), col = ct0 + 16 * (tid >> 6) + (tid & 15);
+    const int r0 = 4 * ((tid & 63) >> 4), c0 = ct0 + 16 * NCT * (tid >> 6) + (tid & 15);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = r0 + 32 * kb + 4 * u + i;
-          if (r < a.Dk && col < a.Dv) s1[r * a.Dv + col] = S[kb][u][i];
-        }
+        for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = r0 + 32 * kb + 16 * u + i, col = c0 + 16 * ct;
+            if (r < a.Dk && col < a.Dv) s1[r * a.Dv + col] = S[kb][u][ct][i];
+          }
   }
 }
 
@@ -787,16 +841,16 @@ void launch_one(const Shape& s, const Scan& a, hipStream_t st) {
     hipLaunchKernelGGL((linattn_one<E, 8>), grid, block, 0, st, s, a, tiles);
 }
 
-// Which chunk kernel a scan takes: key rows, waves (16 columns each).
+// Which chunk kernel a scan takes: key rows, column tiles of a wave.
 struct Class {
-  int dk, nw;
+  int dk, nct;
   bool pieces;
 };
 
 Class class_of(const Scan& a, int32_t dtype) {
   Class c;
   c.dk = a.Dk <= 32 ? 32 : a.Dk <= 64 ? 64 : a.Dk <= 128 ? 128 : 256;
-  c.nw = c.dk == 128 || (c.dk == 256 && dtype == DIFFOPT_BF16) ? 8 : 4;
+  c.nct = c.dk == 128 || (c.dk == 256 && dtype == DIFFOPT_BF16) ? 2 : 1;
   const int vn = dtype == DIFFOPT_F32 ? 4 : 8;
   c.pieces = a.Dk % vn == 0 && a.Dv % vn == 0;
   return c;
@@ -827,7 +881,7 @@ Plan plan_of(int64_t workgroups, int64_t T) {
 }
 
 int64_t col_tiles(const Scan& a, int32_t dtype) {
-  const int ct = 16 * class_of(a, dtype).nw;
+  const int ct = 64 * class_of(a, dtype).nct;
   return (a.Dv + ct - 1) / ct;
 }
 
@@ -874,7 +928,7 @@ int64_t workspace_of(const Shape& s, const Scan* a, int n, int32_t dtype) {
   return bytes;
 }
 
-template <class E, int DK, int NW, bool PIECES>
+template <class E, int DK, int NCT, bool PIECES>
 void launch_class(const Shape& s, const Jobs& jobs, int n, bool states, hipStream_t st) {
   constexpr int SPLIT = sizeof(E) == 2 ? 3 : 1;
   int64_t tiles = 0, main = 0, own = 0;
@@ -890,11 +944,11 @@ void launch_class(const Shape& s, const Jobs& jobs, int n, bool states, hipStrea
     main = w * jobs.scan[i].nq > main ? w * jobs.scan[i].nq : main;
   }
   if (states)
-    hipLaunchKernelGGL((linattn_chunks<E, DK, NW, SPLIT, false, PIECES>), dim3((unsigned)own, n), dim3(64 * NW), 0, st, s, jobs, (int32_t)tiles);
+    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, SPLIT, false, PIECES>), dim3((unsigned)own, n), dim3(kChunkB), 0, st, s, jobs, (int32_t)tiles);
   else if (keep || !PIECES || sizeof(E) == 4)
-    hipLaunchKernelGGL((linattn_chunks<E, DK, NW, SPLIT, true, PIECES>), dim3((unsigned)main, n), dim3(64 * NW), 0, st, s, jobs, (int32_t)tiles);
+    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, SPLIT, true, PIECES>), dim3((unsigned)main, n), dim3(kChunkB), 0, st, s, jobs, (int32_t)tiles);
   else
-    hipLaunchKernelGGL((linattn_chunks<E, DK, NW, sizeof(E) == 2 ? 2 : 1, true, PIECES>), dim3((unsigned)main, n), dim3(64 * NW), 0, st, s, jobs,
+    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, sizeof(E) == 2 ? 2 : 1, true, PIECES>), dim3((unsigned)main, n), dim3(kChunkB), 0, st, s, jobs,
                        (int32_t)tiles);
 }
 
@@ -915,16 +969,16 @@ void launch_chunks(const Shape& s, const Jobs& jobs, int n, bool states, hipStre
       part.scan[k] = jobs.scan[l];
       part.seg[k++] = jobs.seg[l];
     }
-#define DIFFOPT_CLASS(DK, NW)                                        \
-  if (c.dk == DK && c.pieces) launch_class<E, DK, NW, true>(s, part, k, states, st); \
-  if (c.dk == DK && !c.pieces) launch_class<E, DK, NW, false>(s, part, k, states, st);
-    DIFFOPT_CLASS(32, 4)
-    DIFFOPT_CLASS(64, 4)
-    DIFFOPT_CLASS(128, 8)
+#define DIFFOPT_CLASS(DK, NCT)                                        \
+  if (c.dk == DK && c.pieces) launch_class<E, DK, NCT, true>(s, part, k, states, st); \
+  if (c.dk == DK && !c.pieces) launch_class<E, DK, NCT, false>(s, part, k, states, st);
+    DIFFOPT_CLASS(32, 1)
+    DIFFOPT_CLASS(64, 1)
+    DIFFOPT_CLASS(128, 2)
     if constexpr (sizeof(E) == 2) {
-      DIFFOPT_CLASS(256, 8)
+      DIFFOPT_CLASS(256, 2)
     } else {
-      DIFFOPT_CLASS(256, 4)
+      DIFFOPT_CLASS(256, 1)
     }
 #undef DIFFOPT_CLASS
   }
