@@ -23,7 +23,8 @@ struct Scan {
   HeadArr q, k, v, o;
   const float* s0;  // initial state or NULL: [Dk][Dv] blocks, or [Dv][Dk] ones with flip
   float* s1;        // final state or NULL: [Dk][Dv] blocks
-  int32_t flip, nq, nk, Dk, Dv;
+  int32_t flip, flip_seg;  // whether s0 / the segments' states are [Dv][Dk]
+  int32_t nq, nk, Dk, Dv;
   int32_t back;     // tokens run from the last to the first; the state meets a token undecayed
   float qs, ks;     // scale of the outputs, of the update
 };
@@ -399,14 +400,14 @@ __device__ __forceinline__ void stage(E* lds, uint32_t address, int at, const E*
 }
 
 // What a chunk kernel keeps in LDS: K, V, Q of a chunk, the scores' operands, the
-// outputs.
+// outputs; where only states are wanted, K and V of two chunks.
 template <class E, int DK, int NCT, bool OUT>
 struct ChunkLds {
   static constexpr int C = ChunkOf<E, DK>::C, NT = C / 16, NB = C / 32, CT = 64 * NCT;
   static constexpr int kq = Tile<E, DK>::elements(C), kv = Tile<E, CT>::elements(C);
-  static constexpr int all = (OUT ? 2 : 1) * kq + kv;
+  static constexpr int all = (OUT ? 2 : 1) * kq + kv, buffers = OUT ? 1 : 2;
   static constexpr int orow = CT + 16 / (int)sizeof(E);  // elements from an output's row to the next
-  E in[all];
+  E in[buffers * all];
   typename Frag<E>::type P[OUT ? NT * NB * 64 : 1];
   E out[OUT ? C * orow : 1];
 };
@@ -452,7 +453,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   f32x4 S[KB][2][NCT];
   {
     const float* s0 = !OUT ? nullptr : cut ? segments : a.s0 ? a.s0 + state * a.Dk * a.Dv : nullptr;
-    const bool flip = !cut && a.flip;
+    const bool flip = cut ? a.flip_seg : a.flip;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -496,7 +497,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   auto valid = [&](int64_t c) { return (int)(len - c * C < C ? len - c * C : C); };
   if (PIECES && (a.Dk < DK || a.Dv - ct0 < CT)) {  // columns past the widths
     typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
-    for (int i = threadIdx.x; i < Lds::all / KTile::VN; i += B) reinterpret_cast<whole*>(lds.in)[i] = whole{};
+    for (int i = threadIdx.x; i < Lds::buffers * Lds::all / KTile::VN; i += B) reinterpret_cast<whole*>(lds.in)[i] = whole{};
     __syncthreads();
   }
 
@@ -518,27 +519,45 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   E *sK = lds.in, *sV = sK + Lds::kq, *sQ = sV + Lds::kv;
   frag* sP = lds.P;
   const uint32_t address = lds_address(sK);
-  auto stage_k = [&](int64_t c, int h) {
-    stage<E, DK, C, PIECES>(sK, address, 0, k0 + c * C * kst + h * a.k.sh, kst, valid(c), 0, a.Dk, lane, wave);
+  auto stage_k = [&](int64_t c, int h, int at = 0) {
+    stage<E, DK, C, PIECES>(lds.in, address, at, k0 + c * C * kst + h * a.k.sh, kst, valid(c), 0, a.Dk, lane, wave);
   };
-  auto stage_vq = [&](int64_t c, int h) {
-    stage<E, CT, C, PIECES>(sK, address, Lds::kq, v0 + c * C * vst + h * a.v.sh, vst, valid(c), ct0, a.Dv, lane, wave);
-    if (OUT && h == 0) stage<E, DK, C, PIECES>(sK, address, Lds::kq + Lds::kv, q0 + c * C * qst, qst, valid(c), 0, a.Dk, lane, wave);
+  auto stage_vq = [&](int64_t c, int h, int at = 0) {
+    stage<E, CT, C, PIECES>(lds.in, address, at + Lds::kq, v0 + c * C * vst + h * a.v.sh, vst, valid(c), ct0, a.Dv, lane, wave);
+    if (OUT && h == 0) stage<E, DK, C, PIECES>(lds.in, address, Lds::kq + Lds::kv, q0 + c * C * qst, qst, valid(c), 0, a.Dk, lane, wave);
   };
 
   // item n of the walk: k/v head n % nk of chunk first + n / nk.  V and Q of the
   // next item are on their way from the second barrier of this one on, K from its
-  // end on; the other workgroup of the compute unit works meanwhile.
+  // end on; the other workgroup of the compute unit works meanwhile.  Where only
+  // states are wanted, the next item arrives in the other buffer.
   int64_t pending = -1;
   f32x4 O[NT][NCT];
-  if (first < end) stage_vq(first, 0);
-  int h = 0;
+  if (first < end) {
+    stage_vq(first, 0);
+    if (!OUT) stage_k(first, 0);
+  }
+  int h = 0, turn = 0;
   for (int64_t c = first; c < end;) {
     const int L = valid(c);
-    __syncthreads();
-    stage_k(c, h);
+    const bool last_head = h + 1 == a.nk;
+    const int h_next = last_head ? 0 : h + 1;
+    const int64_t c_next = last_head ? c + 1 : c;
+    if (OUT) {
+      __syncthreads();
+      stage_k(c, h);
+    }
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
     __syncthreads();
+    if (!OUT) {
+      sK = lds.in + turn * Lds::all;
+      sV = sK + Lds::kq;
+      turn ^= 1;
+      if (c_next < end) {
+        stage_k(c_next, h_next, turn * Lds::all);
+        stage_vq(c_next, h_next, turn * Lds::all);
+      }
+    }
     if (OUT && PIECES && pending >= 0) {
       store_outputs(pending);
       pending = -1;
@@ -624,13 +643,9 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
           for (int ct = 0; ct < NCT; ++ct) O[t][ct] *= qwc * qt[t];
       }
     }
-    const bool decay = h == 0;
-    const bool last_head = h + 1 == a.nk;
-    const int h_next = last_head ? 0 : h + 1;
-    const int64_t c_next = last_head ? c + 1 : c;
-    __syncthreads();
-    if (c_next < end) stage_vq(c_next, h_next);
     if (OUT) {
+      __syncthreads();
+      if (c_next < end) stage_vq(c_next, h_next);
       if (!odd) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -690,7 +705,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
     }
 
     asm volatile("" : "+v"(m), "+v"(g));
-    if (decay) {
+    if (h == 0) {
       if (L == C && ((c - first) & 7) == 7) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
@@ -917,6 +932,7 @@ int backward_scans(int64_t H, int64_t Hk, int64_t Dk, int64_t Dv, Scan* a) {
     a[i].Dv = (int32_t)(i == 2 ? Dv : Dk);
     a[i].back = i > 0;
     a[i].flip = i < 2;
+    a[i].flip_seg = i == 1;  // dk's states are dv's transposed: it reads those
   }
   return 3;
 }
@@ -924,32 +940,34 @@ int backward_scans(int64_t H, int64_t Hk, int64_t Dk, int64_t Dv, Scan* a) {
 int64_t workspace_of(const Shape& s, const Scan* a, int n, int32_t dtype) {
   const Plan p = plan_of(s, a, n, dtype);
   int64_t bytes = 0;
-  for (int i = 0; i < n; ++i) bytes += segment_bytes(s, a[i], p);
+  for (int i = 0; i < n; ++i) bytes += a[i].flip_seg ? 0 : segment_bytes(s, a[i], p);
   return bytes;
 }
 
 template <class E, int DK, int NCT, bool PIECES>
 void launch_class(const Shape& s, const Jobs& jobs, int n, bool states, hipStream_t st) {
-  constexpr int SPLIT = sizeof(E) == 2 ? 3 : 1;
+  constexpr int MOST = sizeof(E) == 2 ? 3 : 1, SPLIT = sizeof(E) == 2 && PIECES ? 2 : MOST;
   int64_t tiles = 0, main = 0, own = 0;
-  bool keep = false;
+  bool keep = false;  // a state is handed out
   for (int i = 0; i < n; ++i) {
     const int64_t c = col_tiles(jobs.scan[i], sizeof(E) == 4 ? DIFFOPT_F32 : DIFFOPT_BF16);
     tiles = c > tiles ? c : tiles;
-    keep |= jobs.scan[i].s1 != nullptr && jobs.nseg == 1;
+    keep |= jobs.scan[i].s1 != nullptr && (states || jobs.nseg == 1);
   }
   for (int i = 0; i < n; ++i) {
     const int64_t w = s.B * s.Hs * jobs.nseg * tiles;
     own = w > own ? w : own;
     main = w * jobs.scan[i].nq > main ? w * jobs.scan[i].nq : main;
   }
-  if (states)
-    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, SPLIT, false, PIECES>), dim3((unsigned)own, n), dim3(kChunkB), 0, st, s, jobs, (int32_t)tiles);
-  else if (keep || !PIECES || sizeof(E) == 4)
-    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, SPLIT, true, PIECES>), dim3((unsigned)main, n), dim3(kChunkB), 0, st, s, jobs, (int32_t)tiles);
+  const dim3 grid((unsigned)(states ? own : main), n), block(kChunkB);
+  if (states && keep)
+    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, MOST, false, PIECES>), grid, block, 0, st, s, jobs, (int32_t)tiles);
+  else if (states)
+    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, SPLIT, false, PIECES>), grid, block, 0, st, s, jobs, (int32_t)tiles);
+  else if (keep)
+    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, MOST, true, PIECES>), grid, block, 0, st, s, jobs, (int32_t)tiles);
   else
-    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, sizeof(E) == 2 ? 2 : 1, true, PIECES>), dim3((unsigned)main, n), dim3(kChunkB), 0, st, s, jobs,
-                       (int32_t)tiles);
+    hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, SPLIT, true, PIECES>), grid, block, 0, st, s, jobs, (int32_t)tiles);
 }
 
 template <class E>
@@ -1005,28 +1023,35 @@ int run_scans(const char* who, const Shape& s, const Scan* a, const bool* run, i
   if (need > 0 && (!workspace || bytes < need))
     return fail(DIFFOPT_EINVAL, "%s: the workspace has %lld bytes of %lld", who, (long long)(workspace ? bytes : 0), (long long)need);
   if (!aligned_to(workspace, 16)) return fail(DIFFOPT_EINVAL, "%s: the workspace is not 16-byte aligned", who);
-  Jobs jobs{};
-  jobs.nseg = p.nseg;
-  jobs.seg_tokens = p.seg_tokens;
-  char* at = static_cast<char*>(workspace);
-  int k = 0, block = 0;
+  // `walk`: the scans whose outputs are wanted; `own`: those that have states of
+  // their own to find first (dk takes dv's)
+  Jobs walk{}, own{};
+  walk.nseg = own.nseg = p.nseg;
+  walk.seg_tokens = own.seg_tokens = p.seg_tokens;
+  float* at = static_cast<float*>(workspace);
+  int nwalk = 0, nown = 0;
   for (int i = 0; i < n; ++i) {
-    const int64_t b = segment_bytes(s, a[i], p);
+    const bool shared = i + 1 < n && a[i].flip_seg;
     if (run[i]) {
-      jobs.scan[k] = a[i];
-      jobs.seg[k++] = reinterpret_cast<float*>(at);
+      walk.scan[nwalk] = a[i];
+      walk.seg[nwalk++] = at;
     }
-    at += b;
-    block = a[i].Dk * a[i].Dv;
+    if (!shared) {
+      if (run[i] || (i > 0 && a[i - 1].flip_seg && run[i - 1])) {
+        own.scan[nown] = a[i];
+        own.seg[nown++] = at;
+      }
+      at += segment_bytes(s, a[i], p) / 4;
+    }
   }
-  if (k == 0) return DIFFOPT_OK;
+  if (nwalk == 0) return DIFFOPT_OK;
   const bool f32 = dtype == DIFFOPT_F32;
   if (p.nseg > 1) {
-    f32 ? launch_chunks<float>(s, jobs, k, true, st) : launch_chunks<bf16>(s, jobs, k, true, st);
-    const int64_t groups = s.B * s.Hs * ((block + kJoinB - 1) / kJoinB);
-    hipLaunchKernelGGL(linattn_join, dim3((unsigned)groups, k), dim3(kJoinB), 0, st, s, jobs);
+    f32 ? launch_chunks<float>(s, own, nown, true, st) : launch_chunks<bf16>(s, own, nown, true, st);
+    const int64_t groups = s.B * s.Hs * ((own.scan[0].Dk * own.scan[0].Dv + kJoinB - 1) / kJoinB);
+    hipLaunchKernelGGL(linattn_join, dim3((unsigned)groups, nown), dim3(kJoinB), 0, st, s, own);
   }
-  f32 ? launch_chunks<float>(s, jobs, k, false, st) : launch_chunks<bf16>(s, jobs, k, false, st);
+  f32 ? launch_chunks<float>(s, walk, nwalk, false, st) : launch_chunks<bf16>(s, walk, nwalk, false, st);
   return launch_status(who);
 }
 
