@@ -260,59 +260,82 @@ struct Tile {
   static constexpr int elements(int rows) { return rows * W; }
   typedef typename Frag<E>::type frag;
 
+  // xor of parts that depend on (r & 3), (r & 12) and so on alone
   static __device__ __forceinline__ constexpr int mix(int r) {
-    if (sizeof(E) == 4) return NP >= 16 ? (r & 12) | (r & 3) : NP == 8 ? (r >> 1) & 7 : (r >> 2) & 3;
+    if (sizeof(E) == 4) return NP >= 16 ? r & 15 : NP == 8 ? (r >> 1) & 7 : (r >> 2) & 3;
     return NP >= 16 ? ((r & 3) << 2) | ((r >> 1) & 2) | ((r >> 3) & 1) : NP == 8 ? (r & 6) | ((r >> 3) & 1) : ((r >> 1) & 2) | ((r >> 3) & 1);
   }
-  static __device__ __forceinline__ constexpr int at(int r, int piece) { return r * W + (piece ^ mix(r)) * VN; }
-  // element c of row r
-  static __device__ __forceinline__ constexpr int element(int r, int c) { return at(r, c / VN) + c % VN; }
 
-  // elements 32 b + 8 g .. + 8 of row r
-  static __device__ __forceinline__ frag row(const E* base, int r, int b, int g) {
+  // Addresses, in bytes: a part of the lane, xor a constant in the bits of a row's
+  // pieces, plus a constant of whole rows (16 of them leave mix as it is).
+  static constexpr int kRow = W * (int)sizeof(E);
+  static __device__ __forceinline__ const char* to(const E* base, int lane, int piece, int rows) {
+    return reinterpret_cast<const char*>(base) + (lane ^ (piece * 16)) + rows * kRow;
+  }
+
+  // elements 32 b + 8 g .. + 8 of row r + m (r a multiple of 16)
+  static __device__ __forceinline__ int row_lane(int g, int m) { return m * kRow + ((sizeof(E) == 2 ? g : 2 * g) ^ mix(m)) * 16; }
+  static __device__ __forceinline__ frag row(const E* base, int lane, int r, int b) {
     if constexpr (sizeof(E) == 2) {
-      return *reinterpret_cast<const frag*>(base + at(r, 4 * b + g));
+      return *reinterpret_cast<const frag*>(to(base, lane, 4 * b, r));
     } else {
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(base + at(r, 8 * b + 2 * g)), hi = *reinterpret_cast<const f32x4*>(base + at(r, 8 * b + 2 * g + 1));
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(to(base, lane, 8 * b, r)), hi = *reinterpret_cast<const f32x4*>(to(base, lane, 8 * b + 1, r));
       return frag{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     }
   }
-  // elements 32 b + 4 g .. + 4 and 16 further of row r
-  static __device__ __forceinline__ frag halves(const E* base, int r, int b, int g) {
+  // elements 32 b + 4 g .. + 4 and 16 further of row r + m (r a multiple of 16)
+  static __device__ __forceinline__ int halves_lane(int g, int m) {
+    return sizeof(E) == 2 ? m * kRow + ((g >> 1) ^ mix(m)) * 16 + (g & 1) * 8 : m * kRow + (g ^ mix(m)) * 16;
+  }
+  static __device__ __forceinline__ frag halves(const E* base, int lane, int r, int b) {
     typedef E four __attribute__((ext_vector_type(4)));
-    const four lo = *reinterpret_cast<const four*>(base + element(r, 32 * b + 4 * g));
-    const four hi = *reinterpret_cast<const four*>(base + element(r, 32 * b + 16 + 4 * g));
+    constexpr int per = sizeof(E) == 2 ? 4 : 8;  // pieces of 32 elements
+    const four lo = *reinterpret_cast<const four*>(to(base, lane, per * b, r)), hi = *reinterpret_cast<const four*>(to(base, lane, per * b + per / 2, r));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
-  // element col + m, m = lane % 16, of rows 32 b + 4 g .. + 4 and 16 further
-  static __device__ __forceinline__ frag column(const E* base, int b, int col, int g, int m) {
+  // element col + m, m = lane % 16, of rows 32 b + 4 g .. + 4 and 16 further (col a
+  // multiple of 16)
+  static __device__ __forceinline__ int column_lane(int g, int m) {
+    if (sizeof(E) == 2) {
+      const int r = 4 * g + (m >> 2);
+      return r * kRow + (((m & 3) >> 1) ^ mix(r)) * 16 + (m & 1) * 8;
+    }
+    return 4 * g * kRow + ((m >> 2) ^ mix(4 * g)) * 16 + (m & 3) * 4;
+  }
+  static __device__ __forceinline__ frag column(const E* base, int lane, int b, int col) {
     if constexpr (sizeof(E) == 2) {
       typedef short s16x4 __attribute__((ext_vector_type(4)));
       typedef short s16x8 __attribute__((ext_vector_type(8)));
       typedef __attribute__((address_space(3))) s16x4 lds4;
-      const int r = 32 * b + 4 * g + (m >> 2), c = col + 4 * (m & 3);
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(base + element(r, c)));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(base + element(r + 16, c)));
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)to(base, lane, col / 8, 32 * b));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)to(base, lane, col / 8, 32 * b + 16));
       return __builtin_bit_cast(frag, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
       frag f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = base[element(32 * b + (j >> 2) * 16 + 4 * g + (j & 3), col + m)];
+      for (int j = 0; j < 8; ++j)
+        f[j] = *reinterpret_cast<const float*>(to(base, lane, (col / 4) ^ mix(j & 3), 32 * b + (j >> 2) * 16 + (j & 3)));
       return f;
     }
   }
 };
 
 // 16 bytes a lane from memory to LDS: the lanes' pieces follow one another from
-// LDS address `to` (the same in every lane) on.  Counted with the wave's other loads; the
+// LDS address `to` + OFFSET (the same in every lane) on.  Counted with the wave's other loads; the
 // caller waits for all of them before the workgroup's barrier.  (Of the builtin
 // the compiler takes every transposing read to depend, and waits for the next
 // chunk before this one is used.  The instruction has no result register, and
 // nothing else here uses m0, which it takes its address from.)
-template <class E>
+template <int OFFSET, class E>
 __device__ __forceinline__ void load_to_lds(const E* from, uint32_t to) {
-  const uint32_t base = __builtin_amdgcn_readfirstlane(to);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(base), "v"(from) : "memory");
+  asm volatile("s_add_i32 m0, %0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from), "i"(OFFSET) : "memory", "scc");
+}
+
+// All of the wave's loads from memory, those to LDS among them.
+__device__ __forceinline__ void wait_for_loads() {
+  asm volatile("" : : : "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  asm volatile("" : : : "memory");
 }
 
 // The address of a shared object in LDS.
@@ -327,6 +350,22 @@ __device__ __forceinline__ bf16x8 pack(f32x4 a, f32x4 b, bf16) {
 __device__ __forceinline__ Frag<float>::type pack(f32x4 a, f32x4 b, float) {
   return Frag<float>::type{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
+
+// A fragment in fp32, from its registers (the compiler would convert each element
+// again on its own).
+__device__ __forceinline__ Frag<float>::type widened(bf16x8 f) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  u32x4 u = __builtin_bit_cast(u32x4, f);
+  asm volatile("" : "+v"(u));
+  Frag<float>::type y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[2 * i] = __builtin_bit_cast(float, u[i] << 16);
+    y[2 * i + 1] = __builtin_bit_cast(float, u[i] & 0xffff0000u);
+  }
+  return y;
+}
+__device__ __forceinline__ Frag<float>::type widened(Frag<float>::type f) { return f; }
 
 // g^n for n >= 0; lg2 = log2 g may be -inf (g = 0, g^0 = 1).
 __device__ __forceinline__ float power(float lg2, int n) { return n == 0 ? 1.0f : __builtin_amdgcn_exp2f((float)n * lg2); }
@@ -360,29 +399,28 @@ struct ChunkOf {
 
 constexpr int kWaves = 4, kChunkB = 64 * kWaves;
 
-// One matrix of a chunk on its way to LDS (element `at` of what begins at `lds`,
-// LDS address `address`), by a workgroup of four waves: rows
-// 0 .. L - 1 from `head`, st elements apart (negative: back in time), columns
-// col0 .. + W of `width`; rows from L on become zero, columns past the width stay
-// zero from before.  PIECES: the width is whole pieces; else through registers,
+// One matrix of a chunk on its way to LDS, to elements AT .. of what begins at `lds`
+// (this wave's first block of it at LDS address `address`), by a workgroup of four
+// waves: rows 0 .. L - 1 from `head`, st elements apart (negative: back in time),
+// columns col0 .. + W of `width`; rows from L on become zero, columns past the width
+// stay zero from before.  PIECES: the width is whole pieces; else through registers,
 // element by element.
-template <class E, int W, int C, bool PIECES>
-__device__ __forceinline__ void stage(E* lds, uint32_t address, int at, const E* head, int64_t st, int L, int col0, int width, int lane, int wave) {
+template <class E, int W, int C, bool PIECES, int AT, int I = 0>
+__device__ __forceinline__ void stage(E* lds, uint32_t address, const E* head, int64_t st, int L, int col0, int width, int lane, int wave) {
   typedef Tile<E, W> T;
+  typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
   constexpr int N = C / T::RB / kWaves;  // blocks of a wave
   static_assert(N * kWaves * T::RB == C, "whole blocks for every wave");
-  typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
-  const int r0 = wave * T::RB + lane / T::NP;
-  const E* p = head + r0 * st;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int r = r0 + i * (kWaves * T::RB), c = col0 + ((lane % T::NP) ^ T::mix(r)) * T::VN, to = at + (wave + kWaves * i) * T::BLOCK;
+  if constexpr (I < N) {
+    const int r = (wave + kWaves * I) * T::RB + lane / T::NP, c = col0 + ((lane % T::NP) ^ T::mix(r)) * T::VN;
+    const E* p = head + (wave * T::RB + lane / T::NP) * st + I * (kWaves * T::RB * st);
+    whole* to = reinterpret_cast<whole*>(lds + AT + (wave + kWaves * I) * T::BLOCK + lane * T::VN);
     if (PIECES) {
       if (c < width) {
         if (r < L)
-          load_to_lds(p + c, address + to * (int)sizeof(E));
+          load_to_lds<(AT + I * kWaves * T::BLOCK) * (int)sizeof(E)>(p + c, address);
         else
-          *reinterpret_cast<whole*>(lds + to + lane * T::VN) = whole{};
+          *to = whole{};
       }
     } else {
       whole x{};
@@ -393,9 +431,9 @@ __device__ __forceinline__ void stage(E* lds, uint32_t address, int at, const E*
           x[e] = c + e < width ? y : (E)0.0f;
         }
       }
-      *reinterpret_cast<whole*>(lds + to + lane * T::VN) = x;
+      *to = x;
     }
-    p += (kWaves * T::RB) * st;
+    stage<E, W, C, PIECES, AT, I + 1>(lds, address, head, st, L, col0, width, lane, wave);
   }
 }
 
@@ -468,26 +506,25 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
           }
   }
 
-  // g^C rounds once; what that leaves out grows with every chunk and is made
-  // good each eighth one
+  // What the registers hold is the state over `scale`, the product of the decays
+  // since it was last brought up to date (kept to 48 bits: its roundings would add
+  // up over the chunks); scale and 1 / scale ride on the weights of the outputs and
+  // of the values.
   const double gcd = exp(lgd * C);
-  const float gc = uniform((float)gcd);
-  const double gc8 = gc > 0.0f ? gcd * exp(7.0 * log(gcd / (double)gc)) : 0.0;
-  const float g8_hi = uniform((float)gc8), g8_lo = uniform((float)(gc8 - (double)g8_hi));
-  const float gl = uniform((float)exp(lgd * (double)(len % C)));  // the last chunk's, where it is not whole
+  const float gc = uniform((float)gcd), gc_lo = uniform((float)(gcd - (double)(float)gcd));
+  const double gld = exp(lgd * (double)(len % C));  // of the last chunk, where it is not whole
+  const float gl = uniform((float)gld), gl_lo = uniform((float)(gld - (double)(float)gld));
+  float scale = 1.0f, scale_lo = 0.0f;
 
-  // The powers of a chunk's tokens are products of one per lane and one for all
-  // lanes (scalar registers): of the outputs of the state, qw g^(16 t), and of the
-  // values that enter it, kw g^(...) (whole chunks).
+  // The powers of a chunk's tokens are products of one per lane and some that all
+  // lanes share (scalar registers): g^(16 t) and g, g^2, g^3.
   const float ps = a.qs * a.ks;
-  const float qw = a.qs * power(lg2, m_ + 1 - back), kw = a.ks * power(lg2, 12 - 4 * g_);
-  float qt[NT], ks[NB][8];
+  const float qw = a.qs * power(lg2, m_ + 1 - back), kw = a.ks * power(lg2, 12 - 4 * g_ + back);
+  float tiles[NT], step[4];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) qt[t] = uniform(power(lg2, 16 * t));
+  for (int t = 0; t < NT; ++t) tiles[t] = uniform(power(lg2, 16 * t));
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) ks[nb][e] = uniform(power(lg2, C - 13 + back - 32 * nb - 16 * (e >> 2) - (e & 3)));
+  for (int e = 0; e < 4; ++e) step[e] = uniform(power(lg2, e));
 
   const int dir = back ? -1 : 1;
   const E* q0 = OUT ? at<E>(a.q, b, back ? len - 1 : 0, (int64_t)j * a.nq + qh) : nullptr;
@@ -518,13 +555,14 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
 
   E *sK = lds.in, *sV = sK + Lds::kq, *sQ = sV + Lds::kv;
   frag* sP = lds.P;
-  const uint32_t address = lds_address(sK);
+  const uint32_t address = __builtin_amdgcn_readfirstlane(lds_address(lds.in) + wave * 1024);
   auto stage_k = [&](int64_t c, int h, int at = 0) {
-    stage<E, DK, C, PIECES>(lds.in, address, at, k0 + c * C * kst + h * a.k.sh, kst, valid(c), 0, a.Dk, lane, wave);
+    stage<E, DK, C, PIECES, 0>(lds.in + at, address + at * (int)sizeof(E), k0 + c * C * kst + h * a.k.sh, kst, valid(c), 0, a.Dk, lane, wave);
   };
   auto stage_vq = [&](int64_t c, int h, int at = 0) {
-    stage<E, CT, C, PIECES>(lds.in, address, at + Lds::kq, v0 + c * C * vst + h * a.v.sh, vst, valid(c), ct0, a.Dv, lane, wave);
-    if (OUT && h == 0) stage<E, DK, C, PIECES>(lds.in, address, Lds::kq + Lds::kv, q0 + c * C * qst, qst, valid(c), 0, a.Dk, lane, wave);
+    stage<E, CT, C, PIECES, Lds::kq>(lds.in + at, address + at * (int)sizeof(E), v0 + c * C * vst + h * a.v.sh, vst, valid(c), ct0, a.Dv, lane, wave);
+    if (OUT && h == 0)
+      stage<E, DK, C, PIECES, OUT ? Lds::kq + Lds::kv : 0>(lds.in, address, q0 + c * C * qst, qst, valid(c), 0, a.Dk, lane, wave);
   };
 
   // item n of the walk: k/v head n % nk of chunk first + n / nk.  V and Q of the
@@ -533,6 +571,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   // states are wanted, the next item arrives in the other buffer.
   int64_t pending = -1;
   f32x4 O[NT][NCT];
+  wait_for_loads();  // the state's, which the compiler would count in the walk
   if (first < end) {
     stage_vq(first, 0);
     if (!OUT) stage_k(first, 0);
@@ -547,7 +586,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
       __syncthreads();
       stage_k(c, h);
     }
-    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    wait_for_loads();
     __syncthreads();
     if (!OUT) {
       sK = lds.in + turn * Lds::all;
@@ -565,9 +604,9 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
     // what follows from these is made anew in every chunk: kept over the walk, it
     // would cost the registers of a second workgroup
     int m = m_, g = g_;
-    float kwc = kw, qwc = qw;
+    float kwc = kw, qwc = qw * scale;
     asm volatile("" : "+v"(m), "+v"(g), "+v"(kwc), "+v"(qwc));
-    const int gap0 = m - 4 * g;
+    const int gap0 = m - 4 * g, at_row = KTile::row_lane(g, m);
     if (OUT) {
       // P^T by blocks of 16 queries and 32 keys, masked and decayed, as operands of
       // P V; of the six of 64 tokens two waves take three tiles each, two take two
@@ -583,13 +622,14 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
           if (apart >= 0) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
-              P[i] = mfma32(KTile::row(sK + KTile::elements(32) * nb, 16 * i + m, kb, g), KTile::row(sQ + KTile::elements(16) * tq, m, kb, g), P[i]);
+              P[i] = mfma32(KTile::row(sK + KTile::elements(32) * nb, at_row, 16 * i, kb), KTile::row(sQ + KTile::elements(16) * tq, at_row, 0, kb), P[i]);
             if (apart == 0) {
 #pragma unroll
               for (int e = 0; e < 4; ++e) P[i][e] = gap0 >= e ? P[i][e] * (ps * power(lg2, gap0 - e)) : 0.0f;
             } else {
+              const float w = ps * __builtin_amdgcn_exp2f((float)(gap0 + 16 * apart - 3) * lg2);  // a power of at least one
 #pragma unroll
-              for (int e = 0; e < 4; ++e) P[i][e] *= ps * power(lg2, gap0 + 16 * apart - e);
+              for (int e = 0; e < 4; ++e) P[i][e] *= e < 3 ? w * step[3 - e] : w;
             }
           }
         }
@@ -598,11 +638,12 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
     }
 
     asm volatile("" : "+v"(m), "+v"(g));
+    const int at_half = KTile::halves_lane(g, m), at_v = VTile::column_lane(g, m) ^ (wcol / VTile::VN * 16);
     frag V[NB][NCT];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int ct = 0; ct < NCT; ++ct) V[nb][ct] = VTile::column(sV, nb, wcol + 16 * ct, g, m);
+      for (int ct = 0; ct < NCT; ++ct) V[nb][ct] = VTile::column(sV, at_v, nb, 16 * ct);
 
     bool odd = false;
     if (OUT) {
@@ -622,25 +663,21 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
       odd = !__all(z[0] + z[1] + z[2] + z[3] == 0.0f);
       if (h == 0) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int ct = 0; ct < NCT; ++ct) O[t][ct] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
           frag s[NCT];
 #pragma unroll
           for (int ct = 0; ct < NCT; ++ct) s[ct] = pack(S[kb][0][ct], S[kb][1][ct], E());
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
-            const frag q = KTile::halves(sQ, 16 * t + m, kb, g);
+            const frag q = KTile::halves(sQ, at_half, 16 * t, kb);
 #pragma unroll
-            for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(s[ct], q, O[t][ct]);
+            for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(s[ct], q, kb ? O[t][ct] : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
           }
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int ct = 0; ct < NCT; ++ct) O[t][ct] *= qwc * qt[t];
+          for (int ct = 0; ct < NCT; ++ct) O[t][ct] *= qwc * tiles[t];
       }
     }
     if (OUT) {
@@ -705,36 +742,38 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
     }
 
     asm volatile("" : "+v"(m), "+v"(g));
+    const int at_k = KTile::column_lane(g, m);
     if (h == 0) {
-      if (L == C && ((c - first) & 7) == 7) {
+      const float d = L < C ? gl : gc, d_lo = L < C ? gl_lo : gc_lo;
+      const float x = scale * d, y = fmaf(scale, d, -x) + fmaf(scale, d_lo, scale_lo * d);
+      scale = uniform(x + y);
+      scale_lo = uniform(y - (scale - x));
+      if (!(scale > 0x1p-40f)) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) S[kb][u][ct][i] = fmaf(S[kb][u][ct][i], g8_hi, S[kb][u][ct][i] * g8_lo);
-      } else {
-        const float d = L < C ? gl : gc;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int ct = 0; ct < NCT; ++ct) S[kb][u][ct] *= d;
+            for (int ct = 0; ct < NCT; ++ct) S[kb][u][ct] *= scale;
+        scale = 1.0f;
+        scale_lo = 0.0f;
       }
     }
+    const float back_to = uniform(1.0f / scale);
+    kwc *= back_to;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       float w[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = kwc * ks[nb][e];
+      for (int e = 0; e < 8; ++e) {
+        w[e] = kwc * tiles[NT - 1 - 2 * nb - (e >> 2)];
+        if ((e & 3) < 3) w[e] *= step[3 - (e & 3)];
+      }
       if (L < C) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int n = L - 1 + back - 4 * g - (32 * nb + (e >> 2) * 16 + (e & 3));
-          w[e] = n >= back ? a.ks * power(lg2, n) : 0.0f;
+          w[e] = n >= back ? a.ks * back_to * power(lg2, n) : 0.0f;
         }
       }
       // the weighted values in SPLIT parts, each the rounding of what is left
@@ -747,15 +786,14 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
 #pragma unroll
         for (int p = 0; p < SPLIT; ++p) {
           part[p][ct] = __builtin_convertvector(y, frag);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] -= (float)part[p][ct][e];
+          if (p + 1 < SPLIT) y -= widened(part[p][ct]);
         }
       }
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const frag k = KTile::column(sK, nb, 32 * kb + 16 * u, g, m);
+          const frag k = KTile::column(sK, at_k, nb, 32 * kb + 16 * u);
 #pragma unroll
           for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
@@ -791,7 +829,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int r = r0 + 32 * kb + 16 * u + i, col = c0 + 16 * ct;
-            if (r < a.Dk && col < a.Dv) s1[r * a.Dv + col] = S[kb][u][ct][i];
+            if (r < a.Dk && col < a.Dv) s1[r * a.Dv + col] = fmaf(S[kb][u][ct][i], scale, S[kb][u][ct][i] * scale_lo);
           }
   }
 }
