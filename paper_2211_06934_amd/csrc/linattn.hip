@@ -405,18 +405,19 @@ constexpr int kWaves = 4, kChunkB = 64 * kWaves;
 // columns col0 .. + W of `width`; rows from L on become zero, columns past the width
 // stay zero from before.  PIECES: the width is whole pieces; else through registers,
 // element by element.
-template <class E, int W, int C, bool PIECES, int AT, int I = 0>
-__device__ __forceinline__ void stage(E* lds, uint32_t address, const E* head, int64_t st, int L, int col0, int width, int lane, int wave) {
+template <class E, int W, int C, bool PIECES, int AT, bool WHOLE, int I = 0>
+__device__ __forceinline__ void stage_blocks(E* lds, uint32_t address, const E* p, int64_t st, int L, int col0, int width, int lane, int wave) {
   typedef Tile<E, W> T;
   typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
   constexpr int N = C / T::RB / kWaves;  // blocks of a wave
   static_assert(N * kWaves * T::RB == C, "whole blocks for every wave");
   if constexpr (I < N) {
-    const int r = (wave + kWaves * I) * T::RB + lane / T::NP, c = col0 + ((lane % T::NP) ^ T::mix(r)) * T::VN;
-    const E* p = head + (wave * T::RB + lane / T::NP) * st + I * (kWaves * T::RB * st);
+    const int r = (wave + kWaves * I) * T::RB + lane / T::NP, c = ((lane % T::NP) ^ T::mix(r)) * T::VN;
     whole* to = reinterpret_cast<whole*>(lds + AT + (wave + kWaves * I) * T::BLOCK + lane * T::VN);
-    if (PIECES) {
-      if (c < width) {
+    if (WHOLE) {
+      load_to_lds<(AT + I * kWaves * T::BLOCK) * (int)sizeof(E)>(p + c, address);
+    } else if (PIECES) {
+      if (col0 + c < width) {
         if (r < L)
           load_to_lds<(AT + I * kWaves * T::BLOCK) * (int)sizeof(E)>(p + c, address);
         else
@@ -427,14 +428,26 @@ __device__ __forceinline__ void stage(E* lds, uint32_t address, const E* head, i
       if (r < L) {
 #pragma unroll
         for (int e = 0; e < T::VN; ++e) {
-          const E y = p[c + e < width ? c + e : 0];
-          x[e] = c + e < width ? y : (E)0.0f;
+          const E y = p[col0 + c + e < width ? c + e : -col0];
+          x[e] = col0 + c + e < width ? y : (E)0.0f;
         }
       }
       *to = x;
     }
-    stage<E, W, C, PIECES, AT, I + 1>(lds, address, head, st, L, col0, width, lane, wave);
+    stage_blocks<E, W, C, PIECES, AT, WHOLE, I + 1>(lds, address, p + kWaves * T::RB * st, st, L, col0, width, lane, wave);
   }
+}
+
+// `all`: every row and column is there (no lane is left out, which saves the
+// branches).
+template <class E, int W, int C, bool PIECES, int AT>
+__device__ __forceinline__ void stage(bool all, E* lds, uint32_t address, const E* head, int64_t st, int L, int col0, int width, int lane,
+                                      int wave) {
+  const E* p = head + col0 + (wave * Tile<E, W>::RB + lane / Tile<E, W>::NP) * st;
+  if (PIECES && all)
+    stage_blocks<E, W, C, PIECES, AT, true>(lds, address, p, st, L, col0, width, lane, wave);
+  else
+    stage_blocks<E, W, C, PIECES, AT, false>(lds, address, p, st, L, col0, width, lane, wave);
 }
 
 // What a chunk kernel keeps in LDS: K, V, Q of a chunk, the scores' operands, the
@@ -532,7 +545,8 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   const E* v0 = at<E>(a.v, b, back ? len - 1 : 0, (int64_t)j * a.nk);
   const int64_t qst = dir * a.q.st, kst = dir * a.k.st, vst = dir * a.v.st;
   auto valid = [&](int64_t c) { return (int)(len - c * C < C ? len - c * C : C); };
-  if (PIECES && (a.Dk < DK || a.Dv - ct0 < CT)) {  // columns past the widths
+  const bool all_columns = a.Dk == DK && a.Dv - ct0 >= CT;
+  if (PIECES && !all_columns) {  // columns past the widths
     typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
     for (int i = threadIdx.x; i < Lds::buffers * Lds::all / KTile::VN; i += B) reinterpret_cast<whole*>(lds.in)[i] = whole{};
     __syncthreads();
@@ -542,14 +556,20 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   auto store_outputs = [&](int64_t c) {
     const int L = valid(c);
     E* o = at<E>(a.o, b, back ? len - 1 : 0, (int64_t)j * a.nq + qh) + c * C * dir * a.o.st;
-    constexpr int NP = CT / VTile::VN;
+    constexpr int NP = CT / VTile::VN, STEP = B / NP;
+    typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
+    const int r0 = threadIdx.x / NP, col = threadIdx.x % NP * VTile::VN;
+    E* p = o + ct0 + col + r0 * dir * a.o.st;
+    const E* from = lds.out + r0 * Lds::orow + col;
+    if (all_columns && L == C) {
 #pragma unroll
-    for (int i = 0; i < C * NP / B; ++i) {
-      const int item = threadIdx.x + i * B, r = item / NP, col = item % NP * VTile::VN;
-      if (r < L && ct0 + col < a.Dv) {
-        typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
-        *reinterpret_cast<typename Vec<E>::type*>(o + r * dir * a.o.st + ct0 + col) = *reinterpret_cast<const whole*>(lds.out + r * Lds::orow + col);
-      }
+      for (int i = 0; i < C / STEP; ++i)
+        *reinterpret_cast<typename Vec<E>::type*>(p + i * STEP * dir * a.o.st) = *reinterpret_cast<const whole*>(from + i * STEP * Lds::orow);
+    } else {
+#pragma unroll
+      for (int i = 0; i < C / STEP; ++i)
+        if (r0 + i * STEP < L && ct0 + col < a.Dv)
+          *reinterpret_cast<typename Vec<E>::type*>(p + i * STEP * dir * a.o.st) = *reinterpret_cast<const whole*>(from + i * STEP * Lds::orow);
     }
   };
 
@@ -557,12 +577,12 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   frag* sP = lds.P;
   const uint32_t address = __builtin_amdgcn_readfirstlane(lds_address(lds.in) + wave * 1024);
   auto stage_k = [&](int64_t c, int h, int at = 0) {
-    stage<E, DK, C, PIECES, 0>(lds.in + at, address + at * (int)sizeof(E), k0 + c * C * kst + h * a.k.sh, kst, valid(c), 0, a.Dk, lane, wave);
+    stage<E, DK, C, PIECES, 0>(all_columns && valid(c) == C, lds.in + at, address + at * (int)sizeof(E), k0 + c * C * kst + h * a.k.sh, kst, valid(c), 0, a.Dk, lane, wave);
   };
   auto stage_vq = [&](int64_t c, int h, int at = 0) {
-    stage<E, CT, C, PIECES, Lds::kq>(lds.in + at, address + at * (int)sizeof(E), v0 + c * C * vst + h * a.v.sh, vst, valid(c), ct0, a.Dv, lane, wave);
+    stage<E, CT, C, PIECES, Lds::kq>(all_columns && valid(c) == C, lds.in + at, address + at * (int)sizeof(E), v0 + c * C * vst + h * a.v.sh, vst, valid(c), ct0, a.Dv, lane, wave);
     if (OUT && h == 0)
-      stage<E, DK, C, PIECES, OUT ? Lds::kq + Lds::kv : 0>(lds.in, address, q0 + c * C * qst, qst, valid(c), 0, a.Dk, lane, wave);
+      stage<E, DK, C, PIECES, OUT ? Lds::kq + Lds::kv : 0>(all_columns && valid(c) == C, lds.in, address, q0 + c * C * qst, qst, valid(c), 0, a.Dk, lane, wave);
   };
 
   // item n of the walk: k/v head n % nk of chunk first + n / nk.  V and Q of the
@@ -698,23 +718,25 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
         asm volatile("" : "+v"(m), "+v"(g));
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
 #pragma unroll 1
-            for (int sg = 0; sg < 4; ++sg) {
-              const int s = 32 * nb + (e >> 2) * 16 + 4 * sg + (e & 3);
+          for (int n = 0; n < 32; ++n) {  // token 32 nb + 16 (n / 16) + 4 sg + n % 4 of the block, element e of the lanes of group sg
+            const int sg = (n >> 2) & 3, e = ((n >> 4) << 2) | (n & 3), late = 32 * nb + n - m;  // from query 16 t + m >= s on
+            float p[NT];
 #pragma unroll
-              for (int t = 0; t < NT; ++t) {
-                const float p = s <= 16 * t + m ? (float)reinterpret_cast<const E*>(&sP[(t * NB + nb) * 64 + sg * 16 + m])[e] : 0.0f;
+            for (int t = 0; t < NT; ++t) p[t] = late <= 16 * t ? (float)reinterpret_cast<const E*>(&sP[(t * NB + nb) * 64 + sg * 16 + m])[e] : 0.0f;
 #pragma unroll
-                for (int ct = 0; ct < NCT; ++ct)
+            for (int ct = 0; ct < NCT; ++ct) {
+              float own = 0.0f;
 #pragma unroll
-                  for (int i = 0; i < 4; ++i) {
-                    const float v = __shfl((float)V[nb][ct][e], sg * 16 + 4 * g + i, 64);
-                    if (s <= 16 * t + m) O[t][ct][i] = fmaf(p, v, O[t][ct][i]);
-                  }
+              for (int k = 0; k < 8; ++k) own = e == k ? (float)V[nb][ct][k] : own;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float v = __shfl(own, sg * 16 + 4 * g + i, 64);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) O[t][ct][i] = fmaf(p[t], late <= 16 * t ? v : 0.0f, O[t][ct][i]);
               }
             }
+          }
       }
       if (last_head && a.o.p) {
         if (PIECES) {
