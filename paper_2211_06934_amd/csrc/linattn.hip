@@ -216,10 +216,11 @@ __global__ __launch_bounds__(kStepB) void linattn_one(Shape s, Scan a, int32_t c
 //
 // Fragments: v_mfma 16x16 takes row (or column) lane % 16 and, of a block of 32
 // along the contraction, 8 elements per 16-lane group g = lane / 16; it returns
-// column lane % 16, rows 4 g .. + 4.  Along tokens and along the state's rows a
-// block of 32 is numbered 4 g .. + 4 and 16 + 4 g .. + 4, so that two results are
-// an operand as they lie in the registers: P^T as computed for P V, the state for
-// Q S.  V and K^T come out of LDS transposed, four tokens at a time
+// column lane % 16, rows 4 g .. + 4.  Two results are an operand as they lie in
+// the registers, P^T as computed for P V and the state for Q S: a block of 32
+// tokens is numbered 4 g .. + 4 and 16 + 4 g .. + 4; of 32 rows of the state one
+// tile takes 8 g .. + 4, the other 8 g + 4 .. + 4, so that Q is read in whole
+// pieces.  V and K^T come out of LDS transposed, four tokens at a time
 // (ds_read_b64_tr_b16).  The products are computed transposed, so that a lane
 // holds 4 neighbouring elements of one token's output.
 //
@@ -283,16 +284,6 @@ struct Tile {
       return frag{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     }
   }
-  // elements 32 b + 4 g .. + 4 and 16 further of row r + m (r a multiple of 16)
-  static __device__ __forceinline__ int halves_lane(int g, int m) {
-    return sizeof(E) == 2 ? m * kRow + ((g >> 1) ^ mix(m)) * 16 + (g & 1) * 8 : m * kRow + (g ^ mix(m)) * 16;
-  }
-  static __device__ __forceinline__ frag halves(const E* base, int lane, int r, int b) {
-    typedef E four __attribute__((ext_vector_type(4)));
-    constexpr int per = sizeof(E) == 2 ? 4 : 8;  // pieces of 32 elements
-    const four lo = *reinterpret_cast<const four*>(to(base, lane, per * b, r)), hi = *reinterpret_cast<const four*>(to(base, lane, per * b + per / 2, r));
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-  }
   // element col + m, m = lane % 16, of rows 32 b + 4 g .. + 4 and 16 further (col a
   // multiple of 16)
   static __device__ __forceinline__ int column_lane(int g, int m) {
@@ -302,34 +293,34 @@ struct Tile {
     }
     return 4 * g * kRow + ((m >> 2) ^ mix(4 * g)) * 16 + (m & 3) * 4;
   }
-  static __device__ __forceinline__ frag column(const E* base, int lane, int b, int col) {
+  static __device__ __forceinline__ frag column(const E* base, int lane, int b, int col) { return columns(base, lane, b, col / VN, 0); }
+  // the same of element 32 kb + 8 (m / 4) + 4 u + m % 4
+  static __device__ __forceinline__ int spread_lane(int g, int m) {
+    if (sizeof(E) == 2) {
+      const int r = 4 * g + (m >> 2);
+      return r * kRow + ((m & 3) ^ mix(r)) * 16;
+    }
+    return 4 * g * kRow + ((2 * (m >> 2)) ^ mix(4 * g)) * 16 + (m & 3) * 4;
+  }
+  static __device__ __forceinline__ frag spread(const E* base, int lane, int b, int kb, int u) {
+    return sizeof(E) == 2 ? columns(base, lane, b, 4 * kb, u) : columns(base, lane, b, 8 * kb + u, 0);
+  }
+  static __device__ __forceinline__ frag columns(const E* base, int lane, int b, int piece, int half) {
     if constexpr (sizeof(E) == 2) {
       typedef short s16x4 __attribute__((ext_vector_type(4)));
       typedef short s16x8 __attribute__((ext_vector_type(8)));
       typedef __attribute__((address_space(3))) s16x4 lds4;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)to(base, lane, col / 8, 32 * b));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)to(base, lane, col / 8, 32 * b + 16));
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(to(base, lane, piece, 32 * b) + 8 * half));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(to(base, lane, piece, 32 * b + 16) + 8 * half));
       return __builtin_bit_cast(frag, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
       frag f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        f[j] = *reinterpret_cast<const float*>(to(base, lane, (col / 4) ^ mix(j & 3), 32 * b + (j >> 2) * 16 + (j & 3)));
+      for (int j = 0; j < 8; ++j) f[j] = *reinterpret_cast<const float*>(to(base, lane, piece ^ mix(j & 3), 32 * b + (j >> 2) * 16 + (j & 3)));
       return f;
     }
   }
 };
-
-// 16 bytes a lane from memory to LDS: the lanes' pieces follow one another from
-// LDS address `to` + OFFSET (the same in every lane) on.  Counted with the wave's other loads; the
-// caller waits for all of them before the workgroup's barrier.  (Of the builtin
-// the compiler takes every transposing read to depend, and waits for the next
-// chunk before this one is used.  The instruction has no result register, and
-// nothing else here uses m0, which it takes its address from.)
-template <int OFFSET, class E>
-__device__ __forceinline__ void load_to_lds(const E* from, uint32_t to) {
-  asm volatile("s_add_i32 m0, %0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from), "i"(OFFSET) : "memory", "scc");
-}
 
 // All of the wave's loads from memory, those to LDS among them.
 __device__ __forceinline__ void wait_for_loads() {
@@ -374,6 +365,25 @@ __device__ __forceinline__ float power(float lg2, int n) { return n == 0 ? 1.0f 
 __device__ __forceinline__ float uniform(float x) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
 }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+template <class E>
+__device__ __forceinline__ E* uniform(E* p) { return reinterpret_cast<E*>(uniform(reinterpret_cast<int64_t>(p))); }
+
+// 16 bytes a lane from memory, `offset` bytes from `from` on, to LDS: the lanes'
+// pieces follow one another from LDS address `to` + OFFSET (both the same in every
+// lane) on.  Counted with the wave's other loads; the caller waits for all of them
+// before the workgroup's barrier.  (Of the builtin the compiler takes every
+// transposing read to depend, and waits for the next chunk before this one is used.
+// The instruction has no result register, and nothing else here uses m0, which it
+// takes its address from.  The wait covers a pointer that a vector instruction wrote
+// just before.)
+template <int OFFSET>
+__device__ __forceinline__ void load_to_lds(const void* from, uint32_t offset, uint32_t to) {
+  asm volatile("s_add_i32 m0, %0, %3\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(uniform(from)), "i"(OFFSET) : "memory", "scc");
+}
 
 // What a launch runs: up to three scans of one shape, each cut into segments of
 // whole chunks; seg[i] holds the segments' states ([state][segment][Dk][Dv]).
@@ -399,68 +409,82 @@ struct ChunkOf {
 
 constexpr int kWaves = 4, kChunkB = 64 * kWaves;
 
+// Rows of a chunk in memory: row r lies r `st` elements from row 0 (st < 0: back in
+// time).  Addresses are a pointer that all lanes share, to the row that comes first in
+// memory, and a 32-bit offset in bytes (the host sees to it that it holds).
+struct Rows {
+  int64_t st;
+  __device__ __forceinline__ uint32_t offset(int r, int rows, int bytes) const {
+    return (uint32_t)(st < 0 ? rows - 1 - r : r) * (uint32_t)((st < 0 ? -st : st) * bytes);
+  }
+  template <class E>
+  __device__ __forceinline__ E* base(E* row0, int rows) const { return st < 0 ? row0 + (rows - 1) * st : row0; }
+};
+
 // One matrix of a chunk on its way to LDS, to elements AT .. of what begins at `lds`
 // (this wave's first block of it at LDS address `address`), by a workgroup of four
-// waves: rows 0 .. L - 1 from `head`, st elements apart (negative: back in time),
-// columns col0 .. + W of `width`; rows from L on become zero, columns past the width
-// stay zero from before.  PIECES: the width is whole pieces; else through registers,
-// element by element.
-template <class E, int W, int C, bool PIECES, int AT, bool WHOLE, int I = 0>
-__device__ __forceinline__ void stage_blocks(E* lds, uint32_t address, const E* p, int64_t st, int L, int col0, int width, int lane, int wave) {
+// waves: C rows of W columns, whole blocks of pieces a wave.
+template <class E, int W, int C, int AT>
+struct Stage {
   typedef Tile<E, W> T;
   typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
-  constexpr int N = C / T::RB / kWaves;  // blocks of a wave
-  static_assert(N * kWaves * T::RB == C, "whole blocks for every wave");
-  if constexpr (I < N) {
-    const int r = (wave + kWaves * I) * T::RB + lane / T::NP, c = ((lane % T::NP) ^ T::mix(r)) * T::VN;
-    whole* to = reinterpret_cast<whole*>(lds + AT + (wave + kWaves * I) * T::BLOCK + lane * T::VN);
-    if (WHOLE) {
-      load_to_lds<(AT + I * kWaves * T::BLOCK) * (int)sizeof(E)>(p + c, address);
-    } else if (PIECES) {
-      if (col0 + c < width) {
-        if (r < L)
-          load_to_lds<(AT + I * kWaves * T::BLOCK) * (int)sizeof(E)>(p + c, address);
-        else
-          *to = whole{};
+  static constexpr int N = C / T::RB / kWaves, STEP = kWaves * T::RB;  // blocks of a wave, rows between them
+  static_assert(N * STEP == C, "whole blocks for every wave");
+
+  static __device__ __forceinline__ int row_of(int i, int lane, int wave) { return i * STEP + wave * T::RB + lane / T::NP; }
+  static __device__ __forceinline__ int column_of(int i, int lane, int wave) { return ((lane % T::NP) ^ T::mix(row_of(i, lane, wave))) * T::VN; }
+  // a lane's place in memory: its first block's
+  static __device__ __forceinline__ uint32_t offset(Rows m, int lane, int wave) {
+    return m.offset(row_of(0, lane, wave), C, sizeof(E)) + column_of(0, lane, wave) * (int)sizeof(E);
+  }
+
+  // From row 0 at `row0` (its first column here) on.  WHOLE: all rows and columns are
+  // there; else rows from L and columns from `width` on become zero.
+  template <bool WHOLE, int I = 0>
+  static __device__ __forceinline__ void pieces(E* lds, uint32_t address, const E* base, Rows m, uint32_t offset, int L, int width, int lane, int wave) {
+    if constexpr (I < N) {
+      constexpr int to = (AT + I * kWaves * T::BLOCK) * (int)sizeof(E);
+      uint32_t at = offset;
+      if constexpr (STEP % 16 != 0) at += (column_of(I, lane, wave) - column_of(0, lane, wave)) * (int)sizeof(E);
+      if (WHOLE) {
+        load_to_lds<to>(base, at, address);
+      } else if (row_of(I, lane, wave) < L && column_of(I, lane, wave) < width) {
+        load_to_lds<to>(base, at, address);
+      } else {
+        *reinterpret_cast<whole*>(lds + AT + (wave + kWaves * I) * T::BLOCK + lane * T::VN) = whole{};
       }
-    } else {
+      pieces<WHOLE, I + 1>(lds, address, base + STEP * m.st, m, offset, L, width, lane, wave);
+    }
+  }
+  // any width and alignment: through registers, element by element
+  static __device__ __forceinline__ void elements(E* lds, const E* row0, Rows m, int L, int width, int lane, int wave) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = row_of(i, lane, wave), c = column_of(i, lane, wave);
       whole x{};
       if (r < L) {
 #pragma unroll
-        for (int e = 0; e < T::VN; ++e) {
-          const E y = p[col0 + c + e < width ? c + e : -col0];
-          x[e] = col0 + c + e < width ? y : (E)0.0f;
-        }
+        for (int e = 0; e < T::VN; ++e)
+          if (c + e < width) x[e] = row0[r * m.st + c + e];
       }
-      *to = x;
+      *reinterpret_cast<whole*>(lds + AT + (wave + kWaves * i) * T::BLOCK + lane * T::VN) = x;
     }
-    stage_blocks<E, W, C, PIECES, AT, WHOLE, I + 1>(lds, address, p + kWaves * T::RB * st, st, L, col0, width, lane, wave);
   }
-}
+};
 
-// `all`: every row and column is there (no lane is left out, which saves the
-// branches).
-template <class E, int W, int C, bool PIECES, int AT>
-__device__ __forceinline__ void stage(bool all, E* lds, uint32_t address, const E* head, int64_t st, int L, int col0, int width, int lane,
-                                      int wave) {
-  const E* p = head + col0 + (wave * Tile<E, W>::RB + lane / Tile<E, W>::NP) * st;
-  if (PIECES && all)
-    stage_blocks<E, W, C, PIECES, AT, true>(lds, address, p, st, L, col0, width, lane, wave);
-  else
-    stage_blocks<E, W, C, PIECES, AT, false>(lds, address, p, st, L, col0, width, lane, wave);
-}
-
-// What a chunk kernel keeps in LDS: K, V, Q of a chunk, the scores' operands, the
-// outputs; where only states are wanted, K and V of two chunks.
+// What a chunk kernel keeps in LDS: K of two chunks, V and Q of one, the scores'
+// operands and the outputs, which take the place of a K that is done with where they
+// fit there; where only states are wanted, K and V of two chunks.
 template <class E, int DK, int NCT, bool OUT>
 struct ChunkLds {
   static constexpr int C = ChunkOf<E, DK>::C, NT = C / 16, NB = C / 32, CT = 64 * NCT;
   static constexpr int kq = Tile<E, DK>::elements(C), kv = Tile<E, CT>::elements(C);
-  static constexpr int all = (OUT ? 2 : 1) * kq + kv, buffers = OUT ? 1 : 2;
-  static constexpr int orow = CT + 16 / (int)sizeof(E);  // elements from an output's row to the next
-  E in[buffers * all];
+  static constexpr int turn = OUT ? 2 * kq + kv : kq + kv;  // elements from one K to the other
+  static constexpr int all = (OUT ? 3 : 2) * kq + (OUT ? 1 : 2) * kv;
+  static constexpr bool over = OUT && DK >= CT;
+  E in[all];
   typename Frag<E>::type P[OUT ? NT * NB * 64 : 1];
-  E out[OUT ? C * orow : 1];
+  E out[OUT && !over ? kv : 1];
 };
 
 template <class E, int DK, int NCT, int SPLIT, bool OUT, bool PIECES>
@@ -485,7 +509,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   if (b >= sh.B) return;  // the launch's scans differ in heads
   const int j = (int)(state - b * sh.Hs);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g_ = lane >> 4, m_ = lane & 15;
-  const int64_t len = length_of(sh, b);
+  const int64_t len = uniform(length_of(sh, b));
   const double lgd = (double)sh.log_decay[j];
   const float lg2 = (float)(lgd * 1.4426950408889634074);
   const int back = a.back;
@@ -497,14 +521,14 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   const int64_t end = last < live ? last : live;
 
   // the state: tile (kb, u), column tile ct; a lane holds column 16 (NCT wave + ct)
-  // + m, rows 32 kb + 16 u + 4 g + i
+  // + m, rows 32 kb + 8 g + 4 u + i
   const bool cut = jobs.nseg > 1;
   float* segments = cut ? jobs.seg[blockIdx.y] + (state * jobs.nseg + seg) * a.Dk * a.Dv : nullptr;
   const int wcol = 16 * NCT * wave;
   f32x4 S[KB][2][NCT];
   {
     const float* s0 = !OUT ? nullptr : cut ? segments : a.s0 ? a.s0 + state * a.Dk * a.Dv : nullptr;
-    const bool flip = cut ? a.flip_seg : a.flip;
+    const bool flip = cut ? a.flip_seg : a.flip, whole_rows = s0 && flip && a.Dk % 4 == 0;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -513,10 +537,22 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
         for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int r = 32 * kb + 16 * u + 4 * g_ + i, c = ct0 + wcol + 16 * ct + m_;
+            const int r = 32 * kb + 8 * g_ + 4 * u + i, c = ct0 + wcol + 16 * ct + m_;
             const bool in = s0 && r < a.Dk && c < a.Dv;
-            S[kb][u][ct][i] = in ? s0[flip ? c * a.Dk + r : r * a.Dv + c] : 0.0f;
+            S[kb][u][ct][i] = in && !whole_rows ? s0[flip ? c * a.Dk + r : r * a.Dv + c] : 0.0f;
           }
+    if (whole_rows) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int ct = 0; ct < NCT; ++ct) {
+            const int r = 32 * kb + 8 * g_ + 4 * u, c = ct0 + wcol + 16 * ct + m_;
+            typedef f32x4 four __attribute__((aligned(4)));
+            if (r < a.Dk && c < a.Dv) S[kb][u][ct] = *reinterpret_cast<const four*>(s0 + c * a.Dk + r);
+          }
+    }
   }
 
   // What the registers hold is the state over `scale`, the product of the decays
@@ -540,86 +576,95 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   for (int e = 0; e < 4; ++e) step[e] = uniform(power(lg2, e));
 
   const int dir = back ? -1 : 1;
-  const E* q0 = OUT ? at<E>(a.q, b, back ? len - 1 : 0, (int64_t)j * a.nq + qh) : nullptr;
-  const E* k0 = at<E>(a.k, b, back ? len - 1 : 0, (int64_t)j * a.nk);
-  const E* v0 = at<E>(a.v, b, back ? len - 1 : 0, (int64_t)j * a.nk);
-  const int64_t qst = dir * a.q.st, kst = dir * a.k.st, vst = dir * a.v.st;
-  auto valid = [&](int64_t c) { return (int)(len - c * C < C ? len - c * C : C); };
+  const Rows mq{dir * a.q.st}, mk{dir * a.k.st}, mv{dir * a.v.st}, mo{dir * a.o.st};
+  const int64_t t0 = back ? len - 1 - first * C : first * C;  // the walk's first token
+  const int qhead = j * a.nq + qh, khead = j * a.nk;
   const bool all_columns = a.Dk == DK && a.Dv - ct0 >= CT;
-  if (PIECES && !all_columns) {  // columns past the widths
-    typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
-    for (int i = threadIdx.x; i < Lds::buffers * Lds::all / KTile::VN; i += B) reinterpret_cast<whole*>(lds.in)[i] = whole{};
-    __syncthreads();
-  }
+  typedef Stage<E, DK, C, 0> StageK;
+  typedef Stage<E, CT, C, Lds::kq> StageV;
+  typedef Stage<E, DK, C, OUT ? Lds::kq + Lds::kv : 0> StageQ;
+  const uint32_t off_k = StageK::offset(mk, lane, wave), off_v = StageV::offset(mv, lane, wave), off_q = OUT ? StageQ::offset(mq, lane, wave) : 0;
 
   // a finished chunk's outputs, from LDS in whole pieces of a token's row
-  auto store_outputs = [&](int64_t c) {
-    const int L = valid(c);
-    E* o = at<E>(a.o, b, back ? len - 1 : 0, (int64_t)j * a.nq + qh) + c * C * dir * a.o.st;
-    constexpr int NP = CT / VTile::VN, STEP = B / NP;
+  constexpr int OSTEP = B / VTile::NP;
+  const int orow0 = threadIdx.x / VTile::NP, ocol = threadIdx.x % VTile::NP;
+  const uint32_t off_o = mo.offset(orow0, C, sizeof(E)) + ocol * 16;
+  auto store_outputs = [&](const E* out, E* row0, int L) {
     typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
-    const int r0 = threadIdx.x / NP, col = threadIdx.x % NP * VTile::VN;
-    E* p = o + ct0 + col + r0 * dir * a.o.st;
-    const E* from = lds.out + r0 * Lds::orow + col;
-    if (all_columns && L == C) {
+    typedef __attribute__((address_space(1))) typename Vec<E>::type global;
+    int64_t p = reinterpret_cast<int64_t>(mo.base(row0, C));
+    const bool all = all_columns && L == C;
+    whole x[C / OSTEP];
 #pragma unroll
-      for (int i = 0; i < C / STEP; ++i)
-        *reinterpret_cast<typename Vec<E>::type*>(p + i * STEP * dir * a.o.st) = *reinterpret_cast<const whole*>(from + i * STEP * Lds::orow);
-    } else {
+    for (int i = 0; i < C / OSTEP; ++i) {
+      const int r = orow0 + i * OSTEP;
+      x[i] = *reinterpret_cast<const whole*>(out + r * CT + (ocol ^ VTile::mix(r)) * VTile::VN);
+    }
 #pragma unroll
-      for (int i = 0; i < C / STEP; ++i)
-        if (r0 + i * STEP < L && ct0 + col < a.Dv)
-          *reinterpret_cast<typename Vec<E>::type*>(p + i * STEP * dir * a.o.st) = *reinterpret_cast<const whole*>(from + i * STEP * Lds::orow);
+    for (int i = 0; i < C / OSTEP; ++i, p += OSTEP * mo.st * (int)sizeof(E)) {
+      asm volatile("" : "+s"(p));  // a pointer that all lanes share
+      if (all || (orow0 + i * OSTEP < L && ct0 + ocol * VTile::VN < a.Dv)) *(global*)(p + off_o) = x[i];
     }
   };
 
-  E *sK = lds.in, *sV = sK + Lds::kq, *sQ = sV + Lds::kv;
+  const E* sQ = lds.in + (OUT ? Lds::kq + Lds::kv : 0);
   frag* sP = lds.P;
   const uint32_t address = __builtin_amdgcn_readfirstlane(lds_address(lds.in) + wave * 1024);
-  auto stage_k = [&](int64_t c, int h, int at = 0) {
-    stage<E, DK, C, PIECES, 0>(all_columns && valid(c) == C, lds.in + at, address + at * (int)sizeof(E), k0 + c * C * kst + h * a.k.sh, kst, valid(c), 0, a.Dk, lane, wave);
+  auto stage = [&](auto how, const E* row0, Rows m, uint32_t offset, int L, int width, int at) {
+    typedef decltype(how) How;
+    const uint32_t to = address + at * (int)sizeof(E);
+    if (!PIECES)
+      How::elements(lds.in + at, row0, m, L, width, lane, wave);
+    else if (all_columns && L == C)
+      How::template pieces<true>(lds.in + at, to, m.base(row0, C), m, offset, L, width, lane, wave);
+    else
+      How::template pieces<false>(lds.in + at, to, m.base(row0, C), m, offset, L, width, lane, wave);
   };
-  auto stage_vq = [&](int64_t c, int h, int at = 0) {
-    stage<E, CT, C, PIECES, Lds::kq>(all_columns && valid(c) == C, lds.in + at, address + at * (int)sizeof(E), v0 + c * C * vst + h * a.v.sh, vst, valid(c), ct0, a.Dv, lane, wave);
-    if (OUT && h == 0)
-      stage<E, DK, C, PIECES, OUT ? Lds::kq + Lds::kv : 0>(all_columns && valid(c) == C, lds.in, address, q0 + c * C * qst, qst, valid(c), 0, a.Dk, lane, wave);
-  };
+  auto stage_k = [&](const E* row0, int L, int at = 0) { stage(StageK(), row0, mk, off_k, L, a.Dk, at); };
+  auto stage_v = [&](const E* row0, int L, int at = 0) { stage(StageV(), row0, mv, off_v, L, a.Dv - ct0, at); };
+  auto stage_q = [&](const E* row0, int L) { stage(StageQ(), row0, mq, off_q, L, a.Dk, 0); };
 
-  // item n of the walk: k/v head n % nk of chunk first + n / nk.  V and Q of the
-  // next item are on their way from the second barrier of this one on, K from its
-  // end on; the other workgroup of the compute unit works meanwhile.  Where only
-  // states are wanted, the next item arrives in the other buffer.
-  int64_t pending = -1;
+  // item n of the walk: k/v head n % nk of chunk first + n / nk.  K, V and Q of the
+  // next item are on their way from the second barrier of this one on; the other
+  // workgroup of the compute unit works meanwhile.  Where only states are wanted,
+  // the next item arrives in the other buffer.
+  int count = first < end ? (int)(end - first) : 0;  // chunks left
+  int64_t left = len - first * C;                    // tokens left
+  const E *pq = uniform(OUT ? at<E>(a.q, b, t0, qhead) : nullptr), *pk = uniform(at<E>(a.k, b, t0, khead)), *pv = uniform(at<E>(a.v, b, t0, khead) + ct0);
+  E* po = uniform(OUT && a.o.p ? at<E>(a.o, b, t0, qhead) + ct0 : nullptr);
+  E* pending = nullptr;  // row 0 of outputs that wait in LDS
+  int pending_rows = 0;
   f32x4 O[NT][NCT];
   wait_for_loads();  // the state's, which the compiler would count in the walk
-  if (first < end) {
-    stage_vq(first, 0);
-    if (!OUT) stage_k(first, 0);
+  if (count > 0) {
+    const int L = left < C ? (int)left : C;
+    stage_v(pv, L);
+    if (OUT) stage_q(pq, L);
+    stage_k(pk, L);
   }
   int h = 0, turn = 0;
-  for (int64_t c = first; c < end;) {
-    const int L = valid(c);
+  while (count > 0) {
+    const int L = left < C ? (int)left : C;
     const bool last_head = h + 1 == a.nk;
     const int h_next = last_head ? 0 : h + 1;
-    const int64_t c_next = last_head ? c + 1 : c;
-    if (OUT) {
-      __syncthreads();
-      stage_k(c, h);
-    }
+    const int64_t left_next = last_head ? left - C : left;
+    const int L_next = left_next < C ? (int)left_next : C;
+    const bool more = !last_head || count > 1;
+    const int64_t to_chunk = last_head ? C : 0, to_head = last_head ? h : -1;
+    pk += to_chunk * mk.st - to_head * a.k.sh;
+    pv += to_chunk * mv.st - to_head * a.v.sh;
+    if (OUT) pq += to_chunk * mq.st;
     wait_for_loads();
     __syncthreads();
-    if (!OUT) {
-      sK = lds.in + turn * Lds::all;
-      sV = sK + Lds::kq;
-      turn ^= 1;
-      if (c_next < end) {
-        stage_k(c_next, h_next, turn * Lds::all);
-        stage_vq(c_next, h_next, turn * Lds::all);
-      }
+    E *sK = lds.in + turn, *other = lds.in + (turn ^= Lds::turn);
+    const E* sV = OUT ? lds.in + Lds::kq : sK + Lds::kq;
+    if (!OUT && more) {
+      stage_k(pk, L_next, turn);
+      stage_v(pv, L_next, turn);
     }
-    if (OUT && PIECES && pending >= 0) {
-      store_outputs(pending);
-      pending = -1;
+    if (OUT && PIECES && pending) {
+      store_outputs(Lds::over ? other : lds.out, pending, pending_rows);
+      pending = nullptr;
     }
     // what follows from these is made anew in every chunk: kept over the walk, it
     // would cost the registers of a second workgroup
@@ -658,7 +703,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
     }
 
     asm volatile("" : "+v"(m), "+v"(g));
-    const int at_half = KTile::halves_lane(g, m), at_v = VTile::column_lane(g, m) ^ (wcol / VTile::VN * 16);
+    const int at_q = KTile::row_lane(g, m), at_v = VTile::column_lane(g, m) ^ (wcol / VTile::VN * 16);
     frag V[NB][NCT];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -689,7 +734,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
           for (int ct = 0; ct < NCT; ++ct) s[ct] = pack(S[kb][0][ct], S[kb][1][ct], E());
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
-            const frag q = KTile::halves(sQ, at_half, 16 * t, kb);
+            const frag q = KTile::row(sQ, at_q, 16 * t, kb);
 #pragma unroll
             for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(s[ct], q, kb ? O[t][ct] : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
           }
@@ -702,7 +747,11 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
     }
     if (OUT) {
       __syncthreads();
-      if (c_next < end) stage_vq(c_next, h_next);
+      if (more) {
+        stage_k(pk, L_next, turn);
+        stage_v(pv, L_next);
+        if (last_head) stage_q(pq, L_next);
+      }
       if (!odd) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -738,33 +787,24 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
             }
           }
       }
-      if (last_head && a.o.p) {
-        if (PIECES) {
-          typedef E four __attribute__((ext_vector_type(4)));
+      if (!PIECES && last_head && po) {
+        const int col = wcol + 4 * g;
+        E* p = po + m * mo.st + col;
 #pragma unroll
-          for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t) {
 #pragma unroll
-            for (int ct = 0; ct < NCT; ++ct)
-              *reinterpret_cast<four*>(lds.out + (16 * t + m) * Lds::orow + wcol + 16 * ct + 4 * g) = __builtin_convertvector(O[t][ct], four);
-          pending = c;
-        } else {
-          const int col = ct0 + wcol + 4 * g;
-          E* p = at<E>(a.o, b, back ? len - 1 : 0, (int64_t)j * a.nq + qh) + (c * C + m) * dir * a.o.st + col;
+          for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-#pragma unroll
-            for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (16 * t + m < L && col + 16 * ct + i < a.Dv) p[16 * ct + i] = (E)O[t][ct][i];
-            p += 16 * dir * a.o.st;
-          }
+            for (int i = 0; i < 4; ++i)
+              if (16 * t + m < L && ct0 + col + 16 * ct + i < a.Dv) p[16 * ct + i] = (E)O[t][ct][i];
+          p += 16 * mo.st;
         }
+        po += C * mo.st;
       }
     }
 
     asm volatile("" : "+v"(m), "+v"(g));
-    const int at_k = KTile::column_lane(g, m);
+    const int at_k = KTile::spread_lane(g, m);
     if (h == 0) {
       const float d = L < C ? gl : gc, d_lo = L < C ? gl_lo : gc_lo;
       const float x = scale * d, y = fmaf(scale, d, -x) + fmaf(scale, d_lo, scale_lo * d);
@@ -815,24 +855,41 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const frag k = KTile::column(sK, at_k, nb, 32 * kb + 16 * u);
+          const frag k = KTile::spread(sK, at_k, nb, kb, u);
 #pragma unroll
           for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
             for (int p = 0; p < SPLIT; ++p) S[kb][u][ct] = mfma32(k, part[p][ct], S[kb][u][ct]);
         }
     }
-    c = c_next;
+    if (OUT && PIECES && last_head && po) {
+      if (Lds::over) __syncthreads();  // K is done with
+      typedef E four __attribute__((ext_vector_type(4)));
+      E* out = (Lds::over ? sK : lds.out) + m * CT;
+      asm volatile("" : "+v"(m), "+v"(g));
+      constexpr int per = VTile::VN / 4;  // fours of a piece
+      const int piece = (wcol / VTile::VN + g / per) ^ VTile::mix(m);
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct)
+          *reinterpret_cast<four*>(out + 16 * t * CT + (piece ^ (16 * ct / VTile::VN)) * VTile::VN + g % per * 4) = __builtin_convertvector(O[t][ct], four);
+      pending = po;
+      pending_rows = L;
+      po += C * mo.st;
+    }
+    count -= last_head ? 1 : 0;
+    left = left_next;
     h = h_next;
   }
 
-  if (OUT && PIECES && pending >= 0) {
+  if (OUT && PIECES && pending) {
     __syncthreads();
-    store_outputs(pending);
+    store_outputs(Lds::over ? lds.in + (turn ^ Lds::turn) : lds.out, pending, pending_rows);
   }
 
   if (OUT && a.o.p) {  // tokens past the sequence's length
-    E* o = at<E>(a.o, b, 0, (int64_t)j * a.nq + qh);
+    E* o = at<E>(a.o, b, 0, qhead);
     const int64_t from = len > first * C ? len : first * C, to = last * C < sh.T ? last * C : sh.T;
     for (int64_t t = from + wave; t < to; t += kWaves)
       for (int col = ct0 + lane; col < ct0 + CT && col < a.Dv; col += 64) o[t * a.o.st + col] = (E)0.0f;
@@ -841,7 +898,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   if (s1) {
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));  // addresses anew: those of the initial state are not kept over the walk
-    const int r0 = 4 * ((tid & 63) >> 4), c0 = ct0 + 16 * NCT * (tid >> 6) + (tid & 15);
+    const int r0 = 8 * ((tid & 63) >> 4), c0 = ct0 + 16 * NCT * (tid >> 6) + (tid & 15);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -850,7 +907,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
         for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int r = r0 + 32 * kb + 16 * u + i, col = c0 + 16 * ct;
+            const int r = r0 + 32 * kb + 4 * u + i, col = c0 + 16 * ct;
             if (r < a.Dk && col < a.Dv) s1[r * a.Dv + col] = fmaf(S[kb][u][ct][i], scale, S[kb][u][ct][i] * scale_lo);
           }
   }
@@ -889,6 +946,7 @@ __global__ __launch_bounds__(kJoinB) void linattn_join(Shape sh, Jobs jobs) {
 // ---- host -------------------------------------------------------------------
 
 constexpr int kMaxWidth = 256;
+constexpr int kUnit = 64;  // tokens in whole chunks of every kernel
 
 template <class E>
 void launch_tokens(const Shape& s, const Scan& a, hipStream_t st) {
@@ -916,6 +974,15 @@ void launch_one(const Shape& s, const Scan& a, hipStream_t st) {
     hipLaunchKernelGGL((linattn_one<E, 8>), grid, block, 0, st, s, a, tiles);
 }
 
+// A chunk's rows lie within 32-bit offsets.
+bool near_rows(const HeadArr& h, int32_t dtype) { return (h.st < 0 ? -h.st : h.st) <= (int64_t(1) << 31) / kUnit / elem_size(dtype); }
+
+// Loads that go to LDS take addresses of whole 4 bytes.
+bool loads_in_pieces(const HeadArr& h, int32_t dtype) {
+  const int per = 4 / (int)elem_size(dtype);
+  return aligned_to(h.p, 4) && h.sb % per == 0 && h.st % per == 0 && h.sh % per == 0 && near_rows(h, dtype);
+}
+
 // Which chunk kernel a scan takes: key rows, column tiles of a wave.
 struct Class {
   int dk, nct;
@@ -927,7 +994,8 @@ Class class_of(const Scan& a, int32_t dtype) {
   c.dk = a.Dk <= 32 ? 32 : a.Dk <= 64 ? 64 : a.Dk <= 128 ? 128 : 256;
   c.nct = c.dk == 128 || (c.dk == 256 && dtype == DIFFOPT_BF16) ? 2 : 1;
   const int vn = dtype == DIFFOPT_F32 ? 4 : 8;
-  c.pieces = a.Dk % vn == 0 && a.Dv % vn == 0;
+  c.pieces = a.Dk % vn == 0 && a.Dv % vn == 0 && loads_in_pieces(a.q, dtype) && loads_in_pieces(a.k, dtype) && loads_in_pieces(a.v, dtype) &&
+             near_rows(a.o, dtype);
   return c;
 }
 
@@ -942,8 +1010,6 @@ struct Plan {
   int32_t nseg;
   int64_t seg_tokens;  // a multiple of kUnit
 };
-
-constexpr int kUnit = 64;  // whole chunks of every kernel
 
 Plan plan_of(int64_t workgroups, int64_t T) {
   const int64_t units = (T + kUnit - 1) / kUnit;
@@ -1120,7 +1186,7 @@ const char* sizes_wrong(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t Dk,
   if ((H == 0) != (Hk == 0) || (Hk > 0 && H % Hk)) return "H must be a multiple of Hk";
   if (Dk < 1 || Dk > kMaxWidth || Dv < 1 || Dv > kMaxWidth) return "Dk and Dv must be in [1, 256]";
   if (!dtype_ok(dtype)) return "unknown element type";
-  if (H > 65536 || B > (int64_t(1) << 24) || B * Hk > (int64_t(1) << 24) || T > (int64_t(1) << 40)) return "too many heads, sequences or tokens";
+  if (H > 65536 || B > (int64_t(1) << 24) || B * Hk > (int64_t(1) << 24) || T > (int64_t(1) << 35)) return "too many heads, sequences or tokens";
   return nullptr;
 }
 
