@@ -400,13 +400,6 @@ struct ChunkOf {
   static constexpr int C = sizeof(E) == 2 && DK <= 128 ? 64 : 32;
 };
 
-#ifndef FILL
-#define FILL 512
-#endif
-#ifndef MINC
-#define MINC 4
-#endif
-
 constexpr int kWaves = 4, kChunkB = 64 * kWaves;
 
 // Rows of a chunk in memory: row r lies r `st` elements from row 0 (st < 0: back in
@@ -507,6 +500,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   const int qh = (int)(x % nq);
   const int64_t state = x / nq, b = state / sh.Hs;
   if (b >= sh.B) return;  // the launch's scans differ in heads
+  if (!OUT && !a.s1 && seg == jobs.nseg - 1) return;  // nothing follows the last segment
   const int j = (int)(state - b * sh.Hs);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g_ = lane >> 4, m_ = lane & 15;
   const int64_t len = uniform(length_of(sh, b));
@@ -520,40 +514,8 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   const int64_t live = (len + C - 1) / C;  // chunks with tokens
   const int64_t end = last < live ? last : live;
 
-  // the state: tile (kb, u), column tile ct; a lane holds column 16 (NCT wave + ct)
-  // + m, rows 32 kb + 8 g + 4 u + i
-  const bool cut = jobs.nseg > 1;
-  float* segments = cut ? jobs.seg[blockIdx.y] + (state * jobs.nseg + seg) * a.Dk * a.Dv : nullptr;
   const int wcol = 16 * NCT * wave;
-  f32x4 S[KB][2][NCT];
-  {
-    const float* s0 = !OUT ? nullptr : cut ? segments : a.s0 ? a.s0 + state * a.Dk * a.Dv : nullptr;
-    const bool flip = cut ? a.flip_seg : a.flip, whole_rows = s0 && flip && a.Dk % 4 == 0;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = 32 * kb + 8 * g_ + 4 * u + i, c = ct0 + wcol + 16 * ct + m_;
-            const bool in = s0 && r < a.Dk && c < a.Dv;
-            S[kb][u][ct][i] = in && !whole_rows ? s0[flip ? c * a.Dk + r : r * a.Dv + c] : 0.0f;
-          }
-    if (whole_rows) {
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int ct = 0; ct < NCT; ++ct) {
-            const int r = 32 * kb + 8 * g_ + 4 * u, c = ct0 + wcol + 16 * ct + m_;
-            typedef f32x4 four __attribute__((aligned(4)));
-            if (r < a.Dk && c < a.Dv) S[kb][u][ct] = *reinterpret_cast<const four*>(s0 + c * a.Dk + r);
-          }
-    }
-  }
+  const bool all_columns = a.Dk == DK && a.Dv - ct0 >= CT;
 
   // What the registers hold is the state over `scale`, the product of the decays
   // since it was last brought up to date (kept to 48 bits: its roundings would add
@@ -579,7 +541,6 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   const Rows mq{dir * a.q.st}, mk{dir * a.k.st}, mv{dir * a.v.st}, mo{dir * a.o.st};
   const int64_t t0 = back ? len - 1 - first * C : first * C;  // the walk's first token
   const int qhead = j * a.nq + qh, khead = j * a.nk;
-  const bool all_columns = a.Dk == DK && a.Dv - ct0 >= CT;
   typedef Stage<E, DK, C, 0> StageK;
   typedef Stage<E, CT, C, Lds::kq> StageV;
   typedef Stage<E, DK, C, OUT ? Lds::kq + Lds::kv : 0> StageQ;
@@ -635,13 +596,63 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   E* pending = nullptr;  // row 0 of outputs that wait in LDS
   int pending_rows = 0;
   f32x4 O[NT][NCT];
-  wait_for_loads();  // the state's, which the compiler would count in the walk
   if (count > 0) {
     const int L = left < C ? (int)left : C;
     stage_v(pv, L);
     if (OUT) stage_q(pq, L);
     stage_k(pk, L);
   }
+
+  // the state: tile (kb, u), column tile ct; a lane holds column 16 (NCT wave + ct)
+  // + m, rows 32 kb + 8 g + 4 u + i
+  const bool cut = jobs.nseg > 1;
+  float* segments = cut ? jobs.seg[blockIdx.y] + (state * jobs.nseg + seg) * a.Dk * a.Dv : nullptr;
+  f32x4 S[KB][2][NCT];
+  {
+    const float* s0 = !OUT ? nullptr : cut ? segments : a.s0 ? a.s0 + state * a.Dk * a.Dv : nullptr;
+    const bool flip = cut ? a.flip_seg : a.flip;
+    typedef f32x4 four __attribute__((aligned(4)));
+    if (!s0) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int ct = 0; ct < NCT; ++ct) S[kb][u][ct] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    } else if (all_columns && flip) {
+      const float* p = s0 + (ct0 + wcol + m_) * DK + 8 * g_;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int ct = 0; ct < NCT; ++ct) S[kb][u][ct] = *reinterpret_cast<const four*>(p + 16 * ct * DK + 32 * kb + 4 * u);
+    } else if (all_columns) {
+      const int own = 8 * g_ * a.Dv + ct0 + wcol + m_;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) S[kb][u][ct][i] = s0[own + (32 * kb + 4 * u + i) * a.Dv + 16 * ct];
+    } else {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int r = 32 * kb + 8 * g_ + 4 * u + i, c = ct0 + wcol + 16 * ct + m_;
+              S[kb][u][ct][i] = r < a.Dk && c < a.Dv ? s0[flip ? c * a.Dk + r : r * a.Dv + c] : 0.0f;
+            }
+    }
+  }
+
+  wait_for_loads();  // the state's, which the compiler would count in the walk
   int h = 0, turn = 0;
   while (count > 0) {
     const int L = left < C ? (int)left : C;
@@ -898,7 +909,19 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   if (s1) {
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));  // addresses anew: those of the initial state are not kept over the walk
-    const int r0 = 8 * ((tid & 63) >> 4), c0 = ct0 + 16 * NCT * (tid >> 6) + (tid & 15);
+    const int r0 = 8 * ((tid & 63) >> 4), c0 = ct0 + 16 * NCT * (tid >> 6) + (tid & 15), own = r0 * a.Dv + c0;
+    if (all_columns) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct)
+              s1[own + (32 * kb + 4 * u + i) * a.Dv + 16 * ct] = fmaf(S[kb][u][ct][i], scale, S[kb][u][ct][i] * scale_lo);
+      return;
+    }
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -1004,16 +1027,22 @@ Class class_of(const Scan& a, int32_t dtype) {
 // over (two share a compute unit); a cut costs one more read of k and v and the
 // segments' states, so there is none from half of that on, and no segment is
 // shorter than kMinChunks.
-constexpr int kFill = FILL, kMinChunks = MINC;
+#ifndef FILL
+#define FILL 1024
+#endif
+#ifndef MINC
+#define MINC 4
+#endif
+constexpr int kFill = 512, kFillSmall = FILL, kMinChunks = MINC;
 
 struct Plan {
   int32_t nseg;
   int64_t seg_tokens;  // a multiple of kUnit
 };
 
-Plan plan_of(int64_t workgroups, int64_t T) {
+Plan plan_of(int64_t workgroups, int64_t T, int64_t fill) {
   const int64_t units = (T + kUnit - 1) / kUnit;
-  int64_t n = workgroups > 0 ? kFill / workgroups : 1;
+  int64_t n = workgroups > 0 ? fill / workgroups : 1;
   if (n > units / kMinChunks) n = units / kMinChunks;
   if (n < 1) n = 1;
   const int64_t per = units > 0 ? (units + n - 1) / n : 1;
@@ -1033,9 +1062,12 @@ int64_t segment_bytes(const Shape& s, const Scan& a, const Plan& p) {
 }
 
 Plan plan_of(const Shape& s, const Scan* a, int n, int32_t dtype) {
-  int64_t w = 0;
-  for (int i = 0; i < n; ++i) w += main_groups(s, a[i], dtype);
-  return plan_of(w, s.T);
+  int64_t w = 0, fill = kFillSmall;
+  for (int i = 0; i < n; ++i) {
+    w += main_groups(s, a[i], dtype);
+    if (a[i].Dk > 64) fill = kFill;
+  }
+  return plan_of(w, s.T, fill);
 }
 
 // The scans of a call, as the sizes alone make them.
