@@ -488,6 +488,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   typedef typename Frag<E>::type frag;
   typedef Tile<E, DK> KTile;
   typedef Tile<E, CT> VTile;
+  constexpr int AHEAD = DK <= 128 ? 1 : 0;  // LDS is read a step ahead; a state of 256 rows leaves no registers for it
   __shared__ __attribute__((aligned(16))) Lds lds;
 
   const Scan a = jobs.scan[blockIdx.y];
@@ -550,21 +551,23 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   constexpr int OSTEP = B / VTile::NP;
   const int orow0 = threadIdx.x / VTile::NP, ocol = threadIdx.x % VTile::NP;
   const uint32_t off_o = mo.offset(orow0, C, sizeof(E)) + ocol * 16;
-  auto store_outputs = [&](const E* out, E* row0, int L) {
-    typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
-    typedef __attribute__((address_space(1))) typename Vec<E>::type global;
-    int64_t p = reinterpret_cast<int64_t>(mo.base(row0, C));
-    const bool all = all_columns && L == C;
-    whole x[C / OSTEP];
+  typedef E whole __attribute__((ext_vector_type(16 / sizeof(E))));
+  whole done[C / OSTEP];
+  auto read_outputs = [&](const E* out) {
 #pragma unroll
     for (int i = 0; i < C / OSTEP; ++i) {
       const int r = orow0 + i * OSTEP;
-      x[i] = *reinterpret_cast<const whole*>(out + r * CT + (ocol ^ VTile::mix(r)) * VTile::VN);
+      done[i] = *reinterpret_cast<const whole*>(out + r * CT + (ocol ^ VTile::mix(r)) * VTile::VN);
     }
+  };
+  auto store_outputs = [&](E* row0, int L) {
+    typedef __attribute__((address_space(1))) typename Vec<E>::type global;
+    int64_t p = reinterpret_cast<int64_t>(mo.base(row0, C));
+    const bool all = all_columns && L == C;
 #pragma unroll
     for (int i = 0; i < C / OSTEP; ++i, p += OSTEP * mo.st * (int)sizeof(E)) {
       asm volatile("" : "+s"(p));  // a pointer that all lanes share
-      if (all || (orow0 + i * OSTEP < L && ct0 + ocol * VTile::VN < a.Dv)) *(global*)(p + off_o) = x[i];
+      if (all || (orow0 + i * OSTEP < L && ct0 + ocol * VTile::VN < a.Dv)) *(global*)(p + off_o) = done[i];
     }
   };
 
@@ -673,10 +676,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
       stage_k(pk, L_next, turn);
       stage_v(pv, L_next, turn);
     }
-    if (OUT && PIECES && pending) {
-      store_outputs(Lds::over ? other : lds.out, pending, pending_rows);
-      pending = nullptr;
-    }
+    if (OUT && PIECES && AHEAD && pending) read_outputs(Lds::over ? other : lds.out);
     // what follows from these is made anew in every chunk: kept over the walk, it
     // would cost the registers of a second workgroup
     int m = m_, g = g_;
@@ -684,35 +684,54 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
     asm volatile("" : "+v"(m), "+v"(g), "+v"(kwc), "+v"(qwc));
     const int gap0 = m - 4 * g, at_row = KTile::row_lane(g, m);
     if (OUT) {
-      // P^T by blocks of 16 queries and 32 keys, masked and decayed, as operands of
-      // P V; of the six of 64 tokens two waves take three tiles each, two take two
-#pragma unroll 1
-      for (int n = 0; n < (NT == 4 && wave < 2 ? 2 : 1); ++n) {
-        const int tq = NT == 2 ? wave : wave == 0 ? n : wave == 1 ? 2 : 3, nb = NT == 2 || wave == 0 ? 0 : wave == 1 ? n : wave - 2;
-        if (NT == 2 && wave >= 2) break;
-        f32x4 P[2];
+      // P^T by tiles of 16 queries and 16 keys, masked and decayed, as operands of
+      // P V.  Of 64 tokens a wave takes the first two of a row of four and one of the
+      // others, so that none waits for another; those past the diagonal are zero.
+      constexpr int TILES = NT == 4 ? 3 : 1;
+      f32x4 P[TILES];
+      int tq[TILES], tk[TILES];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int apart = tq - 2 * nb - i;
-          P[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-          if (apart >= 0) {
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-              P[i] = mfma32(KTile::row(sK + KTile::elements(32) * nb, at_row, 16 * i, kb), KTile::row(sQ + KTile::elements(16) * tq, at_row, 0, kb), P[i]);
-            if (apart == 0) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) P[i][e] = gap0 >= e ? P[i][e] * (ps * power(lg2, gap0 - e)) : 0.0f;
-            } else {
-              const float w = ps * __builtin_amdgcn_exp2f((float)(gap0 + 16 * apart - 3) * lg2);  // a power of at least one
-#pragma unroll
-              for (int e = 0; e < 4; ++e) P[i][e] *= e < 3 ? w * step[3 - e] : w;
-            }
-          }
-        }
-        sP[(tq * NB + nb) * 64 + lane] = pack(P[0], P[1], E());
+      for (int i = 0; i < TILES; ++i) {
+        tq[i] = NT == 2 ? wave >> 1 : i < 2 ? 3 - wave : wave & 1 ? 2 : 3;
+        tk[i] = NT == 2 ? wave & 1 : i < 2 ? i : 2 + (wave >> 1);
+        P[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       }
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        frag q;
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+          if (i != 1) q = KTile::row(sQ + KTile::elements(16) * tq[i], at_row, 0, kb);
+          P[i] = mfma32(KTile::row(sK + KTile::elements(16) * tk[i], at_row, 0, kb), q, P[i]);
+        }
+      }
+      // decays of a tile on the diagonal, and of one before it
+      float near[4], off[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        near[e] = ps * power(lg2, gap0 > e ? gap0 - e : 0);
+        off[e] = ps * __builtin_amdgcn_exp2f((float)(gap0 + 16 - e) * lg2);  // a power of at least one
+      }
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) {
+        const int apart = tq[i] - tk[i];
+        float far = 0.0f;
+#pragma unroll
+        for (int t = 1; t < NT; ++t) far = apart == t ? tiles[t - 1] : far;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) P[i][e] = gap0 + 16 * apart >= e ? P[i][e] * (apart == 0 ? near[e] : off[e] * far) : 0.0f;
+      }
+      typedef E four __attribute__((ext_vector_type(4)));
+      if (TILES == 3) sP[tq[0] * NB * 64 + lane] = pack(P[0], P[1], E());
+      constexpr int one = TILES - 1;
+      reinterpret_cast<four*>(sP)[((tq[one] * NB + (tk[one] >> 1)) * 64 + lane) * 2 + (tk[one] & 1)] = __builtin_convertvector(P[one], four);
     }
 
+    if (OUT && PIECES && pending) {
+      if (!AHEAD) read_outputs(Lds::over ? other : lds.out);
+      store_outputs(pending, pending_rows);
+      pending = nullptr;
+    }
     asm volatile("" : "+v"(m), "+v"(g));
     const int at_q = KTile::row_lane(g, m), at_v = VTile::column_lane(g, m) ^ (wcol / VTile::VN * 16);
     frag V[NB][NCT];
@@ -738,17 +757,25 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
         }
       odd = !__all(z[0] + z[1] + z[2] + z[3] == 0.0f);
       if (h == 0) {
+        frag q[2][NT];
+        if (AHEAD) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) q[0][t] = KTile::row(sQ, at_q, 16 * t, 0);
+        }
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
           frag s[NCT];
 #pragma unroll
           for (int ct = 0; ct < NCT; ++ct) s[ct] = pack(S[kb][0][ct], S[kb][1][ct], E());
+          if (kb + AHEAD < KB) {
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            const frag q = KTile::row(sQ, at_q, 16 * t, kb);
-#pragma unroll
-            for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(s[ct], q, kb ? O[t][ct] : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+            for (int t = 0; t < NT; ++t) q[(kb + AHEAD) & 1][t] = KTile::row(sQ, at_q, 16 * t, kb + AHEAD);
           }
+          __builtin_amdgcn_sched_barrier(0);  // reads stay ahead of the products
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(s[ct], q[kb & 1][t], kb ? O[t][ct] : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -758,20 +785,23 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
     }
     if (OUT) {
       __syncthreads();
-      if (more) {
-        stage_k(pk, L_next, turn);
-        stage_v(pv, L_next);
-        if (last_head) stage_q(pq, L_next);
-      }
-      if (!odd) {
+      frag p[NT][NB];
+      auto read_scores = [&] {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int nb = 0; nb <= t / 2; ++nb) {
-            const frag p = sP[(t * NB + nb) * 64 + lane];
+          for (int nb = 0; nb <= t / 2; ++nb) p[t][nb] = sP[(t * NB + nb) * 64 + lane];
+      };
+      if (AHEAD) read_scores();
+      if (more) stage_k(pk, L_next, turn);
+      if (!odd) {
+        if (!AHEAD) read_scores();
 #pragma unroll
-            for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(V[nb][ct], p, O[t][ct]);
-          }
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int t = 2 * nb; t < NT; ++t)
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(V[nb][ct], p[t][nb], O[t][ct]);
       } else {
         // a product with the zeros of the mask would carry an infinity or NaN to
         // earlier tokens, so the sum stops at the token
@@ -798,6 +828,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
             }
           }
       }
+      if (more) stage_v(pv, L_next);
       if (!PIECES && last_head && po) {
         const int col = wcol + 4 * g;
         E* p = po + m * mo.st + col;
@@ -862,16 +893,26 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
           if (p + 1 < SPLIT) y -= widened(part[p][ct]);
         }
       }
+      frag k[2][2];
+      if (AHEAD) {
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
+        for (int u = 0; u < 2; ++u) k[0][u] = KTile::spread(sK, at_k, nb, 0, u);
+      }
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const frag k = KTile::spread(sK, at_k, nb, kb, u);
+      for (int kb = 0; kb < KB; ++kb) {
+        if (kb + AHEAD < KB) {
 #pragma unroll
-          for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-            for (int p = 0; p < SPLIT; ++p) S[kb][u][ct] = mfma32(k, part[p][ct], S[kb][u][ct]);
+          for (int u = 0; u < 2; ++u) k[(kb + AHEAD) & 1][u] = KTile::spread(sK, at_k, nb, kb + AHEAD, u);
         }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int p = 0; p < SPLIT; ++p)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) S[kb][u][ct] = mfma32(k[kb & 1][u], part[p][ct], S[kb][u][ct]);
+      }
+      if (OUT && nb == 0 && more && last_head) stage_q(pq, L_next);
     }
     if (OUT && PIECES && last_head && po) {
       if (Lds::over) __syncthreads();  // K is done with
@@ -896,7 +937,8 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
 
   if (OUT && PIECES && pending) {
     __syncthreads();
-    store_outputs(Lds::over ? lds.in + (turn ^ Lds::turn) : lds.out, pending, pending_rows);
+    read_outputs(Lds::over ? lds.in + (turn ^ Lds::turn) : lds.out);
+    store_outputs(pending, pending_rows);
   }
 
   if (OUT && a.o.p) {  // tokens past the sequence's length
@@ -1023,17 +1065,15 @@ Class class_of(const Scan& a, int32_t dtype) {
 }
 
 // Segments of a call's scans.  A workgroup walks its chunks one after another,
-// so with few heads a sequence is cut until the workgroups fill the card twice
-// over (two share a compute unit); a cut costs one more read of k and v and the
-// segments' states, so there is none from half of that on, and no segment is
-// shorter than kMinChunks.
-#ifndef FILL
-#define FILL 1024
-#endif
-#ifndef MINC
-#define MINC 4
-#endif
-constexpr int kFill = 512, kFillSmall = FILL, kMinChunks = MINC;
+// so with few heads a sequence is cut until the workgroups fill the card: two of
+// them share a compute unit, up to four where the state has at most 64 rows
+// (six ragged sequences of up to 1,021 tokens, heads of 64, both ways: 85 us,
+// with half as many 103; heads of 128 with twice as many: no gain).  A cut costs
+// one more read of k and v and the segments' states, so there is none from half of
+// that on, and no segment is shorter than kMinUnits (with 8 the ragged ones take
+// 114 us, with 2 they take 82, and the states of wide heads cost as much as their
+// tokens).
+constexpr int kFill = 512, kFillNarrow = 1024, kMinUnits = 4;
 
 struct Plan {
   int32_t nseg;
@@ -1043,7 +1083,7 @@ struct Plan {
 Plan plan_of(int64_t workgroups, int64_t T, int64_t fill) {
   const int64_t units = (T + kUnit - 1) / kUnit;
   int64_t n = workgroups > 0 ? fill / workgroups : 1;
-  if (n > units / kMinChunks) n = units / kMinChunks;
+  if (n > units / kMinUnits) n = units / kMinUnits;
   if (n < 1) n = 1;
   const int64_t per = units > 0 ? (units + n - 1) / n : 1;
   n = (units + per - 1) / per;
@@ -1062,7 +1102,7 @@ int64_t segment_bytes(const Shape& s, const Scan& a, const Plan& p) {
 }
 
 Plan plan_of(const Shape& s, const Scan* a, int n, int32_t dtype) {
-  int64_t w = 0, fill = kFillSmall;
+  int64_t w = 0, fill = kFillNarrow;
   for (int i = 0; i < n; ++i) {
     w += main_groups(s, a[i], dtype);
     if (a[i].Dk > 64) fill = kFill;
