@@ -6,12 +6,12 @@ flatten/unflatten through a segment table, the leaf-direct ("tree map") form
 of the step that works on the leaves without flattening, fused differentiable
 SGD-momentum and RMSProp (flat and leaf-direct), the zero-order (ES)
 estimator, and the operators of a language model that an inner loop adapts
-(linear attention, query and key norms with rotation, distillation).  ``diffopt`` is its thin Python binding (same entry points; ``operators`` for the
-language model's),
-``tree`` the host-side container walk and ``autograd`` the
-torch.autograd.Functions and meta-optimizers over the fused steps.  Importing
-the package loads the library and raises ImportError if it has not been
-built.
+(linear attention, query and key norms with rotation, distillation).
+``diffopt`` is its thin Python binding (same entry points; ``operators`` for
+the language model's), ``tree`` the host-side container walk, ``autograd`` the
+torch.autograd.Functions and meta-optimizers over the fused steps and
+``language`` those over the language model's operators.  Importing the package
+loads the library and raises ImportError if it has not been built.
 """
 from . import diffopt
 from .diffopt import (DiffoptError, SegTable, adam_bwd, adam_bwd_tree, adam_fwd, adam_fwd_tree,
@@ -30,9 +30,11 @@ from . import tree
 from . import autograd
 from .autograd import (AdamFn, AdamHyper, AdamState, AdamTreeFn, FlatAdam, MetaAdam, MetaRMSProp, MetaSGD,
                        RMSPropHyper, RMSPropTreeFn, SGDHyper, SGDTreeFn, ZeroOrderFn, es_gradient)
+from . import language
+from .language import distillation_loss, linear_attention, linear_attention_step, qknorm_rope
 
 __all__ = [
-    "diffopt", "operators", "tree", "autograd", "DiffoptError", "SegTable", "adam_bwd", "adam_fwd",
+    "diffopt", "operators", "tree", "autograd", "language", "DiffoptError", "SegTable", "adam_bwd", "adam_fwd",
     "adam_unrolled_bwd", "adam_unrolled_fwd", "adam_fwd_tree", "adam_bwd_tree",
     "adam_unrolled_fwd_tree", "adam_unrolled_bwd_tree", "sgd_fwd", "sgd_bwd", "rmsprop_fwd", "rmsprop_bwd",
     "sgd_fwd_tree", "sgd_bwd_tree", "rmsprop_fwd_tree", "rmsprop_bwd_tree",
@@ -44,4 +46,5 @@ __all__ = [
     "linattn_fwd", "linattn_bwd", "linattn_step", "linattn_workspace",
     "qknorm_rope_fwd", "qknorm_rope_bwd", "qknorm_rope_bwd_bwd", "qknorm_rope_workspace",
     "distill_fwd", "distill_bwd", "distill_fwd_bwd", "distill_bwd_bwd", "distill_workspace",
+    "linear_attention", "linear_attention_step", "qknorm_rope", "distillation_loss",
 ]

@@ -1,0 +1,243 @@
+"""The differentiable operators of a language model: first and second
+derivatives through torch.autograd against fp64 ones of plain formulas, inside
+MetaAdam's inner loop, the example that runs them together, and refusals."""
+import math
+import os
+import sys
+
+import pytest
+import torch
+
+from lm_reference import F32, assert_close, distill, linattn, qknorm_rope, tol
+
+pytestmark = pytest.mark.gpu
+
+sys.path.insert(0, os.path.join(os.path.dirname(os.path.abspath(__file__)), "..", "examples"))
+
+
+def _twice(fn, args, seed, dtype=torch.float32):
+    """[values], [first derivatives], [second ones] of fn(*args): a cotangent for each output, then for each gradient."""
+    args = [a.detach().clone().requires_grad_(True) for a in args]
+    out = fn(*args)
+    gen = torch.Generator().manual_seed(seed)
+    cots = [torch.randn(o.shape, generator=gen).to(o.dtype).to(o.device).requires_grad_(True) for o in out]
+    first = torch.autograd.grad(out, args, cots, create_graph=True)
+    cc = [torch.randn(g.shape, generator=gen).to(g.dtype).to(g.device) for g in first]
+    second = torch.autograd.grad(first, [*cots, *args], cc)
+    return out, first, second
+
+
+def _rounded(*xs, dtype):
+    return [x.to(dtype) for x in xs]
+
+
+def _compare(ours, ref, bounds, what):
+    for group, r, bound, order in zip(ours, ref, bounds, ("value", "gradient", "second")):
+        for i, (x, y) in enumerate(zip(group, r)):
+            assert_close(x, y, bound, "%s %s %d" % (what, order, i))
+
+
+# fp32: the second derivative's terms are sums of up to three results, each
+# within F32 of its own norm; inputs are independent, so they do not cancel.
+# bf16: each of up to three results is rounded, and their sum once more.
+def _bounds(dtype, products):
+    one = tol(dtype, products)
+    return one, one, (3.0 ** 0.5 * F32 if dtype == torch.float32 else one + 2.0 ** -8)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(2, 1, 2, 2, 16, 16), (2, 3, 4, 2, 8, 24), (1, 70, 4, 2, 32, 16), (2, 131, 2, 2, 33, 17)])
+def test_linear_attention_twice(shape, dtype):
+    import paper_2211_06934_amd as P
+    B, T, H, Hk, Dk, Dv = shape
+    gen = torch.Generator().manual_seed(11)
+    new = lambda *s: torch.randn(*s, generator=gen)
+    q, k, v = _rounded(new(B, T, H, Dk), new(B, T, Hk, Dk), new(B, T, Hk, Dv), dtype=dtype)
+    s0, lg = new(B, Hk, Dk, Dv), -torch.rand(Hk, generator=gen) * 0.2
+    lengths = torch.tensor([T, max(T - 2, 0)][:B], dtype=torch.int32)
+    ours = _twice(lambda *a: P.linear_attention(*a[:3], lg.cuda(), a[3], lengths.cuda(), 0.5, return_state=True),
+                  [x.cuda() for x in (q, k, v, s0)], 3)
+    ref = _twice_as(lambda *a: linattn(*a[:3], lg, a[3], lengths, 0.5), (q, k, v, s0), 3, ours)
+    _compare(ours, ref, _bounds(dtype, True), "linear attention")
+
+
+def _twice_as(fn, args, seed, ours):
+    """_twice in fp64 with the cotangents' values that `ours` had (of its outputs' types)."""
+    args = [a.detach().double().requires_grad_(True) for a in args]
+    out = fn(*args)
+    gen = torch.Generator().manual_seed(seed)
+    cots = [torch.randn(o.shape, generator=gen).to(o.dtype).double().requires_grad_(True) for o in ours[0]]
+    first = torch.autograd.grad(out, args, cots, create_graph=True)
+    cc = [torch.randn(g.shape, generator=gen).to(g.dtype).double() for g in ours[1]]
+    second = torch.autograd.grad(first, [*cots, *args], cc)
+    return out, first, second
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rot,interleaved", [(0, False), (16, False), (8, True)])
+def test_qknorm_rope_twice(rot, interleaved, dtype):
+    import paper_2211_06934_amd as P
+    B, T, H, Hk, D = 2, 9, 4, 2, 16
+    gen = torch.Generator().manual_seed(5)
+    q, k = _rounded(torch.randn(B, T, H, D, generator=gen), torch.randn(B, T, Hk, D, generator=gen), dtype=dtype)
+    qw, kw = (1 + 0.3 * torch.randn(D, generator=gen) for _ in range(2))
+    angle = torch.rand(T, rot // 2, generator=gen) * 6
+    cos, sin = (torch.cos(angle), torch.sin(angle)) if rot else (None, None)
+    where = torch.arange(T).expand(B, T)
+    tables = [None if t is None else t.cuda() for t in (cos, sin)]
+    ours = _twice(lambda q, k, a, b: P.qknorm_rope(q, k, a, b, *tables, eps=1e-5, interleaved=interleaved),
+                  [x.cuda() for x in (q, k, qw, kw)], 8)
+
+    def plain(q, k, a, b):
+        return qknorm_rope(q, a, cos, sin, where, 1e-5, interleaved), qknorm_rope(k, b, cos, sin, where, 1e-5, interleaved)
+
+    _compare(ours, _twice_as(plain, (q, k, qw, kw), 8, ours), _bounds(dtype, False), "norms")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,V,K,temperature", [(5, 97, 7, 1.0), (3, 1030, 16, 2.0), (2, 33, 1, 0.5)])
+def test_distillation_twice(N, V, K, temperature, dtype):
+    import paper_2211_06934_amd as P
+    gen = torch.Generator().manual_seed(21)
+    (logits,) = _rounded(2 * torch.randn(N, V, generator=gen), dtype=dtype)
+    ids = torch.stack([torch.randperm(V, generator=gen)[:K] for _ in range(N)])
+    teacher = 2 * torch.randn(N, K, generator=gen)
+    if K > 1:
+        ids[0, 1] = -1
+        teacher[1, 0] = -math.inf
+        ids[-1] = -1  # a row without entries
+    ours = _twice(lambda x, t: (P.distillation_loss(x, ids.cuda(), t, temperature),), [logits.cuda(), teacher.cuda()], 2)
+    keep = (ids >= 0) & (teacher != -math.inf)
+    far = torch.where(keep, teacher, torch.zeros(()))  # the reference differentiates only kept entries
+    ref = _twice_as(lambda x, t: (distill(x, torch.where(keep, ids, torch.full((), -1)), t, temperature),), (logits, far), 2, ours)
+    _compare(ours, ref, _bounds(dtype, False), "distillation")
+
+
+def test_third_order_of_linear_attention():
+    # any order: the third derivative along one direction against differences of the second (both fp32; the second is a
+    # polynomial of degree at most 1 in each operand, so a central difference along k alone is exact but for rounding)
+    import paper_2211_06934_amd as P
+    gen = torch.Generator().manual_seed(2)
+    q, k, v, d = (torch.randn(1, 20, 2, 8, generator=gen).cuda() for _ in range(4))
+    lg = torch.tensor([-0.1, -0.02]).cuda()
+    w = [torch.randn(1, 20, 2, 8, generator=gen).cuda() for _ in range(3)]
+
+    def second(k):
+        x = [t.clone().requires_grad_(True) for t in (q, v)]
+        k = k.clone().requires_grad_(True)
+        out = P.linear_attention(x[0], k, x[1], lg)
+        (gq,) = torch.autograd.grad((out * w[0]).sum(), [x[0]], create_graph=True)
+        (gv,) = torch.autograd.grad((gq * w[1]).sum(), [x[1]], create_graph=True)
+        return (gv * w[2]).sum(), k
+
+    value, kk = second(k)
+    (third,) = torch.autograd.grad(value, [kk])
+    got = float((third.double() * d.double()).sum())
+    hi, lo = float(second(k + d)[0].detach()), float(second(k - d)[0].detach())
+    # fp32 sums of 2560 products: a few 1e-6 of the larger value
+    assert abs(got - (hi - lo) / 2) <= 2e-5 * max(abs(hi), abs(lo))
+
+
+# A chain of about thirty operations through two inner steps and back, each
+# within one rounding (or F32) of its norm, adding like a random walk; sums may
+# cancel to a tenth of their terms: 10 sqrt(30) of the unit.
+@pytest.mark.parametrize("dtype,bound", [(torch.float32, 55 * F32), (torch.bfloat16, 55 * 2.0 ** -8)])
+def test_meta_gradient_through_the_inner_loop(dtype, bound):
+    """The gradient of the outer loss to the teacher's logits through two inner steps of MetaSGD with momentum (smooth in
+    its gradients, as Adam's first steps are not), against the same loop in fp64 from plain formulas."""
+    import distill_inner_loop as E
+    import paper_2211_06934_amd as P
+    gen = torch.Generator().manual_seed(0)
+    vocab, B, T, K, H, Hk, D = 31, 2, 9, 4, 2, 1, 8
+    torch.manual_seed(0)
+    student = E.Student(vocab, 24, H, Hk, D, 16, dtype)
+    start = {n: t.clone() for n, t in student.state_dict().items()}
+    x, target = (torch.randint(vocab, (B, T), generator=gen) for _ in range(2))
+    ids = torch.randint(vocab, (B, T, K), generator=gen)
+    t0 = torch.randn(B, T, K, generator=gen)
+
+    student = student.cuda()
+    teacher = t0.cuda().requires_grad_(True)
+    opt = P.MetaSGD(student, lr=0.3, momentum=0.9)
+    for _ in range(2):
+        opt.step(E.inner_loss(student, x.cuda(), ids.cuda(), teacher))
+    (grad,) = torch.autograd.grad(E.outer_loss(student, x.cuda(), target.cuda()), [teacher])
+
+    names = [n for n, _ in student.named_parameters()]
+    where = torch.arange(T).expand(B, T)
+
+    def logits(p):
+        h = p["embed"][x]
+        q, k, v = (h @ p["qkv"].T).unflatten(-1, (-1, D)).split([H, Hk, Hk], 2)
+        q, k = (qknorm_rope(y, p[w], start["cos"], start["sin"], where, 1e-6, False) for y, w in ((q, "q_weight"), (k, "k_weight")))
+        out, _ = linattn(q, k, v, start["log_decay"], scale=D ** -0.5)
+        return ((h + out.flatten(2) @ p["mix"].T) @ p["top"].T).flatten(0, 1)
+
+    p = {n: start[n].double().requires_grad_(True) for n in names}
+    t = t0.double().requires_grad_(True)
+    trace = [torch.zeros_like(p[n]) for n in names]
+    for _ in range(2):
+        loss = distill(logits(p), ids.flatten(0, 1), t.flatten(0, 1), 2.0).mean()
+        g = torch.autograd.grad(loss, [p[n] for n in names], create_graph=True)
+        trace = [y + 0.9 * z for y, z in zip(g, trace)]
+        p = {n: p[n] - 0.3 * y for n, y in zip(names, trace)}
+    (ref,) = torch.autograd.grad(torch.nn.functional.cross_entropy(logits(p), target.flatten()), [t])
+    assert float((grad.double().cpu() - ref).norm()) <= bound * float(ref.norm())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_example(dtype, capsys):
+    import distill_inner_loop as E
+    outer, inner, got = E.main(["--outer", "4", "--inner", "2", "--dtype", dtype])
+    assert all(math.isfinite(x) for x in outer + inner)
+    assert outer[-1] < outer[0]  # the teacher learns
+    assert inner[-1] < inner[0]  # the student learns from it
+    assert got.shape == (8, 8)
+
+
+def test_generation_agrees_with_the_prompt():
+    """A token at a time from the prompt's state gives the logits that one call over all tokens gives."""
+    import distill_inner_loop as E
+    torch.manual_seed(3)
+    student = E.Student().cuda()
+    tokens = torch.randint(257, (3, 30), generator=torch.Generator().manual_seed(1)).cuda()
+    with torch.no_grad():
+        whole = student(tokens)
+        _, state = student(tokens[:, :20], return_state=True)
+        for t in range(20, 30):
+            assert_close(student.step(tokens[:, t], t, state), whole[:, t].double().cpu(), 4 * F32)  # and three matrix products
+
+
+def test_expanded_cotangents_and_operands():
+    import paper_2211_06934_amd as P
+    gen = torch.Generator().manual_seed(4)
+    q, k, v = (torch.randn(2, 12, 2, 8, generator=gen).cuda().requires_grad_(True) for _ in range(3))
+    lg = torch.full((2,), -0.1).cuda()
+    one = P.linear_attention(q, k[:, :, :1].expand(-1, -1, 2, -1), v.transpose(2, 3).contiguous().transpose(2, 3), lg).sum()
+    grads = torch.autograd.grad(one, [q, k, v], create_graph=True)
+    torch.autograd.grad(sum(g.sum() for g in grads), [q, k, v])
+    out, _ = linattn(q.detach().cpu(), k[:, :, :1].expand(-1, -1, 2, -1).detach().cpu(), v.detach().cpu(), lg.cpu())
+    assert abs(float(one) - float(out.sum())) <= 1e-4 * float(out.abs().sum()) ** 0.5 * 10
+
+
+def test_refusals():
+    import paper_2211_06934_amd as P
+    q = torch.randn(1, 3, 2, 8).cuda()
+    lg = torch.zeros(2).cuda()
+    with pytest.raises(ValueError, match="log_decay"):
+        P.linear_attention(q, q, q, lg.clone().requires_grad_(True))
+    with pytest.raises(ValueError, match="cos"):
+        c = torch.ones(4, 4).cuda().requires_grad_(True)
+        P.qknorm_rope(q, q, cos=c, sin=c)
+    with pytest.raises(ValueError, match="state"):
+        P.linear_attention(q, q, q, lg, state=torch.zeros(1, 2, 8, 4).cuda())
+    with pytest.raises(ValueError, match="float16"):
+        P.linear_attention(q.half(), q.half(), q.half(), lg)
+    x, t = torch.randn(2, 9).cuda().requires_grad_(True), torch.randn(2, 3).cuda()
+    ids = torch.zeros(2, 3, dtype=torch.int64).cuda()
+    with pytest.raises(ValueError, match="teacher"):
+        P.distillation_loss(x, ids, t[:, :2])
+    (g,) = torch.autograd.grad(P.distillation_loss(x, ids, t).sum(), [x], create_graph=True)
+    (h,) = torch.autograd.grad(g.square().sum(), [x], create_graph=True)
+    with pytest.raises(RuntimeError):  # a third order is refused, not taken as zero
+        torch.autograd.grad(h.sum(), [x])
