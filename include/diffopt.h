@@ -506,7 +506,9 @@ int diffopt_es_weights(const float* fvals, const float* f0,
  * of its backward too: as an entry point of its own (..._bwd_bwd), or, for
  * linear attention, as calls of its own forward and backward.
  * Element types: DIFFOPT_F32, or DIFFOPT_BF16 for activations; every sum,
- * softmax statistic, norm and state is fp32, each result is rounded once.
+ * softmax statistic, norm and state is fp32, each result is rounded once
+ * (linear attention over bf16 also rounds its scores, and the state where it
+ * meets a query, to bf16: operands of matrix products).
  */
 #define DIFFOPT_F32 0
 #define DIFFOPT_BF16 1
@@ -515,7 +517,8 @@ int diffopt_es_weights(const float* fvals, const float* f0,
  * a head are contiguous, the other axes have strides in elements (any sign;
  * an axis of an input may be broadcast with stride 0, outputs must not
  * overlap themselves).  Pointers need the element type's alignment only;
- * 16-byte aligned rows are fastest, the results do not depend on it.       */
+ * 16-byte aligned rows are fastest (results agree but for the roundings of
+ * sums in another order).                                                   */
 typedef struct diffopt_heads {
   void* data;
   int64_t stride_b, stride_t, stride_h;
@@ -533,7 +536,7 @@ typedef struct diffopt_heads {
  *   lengths    DEVICE int32 [B] in [0, T] (clamped), or NULL for T
  *   state, state_out  fp32 [B][Hk][Dk][Dv], or NULL (zeros / not wanted);
  *              state_out may be state
- *   1 <= Dk, Dv <= 256; H a multiple of Hk; scale finite
+ *   1 <= Dk, Dv <= 256; H a multiple of Hk; scale finite; T <= 2^35
  *   workspace  device scratch of diffopt_linattn_workspace(..., backward 0)
  *              bytes (its contents do not matter, 16-byte aligned); NULL if
  *              that is 0
@@ -554,9 +557,10 @@ int diffopt_linattn_fwd(const diffopt_heads* q, const diffopt_heads* k,
  *   dstate = scale sum_t g^(t+1) q_t dout_t^T + g^L dstate_out,  L = lengths[b]
  * with sums over the query heads that share a k/v head in dk, dv and dstate.
  * Each of dq, dk, dv (pointers to the struct) and dstate may be NULL: it is
- * then not computed.  dstate must be neither dstate_out nor state.  Rows from L on get 0.  log_decay is a constant of the
- * operator: it has no gradient.  The three results are the forward's sum on
- * permuted operands, so a derivative of any order is made of the same calls. */
+ * then not computed.  dstate must be neither dstate_out nor state.  Rows from
+ * L on get 0.  log_decay is a constant of the operator: it has no gradient.
+ * The three results are the forward's sum on permuted operands, so a
+ * derivative of any order is made of the same calls.                       */
 int diffopt_linattn_bwd(const diffopt_heads* dout, const float* dstate_out,
                         const diffopt_heads* q, const diffopt_heads* k,
                         const diffopt_heads* v, const float* log_decay,

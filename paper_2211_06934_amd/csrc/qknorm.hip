@@ -205,9 +205,8 @@ __global__ __launch_bounds__(kQB) void qknorm_any(QkShape s, QkArgs A, int32_t q
 // lanes of a group of LPG and a wave 64 / LPG heads at a time.  A wave takes a
 // token (or one of the `per` parts of its heads, where there are few tokens) and
 // walks its heads, so that the rotation's row is read once and the weights stay
-// in registers.  The launch covers the card with kPieceBlocks workgroups, which
-// walk the tokens.
-constexpr int kPieceBlocks = 1024;
+// in registers.  The launch covers the card with as many workgroups as
+// it holds at once, which walk the tokens (piece_blocks).
 
 template <class E, int DIR, int LPG, bool INTER>
 __global__ __launch_bounds__(kQB) void qknorm_pieces(QkShape s, QkArgs A, int32_t per) {
@@ -444,9 +443,18 @@ struct Plan {
   Blocks blocks;
 };
 
+// Workgroups of a launch in pieces: what the registers of a direction let the card
+// hold at once, so that all walk the same share.  Four a compute unit forward (five
+// fit and take the same 63 us for 16,384 tokens of 40 heads of 128 in bf16, 5.3
+// TB/s); three in the backward (111 us, 4.6 TB/s; four, of which one waits for its
+// turn, 123) and in fp32's second one (18.5 us for 4,072 tokens of 16 heads of 64;
+// four 21.1); two in bf16's.
+int64_t piece_blocks(int32_t dtype, Dir dir) { return 256 * (dir == kFwd ? 4 : dir == kSecond && dtype == DIFFOPT_BF16 ? 2 : 3); }
+
 // Widths that fall into pairs of pieces, with up to 32 lanes a head, and counts
 // of tokens that 32 bits index.
-Plan plan_of(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t D, int64_t rot, int32_t dtype) {
+Plan plan_of(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t D, int64_t rot, int32_t dtype, Dir dir) {
+  const int64_t most = piece_blocks(dtype, dir);
   Plan p{};
   const int two = dtype == DIFFOPT_F32 ? 8 : 16;  // elements of a lane
   const int64_t lanes = D / two;
@@ -455,13 +463,13 @@ Plan plan_of(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t D, int64_t rot
     for (p.lpg = 4; p.lpg < lanes;) p.lpg *= 2;
     // a token's heads are split until the card has waves enough
     const int64_t hpw = 64 / p.lpg, parts = std::max((H + hpw - 1) / hpw, (Hk + hpw - 1) / hpw);
-    int64_t per = (int64_t)kPieceBlocks * kQWaves / (B * T);
+    int64_t per = most * kQWaves / (B * T);
     per = per < 1 ? 1 : per > parts ? parts : per;
     if (per > 256) per = 256;
     if (per < 1) per = 1;
     p.per = (int32_t)per;
     const int64_t need = (B * T * per + kQWaves - 1) / kQWaves;
-    p.grid = (int32_t)(need < kPieceBlocks ? need : kPieceBlocks);
+    p.grid = (int32_t)(need < most ? need : most);
     p.blocks = Blocks{p.grid, p.grid};
     return p;
   }
@@ -469,8 +477,8 @@ Plan plan_of(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t D, int64_t rot
   auto side = [&](double n) -> int32_t {  // a wave per head up to kMaxBlocks workgroups in all
     if (n == 0) return 0;
     double b = std::ceil(n / kQWaves);
-    const double most = std::floor(kMaxBlocks * (n / (nq + nk)));
-    if (b > most) b = most;
+    const double share = std::floor(kMaxBlocks * (n / (nq + nk)));
+    if (b > share) b = share;
     return b < 1 ? 1 : (int32_t)b;
   };
   p.blocks = Blocks{side(nq), side(nk)};
@@ -544,7 +552,7 @@ void launch_dir(const QkShape& s, const QkArgs& A, const Plan& p, hipStream_t st
 
 template <int DIR>
 int launch(const char* who, const QkShape& s, const QkArgs& A, int32_t dtype, hipStream_t st) {
-  const Plan p = plan_of(s.B, s.T, s.H, s.Hk, s.D, s.rot, dtype);
+  const Plan p = plan_of(s.B, s.T, s.H, s.Hk, s.D, s.rot, dtype, (Dir)DIR);
   if (p.grid > 0) {
     if (dtype == DIFFOPT_F32)
       launch_dir<float, DIR>(s, A, p, st);
@@ -565,11 +573,12 @@ int launch(const char* who, const QkShape& s, const QkArgs& A, int32_t dtype, hi
 int64_t workspace_of(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t D) {
   int64_t most = 0;
   for (int32_t dtype : {DIFFOPT_F32, DIFFOPT_BF16})
-    for (int64_t rot : {(int64_t)0, (int64_t)1}) {  // 1: a rotated part that does not fall into pieces
-      const Plan p = plan_of(B, T, H, Hk, D, rot, dtype);
-      const int64_t n = ((int64_t)p.blocks.q + p.blocks.k) * D * 4;
-      most = n > most ? n : most;
-    }
+    for (int64_t rot : {(int64_t)0, (int64_t)1})  // 1: a rotated part that does not fall into pieces
+      for (Dir dir : {kBwd, kSecond}) {
+        const Plan p = plan_of(B, T, H, Hk, D, rot, dtype, dir);
+        const int64_t n = ((int64_t)p.blocks.q + p.blocks.k) * D * 4;
+        most = n > most ? n : most;
+      }
   return most;
 }
 

@@ -241,3 +241,18 @@ def test_refusals():
     (h,) = torch.autograd.grad(g.square().sum(), [x], create_graph=True)
     with pytest.raises(RuntimeError):  # a third order is refused, not taken as zero
         torch.autograd.grad(h.sum(), [x])
+
+
+@pytest.mark.parametrize("call", ["linear_attention", "qknorm_rope", "distillation_loss", "linear_attention_step"])
+def test_host_tensors_are_refused(call):
+    import paper_2211_06934_amd as P
+    q = torch.zeros(1, 3, 2, 8)
+    with pytest.raises(ValueError, match="device memory"):
+        if call == "linear_attention":
+            P.linear_attention(q, q, q, torch.zeros(2))
+        elif call == "qknorm_rope":
+            P.qknorm_rope(q, q)
+        elif call == "distillation_loss":
+            P.distillation_loss(torch.zeros(2, 9), torch.zeros(2, 3, dtype=torch.int64), torch.zeros(2, 3))
+        else:
+            P.linear_attention_step(q[:, 0], q[:, 0], q[:, 0], torch.zeros(2), torch.zeros(1, 2, 8, 8))
