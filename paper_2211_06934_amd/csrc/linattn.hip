@@ -493,13 +493,13 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
 
   const Scan a = jobs.scan[blockIdx.y];
   const int nq = OUT ? a.nq : 1;
-  int64_t x = blockIdx.x;
-  const int ct0 = (int)(x % col_tiles) * CT;
-  x /= col_tiles;
-  const int seg = (int)(x % jobs.nseg);
-  x /= jobs.nseg;
-  const int qh = (int)(x % nq);
-  const int64_t state = x / nq, b = state / sh.Hs;
+  uint32_t x = blockIdx.x;
+  const int ct0 = (int)(x % (uint32_t)col_tiles) * CT;
+  x /= (uint32_t)col_tiles;
+  const int seg = (int)(x % (uint32_t)jobs.nseg);
+  x /= (uint32_t)jobs.nseg;
+  const int qh = (int)(x % (uint32_t)nq);
+  const int64_t state = x / (uint32_t)nq, b = (uint32_t)state / (uint32_t)sh.Hs;
   if (b >= sh.B) return;  // the launch's scans differ in heads
   if (!OUT && !a.s1 && seg == jobs.nseg - 1) return;  // nothing follows the last segment
   const int j = (int)(state - b * sh.Hs);
@@ -517,26 +517,6 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
 
   const int wcol = 16 * NCT * wave;
   const bool all_columns = a.Dk == DK && a.Dv - ct0 >= CT;
-
-  // What the registers hold is the state over `scale`, the product of the decays
-  // since it was last brought up to date (kept to 48 bits: its roundings would add
-  // up over the chunks); scale and 1 / scale ride on the weights of the outputs and
-  // of the values.
-  const double gcd = exp(lgd * C);
-  const float gc = uniform((float)gcd), gc_lo = uniform((float)(gcd - (double)(float)gcd));
-  const double gld = exp(lgd * (double)(len % C));  // of the last chunk, where it is not whole
-  const float gl = uniform((float)gld), gl_lo = uniform((float)(gld - (double)(float)gld));
-  float scale = 1.0f, scale_lo = 0.0f;
-
-  // The powers of a chunk's tokens are products of one per lane and some that all
-  // lanes share (scalar registers): g^(16 t) and g, g^2, g^3.
-  const float ps = a.qs * a.ks;
-  const float qw = a.qs * power(lg2, m_ + 1 - back), kw = a.ks * power(lg2, 12 - 4 * g_ + back);
-  float tiles[NT], step[4];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) tiles[t] = uniform(power(lg2, 16 * t));
-#pragma unroll
-  for (int e = 0; e < 4; ++e) step[e] = uniform(power(lg2, e));
 
   const int dir = back ? -1 : 1;
   const Rows mq{dir * a.q.st}, mk{dir * a.k.st}, mv{dir * a.v.st}, mo{dir * a.o.st};
@@ -605,6 +585,26 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
     if (OUT) stage_q(pq, L);
     stage_k(pk, L);
   }
+
+  // What the registers hold is the state over `scale`, the product of the decays
+  // since it was last brought up to date (kept to 48 bits: its roundings would add
+  // up over the chunks); scale and 1 / scale ride on the weights of the outputs and
+  // of the values.
+  const double gcd = exp(lgd * C);
+  const float gc = uniform((float)gcd), gc_lo = uniform((float)(gcd - (double)(float)gcd));
+  const double gld = len % C ? exp(lgd * (double)(len % C)) : 1.0;  // of the last chunk, where it is not whole
+  const float gl = uniform((float)gld), gl_lo = uniform((float)(gld - (double)(float)gld));
+  float scale = 1.0f, scale_lo = 0.0f;
+
+  // The powers of a chunk's tokens are products of one per lane and some that all
+  // lanes share (scalar registers): g^(16 t) and g, g^2, g^3.
+  const float ps = a.qs * a.ks;
+  const float qw = a.qs * power(lg2, m_ + 1 - back), kw = a.ks * power(lg2, 12 - 4 * g_ + back);
+  float tiles[NT], step[4];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) tiles[t] = uniform(power(lg2, 16 * t));
+#pragma unroll
+  for (int e = 0; e < 4; ++e) step[e] = uniform(power(lg2, e));
 
   // the state: tile (kb, u), column tile ct; a lane holds column 16 (NCT wave + ct)
   // + m, rows 32 kb + 8 g + 4 u + i
