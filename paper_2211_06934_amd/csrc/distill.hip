@@ -271,7 +271,8 @@ __device__ __forceinline__ Slice slice_of(const Rows& r, int64_t block, int32_t 
   return s;
 }
 
-// A slice's max and sum, for rows that several workgroups share.
+// A slice's max and sum, for rows that several workgroups share.  One read of the
+// row, bound by latency for few of them (8 rows of 512 KiB: 4.5 us).
 template <class E_>
 __global__ __launch_bounds__(kDB) void distill_parts(Rows r, float* parts, int32_t slices, int64_t per) {
   __shared__ Reduce R;
@@ -313,9 +314,15 @@ enum Stats {
   kParts   // slices of the row
 };
 
+// A row (or a slice of one): the loss, with BWD its gradients.  Bound by memory, each
+// logit read once and each gradient written once: 4,096 rows of 50,021 bf16 logits,
+// 820 MB, take 174 us (4.7 TB/s; a copy of that size reaches 4.9 to 5.3), 1,024 rows
+// of 32,000 fp32 ones 54 us (4.9 TB/s).  With the exponentials kept in fp32 rather
+// than the packed logits half as many rows are in flight and it takes 192 us.
 template <class E_, int STATS, bool BWD, int B = kDB, int NV = 1>
-__global__ __launch_bounds__(B, (STATS == kKept ? kept_waves(B, NV) : 1)) void distill_row(Rows r, const float* dloss, float* loss, float* stats, E_* dlogits, int64_t drow_stride,
-                                                 float* dteacher, const float* parts, int32_t slices, int64_t per) {
+__global__ __launch_bounds__(B, (STATS == kKept ? kept_waves(B, NV) : 1)) void distill_row(
+    Rows r, const float* dloss, float* loss, float* stats, E_* dlogits, int64_t drow_stride, float* dteacher, const float* parts,
+    int32_t slices, int64_t per) {
   constexpr bool FWD = STATS != kGiven;
   __shared__ Entries E;
   __shared__ Reduce R;
@@ -468,6 +475,7 @@ __device__ __forceinline__ float block_sum(float x, Reduce& R) {
   return x;
 }
 
+// A slice's sum of p a, for rows that several workgroups share.
 template <class E_>
 __global__ __launch_bounds__(kDB) void distill_second_parts(Rows r, Second t, float* parts, int32_t slices, int64_t per) {
   __shared__ Reduce R;
@@ -477,6 +485,9 @@ __global__ __launch_bounds__(kDB) void distill_second_parts(Rows r, Second t, fl
   if (threadIdx.x == 0) parts[blockIdx.x] = pa;
 }
 
+// The gradient's own vector-Jacobian product for a row (or a slice of one): logits
+// and a read once, a result written.  Bound by memory: 1,024 rows of 32,000 fp32
+// logits, 393 MB, take 86 us (4.6 TB/s).
 template <class E_, int STATS, int B = kDB, int NV = 1>
 __global__ __launch_bounds__(B) void distill_second(Rows r, Second t, const float* parts, int32_t slices, int64_t per) {
   __shared__ Entries E;
@@ -638,9 +649,16 @@ int check_out_rows(const char* who, const void* out, int64_t stride, int64_t V, 
   return DIFFOPT_OK;
 }
 
-// Workgroups of a row: with fewer rows than kFewRows each is cut into slices of
-// at least kSliceBytes until kFillRows workgroups run.
+// Workgroups of a row: with fewer rows than kFewRows long ones are cut into slices
+// of at least kSliceBytes until kFillRows workgroups run.  fp32, the loss alone, cut
+// and whole: 8 rows of 512 KiB 8.4 and 15.4 us, 200 of them 23.6 and 28.7, 512 of
+// them 47.1 and 42.6.  Rows that a workgroup keeps in registers (up to 256 KiB) are
+// cut where there are fewer than kVeryFewRows (8 of 256 KiB 7.6 and 10.0, with the
+// gradient 10.7 and 13.0; 64 of them 10.4 and 10.2, with the gradient 18.3 and 15.5)
+// and longer than kShortBytes (8 of 125 KiB 7.6 and 7.3, with the gradient 10.8 and
+// 9.4).
 constexpr int64_t kFewRows = 256, kFillRows = 1024, kSliceBytes = 8192;
+constexpr int64_t kVeryFewRows = 32, kShortBytes = 128 * 1024, kLongBytes = 256 * 1024;
 
 struct Cut {
   int32_t slices;
@@ -648,7 +666,7 @@ struct Cut {
 };
 
 Cut cut_of(int64_t N, int64_t V, int32_t dtype) {
-  if (N >= kFewRows || N == 0) return Cut{1, V};
+  if (N >= kFewRows || N == 0 || V * elem_size(dtype) <= (N < kVeryFewRows ? kShortBytes : kLongBytes)) return Cut{1, V};
   int64_t n = kFillRows / N;
   const int64_t most = V * elem_size(dtype) / kSliceBytes;
   n = n > most ? most : n;

@@ -47,8 +47,12 @@ __device__ __forceinline__ E* at(const HeadArr& h, int64_t b, int64_t t, int64_t
   return static_cast<E*>(h.p) + b * h.sb + t * h.st + head * h.sh;
 }
 
-// Token after token: a workgroup holds 64 columns of one state, a lane R rows
-// by 4 columns of them.  For single tokens and short sequences.
+// Single tokens of any width and alignment (the others: linattn_one).  A workgroup
+// holds 64 columns of one state, a lane R rows by 4 columns of them, read and
+// written element by element.  Bound by the state's memory: 256 sequences of 16
+// heads of 128 take 241 us (2.2 TB/s), which linattn_one moves in 101.  Sequences
+// take chunks from two tokens on: token by token one of 2 tokens and 16 heads takes
+// 14 us against 10, 32 of 4 tokens 48 against 20.
 constexpr int kTokenB = 256, kTokenCols = 64;
 
 template <class E, int R>
@@ -136,7 +140,10 @@ __global__ __launch_bounds__(kTokenB) void linattn_tokens(Shape s, Scan a, int32
 // all its rows; a lane holds 4 columns of R rows, so that every load of a call
 // is in flight at once and the product with q is joined over lanes and waves.
 // Few columns a workgroup (32) put a single sequence's states on many compute
-// units; whole lines of 128 bytes a row are enough for the memory as well.
+// units; whole lines of 128 bytes a row are enough for the memory as well.  Heads
+// of 128, 16 a sequence: one sequence 3.9 us, bound by latency; 256 of them (537
+// MB) 101 us repeated in a graph, 120 us on fresh states (4.5 TB/s), bound by
+// memory.
 constexpr int kStepB = 256, kStepCG = 8, kStepGroup = 8;
 
 template <class E, int R>
@@ -228,6 +235,18 @@ __global__ __launch_bounds__(kStepB) void linattn_one(Shape s, Scan a, int32_t c
 // outputs are bf16 too); the state itself is fp32 and its update takes W_k V in
 // SPLIT bf16 parts, exact to 2^-8 SPLIT: two where only outputs follow, three
 // where a state is handed out.  fp32 runs on the fp32 matrix instructions.
+//
+// What bounds it is the walk: a chunk's products need one another (scores, barrier,
+// outputs, state), and a compute unit holds two workgroups of 128 columns (72 KiB of
+// LDS, 256 registers) to fill each other's waits.  Of 5.8 us a chunk of 64 tokens
+// the matrix unit works a third.  bf16, 16 heads of 128:
+//   16,384 tokens: 64 us for the outputs (4.2 TB/s of q, k, v, o and states), 42 for
+//   the segments' states, 16 for their join; the bytes alone would take 43
+//   2 x 8,192 tokens backward: 173 us for dq, dk, dv (805 MB, 4.7 TB/s), 67 states
+// Eight waves of 16 columns on two buffers, one workgroup a compute unit, took 530
+// us for both ways of the latter where two workgroups of four waves took 442; chunks
+// through registers instead of straight to LDS 710.  For dq, dk, dv the operands are
+// read three times: one walk of all three would need three states in registers.
 
 template <class E>
 struct Frag;
@@ -980,6 +999,8 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
 
 // The segments' own states to the states before them, in place, and the last:
 //   before_0 = s0, before_{i+1} = g^(tokens of i) before_i + own_i
+// One element a lane, eight segments in flight; bound by memory (32 segments of 16
+// heads of 128, 67 MB: 16 us, 4.1 TB/s).
 constexpr int kJoinB = 256, kJoinAhead = 8;
 __global__ __launch_bounds__(kJoinB) void linattn_join(Shape sh, Jobs jobs) {
   const Scan& a = jobs.scan[blockIdx.y];
@@ -1200,22 +1221,9 @@ void launch_chunks(const Shape& s, const Jobs& jobs, int n, bool states, hipStre
   }
 }
 
-// Sequences of up to this many tokens go token after token.
-constexpr int kFewTokens = 4;
-
 // Runs the scans whose `run` is set; `a` holds all the call's scans, by which
 // the plan goes.
 int run_scans(const char* who, const Shape& s, const Scan* a, const bool* run, int n, int32_t dtype, void* workspace, int64_t bytes, hipStream_t st) {
-  if (s.T <= kFewTokens) {
-    for (int i = 0; i < n; ++i)
-      if (run[i]) {
-        if (dtype == DIFFOPT_F32)
-          launch_tokens<float>(s, a[i], st);
-        else
-          launch_tokens<bf16>(s, a[i], st);
-      }
-    return launch_status(who);
-  }
   const Plan p = plan_of(s, a, n, dtype);
   const int64_t need = workspace_of(s, a, n, dtype);
   if (need > 0 && (!workspace || bytes < need))
@@ -1289,7 +1297,7 @@ using namespace diffopt;
 extern "C" int64_t diffopt_linattn_workspace(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t Dk, int64_t Dv,
                                              int32_t dtype, int32_t backward) {
   if (sizes_wrong(B, T, H, Hk, Dk, Dv, dtype)) return -1;
-  if (B == 0 || Hk == 0 || T <= kFewTokens) return 0;
+  if (B == 0 || Hk == 0 || T == 0) return 0;
   Scan a[3];
   const int n = backward ? backward_scans(H, Hk, Dk, Dv, a) : forward_scans(H, Hk, Dk, Dv, a);
   return workspace_of(Shape{B, T, (int32_t)Hk, nullptr, nullptr}, a, n, dtype);

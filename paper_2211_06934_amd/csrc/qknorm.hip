@@ -59,7 +59,10 @@ __device__ __forceinline__ int64_t position_of(const QkShape& s, int64_t b, int6
                                : static_cast<const int64_t*>(s.positions)[at];
 }
 
-// NP pairs per lane: heads of up to 128 NP elements.
+// Any width and few heads: NP pairs per lane, heads of up to 128 NP elements, a wave
+// for each.  Element by element, so bound by the number of loads: 16,384 tokens of 40
+// heads of 128 in bf16 take 219 us forward and 415 backward, where pieces take 63 and
+// 111; one token's 3.0 and 3.4 us are latency.
 template <class E, int DIR, int NP>
 __global__ __launch_bounds__(kQB) void qknorm_any(QkShape s, QkArgs A, int32_t q_blocks) {
   const int side = (int)blockIdx.x >= q_blocks;
@@ -405,7 +408,9 @@ __global__ __launch_bounds__(kQB) void qknorm_pieces(QkShape s, QkArgs A, int32_
   }
 }
 
-// dw[d] = the sum of the workgroups' parts: one workgroup per 8 elements of a side.
+// dw[d] = the sum of the workgroups' parts: one workgroup per 8 elements of a side,
+// 32 rows of parts at a time; bound by latency (768 parts of 128 elements of two
+// sides, 0.8 MB: 4.9 us).
 constexpr int kRB = 256, kRCols = 8, kRRows = kRB / kRCols;
 __global__ __launch_bounds__(kRB) void qknorm_weights(const float* partial, int32_t q_blocks, int32_t k_blocks, int32_t D,
                                                       float* dwq, float* dwk) {
@@ -452,13 +457,18 @@ struct Plan {
 int64_t piece_blocks(int32_t dtype, Dir dir) { return 256 * (dir == kFwd ? 4 : dir == kSecond && dtype == DIFFOPT_BF16 ? 2 : 3); }
 
 // Widths that fall into pairs of pieces, with up to 32 lanes a head, and counts
-// of tokens that 32 bits index.
+// of tokens that 32 bits index.  Calls of few heads take a wave for each instead,
+// which starts sooner (40 heads of 128 in bf16, forward and backward: 3.0 and 3.4
+// us against 3.6 and 4.5; 64 tokens of them 3.6 and 3.9 against 3.9 and 4.8; but
+// 1,024 tokens 14.4 and 18.2 against 6.3 and 8.5).
+constexpr double kFewHeads = 4096.0;
+
 Plan plan_of(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t D, int64_t rot, int32_t dtype, Dir dir) {
   const int64_t most = piece_blocks(dtype, dir);
   Plan p{};
   const int two = dtype == DIFFOPT_F32 ? 8 : 16;  // elements of a lane
   const int64_t lanes = D / two;
-  if (D % two == 0 && rot % two == 0 && lanes <= (dtype == DIFFOPT_F32 ? 32 : 16) && (double)B * T * 256.0 < 2147483648.0 && B * T > 0) {
+  if (D % two == 0 && rot % two == 0 && (double)B * T * (H + Hk) > kFewHeads && lanes <= (dtype == DIFFOPT_F32 ? 32 : 16) && (double)B * T * 256.0 < 2147483648.0 && B * T > 0) {
     p.pieces = true;
     for (p.lpg = 4; p.lpg < lanes;) p.lpg *= 2;
     // a token's heads are split until the card has waves enough
