@@ -536,7 +536,8 @@ typedef struct diffopt_heads {
  *   lengths    DEVICE int32 [B] in [0, T] (clamped), or NULL for T
  *   state, state_out  fp32 [B][Hk][Dk][Dv], or NULL (zeros / not wanted);
  *              state_out may be state
- *   1 <= Dk, Dv <= 256; H a multiple of Hk; scale finite; T <= 2^35
+ *   1 <= Dk, Dv <= 256; H a multiple of Hk, <= 65536; scale finite;
+ *              T <= 2^35; B H ceil(max(Dk, Dv) / 32) < 2^24
  *   workspace  device scratch of diffopt_linattn_workspace(..., backward 0)
  *              bytes (its contents do not matter, 16-byte aligned); NULL if
  *              that is 0
@@ -664,7 +665,7 @@ int64_t diffopt_qknorm_rope_workspace(int64_t B, int64_t T, int64_t H,
  *            A negative id, or a teacher logit of -inf, is no entry; a row
  *            with none has loss 0 and gradients 0.  An id >= V makes its
  *            row's results NaN.  Entries of one token add up.
- *   teacher  fp32 [N][K];  1 <= K <= 1024
+ *   teacher  fp32 [N][K];  1 <= K <= 1024;  N < 2^22
  *   loss     fp32 [N]
  *   stats    fp32 [N][2]: the row's max and its sum of exp((x - max) / T),
  *            which the backwards take

@@ -20,6 +20,7 @@ namespace {
 
 constexpr int kDB = 512;       // threads per workgroup
 constexpr int kMaxK = 1024;    // entries of a row
+constexpr int64_t kMostRows = int64_t(1) << 22;  // a launch has fewer than 2^32 threads, a workgroup of up to 1024 for each row
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Rows {
@@ -620,7 +621,7 @@ __global__ __launch_bounds__(B) void distill_second(Rows r, Second t, const floa
 int check_rows(const char* who, const void* logits, int64_t row_stride, int64_t N, int64_t V, int32_t dtype,
                const void* ids, int32_t id_bytes, const float* teacher, int64_t K, double temperature, Rows* r) {
   if (N < 0) return fail(DIFFOPT_EINVAL, "%s: N must be >= 0", who);
-  if (N > 0x7fffffff) return fail(DIFFOPT_EINVAL, "%s: N must be below 2^31", who);
+  if (N >= kMostRows) return fail(DIFFOPT_EINVAL, "%s: N must be below 2^22", who);
   if (V < 1 || V > 0x7fffffff) return fail(DIFFOPT_EINVAL, "%s: V must be in [1, 2^31)", who);
   if (!dtype_ok(dtype)) return fail(DIFFOPT_EINVAL, "%s: unknown element type %d", who, (int)dtype);
   if (id_bytes != 4 && id_bytes != 8) return fail(DIFFOPT_EINVAL, "%s: id_bytes must be 4 or 8", who);
@@ -767,7 +768,7 @@ int check_workspace(const char* who, const Rows& r, int32_t dtype, void* workspa
 using namespace diffopt;
 
 extern "C" int64_t diffopt_distill_workspace(int64_t N, int64_t V, int32_t dtype, int64_t K) {
-  if (N < 0 || N > 0x7fffffff || V < 1 || V > 0x7fffffff || !dtype_ok(dtype) || K < 1 || K > kMaxK) return -1;
+  if (N < 0 || N >= kMostRows || V < 1 || V > 0x7fffffff || !dtype_ok(dtype) || K < 1 || K > kMaxK) return -1;
   const Cut c = cut_of(N, V, dtype);
   return c.slices > 1 ? N * c.slices * 8 : 0;
 }

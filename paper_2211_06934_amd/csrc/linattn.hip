@@ -1266,7 +1266,11 @@ const char* sizes_wrong(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t Dk,
   if ((H == 0) != (Hk == 0) || (Hk > 0 && H % Hk)) return "H must be a multiple of Hk";
   if (Dk < 1 || Dk > kMaxWidth || Dv < 1 || Dv > kMaxWidth) return "Dk and Dv must be in [1, 256]";
   if (!dtype_ok(dtype)) return "unknown element type";
-  if (H > 65536 || B > (int64_t(1) << 24) || B * Hk > (int64_t(1) << 24) || T > (int64_t(1) << 35)) return "too many heads, sequences or tokens";
+  // a launch has fewer than 2^32 threads, a workgroup of 256 for each head and 32
+  // columns at most
+  constexpr int64_t kMost = int64_t(1) << 24;
+  if (H > 65536 || B >= kMost || B * H * (((Dk > Dv ? Dk : Dv) + 31) / 32) >= kMost || T > (int64_t(1) << 35))
+    return "too many heads, sequences or tokens";
   return nullptr;
 }
 

@@ -41,6 +41,7 @@ def _linattn(**change):
     (dict(scale=math.inf), "scale"), (dict(scale=1e300), "scale"), (dict(lg=None), "null log_decay"), (dict(lg=odd), "aligned"),
     (dict(lengths=odd), "aligned"), (dict(state=odd), "aligned"), (dict(state_out=odd), "aligned"), (dict(q=None), "null q"),
     (dict(out=None), "null out"), (dict(T=1 << 36), "too many"), (dict(H=1 << 17, Hk=1), "too many"), (dict(B=1 << 25), "too many"),
+    (dict(B=1 << 18, H=64, Hk=64, Dk=8, Dv=8), "too many"), (dict(B=1 << 17, H=64, Hk=64, Dk=8, Dv=64), "too many"),
 ])
 def test_linattn_fwd_refuses(change, word):
     _refused(_linattn(**change), word)
@@ -131,7 +132,7 @@ def _distill(**change):
                                    a["stats"], a["ws"], a["nws"], None)
 
 
-@pytest.mark.parametrize("change", [dict(N=-1), dict(V=-1), dict(K=0), dict(K=1025), dict(dtype=5), dict(ib=3), dict(T=0.0), dict(T=-1.0),
+@pytest.mark.parametrize("change", [dict(N=-1), dict(N=1 << 22), dict(V=-1), dict(K=0), dict(K=1025), dict(dtype=5), dict(ib=3), dict(T=0.0), dict(T=-1.0),
                                     dict(T=math.nan), dict(T=math.inf), dict(x=None), dict(ids=None), dict(t=None), dict(loss=None),
                                     dict(stats=None), dict(x=odd), dict(t=odd), dict(ids=ctypes.c_void_p(68), ib=8), dict(stats=odd)])
 def test_distill_refuses(change):
