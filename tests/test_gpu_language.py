@@ -217,7 +217,7 @@ def test_expanded_cotangents_and_operands():
     grads = torch.autograd.grad(one, [q, k, v], create_graph=True)
     torch.autograd.grad(sum(g.sum() for g in grads), [q, k, v])
     out, _ = linattn(q.detach().cpu(), k[:, :, :1].expand(-1, -1, 2, -1).detach().cpu(), v.detach().cpu(), lg.cpu())
-    assert abs(float(one) - float(out.sum())) <= 1e-4 * float(out.abs().sum()) ** 0.5 * 10
+    assert abs(float(one.detach()) - float(out.sum())) <= 1e-4 * float(out.abs().sum()) ** 0.5 * 10
 
 
 def test_refusals():
