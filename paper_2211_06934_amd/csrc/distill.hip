@@ -49,13 +49,18 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 __device__ __forceinline__ float safe_max(float m) { return m == -kInf ? 0.0f : m; }
 
 // exp((x - b) / T) for many x and one b: 2^(x c - b c) by one multiply-add, with
-// what the rounding of b c leaves out as a factor of its own.  Where b c
-// overflows, `wide` takes the difference first.
+// what the rounding of b c leaves out as a factor of its own.  That factor and what
+// it corrects are 2^-+r with |r| up to half a last place of b c: harmless while |b c|
+// stays below 2^24 (|r| <= 1/2), infinite times zero from about 2^31 on.  `wide` takes
+// the difference first; the factor goes with the form that a wave has taken.
 struct Shift {
   float b, c, bc;
   bool wide;
-  __device__ __forceinline__ Shift(float b_, float c_) : b(b_), c(c_), bc(b_ * c_), wide(!(__builtin_fabsf(bc) < 1e30f)) {}
-  __device__ __forceinline__ float factor() const { return wide ? 1.0f : exp2_fast(-__builtin_fmaf(b, c, -bc)); }
+  __device__ __forceinline__ Shift(float b_, float c_) : b(b_), c(c_), bc(b_ * c_), wide(!(__builtin_fabsf(bc) < 0x1p24f)) {}
+  template <bool WIDE>
+  __device__ __forceinline__ float factor() const {
+    return WIDE ? 1.0f : exp2_fast(-__builtin_fmaf(b, c, -bc));
+  }
   template <bool WIDE>
   __device__ __forceinline__ float part(float x) const {
     return exp2_fast(WIDE ? (x - b) * c : __builtin_fmaf(x, c, -bc));
@@ -364,7 +369,7 @@ __global__ __launch_bounds__(B, (STATS == kKept ? kept_waves(B, NV) : 1)) void d
 #pragma unroll
         for (int k = 0; k < N; ++k) run.s += sh.part<wide.value>(e[k]);
       }
-      run.s *= sh.factor();
+      run.s *= sh.factor<wide.value>();
     };
     if (__any(sh.wide))
       sum(std::true_type{});
@@ -403,7 +408,6 @@ __global__ __launch_bounds__(B, (STATS == kKept ? kept_waves(B, NV) : 1)) void d
   auto one = [&](int64_t at, float e) { dx[at] = (E_)(some ? w * exp2_fast((e - m) * c) : 0.0f); };
   if (STATS == kKept) {
     const Shift sh(m, c);
-    const float f = w * sh.factor();
     auto write = [&](auto value) {
 #pragma unroll
       for (int i = 0; i < NV; ++i)
@@ -419,9 +423,9 @@ __global__ __launch_bounds__(B, (STATS == kKept ? kept_waves(B, NV) : 1)) void d
     if (!some)
       write([](float) { return 0.0f; });
     else if (sh.wide)
-      write([&](float e) { return f * sh.part<true>(e); });
+      write([&](float e) { return w * sh.part<true>(e); });
     else
-      write([&](float e) { return f * sh.part<false>(e); });
+      write([&, f = w * sh.factor<false>()](float e) { return f * sh.part<false>(e); });
   } else {
     over_row(
         x, sl.c0, sl.c1,
@@ -530,7 +534,7 @@ __global__ __launch_bounds__(B) void distill_second(Rows r, Second t, const floa
 #pragma unroll
         for (int k = 0; k < Vec<E_>::N; ++k) pa += sh.part<wide.value>(e[k]) * u[k];
       }
-      pa *= sh.factor();
+      pa *= sh.factor<wide.value>();
     };
     if (sh.wide)
       sum(std::true_type{});
@@ -576,7 +580,6 @@ __global__ __launch_bounds__(B) void distill_second(Rows r, Second t, const floa
   };
   auto one = [&](int64_t at, float v, float u) { y[at] = (E_)(dense ? w * exp2_fast((v - m) * c) * (u - pa) : 0.0f); };
   if (STATS == kKept && a) {
-    const float f = w * sh.factor();
     auto write = [&](auto value) {
 #pragma unroll
       for (int i = 0; i < NV; ++i)
@@ -593,9 +596,9 @@ __global__ __launch_bounds__(B) void distill_second(Rows r, Second t, const floa
     if (!some)
       write([](float, float) { return 0.0f; });
     else if (sh.wide)
-      write([&](float e, float u) { return f * sh.part<true>(e) * (u - pa); });
+      write([&](float e, float u) { return w * sh.part<true>(e) * (u - pa); });
     else
-      write([&](float e, float u) { return f * sh.part<false>(e) * (u - pa); });
+      write([&, f = w * sh.factor<false>()](float e, float u) { return f * sh.part<false>(e) * (u - pa); });
   } else {
     const E_* b = a ? a : x;
     over_row(
