@@ -632,7 +632,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   float* segments = cut ? jobs.seg[blockIdx.y] + (state * jobs.nseg + seg) * a.Dk * a.Dv : nullptr;
   f32x4 S[KB][2][NCT];
   {
-    const float* s0 = !OUT ? nullptr : cut ? segments : a.s0 ? a.s0 + state * a.Dk * a.Dv : nullptr;
+    const float* s0 = cut ? (OUT ? segments : nullptr) : a.s0 ? a.s0 + state * a.Dk * a.Dv : nullptr;
     const bool flip = cut ? a.flip_seg : a.flip;
     typedef f32x4 four __attribute__((aligned(4)));
     if (!s0) {
@@ -967,7 +967,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
     for (int64_t t = from + wave; t < to; t += kWaves)
       for (int col = ct0 + lane; col < ct0 + CT && col < a.Dv; col += 64) o[t * a.o.st + col] = (E)0.0f;
   }
-  float* s1 = !OUT ? segments : !cut && a.s1 && qh == 0 ? a.s1 + state * a.Dk * a.Dv : nullptr;
+  float* s1 = cut ? (OUT ? nullptr : segments) : a.s1 && qh == 0 ? a.s1 + state * a.Dk * a.Dv : nullptr;
   if (s1) {
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));  // addresses anew: those of the initial state are not kept over the walk
@@ -1165,14 +1165,13 @@ int64_t workspace_of(const Shape& s, const Scan* a, int n, int32_t dtype) {
 }
 
 template <class E, int DK, int NCT, bool PIECES>
-void launch_class(const Shape& s, const Jobs& jobs, int n, bool states, hipStream_t st) {
+void launch_class(const Shape& s, const Jobs& jobs, int n, bool states, bool keep, hipStream_t st) {
   constexpr int MOST = sizeof(E) == 2 ? 3 : 1, SPLIT = sizeof(E) == 2 && PIECES ? 2 : MOST;
   int64_t tiles = 0, main = 0, own = 0;
-  bool keep = false;  // a state is handed out
   for (int i = 0; i < n; ++i) {
     const int64_t c = col_tiles(jobs.scan[i], sizeof(E) == 4 ? DIFFOPT_F32 : DIFFOPT_BF16);
     tiles = c > tiles ? c : tiles;
-    keep |= jobs.scan[i].s1 != nullptr && (states || jobs.nseg == 1);
+    keep |= jobs.scan[i].s1 != nullptr && (states || jobs.nseg == 1);  // a state is handed out
   }
   for (int i = 0; i < n; ++i) {
     const int64_t w = s.B * s.Hs * jobs.nseg * tiles;
@@ -1190,8 +1189,9 @@ void launch_class(const Shape& s, const Jobs& jobs, int n, bool states, hipStrea
     hipLaunchKernelGGL((linattn_chunks<E, DK, NCT, SPLIT, true, PIECES>), grid, block, 0, st, s, jobs, (int32_t)tiles);
 }
 
+// `keep`: the values' parts as where a state is handed out, also if none is.
 template <class E>
-void launch_chunks(const Shape& s, const Jobs& jobs, int n, bool states, hipStream_t st) {
+void launch_chunks(const Shape& s, const Jobs& jobs, int n, bool states, bool keep, hipStream_t st) {
   // scans of one class share a launch
   bool done[3] = {false, false, false};
   const int32_t dtype = sizeof(E) == 4 ? DIFFOPT_F32 : DIFFOPT_BF16;
@@ -1208,8 +1208,8 @@ void launch_chunks(const Shape& s, const Jobs& jobs, int n, bool states, hipStre
       part.seg[k++] = jobs.seg[l];
     }
 #define DIFFOPT_CLASS(DK, NCT)                                        \
-  if (c.dk == DK && c.pieces) launch_class<E, DK, NCT, true>(s, part, k, states, st); \
-  if (c.dk == DK && !c.pieces) launch_class<E, DK, NCT, false>(s, part, k, states, st);
+  if (c.dk == DK && c.pieces) launch_class<E, DK, NCT, true>(s, part, k, states, keep, st); \
+  if (c.dk == DK && !c.pieces) launch_class<E, DK, NCT, false>(s, part, k, states, keep, st);
     DIFFOPT_CLASS(32, 1)
     DIFFOPT_CLASS(64, 1)
     DIFFOPT_CLASS(128, 2)
@@ -1254,11 +1254,19 @@ int run_scans(const char* who, const Shape& s, const Scan* a, const bool* run, i
   if (nwalk == 0) return DIFFOPT_OK;
   const bool f32 = dtype == DIFFOPT_F32;
   if (p.nseg > 1) {
-    f32 ? launch_chunks<float>(s, own, nown, true, st) : launch_chunks<bf16>(s, own, nown, true, st);
+    f32 ? launch_chunks<float>(s, own, nown, true, false, st) : launch_chunks<bf16>(s, own, nown, true, false, st);
     const int64_t groups = s.B * s.Hs * ((own.scan[0].Dk * own.scan[0].Dv + kJoinB - 1) / kJoinB);
     hipLaunchKernelGGL(linattn_join, dim3((unsigned)groups, nown), dim3(kJoinB), 0, st, s, own);
   }
-  f32 ? launch_chunks<float>(s, walk, nwalk, false, st) : launch_chunks<bf16>(s, walk, nwalk, false, st);
+  // A state in place, in one segment, that several workgroups begin from (one for each
+  // query head): no order holds between one's last store and another's loads, so the
+  // outputs come first and the state in a launch of its own, a workgroup for each.
+  Scan& only = walk.scan[0];
+  const bool after = p.nseg == 1 && nwalk == 1 && only.nq > 1 && only.s1 && only.s1 == only.s0;
+  const Jobs state = walk;
+  if (after) only.s1 = nullptr;
+  f32 ? launch_chunks<float>(s, walk, nwalk, false, after, st) : launch_chunks<bf16>(s, walk, nwalk, false, after, st);
+  if (after) f32 ? launch_chunks<float>(s, state, 1, true, true, st) : launch_chunks<bf16>(s, state, 1, true, true, st);
   return launch_status(who);
 }
 
