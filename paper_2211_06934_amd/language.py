@@ -152,6 +152,8 @@ def linear_attention_step(q, k, v, log_decay, state, scale: float = 1.0) -> torc
         q, k, v = _dense(q), _dense(k), _dense(v)
         out = torch.empty(*q.shape[:2], v.shape[2], dtype=q.dtype, device=q.device)
         _o.linattn_step(q, k, v, log_decay, state, out, scale)
+    if not state.is_inference():  # the kernel wrote past torch: a graph that saved the state has to notice
+        torch.autograd.graph.increment_version(state)
     return out
 
 
