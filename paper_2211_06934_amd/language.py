@@ -147,7 +147,12 @@ def linear_attention(q, k, v, log_decay, state=None, lengths=None, scale: float 
 
 def linear_attention_step(q, k, v, log_decay, state, scale: float = 1.0) -> torch.Tensor:
     """One token of every sequence for generation: q [B, H, Dk], k [B, Hk, Dk], v [B, Hk, Dv] -> out [B, H, Dv]; `state` is
-    updated in place.  Not differentiable."""
+    updated in place.  Not differentiable: an operand that asks for a gradient is refused, but under torch.no_grad()."""
+    if torch.is_grad_enabled():
+        for x, what in ((q, "q"), (k, "k"), (v, "v"), (log_decay, "log_decay"), (state, "state")):
+            if isinstance(x, torch.Tensor) and x.requires_grad:
+                raise ValueError("linear_attention_step: %s asks for a gradient, and single tokens have none: detach it, or step "
+                                 "under torch.no_grad()" % what)
     with torch.no_grad():
         q, k, v = _dense(q), _dense(k), _dense(v)
         out = torch.empty(*q.shape[:2], v.shape[2], dtype=q.dtype, device=q.device)

@@ -41,6 +41,18 @@ def test_a_view_moves_its_base(step):
     assert states._version > before and float(states[1].min()) == 1.0 and not states[0].any()
 
 
+@pytest.mark.parametrize("name", ["q", "k", "v", "log_decay", "state"])
+def test_operands_that_ask_for_gradients_are_refused(step, name):
+    a = _operands()
+    a[name] = a[name].requires_grad_()
+    with pytest.raises(ValueError, match=name):
+        step(**a)
+    assert not a["state"].any()  # nothing was run
+    with torch.no_grad():
+        assert not step(**a).requires_grad
+    assert float(a["state"].detach().max()) == 1.0
+
+
 def test_inference_tensors(step):
     with torch.inference_mode():
         a = _operands()
