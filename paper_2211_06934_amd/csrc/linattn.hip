@@ -421,6 +421,7 @@ struct ChunkOf {
 };
 
 constexpr int kWaves = 4, kChunkB = 64 * kWaves;
+constexpr int kRescale = 8;
 
 // Rows of a chunk in memory: row r lies r `st` elements from row 0 (st < 0: back in
 // time).  Addresses are a pointer that all lanes share, to the row that comes first in
@@ -606,10 +607,12 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
     stage_k(pk, L);
   }
 
-  // What the registers hold is the state over `scale`, the product of the decays
-  // since it was last brought up to date (kept to 48 bits: its roundings would add
-  // up over the chunks); scale and 1 / scale ride on the weights of the outputs and
-  // of the values.
+  // What the registers hold is the state over `scale`: the product of the decays since
+  // the beginning (kept to 48 bits, as its roundings would add up over the chunks),
+  // times a power of two that keeps it between 1 and 2^(kRescale + 1).  So the registers
+  // never hold more than the state itself, and 1 / scale, which rides on the weights of
+  // the values, is never above 1: nothing overflows that the recurrence would not
+  // (states below 2^-117 lose their last bits).  scale rides on the outputs' weights.
   const double gcd = exp(lgd * C);
   const float gc = uniform((float)gcd), gc_lo = uniform((float)(gcd - (double)(float)gcd));
   const double gld = len % C ? exp(lgd * (double)(len % C)) : 1.0;  // of the last chunk, where it is not whole
@@ -872,15 +875,18 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
       const float x = scale * d, y = fmaf(scale, d, -x) + fmaf(scale, d_lo, scale_lo * d);
       scale = uniform(x + y);
       scale_lo = uniform(y - (scale - x));
-      if (!(scale > 0x1p-40f)) {
+      if (!(scale >= 1.0f)) {
+        const bool far = !(scale > 0x1p-60f);  // hardly anything is left, or nothing at all
+        const uint32_t bits = __builtin_bit_cast(uint32_t, scale) & 0x7f800000u, one = 127u << 23, top = (uint32_t)kRescale << 23;
+        const float down = far ? scale : __builtin_bit_cast(float, bits - top), up = __builtin_bit_cast(float, 2 * one - bits + top);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int ct = 0; ct < NCT; ++ct) S[kb][u][ct] *= scale;
-        scale = 1.0f;
-        scale_lo = 0.0f;
+            for (int ct = 0; ct < NCT; ++ct) S[kb][u][ct] *= down;
+        scale = far ? 1.0f : scale * up;
+        scale_lo = far ? 0.0f : scale_lo * up;
       }
     }
     const float back_to = uniform(1.0f / scale);
