@@ -572,13 +572,14 @@ __global__ __launch_bounds__(B) void distill_second(Rows r, Second t, const floa
   }
   const float w = some ? g * inv : 0.0f;
   const bool dense = a && some;
+  const float rest = bad ? kNan : 0.0f;  // where no cotangent of dlogits is given
   auto piece = [&](int64_t at, const float* e, const float* u) {
     float z[Vec<E_>::N];
 #pragma unroll
-    for (int i = 0; i < Vec<E_>::N; ++i) z[i] = dense ? w * exp2_fast((e[i] - m) * c) * (u[i] - pa) : 0.0f;
+    for (int i = 0; i < Vec<E_>::N; ++i) z[i] = dense ? w * exp2_fast((e[i] - m) * c) * (u[i] - pa) : rest;
     store_vec(y + at, z);
   };
-  auto one = [&](int64_t at, float v, float u) { y[at] = (E_)(dense ? w * exp2_fast((v - m) * c) * (u - pa) : 0.0f); };
+  auto one = [&](int64_t at, float v, float u) { y[at] = (E_)(dense ? w * exp2_fast((v - m) * c) * (u - pa) : rest); };
   if (STATS == kKept && a) {
     auto write = [&](auto value) {
 #pragma unroll
