@@ -12,11 +12,6 @@
 namespace diffopt {
 namespace {
 
-struct HeadArr {
-  void* p;
-  int64_t sb, st, sh;
-};
-
 // One scan: state head j of sequence b reads query heads j nq .. + nq and k/v
 // heads j nk .. + nk (one of nq, nk is 1).
 struct Scan {
@@ -1287,13 +1282,6 @@ const char* sizes_wrong(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t Dk,
   if (H > 65536 || B >= kMost || B * H * (((Dk > Dv ? Dk : Dv) + 31) / 32) >= kMost || T > (int64_t(1) << 35))
     return "too many heads, sequences or tokens";
   return nullptr;
-}
-
-int check_heads(const char* who, const char* what, const diffopt_heads* h, int32_t dtype, HeadArr* out) {
-  if (!h || !h->data) return fail(DIFFOPT_EINVAL, "%s: null %s", who, what);
-  if (!aligned_to(h->data, elem_size(dtype))) return fail(DIFFOPT_EINVAL, "%s: %s is not aligned to its elements", who, what);
-  *out = HeadArr{h->data, h->stride_b, h->stride_t, h->stride_h};
-  return DIFFOPT_OK;
 }
 
 int check_call(const char* who, int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t Dk, int64_t Dv, int32_t dtype, double scale,

@@ -64,8 +64,21 @@ __device__ __forceinline__ float wave_max(float x) {
   return x;
 }
 
+// A [B][T][heads][width] operand: strides in elements.
+struct HeadArr {
+  void* p;
+  int64_t sb, st, sh;
+};
+
 inline bool dtype_ok(int32_t dtype) { return dtype == DIFFOPT_F32 || dtype == DIFFOPT_BF16; }
 inline int64_t elem_size(int32_t dtype) { return dtype == DIFFOPT_F32 ? 4 : 2; }
 inline bool aligned_to(const void* p, int64_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
+
+inline int check_heads(const char* who, const char* what, const diffopt_heads* h, int32_t dtype, HeadArr* out) {
+  if (!h || !h->data) return fail(DIFFOPT_EINVAL, "%s: null %s", who, what);
+  if (!aligned_to(h->data, elem_size(dtype))) return fail(DIFFOPT_EINVAL, "%s: %s is not aligned to its elements", who, what);
+  *out = HeadArr{h->data, h->stride_b, h->stride_t, h->stride_h};
+  return DIFFOPT_OK;
+}
 
 }  // namespace diffopt

@@ -22,11 +22,6 @@ constexpr int kQB = 256;        // threads per workgroup
 constexpr int kQWaves = kQB / 64;
 constexpr int kMaxBlocks = 2048;  // workgroups per launch (they walk the heads)
 
-struct HeadArr {
-  void* p;
-  int64_t sb, st, sh;
-};
-
 struct QkShape {
   int64_t B, T;
   int32_t H, Hk, D, rot, interleaved;
@@ -494,13 +489,6 @@ Plan plan_of(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t D, int64_t rot
   p.blocks = Blocks{side(nq), side(nk)};
   p.grid = p.blocks.q + p.blocks.k;
   return p;
-}
-
-int check_heads(const char* who, const char* what, const diffopt_heads* h, int32_t dtype, HeadArr* out) {
-  if (!h || !h->data) return fail(DIFFOPT_EINVAL, "%s: null %s", who, what);
-  if (!aligned_to(h->data, elem_size(dtype))) return fail(DIFFOPT_EINVAL, "%s: %s is not aligned to its elements", who, what);
-  *out = HeadArr{h->data, h->stride_b, h->stride_t, h->stride_h};
-  return DIFFOPT_OK;
 }
 
 bool sizes_ok(int64_t B, int64_t T, int64_t H, int64_t Hk, int64_t D) {
