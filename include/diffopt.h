@@ -518,7 +518,9 @@ int diffopt_es_weights(const float* fvals, const float* f0,
  * an axis of an input may be broadcast with stride 0, outputs must not
  * overlap themselves).  Pointers need the element type's alignment only;
  * 16-byte aligned rows are fastest (results agree but for the roundings of
- * sums in another order).                                                   */
+ * sums in another order).  Results must not overlap operands or one another
+ * where an entry point does not say that they may; where one begins at an
+ * address of the other the call is refused.                                 */
 typedef struct diffopt_heads {
   void* data;
   int64_t stride_b, stride_t, stride_h;
@@ -535,7 +537,7 @@ typedef struct diffopt_heads {
  *   log_decay  DEVICE fp32 [Hk], <= 0 (0: no decay; -inf: the token alone)
  *   lengths    DEVICE int32 [B] in [0, T] (clamped), or NULL for T
  *   state, state_out  fp32 [B][Hk][Dk][Dv], or NULL (zeros / not wanted);
- *              state_out may be state
+ *              state_out may be state, else lies apart from it
  *   1 <= Dk, Dv <= 256; H a multiple of Hk, <= 65536; scale finite;
  *              T <= 2^35; B H ceil(max(Dk, Dv) / 32) < 2^24
  *   workspace  device scratch of diffopt_linattn_workspace(..., backward 0)
@@ -558,8 +560,8 @@ int diffopt_linattn_fwd(const diffopt_heads* q, const diffopt_heads* k,
  *   dstate = scale sum_t g^(t+1) q_t dout_t^T + g^L dstate_out,  L = lengths[b]
  * with sums over the query heads that share a k/v head in dk, dv and dstate.
  * Each of dq, dk, dv (pointers to the struct) and dstate may be NULL: it is
- * then not computed.  dstate must be neither dstate_out nor state.  Rows from
- * L on get 0.  log_decay is a constant of the operator: it has no gradient.
+ * then not computed.  dstate must lie apart from dstate_out and state.  Rows
+ * from L on get 0.  log_decay is a constant of the operator: it has no gradient.
  * The three results are the forward's sum on permuted operands, so a
  * derivative of any order is made of the same calls.                       */
 int diffopt_linattn_bwd(const diffopt_heads* dout, const float* dstate_out,

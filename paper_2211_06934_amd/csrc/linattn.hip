@@ -1223,14 +1223,33 @@ void launch_chunks(const Shape& s, const Jobs& jobs, int n, bool states, bool ke
   }
 }
 
-// Runs the scans whose `run` is set; `a` holds all the call's scans, by which
-// the plan goes.
-int run_scans(const char* who, const Shape& s, const Scan* a, const bool* run, int n, int32_t dtype, void* workspace, int64_t bytes, hipStream_t st) {
-  const Plan p = plan_of(s, a, n, dtype);
+// Workgroups write results while others still read operands, in no order: a result
+// at the address of an operand or of another result is refused.  (Other overlaps, of
+// views that are cut differently, are the caller's to avoid.)
+int check_apart(const char* who, std::initializer_list<const void*> results, std::initializer_list<const void*> operands) {
+  for (auto r = results.begin(); r != results.end(); ++r) {
+    if (!*r) continue;
+    for (const void* p : operands)
+      if (*r == p) return fail(DIFFOPT_EINVAL, "%s: a result must not be an operand", who);
+    for (auto t = results.begin(); t != r; ++t)
+      if (*r == *t) return fail(DIFFOPT_EINVAL, "%s: two results must not be one tensor", who);
+  }
+  return DIFFOPT_OK;
+}
+
+// A call's workspace against what its scans need.
+int check_workspace(const char* who, const Shape& s, const Scan* a, int n, int32_t dtype, void* workspace, int64_t bytes) {
   const int64_t need = workspace_of(s, a, n, dtype);
   if (need > 0 && (!workspace || bytes < need))
     return fail(DIFFOPT_EINVAL, "%s: the workspace has %lld bytes of %lld", who, (long long)(workspace ? bytes : 0), (long long)need);
   if (!aligned_to(workspace, 16)) return fail(DIFFOPT_EINVAL, "%s: the workspace is not 16-byte aligned", who);
+  return DIFFOPT_OK;
+}
+
+// Runs the scans whose `run` is set; `a` holds all the call's scans, by which
+// the plan goes.
+int run_scans(const char* who, const Shape& s, const Scan* a, const bool* run, int n, int32_t dtype, void* workspace, hipStream_t st) {
+  const Plan p = plan_of(s, a, n, dtype);
   // `walk`: the scans whose outputs are wanted; `own`: those that have states of
   // their own to find first (dk takes dv's)
   Jobs walk{}, own{};
@@ -1335,7 +1354,12 @@ extern "C" int diffopt_linattn_fwd(const diffopt_heads* q, const diffopt_heads* 
   a[0].qs = (float)scale;
   a[0].ks = 1.0f;
   const bool run[1] = {true};
-  return run_scans(who, Shape{B, T, (int32_t)Hk, log_decay, lengths}, a, run, 1, dtype, workspace, workspace_bytes, as_stream(stream));
+  const Shape s{B, T, (int32_t)Hk, log_decay, lengths};
+  rc = check_workspace(who, s, a, 1, dtype, workspace, workspace_bytes);
+  if (!rc) rc = check_apart(who, {a[0].o.p}, {a[0].q.p, a[0].k.p, a[0].v.p});
+  if (!rc && state != state_out && overlap(state, B * Hk * Dk * Dv * 4, state_out, B * Hk * Dk * Dv * 4))
+    rc = fail(DIFFOPT_EINVAL, "%s: state_out must be state or lie apart from it", who);
+  return rc ? rc : run_scans(who, s, a, run, 1, dtype, workspace, as_stream(stream));
 }
 
 extern "C" int diffopt_linattn_bwd(const diffopt_heads* dout, const float* dstate_out, const diffopt_heads* q,
@@ -1348,7 +1372,8 @@ extern "C" int diffopt_linattn_bwd(const diffopt_heads* dout, const float* dstat
   static const char* who = "diffopt_linattn_bwd";
   int rc = check_call(who, B, T, H, Hk, Dk, Dv, dtype, scale, log_decay, lengths, {state, dstate_out, dstate});
   if (rc || B == 0 || Hk == 0) return rc;
-  if (dstate && (dstate == dstate_out || dstate == state))
+  const int64_t state_bytes = B * Hk * Dk * Dv * 4;
+  if (overlap(dstate, state_bytes, dstate_out, state_bytes) || overlap(dstate, state_bytes, state, state_bytes))
     return fail(DIFFOPT_EINVAL, "%s: dstate must be neither dstate_out nor state", who);
   HeadArr Q{}, K{}, V{}, DO{};
   Scan a[3];
@@ -1374,7 +1399,10 @@ extern "C" int diffopt_linattn_bwd(const diffopt_heads* dout, const float* dstat
   }
   a[2].s1 = dstate;
   const bool run[3] = {a[0].o.p != nullptr, a[1].o.p != nullptr, a[2].o.p != nullptr || dstate != nullptr};
-  return run_scans(who, Shape{B, T, (int32_t)Hk, log_decay, lengths}, a, run, 3, dtype, workspace, workspace_bytes, as_stream(stream));
+  const Shape s{B, T, (int32_t)Hk, log_decay, lengths};
+  rc = check_workspace(who, s, a, 3, dtype, workspace, workspace_bytes);
+  if (!rc) rc = check_apart(who, {a[0].o.p, a[1].o.p, a[2].o.p}, {DO.p, Q.p, K.p, V.p});
+  return rc ? rc : run_scans(who, s, a, run, 3, dtype, workspace, as_stream(stream));
 }
 
 extern "C" int diffopt_linattn_step(const diffopt_heads* q, const diffopt_heads* k, const diffopt_heads* v,
@@ -1391,6 +1419,7 @@ extern "C" int diffopt_linattn_step(const diffopt_heads* q, const diffopt_heads*
   if (!rc) rc = check_heads(who, "k", k, dtype, &a[0].k);
   if (!rc) rc = check_heads(who, "v", v, dtype, &a[0].v);
   if (!rc) rc = check_heads(who, "out", out, dtype, &a[0].o);
+  if (!rc) rc = check_apart(who, {a[0].o.p}, {a[0].q.p, a[0].k.p, a[0].v.p});
   if (rc) return rc;
   a[0].s0 = state;
   a[0].s1 = state;

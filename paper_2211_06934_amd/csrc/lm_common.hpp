@@ -81,4 +81,11 @@ inline int check_heads(const char* who, const char* what, const diffopt_heads* h
   return DIFFOPT_OK;
 }
 
+// Whether a and b (either may be NULL) share bytes.
+inline bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  if (!a || !b) return false;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + (uint64_t)b_bytes && y < x + (uint64_t)a_bytes;
+}
+
 }  // namespace diffopt
