@@ -671,7 +671,9 @@ int64_t diffopt_qknorm_rope_workspace(int64_t B, int64_t T, int64_t H,
  *   loss     fp32 [N]
  *   stats    fp32 [N][2]: the row's max and its sum of exp((x - max) / T),
  *            which the backwards take
- *   workspace  diffopt_distill_workspace() bytes, or NULL if that is 0       */
+ *   workspace  diffopt_distill_workspace() bytes, or NULL if that is 0
+ * Results must not overlap operands or one another where an entry point does
+ * not say that they may.                                                    */
 int diffopt_distill_fwd(const void* logits, int64_t row_stride, int64_t N,
                         int64_t V, int32_t dtype, const void* ids,
                         int32_t id_bytes, const float* teacher, int64_t K,
@@ -680,7 +682,8 @@ int diffopt_distill_fwd(const void* logits, int64_t row_stride, int64_t N,
                         void* stream);
 
 /* Its vector-Jacobian product, for the cotangent dloss [N]:
- *   dlogits = dloss T (p - sum_j q_j e[ids_j])  (may be logits)
+ *   dlogits = dloss T (p - sum_j q_j e[ids_j])  (may be logits, rows as far
+ *             apart)
  *   dteacher_j = dloss T q_j (l_j - sum_i q_i l_i), fp32 [N][K], or NULL     */
 int diffopt_distill_bwd(const float* dloss, const void* logits,
                         int64_t row_stride, int64_t N, int64_t V,

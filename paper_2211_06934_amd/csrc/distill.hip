@@ -654,6 +654,23 @@ int check_out_rows(const char* who, const void* out, int64_t stride, int64_t V, 
   return DIFFOPT_OK;
 }
 
+// fp32 arrays of a call: a result of a row is written while other waves, or the
+// row's other workgroups, still read its operands.
+struct Floats {
+  const float* p;
+  int64_t n;
+};
+
+int check_apart(const char* who, std::initializer_list<Floats> results, std::initializer_list<Floats> operands) {
+  for (auto r = results.begin(); r != results.end(); ++r) {
+    for (const Floats& o : operands)
+      if (overlap(r->p, r->n * 4, o.p, o.n * 4)) return fail(DIFFOPT_EINVAL, "%s: a result must not be an operand", who);
+    for (auto t = results.begin(); t != r; ++t)
+      if (overlap(r->p, r->n * 4, t->p, t->n * 4)) return fail(DIFFOPT_EINVAL, "%s: two results must not be one array", who);
+  }
+  return DIFFOPT_OK;
+}
+
 // Workgroups of a row: with fewer rows than kFewRows long ones are cut into slices
 // of at least kSliceBytes until kFillRows workgroups run.  fp32, the loss alone, cut
 // and whole: 8 rows of 512 KiB 8.4 and 15.4 us, 200 of them 23.6 and 28.7, 512 of
@@ -790,6 +807,7 @@ extern "C" int diffopt_distill_fwd(const void* logits, int64_t row_stride, int64
   rc = check_aligned(who, {loss, stats});
   if (rc) return rc;
   rc = check_workspace(who, r, dtype, workspace, workspace_bytes);
+  if (!rc) rc = check_apart(who, {{loss, N}, {stats, 2 * N}}, {{teacher, N * K}});
   if (rc) return rc;
   float* parts = static_cast<float*>(workspace);
   return dtype == DIFFOPT_F32 ? fwd_rows<float>(who, r, dtype, loss, stats, parts, as_stream(stream))
@@ -808,6 +826,9 @@ extern "C" int diffopt_distill_bwd(const float* dloss, const void* logits, int64
   if (!dloss || !stats) return fail(DIFFOPT_EINVAL, "%s: null required pointer", who);
   rc = check_aligned(who, {dloss, stats, dteacher});
   if (!rc) rc = check_out_rows(who, dlogits, drow_stride, V, N, dtype);
+  if (!rc && dlogits == logits && N > 1 && drow_stride != row_stride)
+    rc = fail(DIFFOPT_EINVAL, "%s: dlogits in the logits' place must have their row stride", who);
+  if (!rc) rc = check_apart(who, {{dteacher, N * K}}, {{dloss, N}, {teacher, N * K}, {stats, 2 * N}});
   if (rc) return rc;
   return dtype == DIFFOPT_F32 ? bwd_rows<float>(who, r, dtype, dloss, stats, dlogits, drow_stride, dteacher, as_stream(stream))
                               : bwd_rows<bf16>(who, r, dtype, dloss, stats, dlogits, drow_stride, dteacher, as_stream(stream));
@@ -829,6 +850,7 @@ extern "C" int diffopt_distill_fwd_bwd(const float* dloss, const void* logits, i
   if (rc) return rc;
   if (dlogits == logits) return fail(DIFFOPT_EINVAL, "%s: dlogits must not be logits", who);
   rc = check_workspace(who, r, dtype, workspace, workspace_bytes);
+  if (!rc) rc = check_apart(who, {{loss, N}, {stats, 2 * N}, {dteacher, N * K}}, {{dloss, N}, {teacher, N * K}});
   if (rc) return rc;
   float* parts = static_cast<float*>(workspace);
   return dtype == DIFFOPT_F32
@@ -856,6 +878,8 @@ extern "C" int diffopt_distill_bwd_bwd(const void* ddlogits, int64_t ddrow_strid
   if (out_logits == logits || out_logits == ddlogits)
     return fail(DIFFOPT_EINVAL, "%s: out_logits must be neither logits nor ddlogits", who);
   rc = check_workspace(who, r, dtype, workspace, workspace_bytes);
+  if (!rc)
+    rc = check_apart(who, {{out_dloss, N}, {out_teacher, N * K}}, {{ddteacher, N * K}, {dloss, N}, {teacher, N * K}, {stats, 2 * N}});
   if (rc) return rc;
   const Second t{ddlogits, ddrow_stride, ddteacher, dloss, stats, out_dloss, out_teacher, out_logits, out_row_stride};
   float* parts = static_cast<float*>(workspace);

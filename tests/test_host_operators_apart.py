@@ -58,3 +58,33 @@ def test_linattn_step_out_is_no_operand(operand):
     lib, _, _ = _binding()
     rc = lib.diffopt_linattn_step(_h(0x10000), _h(0x20000), _h(0x30000), _p(64), 2, 4, 2, 8, 8, F32, 1.0, _p(0x80000), _h(operand), None)
     _refused(rc, "must not be an operand")
+
+
+def _distill(name, **change):
+    lib, _, _ = _binding()
+    a = dict(logits=0x100000, stride=64, ids=0x200000, teacher=0x210000, dloss=0x220000, loss=0x230000, stats=0x240000, dlogits=0x300000, dstride=64,
+             dteacher=0x250000, ddlogits=0x400000, ddteacher=0x260000, out_dloss=0x270000, out_logits=0x500000, out_teacher=0x280000)
+    a.update(change)
+    p = {k: v if k in ("stride", "dstride") else _p(v) for k, v in a.items()}
+    rows = (p["logits"], p["stride"], 3, 50, F32, p["ids"], 4, p["teacher"], 5, 1.0)
+    if name == "fwd":
+        return lib.diffopt_distill_fwd(*rows, p["loss"], p["stats"], None, 0, None)
+    if name == "bwd":
+        return lib.diffopt_distill_bwd(p["dloss"], *rows, p["stats"], p["dlogits"], p["dstride"], p["dteacher"], None)
+    if name == "fwd_bwd":
+        return lib.diffopt_distill_fwd_bwd(p["dloss"], *rows, p["loss"], p["stats"], p["dlogits"], p["dstride"], p["dteacher"], None, 0, None)
+    return lib.diffopt_distill_bwd_bwd(p["ddlogits"], 64, p["ddteacher"], p["dloss"], *rows, p["stats"], p["out_dloss"], p["out_logits"], 64,
+                                       p["out_teacher"], None, 0, None)
+
+
+@pytest.mark.parametrize("name,change,word", [
+    ("bwd", dict(dlogits=0x100000, dstride=128), "row stride"), ("bwd", dict(dlogits=0x100000, stride=50), "row stride"),
+    ("fwd", dict(loss=0x210000), "an operand"), ("fwd", dict(stats=0x210000 + 4 * 14), "an operand"), ("fwd", dict(loss=0x240000 + 20), "two results"),
+    ("bwd", dict(dteacher=0x210000), "an operand"), ("bwd", dict(dteacher=0x220008), "an operand"), ("bwd", dict(dteacher=0x240000), "an operand"),
+    ("fwd_bwd", dict(loss=0x220000), "an operand"), ("fwd_bwd", dict(dteacher=0x210000), "an operand"),
+    ("fwd_bwd", dict(stats=0x230000), "two results"), ("fwd_bwd", dict(dteacher=0x230004), "two results"),
+    ("bwd_bwd", dict(out_dloss=0x220000), "an operand"), ("bwd_bwd", dict(out_teacher=0x260000), "an operand"),
+    ("bwd_bwd", dict(out_teacher=0x210000), "an operand"), ("bwd_bwd", dict(out_dloss=0x280000), "two results"),
+])
+def test_distill_results_are_apart(name, change, word):
+    _refused(_distill(name, **change), word)
