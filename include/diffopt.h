@@ -603,7 +603,8 @@ int diffopt_linattn_step(const diffopt_heads* q, const diffopt_heads* k,
  *              first + t without positions.  A position outside [0, rows)
  *              gives that token NaN.
  *   1 <= D <= 1024; rot even, 0 <= rot <= D; eps >= 0
- * q_out may be q and k_out k.                                              */
+ * q_out may be q and k_out k (of the same strides); else results lie apart
+ * from the operands and from one another, here and in the backwards.        */
 int diffopt_qknorm_rope_fwd(const diffopt_heads* q, const diffopt_heads* k,
                             const float* q_weight, const float* k_weight,
                             const float* cos, const float* sin, int64_t rows,

@@ -12,6 +12,7 @@
 // Widths that fall into pairs of 16-byte pieces take qknorm_pieces, others
 // qknorm_any, a wave per head with single elements.
 #include <algorithm>
+#include <initializer_list>
 
 #include "lm_common.hpp"
 
@@ -599,6 +600,32 @@ int check_both(const char* who, const char* what, const diffopt_heads* q, const 
   return rc;
 }
 
+// A head's results may take the place of its operands, which the same lanes have read
+// by then: the same tensor of the same side.  Anything else at one address (q's results
+// over k's operands, rows another distance apart, two results) would be written while
+// other waves read it.
+int check_apart(const char* who, const QkShape& s, std::initializer_list<const HeadArr*> results, std::initializer_list<const HeadArr*> operands,
+                float* const dw[2]) {
+  const int64_t heads[2] = {s.H, s.Hk};
+  auto same = [&](const HeadArr& a, const HeadArr& b, int side) {
+    return (s.B <= 1 || a.sb == b.sb) && (s.T <= 1 || a.st == b.st) && (heads[side] <= 1 || a.sh == b.sh);
+  };
+  for (auto r = results.begin(); r != results.end(); ++r)
+    for (int i = 0; i < 2; ++i) {
+      const HeadArr& x = (*r)[i];
+      if (!x.p) continue;
+      for (const HeadArr* o : operands)
+        for (int j = 0; j < 2; ++j)
+          if (x.p == o[j].p && !(i == j && same(x, o[j], i)))
+            return fail(DIFFOPT_EINVAL, "%s: a result must not be an operand of other heads or strides", who);
+      for (auto t = results.begin(); t <= r; ++t)
+        for (int j = 0; j < (t == r ? i : 2); ++j)
+          if (x.p == (*t)[j].p) return fail(DIFFOPT_EINVAL, "%s: two results must not be one tensor", who);
+    }
+  if (overlap(dw[0], s.D * 4, dw[1], s.D * 4)) return fail(DIFFOPT_EINVAL, "%s: two results must not be one tensor", who);
+  return DIFFOPT_OK;
+}
+
 int check_floats(const char* who, const float* const* p, int n) {
   for (int i = 0; i < n; ++i)
     if (!aligned_to(p[i], 4)) return fail(DIFFOPT_EINVAL, "%s: pointer %p is not 4-byte aligned", who, (const void*)p[i]);
@@ -631,6 +658,7 @@ extern "C" int diffopt_qknorm_rope_fwd(const diffopt_heads* q, const diffopt_hea
   if (!rc) rc = check_both(who, "q_out or k_out", q_out, k_out, s, dtype, A.o0);
   const float* f[] = {q_weight, k_weight};
   if (!rc) rc = check_floats(who, f, 2);
+  if (!rc) rc = check_apart(who, s, {A.o0}, {A.x}, A.dw);
   if (rc) return rc;
   A.w[0] = q_weight;
   A.w[1] = k_weight;
@@ -660,6 +688,7 @@ extern "C" int diffopt_qknorm_rope_bwd(const diffopt_heads* dq_out, const diffop
   const float* f[] = {q_weight, k_weight, dq_weight, dk_weight};
   if (!rc) rc = check_floats(who, f, 4);
   if (!rc) rc = check_workspace(who, s, &A, workspace, workspace_bytes);
+  if (!rc) rc = check_apart(who, s, {A.o0}, {A.x, A.dy}, A.dw);
   if (rc) return rc;
   A.w[0] = q_weight;
   A.w[1] = k_weight;
@@ -693,6 +722,7 @@ extern "C" int diffopt_qknorm_rope_bwd_bwd(
   const float* f[] = {q_weight, k_weight, ddq_weight, ddk_weight, out_q_weight, out_k_weight};
   if (!rc) rc = check_floats(who, f, 6);
   if (!rc) rc = check_workspace(who, s, &A, workspace, workspace_bytes);
+  if (!rc) rc = check_apart(who, s, {A.o0, A.o1}, {A.x, A.dy, A.a}, A.dw);
   if (rc) return rc;
   A.w[0] = q_weight;
   A.w[1] = k_weight;

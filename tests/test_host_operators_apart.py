@@ -88,3 +88,37 @@ def _distill(name, **change):
 ])
 def test_distill_results_are_apart(name, change, word):
     _refused(_distill(name, **change), word)
+
+
+def _qknorm(name, **change):
+    lib, _, Heads = _binding()
+    # q [2, 9, 4, 16], k [2, 9, 2, 16], every operand and result in a place of its own
+    names = ("q", "k", "q_out", "k_out", "dq_out", "dk_out", "dq", "dk", "ddq", "ddk", "out_dq_out", "out_dk_out", "out_q", "out_k")
+    a = {n: Heads((i + 1) << 16, 9 * 16 * (2 if "k" in n else 4), 16 * (2 if "k" in n else 4), 16) for i, n in enumerate(names)}
+    a["dwq"], a["dwk"] = 0x800000, 0x810000
+    for n, v in change.items():
+        a[n] = v if isinstance(v, int) else a[v] if isinstance(v, str) else Heads(*v)
+    h = lambda n: ctypes.byref(a[n])  # noqa: E731
+    shape = (None, None, _p(64), _p(64), 32, None, 0, 0, 2, 9, 4, 2, 16, 8, 0, F32, 1e-6)
+    ws = (_p(0x900000), lib.diffopt_qknorm_rope_workspace(2, 9, 4, 2, 16), None)
+    if name == "fwd":
+        return lib.diffopt_qknorm_rope_fwd(h("q"), h("k"), *shape, h("q_out"), h("k_out"), None)
+    if name == "bwd":
+        return lib.diffopt_qknorm_rope_bwd(h("dq_out"), h("dk_out"), h("q"), h("k"), *shape, h("dq"), h("dk"), _p(a["dwq"]), _p(a["dwk"]), *ws)
+    return lib.diffopt_qknorm_rope_bwd_bwd(h("ddq"), h("ddk"), None, None, h("dq_out"), h("dk_out"), h("q"), h("k"), *shape, h("out_dq_out"),
+                                           h("out_dk_out"), h("out_q"), h("out_k"), _p(a["dwq"]), _p(a["dwk"]), *ws)
+
+
+Q = 1 << 16  # q's address; its strides are 576, 64, 16
+
+
+@pytest.mark.parametrize("name,change,word", [
+    ("fwd", dict(q_out=(Q, 576, 16, 144)), "an operand"), ("fwd", dict(q_out=(Q, 1152, 64, 16)), "an operand"), ("fwd", dict(q_out="k"), "an operand"),
+    ("fwd", dict(k_out="q"), "an operand"), ("fwd", dict(k_out="q_out"), "two results"),
+    ("bwd", dict(dq="dk_out"), "an operand"), ("bwd", dict(dk="q"), "an operand"), ("bwd", dict(dk="dq"), "two results"),
+    ("bwd", dict(dwk=0x800000 + 60), "two results"),
+    ("bwd_bwd", dict(out_q="ddk"), "an operand"), ("bwd_bwd", dict(out_dk_out="q"), "an operand"), ("bwd_bwd", dict(out_q="out_dq_out"), "two results"),
+    ("bwd_bwd", dict(out_k="out_dq_out"), "two results"),
+])
+def test_qknorm_rope_results_are_apart(name, change, word):
+    _refused(_qknorm(name, **change), word)
