@@ -42,92 +42,71 @@ __device__ __forceinline__ E* at(const HeadArr& h, int64_t b, int64_t t, int64_t
   return static_cast<E*>(h.p) + b * h.sb + t * h.st + head * h.sh;
 }
 
-// Single tokens of any width and alignment (the others: linattn_one).  A workgroup
-// holds 64 columns of one state, a lane R rows by 4 columns of them, read and
-// written element by element.  Bound by the state's memory: 256 sequences of 16
-// heads of 128 take 241 us (2.2 TB/s), which linattn_one moves in 101.  Sequences
-// take chunks from two tokens on: token by token one of 2 tokens and 16 heads takes
-// 14 us against 10, 32 of 4 tokens 48 against 20.
-constexpr int kTokenB = 256, kTokenCols = 64;
+// One token of any width and alignment (the others: linattn_one).  A workgroup holds
+// 64 columns of one state, a lane R rows by 4 columns of them, read and written
+// element by element.  Bound by the state's memory, in pieces of 4 bytes: 256 sequences
+// of 16 heads of 128 whose states lie 4 bytes off a piece take 282 us in bf16 and 247 in
+// fp32 (1.9 and 2.2 TB/s), where linattn_one takes 120 for aligned ones.
+constexpr int kAnyB = 256, kAnyCols = 64;
 
 template <class E, int R>
-__global__ __launch_bounds__(kTokenB) void linattn_tokens(Shape s, Scan a, int32_t col_tiles) {
+__global__ __launch_bounds__(kAnyB) void linattn_one_any(Shape s, Scan a, int32_t col_tiles) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int rg = lane >> 2;
-  const int64_t state = blockIdx.x / col_tiles, b = state / s.Hs;
+  const int64_t state = blockIdx.x / (uint32_t)col_tiles, b = state / s.Hs;
   const int j = (int)(state - b * s.Hs);
-  const int c0 = (int)(blockIdx.x % col_tiles) * kTokenCols + wave * 16 + (lane & 3) * 4;
+  const int c0 = (int)(blockIdx.x % (uint32_t)col_tiles) * kAnyCols + wave * 16 + (lane & 3) * 4;
   // the decay to 48 bits: one rounding of it would grow with every token
   const double gd = exp((double)s.log_decay[j]);
   const float g = (float)gd, g_lo = (float)(gd - (double)g);
-  const int64_t L = length_of(s, b), block = state * a.Dk * a.Dv;
-  float S[R][4];
+  const int64_t block = state * a.Dk * a.Dv;
+  float S[R][4], vv[4];
+  // all loads before the first store: they may be the same memory
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const int r = rg + 16 * i;
-      S[i][c] = a.s0 && r < a.Dk && c0 + c < a.Dv ? a.s0[block + (a.flip ? (c0 + c) * a.Dk + r : r * a.Dv + c0 + c)] : 0.0f;
+      S[i][c] = r < a.Dk && c0 + c < a.Dv ? a.s0[block + r * a.Dv + c0 + c] : 0.0f;
     }
-  for (int64_t n = 0; n < L; ++n) {
-    const int64_t t = a.back ? L - 1 - n : n;
-    if (!a.back || n > 0)
+  const E *k = at<E>(a.k, b, 0, j), *v = at<E>(a.v, b, 0, j);
 #pragma unroll
-      for (int i = 0; i < R; ++i)
+  for (int c = 0; c < 4; ++c) vv[c] = c0 + c < a.Dv ? (float)v[c0 + c] : 0.0f;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) S[i][c] = fmaf(S[i][c], g, S[i][c] * g_lo);
-    for (int h = 0; h < a.nk; ++h) {
-      const E *k = at<E>(a.k, b, t, j * a.nk + h), *v = at<E>(a.v, b, t, j * a.nk + h);
-      float vv[4];
+  for (int i = 0; i < R; ++i) {
+    const int r = rg + 16 * i;
+    const float kk = r < a.Dk ? (float)k[r] : 0.0f;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) vv[c] = c0 + c < a.Dv ? (float)v[c0 + c] * a.ks : 0.0f;
+    for (int c = 0; c < 4; ++c) S[i][c] = fmaf(kk, vv[c], fmaf(S[i][c], g, S[i][c] * g_lo));
+  }
+  for (int h = 0; h < a.nq; ++h) {
+    const E* q = at<E>(a.q, b, 0, (int64_t)j * a.nq + h);
+    float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        const int r = rg + 16 * i;
-        const float kk = r < a.Dk ? (float)k[r] : 0.0f;
+    for (int i = 0; i < R; ++i) {
+      const int r = rg + 16 * i;
+      const float qq = r < a.Dk ? (float)q[r] : 0.0f;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) S[i][c] = fmaf(kk, vv[c], S[i][c]);
-      }
+      for (int c = 0; c < 4; ++c) o[c] = fmaf(qq, S[i][c], o[c]);
     }
-    if (!a.o.p) continue;
-    for (int h = 0; h < a.nq; ++h) {
-      const E* q = at<E>(a.q, b, t, j * a.nq + h);
-      float o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        const int r = rg + 16 * i;
-        const float qq = r < a.Dk ? (float)q[r] : 0.0f;
+    for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) o[c] = fmaf(qq, S[i][c], o[c]);
-      }
+      for (int m = 4; m < 64; m <<= 1) o[c] += __shfl_xor(o[c], m, 64);
+    if (rg == 0) {
+      E* out = at<E>(a.o, b, 0, (int64_t)j * a.nq + h);
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int m = 4; m < 64; m <<= 1) o[c] += __shfl_xor(o[c], m, 64);
-      if (rg == 0) {
-        E* out = at<E>(a.o, b, t, j * a.nq + h);
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (c0 + c < a.Dv) out[c0 + c] = (E)(o[c] * a.qs);
-      }
+        if (c0 + c < a.Dv) out[c0 + c] = (E)(o[c] * a.qs);
     }
   }
-  if (a.o.p && rg == 0)
-    for (int64_t t = L; t < s.T; ++t)
-      for (int h = 0; h < a.nq; ++h)
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (c0 + c < a.Dv) at<E>(a.o, b, t, j * a.nq + h)[c0 + c] = (E)0.0f;
-  if (a.s1) {
-    const float last = a.back && L > 0 ? g : 1.0f;
+  for (int i = 0; i < R; ++i)
 #pragma unroll
-    for (int i = 0; i < R; ++i)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int r = rg + 16 * i;
-        if (r < a.Dk && c0 + c < a.Dv) a.s1[block + r * a.Dv + c0 + c] = S[i][c] * last;
-      }
-  }
+    for (int c = 0; c < 4; ++c) {
+      const int r = rg + 16 * i;
+      if (r < a.Dk && c0 + c < a.Dv) a.s1[block + r * a.Dv + c0 + c] = S[i][c];
+    }
 }
 
 // One token: the state is read and written once, which is nearly all there is
@@ -1037,15 +1016,15 @@ constexpr int kMaxWidth = 256;
 constexpr int kUnit = 64;  // tokens in whole chunks of every kernel
 
 template <class E>
-void launch_tokens(const Shape& s, const Scan& a, hipStream_t st) {
-  const int tiles = (a.Dv + kTokenCols - 1) / kTokenCols;
-  const dim3 grid((unsigned)(s.B * s.Hs * tiles)), block(kTokenB);
+void launch_any(const Shape& s, const Scan& a, hipStream_t st) {
+  const int tiles = (a.Dv + kAnyCols - 1) / kAnyCols;
+  const dim3 grid((unsigned)(s.B * s.Hs * tiles)), block(kAnyB);
   if (a.Dk <= 64)
-    hipLaunchKernelGGL((linattn_tokens<E, 4>), grid, block, 0, st, s, a, tiles);
+    hipLaunchKernelGGL((linattn_one_any<E, 4>), grid, block, 0, st, s, a, tiles);
   else if (a.Dk <= 128)
-    hipLaunchKernelGGL((linattn_tokens<E, 8>), grid, block, 0, st, s, a, tiles);
+    hipLaunchKernelGGL((linattn_one_any<E, 8>), grid, block, 0, st, s, a, tiles);
   else
-    hipLaunchKernelGGL((linattn_tokens<E, 16>), grid, block, 0, st, s, a, tiles);
+    hipLaunchKernelGGL((linattn_one_any<E, 16>), grid, block, 0, st, s, a, tiles);
 }
 
 template <class E>
@@ -1429,8 +1408,8 @@ extern "C" int diffopt_linattn_step(const diffopt_heads* q, const diffopt_heads*
   hipStream_t st = as_stream(stream);
   const bool pieces = Dv % 4 == 0 && aligned_to(state, 16);  // rows of whole 16-byte pieces
   if (dtype == DIFFOPT_F32)
-    pieces ? launch_one<float>(s, a[0], st) : launch_tokens<float>(s, a[0], st);
+    pieces ? launch_one<float>(s, a[0], st) : launch_any<float>(s, a[0], st);
   else
-    pieces ? launch_one<bf16>(s, a[0], st) : launch_tokens<bf16>(s, a[0], st);
+    pieces ? launch_one<bf16>(s, a[0], st) : launch_any<bf16>(s, a[0], st);
   return launch_status(who);
 }
