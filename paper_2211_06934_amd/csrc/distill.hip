@@ -630,9 +630,9 @@ int check_rows(const char* who, const void* logits, int64_t row_stride, int64_t 
   if (!dtype_ok(dtype)) return fail(DIFFOPT_EINVAL, "%s: unknown element type %d", who, (int)dtype);
   if (id_bytes != 4 && id_bytes != 8) return fail(DIFFOPT_EINVAL, "%s: id_bytes must be 4 or 8", who);
   if (K < 1 || K > kMaxK) return fail(DIFFOPT_EINVAL, "%s: K must be in [1, %d]", who, kMaxK);
-  if (!(std::isfinite(temperature) && temperature > 0.0 && std::isfinite((float)(1.0 / temperature)) && (float)temperature > 0.0f &&
+  if (!(std::isfinite(temperature) && temperature > 0.0 && std::isfinite((float)(1.0 / temperature) * kLog2e) && (float)temperature > 0.0f &&
         std::isfinite((float)temperature)))
-    return fail(DIFFOPT_EINVAL, "%s: temperature must be finite and > 0", who);
+    return fail(DIFFOPT_EINVAL, "%s: temperature and log2(e) / temperature must be finite and > 0 in fp32", who);
   if (N == 0) return DIFFOPT_OK;
   if (!logits || !ids || !teacher) return fail(DIFFOPT_EINVAL, "%s: null required pointer", who);
   if (!aligned_to(logits, elem_size(dtype)) || !aligned_to(ids, id_bytes) || !aligned_to(teacher, 4))
