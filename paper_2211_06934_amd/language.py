@@ -141,6 +141,7 @@ def linear_attention(q, k, v, log_decay, state=None, lengths=None, scale: float 
     number of times."""
     if isinstance(log_decay, torch.Tensor) and log_decay.requires_grad:
         raise ValueError("linear_attention: log_decay has no gradient: pass a tensor that does not require one")
+    _o._dims(q, k, v, 4)
     out, s1 = LinearAttentionFn.apply(_dense(q), _dense(k), _dense(v), _whole(state), log_decay, lengths, float(scale), bool(return_state))
     return (out, s1) if return_state else out
 
@@ -153,6 +154,7 @@ def linear_attention_step(q, k, v, log_decay, state, scale: float = 1.0) -> torc
             if isinstance(x, torch.Tensor) and x.requires_grad:
                 raise ValueError("linear_attention_step: %s asks for a gradient, and single tokens have none: detach it, or step "
                                  "under torch.no_grad()" % what)
+    _o._dims(q, k, v, 3)
     with torch.no_grad():
         q, k, v = _dense(q), _dense(k), _dense(v)
         out = torch.empty(*q.shape[:2], v.shape[2], dtype=q.dtype, device=q.device)

@@ -8,3 +8,20 @@ from test_host_operators import _distill, _refused
 def test_temperatures_whose_inverse_overflows_are_refused(T):
     # 1 / T is finite in fp32 from 2.94e-39 on, log2(e) / T, by which the kernels scale, only from 4.24e-39 on
     _refused(_distill(T=T), "temperature")
+
+
+@pytest.mark.parametrize("call", ["linear_attention", "linear_attention_step"])
+@pytest.mark.parametrize("name", ["q", "k", "v"])
+@pytest.mark.parametrize("bad", [(8,), (2, 8), ()])
+def test_operands_of_other_axes_are_named(call, name, bad):
+    import torch
+
+    import paper_2211_06934_amd as P
+    shape = (1, 3, 2, 8) if call == "linear_attention" else (1, 2, 8)
+    a = {n: torch.zeros(bad if n == name else shape) for n in ("q", "k", "v")}
+    extra = {} if call == "linear_attention" else dict(state=torch.zeros(1, 2, 8, 8))
+    with pytest.raises(ValueError, match="%s: expected a tensor of %d axes" % (name, len(shape))):
+        getattr(P, call)(a["q"], a["k"], a["v"], torch.zeros(2), **extra)
+    a[name] = None
+    with pytest.raises(ValueError, match="%s: expected a tensor" % name):
+        getattr(P, call)(a["q"], a["k"], a["v"], torch.zeros(2), **extra)
