@@ -384,7 +384,7 @@ struct Scratch {
     if (need < 0) throw Other{};
     if (given != Py_None) {
       const at::Tensor& t = tensor_of(given);
-      if (t.scalar_type() != at::kByte || !t.is_cuda() || !t.is_contiguous() || t.numel() < need) throw Other{};
+      if (t.scalar_type() != at::kByte || t.device() != like.device() || !t.is_contiguous() || t.numel() < need) throw Other{};
       p = t.data_ptr();
       bytes = t.numel();
     } else if (need > 0) {

@@ -134,6 +134,8 @@ def _scratch(given, need: int, device, stream):
         pass
     elif not isinstance(given, torch.Tensor) or given.dtype != torch.uint8 or not given.is_cuda or not given.is_contiguous():
         raise ValueError("workspace: expected a contiguous uint8 tensor in device memory")
+    elif given.device != device:
+        raise ValueError("workspace: expected a tensor on %s, got %s" % (device, given.device))
     elif given.numel() < need:
         raise ValueError("workspace: expected at least %d bytes, got %d" % (need, given.numel()))
     return given, (None if given is None else given.data_ptr() or None), 0 if given is None else given.numel()

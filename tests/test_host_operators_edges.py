@@ -25,3 +25,24 @@ def test_operands_of_other_axes_are_named(call, name, bad):
     a[name] = None
     with pytest.raises(ValueError, match="%s: expected a tensor" % name):
         getattr(P, call)(a["q"], a["k"], a["v"], torch.zeros(2), **extra)
+
+
+def test_workspaces_on_another_device_are_refused():
+    import torch
+
+    import paper_2211_06934_amd as P
+
+    class On(torch.Tensor):  # bytes that say which device they are on, without one
+        @staticmethod
+        def __new__(cls, n, device):
+            return torch.Tensor._make_wrapper_subclass(cls, (n,), dtype=torch.uint8, device=device)
+
+        def data_ptr(self):
+            return 64
+
+        __torch_dispatch__ = None
+
+    one, two = torch.device("cuda", 0), torch.device("cuda", 1)
+    assert P.operators._scratch(On(256, one), 256, one, None)[1:] == (64, 256)
+    with pytest.raises(ValueError, match="cuda:1"):
+        P.operators._scratch(On(256, two), 256, one, None)
