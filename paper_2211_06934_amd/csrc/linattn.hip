@@ -130,12 +130,12 @@ __global__ __launch_bounds__(kStepB) void linattn_one(Shape s, Scan a, int32_t c
   const int64_t b = state / s.Hs;
   const int j = (int)(state - b * s.Hs), c0 = ((int)(blockIdx.x % (uint32_t)col_tiles) * kStepCG + cg) * 4;
   const bool in = c0 < a.Dv;
-  const float* s0 = a.s0 + state * a.Dk * a.Dv + (in ? c0 : 0);
+  const float* s0 = a.s0 + state * a.Dk * a.Dv + c0;
   f32x4 S[R];
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int r = rg + i * RG;
-    S[i] = r < a.Dk ? *reinterpret_cast<const f32x4*>(s0 + r * a.Dv) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    S[i] = in && r < a.Dk ? *reinterpret_cast<const f32x4*>(s0 + r * a.Dv) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
   const E *k = at<E>(a.k, b, 0, j), *v = at<E>(a.v, b, 0, j);
   float kk[R];
