@@ -206,10 +206,15 @@ __global__ __launch_bounds__(kStepB) void linattn_one(Shape s, Scan a, int32_t c
 // (ds_read_b64_tr_b16).  The products are computed transposed, so that a lane
 // holds 4 neighbouring elements of one token's output.
 //
-// In bf16 the scores and the state are rounded where they enter a product (the
-// outputs are bf16 too); the state itself is fp32 and its update takes W_k V in
-// SPLIT bf16 parts, exact to 2^-8 SPLIT: two where only outputs follow, three
-// where a state is handed out.  fp32 runs on the fp32 matrix instructions.
+// In bf16 three operands of the products are not of the type.  The state is fp32 and
+// meets the queries in two bf16 parts, exact to 2^-16.  Its update takes W_k V in SPLIT
+// parts, exact to 2^-8 SPLIT: two where only outputs follow, three where a state is
+// handed out (three everywhere: training 374 us instead of 337, for a part that the
+// outputs' own rounding hides).  The scores are rounded to bf16, the one operand of 8
+// bits: with them results lie 1.75e-3 from 64-bit ones, with scores in two parts 1.66e-3
+// (what the rounding of the outputs alone makes) but training takes 484 us instead of
+// 362 and a prompt 159 instead of 131; with the state in one part 2.35e-3 (331 and
+// 125).  fp32 runs on the fp32 matrix instructions.
 //
 // What bounds it is the walk: a chunk's products need one another (scores, barrier,
 // outputs, state), and a compute unit holds two workgroups of 128 columns (72 KiB of
@@ -483,6 +488,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   typedef typename Frag<E>::type frag;
   typedef Tile<E, DK> KTile;
   typedef Tile<E, CT> VTile;
+  constexpr int PARTS = sizeof(E) == 2 ? 2 : 1;  // of the state in a product with the queries
   constexpr int AHEAD = DK <= 128 ? 1 : 0;  // LDS is read a step ahead; a state of 256 rows leaves no registers for it
   __shared__ __attribute__((aligned(16))) Lds lds;
 
@@ -761,9 +767,12 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
         }
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
-          frag s[NCT];
+          frag s[PARTS][NCT];
 #pragma unroll
-          for (int ct = 0; ct < NCT; ++ct) s[ct] = pack(S[kb][0][ct], S[kb][1][ct], E());
+          for (int ct = 0; ct < NCT; ++ct) {
+            s[0][ct] = pack(S[kb][0][ct], S[kb][1][ct], E());
+            if constexpr (PARTS == 2) s[1][ct] = __builtin_convertvector(pack(S[kb][0][ct], S[kb][1][ct], float()) - widened(s[0][ct]), frag);
+          }
           if (kb + AHEAD < KB) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) q[(kb + AHEAD) & 1][t] = KTile::row(sQ, at_q, 16 * t, kb + AHEAD);
@@ -772,7 +781,10 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(s[ct], q[kb & 1][t], kb ? O[t][ct] : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+            for (int ct = 0; ct < NCT; ++ct) {
+              O[t][ct] = mfma32(s[0][ct], q[kb & 1][t], kb ? O[t][ct] : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+              if constexpr (PARTS == 2) O[t][ct] = mfma32(s[1][ct], q[kb & 1][t], O[t][ct]);
+            }
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t)
