@@ -206,15 +206,15 @@ __global__ __launch_bounds__(kStepB) void linattn_one(Shape s, Scan a, int32_t c
 // (ds_read_b64_tr_b16).  The products are computed transposed, so that a lane
 // holds 4 neighbouring elements of one token's output.
 //
-// In bf16 three operands of the products are not of the type.  The state is fp32 and
-// meets the queries in two bf16 parts, exact to 2^-16.  Its update takes W_k V in SPLIT
-// parts, exact to 2^-8 SPLIT: two where only outputs follow, three where a state is
-// handed out (three everywhere: training 374 us instead of 337, for a part that the
-// outputs' own rounding hides).  The scores are rounded to bf16, the one operand of 8
-// bits: with them results lie 1.75e-3 from 64-bit ones, with scores in two parts 1.66e-3
-// (what the rounding of the outputs alone makes) but training takes 484 us instead of
-// 362 and a prompt 159 instead of 131; with the state in one part 2.35e-3 (331 and
-// 125).  fp32 runs on the fp32 matrix instructions.
+// In bf16 three operands of the products are not of the type, and are taken in parts
+// of bf16, each the rounding of what the ones before leave out.  The scores and the
+// fp32 state meet the values and the queries in two, exact to 2^-16; the state's update
+// takes W_k V in SPLIT, exact to 2^-8 SPLIT: two where only outputs follow, three where
+// a state is handed out (three everywhere: training 374 us instead of 337, for a part
+// that the outputs' own rounding hides).  So results lie 1.66e-3 from 64-bit ones, which
+// is the rounding of the outputs alone.  With one part of the scores they lie at 1.75e-3
+// and training takes 362 us instead of 373, a prompt 132 instead of 133; with one of the
+// state too 2.35e-3, 331 and 121.  fp32 runs on the fp32 matrix instructions.
 //
 // What bounds it is the walk: a chunk's products need one another (scores, barrier,
 // outputs, state), and a compute unit holds two workgroups of 128 columns (72 KiB of
@@ -476,7 +476,11 @@ struct ChunkLds {
   static constexpr int all = (OUT ? 3 : 2) * kq + (OUT ? 1 : 2) * kv;
   static constexpr bool over = OUT && DK >= CT;
   E in[all];
-  typename Frag<E>::type P[OUT ? NT * NB * 64 : 1];
+  static constexpr int PARTS = sizeof(E) == 2 ? 2 : 1;  // of the state and the scores in a product
+  // the scores of 16 queries and 32 keys, as far as the diagonal goes, by parts
+  static constexpr int scores = NT + 2 * (NB - 1);
+  static __device__ __forceinline__ constexpr int score(int t, int nb) { return (t + 2 * nb) * 64; }
+  typename Frag<E>::type P[OUT ? PARTS * scores * 64 : 1];
   E out[OUT && !over ? kv : 1];
 };
 
@@ -488,7 +492,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   typedef typename Frag<E>::type frag;
   typedef Tile<E, DK> KTile;
   typedef Tile<E, CT> VTile;
-  constexpr int PARTS = sizeof(E) == 2 ? 2 : 1;  // of the state in a product with the queries
+  constexpr int PARTS = Lds::PARTS;
   constexpr int AHEAD = DK <= 128 ? 1 : 0;  // LDS is read a step ahead; a state of 256 rows leaves no registers for it
   __shared__ __attribute__((aligned(16))) Lds lds;
 
@@ -725,9 +729,18 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
         for (int e = 0; e < 4; ++e) P[i][e] = gap0 + 16 * apart >= e ? P[i][e] * (apart == 0 ? near[e] : off[e] * far) : 0.0f;
       }
       typedef E four __attribute__((ext_vector_type(4)));
-      if (TILES == 3) sP[tq[0] * NB * 64 + lane] = pack(P[0], P[1], E());
       constexpr int one = TILES - 1;
-      reinterpret_cast<four*>(sP)[((tq[one] * NB + (tk[one] >> 1)) * 64 + lane) * 2 + (tk[one] & 1)] = __builtin_convertvector(P[one], four);
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) {
+        frag* to = sP + p * Lds::scores * 64 + lane;
+        if (TILES == 3) to[Lds::score(tq[0], 0)] = pack(P[0], P[1], E());
+        reinterpret_cast<four*>(to + Lds::score(tq[one], tk[one] >> 1))[tk[one] & 1] = __builtin_convertvector(P[one], four);
+        if (p + 1 < PARTS)
+#pragma unroll
+          for (int i = 0; i < TILES; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) P[i][e] -= (float)(E)P[i][e];
+      }
     }
 
     if (OUT && PIECES && pending) {
@@ -799,7 +812,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int nb = 0; nb <= t / 2; ++nb) p[t][nb] = sP[(t * NB + nb) * 64 + lane];
+          for (int nb = 0; nb <= t / 2; ++nb) p[t][nb] = sP[Lds::score(t, nb) + lane];
       };
       if (AHEAD) read_scores();
       if (more) stage_k(pk, L_next, turn);
@@ -811,6 +824,16 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
           for (int t = 2 * nb; t < NT; ++t)
 #pragma unroll
             for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(V[nb][ct], p[t][nb], O[t][ct]);
+        if constexpr (PARTS == 2) {
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int t = 2 * nb; t < NT; ++t) {
+              const frag low = sP[Lds::scores * 64 + Lds::score(t, nb) + lane];
+#pragma unroll
+              for (int ct = 0; ct < NCT; ++ct) O[t][ct] = mfma32(V[nb][ct], low, O[t][ct]);
+            }
+        }
       } else {
         // a product with the zeros of the mask would carry an infinity or NaN to
         // earlier tokens, so the sum stops at the token
@@ -822,7 +845,12 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
             const int sg = (n >> 2) & 3, e = ((n >> 4) << 2) | (n & 3), late = 32 * nb + n - m;  // from query 16 t + m >= s on
             float p[NT];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) p[t] = late <= 16 * t ? (float)reinterpret_cast<const E*>(&sP[(t * NB + nb) * 64 + sg * 16 + m])[e] : 0.0f;
+            for (int t = 0; t < NT; ++t) {
+              p[t] = 0.0f;
+#pragma unroll
+              for (int part = 0; part < PARTS; ++part)
+                p[t] += late <= 16 * t ? (float)reinterpret_cast<const E*>(&sP[part * Lds::scores * 64 + Lds::score(t, nb) + sg * 16 + m])[e] : 0.0f;
+            }
 #pragma unroll
             for (int ct = 0; ct < NCT; ++ct) {
               float own = 0.0f;
