@@ -507,8 +507,10 @@ int diffopt_es_weights(const float* fvals, const float* f0,
  * linear attention, as calls of its own forward and backward.
  * Element types: DIFFOPT_F32, or DIFFOPT_BF16 for activations; every sum,
  * softmax statistic, norm and state is fp32, each result is rounded once
- * (linear attention over bf16 also rounds its scores, and the state where it
- * meets a query, to bf16: operands of matrix products).
+ * (linear attention over bf16 takes its fp32 scores, states and weighted
+ * values into matrix products in parts of bf16, exact to 2^-16 of each, and to
+ * 2^-24 for the values where a state is handed out: asking for state_out may
+ * move an element of out to a neighbour).
  */
 #define DIFFOPT_F32 0
 #define DIFFOPT_BF16 1
@@ -533,6 +535,9 @@ typedef struct diffopt_heads {
  *   state_out = S_{lengths[b]-1}         (state for a length of 0)
  * (an unrolled inner loop in itself: the update is a decayed gradient step on
  * -<S^T k, v>).  Tokens from lengths[b] on are not read and get out = 0.
+ * Whatever the recurrence holds in fp32 does not overflow.  With infinite or
+ * NaN operands a result is finite exactly where the recurrence's is; which of
+ * the others are infinite and which NaN is not promised.
  *   q [B][T][H][Dk], k [B][T][Hk][Dk], v [B][T][Hk][Dv], out [B][T][H][Dv]
  *   log_decay  DEVICE fp32 [Hk], <= 0 (0: no decay; -inf: the token alone)
  *   lengths    DEVICE int32 [B] in [0, T] (clamped), or NULL for T
