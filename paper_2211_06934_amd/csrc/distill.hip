@@ -309,7 +309,10 @@ __device__ __forceinline__ float same_token(const float* w, const Entries& E, in
 // Waves of a SIMD that the compiler has to leave room for where rows stay in
 // registers: rows of 104 KiB at three workgroups a compute unit (80 registers, 52
 // of them the row's) took 175 us for 4096 rows of 50,021 bf16 logits, at two 186,
-// at four (with spills) 199; elsewhere its own choice is as good.
+// at four (with spills) 199.  Elsewhere its own choice stands: made to leave room for
+// more, rows of 64 KiB (4,096 of 32,001 bf16 logits) take 115 us instead of 118, those of
+// up to 32 KiB the same within 1%, of 125 KiB 71 instead of 62 (1,024 of 32,000 fp32
+// logits) and of 254 KiB 223 instead of 125 (spills).
 constexpr int kept_waves(int B, int NV) { return B == 512 && NV == 13 ? 6 : 1; }
 
 // Where a row's max and sum come from.

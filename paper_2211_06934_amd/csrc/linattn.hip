@@ -217,16 +217,18 @@ __global__ __launch_bounds__(kStepB) void linattn_one(Shape s, Scan a, int32_t c
 // state too 2.35e-3, 331 and 121.  fp32 runs on the fp32 matrix instructions.
 //
 // What bounds it is the walk: a chunk's products need one another (scores, barrier,
-// outputs, state), and a compute unit holds two workgroups of 128 columns (72 KiB of
-// LDS, 256 registers) to fill each other's waits.  Of 5.8 us a chunk of 64 tokens
-// the matrix unit works a third.  bf16, 16 heads of 128:
-//   16,384 tokens: 64 us for the outputs (4.2 TB/s of q, k, v, o and states), 42 for
-//   the segments' states, 16 for their join; the bytes alone would take 43
-//   2 x 8,192 tokens backward: 173 us for dq, dk, dv (805 MB, 4.7 TB/s), 67 states
-// Eight waves of 16 columns on two buffers, one workgroup a compute unit, took 530
-// us for both ways of the latter where two workgroups of four waves took 442; chunks
-// through registers instead of straight to LDS 710.  For dq, dk, dv the operands are
-// read three times: one walk of all three would need three states in registers.
+// outputs, state), and a compute unit holds two workgroups of 128 columns (76 KiB of
+// LDS, 256 registers, 10 of them spilled) to fill each other's waits.  The matrix unit
+// is busy 31% of the outputs' cycles forward and 35% backward, 24 to 35% of the states'
+// (counters).  bf16, 16 heads of 128:
+//   16,384 tokens: 77 us for the outputs (3.9 TB/s of q, k, v, o and states), 43 for
+//   the segments' states, 17 for their join; the bytes alone would take 43
+//   2 x 8,192 tokens backward: 218 us for dq, dk, dv (805 MB, 3.7 TB/s), 74 states
+// Before the operands had parts, eight waves of 16 columns on two buffers, one
+// workgroup a compute unit, took 530 us for both ways of the latter where two
+// workgroups of four waves took 442; chunks through registers instead of straight to
+// LDS 710.  For dq, dk, dv the operands are read three times: one walk of all three
+// would need three states in registers.
 
 template <class E>
 struct Frag;
@@ -1108,13 +1110,13 @@ Class class_of(const Scan& a, int32_t dtype) {
 
 // Segments of a call's scans.  A workgroup walks its chunks one after another,
 // so with few heads a sequence is cut until the workgroups fill the card: two of
-// them share a compute unit, up to four where the state has at most 64 rows
-// (six ragged sequences of up to 1,021 tokens, heads of 64, both ways: 85 us,
-// with half as many 103; heads of 128 with twice as many: no gain).  A cut costs
-// one more read of k and v and the segments' states, so there is none from half of
-// that on, and no segment is shorter than kMinUnits (with 8 the ragged ones take
-// 114 us, with 2 they take 82, and the states of wide heads cost as much as their
-// tokens).
+// them share a compute unit, three or more where the state has at most 64 rows
+// (six ragged sequences of up to 1,021 tokens, heads of 64, both ways: 86 us for
+// four, 86 for three, 105 for two; a prompt of 16,384 tokens with heads of 128: 134 for
+// two, 164 for four).  A cut costs one more read of k and v and the segments' states,
+// so there is none from half of that on, and no segment is shorter than kMinUnits (with
+// 8 the ragged ones take 114 us, with 2 they take 83, and the states of wide heads cost
+// as much as their tokens).
 constexpr int kFill = 512, kFillNarrow = 1024, kMinUnits = 4;
 
 struct Plan {

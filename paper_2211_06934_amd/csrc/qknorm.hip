@@ -449,7 +449,8 @@ struct Plan {
 // fit and take the same 63 us for 16,384 tokens of 40 heads of 128 in bf16, 5.3
 // TB/s); three in the backward (111 us, 4.6 TB/s; four, of which one waits for its
 // turn, 123) and in fp32's second one (18.5 us for 4,072 tokens of 16 heads of 64;
-// four 21.1); two in bf16's.
+// four 21.1); two in bf16's (all three directions of 16,384 tokens of 40 heads of 128:
+// 355 us, three 381; of 4,072 tokens of 16 heads of 64 50 and 59).
 int64_t piece_blocks(int32_t dtype, Dir dir) { return 256 * (dir == kFwd ? 4 : dir == kSecond && dtype == DIFFOPT_BF16 ? 2 : 3); }
 
 // Widths that fall into pairs of pieces, with up to 32 lanes a head, and counts
