@@ -535,7 +535,8 @@ typedef struct diffopt_heads {
  *   state_out = S_{lengths[b]-1}         (state for a length of 0)
  * (an unrolled inner loop in itself: the update is a decayed gradient step on
  * -<S^T k, v>).  Tokens from lengths[b] on are not read and get out = 0.
- * Whatever the recurrence holds in fp32 does not overflow.  With infinite or
+ * States stay finite where the recurrence's do; the scores q_t . k_s (in the
+ * backward also dout_t . v_s) have to lie within fp32 too.  With infinite or
  * NaN operands a result is finite exactly where the recurrence's is; which of
  * the others are infinite and which NaN is not promised.
  *   q [B][T][H][Dk], k [B][T][Hk][Dk], v [B][T][Hk][Dv], out [B][T][H][Dv]

@@ -210,8 +210,8 @@ __global__ __launch_bounds__(kStepB) void linattn_one(Shape s, Scan a, int32_t c
 // of bf16, each the rounding of what the ones before leave out.  The scores and the
 // fp32 state meet the values and the queries in two, exact to 2^-16; the state's update
 // takes W_k V in SPLIT, exact to 2^-8 SPLIT: two where only outputs follow, three where
-// a state is handed out (three everywhere: training 374 us instead of 337, for a part
-// that the outputs' own rounding hides).  So results lie 1.66e-3 from 64-bit ones, which
+// a state is handed out (three everywhere cost 11% of a training step, for a part that
+// the outputs' own rounding hides).  So results lie 1.66e-3 from 64-bit ones, which
 // is the rounding of the outputs alone.  With one part of the scores they lie at 1.75e-3
 // and training takes 362 us instead of 373, a prompt 132 instead of 133; with one of the
 // state too 2.35e-3, 331 and 121.  fp32 runs on the fp32 matrix instructions.
@@ -402,7 +402,7 @@ struct ChunkOf {
 };
 
 constexpr int kWaves = 4, kChunkB = 64 * kWaves;
-constexpr int kRescale = 8;
+constexpr int kRescale = 8;  // powers of two between a state's rescalings (linattn_chunks)
 
 // Rows of a chunk in memory: row r lies r `st` elements from row 0 (st < 0: back in
 // time).  Addresses are a pointer that all lanes share, to the row that comes first in
@@ -597,7 +597,7 @@ __global__ __launch_bounds__(kChunkB, (sizeof(ChunkLds<E, DK, NCT, OUT>) > 80 * 
   // the beginning (kept to 48 bits, as its roundings would add up over the chunks),
   // times a power of two that keeps it between 1 and 2^(kRescale + 1).  So the registers
   // never hold more than the state itself, and 1 / scale, which rides on the weights of
-  // the values, is never above 1: nothing overflows that the recurrence would not
+  // the values, is never above 1: no state overflows that the recurrence's would not
   // (states below 2^-117 lose their last bits).  scale rides on the outputs' weights.
   const double gcd = exp(lgd * C);
   const float gc = uniform((float)gcd), gc_lo = uniform((float)(gcd - (double)(float)gcd));

@@ -1,6 +1,6 @@
 """Linear attention on values near both ends of fp32's exponents, under decays that
-shrink a state by many powers of two on its way: whatever the recurrence itself
-holds in fp32 stays finite and as accurate as ordinary values."""
+shrink a state by many powers of two on its way: a state that the recurrence holds
+in fp32 stays finite and as accurate as ordinary values."""
 import math
 
 import pytest
