@@ -736,6 +736,74 @@ int diffopt_distill_bwd_bwd(const void* ddlogits, int64_t ddrow_stride,
 int64_t diffopt_distill_workspace(int64_t N, int64_t V, int32_t dtype,
                                   int64_t K);
 
+/* A gated linear recurrence over sequences, for each of C channels:
+ *   h_t = a_t h_{t-1} + x_t,  a_t = exp(log_gate_t)   t = 0 .. lengths[b] - 1
+ *   state_out = h_{lengths[b]-1}                      (h_{-1} = state)
+ * Tokens from lengths[b] on are not read and get h = 0.  A gate of -inf
+ * forgets what came before.  Gates above 0 are taken too; where the product of
+ * a run of them leaves fp32, results do.
+ *   log_gate, x, h  [B][T][C]: diffopt_heads whose heads are not used
+ *   lengths    DEVICE int32 [B] in [0, T] (clamped), or NULL for T
+ *   state, state_out  fp32 [B][C], or NULL (zeros / not wanted); state_out
+ *              may be state
+ *   B T C < 2^35, T <= 2^35; B ceil(C / 64) ceil(T / 64) < 2^23 - 1
+ *   workspace  device scratch of diffopt_gscan_workspace(..., order 0) bytes
+ *              (its contents do not matter); NULL if that is 0
+ * B or C == 0 is a no-op, T == 0 one but for state_out.                    */
+int diffopt_gscan_fwd(const diffopt_heads* log_gate, const diffopt_heads* x,
+                      const int32_t* lengths, const float* state, int64_t B,
+                      int64_t T, int64_t C, int32_t dtype,
+                      const diffopt_heads* h, float* state_out,
+                      void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Its vector-Jacobian product, for cotangents dh and dstate_out (NULL: 0).
+ * With e_L = dstate_out, going back in time,
+ *   dx_t = dh_t + e_{t+1},  e_t = a_t dx_t,  dlog_gate_t = e_t h_{t-1}
+ *   dstate = e_0
+ * h is computed again from the operands, in the same pass.  dlog_gate and dx
+ * (pointers to the struct) and dstate may be NULL: not wanted.  Rows from
+ * lengths[b] on get 0.  States lie apart from one another.  workspace: order
+ * 1.                                                                       */
+int diffopt_gscan_bwd(const diffopt_heads* dh, const float* dstate_out,
+                      const diffopt_heads* log_gate, const diffopt_heads* x,
+                      const int32_t* lengths, const float* state, int64_t B,
+                      int64_t T, int64_t C, int32_t dtype,
+                      const diffopt_heads* dlog_gate, const diffopt_heads* dx,
+                      float* dstate, void* workspace, int64_t workspace_bytes,
+                      void* stream);
+
+/* The vector-Jacobian product of that backward, for cotangents ddlog_gate = r,
+ * ddx = p and ddstate = s (NULL: 0) of its results:
+ *   y_t = a_t (y_{t-1} + r_t h_{t-1}) + p_t,  y_{-1} = s     forwards,
+ *   v_t = r_t dx_t + f_{t+1},  f_t = a_t v_t,  f_L = 0       backwards:
+ *   out_dh = y,  out_dstate_out = y_{L-1},  out_x_t = f_{t+1}
+ *   out_log_gate_t = a_t (dx_t y_{t-1} + v_t h_{t-1}),  out_state = f_0
+ * out_dstate_out and out_state may be NULL.  workspace: order 2.           */
+int diffopt_gscan_bwd_bwd(const diffopt_heads* ddlog_gate,
+                          const diffopt_heads* ddx, const float* ddstate,
+                          const diffopt_heads* dh, const float* dstate_out,
+                          const diffopt_heads* log_gate,
+                          const diffopt_heads* x, const int32_t* lengths,
+                          const float* state, int64_t B, int64_t T, int64_t C,
+                          int32_t dtype, const diffopt_heads* out_dh,
+                          float* out_dstate_out,
+                          const diffopt_heads* out_log_gate,
+                          const diffopt_heads* out_x, float* out_state,
+                          void* workspace, int64_t workspace_bytes,
+                          void* stream);
+
+/* Bytes of workspace those calls need (0: none): order 0 the forward, 1 the
+ * backward, 2 the backward's; -1 for sizes that they refuse.               */
+int64_t diffopt_gscan_workspace(int64_t B, int64_t T, int64_t C, int32_t dtype,
+                                int32_t order);
+
+/* One token for each of B sequences, the state fp32 [B][C] in place:
+ *   state = exp(log_gate) state + x,  out = state
+ * (the strides of the time axis are not used).                             */
+int diffopt_gscan_step(const diffopt_heads* log_gate, const diffopt_heads* x,
+                       int64_t B, int64_t C, int32_t dtype, float* state,
+                       const diffopt_heads* out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

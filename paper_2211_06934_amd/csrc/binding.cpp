@@ -11,6 +11,7 @@
 // that pass every check) and returns None for anything else; the Python
 // caller then takes its own path, which accepts or refuses the arguments with
 // its own messages.  No check is remembered from one call to the next.
+#include <c10/core/impl/DeviceGuardImplInterface.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/torch.h>
 
@@ -311,6 +312,10 @@ struct Call {
   void check(const at::Tensor& t, at::ScalarType type, at::IntArrayRef shape) const {
     if (!t.is_cuda() || t.scalar_type() != type || t.device() != like->device() || t.sizes() != shape) throw Other{};
   }
+  // The operands live on the device that the call launches on.
+  void current() const {
+    if (like->device() != c10::impl::getDeviceGuardImpl(c10::DeviceType::CUDA)->getDevice()) throw Other{};
+  }
   // A result's elements must not overlap (diffopt.operators._apart).
   static void apart(const at::Tensor& t) {
     if (t.is_contiguous()) return;
@@ -347,6 +352,22 @@ struct Call {
     if (shape[2] > 1 && t.stride(2) != 1 && t.numel() > 0) throw Other{};
     if (result) apart(t);
     return diffopt_heads{t.data_ptr(), t.stride(0), 0, t.stride(1)};
+  }
+  // [B, T, width]
+  diffopt_heads seq(PyObject* o, at::IntArrayRef shape, bool result) const {
+    const at::Tensor& t = tensor_of(o);
+    check(t, like->scalar_type(), shape);
+    if (shape[2] > 1 && t.stride(2) != 1 && t.numel() > 0) throw Other{};
+    if (result) apart(t);
+    return diffopt_heads{t.data_ptr(), t.stride(0), t.stride(1), 0};
+  }
+  // [B, width], as one token
+  diffopt_heads row(PyObject* o, at::IntArrayRef shape, bool result) const {
+    const at::Tensor& t = tensor_of(o);
+    check(t, like->scalar_type(), shape);
+    if (shape[1] > 1 && t.stride(1) != 1 && t.numel() > 0) throw Other{};
+    if (result) apart(t);
+    return diffopt_heads{t.data_ptr(), t.stride(0), 0, 0};
   }
   void* flat(PyObject* o, at::ScalarType type, at::IntArrayRef shape, bool optional = false) const {
     if (optional && o == Py_None) return nullptr;
@@ -708,6 +729,90 @@ PyObject* distill_bwd_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   });
 }
 
+// What the calls of gscan share: the sizes, and the operands' shape.
+struct Gscan {
+  int64_t B, T, C;
+  explicit Gscan(const Call& c) {
+    if (c.like->dim() != 3) throw Other{};
+    c.current();
+    B = c.like->size(0);
+    T = c.like->size(1);
+    C = c.like->size(2);
+  }
+  diffopt_heads seq(Call& c, bool result = false) const { return c.seq(c.next(), {B, T, C}, result); }
+  float* state(Call& c) const { return c.floats(c.next(), {B, C}, true); }
+  const int32_t* lengths(Call& c) const { return static_cast<int32_t*>(c.flat(c.next(), at::kInt, {B}, true)); }
+};
+
+// (log_gate, x, h, state, state_out, lengths, workspace, stream)
+PyObject* gscan_fwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return operator_call(args, nargs, 8, 1, [](Call& c, int32_t type) {
+    const Gscan g(c);
+    const diffopt_heads lg = g.seq(c), x = g.seq(c), h = g.seq(c, true);
+    const float* s0 = g.state(c);
+    float* s1 = g.state(c);
+    const int32_t* n = g.lengths(c);
+    const Scratch w(c.next(), diffopt_gscan_workspace(g.B, g.T, g.C, type, 0), *c.like);
+    void* stream = c.stream(c.next());
+    return unlocked([&] { return diffopt_gscan_fwd(&lg, &x, n, s0, g.B, g.T, g.C, type, &h, s1, w.p, w.bytes, stream); });
+  });
+}
+
+// (dh, log_gate, x, dlog_gate, dx, state, dstate_out, dstate, lengths, workspace, stream)
+PyObject* gscan_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return operator_call(args, nargs, 11, 2, [](Call& c, int32_t type) {
+    const Gscan g(c);
+    const diffopt_heads dh = g.seq(c), lg = g.seq(c), x = g.seq(c);
+    diffopt_heads out[2];
+    const diffopt_heads* d[2];
+    for (int i = 0; i < 2; ++i) {
+      PyObject* o = c.next();
+      d[i] = o == Py_None ? nullptr : &out[i];
+      if (d[i]) out[i] = c.seq(o, {g.B, g.T, g.C}, true);
+    }
+    const float *s0 = g.state(c), *ds1 = g.state(c);
+    float* ds0 = g.state(c);
+    const int32_t* n = g.lengths(c);
+    const Scratch w(c.next(), diffopt_gscan_workspace(g.B, g.T, g.C, type, 1), *c.like);
+    void* stream = c.stream(c.next());
+    return unlocked([&] {
+      return diffopt_gscan_bwd(&dh, ds1, &lg, &x, n, s0, g.B, g.T, g.C, type, d[0], d[1], ds0, w.p, w.bytes, stream);
+    });
+  });
+}
+
+// (ddlog_gate, ddx, dh, log_gate, x, out_dh, out_log_gate, out_x, state, dstate_out, ddstate, out_dstate_out, out_state, lengths,
+//  workspace, stream)
+PyObject* gscan_bwd_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return operator_call(args, nargs, 16, 4, [](Call& c, int32_t type) {
+    const Gscan g(c);
+    const diffopt_heads r = g.seq(c), p = g.seq(c), dh = g.seq(c), lg = g.seq(c), x = g.seq(c);
+    const diffopt_heads oh = g.seq(c, true), og = g.seq(c, true), ox = g.seq(c, true);
+    const float *s0 = g.state(c), *ds1 = g.state(c), *dds0 = g.state(c);
+    float *o1 = g.state(c), *o0 = g.state(c);
+    const int32_t* n = g.lengths(c);
+    const Scratch w(c.next(), diffopt_gscan_workspace(g.B, g.T, g.C, type, 2), *c.like);
+    void* stream = c.stream(c.next());
+    return unlocked([&] {
+      return diffopt_gscan_bwd_bwd(&r, &p, dds0, &dh, ds1, &lg, &x, n, s0, g.B, g.T, g.C, type, &oh, o1, &og, &ox, o0, w.p, w.bytes, stream);
+    });
+  });
+}
+
+// (log_gate, x, state, out, stream)
+PyObject* gscan_step(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return operator_call(args, nargs, 5, 1, [](Call& c, int32_t type) {
+    if (c.like->dim() != 2) throw Other{};
+    c.current();
+    const int64_t B = c.like->size(0), C = c.like->size(1);
+    const diffopt_heads lg = c.row(c.next(), {B, C}, false), x = c.row(c.next(), {B, C}, false);
+    float* state = c.floats(c.next(), {B, C});
+    const diffopt_heads out = c.row(c.next(), {B, C}, true);
+    void* stream = c.stream(c.next());
+    return unlocked([&] { return diffopt_gscan_step(&lg, &x, B, C, type, state, &out, stream); });
+  });
+}
+
 #define ENTRY(name) \
   {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&entry<&diffopt_##name>)), METH_FASTCALL, nullptr}
 
@@ -745,6 +850,10 @@ PyMethodDef methods[] = {
     OPERATOR(distill_bwd),
     OPERATOR(distill_fwd_bwd),
     OPERATOR(distill_bwd_bwd),
+    OPERATOR(gscan_fwd),
+    OPERATOR(gscan_bwd),
+    OPERATOR(gscan_bwd_bwd),
+    OPERATOR(gscan_step),
     {"leaf_pointers", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&leaf_pointers)), METH_FASTCALL, nullptr},
     {"leaf_shapes", &leaf_shapes, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};

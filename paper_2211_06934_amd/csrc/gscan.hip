@@ -1,0 +1,717 @@
+// A gated linear recurrence over sequences on gfx950 and its derivatives
+// (formulas in diffopt.h): h_t = a_t h_{t-1} + x_t for each channel, a = exp(log_gate).
+//
+// A run of tokens maps the state that enters it linearly: h -> A h + X with
+// A = exp(sum of its log gates) and X its own state from zero.  The adjoint e
+// runs the other way through the same gates, e -> A e + E, and the two
+// recurrences of the second derivative are coupled to them by r alone:
+// y -> A (y + rho h) + Y and f -> A (f + rho e) + F with rho the sum of r.  So
+// a run is known by A and one to five numbers a channel.  The logarithm of A is
+// kept, not A: a sum's rounding does not drift where a long product's does.
+//
+// A workgroup of kW waves holds a chunk of kW U tokens of 64 VEC channels in
+// registers, each wave U tokens of it, so that an operand is read once for both
+// directions.  Waves tell one another their runs through LDS.  Longer
+// sequences are cut into one chunk a workgroup: a first launch writes each
+// chunk's run, a small one turns runs into the states that enter each chunk, a
+// third walks the chunks.  A token past its sequence's end maps every state to
+// itself.
+#include <initializer_list>
+
+#include "lm_common.hpp"
+
+namespace diffopt {
+namespace {
+
+constexpr int kW = 8;  // waves of a chunk
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int64_t kMostGroups = (int64_t(1) << 32) / (64 * kW) - 1;  // a launch has fewer than 2^32 threads
+
+enum Mode { kFwd, kBwd, kSecond };
+
+// What a run is known by: kL, kX always, kE for the adjoint, the others for the second derivative.
+enum Field { kL, kX, kE, kRho, kY, kF };
+constexpr int fields(int mode) { return mode == kFwd ? 2 : mode == kBwd ? 3 : 6; }
+
+struct Scan {
+  HeadArr lg, x, dh, r, p;                  // operands
+  HeadArr out[3];                           // h / dlog_gate, dx / out_dh, out_log_gate, out_x
+  const int32_t* lengths;
+  const float *state, *dstate_out, *ddstate;
+  float *end, *begin, *end2;                // the state (or y) after the last token, the adjoint (or f) before the first
+  float* parts;                             // [B][S][fields][C]: chunks' runs, then the states that enter them
+  int64_t T, C, S;
+  int32_t cols, inline_join;
+};
+
+template <class E, int VEC>
+struct Pack {
+  typedef E type __attribute__((ext_vector_type(VEC), aligned(alignof(E))));
+};
+template <class E>
+struct Pack<E, 1> {
+  typedef E type;
+};
+
+template <class E, int VEC>
+__device__ __forceinline__ void load_pack(const E* at, float* v) {
+  const auto x = *reinterpret_cast<const typename Pack<E, VEC>::type*>(at);
+  if constexpr (VEC == 1) {
+    v[0] = (float)x;
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = (float)x[i];
+  }
+}
+
+template <class E, int VEC>
+__device__ __forceinline__ void store_pack(E* at, const float* v) {
+  if constexpr (VEC == 1) {
+    *at = (E)v[0];
+  } else {
+    typedef float wide __attribute__((ext_vector_type(VEC)));
+    typedef E whole __attribute__((ext_vector_type(VEC)));
+    wide w;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) w[i] = v[i];
+    *reinterpret_cast<typename Pack<E, VEC>::type*>(at) = __builtin_convertvector(w, whole);
+  }
+}
+
+__device__ __forceinline__ float gate(float lg) { return __builtin_amdgcn_exp2f(lg * kLog2e); }
+
+// States of VEC channels that pass through a run forwards (h, y) and backwards (e, f).
+template <int VEC>
+struct States {
+  float h[VEC], y[VEC], e[VEC], f[VEC];
+};
+
+// f(channel, field) gives the run.
+template <int MODE, class R>
+__device__ __forceinline__ void pass_fwd(float& h, float& y, const R& run) {
+  const float A = gate(run(kL));
+  if (MODE == kSecond) y = A * (y + run(kRho) * h) + run(kY);
+  h = A * h + run(kX);
+}
+
+template <int MODE, class R>
+__device__ __forceinline__ void pass_bwd(float& e, float& f, const R& run) {
+  const float A = gate(run(kL));
+  if (MODE == kSecond) f = A * (f + run(kRho) * e) + run(kF);
+  e = A * e + run(kE);
+}
+
+// Where a workgroup, a wave and a lane work.
+template <int VEC>
+struct Place {
+  int64_t b, seg, c, len;
+  bool on;  // the lane has channels; the last one's may be the neighbour's too, with the same values
+  __device__ __forceinline__ Place(const Scan& s) {
+    int64_t block = blockIdx.x;
+    const int64_t col = block % s.cols;
+    block /= s.cols;
+    seg = block % s.S;
+    b = block / s.S;
+    c = (col * 64 + (threadIdx.x & 63)) * VEC;
+    on = c < s.C;
+    if (c + VEC > s.C) c = s.C - VEC;  // C >= VEC
+    len = s.T;
+    if (s.lengths) {
+      const int64_t n = s.lengths[b];
+      len = n < 0 ? 0 : n < len ? n : len;
+    }
+  }
+};
+
+// A wave's tokens [t0, t0 + U) of VEC channels.
+template <class E, int MODE, int VEC, int U>
+struct Tokens {
+  float a[U][VEC], x[U][VEC], dh[MODE >= kBwd ? U : 1][VEC], r[MODE == kSecond ? U : 1][VEC], p[MODE == kSecond ? U : 1][VEC];
+  float run[fields(MODE)][VEC];
+
+  static __device__ __forceinline__ void rows(const HeadArr& h, const Place<VEC>& at, int64_t t0, float (*v)[VEC]) {
+    const E* p = static_cast<const E*>(h.p) + at.b * h.sb + at.c;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t t = t0 + u < at.len ? t0 + u : t0;  // a row that is there, for tokens past the end
+      load_pack<E, VEC>(p + t * h.st, v[u]);
+    }
+  }
+  static __device__ __forceinline__ void no_rows(float (*v)[VEC]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[u][i] = 0.0f;
+  }
+
+  // All of the tokens' operands on their way at once.
+  __device__ __forceinline__ void load(const Scan& s, const Place<VEC>& at, int64_t t0) {
+    if (t0 < at.len) {
+      rows(s.lg, at, t0, a);
+      rows(s.x, at, t0, x);
+      if constexpr (MODE >= kBwd) rows(s.dh, at, t0, dh);
+      if constexpr (MODE == kSecond) {
+        rows(s.r, at, t0, r);
+        rows(s.p, at, t0, p);
+      }
+    } else {
+      no_rows(a);
+      no_rows(x);
+      if constexpr (MODE >= kBwd) no_rows(dh);
+      if constexpr (MODE == kSecond) {
+        no_rows(r);
+        no_rows(p);
+      }
+    }
+  }
+
+  // Log gates become gates; tokens past the end the identity; the run of the rest.
+  __device__ __forceinline__ void finish(const Place<VEC>& at, int64_t t0) {
+#pragma unroll
+    for (int f = 0; f < fields(MODE); ++f)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) run[f][i] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool live = t0 + u < at.len;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float lg = live ? a[u][i] : 0.0f;
+        run[kL][i] += lg;
+        a[u][i] = gate(lg);
+        if (!live) {
+          x[u][i] = 0.0f;
+          if constexpr (MODE >= kBwd) dh[u][i] = 0.0f;
+          if constexpr (MODE == kSecond) r[u][i] = p[u][i] = 0.0f;
+        }
+        if constexpr (MODE == kSecond) {
+          run[kRho][i] += r[u][i];
+          run[kY][i] = a[u][i] * (run[kY][i] + r[u][i] * run[kX][i]) + p[u][i];
+        }
+        run[kX][i] = a[u][i] * run[kX][i] + x[u][i];
+      }
+    }
+    if constexpr (MODE >= kBwd)
+#pragma unroll
+      for (int u = U - 1; u >= 0; --u)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const float g = dh[u][i] + run[kE][i];
+          if constexpr (MODE == kSecond) run[kF][i] = a[u][i] * (r[u][i] * g + run[kF][i]);
+          run[kE][i] = a[u][i] * g;
+        }
+  }
+};
+
+// Waves' runs: channel i of a lane's VEC lies 64 floats on, so that a wave's
+// lanes read neighbouring words.
+template <int MODE, int VEC>
+struct Runs {
+  float v[kW][fields(MODE)][VEC][64];
+  template <class Tok>
+  __device__ __forceinline__ void put(int wave, int lane, const Tok& t) {
+#pragma unroll
+    for (int f = 0; f < fields(MODE); ++f)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[wave][f][i][lane] = t.run[f][i];
+  }
+};
+
+__device__ __forceinline__ float* part_of(const Scan& s, int nf, int64_t b, int64_t seg) { return s.parts + (b * s.S + seg) * nf * s.C; }
+
+// A chunk's run, for sequences of more than one chunk.
+template <class E, int MODE, int VEC, int U>
+__global__ __launch_bounds__(64 * kW) void gscan_runs(Scan s) {
+  __shared__ Runs<MODE, VEC> R;
+  constexpr int NF = fields(MODE);
+  const Place<VEC> at(s);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t t0 = (at.seg * kW + wave) * U;
+  Tokens<E, MODE, VEC, U> tok;
+  tok.load(s, at, t0);
+  tok.finish(at, t0);
+  R.put(wave, lane, tok);
+  __syncthreads();
+  if (wave != 0 || !at.on) return;
+  float* to = part_of(s, NF, at.b, at.seg) + at.c;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    float L = 0.0f, rho = 0.0f, h = 0.0f, y = 0.0f, e = 0.0f, f = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kW; ++w) {
+      L += R.v[w][kL][i][lane];
+      if constexpr (MODE == kSecond) rho += R.v[w][kRho][i][lane];
+      pass_fwd<MODE>(h, y, [&](int k) { return R.v[w][k][i][lane]; });
+    }
+    if constexpr (MODE >= kBwd)
+#pragma unroll
+      for (int w = kW - 1; w >= 0; --w) pass_bwd<MODE>(e, f, [&](int k) { return R.v[w][k][i][lane]; });
+    to[i] = L;
+    to[s.C + i] = h;
+    if constexpr (MODE >= kBwd) to[2 * s.C + i] = e;
+    if constexpr (MODE == kSecond) {
+      to[3 * s.C + i] = rho;
+      to[4 * s.C + i] = y;
+      to[5 * s.C + i] = f;
+    }
+  }
+}
+
+// Chunks' runs become the states that enter each chunk: kX holds h, kY y, kE e
+// and kF f.  A workgroup has 64 channels of a sequence, its waves share the
+// chunks.
+constexpr int kJW = 16, kBatch = 8;
+template <int MODE>
+__global__ __launch_bounds__(64 * kJW) void gscan_join(Scan s) {
+  constexpr int NF = fields(MODE);
+  __shared__ float v[kJW][NF][64];
+  const int64_t cols = (s.C + 63) / 64, b = blockIdx.x / cols;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c0 = (blockIdx.x - b * cols) * 64 + lane, c = c0 < s.C ? c0 : s.C - 1;
+  const int64_t per = (s.S + kJW - 1) / kJW, s0 = wave * per < s.S ? wave * per : s.S, s1 = s0 + per < s.S ? s0 + per : s.S;
+  float L = 0.0f, rho = 0.0f, h = 0.0f, y = 0.0f, e = 0.0f, f = 0.0f;
+  float run[kBatch][NF];
+  // chunks [first, first + kBatch) of the wave's, all loads at once
+  const auto load = [&](int64_t first) {
+#pragma unroll
+    for (int n = 0; n < kBatch; ++n) {
+      const int64_t seg = first + n < s1 ? first + n : s1 - 1;
+      const float* at = part_of(s, NF, b, seg) + c;
+#pragma unroll
+      for (int k = 0; k < NF; ++k) run[n][k] = at[k * s.C];
+    }
+  };
+  const int64_t batches = (s1 - s0 + kBatch - 1) / kBatch;
+  for (int64_t n0 = 0; n0 < batches; ++n0) {
+    load(s0 + n0 * kBatch);
+#pragma unroll
+    for (int n = 0; n < kBatch; ++n)
+      if (s0 + n0 * kBatch + n < s1) {
+        L += run[n][kL];
+        if constexpr (MODE == kSecond) rho += run[n][kRho];
+        pass_fwd<MODE>(h, y, [&](int k) { return run[n][k]; });
+      }
+  }
+  if constexpr (MODE >= kBwd)
+    for (int64_t n0 = batches - 1; n0 >= 0; --n0) {
+      if (batches > 1) load(s0 + n0 * kBatch);
+#pragma unroll
+      for (int n = kBatch - 1; n >= 0; --n)
+        if (s0 + n0 * kBatch + n < s1) pass_bwd<MODE>(e, f, [&](int k) { return run[n][k]; });
+    }
+  v[wave][kL][lane] = L;
+  v[wave][kX][lane] = h;
+  if constexpr (MODE >= kBwd) v[wave][kE][lane] = e;
+  if constexpr (MODE == kSecond) {
+    v[wave][kRho][lane] = rho;
+    v[wave][kY][lane] = y;
+    v[wave][kF][lane] = f;
+  }
+  h = s.state ? s.state[b * s.C + c] : 0.0f;
+  y = MODE == kSecond && s.ddstate ? s.ddstate[b * s.C + c] : 0.0f;
+  e = MODE >= kBwd && s.dstate_out ? s.dstate_out[b * s.C + c] : 0.0f;
+  f = 0.0f;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) pass_fwd<MODE>(h, y, [&](int k) { return v[w][k][lane]; });
+  if constexpr (MODE >= kBwd)
+    for (int w = kJW - 1; w > wave; --w) pass_bwd<MODE>(e, f, [&](int k) { return v[w][k][lane]; });
+  if (c0 >= s.C) return;
+  // the adjoint's way first: the forward way reads nothing that it writes
+  if constexpr (MODE >= kBwd)
+    for (int64_t n0 = batches - 1; n0 >= 0; --n0) {
+      if (batches > 1) load(s0 + n0 * kBatch);
+#pragma unroll
+      for (int n = kBatch - 1; n >= 0; --n) {
+        const int64_t seg = s0 + n0 * kBatch + n;
+        if (seg >= s1) continue;
+        float* at = part_of(s, NF, b, seg) + c;
+        at[kE * s.C] = e;
+        if constexpr (MODE == kSecond) at[kF * s.C] = f;
+        pass_bwd<MODE>(e, f, [&](int k) { return run[n][k]; });
+      }
+    }
+  for (int64_t n0 = 0; n0 < batches; ++n0) {
+    if (batches > 1) load(s0 + n0 * kBatch);
+#pragma unroll
+    for (int n = 0; n < kBatch; ++n) {
+      const int64_t seg = s0 + n0 * kBatch + n;
+      if (seg >= s1) continue;
+      float* at = part_of(s, NF, b, seg) + c;
+      at[kX * s.C] = h;
+      if constexpr (MODE == kSecond) at[kY * s.C] = y;
+      pass_fwd<MODE>(h, y, [&](int k) { return run[n][k]; });
+    }
+  }
+}
+
+// The states that enter a chunk, from both sides.
+template <int MODE, int VEC>
+__device__ __forceinline__ void enter(const Scan& s, const Place<VEC>& at, States<VEC>& st) {
+  constexpr int NF = fields(MODE);
+  const int64_t first = at.b * s.C + at.c;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    if (s.S > 1 && !s.inline_join) {
+      const float* from = part_of(s, NF, at.b, at.seg) + at.c + i;
+      st.h[i] = from[kX * s.C];
+      if constexpr (MODE >= kBwd) st.e[i] = from[kE * s.C];
+      if constexpr (MODE == kSecond) {
+        st.y[i] = from[kY * s.C];
+        st.f[i] = from[kF * s.C];
+      }
+    } else {
+      st.h[i] = s.state ? s.state[first + i] : 0.0f;
+      st.y[i] = MODE == kSecond && s.ddstate ? s.ddstate[first + i] : 0.0f;
+      st.e[i] = MODE >= kBwd && s.dstate_out ? s.dstate_out[first + i] : 0.0f;
+      st.f[i] = 0.0f;
+    }
+  }
+  if (s.S > 1 && s.inline_join) {
+    for (int64_t seg = 0; seg < at.seg; ++seg) {
+      const float* run = part_of(s, NF, at.b, seg) + at.c;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) pass_fwd<MODE>(st.h[i], st.y[i], [&](int k) { return run[k * s.C + i]; });
+    }
+    if constexpr (MODE >= kBwd)
+      for (int64_t seg = s.S - 1; seg > at.seg; --seg) {
+        const float* run = part_of(s, NF, at.b, seg) + at.c;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) pass_bwd<MODE>(st.e[i], st.f[i], [&](int k) { return run[k * s.C + i]; });
+      }
+  }
+}
+
+template <class E, int VEC, int U>
+__device__ __forceinline__ void store_rows(const Scan& s, const HeadArr& h, const Place<VEC>& at, int64_t t0, float (*v)[VEC]) {
+  E* p = static_cast<E*>(h.p) + at.b * h.sb + at.c;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (t0 + u >= at.len) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[u][i] = 0.0f;
+    }
+    if (t0 + u < s.T) store_pack<E, VEC>(p + (t0 + u) * h.st, v[u]);
+  }
+}
+
+// A chunk's results.
+template <class E, int MODE, int VEC, int U>
+__global__ __launch_bounds__(64 * kW) void gscan_walk(Scan s) {
+  __shared__ Runs<MODE, VEC> R;
+  const Place<VEC> at(s);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t t0 = (at.seg * kW + wave) * U;
+  Tokens<E, MODE, VEC, U> tok;
+  tok.load(s, at, t0);
+  States<VEC> st;
+  enter<MODE, VEC>(s, at, st);
+  tok.finish(at, t0);
+  R.put(wave, lane, tok);
+  __syncthreads();  // also: every wave has read the state that the last one may now overwrite
+  if (!at.on) return;
+  for (int w = 0; w < wave; ++w)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) pass_fwd<MODE>(st.h[i], st.y[i], [&](int k) { return R.v[w][k][i][lane]; });
+  if constexpr (MODE >= kBwd)
+    for (int w = kW - 1; w > wave; --w)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) pass_bwd<MODE>(st.e[i], st.f[i], [&](int k) { return R.v[w][k][i][lane]; });
+  const bool last = at.seg == s.S - 1 && wave == kW - 1, first = at.seg == 0 && wave == 0;
+  const int64_t state = at.b * s.C + at.c;
+  if constexpr (MODE == kFwd) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) tok.x[u][i] = st.h[i] = tok.a[u][i] * st.h[i] + tok.x[u][i];
+    store_rows<E, VEC, U>(s, s.out[0], at, t0, tok.x);
+    if (last && s.end)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) s.end[state + i] = st.h[i];
+  } else if constexpr (MODE == kBwd) {
+    float dlg[U][VEC];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        dlg[u][i] = st.h[i];
+        st.h[i] = tok.a[u][i] * st.h[i] + tok.x[u][i];
+      }
+#pragma unroll
+    for (int u = U - 1; u >= 0; --u)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float g = tok.dh[u][i] + st.e[i];
+        st.e[i] = tok.a[u][i] * g;
+        dlg[u][i] *= st.e[i];
+        tok.dh[u][i] = g;
+      }
+    if (s.out[0].p) store_rows<E, VEC, U>(s, s.out[0], at, t0, dlg);
+    if (s.out[1].p) store_rows<E, VEC, U>(s, s.out[1], at, t0, tok.dh);
+    if (first && s.begin)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) s.begin[state + i] = st.e[i];
+  } else {
+    float hp[U][VEC], yp[U][VEC];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        hp[u][i] = st.h[i];
+        yp[u][i] = st.y[i];
+        tok.p[u][i] = st.y[i] = tok.a[u][i] * (st.y[i] + tok.r[u][i] * st.h[i]) + tok.p[u][i];
+        st.h[i] = tok.a[u][i] * st.h[i] + tok.x[u][i];
+      }
+    store_rows<E, VEC, U>(s, s.out[0], at, t0, tok.p);
+    if (last && s.end)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) s.end[state + i] = st.y[i];
+#pragma unroll
+    for (int u = U - 1; u >= 0; --u)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float a = tok.a[u][i], g = tok.dh[u][i] + st.e[i], v = tok.r[u][i] * g + st.f[i];
+        tok.x[u][i] = st.f[i];
+        hp[u][i] = a * (g * yp[u][i] + hp[u][i] * v);
+        st.e[i] = a * g;
+        st.f[i] = a * v;
+      }
+    store_rows<E, VEC, U>(s, s.out[1], at, t0, hp);
+    store_rows<E, VEC, U>(s, s.out[2], at, t0, tok.x);
+    if (first && s.begin)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) s.begin[state + i] = st.f[i];
+  }
+}
+
+// One token of every sequence, the state in place.
+template <class E, int VEC>
+__global__ __launch_bounds__(kBlock) void gscan_one(HeadArr lg, HeadArr x, HeadArr out, float* state, int64_t C, int64_t cols, int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+  if (i >= n) return;
+  const int64_t b = i / cols;
+  const int64_t c = (i - b * cols) * VEC;
+  float g[VEC], v[VEC], h[VEC];
+  float* const at = state + b * C + c;
+  load_pack<float, VEC>(at, h);
+  load_pack<E, VEC>(static_cast<const E*>(lg.p) + b * lg.sb + c, g);
+  load_pack<E, VEC>(static_cast<const E*>(x.p) + b * x.sb + c, v);
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) h[k] = gate(g[k]) * h[k] + v[k];
+  store_pack<float, VEC>(at, h);
+  store_pack<E, VEC>(static_cast<E*>(out.p) + b * out.sb + c, h);
+}
+
+// ---- host -------------------------------------------------------------------
+
+constexpr int kU = 8;  // tokens of a wave
+constexpr int64_t kChunk = kW * kU;
+constexpr int64_t kInlineJoin = 8;
+
+int64_t chunks_of(int64_t T) { return T <= kChunk ? 1 : (T + kChunk - 1) / kChunk; }
+
+int64_t workspace_bytes(int64_t B, int64_t T, int64_t C, int mode) {
+  const int64_t S = chunks_of(T);
+  return B == 0 || C == 0 || S == 1 ? 0 : B * S * fields(mode) * C * 4;
+}
+
+bool sizes_ok(int64_t B, int64_t T, int64_t C) {
+  if (B < 0 || T < 0 || C < 0) return false;
+  if (B == 0 || C == 0) return true;
+  if (T > (int64_t(1) << 35) || C > (int64_t(1) << 31) || B > (int64_t(1) << 31)) return false;
+  const int64_t cols = (C + 63) / 64, S = chunks_of(T);  // at most 2^25, 2^29
+  return cols <= kMostGroups / S && B <= kMostGroups / (cols * S);
+}
+
+template <class E, int MODE, int VEC>
+int launch(const char* who, Scan s, int64_t B, hipStream_t st) {
+  s.cols = (int32_t)((s.C + 64 * VEC - 1) / (64 * VEC));
+  const dim3 grid((unsigned)(B * s.S * s.cols)), block(64 * kW);
+  if (s.S > 1) {
+    hipLaunchKernelGGL((gscan_runs<E, MODE, VEC, kU>), grid, block, 0, st, s);
+    if (!s.inline_join) hipLaunchKernelGGL((gscan_join<MODE>), dim3((unsigned)(B * ((s.C + 63) / 64))), dim3(64 * kJW), 0, st, s);
+  }
+  hipLaunchKernelGGL((gscan_walk<E, MODE, VEC, kU>), grid, block, 0, st, s);
+  return launch_status(who);
+}
+
+template <int MODE>
+int run(const char* who, const Scan& s, int64_t B, int32_t dtype, hipStream_t st) {
+  constexpr int V = MODE == kSecond ? 2 : 4;
+  if (s.C < 64 * V) return dtype == DIFFOPT_F32 ? launch<float, MODE, 1>(who, s, B, st) : launch<bf16, MODE, 1>(who, s, B, st);
+  return dtype == DIFFOPT_F32 ? launch<float, MODE, V>(who, s, B, st) : launch<bf16, MODE, V>(who, s, B, st);
+}
+
+struct Operand {
+  const char* name;
+  const diffopt_heads* given;
+  HeadArr* to;
+  bool optional = false;
+};
+
+// The [B][T][C] operands and results of a call: there, aligned, no result where an operand or another result begins.
+int check_arrays(const char* who, int32_t dtype, std::initializer_list<Operand> operands, std::initializer_list<Operand> results) {
+  for (const Operand& o : operands)
+    if (int rc = check_heads(who, o.name, o.given, dtype, o.to)) return rc;
+  for (const Operand& o : results)
+    if (!o.optional || o.given)
+      if (int rc = check_heads(who, o.name, o.given, dtype, o.to)) return rc;
+  for (auto r = results.begin(); r != results.end(); ++r) {
+    if (!r->to->p) continue;
+    for (const Operand& o : operands)
+      if (r->to->p == o.to->p) return fail(DIFFOPT_EINVAL, "%s: %s must not be %s", who, r->name, o.name);
+    for (auto t = results.begin(); t != r; ++t)
+      if (r->to->p == t->to->p) return fail(DIFFOPT_EINVAL, "%s: %s must not be %s", who, r->name, t->name);
+  }
+  return DIFFOPT_OK;
+}
+
+struct States32 {
+  const char* name;
+  const float* p;
+};
+
+// [B][C] states: aligned; no result over an operand or another result.
+int check_states(const char* who, int64_t bytes, std::initializer_list<States32> operands, std::initializer_list<States32> results) {
+  for (const auto& list : {operands, results})
+    for (const States32& s : list)
+      if (!aligned_to(s.p, 4)) return fail(DIFFOPT_EINVAL, "%s: %s is not 4-byte aligned", who, s.name);
+  for (auto r = results.begin(); r != results.end(); ++r) {
+    for (const States32& o : operands)
+      if (overlap(r->p, bytes, o.p, bytes)) return fail(DIFFOPT_EINVAL, "%s: %s must lie apart from %s", who, r->name, o.name);
+    for (auto t = results.begin(); t != r; ++t)
+      if (overlap(r->p, bytes, t->p, bytes)) return fail(DIFFOPT_EINVAL, "%s: %s must lie apart from %s", who, r->name, t->name);
+  }
+  return DIFFOPT_OK;
+}
+
+int check_call(const char* who, const int32_t* lengths, int64_t B, int64_t T, int64_t C, int32_t dtype) {
+  if (B < 0 || T < 0 || C < 0) return fail(DIFFOPT_EINVAL, "%s: sizes must be >= 0", who);
+  if (!sizes_ok(B, T, C)) return fail(DIFFOPT_EINVAL, "%s: too many sequences, tokens or channels", who);
+  if (!dtype_ok(dtype)) return fail(DIFFOPT_EINVAL, "%s: unknown element type %d", who, (int)dtype);
+  if (!aligned_to(lengths, 4)) return fail(DIFFOPT_EINVAL, "%s: lengths is not 4-byte aligned", who);
+  return DIFFOPT_OK;
+}
+
+int check_workspace(const char* who, int64_t B, int64_t T, int64_t C, int mode, const void* workspace, int64_t bytes) {
+  const int64_t need = workspace_bytes(B, T, C, mode);
+  if (need > 0 && (!workspace || bytes < need))
+    return fail(DIFFOPT_EINVAL, "%s: the workspace has %lld bytes of %lld", who, (long long)(workspace ? bytes : 0), (long long)need);
+  if (!aligned_to(workspace, 4)) return fail(DIFFOPT_EINVAL, "%s: the workspace is not 4-byte aligned", who);
+  return DIFFOPT_OK;
+}
+
+}  // namespace
+}  // namespace diffopt
+
+using namespace diffopt;
+
+extern "C" int64_t diffopt_gscan_workspace(int64_t B, int64_t T, int64_t C, int32_t dtype, int32_t order) {
+  if (!sizes_ok(B, T, C) || !dtype_ok(dtype) || order < 0 || order > 2) return -1;
+  return workspace_bytes(B, T, C, order);
+}
+
+extern "C" int diffopt_gscan_fwd(const diffopt_heads* log_gate, const diffopt_heads* x, const int32_t* lengths, const float* state, int64_t B,
+                                 int64_t T, int64_t C, int32_t dtype, const diffopt_heads* h, float* state_out, void* workspace,
+                                 int64_t workspace_bytes, void* stream) {
+  clear_error();
+  static const char* who = "diffopt_gscan_fwd";
+  int rc = check_call(who, lengths, B, T, C, dtype);
+  if (rc || B == 0 || C == 0) return rc;
+  Scan s{};
+  if (T > 0) rc = check_arrays(who, dtype, {{"log_gate", log_gate, &s.lg}, {"x", x, &s.x}}, {{"h", h, &s.out[0]}});
+  const bool in_place = state && state_out == state;
+  if (!rc) rc = check_states(who, 4 * B * C, {{"state", in_place ? nullptr : state}}, {{"state_out", state_out}});
+  if (!rc) rc = check_workspace(who, B, T, C, kFwd, workspace, workspace_bytes);
+  if (rc || (T == 0 && !state_out)) return rc;
+  s.lengths = lengths;
+  s.state = state;
+  s.end = state_out;
+  s.parts = static_cast<float*>(workspace);
+  s.T = T;
+  s.C = C;
+  s.S = chunks_of(T);
+  s.inline_join = s.S <= kInlineJoin && !in_place;
+  return run<kFwd>(who, s, B, dtype, as_stream(stream));
+}
+
+extern "C" int diffopt_gscan_bwd(const diffopt_heads* dh, const float* dstate_out, const diffopt_heads* log_gate, const diffopt_heads* x,
+                                 const int32_t* lengths, const float* state, int64_t B, int64_t T, int64_t C, int32_t dtype,
+                                 const diffopt_heads* dlog_gate, const diffopt_heads* dx, float* dstate, void* workspace,
+                                 int64_t workspace_bytes, void* stream) {
+  clear_error();
+  static const char* who = "diffopt_gscan_bwd";
+  int rc = check_call(who, lengths, B, T, C, dtype);
+  if (rc || B == 0 || C == 0) return rc;
+  Scan s{};
+  if (T > 0)
+    rc = check_arrays(who, dtype, {{"log_gate", log_gate, &s.lg}, {"x", x, &s.x}, {"dh", dh, &s.dh}},
+                      {{"dlog_gate", dlog_gate, &s.out[0], true}, {"dx", dx, &s.out[1], true}});
+  if (!rc) rc = check_states(who, 4 * B * C, {{"state", state}, {"dstate_out", dstate_out}}, {{"dstate", dstate}});
+  if (!rc) rc = check_workspace(who, B, T, C, kBwd, workspace, workspace_bytes);
+  if (rc || ((T == 0 || (!dlog_gate && !dx)) && !dstate)) return rc;
+  s.lengths = lengths;
+  s.state = state;
+  s.dstate_out = dstate_out;
+  s.begin = dstate;
+  s.parts = static_cast<float*>(workspace);
+  s.T = T;
+  s.C = C;
+  s.S = chunks_of(T);
+  s.inline_join = s.S <= kInlineJoin;
+  return run<kBwd>(who, s, B, dtype, as_stream(stream));
+}
+
+extern "C" int diffopt_gscan_bwd_bwd(const diffopt_heads* ddlog_gate, const diffopt_heads* ddx, const float* ddstate, const diffopt_heads* dh,
+                                     const float* dstate_out, const diffopt_heads* log_gate, const diffopt_heads* x, const int32_t* lengths,
+                                     const float* state, int64_t B, int64_t T, int64_t C, int32_t dtype, const diffopt_heads* out_dh,
+                                     float* out_dstate_out, const diffopt_heads* out_log_gate, const diffopt_heads* out_x, float* out_state,
+                                     void* workspace, int64_t workspace_bytes, void* stream) {
+  clear_error();
+  static const char* who = "diffopt_gscan_bwd_bwd";
+  int rc = check_call(who, lengths, B, T, C, dtype);
+  if (rc || B == 0 || C == 0) return rc;
+  Scan s{};
+  if (T > 0)
+    rc = check_arrays(who, dtype,
+                      {{"ddlog_gate", ddlog_gate, &s.r}, {"ddx", ddx, &s.p}, {"dh", dh, &s.dh}, {"log_gate", log_gate, &s.lg}, {"x", x, &s.x}},
+                      {{"out_dh", out_dh, &s.out[0]}, {"out_log_gate", out_log_gate, &s.out[1]}, {"out_x", out_x, &s.out[2]}});
+  if (!rc)
+    rc = check_states(who, 4 * B * C, {{"state", state}, {"dstate_out", dstate_out}, {"ddstate", ddstate}},
+                      {{"out_dstate_out", out_dstate_out}, {"out_state", out_state}});
+  if (!rc) rc = check_workspace(who, B, T, C, kSecond, workspace, workspace_bytes);
+  if (rc || (T == 0 && !out_dstate_out && !out_state)) return rc;
+  s.lengths = lengths;
+  s.state = state;
+  s.dstate_out = dstate_out;
+  s.ddstate = ddstate;
+  s.end = out_dstate_out;
+  s.begin = out_state;
+  s.parts = static_cast<float*>(workspace);
+  s.T = T;
+  s.C = C;
+  s.S = chunks_of(T);
+  s.inline_join = s.S <= kInlineJoin;
+  return run<kSecond>(who, s, B, dtype, as_stream(stream));
+}
+
+extern "C" int diffopt_gscan_step(const diffopt_heads* log_gate, const diffopt_heads* x, int64_t B, int64_t C, int32_t dtype, float* state,
+                                  const diffopt_heads* out, void* stream) {
+  clear_error();
+  static const char* who = "diffopt_gscan_step";
+  int rc = check_call(who, nullptr, B, 1, C, dtype);
+  if (rc || B == 0 || C == 0) return rc;
+  HeadArr lg, xs, o;
+  rc = check_arrays(who, dtype, {{"log_gate", log_gate, &lg}, {"x", x, &xs}}, {{"out", out, &o}});
+  if (rc) return rc;
+  if (!state) return fail(DIFFOPT_EINVAL, "%s: null state", who);
+  if (!aligned_to(state, 4)) return fail(DIFFOPT_EINVAL, "%s: state is not 4-byte aligned", who);
+  if (state == lg.p || state == xs.p || state == o.p) return fail(DIFFOPT_EINVAL, "%s: state must lie apart from the operands and out", who);
+  const hipStream_t st = as_stream(stream);
+  const auto go = [&](auto kernel, int vec) {
+    const int64_t cols = C / vec, n = B * cols;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((n + kBlock - 1) / kBlock)), dim3(kBlock), 0, st, lg, xs, o, state, C, cols, n);
+    return launch_status(who);
+  };
+  if (C % 4 == 0) return dtype == DIFFOPT_F32 ? go(gscan_one<float, 4>, 4) : go(gscan_one<bf16, 4>, 4);
+  return dtype == DIFFOPT_F32 ? go(gscan_one<float, 1>, 1) : go(gscan_one<bf16, 1>, 1);
+}

@@ -8,15 +8,15 @@ so each Function here has a backward that is a Function itself:
   and bilinear in (k, v), its gradients are the same sum on permuted operands,
   and the derivative of a gradient is made of the operator's own calls.  Any
   order of differentiation works.
-* ``qknorm_rope`` and ``distillation_loss``: differentiable twice, by kernels
-  for the backward and for the backward's backward.  Asking for a third order
-  raises an error.
+* ``qknorm_rope``, ``gated_scan`` and ``distillation_loss``: differentiable
+  twice, by kernels for the backward and for the backward's backward.  Asking
+  for a third order raises an error.
 
 Tensors are brought into a shape that the kernels read (whole heads, whole
 rows) before a Function is applied, so that what it saves are its inputs.
 
-``linear_attention_step`` is the single-token form for generation: no graph,
-the state updated in place.
+``linear_attention_step`` and ``gated_scan_step`` are the single-token forms
+for generation: no graph, the state updated in place.
 """
 from __future__ import annotations
 
@@ -159,6 +159,83 @@ def linear_attention_step(q, k, v, log_decay, state, scale: float = 1.0) -> torc
         q, k, v = _dense(q), _dense(k), _dense(v)
         out = torch.empty(*q.shape[:2], v.shape[2], dtype=q.dtype, device=q.device)
         _o.linattn_step(q, k, v, log_decay, state, out, scale)
+    if not state.is_inference():  # the kernel wrote past torch: a graph that saved the state has to notice
+        torch.autograd.graph.increment_version(state)
+    return out
+
+
+# ---- gated recurrence -------------------------------------------------------
+
+
+class GatedScanFn(torch.autograd.Function):
+    """(log_gate, x, state) -> (h, state_out); state may be None."""
+
+    @staticmethod
+    def forward(ctx, log_gate, x, state, lengths, want_state: bool):
+        h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        s1 = torch.empty(x.shape[0], x.shape[2], device=x.device) if want_state else None
+        _o.gscan_fwd(log_gate, x, h, state, s1, lengths)
+        ctx.save_for_backward(log_gate, x, state, lengths)
+        ctx.set_materialize_grads(False)
+        return h, s1
+
+    @staticmethod
+    def backward(ctx, dh, ds1):
+        log_gate, x, state, lengths = ctx.saved_tensors
+        if dh is None and ds1 is None:
+            return (None,) * 5
+        dh = torch.zeros(x.shape, dtype=x.dtype, device=x.device) if dh is None else _dense(dh)
+        return (*GatedScanGradFn.apply(dh, _whole(ds1), log_gate, x, state, lengths), None, None)
+
+
+class GatedScanGradFn(torch.autograd.Function):
+    """(dh, dstate_out, log_gate, x, state) -> (dlog_gate, dx, dstate)."""
+
+    @staticmethod
+    def forward(ctx, dh, ds1, log_gate, x, state, lengths):
+        dg, dx = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for _ in range(2))
+        ds = None if state is None else torch.empty_like(state)
+        _o.gscan_bwd(dh, log_gate, x, dg, dx, state, ds1, ds, lengths)
+        ctx.save_for_backward(dh, ds1, log_gate, x, state, lengths)
+        ctx.set_materialize_grads(False)
+        return dg, dx, ds
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, r, p, s):
+        dh, ds1, log_gate, x, state, lengths = ctx.saved_tensors
+        if r is None and p is None and s is None:
+            return (None,) * 6
+        new = lambda like: torch.empty(like.shape, dtype=like.dtype, device=like.device)
+        zero = lambda c: torch.zeros(x.shape, dtype=x.dtype, device=x.device) if c is None else _dense(c)
+        oh, og, ox = new(x), new(x), new(x)
+        o1, o0 = (None if like is None else new(like) for like in (ds1, state))
+        _o.gscan_bwd_bwd(zero(r), zero(p), dh, log_gate, x, oh, og, ox, state, ds1, _whole(s), o1, o0, lengths)
+        return oh, o1, og, ox, o0, None
+
+
+def gated_scan(log_gate, x, state=None, lengths=None, return_state: bool = False):
+    """h_t = exp(log_gate_t) h_{t-1} + x_t for each channel, over sequences: log_gate and x [B, T, C], both fp32 or both bf16.
+
+    state: fp32 [B, C] before the first token (None: zeros).  lengths: int32 [B]; tokens from there on give zeros.  A gate
+    of -inf forgets what came before (where another document begins).  Returns h [B, T, C], with return_state also the
+    state after the last token.  Differentiable twice in log_gate, x and state."""
+    h, s1 = GatedScanFn.apply(_dense(log_gate), _dense(x), _whole(state), lengths, bool(return_state))
+    return (h, s1) if return_state else h
+
+
+def gated_scan_step(log_gate, x, state) -> torch.Tensor:
+    """One token of every sequence for generation: log_gate, x [B, C] -> h [B, C]; `state` is updated in place.  Not
+    differentiable: an operand that asks for a gradient is refused, but under torch.no_grad()."""
+    if torch.is_grad_enabled():
+        for t, what in ((log_gate, "log_gate"), (x, "x"), (state, "state")):
+            if isinstance(t, torch.Tensor) and t.requires_grad:
+                raise ValueError("gated_scan_step: %s asks for a gradient, and single tokens have none: detach it, or step "
+                                 "under torch.no_grad()" % what)
+    with torch.no_grad():
+        log_gate, x = _dense(log_gate), _dense(x)
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        _o.gscan_step(log_gate, x, state, out)
     if not state.is_inference():  # the kernel wrote past torch: a graph that saved the state has to notice
         torch.autograd.graph.increment_version(state)
     return out

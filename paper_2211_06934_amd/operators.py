@@ -49,6 +49,12 @@ _SIGNATURES = {
     "diffopt_distill_fwd_bwd": (_i32, [_vp, *_ROWS, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _vp]),
     "diffopt_distill_bwd_bwd": (_i32, [_vp, _i64, _vp, _vp, *_ROWS, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _vp]),
     "diffopt_distill_workspace": (_i64, [_i64, _i64, _i32, _i64]),
+    "diffopt_gscan_fwd": (_i32, [_hp, _hp, _vp, _vp, _i64, _i64, _i64, _i32, _hp, _vp, _vp, _i64, _vp]),
+    "diffopt_gscan_bwd": (_i32, [_hp, _vp, _hp, _hp, _vp, _vp, _i64, _i64, _i64, _i32, _hp, _hp, _vp, _vp, _i64, _vp]),
+    "diffopt_gscan_bwd_bwd": (_i32, [_hp, _hp, _vp, _hp, _vp, _hp, _hp, _vp, _vp, _i64, _i64, _i64, _i32, _hp, _vp, _hp, _hp, _vp, _vp,
+                                     _i64, _vp]),
+    "diffopt_gscan_workspace": (_i64, [_i64, _i64, _i64, _i32, _i32]),
+    "diffopt_gscan_step": (_i32, [_hp, _hp, _i64, _i64, _i32, _vp, _hp, _vp]),
 }
 for _name, (_res, _args) in _SIGNATURES.items():
     if not hasattr(_lib, _name):
@@ -114,6 +120,12 @@ def _type_of(x, what: str) -> int:
     if x.dtype not in _DTYPES:
         raise ValueError("%s: expected dtype torch.float32 or torch.bfloat16, got %s" % (what, x.dtype))
     return _DTYPES[x.dtype]
+
+
+def _current(x, what: str) -> None:
+    """A call launches on the current device: its operands live there."""
+    if x.device.index != torch.cuda.current_device():
+        raise ValueError("%s: lives on %s, the current device is cuda:%d" % (what, x.device, torch.cuda.current_device()))
 
 
 def _here(workspace, stream) -> bool:
@@ -411,3 +423,102 @@ def distill_bwd_bwd(ddlogits, ddteacher, dloss, logits, ids, teacher, stats, out
     _check(_lib.diffopt_distill_bwd_bwd(pa, astride, _flat(ddteacher, "ddteacher", logits, (N, K), True), pg, *args, ps,
                                         _flat(out_dloss, "out_dloss", logits, (N,), True), po, ostride,
                                         _flat(out_teacher, "out_teacher", logits, (N, K), True), ws, nws, _stream(stream)))
+
+
+# ---- gated recurrence -------------------------------------------------------
+
+
+def _seq(x, what: str, like: torch.Tensor, shape, result: bool = False, optional: bool = False):
+    """A [B, T, C] tensor of the call's type as the C struct."""
+    if x is None and optional:
+        return None
+    _tensor(x, what, like.dtype, shape, like.device)
+    if x.shape[2] > 1 and x.stride(2) != 1 and x.numel() > 0:
+        raise ValueError("%s: a token's elements must be contiguous" % what)
+    if result:
+        _apart(x, what)
+    return _Heads(x.data_ptr() or None, x.stride(0), x.stride(1), 0)
+
+
+def _scan_sizes(x):
+    dt = _type_of(x, "x")
+    if x.dim() != 3:
+        raise ValueError("x: expected a tensor of 3 axes")
+    _current(x, "x")
+    return (*x.shape, dt)
+
+
+def gscan_workspace(B: int, T: int, C: int, dtype=torch.float32, order: int = 0) -> int:
+    """diffopt_gscan_workspace: bytes that gscan_fwd (order 0), gscan_bwd (1) or gscan_bwd_bwd (2) needs for these sizes."""
+    n = int(_lib.diffopt_gscan_workspace(B, T, C, _DTYPES[dtype], order))
+    if n < 0:
+        raise ValueError("gscan: sizes that the operator refuses")
+    return n
+
+
+def gscan_fwd(log_gate, x, h, state=None, state_out=None, lengths=None, workspace=None, stream=None) -> None:
+    """diffopt_gscan_fwd: h_t = exp(log_gate_t) h_{t-1} + x_t.
+
+    log_gate, x, h [B, T, C]; state, state_out fp32 [B, C] before the first and after the last token; lengths int32 [B]
+    (tokens from there on are padding)."""
+    if _here(workspace, stream) and _done(_native.gscan_fwd(
+            log_gate, x, h, state, state_out, lengths, workspace, _stream(stream))):
+        return
+    B, T, C, dt = _scan_sizes(x)
+    cg, cx, ch = _seq(log_gate, "log_gate", x, (B, T, C)), _seq(x, "x", x, (B, T, C)), _seq(h, "h", x, (B, T, C), True)
+    ln = _flat(lengths, "lengths", x, (B,), True, torch.int32)
+    s0, s1 = _flat(state, "state", x, (B, C), True), _flat(state_out, "state_out", x, (B, C), True)
+    keep, ws, nws = _scratch(workspace, _lib.diffopt_gscan_workspace(B, T, C, dt, 0), x.device, stream)
+    _check(_lib.diffopt_gscan_fwd(_ref(cg), _ref(cx), ln, s0, B, T, C, dt, _ref(ch), s1, ws, nws, _stream(stream)))
+
+
+def gscan_bwd(dh, log_gate, x, dlog_gate, dx, state=None, dstate_out=None, dstate=None, lengths=None, workspace=None,
+              stream=None) -> None:
+    """diffopt_gscan_bwd: gradients of gscan_fwd for the cotangents dh and dstate_out; any of dlog_gate, dx, dstate may be None."""
+    if _here(workspace, stream) and _done(_native.gscan_bwd(
+            dh, log_gate, x, dlog_gate, dx, state, dstate_out, dstate, lengths, workspace, _stream(stream))):
+        return
+    B, T, C, dt = _scan_sizes(x)
+    cd, cg, cx = (_seq(t, w, x, (B, T, C)) for t, w in ((dh, "dh"), (log_gate, "log_gate"), (x, "x")))
+    og, ox = (_seq(t, w, x, (B, T, C), True, True) for t, w in ((dlog_gate, "dlog_gate"), (dx, "dx")))
+    ln = _flat(lengths, "lengths", x, (B,), True, torch.int32)
+    s0, ds1, ds0 = (_flat(t, w, x, (B, C), True) for t, w in ((state, "state"), (dstate_out, "dstate_out"), (dstate, "dstate")))
+    keep, ws, nws = _scratch(workspace, _lib.diffopt_gscan_workspace(B, T, C, dt, 1), x.device, stream)
+    _check(_lib.diffopt_gscan_bwd(_ref(cd), ds1, _ref(cg), _ref(cx), ln, s0, B, T, C, dt, _ref(og), _ref(ox), ds0, ws, nws,
+                                  _stream(stream)))
+
+
+def gscan_bwd_bwd(ddlog_gate, ddx, dh, log_gate, x, out_dh, out_log_gate, out_x, state=None, dstate_out=None, ddstate=None,
+                  out_dstate_out=None, out_state=None, lengths=None, workspace=None, stream=None) -> None:
+    """diffopt_gscan_bwd_bwd: gradients of gscan_bwd for cotangents of dlog_gate, dx and dstate (ddstate None: zero);
+    out_dstate_out and out_state may be None."""
+    if _here(workspace, stream) and _done(_native.gscan_bwd_bwd(
+            ddlog_gate, ddx, dh, log_gate, x, out_dh, out_log_gate, out_x, state, dstate_out, ddstate, out_dstate_out, out_state,
+            lengths, workspace, _stream(stream))):
+        return
+    B, T, C, dt = _scan_sizes(x)
+    cr, cp, cd, cg, cx = (_seq(t, w, x, (B, T, C)) for t, w in ((ddlog_gate, "ddlog_gate"), (ddx, "ddx"), (dh, "dh"),
+                                                                (log_gate, "log_gate"), (x, "x")))
+    oh, og, ox = (_seq(t, w, x, (B, T, C), True) for t, w in ((out_dh, "out_dh"), (out_log_gate, "out_log_gate"), (out_x, "out_x")))
+    ln = _flat(lengths, "lengths", x, (B,), True, torch.int32)
+    s0, ds1, dds0, o1, o0 = (_flat(t, w, x, (B, C), True) for t, w in (
+        (state, "state"), (dstate_out, "dstate_out"), (ddstate, "ddstate"), (out_dstate_out, "out_dstate_out"), (out_state, "out_state")))
+    keep, ws, nws = _scratch(workspace, _lib.diffopt_gscan_workspace(B, T, C, dt, 2), x.device, stream)
+    _check(_lib.diffopt_gscan_bwd_bwd(_ref(cr), _ref(cp), dds0, _ref(cd), ds1, _ref(cg), _ref(cx), ln, s0, B, T, C, dt, _ref(oh), o1,
+                                      _ref(og), _ref(ox), o0, ws, nws, _stream(stream)))
+
+
+def gscan_step(log_gate, x, state, out, stream=None) -> None:
+    """diffopt_gscan_step: one token per sequence, log_gate, x, out [B, C]; state fp32 [B, C] is updated in place."""
+    if _done(_native.gscan_step(log_gate, x, state, out, _stream(stream))):
+        return
+    dt = _type_of(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x: expected a tensor of 2 axes")
+    _current(x, "x")
+    B, C = x.shape
+    ops = []
+    for t, w in ((log_gate, "log_gate"), (x, "x"), (out, "out")):
+        _tensor(t, w, x.dtype, (B, C), x.device)
+        ops.append(_seq(t.unsqueeze(1), w, x, (B, 1, C), w == "out"))
+    _check(_lib.diffopt_gscan_step(_ref(ops[0]), _ref(ops[1]), B, C, dt, _flat(state, "state", x, (B, C)), _ref(ops[2]), _stream(stream)))

@@ -1,0 +1,94 @@
+"""CPU-side checks of the gated recurrence's entry points: refusals come before
+any device call, with their messages, and the workspaces' sizes.  No kernel is
+launched and no pointer is followed."""
+import ctypes
+
+import pytest
+
+F32, BF16 = 0, 1
+f = ctypes.c_void_p(64)  # never followed
+odd = ctypes.c_void_p(66)
+
+
+def _binding():
+    import paper_2211_06934_amd as P
+    return P.diffopt._lib, P.last_error, P.operators._Heads
+
+
+def _refused(rc, word):
+    assert rc == -1 and word in _binding()[1](), (rc, _binding()[1]())
+
+
+def _seq(at):
+    return ctypes.byref(_binding()[2](at, 64, 16, 0))
+
+
+def _call(name, **change):
+    lib = _binding()[0]
+    a = dict(lg=_seq(64), x=_seq(128), dh=_seq(192), r=_seq(256), p=_seq(320), o=_seq(384), o1=_seq(448), o2=_seq(512), lengths=None, s0=None, ds1=None,
+             dds=None, s1=None, s2=None, B=2, T=9, C=8, dtype=F32, ws=None, nws=0)
+    a.update(change)
+    sizes = (a["lengths"], a["s0"], a["B"], a["T"], a["C"], a["dtype"])
+    if name == "fwd":
+        return lib.diffopt_gscan_fwd(a["lg"], a["x"], *sizes, a["o"], a["s1"], a["ws"], a["nws"], None)
+    if name == "bwd":
+        return lib.diffopt_gscan_bwd(a["dh"], a["ds1"], a["lg"], a["x"], *sizes, a["o"], a["o1"], a["s1"], a["ws"], a["nws"], None)
+    if name == "bwd_bwd":
+        return lib.diffopt_gscan_bwd_bwd(a["r"], a["p"], a["dds"], a["dh"], a["ds1"], a["lg"], a["x"], *sizes, a["o"], a["s1"], a["o1"], a["o2"], a["s2"],
+                                         a["ws"], a["nws"], None)
+    return lib.diffopt_gscan_step(a["lg"], a["x"], a["B"], a["C"], a["dtype"], a["s0"], a["o"], None)
+
+
+@pytest.mark.parametrize("name", ["fwd", "bwd", "bwd_bwd"])
+@pytest.mark.parametrize("change,word", [
+    (dict(B=-1), "must be >= 0"), (dict(T=-1), "must be >= 0"), (dict(C=-1), "must be >= 0"), (dict(dtype=4), "element type"), (dict(T=1 << 36), "too many"),
+    (dict(B=1 << 40), "too many"), (dict(C=1 << 40), "too many"), (dict(B=1 << 20, C=1 << 12, T=1), "too many"), (dict(B=1, T=1 << 30), "too many"),
+    (dict(lengths=odd), "lengths"), (dict(s0=odd), "state is not"), (dict(s1=odd), "aligned"), (dict(lg=None), "null log_gate"), (dict(x=None), "null x"),
+    (dict(T=1000), "the workspace has 0 bytes"),
+])
+def test_refusals(name, change, word):
+    _refused(_call(name, **change), word)
+
+
+def test_alignment_of_elements():
+    _refused(_call("fwd", x=_seq(66)), "x is not aligned")
+    _refused(_call("bwd", dh=_seq(65), dtype=BF16), "dh is not aligned")
+
+
+def test_results_lie_apart():
+    _refused(_call("fwd", o=_seq(64)), "h must not be log_gate")
+    _refused(_call("fwd", o=_seq(128)), "h must not be x")
+    _refused(_call("fwd", o=None), "null h")
+    _refused(_call("fwd", s0=f, s1=ctypes.c_void_p(68)), "state_out must lie apart from state")
+    _refused(_call("bwd", o=_seq(192)), "dlog_gate must not be dh")
+    _refused(_call("bwd", o1=_seq(384)), "dx must not be dlog_gate")
+    _refused(_call("bwd", s0=f, s1=f), "dstate must lie apart from state")
+    _refused(_call("bwd", ds1=f, s1=ctypes.c_void_p(64 + 60)), "dstate must lie apart from dstate_out")
+    for k, word in (("o", "out_dh"), ("o1", "out_log_gate"), ("o2", "out_x")):
+        _refused(_call("bwd_bwd", **{k: _seq(256)}), word + " must not be ddlog_gate")
+        _refused(_call("bwd_bwd", **{k: None}), "null " + word)
+    _refused(_call("bwd_bwd", s1=f, s2=f), "out_state must lie apart from out_dstate_out")
+    _refused(_call("bwd_bwd", dds=f, s2=f), "out_state must lie apart from ddstate")
+    _refused(_call("step", s0=ctypes.c_void_p(384)), "state must lie apart")
+    _refused(_call("step", s0=f), "state must lie apart")
+    _refused(_call("step"), "null state")
+    _refused(_call("step", s0=odd), "state is not")
+
+
+def test_calls_with_nothing_to_do():
+    for name in ("fwd", "bwd", "bwd_bwd"):
+        assert _call(name, B=0) == 0 and _call(name, C=0) == 0 and _call(name, T=0) == 0
+    assert _call("bwd", o=None, o1=None) == 0
+    assert _call("step", B=0) == 0
+
+
+def test_workspaces():
+    size = _binding()[0].diffopt_gscan_workspace
+    for order in range(3):
+        assert size(2, 64, 100, F32, order) == 0 and size(0, 1 << 20, 100, F32, order) == 0
+        need = size(2, 1000, 100, F32, order)
+        assert need > 0 and need % 4 == 0
+        name = ("fwd", "bwd", "bwd_bwd")[order]
+        _refused(_call(name, T=1000, C=100, ws=f, nws=need - 1), "the workspace has")
+        _refused(_call(name, T=1000, C=100, ws=odd, nws=need), "not 4-byte aligned")
+    assert size(2, -1, 100, F32, 0) == size(2, 9, 100, 7, 0) == size(2, 9, 100, F32, 3) == size(1 << 40, 9, 100, F32, 0) == -1
