@@ -804,6 +804,92 @@ int diffopt_gscan_step(const diffopt_heads* log_gate, const diffopt_heads* x,
                        int64_t B, int64_t C, int32_t dtype, float* state,
                        const diffopt_heads* out, void* stream);
 
+/* Log probabilities of given tokens.  For each of N rows of logits x, with
+ * l_j = log softmax(x / T)_j and p_j = exp(l_j),
+ *   logprob = l[ids],  entropy = -sum_j p_j l_j
+ *   top_logprob, top_ids  the K largest l and their tokens, falling; the
+ *            lowest id first among equals.  A logit of -inf is no alternative:
+ *            where fewer than K are left, -inf and id -1 stand.
+ *   logits   [N] rows of V elements, row_stride elements apart
+ *   ids      [N] int32 or int64 (by id_bytes), or NULL: no tokens are given,
+ *            logprob is NULL and every row counts.  A negative id is a row of
+ *            padding, which is not read: logprob, entropy and gradients are 0,
+ *            its alternatives (-inf, -1).  An id >= V makes its row's results
+ *            NaN.
+ *   logprob, entropy  fp32 [N]; entropy may be NULL
+ *   stats    fp32 [N][2]: the row's max and its sum of exp((x - max) / T),
+ *            which the backwards take
+ *   top_logprob fp32 [N][K], top_ids [N][K] int32 or int64 (by top_id_bytes);
+ *            0 <= K <= 128, and NULL for K = 0;  N < 2^22
+ *   workspace  diffopt_logprob_workspace() bytes, or NULL if that is 0
+ * Log probabilities and entropies near 0 are right to 2^-22 absolutely.  A row
+ * that is no distribution (a NaN or +inf, or -inf alone) has NaN for its
+ * results and -1 for its top_ids.  Results must not overlap operands or one
+ * another where an entry point does not say that they may.                  */
+int diffopt_logprob_fwd(const void* logits, int64_t row_stride, int64_t N,
+                        int64_t V, int32_t dtype, const void* ids,
+                        int32_t id_bytes, double temperature, float* logprob,
+                        float* entropy, float* stats, float* top_logprob,
+                        void* top_ids, int32_t top_id_bytes, int64_t K,
+                        void* workspace, int64_t workspace_bytes,
+                        void* stream);
+
+/* Its vector-Jacobian product, for cotangents g = dlogprob, h = dentropy [N]
+ * and c = dtop_logprob [N][K] (each may be NULL: 0; K = 0 without the last):
+ *   dlogits_j = 1/T (g [j = ids] + sum_k c_k [j = top_ids_k]
+ *                    - p_j (g + sum_k c_k + h (l_j + entropy)))
+ * entropy goes with dentropy and top_ids with dtop_logprob, as the forward
+ * wrote them; entries with id -1 take no part.  dlogits may be logits, rows as
+ * far apart.                                                                */
+int diffopt_logprob_bwd(const float* dlogprob, const float* dentropy,
+                        const float* entropy, const float* dtop_logprob,
+                        const void* top_ids, int32_t top_id_bytes, int64_t K,
+                        const void* logits, int64_t row_stride, int64_t N,
+                        int64_t V, int32_t dtype, const void* ids,
+                        int32_t id_bytes, double temperature,
+                        const float* stats, void* dlogits, int64_t drow_stride,
+                        void* stream);
+
+/* Both at once, for a caller that knows the cotangents before the results
+ * (the weights of a mean): the logits are read from memory once.  dentropy
+ * and entropy may be NULL; dlogits must not be logits.                      */
+int diffopt_logprob_fwd_bwd(const float* dlogprob, const float* dentropy,
+                            const void* logits, int64_t row_stride, int64_t N,
+                            int64_t V, int32_t dtype, const void* ids,
+                            int32_t id_bytes, double temperature,
+                            float* logprob, float* entropy, float* stats,
+                            void* dlogits, int64_t drow_stride,
+                            void* workspace, int64_t workspace_bytes,
+                            void* stream);
+
+/* The vector-Jacobian product of the backward, for the cotangent ddlogits = a
+ * of dlogits (element type, rows ddrow_stride apart).  With [.] the average
+ * under p, G = g + sum_k c_k and k = [(a - [a]) (l + entropy)]:
+ *   out_dlogprob = (a[ids] - [a]) / T,  out_dtop_logprob_k = (a[top_ids_k] - [a]) / T
+ *   out_dentropy = -k / T
+ *   out_logits_i = -p_i/T^2 (G (a_i - [a])
+ *                   + h ((a_i - [a]) (l_i + entropy + 1) - k))
+ * out_dlogprob, out_dentropy [N] and out_dtop_logprob [N][K] may be NULL;
+ * out_dentropy needs entropy.  The choice of the alternatives is a constant.
+ * out_logits must be neither logits nor ddlogits.                           */
+int diffopt_logprob_bwd_bwd(const void* ddlogits, int64_t ddrow_stride,
+                            const float* dlogprob, const float* dentropy,
+                            const float* entropy, const float* dtop_logprob,
+                            const void* top_ids, int32_t top_id_bytes,
+                            int64_t K, const void* logits, int64_t row_stride,
+                            int64_t N, int64_t V, int32_t dtype,
+                            const void* ids, int32_t id_bytes,
+                            double temperature, const float* stats,
+                            float* out_dlogprob, float* out_dentropy,
+                            float* out_dtop_logprob, void* out_logits,
+                            int64_t out_row_stride, void* workspace,
+                            int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that logprob_fwd needs for K alternatives, and for K = 0
+ * logprob_fwd_bwd and _bwd_bwd; -1 for sizes they refuse.                   */
+int64_t diffopt_logprob_workspace(int64_t N, int64_t V, int32_t dtype,
+                                  int64_t K);
+
 #ifdef __cplusplus
 }
 #endif

@@ -7,7 +7,7 @@ of the step that works on the leaves without flattening, fused differentiable
 SGD-momentum and RMSProp (flat and leaf-direct), the zero-order (ES)
 estimator, and the operators of a language model that an inner loop adapts
 (linear attention, a gated recurrence, query and key norms with rotation,
-distillation).
+distillation, log probabilities of tokens).
 ``diffopt`` is its thin Python binding (same entry points; ``operators`` for
 the language model's), ``tree`` the host-side container walk, ``autograd`` the
 torch.autograd.Functions and meta-optimizers over the fused steps and
@@ -27,14 +27,15 @@ from . import operators
 from .operators import (linattn_fwd, linattn_bwd, linattn_step, linattn_workspace,
                         qknorm_rope_fwd, qknorm_rope_bwd, qknorm_rope_bwd_bwd, qknorm_rope_workspace,
                         distill_fwd, distill_bwd, distill_fwd_bwd, distill_bwd_bwd, distill_workspace,
-                        gscan_fwd, gscan_bwd, gscan_bwd_bwd, gscan_step, gscan_workspace)
+                        gscan_fwd, gscan_bwd, gscan_bwd_bwd, gscan_step, gscan_workspace,
+                        logprob_fwd, logprob_bwd, logprob_fwd_bwd, logprob_bwd_bwd, logprob_workspace)
 from . import tree
 from . import autograd
 from .autograd import (AdamFn, AdamHyper, AdamState, AdamTreeFn, FlatAdam, MetaAdam, MetaRMSProp, MetaSGD,
                        RMSPropHyper, RMSPropTreeFn, SGDHyper, SGDTreeFn, ZeroOrderFn, es_gradient)
 from . import language
-from .language import (distillation_loss, gated_scan, gated_scan_step, linear_attention, linear_attention_step,
-                       qknorm_rope)
+from .language import (TokenLogprobs, distillation_loss, gated_scan, gated_scan_step, linear_attention,
+                       linear_attention_step, qknorm_rope, token_logprobs)
 
 __all__ = [
     "diffopt", "operators", "tree", "autograd", "language", "DiffoptError", "SegTable", "adam_bwd", "adam_fwd",
@@ -51,4 +52,5 @@ __all__ = [
     "distill_fwd", "distill_bwd", "distill_fwd_bwd", "distill_bwd_bwd", "distill_workspace",
     "linear_attention", "linear_attention_step", "qknorm_rope", "distillation_loss",
     "gscan_fwd", "gscan_bwd", "gscan_bwd_bwd", "gscan_step", "gscan_workspace", "gated_scan", "gated_scan_step",
+    "logprob_fwd", "logprob_bwd", "logprob_fwd_bwd", "logprob_bwd_bwd", "logprob_workspace", "token_logprobs", "TokenLogprobs",
 ]

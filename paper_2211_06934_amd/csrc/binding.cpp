@@ -729,6 +729,139 @@ PyObject* distill_bwd_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   });
 }
 
+// What the calls of logprob share.
+struct Logprob {
+  int64_t N, V, stride, K = 0;
+  const void *logits, *ids = nullptr;
+  int32_t id_bytes = 0, top_bytes = 0;
+
+  Logprob(Call& c, PyObject* x, PyObject* i) {
+    if (c.like->dim() != 2) throw Other{};
+    c.current();
+    N = c.like->size(0);
+    V = c.like->size(1);
+    logits = rows(c, x, false, &stride);
+    ids = tokens(c, i, {N}, &id_bytes);
+  }
+  void* rows(Call& c, PyObject* o, bool result, int64_t* step) const {
+    const at::Tensor& t = tensor_of(o);
+    c.check(t, c.like->scalar_type(), {N, V});
+    if (V > 1 && t.stride(1) != 1 && t.numel() > 0) throw Other{};
+    if (result) Call::apart(t);
+    *step = t.stride(0);
+    return t.data_ptr();
+  }
+  static void* tokens(Call& c, PyObject* o, at::IntArrayRef shape, int32_t* bytes) {
+    const at::Tensor* t = optional_tensor(o);
+    if (!t) return nullptr;
+    if (t->scalar_type() != at::kInt && t->scalar_type() != at::kLong) throw Other{};
+    *bytes = static_cast<int32_t>(t->element_size());
+    return c.flat(o, t->scalar_type(), shape);
+  }
+  // a row's alternatives: values and ids, or neither
+  struct Top {
+    float* values = nullptr;
+    void* ids = nullptr;
+  };
+  Top top(Call& c, PyObject* values, PyObject* i) {
+    Top t;
+    if (const at::Tensor* v = optional_tensor(values)) {
+      if (v->dim() != 2 || i == Py_None) throw Other{};
+      K = v->size(1);
+      t.values = c.floats(values, {N, K});
+      t.ids = tokens(c, i, {N, K}, &top_bytes);
+    }
+    return t;
+  }
+};
+
+// (logits, ids, logprob, stats, entropy, top_logprob, top_ids, temperature, workspace, stream)
+PyObject* logprob_fwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return operator_call(args, nargs, 10, 0, [](Call& c, int32_t type) {
+    PyObject *x = c.next(), *i = c.next();
+    Logprob d(c, x, i);
+    float *lp = c.floats(c.next(), {d.N}, true), *stats = c.floats(c.next(), {d.N, 2}), *ent = c.floats(c.next(), {d.N}, true);
+    PyObject *tv = c.next(), *ti = c.next();
+    if (tv == Py_None && ti != Py_None) throw Other{};
+    const Logprob::Top t = d.top(c, tv, ti);
+    const double T = c.number(c.next());
+    const Scratch w(c.next(), diffopt_logprob_workspace(d.N, d.V, type, d.K), *c.like);
+    void* stream = c.stream(c.next());
+    return unlocked([&] {
+      return diffopt_logprob_fwd(d.logits, d.stride, d.N, d.V, type, d.ids, d.id_bytes, T, lp, ent, stats, t.values, t.ids, d.top_bytes, d.K, w.p,
+                                 w.bytes, stream);
+    });
+  });
+}
+
+// (logits, ids, stats, dlogits, dlogprob, dentropy, entropy, dtop_logprob, top_ids, temperature, stream)
+PyObject* logprob_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return operator_call(args, nargs, 11, 0, [](Call& c, int32_t type) {
+    PyObject *x = c.next(), *i = c.next();
+    Logprob d(c, x, i);
+    const float* stats = c.floats(c.next(), {d.N, 2});
+    int64_t dstride;
+    void* dx = d.rows(c, c.next(), true, &dstride);
+    const float *g = c.floats(c.next(), {d.N}, true), *h = c.floats(c.next(), {d.N}, true), *ent = c.floats(c.next(), {d.N}, true);
+    PyObject *tv = c.next(), *ti = c.next();
+    const Logprob::Top t = d.top(c, tv, ti);
+    const double T = c.number(c.next());
+    void* stream = c.stream(c.next());
+    return unlocked([&] {
+      return diffopt_logprob_bwd(g, h, ent, t.values, t.ids, d.top_bytes, d.K, d.logits, d.stride, d.N, d.V, type, d.ids, d.id_bytes, T, stats, dx,
+                                 dstride, stream);
+    });
+  });
+}
+
+// (dlogprob, logits, ids, logprob, stats, dlogits, dentropy, entropy, temperature, workspace, stream)
+PyObject* logprob_fwd_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return operator_call(args, nargs, 11, 1, [](Call& c, int32_t type) {
+    PyObject *og = c.next(), *x = c.next(), *i = c.next();
+    Logprob d(c, x, i);
+    const float* g = c.floats(og, {d.N});
+    float *lp = c.floats(c.next(), {d.N}), *stats = c.floats(c.next(), {d.N, 2});
+    int64_t dstride;
+    void* dx = d.rows(c, c.next(), true, &dstride);
+    const float* h = c.floats(c.next(), {d.N}, true);
+    float* ent = c.floats(c.next(), {d.N}, true);
+    const double T = c.number(c.next());
+    const Scratch w(c.next(), diffopt_logprob_workspace(d.N, d.V, type, 0), *c.like);
+    void* stream = c.stream(c.next());
+    return unlocked([&] {
+      return diffopt_logprob_fwd_bwd(g, h, d.logits, d.stride, d.N, d.V, type, d.ids, d.id_bytes, T, lp, ent, stats, dx, dstride, w.p, w.bytes,
+                                     stream);
+    });
+  });
+}
+
+// (ddlogits, logits, ids, stats, out_logits, dlogprob, dentropy, entropy, dtop_logprob, top_ids, out_dlogprob, out_dentropy,
+//  out_dtop_logprob, temperature, workspace, stream)
+PyObject* logprob_bwd_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return operator_call(args, nargs, 16, 1, [](Call& c, int32_t type) {
+    PyObject *oa = c.next(), *x = c.next(), *i = c.next();
+    Logprob d(c, x, i);
+    int64_t astride, ostride;
+    const void* a = d.rows(c, oa, false, &astride);
+    const float* stats = c.floats(c.next(), {d.N, 2});
+    void* out = d.rows(c, c.next(), true, &ostride);
+    const float *g = c.floats(c.next(), {d.N}, true), *h = c.floats(c.next(), {d.N}, true), *ent = c.floats(c.next(), {d.N}, true);
+    PyObject *tv = c.next(), *ti = c.next();
+    const Logprob::Top t = d.top(c, tv, ti);
+    float *out_g = c.floats(c.next(), {d.N}, true), *out_h = c.floats(c.next(), {d.N}, true);
+    PyObject* ot = c.next();
+    if (ot != Py_None && tv == Py_None) throw Other{};
+    float* out_t = c.floats(ot, {d.N, d.K}, true);
+    const double T = c.number(c.next());
+    const Scratch w(c.next(), diffopt_logprob_workspace(d.N, d.V, type, 0), *c.like);
+    void* stream = c.stream(c.next());
+    return unlocked([&] {
+      return diffopt_logprob_bwd_bwd(a, astride, g, h, ent, t.values, t.ids, d.top_bytes, d.K, d.logits, d.stride, d.N, d.V, type, d.ids, d.id_bytes, T,
+                                     stats, out_g, out_h, out_t, out, ostride, w.p, w.bytes, stream);
+    });
+  });
+}
+
 // What the calls of gscan share: the sizes, and the operands' shape.
 struct Gscan {
   int64_t B, T, C;
@@ -850,6 +983,10 @@ PyMethodDef methods[] = {
     OPERATOR(distill_bwd),
     OPERATOR(distill_fwd_bwd),
     OPERATOR(distill_bwd_bwd),
+    OPERATOR(logprob_fwd),
+    OPERATOR(logprob_bwd),
+    OPERATOR(logprob_fwd_bwd),
+    OPERATOR(logprob_bwd_bwd),
     OPERATOR(gscan_fwd),
     OPERATOR(gscan_bwd),
     OPERATOR(gscan_bwd_bwd),

@@ -8,9 +8,9 @@ so each Function here has a backward that is a Function itself:
   and bilinear in (k, v), its gradients are the same sum on permuted operands,
   and the derivative of a gradient is made of the operator's own calls.  Any
   order of differentiation works.
-* ``qknorm_rope``, ``gated_scan`` and ``distillation_loss``: differentiable
-  twice, by kernels for the backward and for the backward's backward.  Asking
-  for a third order raises an error.
+* ``qknorm_rope``, ``gated_scan``, ``distillation_loss`` and
+  ``token_logprobs``: differentiable twice, by kernels for the backward and for
+  the backward's backward.  Asking for a third order raises an error.
 
 Tensors are brought into a shape that the kernels read (whole heads, whole
 rows) before a Function is applied, so that what it saves are its inputs.
@@ -20,7 +20,7 @@ for generation: no graph, the state updated in place.
 """
 from __future__ import annotations
 
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 from torch.autograd.function import once_differentiable
@@ -352,3 +352,75 @@ def distillation_loss(logits, ids, teacher, temperature: float = 1.0) -> torch.T
     (int32 or int64): T^2 KL(softmax(teacher / T) || softmax(logits / T)) over the row's entries.  A negative id or a
     teacher logit of -inf is no entry; a row without entries has loss 0.  Differentiable twice in logits and teacher."""
     return DistillationFn.apply(_dense(logits), _whole(teacher), _whole(ids), float(temperature))
+
+
+# ---- log probabilities ------------------------------------------------------
+
+
+class TokenLogprobs(NamedTuple):
+    """What token_logprobs gives; what was not asked for is None."""
+    logprob: Optional[torch.Tensor]
+    entropy: Optional[torch.Tensor]
+    top_logprob: Optional[torch.Tensor]
+    top_ids: Optional[torch.Tensor]
+
+
+class TokenLogprobsFn(torch.autograd.Function):
+    """logits -> (logprob, entropy, top_logprob, top_ids), those that are asked for."""
+
+    @staticmethod
+    def forward(ctx, logits, ids, temperature: float, entropy: bool, top: int):
+        N = logits.shape[0]
+        new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)
+        lp, ent, stats = None if ids is None else new(N), new(N) if entropy else None, new(N, 2)
+        tops, top_ids = (new(N, top), new(N, top, dtype=torch.int64)) if top > 0 else (None, None)
+        _o.logprob_fwd(logits, ids, lp, stats, ent, tops, top_ids, temperature)
+        ctx.save_for_backward(logits, ids, stats, top_ids, ent)
+        ctx.temperature = temperature
+        ctx.set_materialize_grads(False)
+        if top_ids is not None:
+            ctx.mark_non_differentiable(top_ids)
+        return lp, ent, tops, top_ids
+
+    @staticmethod
+    def backward(ctx, g, h, c, _):
+        logits, ids, stats, top_ids, ent = ctx.saved_tensors
+        if g is None and h is None and c is None:
+            return (None,) * 5
+        # the entropy enters as a number: what depends on it is in the gradient's own formula
+        ent = None if ent is None else ent.detach()
+        return TokenLogprobsGradFn.apply(_whole(g), _whole(h), _whole(c), logits, ids, stats, ent, top_ids, ctx.temperature), None, None, None, None
+
+
+class TokenLogprobsGradFn(torch.autograd.Function):
+    """(dlogprob, dentropy, dtop_logprob, logits) -> dlogits."""
+
+    @staticmethod
+    def forward(ctx, g, h, c, logits, ids, stats, ent, top_ids, temperature: float):
+        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        top_ids = None if c is None else top_ids
+        ent = None if h is None else ent
+        _o.logprob_bwd(logits, ids, stats, dlogits, g, h, ent, c, top_ids, temperature)
+        ctx.save_for_backward(g, h, c, logits, ids, stats, ent, top_ids)
+        ctx.temperature = temperature
+        return dlogits
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, a):
+        g, h, c, logits, ids, stats, ent, top_ids = ctx.saved_tensors
+        og, oh, oc = (None if x is None else torch.empty_like(x) for x in (g, h, c))
+        ol = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        _o.logprob_bwd_bwd(_dense(a), logits, ids, stats, ol, g, h, ent, c, top_ids, og, oh, oc, ctx.temperature)
+        return og, oh, oc, ol, None, None, None, None, None
+
+
+def token_logprobs(logits, ids=None, temperature: float = 1.0, entropy: bool = False, top: int = 0) -> TokenLogprobs:
+    """Log probabilities [N] of the tokens ids [N] (int32 or int64) under softmax(logits / temperature) of logits [N, V]
+    (fp32 or bf16); with entropy that of each row, with top the log probabilities and ids of the row's likeliest tokens, both
+    [N, top], falling, the lowest id first among equals (-inf and -1 where the logits leave fewer).  A negative id is a row
+    of padding: zeros.  Without ids (generation) logprob is None.  The alternatives are ids and a teacher's logits as
+    distillation_loss takes them.  Differentiable twice in logits."""
+    if int(top) < 0:
+        raise ValueError("token_logprobs: top must be >= 0")
+    return TokenLogprobs(*TokenLogprobsFn.apply(_dense(logits), _whole(ids), float(temperature), bool(entropy), int(top)))

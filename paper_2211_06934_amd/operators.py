@@ -33,6 +33,8 @@ class _Heads(ctypes.Structure):
 _hp = ctypes.POINTER(_Heads)
 _QK = [_vp, _vp, _vp, _vp, _i64, _vp, _i32, _i64, _i64, _i64, _i64, _i64, _i64, _i64, _i32, _i32, _f64]
 _ROWS = [_vp, _i64, _i64, _i64, _i32, _vp, _i32, _vp, _i64, _f64]
+_NAMED = [_vp, _vp, _vp, _vp, _vp, _i32, _i64]  # cotangents of logprob's results, top ids and their count
+_SCORED = [_vp, _i64, _i64, _i64, _i32, _vp, _i32, _f64]
 _SIGNATURES = {
     "diffopt_linattn_fwd": (_i32, [_hp, _hp, _hp, _vp, _vp, _vp, *[_i64] * 6, _i32, _f64, _hp, _vp, _vp, _i64, _vp]),
     "diffopt_linattn_bwd": (_i32, [_hp, _vp, _hp, _hp, _hp, _vp, _vp, _vp, *[_i64] * 6, _i32, _f64, _hp, _hp, _hp, _vp, _vp, _i64,
@@ -49,6 +51,11 @@ _SIGNATURES = {
     "diffopt_distill_fwd_bwd": (_i32, [_vp, *_ROWS, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _vp]),
     "diffopt_distill_bwd_bwd": (_i32, [_vp, _i64, _vp, _vp, *_ROWS, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _vp]),
     "diffopt_distill_workspace": (_i64, [_i64, _i64, _i32, _i64]),
+    "diffopt_logprob_fwd": (_i32, [_vp, _i64, _i64, _i64, _i32, _vp, _i32, _f64, _vp, _vp, _vp, _vp, _vp, _i32, _i64, _vp, _i64, _vp]),
+    "diffopt_logprob_bwd": (_i32, [*_NAMED, *_SCORED, _vp, _vp, _i64, _vp]),
+    "diffopt_logprob_fwd_bwd": (_i32, [_vp, _vp, *_SCORED, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "diffopt_logprob_bwd_bwd": (_i32, [_vp, _i64, *_NAMED, *_SCORED, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "diffopt_logprob_workspace": (_i64, [_i64, _i64, _i32, _i64]),
     "diffopt_gscan_fwd": (_i32, [_hp, _hp, _vp, _vp, _i64, _i64, _i64, _i32, _hp, _vp, _vp, _i64, _vp]),
     "diffopt_gscan_bwd": (_i32, [_hp, _vp, _hp, _hp, _vp, _vp, _i64, _i64, _i64, _i32, _hp, _hp, _vp, _vp, _i64, _vp]),
     "diffopt_gscan_bwd_bwd": (_i32, [_hp, _hp, _vp, _hp, _vp, _hp, _hp, _vp, _vp, _i64, _i64, _i64, _i32, _hp, _vp, _hp, _hp, _vp, _vp,
@@ -423,6 +430,121 @@ def distill_bwd_bwd(ddlogits, ddteacher, dloss, logits, ids, teacher, stats, out
     _check(_lib.diffopt_distill_bwd_bwd(pa, astride, _flat(ddteacher, "ddteacher", logits, (N, K), True), pg, *args, ps,
                                         _flat(out_dloss, "out_dloss", logits, (N,), True), po, ostride,
                                         _flat(out_teacher, "out_teacher", logits, (N, K), True), ws, nws, _stream(stream)))
+
+
+# ---- log probabilities ------------------------------------------------------
+
+
+def logprob_workspace(N: int, V: int, K: int = 0, dtype=torch.float32) -> int:
+    """diffopt_logprob_workspace: bytes that logprob_fwd needs for K alternatives, with K = 0 logprob_fwd_bwd and
+    logprob_bwd_bwd."""
+    n = int(_lib.diffopt_logprob_workspace(N, V, _DTYPES[dtype], K))
+    if n < 0:
+        raise ValueError("logprob: sizes that the operator refuses")
+    return n
+
+
+def _scored(logits, ids, temperature):
+    """(N, V, element type, the C arguments that the calls share)."""
+    dt = _type_of(logits, "logits")
+    if logits.dim() != 2:
+        raise ValueError("logits: expected a tensor of 2 axes")
+    _current(logits, "logits")
+    N, V = logits.shape
+    p, stride = _rows(logits, "logits", logits, (N, V))
+    at, size = _ids(ids, "ids", logits, (N,))
+    return N, V, dt, [p, stride, N, V, dt, at, size, float(temperature)]
+
+
+def _ids(x, what, like, shape):
+    """(address, bytes of one) of int32 or int64 ids; None has none."""
+    if x is None:
+        return None, 0
+    if not isinstance(x, torch.Tensor) or x.dtype not in (torch.int32, torch.int64):
+        raise ValueError("%s: expected an int32 or int64 tensor" % what)
+    return _flat(x, what, like, shape, dtype=x.dtype), x.element_size()
+
+
+def _top(values, what, top_ids, like, N):
+    """(K, values' address, ids' address, bytes of an id) of a row's alternatives, or none."""
+    if values is None:
+        return 0, None, None, 0
+    if not isinstance(values, torch.Tensor) or values.dim() != 2:
+        raise ValueError("%s: expected a tensor of 2 axes" % what)
+    K = values.shape[1]
+    if top_ids is None:
+        raise ValueError("top_ids: wanted with %s" % what)
+    return (K, _flat(values, what, like, (N, K)), *_ids(top_ids, "top_ids", like, (N, K)))
+
+
+def logprob_fwd(logits, ids, logprob, stats, entropy=None, top_logprob=None, top_ids=None, temperature: float = 1.0, workspace=None,
+                stream=None) -> None:
+    """diffopt_logprob_fwd: logprob [N] of the tokens ids [N] under softmax(logits / temperature) of logits [N, V], the
+    entropy [N] of each row and its K likeliest tokens, top_logprob and top_ids [N, K] (any of these three None); stats
+    [N, 2] is what the backwards take.  ids and logprob may both be None."""
+    if _here(workspace, stream) and _done(_native.logprob_fwd(
+            logits, ids, logprob, stats, entropy, top_logprob, top_ids, temperature, workspace, _stream(stream))):
+        return
+    N, V, dt, args = _scored(logits, ids, temperature)
+    if top_logprob is None and top_ids is not None:
+        raise ValueError("top_logprob: wanted with top_ids")
+    K, pt, pi, size = _top(top_logprob, "top_logprob", top_ids, logits, N)
+    pl, pe, ps = _flat(logprob, "logprob", logits, (N,), True), _flat(entropy, "entropy", logits, (N,), True), _flat(stats, "stats", logits, (N, 2))
+    keep, ws, nws = _scratch(workspace, _lib.diffopt_logprob_workspace(N, V, dt, K), logits.device, stream)
+    _check(_lib.diffopt_logprob_fwd(*args, pl, pe, ps, pt, pi, size, K, ws, nws, _stream(stream)))
+
+
+def logprob_bwd(logits, ids, stats, dlogits, dlogprob=None, dentropy=None, entropy=None, dtop_logprob=None, top_ids=None,
+                temperature: float = 1.0, stream=None) -> None:
+    """diffopt_logprob_bwd: gradient of logprob_fwd for cotangents of its results (each may be None: zero); entropy and
+    top_ids as logprob_fwd wrote them go with dentropy and dtop_logprob.  dlogits may be logits."""
+    if _done(_native.logprob_bwd(logits, ids, stats, dlogits, dlogprob, dentropy, entropy, dtop_logprob, top_ids, temperature,
+                                 _stream(stream))):
+        return
+    N, V, dt, args = _scored(logits, ids, temperature)
+    K, pt, pi, size = _top(dtop_logprob, "dtop_logprob", top_ids, logits, N)
+    pg, ph, pe = (_flat(x, w, logits, (N,), True) for x, w in ((dlogprob, "dlogprob"), (dentropy, "dentropy"), (entropy, "entropy")))
+    ps = _flat(stats, "stats", logits, (N, 2))
+    pd, dstride = _rows(dlogits, "dlogits", logits, (N, V), True)
+    _check(_lib.diffopt_logprob_bwd(pg, ph, pe, pt, pi, size, K, *args, ps, pd, dstride, _stream(stream)))
+
+
+def logprob_fwd_bwd(dlogprob, logits, ids, logprob, stats, dlogits, dentropy=None, entropy=None, temperature: float = 1.0,
+                    workspace=None, stream=None) -> None:
+    """diffopt_logprob_fwd_bwd: the results and the gradient for cotangents known beforehand, the logits read once;
+    dentropy and entropy may be None."""
+    if _here(workspace, stream) and _done(_native.logprob_fwd_bwd(
+            dlogprob, logits, ids, logprob, stats, dlogits, dentropy, entropy, temperature, workspace, _stream(stream))):
+        return
+    N, V, dt, args = _scored(logits, ids, temperature)
+    pg, ph = _flat(dlogprob, "dlogprob", logits, (N,)), _flat(dentropy, "dentropy", logits, (N,), True)
+    pl, pe, ps = _flat(logprob, "logprob", logits, (N,)), _flat(entropy, "entropy", logits, (N,), True), _flat(stats, "stats", logits, (N, 2))
+    pd, dstride = _rows(dlogits, "dlogits", logits, (N, V), True)
+    keep, ws, nws = _scratch(workspace, _lib.diffopt_logprob_workspace(N, V, dt, 0), logits.device, stream)
+    _check(_lib.diffopt_logprob_fwd_bwd(pg, ph, *args, pl, pe, ps, pd, dstride, ws, nws, _stream(stream)))
+
+
+def logprob_bwd_bwd(ddlogits, logits, ids, stats, out_logits, dlogprob=None, dentropy=None, entropy=None, dtop_logprob=None,
+                    top_ids=None, out_dlogprob=None, out_dentropy=None, out_dtop_logprob=None, temperature: float = 1.0,
+                    workspace=None, stream=None) -> None:
+    """diffopt_logprob_bwd_bwd: gradients of logprob_bwd for the cotangent ddlogits of dlogits; out_dlogprob, out_dentropy
+    (which needs entropy) and out_dtop_logprob may be None."""
+    if _here(workspace, stream) and _done(_native.logprob_bwd_bwd(
+            ddlogits, logits, ids, stats, out_logits, dlogprob, dentropy, entropy, dtop_logprob, top_ids, out_dlogprob, out_dentropy,
+            out_dtop_logprob, temperature, workspace, _stream(stream))):
+        return
+    N, V, dt, args = _scored(logits, ids, temperature)
+    K, pt, pi, size = _top(dtop_logprob, "dtop_logprob", top_ids, logits, N)
+    pa, astride = _rows(ddlogits, "ddlogits", logits, (N, V))
+    po, ostride = _rows(out_logits, "out_logits", logits, (N, V), True)
+    pg, ph, pe, og, oh = (_flat(x, w, logits, (N,), True) for x, w in ((dlogprob, "dlogprob"), (dentropy, "dentropy"), (entropy, "entropy"),
+                                                                       (out_dlogprob, "out_dlogprob"), (out_dentropy, "out_dentropy")))
+    if out_dtop_logprob is not None and dtop_logprob is None:
+        raise ValueError("out_dtop_logprob: wanted without dtop_logprob")
+    ot, ps = _flat(out_dtop_logprob, "out_dtop_logprob", logits, (N, K), True), _flat(stats, "stats", logits, (N, 2))
+    keep, ws, nws = _scratch(workspace, _lib.diffopt_logprob_workspace(N, V, dt, 0), logits.device, stream)
+    _check(_lib.diffopt_logprob_bwd_bwd(pa, astride, pg, ph, pe, pt, pi, size, K, *args, ps, og, oh, ot, po, ostride, ws, nws,
+                                        _stream(stream)))
 
 
 # ---- gated recurrence -------------------------------------------------------
