@@ -416,6 +416,53 @@ int diffopt_rmsprop_bwd_tree(const diffopt_segtable* table,
                              const uint64_t* dmom_in, void* stream);
 
 /* -------------------------------------------------------------------------
+ * The global norm of a gradient and clipping to it (what an inner step does to
+ * its gradients before the update), over one flat buffer of n elements or over
+ * the leaves of a tree:
+ *   norm = sqrt(sum grad^2),  c = min(1, max_norm / (norm + eps)),  out = c grad
+ * The sum is fp64 in an order that the sizes alone decide; c is rounded once.
+ *   stats    fp32 [2], written: the norm and c, which the backward takes
+ *   out      may be grad; NULL: the norm and c alone
+ *   max_norm >= 0 (infinity: never clipped), eps >= 0
+ *   workspace  device scratch of diffopt_clip_norm_workspace(_tree) bytes (its
+ *            contents do not matter, 8-byte aligned); NULL if that is 0
+ * A norm that is not finite is handed on as it is: with an infinite element c
+ * is 0 and that element's result NaN, a NaN makes every result NaN.
+ * n == 0 writes stats only; n < 2^36.  Tree forms take DEVICE arrays of leaf addresses in
+ * table order, as the leaf-direct steps do; a leaf of out is the same leaf of
+ * grad or lies apart from every leaf of it.                                 */
+int diffopt_clip_norm_fwd(const float* grad, int64_t n, double max_norm,
+                          double eps, float* out, float* stats,
+                          void* workspace, int64_t workspace_bytes,
+                          void* stream);
+int diffopt_clip_norm_fwd_tree(const diffopt_segtable* table,
+                               const uint64_t* grad, double max_norm,
+                               double eps, const uint64_t* out, float* stats,
+                               void* workspace, int64_t workspace_bytes,
+                               void* stream);
+
+/* Their vector-Jacobian product, for cotangents dout and dnorm (a DEVICE fp32
+ * scalar; either NULL: 0):
+ *   dgrad = c dout + grad (dnorm - [c < 1] c <dout, grad> / (norm + eps)) / norm
+ * and 0 in place of the second term for a norm of 0.  dgrad may be dout or
+ * grad.                                                                     */
+int diffopt_clip_norm_bwd(const float* dout, const float* dnorm,
+                          const float* grad, const float* stats, int64_t n,
+                          double eps, float* dgrad, void* workspace,
+                          int64_t workspace_bytes, void* stream);
+int diffopt_clip_norm_bwd_tree(const diffopt_segtable* table,
+                               const uint64_t* dout, const float* dnorm,
+                               const uint64_t* grad, const float* stats,
+                               double eps, const uint64_t* dgrad,
+                               void* workspace, int64_t workspace_bytes,
+                               void* stream);
+
+/* Bytes of workspace those calls need (0: none); -1 for a size that they
+ * refuse, or a NULL table.                                                 */
+int64_t diffopt_clip_norm_workspace(int64_t n);
+int64_t diffopt_clip_norm_workspace_tree(const diffopt_segtable* table);
+
+/* -------------------------------------------------------------------------
  * Zero-order (evolution-strategies) gradient estimation (Sec. 2.2
  * "Zero-order Differentiation"): grad f_s(theta) = (1/s) E_z[f(theta + s z) z]
  * for the Gaussian smoothing f_s(theta) = E_z[f(theta + s z)], z ~ N(0, I),

@@ -134,13 +134,70 @@ class AdamTreeFn(torch.autograd.Function):
         return (None, None, None, *dP, *dg, *dm, *dv)
 
 
+class ClipNormTreeFn(torch.autograd.Function):
+    """Gradients clipped to their global norm, leaf-direct, differentiable.
+
+    apply(table, max_norm, eps, *leaves) with leaves = g_1..g_S (fp32) returns
+    c g_1..c g_S and the norm, c = min(1, max_norm / (norm + eps))."""
+
+    @staticmethod
+    def forward(ctx, table, max_norm: float, eps: float, *leaves):
+        g = [x.contiguous() for x in leaves]
+        dev = g[0].device
+        out = [torch.empty_like(x) for x in g]
+        stats = torch.empty(2, device=dev)
+        a = _ptrs((g, out), dev)
+        _d.clip_norm_fwd_tree(table, a[0], max_norm, a[1], stats, eps)
+        ctx.save_for_backward(stats, *g)
+        ctx.table, ctx.eps = table, eps
+        ctx.set_materialize_grads(False)
+        return (*out, stats[0].clone())
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, *cots):
+        stats, *g = ctx.saved_tensors
+        dev = stats.device
+        dout, dnorm = cots[:-1], cots[-1]
+        if all(c is None for c in dout):
+            dout = None
+            if dnorm is None:
+                return (None,) * (3 + len(g))
+        else:
+            dout = [torch.zeros_like(x) if c is None else c.contiguous() for c, x in zip(dout, g)]
+        dg = [torch.empty_like(x) for x in g]
+        a = _ptrs((dout, g, dg), dev)
+        _d.clip_norm_bwd_tree(ctx.table, a[0], dnorm, a[1], stats, a[2], ctx.eps)
+        return (None, None, None, *dg)
+
+
+def clip_grad_norm(grads, max_norm: float, eps: float = 1e-6):
+    """(clipped, norm): a tree of fp32 gradients (as tree.tree_leaves takes them) scaled by min(1, max_norm / (norm + eps)),
+    norm the square root of the sum of all elements' squares.  Differentiable once, as the fused steps are."""
+    from .tree import _table_of, tree_build, tree_leaves
+    leaves, td = tree_leaves(grads)
+    if not leaves:
+        raise ValueError("tree has no tensor leaves")
+    dev = leaves[0].device
+    for x in leaves:
+        if x.dtype != torch.float32 or x.device != dev:
+            raise ValueError("clip_grad_norm takes fp32 gradients on one device")
+        if not x.is_cuda:
+            raise ValueError("clip_grad_norm: gradients must live in device memory")
+    table = _table_of(tuple(tuple(x.shape) for x in leaves), torch.float32, dev)
+    *out, norm = ClipNormTreeFn.apply(table, float(max_norm), float(eps), *leaves)
+    return tree_build(td, out), norm
+
+
 class _MetaOptimizer:
     """Module-parameter plumbing shared by the object-oriented optimizers
     (Listing 1, OOP API): the trainable parameters in registration order, one
     cached segment table for their shapes, and the installation of updated,
-    non-leaf tensors as the module's parameters."""
+    non-leaf tensors as the module's parameters.  With max_norm the gradients
+    are clipped to that global norm before the update, and the meta-gradient
+    goes through the clipping too; grad_norm is the last step's norm."""
 
-    def __init__(self, module: torch.nn.Module):
+    def __init__(self, module: torch.nn.Module, max_norm=None):
         from .tree import segment_table
         self.module = module
         self.names = [n for n, p in module.named_parameters() if p.requires_grad]
@@ -150,6 +207,9 @@ class _MetaOptimizer:
         if any(p.dtype != torch.float32 or p.device != params[0].device for p in params):
             raise ValueError("the fused optimizers take fp32 parameters on one device")
         self.table = segment_table([tuple(p.shape) for p in params], params[0].dtype, params[0].device)
+        if max_norm is not None and not max_norm >= 0:
+            raise ValueError("max_norm must be >= 0")
+        self.max_norm, self.grad_norm = max_norm, None
 
     def _owner(self, name):
         mod = self.module
@@ -168,6 +228,15 @@ class _MetaOptimizer:
 
     def params(self):
         return [self._get(n) for n in self.names]
+
+    def _grads(self, loss, params):
+        """The loss's gradients with the graph kept, clipped where the optimizer clips."""
+        grads = torch.autograd.grad(loss, params, create_graph=True)
+        if self.max_norm is None:
+            return grads
+        *grads, norm = ClipNormTreeFn.apply(self.table, float(self.max_norm), 1e-6, *grads)
+        self.grad_norm = norm.detach()
+        return grads
 
     def _install(self, new_params) -> None:
         for name, p in zip(self.names, new_params):
@@ -190,8 +259,8 @@ class MetaAdam(_MetaOptimizer):
     gradient).  ``detach_()`` cuts the graph, e.g. between outer iterations.
     """
 
-    def __init__(self, module: torch.nn.Module, lr=1e-3, b1=0.9, b2=0.999, eps=1e-8, eps_root=0.0):
-        super().__init__(module)
+    def __init__(self, module: torch.nn.Module, lr=1e-3, b1=0.9, b2=0.999, eps=1e-8, eps_root=0.0, max_norm=None):
+        super().__init__(module, max_norm)
         self.hyper = AdamHyper(lr, b1, b2, eps, eps_root)
         params = self.params()
         self.mu = [torch.zeros_like(p) for p in params]
@@ -200,7 +269,7 @@ class MetaAdam(_MetaOptimizer):
 
     def step(self, loss: torch.Tensor) -> None:
         params = self.params()
-        grads = torch.autograd.grad(loss, params, create_graph=True)
+        grads = self._grads(loss, params)
         out = AdamTreeFn.apply(self.table, self.count, self.hyper, *params, *grads, *self.mu, *self.nu)
         S = len(params)
         self._install(out[:S])
@@ -344,14 +413,14 @@ class MetaSGD(_MetaOptimizer):
     module's parameters; each step is one leaf-direct launch (SGDTreeFn).  The
     trace starts absent (zero), as torch.optim's first momentum step."""
 
-    def __init__(self, module: torch.nn.Module, lr=0.1, momentum=0.0, nesterov=False):
-        super().__init__(module)
+    def __init__(self, module: torch.nn.Module, lr=0.1, momentum=0.0, nesterov=False, max_norm=None):
+        super().__init__(module, max_norm)
         self.hyper = SGDHyper(lr, momentum, nesterov)
         self.trace = None
 
     def step(self, loss: torch.Tensor) -> None:
         params = self.params()
-        grads = torch.autograd.grad(loss, params, create_graph=True)
+        grads = self._grads(loss, params)
         has_trace = self.trace is not None
         out = SGDTreeFn.apply(self.table, self.hyper, has_trace, *params, *grads, *(self.trace or []))
         S = len(params)
@@ -369,15 +438,15 @@ class MetaRMSProp(_MetaOptimizer):
     """Object-oriented differentiable RMSProp (momentum optional) over a
     module's parameters; each step is one leaf-direct launch (RMSPropTreeFn)."""
 
-    def __init__(self, module: torch.nn.Module, lr=1e-2, alpha=0.99, eps=1e-8, eps_root=0.0, momentum=0.0):
-        super().__init__(module)
+    def __init__(self, module: torch.nn.Module, lr=1e-2, alpha=0.99, eps=1e-8, eps_root=0.0, momentum=0.0, max_norm=None):
+        super().__init__(module, max_norm)
         self.hyper = RMSPropHyper(lr, alpha, eps, eps_root, momentum)
         self.nu = [torch.zeros_like(p) for p in self.params()]
         self.mom = None
 
     def step(self, loss: torch.Tensor) -> None:
         params = self.params()
-        grads = torch.autograd.grad(loss, params, create_graph=True)
+        grads = self._grads(loss, params)
         has_mom = self.mom is not None
         out = RMSPropTreeFn.apply(self.table, self.hyper, has_mom, *params, *grads, *self.nu, *(self.mom or []))
         S = len(params)

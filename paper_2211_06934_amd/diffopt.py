@@ -74,6 +74,12 @@ def _load_library():
         "diffopt_es_perturb_gaussian": (ctypes.c_int, [vp, i64, i64, ctypes.c_uint64, f64, i32, vp, vp]),
         "diffopt_es_estimate_gaussian": (ctypes.c_int, [vp, vp, i64, i32, i64, ctypes.c_uint64, f64, vp, vp]),
         "diffopt_es_weights": (ctypes.c_int, [vp, vp, i64, i32, f64, vp, vp]),
+        "diffopt_clip_norm_fwd": (ctypes.c_int, [vp, i64, f64, f64, vp, vp, vp, i64, vp]),
+        "diffopt_clip_norm_fwd_tree": (ctypes.c_int, [vp, vp, f64, f64, vp, vp, vp, i64, vp]),
+        "diffopt_clip_norm_bwd": (ctypes.c_int, [vp, vp, vp, vp, i64, f64, vp, vp, i64, vp]),
+        "diffopt_clip_norm_bwd_tree": (ctypes.c_int, [vp, vp, vp, vp, vp, f64, vp, vp, i64, vp]),
+        "diffopt_clip_norm_workspace": (i64, [i64]),
+        "diffopt_clip_norm_workspace_tree": (i64, [vp]),
     }
     for name, (res, args) in sig.items():
         if not hasattr(lib, name):
@@ -574,6 +580,97 @@ def rmsprop_bwd_tree(table: SegTable, dparams_out, dnu_out, dmom_out, grad, nu, 
         float(lr), float(alpha), float(eps), float(eps_root), float(momentum),
         *[_leaf_array(x, w, k) for x, w in ((dgrad, "dgrad"), (dnu_in, "dnu_in"), (dmom_in, "dmom_in"))],
         _stream(stream)))
+
+
+# ---- global norm and clipping
+
+
+def clip_norm_workspace(n: int) -> int:
+    """diffopt_clip_norm_workspace: bytes that clip_norm_fwd and clip_norm_bwd need for n elements."""
+    need = int(_lib.diffopt_clip_norm_workspace(n))
+    if need < 0:
+        raise ValueError("clip_norm: a size that the operator refuses")
+    return need
+
+
+def clip_norm_workspace_tree(table: SegTable) -> int:
+    """diffopt_clip_norm_workspace_tree: bytes that clip_norm_fwd_tree and clip_norm_bwd_tree need for this table."""
+    return int(_lib.diffopt_clip_norm_workspace_tree(table.handle))
+
+
+def _clip_scratch(given, need: int, like: torch.Tensor, stream):
+    """(tensor kept alive, address, bytes) of a call's workspace; its own is allocated on the call's stream."""
+    if given is None:
+        if need == 0:
+            return None, None, 0
+        if stream is None:
+            given = torch.empty(need, dtype=torch.uint8, device=like.device)
+        else:
+            with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=like.device)):
+                given = torch.empty(need, dtype=torch.uint8, device=like.device)
+    elif not isinstance(given, torch.Tensor) or given.dtype != torch.uint8 or not given.is_cuda or not given.is_contiguous():
+        raise ValueError("workspace: expected a contiguous uint8 tensor in device memory")
+    elif given.device != like.device:
+        raise ValueError("workspace: expected a tensor on %s, got %s" % (like.device, given.device))
+    elif given.numel() < need:
+        raise ValueError("workspace: expected at least %d bytes, got %d" % (need, given.numel()))
+    return given, given.data_ptr() or None, given.numel()
+
+
+def _on_device(*named) -> None:
+    """The tensors of a call live on the device that it launches on."""
+    for x, what in named:
+        if isinstance(x, torch.Tensor) and x.is_cuda and x.device.index != torch.cuda.current_device():
+            raise ValueError("%s: lives on %s, the current device is cuda:%d" % (what, x.device, torch.cuda.current_device()))
+
+
+def _stats(stats) -> torch.Tensor:
+    if not isinstance(stats, torch.Tensor):
+        raise TypeError("stats: expected a torch.Tensor")
+    _addr(stats, "stats", n=2)
+    return stats
+
+
+def clip_norm_fwd(grad, max_norm: float, out, stats, eps: float = 1e-6, workspace=None, stream=None) -> None:
+    """diffopt_clip_norm_fwd: stats [2] = the norm of grad and c = min(1, max_norm / (norm + eps)); out = c grad (out may be
+    grad, or None)."""
+    if not isinstance(grad, torch.Tensor):
+        raise TypeError("grad: expected a torch.Tensor")
+    n = grad.numel()
+    keep, ws, nws = _clip_scratch(workspace, clip_norm_workspace(n), _stats(stats), stream)
+    _on_device((grad, "grad"), (out, "out"), (stats, "stats"))
+    _check(_lib.diffopt_clip_norm_fwd(_addr(grad, "grad", n=n), n, float(max_norm), float(eps), _addr(out, "out", n=n), _addr(stats, "stats"), ws, nws,
+                                      _stream(stream)))
+
+
+def clip_norm_bwd(dout, dnorm, grad, stats, dgrad, eps: float = 1e-6, workspace=None, stream=None) -> None:
+    """diffopt_clip_norm_bwd: gradient of clip_norm_fwd for cotangents of out and of the norm (either None: zero); dgrad may be
+    dout or grad."""
+    if not isinstance(grad, torch.Tensor):
+        raise TypeError("grad: expected a torch.Tensor")
+    n = grad.numel()
+    keep, ws, nws = _clip_scratch(workspace, clip_norm_workspace(n), _stats(stats), stream)
+    _on_device((dout, "dout"), (dnorm, "dnorm"), (grad, "grad"), (stats, "stats"), (dgrad, "dgrad"))
+    _check(_lib.diffopt_clip_norm_bwd(_addr(dout, "dout", n=n), _addr(dnorm, "dnorm", n=1), _addr(grad, "grad", n=n), _addr(stats, "stats"), n,
+                                      float(eps), _addr(dgrad, "dgrad", n=n), ws, nws, _stream(stream)))
+
+
+def clip_norm_fwd_tree(table: SegTable, grad, max_norm: float, out, stats, eps: float = 1e-6, workspace=None, stream=None) -> None:
+    """diffopt_clip_norm_fwd_tree: clip_norm_fwd over the leaves of a tree (out may be grad, or None)."""
+    k = len(table.numel)
+    keep, ws, nws = _clip_scratch(workspace, clip_norm_workspace_tree(table), _stats(stats), stream)
+    _on_device((grad, "grad"), (out, "out"), (stats, "stats"))
+    _check(_lib.diffopt_clip_norm_fwd_tree(table.handle, _leaf_array(grad, "grad", k), float(max_norm), float(eps), _leaf_array(out, "out", k),
+                                           _addr(stats, "stats"), ws, nws, _stream(stream)))
+
+
+def clip_norm_bwd_tree(table: SegTable, dout, dnorm, grad, stats, dgrad, eps: float = 1e-6, workspace=None, stream=None) -> None:
+    """diffopt_clip_norm_bwd_tree: clip_norm_bwd over the leaves of a tree (dgrad may be dout or grad)."""
+    k = len(table.numel)
+    keep, ws, nws = _clip_scratch(workspace, clip_norm_workspace_tree(table), _stats(stats), stream)
+    _on_device((dout, "dout"), (dnorm, "dnorm"), (grad, "grad"), (stats, "stats"), (dgrad, "dgrad"))
+    _check(_lib.diffopt_clip_norm_bwd_tree(table.handle, _leaf_array(dout, "dout", k), _addr(dnorm, "dnorm", n=1), _leaf_array(grad, "grad", k),
+                                           _addr(stats, "stats"), float(eps), _leaf_array(dgrad, "dgrad", k), ws, nws, _stream(stream)))
 
 
 # ---- zero-order (ES) gradient estimation
