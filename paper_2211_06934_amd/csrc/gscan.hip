@@ -17,13 +17,14 @@
 // third walks the chunks.  A token past its sequence's end maps every state to
 // itself.
 #include <initializer_list>
+#include <type_traits>
 
 #include "lm_common.hpp"
 
 namespace diffopt {
 namespace {
 
-constexpr int kW = 8;  // waves of a chunk
+constexpr int kW = 8;  // waves of a chunk, and the most chunks whose runs the walk joins itself
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int64_t kMostGroups = (int64_t(1) << 32) / (64 * kW) - 1;  // a launch has fewer than 2^32 threads
 
@@ -41,7 +42,8 @@ struct Scan {
   float *end, *begin, *end2;                // the state (or y) after the last token, the adjoint (or f) before the first
   float* parts;                             // [B][S][fields][C]: chunks' runs, then the states that enter them
   int64_t T, C, S;
-  int32_t cols, inline_join;
+  int32_t cols;
+  bool in_place;  // chunks after the first must not read the state, which the last one overwrites
 };
 
 template <class E, int VEC>
@@ -167,30 +169,33 @@ struct Tokens {
 
   // Log gates become gates; tokens past the end the identity; the run of the rest.
   __device__ __forceinline__ void finish(const Place<VEC>& at, int64_t t0) {
+    if (t0 + U > at.len) {  // the same for the wave
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (t0 + u >= at.len)
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            a[u][i] = x[u][i] = 0.0f;
+            if constexpr (MODE >= kBwd) dh[u][i] = 0.0f;
+            if constexpr (MODE == kSecond) r[u][i] = p[u][i] = 0.0f;
+          }
+    }
 #pragma unroll
     for (int f = 0; f < fields(MODE); ++f)
 #pragma unroll
       for (int i = 0; i < VEC; ++i) run[f][i] = 0.0f;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool live = t0 + u < at.len;
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
-        const float lg = live ? a[u][i] : 0.0f;
-        run[kL][i] += lg;
-        a[u][i] = gate(lg);
-        if (!live) {
-          x[u][i] = 0.0f;
-          if constexpr (MODE >= kBwd) dh[u][i] = 0.0f;
-          if constexpr (MODE == kSecond) r[u][i] = p[u][i] = 0.0f;
-        }
+        run[kL][i] += a[u][i];
+        a[u][i] = gate(a[u][i]);
         if constexpr (MODE == kSecond) {
           run[kRho][i] += r[u][i];
           run[kY][i] = a[u][i] * (run[kY][i] + r[u][i] * run[kX][i]) + p[u][i];
         }
         run[kX][i] = a[u][i] * run[kX][i] + x[u][i];
       }
-    }
     if constexpr (MODE >= kBwd)
 #pragma unroll
       for (int u = U - 1; u >= 0; --u)
@@ -344,14 +349,15 @@ __global__ __launch_bounds__(64 * kJW) void gscan_join(Scan s) {
   }
 }
 
-// The states that enter a chunk, from both sides.
-template <int MODE, int VEC>
+// The states that enter a chunk, from both sides: from the join, or those that
+// enter the sequence.
+template <int MODE, int VEC, bool JOIN>
 __device__ __forceinline__ void enter(const Scan& s, const Place<VEC>& at, States<VEC>& st) {
   constexpr int NF = fields(MODE);
   const int64_t first = at.b * s.C + at.c;
 #pragma unroll
   for (int i = 0; i < VEC; ++i) {
-    if (s.S > 1 && !s.inline_join) {
+    if constexpr (!JOIN) {
       const float* from = part_of(s, NF, at.b, at.seg) + at.c + i;
       st.h[i] = from[kX * s.C];
       if constexpr (MODE >= kBwd) st.e[i] = from[kE * s.C];
@@ -365,19 +371,6 @@ __device__ __forceinline__ void enter(const Scan& s, const Place<VEC>& at, State
       st.e[i] = MODE >= kBwd && s.dstate_out ? s.dstate_out[first + i] : 0.0f;
       st.f[i] = 0.0f;
     }
-  }
-  if (s.S > 1 && s.inline_join) {
-    for (int64_t seg = 0; seg < at.seg; ++seg) {
-      const float* run = part_of(s, NF, at.b, seg) + at.c;
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) pass_fwd<MODE>(st.h[i], st.y[i], [&](int k) { return run[k * s.C + i]; });
-    }
-    if constexpr (MODE >= kBwd)
-      for (int64_t seg = s.S - 1; seg > at.seg; --seg) {
-        const float* run = part_of(s, NF, at.b, seg) + at.c;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) pass_bwd<MODE>(st.e[i], st.f[i], [&](int k) { return run[k * s.C + i]; });
-      }
   }
 }
 
@@ -394,21 +387,40 @@ __device__ __forceinline__ void store_rows(const Scan& s, const HeadArr& h, cons
   }
 }
 
-// A chunk's results.
-template <class E, int MODE, int VEC, int U>
-__global__ __launch_bounds__(64 * kW) void gscan_walk(Scan s) {
+// A chunk's results.  JOIN: the sequence has at most kW chunks, whose runs the
+// workgroup joins itself.
+template <class E, int MODE, int VEC, int U, bool JOIN>
+__global__ __launch_bounds__(64 * kW, (MODE == kSecond && JOIN ? 4 : 1)) void gscan_walk(Scan s) {
   __shared__ Runs<MODE, VEC> R;
+  __shared__ std::conditional_t<JOIN, Runs<MODE, VEC>, char> J;
   const Place<VEC> at(s);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t t0 = (at.seg * kW + wave) * U;
   Tokens<E, MODE, VEC, U> tok;
   tok.load(s, at, t0);
   States<VEC> st;
-  enter<MODE, VEC>(s, at, st);
+  enter<MODE, VEC, JOIN>(s, at, st);
+  if constexpr (JOIN)
+    if (s.S > 1 && wave < s.S) {  // a wave brings one chunk's run
+      const float* run = part_of(s, fields(MODE), at.b, wave) + at.c;
+#pragma unroll
+      for (int f = 0; f < fields(MODE); ++f)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) J.v[wave][f][i][lane] = run[f * s.C + i];
+    }
   tok.finish(at, t0);
   R.put(wave, lane, tok);
   __syncthreads();  // also: every wave has read the state that the last one may now overwrite
   if (!at.on) return;
+  if constexpr (JOIN) {
+    for (int c = 0; c < (int)at.seg; ++c)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) pass_fwd<MODE>(st.h[i], st.y[i], [&](int k) { return J.v[c][k][i][lane]; });
+    if constexpr (MODE >= kBwd)
+      for (int c = (int)s.S - 1; c > (int)at.seg; --c)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) pass_bwd<MODE>(st.e[i], st.f[i], [&](int k) { return J.v[c][k][i][lane]; });
+  }
   for (int w = 0; w < wave; ++w)
 #pragma unroll
     for (int i = 0; i < VEC; ++i) pass_fwd<MODE>(st.h[i], st.y[i], [&](int k) { return R.v[w][k][i][lane]; });
@@ -505,8 +517,6 @@ __global__ __launch_bounds__(kBlock) void gscan_one(HeadArr lg, HeadArr x, HeadA
 
 constexpr int kU = 8;  // tokens of a wave
 constexpr int64_t kChunk = kW * kU;
-constexpr int64_t kInlineJoin = 8;
-
 int64_t chunks_of(int64_t T) { return T <= kChunk ? 1 : (T + kChunk - 1) / kChunk; }
 
 int64_t workspace_bytes(int64_t B, int64_t T, int64_t C, int mode) {
@@ -526,17 +536,19 @@ template <class E, int MODE, int VEC>
 int launch(const char* who, Scan s, int64_t B, hipStream_t st) {
   s.cols = (int32_t)((s.C + 64 * VEC - 1) / (64 * VEC));
   const dim3 grid((unsigned)(B * s.S * s.cols)), block(64 * kW);
-  if (s.S > 1) {
-    hipLaunchKernelGGL((gscan_runs<E, MODE, VEC, kU>), grid, block, 0, st, s);
-    if (!s.inline_join) hipLaunchKernelGGL((gscan_join<MODE>), dim3((unsigned)(B * ((s.C + 63) / 64))), dim3(64 * kJW), 0, st, s);
+  if (s.S > 1) hipLaunchKernelGGL((gscan_runs<E, MODE, VEC, kU>), grid, block, 0, st, s);
+  if (s.S <= kW && !s.in_place) {
+    hipLaunchKernelGGL((gscan_walk<E, MODE, VEC, kU, true>), grid, block, 0, st, s);
+  } else {
+    if (s.S > 1) hipLaunchKernelGGL((gscan_join<MODE>), dim3((unsigned)(B * ((s.C + 63) / 64))), dim3(64 * kJW), 0, st, s);
+    hipLaunchKernelGGL((gscan_walk<E, MODE, VEC, kU, false>), grid, block, 0, st, s);
   }
-  hipLaunchKernelGGL((gscan_walk<E, MODE, VEC, kU>), grid, block, 0, st, s);
   return launch_status(who);
 }
 
 template <int MODE>
 int run(const char* who, const Scan& s, int64_t B, int32_t dtype, hipStream_t st) {
-  constexpr int V = MODE == kSecond ? 2 : 4;
+  constexpr int V = MODE == kSecond ? 2 : 1;
   if (s.C < 64 * V) return dtype == DIFFOPT_F32 ? launch<float, MODE, 1>(who, s, B, st) : launch<bf16, MODE, 1>(who, s, B, st);
   return dtype == DIFFOPT_F32 ? launch<float, MODE, V>(who, s, B, st) : launch<bf16, MODE, V>(who, s, B, st);
 }
@@ -630,7 +642,7 @@ extern "C" int diffopt_gscan_fwd(const diffopt_heads* log_gate, const diffopt_he
   s.T = T;
   s.C = C;
   s.S = chunks_of(T);
-  s.inline_join = s.S <= kInlineJoin && !in_place;
+  s.in_place = in_place && s.S > 1;
   return run<kFwd>(who, s, B, dtype, as_stream(stream));
 }
 
@@ -657,7 +669,6 @@ extern "C" int diffopt_gscan_bwd(const diffopt_heads* dh, const float* dstate_ou
   s.T = T;
   s.C = C;
   s.S = chunks_of(T);
-  s.inline_join = s.S <= kInlineJoin;
   return run<kBwd>(who, s, B, dtype, as_stream(stream));
 }
 
@@ -690,7 +701,6 @@ extern "C" int diffopt_gscan_bwd_bwd(const diffopt_heads* ddlog_gate, const diff
   s.T = T;
   s.C = C;
   s.S = chunks_of(T);
-  s.inline_join = s.S <= kInlineJoin;
   return run<kSecond>(who, s, B, dtype, as_stream(stream));
 }
 
