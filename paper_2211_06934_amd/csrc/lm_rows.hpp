@@ -236,10 +236,10 @@ struct Cut {
   int64_t per;
 };
 
-inline Cut cut_of(int64_t N, int64_t V, int32_t dtype) {
+inline Cut cut_of(int64_t N, int64_t V, int32_t dtype, int64_t slice_bytes = kSliceBytes) {
   if (N >= kFewRows || N == 0 || V * elem_size(dtype) <= (N < kVeryFewRows ? kShortBytes : kLongBytes)) return Cut{1, V};
   int64_t n = kFillRows / N;
-  const int64_t most = V * elem_size(dtype) / kSliceBytes;
+  const int64_t most = V * elem_size(dtype) / slice_bytes;
   n = n > most ? most : n;
   if (n < 2) return Cut{1, V};
   int64_t per = (V + n - 1) / n;

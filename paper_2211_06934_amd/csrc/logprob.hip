@@ -5,10 +5,10 @@
 // One workgroup per row, or per slice of one where there are few rows.  One
 // pass over a row with a running maximum m gives s = sum e and t = sum e d, with
 // d = (x - m) / T and e = exp(d): the entropy is log s - t / s.  Each lane's own
-// maximum also says where the alternatives are: the K-th largest of the lanes'
-// maxima is at most the K-th largest logit, so only lanes at or above it look
-// at their elements again, and hardly more than K of those pass (512 lanes, K =
-// 64: 68 expected of independent logits).  They are ranked by value and lowest
+// maximum also says where the alternatives are: the K-th largest maximum of groups
+// of lanes is at most the K-th largest logit, so only lanes at or above it look
+// at their elements again, and hardly more than K of those pass (of independent
+// logits 24 for K = 20 and 64 groups, 177 for K = 128 and 256).  They are ranked by value and lowest
 // id in LDS.  A row of so many equal logits that they do not fit there takes
 // eight counting passes over the digits of (value, id) instead.
 // The gradient's dense part takes the row from registers where the same call
@@ -86,6 +86,7 @@ struct Sums {
     s += p.s;
     t += p.t;
   }
+  // Values and no new maximum below them.
   template <int N, bool ENT>
   __device__ __forceinline__ void piece(const float* e, float c) {
     float vm = e[0];
@@ -98,14 +99,9 @@ struct Sums {
   }
   template <bool ENT>
   __device__ __forceinline__ void all(float (*R)[3], float c) {  // over the workgroup
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      Sums p;
-      p.m = __shfl_xor(m, o, 64);
-      p.s = __shfl_xor(s, o, 64);
-      p.t = ENT ? __shfl_xor(t, o, 64) : 0.0f;
-      join<ENT>(p, c);
-    }
+    shift<ENT>(wave_max(m), c);
+    s = wave_sum(s);
+    if (ENT) t = wave_sum(t);
     const int wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) {
@@ -114,13 +110,20 @@ struct Sums {
       R[wave][2] = t;
     }
     __syncthreads();
-    *this = Sums();
-    for (int w = 0; w < nw; ++w) {
-      Sums p;
-      p.m = R[w][0];
-      p.s = R[w][1];
-      p.t = R[w][2];
-      join<ENT>(p, c);
+    // a wave's lanes take one wave each: nw <= 16
+    const int w = threadIdx.x & 15;
+    const bool in = w < nw;
+    m = in ? R[w][0] : -kInf;
+    s = in ? R[w][1] : 0.0f;
+    t = in ? R[w][2] : 0.0f;
+    float M = m;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+    shift<ENT>(M, c);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) {
+      s += __shfl_xor(s, o, 64);
+      if (ENT) t += __shfl_xor(t, o, 64);
     }
   }
   // whether they are those of a distribution: no NaN, no +inf, not -inf alone
@@ -128,19 +131,63 @@ struct Sums {
   __device__ __forceinline__ float entropy() const { return fmaxf(logf(s) - kLn2 * (t / s), 0.0f); }  // of good ones
 };
 
-template <class E_, bool ENT>
-__device__ __forceinline__ void row_sums(const E_* x, int64_t c0, int64_t c1, float c, Sums& sums) {
-  over_row(
-      x, c0, c1,
-      [&](int64_t at) {
-        float e[Vec<E_>::N];
-        load_floats(x + at, e);
-        sums.template piece<Vec<E_>::N, ENT>(e, c);
-      },
-      [&](int64_t at) {
-        const float e = (float)x[at];
-        sums.template piece<1, ENT>(&e, c);
-      });
+// How a workgroup of B lanes shares elements [c0, c1) of a row: 16-byte pieces
+// from the first aligned one on, lane after lane, and one of the elements around
+// them.
+template <class E_, int B>
+struct Share {
+  static constexpr int N = Vec<E_>::N;
+  const E_* x;
+  int64_t c0;
+  int32_t head, nv, n;
+  __device__ __forceinline__ Share(const E_* x_, int64_t c0_, int64_t c1) : x(x_), c0(c0_), n((int32_t)(c1 - c0_)) {
+    head = (int32_t)head_of(x + c0, n);
+    nv = (n - head) / N;
+  }
+  __device__ __forceinline__ int64_t piece(int32_t i) const { return c0 + head + (int64_t)i * N; }
+  __device__ __forceinline__ bool has_single(int32_t lane) const { return lane < n - nv * N; }
+  __device__ __forceinline__ int64_t single(int32_t lane) const { return c0 + (lane < head ? lane : lane + (int64_t)nv * N); }
+  // what a lane has, for the others to look at
+  __device__ __forceinline__ int32_t items() const { return (nv + B - 1) / B + 1; }
+  template <class F>
+  __device__ __forceinline__ void item(int32_t lane, int32_t j, F f) const {
+    const int32_t i = lane + (j - 1) * B;
+    if (j == 0) {
+      if (has_single(lane)) f((float)x[single(lane)], single(lane));
+    } else if (i < nv) {
+      float e[N];
+      load_floats(x + piece(i), e);
+#pragma unroll
+      for (int k = 0; k < N; ++k) f(e[k], piece(i) + k);
+    }
+  }
+};
+
+// A lane's sums over its share, kAhead pieces on their way at once (2,048 rows of
+// 50,021 bf16 logits: 39.5 us, with two 41.7, with six 43.3, with eight 44.2).
+constexpr int kAhead = 4;
+template <class E_, int B, bool ENT>
+__device__ __forceinline__ void row_sums(const Share<E_, B>& sh, float c, Sums& sums) {
+  constexpr int N = Vec<E_>::N;
+  int32_t i = threadIdx.x;
+  for (; i + (kAhead - 1) * B < sh.nv; i += kAhead * B) {
+    float e[kAhead][N];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) load_floats(sh.x + sh.piece(i + a * B), e[a]);
+    sums.template piece<kAhead * N, ENT>(&e[0][0], c);
+  }
+  // fewer than kAhead pieces are left, and the element beside them
+  const bool single = sh.has_single(threadIdx.x);
+  const float one = single ? (float)sh.x[sh.single(threadIdx.x)] : -kInf;
+  if (i < sh.nv) {
+    float e[kAhead - 1][N];
+#pragma unroll
+    for (int a = 0; a < kAhead - 1; ++a) load_floats(sh.x + sh.piece(i + a * B < sh.nv ? i + a * B : i), e[a]);
+#pragma unroll
+    for (int a = 0; a < kAhead - 1; ++a)
+      if (i + a * B < sh.nv) sums.template piece<N, ENT>(e[a], c);
+  }
+  if (single) sums.template piece<1, ENT>(&one, c);
 }
 
 // ---- alternatives -----------------------------------------------------------
@@ -157,45 +204,71 @@ __device__ __forceinline__ uint64_t key_of(float x, int64_t id) { return (uint64
 
 struct Select {
   uint64_t found[kCap], prefix;
-  uint32_t lane_key[kLB], hist[256], count, floor, left, enough;
+  uint32_t lane_key[kLB], hist[256], count, lanes, floor, left, enough;
+  uint16_t lane[kLB];
 };
 
-// The K largest of what a workgroup of B lanes holds: visit(f) calls f(value, id)
-// for each of a lane's elements, largest being the largest of them; emit(rank,
-// value, id) takes the results, (-inf, -1) where fewer values are above -inf.
-template <int B, class Visit, class Emit>
-__device__ __forceinline__ void select_top(Select& S, int K, float largest, Visit visit, Emit emit) {
-  constexpr int kWaves = B / 64;
+// The largest value of the leading 16 bits (all of a bf16 value's) that K of 64 G
+// groups of lanes reach, by one wave.
+constexpr int kFewTop = 48;
+template <int B, int G>
+__device__ __forceinline__ uint32_t floor_of(const Select& S, int K) {
+  constexpr int kLanes = B / (64 * G);  // of a group
+  uint32_t k[G], floor = 0;
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    k[g] = 0;
+#pragma unroll
+    for (int w = 0; w < kLanes; ++w) {
+      const uint32_t l = S.lane_key[64 * (g * kLanes + w) + threadIdx.x];
+      k[g] = l > k[g] ? l : k[g];
+    }
+    k[g] >>= 16;
+  }
+  for (int bit = 15; bit >= 0; --bit) {
+    const uint32_t more = floor | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int g = 0; g < G; ++g) n += __popcll(__ballot(k[g] >= more));
+    if (n >= K) floor = more;
+  }
+  return floor << 16;
+}
+
+// The K largest of what a workgroup of B lanes shares: of(lane, j, f) calls
+// f(value, id) for item j < items() of a lane, largest is the largest value of this
+// lane's; emit(rank, value, id) takes the results, (-inf, -1) where fewer values
+// are above -inf.
+template <int B, class Of, class Emit>
+__device__ __forceinline__ void select_top(Select& S, int K, float largest, const Of& of, Emit emit) {
   const int tid = threadIdx.x;
   const uint32_t own = key_of(largest);
   S.lane_key[tid] = own;
-  if (tid == 0) S.count = 0;
+  if (tid == 0) S.count = S.lanes = 0;
   __syncthreads();
-  if (tid < 64) {  // the largest 16 leading bits that K lanes reach; all bits of a bf16 value
-    uint32_t k[kWaves], floor = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) k[w] = S.lane_key[64 * w + tid] >> 16;
-    for (int bit = 15; bit >= 0; --bit) {
-      const uint32_t more = floor | 1u << bit;
-      int n = 0;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) n += __popcll(__ballot(k[w] >= more));
-      if (n >= K) floor = more;
-    }
-    if (tid == 0) S.floor = floor << 16;
+  if (tid < 64) {
+    const uint32_t floor = K <= kFewTop ? floor_of<B, 1>(S, K) : floor_of<B, (B < 256 ? B / 64 : 4)>(S, K);
+    if (tid == 0) S.floor = floor;
   }
   __syncthreads();
   const uint32_t floor = S.floor;
-  const auto collect = [&](uint64_t from) {
-    visit([&](float v, int64_t id) {
+  const int items = of.items();
+  const auto put = [&](uint64_t from) {
+    return [&S, from](float v, int64_t id) {
       const uint64_t k = key_of(v, id);
       if (v > -kInf && k >= from) {
         const uint32_t i = atomicAdd(&S.count, 1u);
         if (i < kCap) S.found[i] = k;
       }
-    });
+    };
   };
-  if (own >= floor) collect((uint64_t)floor << 32);
+  if (own >= floor) S.lane[atomicAdd(&S.lanes, 1u)] = (uint16_t)tid;
+  __syncthreads();
+  // all lanes share what those lanes have: one round trip to the caches, not one an item
+  for (int i = tid; i < (int)S.lanes * items; i += B) {
+    const int l = i / items;
+    of.item(S.lane[l], i - l * items, put((uint64_t)floor << 32));
+  }
   __syncthreads();
   if (S.count > kCap) {  // the same for all lanes; the K-th key digit by digit, until at most kCap keys are not below it
     uint64_t prefix = 0;
@@ -204,10 +277,11 @@ __device__ __forceinline__ void select_top(Select& S, int K, float largest, Visi
       __syncthreads();
       for (int i = tid; i < 256; i += B) S.hist[i] = 0;
       __syncthreads();
-      visit([&](float v, int64_t id) {
-        const uint64_t k = key_of(v, id);
-        if (v > -kInf && (shift == 56 || k >> (shift + 8) == prefix >> (shift + 8))) atomicAdd(&S.hist[k >> shift & 255], 1u);
-      });
+      for (int j = 0; j < items; ++j)
+        of.item(tid, j, [&](float v, int64_t id) {
+          const uint64_t k = key_of(v, id);
+          if (v > -kInf && (shift == 56 || k >> (shift + 8) == prefix >> (shift + 8))) atomicAdd(&S.hist[k >> shift & 255], 1u);
+        });
       __syncthreads();
       if (tid == 0) {
         uint32_t n = left;
@@ -223,7 +297,7 @@ __device__ __forceinline__ void select_top(Select& S, int K, float largest, Visi
       left = S.left;
       if (S.enough || shift == 0) break;
     }
-    collect(prefix);
+    for (int j = 0; j < items; ++j) of.item(tid, j, put(prefix));
     __syncthreads();
   }
   const int n = (int)(S.count < kCap ? S.count : kCap);
@@ -285,9 +359,9 @@ __device__ __forceinline__ void finish(const Rows& r, const Results& o, int64_t 
 }
 
 // ... and its alternatives, by the workgroup.
-template <int B, class Visit>
+template <int B, class Of>
 __device__ __forceinline__ void finish_top(const Rows& r, const Results& o, Select& S, int64_t row, const Token& tok, const Sums& sums, float largest,
-                                           Visit visit) {
+                                           const Of& of) {
   const float ls = logf(sums.s);
   if (!tok.live || tok.bad || !sums.good()) {
     for (int k = threadIdx.x; k < o.K; k += B) {
@@ -296,7 +370,7 @@ __device__ __forceinline__ void finish_top(const Rows& r, const Results& o, Sele
     }
     return;
   }
-  select_top<B>(S, o.K, largest, visit, [&](int rank, float v, int64_t id) {
+  select_top<B>(S, o.K, largest, of, [&](int rank, float v, int64_t id) {
     o.top_logprob[row * o.K + rank] = id < 0 ? -kInf : (v - sums.m) * r.invT - ls;
     set_id(o.top_ids, o.top_bytes, row * o.K + rank, id);
   });
@@ -304,30 +378,20 @@ __device__ __forceinline__ void finish_top(const Rows& r, const Results& o, Sele
 
 // A row (or a slice of one), read once; lanes that may hold an alternative look
 // at theirs again, from the caches.
-template <class E_, bool ENT, bool TOP>
-__global__ __launch_bounds__(kLB) void logprob_row(Rows r, Results o, Parts parts) {
+template <class E_, bool ENT, bool TOP, int B>
+__global__ __launch_bounds__(B) void logprob_row(Rows r, Results o, Parts parts) {
   __shared__ float R[kMaxWaves][3];
   __shared__ std::conditional_t<TOP, Select, int> S;
   const Slice sl = slice_of(r, parts.slices, parts.per);
   const Token tok = token_of(r, sl.row);
   const E_* x = static_cast<const E_*>(r.logits) + sl.row * r.row_stride;
   const float c = r.invT * kLog2e;
+  const Share<E_, B> share(x, sl.c0, sl.c1);
   Sums sums;
-  if (tok.live) row_sums<E_, ENT>(x, sl.c0, sl.c1, c, sums);
+  if (tok.live) row_sums<E_, B, ENT>(share, c, sums);
   else if (parts.slices > 1) return;  // nothing of it is read
   const float largest = sums.m;
   sums.all<ENT>(R, c);
-  const auto visit = [&](auto f) {
-    over_row(
-        x, sl.c0, sl.c1,
-        [&](int64_t at) {
-          float e[Vec<E_>::N];
-          load_floats(x + at, e);
-#pragma unroll
-          for (int i = 0; i < Vec<E_>::N; ++i) f(e[i], at + i);
-        },
-        [&](int64_t at) { f((float)x[at], at); });
-  };
   if (parts.slices > 1) {
     if (threadIdx.x == 0) {
       float* to = parts.sums(blockIdx.x);
@@ -336,15 +400,30 @@ __global__ __launch_bounds__(kLB) void logprob_row(Rows r, Results o, Parts part
       to[2] = sums.t;
     }
     if constexpr (TOP)
-      select_top<kLB>(S, o.K, largest, visit, [&](int rank, float v, int64_t id) {
+      select_top<B>(S, o.K, largest, share, [&](int rank, float v, int64_t id) {
         parts.values(blockIdx.x)[rank] = v;
         parts.ids(blockIdx.x)[rank] = (int32_t)id;
       });
     return;
   }
   if (threadIdx.x == 0) finish(r, o, sl.row, tok, tok.id >= 0 ? (float)x[tok.id] : 0.0f, sums);
-  if constexpr (TOP) finish_top<kLB>(r, o, S, sl.row, tok, sums, largest, visit);
+  if constexpr (TOP) finish_top<B>(r, o, S, sl.row, tok, sums, largest, share);
 }
+
+// What the slices of a row found, shared by the lanes that join them.
+struct Found {
+  const Parts& parts;
+  int64_t first;
+  int32_t n;
+  __device__ __forceinline__ int32_t items() const { return (n + kJB - 1) / kJB; }
+  template <class F>
+  __device__ __forceinline__ void item(int32_t lane, int32_t j, F f) const {
+    const int32_t i = lane + j * kJB;
+    if (i >= n) return;
+    const int32_t slice = i / parts.K, k = i - slice * parts.K;
+    f(parts.values(first + slice)[k], (int64_t)parts.ids(first + slice)[k]);
+  }
+};
 
 // A row from its slices' sums and largest logits.
 template <class E_, bool ENT, bool TOP>
@@ -357,20 +436,15 @@ __global__ __launch_bounds__(kJB) void logprob_join(Rows r, Results o, Parts par
   const float c = r.invT * kLog2e;
   Sums sums;
   float largest = -kInf;
-  const int n = parts.slices * parts.K;
-  const auto visit = [&](auto f) {
-    for (int i = threadIdx.x; i < n; i += kJB) {
-      const int slice = i / parts.K, k = i - slice * parts.K;
-      f(parts.values(first + slice)[k], (int64_t)parts.ids(first + slice)[k]);
-    }
-  };
+  const Found found{parts, first, parts.slices * parts.K};
   if (tok.live) {
     for (int i = threadIdx.x; i < parts.slices; i += kJB) sums.join<ENT>(parts.get(first + i), c);
-    if constexpr (TOP) visit([&](float v, int64_t) { largest = fmaxf(largest, v); });
+    if constexpr (TOP)
+      for (int j = 0; j < found.items(); ++j) found.item(threadIdx.x, j, [&](float v, int64_t) { largest = fmaxf(largest, v); });
   }
   sums.all<ENT>(R, c);
   if (threadIdx.x == 0) finish(r, o, row, tok, tok.id >= 0 ? (float)x[tok.id] : 0.0f, sums);
-  if constexpr (TOP) finish_top<kJB>(r, o, S, row, tok, sums, largest, visit);
+  if constexpr (TOP) finish_top<kJB>(r, o, S, row, tok, sums, largest, found);
 }
 
 // ---- gradient ---------------------------------------------------------------
@@ -482,7 +556,7 @@ __global__ __launch_bounds__(B, (STATS == kKept ? kept_waves(B, NV) : 1)) void l
       kept.load(x, (E_)-kInf);
     }
     if (threadIdx.x < 64) load_named(r, t, row, tok, x, M, lane);  // before dlogits, which may be logits, is written
-    if constexpr (STATS == kRead) row_sums<E_, ENT>(x, 0, r.V, c, sums);
+    if constexpr (STATS == kRead) row_sums<E_, B, ENT>(Share<E_, B>(x, 0, r.V), c, sums);
     if constexpr (STATS == kParts)
       for (int i = threadIdx.x; i < parts.slices; i += B) sums.join<ENT>(parts.get(row * parts.slices + i), c);
     if constexpr (STATS == kKept) {
@@ -856,8 +930,17 @@ int check_cotangents(const char* who, const Rows& r, const Cotangents& t) {
   return check_aligned(who, {t.dlogprob, t.dentropy, t.entropy, t.dtop});
 }
 
+// Slices are longer than distillation's, whose join has no alternatives to rank: 8
+// rows of 512 KiB with 20 of them 13.3 us in slices of 8 KiB, 11.8 of 16, 11.6 of 32.
+Cut row_cut(int64_t N, int64_t V, int32_t dtype) { return cut_of(N, V, dtype, 16384); }
+
+// Lanes of a row: 8,000 rows of 4,000 bf16 logits with 5 alternatives take 27.5 us
+// with 128, 28.5 with 256 and 51.6 with 512; 4,000 of 16,000 31.5, 31.5 and 38.0; 2,048
+// of 50,021 42.0, 41.8 and 41.9 (without alternatives 38 with 512, 43 with 256).
+constexpr int64_t kShortRow = 16384, kMiddleRow = 65536;
+
 int64_t parts_bytes(int64_t N, int64_t V, int32_t dtype, int64_t K) {
-  const Cut c = cut_of(N, V, dtype);
+  const Cut c = row_cut(N, V, dtype);
   return c.slices > 1 ? N * c.slices * (4 + 2 * K) * 4 : 0;
 }
 
@@ -875,9 +958,12 @@ Parts parts_of(const Cut& c, int64_t K, void* workspace) { return Parts{static_c
 
 template <class E_, bool ENT, bool TOP>
 int fwd_rows(const char* who, const Rows& r, int32_t dtype, const Results& o, void* workspace, hipStream_t st) {
-  const Cut c = cut_of(r.N, r.V, dtype);
+  const Cut c = row_cut(r.N, r.V, dtype);
   const Parts p = parts_of(c, TOP ? o.K : 0, workspace);
-  DIFFOPT_LAUNCH((logprob_row<E_, ENT, TOP>), r.N * c.slices, kLB, r, o, p);
+  const int64_t bytes = c.per * elem_size(dtype);
+  if (bytes <= kShortRow) DIFFOPT_LAUNCH((logprob_row<E_, ENT, TOP, 128>), r.N * c.slices, 128, r, o, p);
+  else if (bytes <= kMiddleRow) DIFFOPT_LAUNCH((logprob_row<E_, ENT, TOP, 256>), r.N * c.slices, 256, r, o, p);
+  else DIFFOPT_LAUNCH((logprob_row<E_, ENT, TOP, kLB>), r.N * c.slices, kLB, r, o, p);
   if (c.slices > 1) DIFFOPT_LAUNCH((logprob_join<E_, ENT, TOP>), r.N, kJB, r, o, p);
   return launch_status(who);
 }
@@ -885,7 +971,7 @@ int fwd_rows(const char* who, const Rows& r, int32_t dtype, const Results& o, vo
 template <class E_, bool ENT>
 int bwd_rows(const char* who, const Rows& r, int32_t dtype, const Cotangents& t, const float* stats, void* dx, int64_t dstride, hipStream_t st) {
   // over the logits in place, a row's workgroups would overwrite one another's named tokens
-  const Cut c = dx == r.logits ? Cut{1, r.V} : cut_of(r.N, r.V, dtype);
+  const Cut c = dx == r.logits ? Cut{1, r.V} : row_cut(r.N, r.V, dtype);
   DIFFOPT_LAUNCH((logprob_grad<E_, kGiven, ENT>), r.N * c.slices, kLB, r, Results{}, t, stats, static_cast<E_*>(dx), dstride, parts_of(c, 0, nullptr));
   return launch_status(who);
 }
@@ -893,12 +979,12 @@ int bwd_rows(const char* who, const Rows& r, int32_t dtype, const Cotangents& t,
 template <class E_, bool ENT>
 int both_rows(const char* who, const Rows& r, int32_t dtype, const Results& o, const Cotangents& t, void* dlogits, int64_t dstride, void* workspace,
               hipStream_t st) {
-  const Cut c = cut_of(r.N, r.V, dtype);
+  const Cut c = row_cut(r.N, r.V, dtype);
   const Parts p = parts_of(c, 0, workspace);
   E_* dx = static_cast<E_*>(dlogits);
   const float* none = nullptr;
   if (c.slices > 1) {
-    DIFFOPT_LAUNCH((logprob_row<E_, ENT, false>), r.N * c.slices, kLB, r, o, p);
+    DIFFOPT_LAUNCH((logprob_row<E_, ENT, false, kLB>), r.N * c.slices, kLB, r, o, p);
     DIFFOPT_LAUNCH((logprob_grad<E_, kParts, ENT>), r.N * c.slices, kLB, r, o, t, none, dx, dstride, p);
     return launch_status(who);
   }
@@ -922,7 +1008,7 @@ int both_rows(const char* who, const Rows& r, int32_t dtype, const Results& o, c
 
 template <class E_, bool ENT>
 int second_rows(const char* who, const Rows& r, int32_t dtype, const Cotangents& t, const Second& q, void* workspace, hipStream_t st) {
-  const Cut c = cut_of(r.N, r.V, dtype);
+  const Cut c = row_cut(r.N, r.V, dtype);
   const Parts p = parts_of(c, 0, workspace);
   if (c.slices > 1) {
     DIFFOPT_LAUNCH((logprob_second_parts<E_, ENT>), r.N * c.slices, kLB, r, t, q, p);
