@@ -729,6 +729,90 @@ PyObject* distill_bwd_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   });
 }
 
+// ---- global norm and clipping (diffopt.py) ----------------------------------
+
+// (grad, max_norm, out, stats, eps, workspace, stream)
+PyObject* clip_norm_fwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return operator_call(args, nargs, 7, 3, [](Call& c, int32_t) {
+    c.current();
+    const at::Tensor& g = tensor_of(c.args[0]);
+    const float* grad = c.floats(c.next(), g.sizes());
+    const double max_norm = c.number(c.next());
+    PyObject* o = c.next();
+    const at::Tensor* out = optional_tensor(o);
+    if (out && out->numel() != g.numel()) throw Other{};
+    float *po = out ? c.floats(o, out->sizes()) : nullptr, *stats = c.floats(c.next(), {2});
+    const double eps = c.number(c.next());
+    const int64_t n = g.numel();
+    const Scratch w(c.next(), diffopt_clip_norm_workspace(n), *c.like);
+    void* stream = c.stream(c.next());
+    return unlocked([&] { return diffopt_clip_norm_fwd(grad, n, max_norm, eps, po, stats, w.p, w.bytes, stream); });
+  });
+}
+
+// A tensor of n fp32 elements of any shape, or None.
+float* counted(Call& c, PyObject* o, int64_t n) {
+  const at::Tensor* t = optional_tensor(o);
+  if (!t) return nullptr;
+  if (t->numel() != n) throw Other{};
+  return c.floats(o, t->sizes());
+}
+
+// (dout, dnorm, grad, stats, dgrad, eps, workspace, stream)
+PyObject* clip_norm_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return operator_call(args, nargs, 8, 3, [](Call& c, int32_t) {
+    c.current();
+    const int64_t n = tensor_of(c.args[2]).numel();
+    const float *dout = counted(c, c.next(), n), *dnorm = counted(c, c.next(), 1), *grad = counted(c, c.next(), n), *stats = c.floats(c.next(), {2});
+    float* dgrad = counted(c, c.next(), n);
+    const double eps = c.number(c.next());
+    const Scratch w(c.next(), diffopt_clip_norm_workspace(n), *c.like);
+    void* stream = c.stream(c.next());
+    return unlocked([&] { return diffopt_clip_norm_bwd(dout, dnorm, grad, stats, n, eps, dgrad, w.p, w.bytes, stream); });
+  });
+}
+
+const uint64_t* leaf_array(Call& c, PyObject* o, int64_t k) {
+  return o == Py_None ? nullptr : static_cast<const uint64_t*>(c.flat(o, at::kLong, {k}));
+}
+
+// (leaves, table, grad, max_norm, out, stats, eps, workspace, stream)
+PyObject* clip_norm_fwd_tree(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return operator_call(args, nargs, 9, 5, [](Call& c, int32_t) {
+    c.current();
+    const int64_t k = c.integer(c.next());
+    const diffopt_segtable* table = static_cast<const diffopt_segtable*>(c.stream(c.next()));
+    const uint64_t* grad = leaf_array(c, c.next(), k);
+    const double max_norm = c.number(c.next());
+    const uint64_t* out = leaf_array(c, c.next(), k);
+    float* stats = c.floats(c.next(), {2});
+    const double eps = c.number(c.next());
+    const Scratch w(c.next(), diffopt_clip_norm_workspace_tree(table), *c.like);
+    void* stream = c.stream(c.next());
+    return unlocked([&] { return diffopt_clip_norm_fwd_tree(table, grad, max_norm, eps, out, stats, w.p, w.bytes, stream); });
+  });
+}
+
+// (leaves, table, dout, dnorm, grad, stats, dgrad, eps, workspace, stream)
+PyObject* clip_norm_bwd_tree(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return operator_call(args, nargs, 10, 5, [](Call& c, int32_t) {
+    c.current();
+    const int64_t k = c.integer(c.next());
+    const diffopt_segtable* table = static_cast<const diffopt_segtable*>(c.stream(c.next()));
+    const uint64_t* dout = leaf_array(c, c.next(), k);
+    const float* dnorm = counted(c, c.next(), 1);
+    const uint64_t* grad = leaf_array(c, c.next(), k);
+    const float* stats = c.floats(c.next(), {2});
+    const uint64_t* dgrad = leaf_array(c, c.next(), k);
+    const double eps = c.number(c.next());
+    const Scratch w(c.next(), diffopt_clip_norm_workspace_tree(table), *c.like);
+    void* stream = c.stream(c.next());
+    return unlocked([&] { return diffopt_clip_norm_bwd_tree(table, dout, dnorm, grad, stats, eps, dgrad, w.p, w.bytes, stream); });
+  });
+}
+
+// ---- language-model operators, continued ------------------------------------
+
 // What the calls of logprob share.
 struct Logprob {
   int64_t N, V, stride, K = 0;
@@ -983,6 +1067,10 @@ PyMethodDef methods[] = {
     OPERATOR(distill_bwd),
     OPERATOR(distill_fwd_bwd),
     OPERATOR(distill_bwd_bwd),
+    OPERATOR(clip_norm_fwd),
+    OPERATOR(clip_norm_bwd),
+    OPERATOR(clip_norm_fwd_tree),
+    OPERATOR(clip_norm_bwd_tree),
     OPERATOR(logprob_fwd),
     OPERATOR(logprob_bwd),
     OPERATOR(logprob_fwd_bwd),

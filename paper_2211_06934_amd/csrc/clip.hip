@@ -3,7 +3,8 @@
 //
 // Two launches: partial sums in fp64, one a workgroup, in an order that the
 // sizes alone decide; then every wave adds the few hundred partial sums while
-// its elements are on their way, and scales them.  fp64 holds a square of any
+// its elements are on their way, and scales them (a launch of its own that makes
+// them one costs more: 20M elements 40.3 us against 38.7, 354M 754 against 745).  fp64 holds a square of any
 // fp32 value and its sum to far below an fp32 rounding, at no cost: two
 // instructions for an element of four bytes.  Bound by memory, the elements
 // being read twice; the second pass goes backwards, so that it begins with
@@ -24,9 +25,13 @@
 namespace diffopt {
 namespace {
 
-constexpr int kSumBlock = 1024, kScaleBlock = 256;
-constexpr int kSumWaves = kSumBlock / 64, kScaleWaves = kScaleBlock / 64;
-constexpr int kMostParts = 512;  // two workgroups of sums a compute unit
+constexpr int kScaleBlock = 256, kScaleWaves = kScaleBlock / 64;
+// Waves of a workgroup of sums, and how many workgroups there are at most.  One
+// large workgroup a compute unit is best for long runs of tiles (354M elements:
+// 235 us; 2 of 8 waves 243, 4 of 8 250, 8 of 4 257), more and smaller ones where
+// there are few (2M in 338 leaves: 11.8 us, 2 of 8 waves 10.4).
+constexpr int kManyWaves = 16, kManyParts = 256, kFewWaves = 8, kMostParts = 512;
+constexpr int64_t kManyTiles = 16384;
 constexpr int kGroups = (int)(kTileGroups / 64);  // of a lane
 constexpr int kAloneBlock = 1024, kAloneEach = 8;
 constexpr int64_t kAlone = kAloneBlock * kAloneEach;
@@ -53,7 +58,7 @@ struct Leaf {
 
 template <int NA>
 struct Window {
-  int64_t goff[kWindowMax + 1], numel[kWindowMax];
+  int64_t goff[kWindowMax], numel[kWindowMax];
   uint64_t p[NA][kWindowMax];
 };
 
@@ -72,9 +77,10 @@ struct Tile {
   Leaf<NA> one;  // of a tile inside one leaf
   int64_t first;
   int W;         // leaves of the window; 0: one leaf
+  int mine, lane;  // window place of the leaf that has the lane's eight consecutive groups
 
-  __device__ __forceinline__ Tile(const Space& sp_, const Operands<NA>& ops, Window<NA>& win_, int64_t b, int lane)
-      : sp(sp_), win(win_), one{0, sp_.n, {}}, first(b * kTileGroups + lane), W(0) {
+  __device__ __forceinline__ Tile(const Space& sp_, const Operands<NA>& ops, Window<NA>& win_, int64_t b, int lane_)
+      : sp(sp_), win(win_), one{0, sp_.n, {}}, first(b * kTileGroups + lane_), W(0), mine(0), lane(lane_) {
     if constexpr (FLAT) {
 #pragma unroll
       for (int q = 0; q < NA; ++q) one.p[q] = reinterpret_cast<uint64_t>(ops.a[q]);
@@ -93,27 +99,34 @@ struct Tile {
       for (int q = 0; q < NA; ++q) one.p[q] = caddr<uint64_t>(ops.a[q])[at];
       return;
     }
-    for (int t = lane; t <= W; t += 64) {
+    const auto stage = [&](int t, auto dense) {  // with dense the addresses do not wait for the entries
       const SegEntry e = sp.seg[j0 + t];
-      win.goff[t] = e.goff;
-      if (t < W) {
-        const int64_t at = sp.dense_orig ? j0 + t : e.orig;
-        win.numel[t] = e.numel;
+      uint64_t v[NA];
 #pragma unroll
-        for (int q = 0; q < NA; ++q) win.p[q][t] = static_cast<const uint64_t*>(ops.a[q])[at];
-      }
-    }
+      for (int q = 0; q < NA; ++q) v[q] = static_cast<const uint64_t*>(ops.a[q])[decltype(dense)::value ? j0 + t : e.orig];
+      win.goff[t] = e.goff;
+      win.numel[t] = e.numel;
+#pragma unroll
+      for (int q = 0; q < NA; ++q) win.p[q][t] = v[q];
+    };
+    for (int t = lane; t < W; t += 64)
+      if (sp.dense_orig) stage(t, std::true_type{});
+      else stage(t, std::false_type{});
     wave_sync();
-  }
-
-  __device__ __forceinline__ Leaf<NA> find(int64_t g) const {
-    if (FLAT || W == 0) return one;
-    int lo = 0, hi = W - 1;  // goff[0] <= g
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (win.goff[mid] <= g) lo = mid;
+    // Leaves begin at multiples of kLeafGroupAlign groups: a lane searches for one such run of the tile, the others ask it.
+    static_assert(kTileGroups == 64 * kLeafGroupAlign, "a lane has one run of groups that share a leaf");
+    const int64_t g = b * kTileGroups + lane * kLeafGroupAlign;
+    int hi = W - 1;  // goff[0] <= g
+    while (mine < hi) {
+      const int mid = (mine + hi + 1) >> 1;
+      if (win.goff[mid] <= g) mine = mid;
       else hi = mid - 1;
     }
+  }
+
+  __device__ __forceinline__ Leaf<NA> find(int u) const {
+    if (FLAT || W == 0) return one;
+    const int lo = __shfl(mine, u * (64 / (int)kLeafGroupAlign) + lane / (int)kLeafGroupAlign, 64);
     Leaf<NA> leaf{win.goff[lo], win.numel[lo], {}};
 #pragma unroll
     for (int q = 0; q < NA; ++q) leaf.p[q] = win.p[q][lo];
@@ -125,7 +138,7 @@ struct Tile {
   template <class F>
   __device__ __forceinline__ void group(int u, F f) const {
     const int64_t g = first + u * 64;
-    const Leaf<NA> leaf = find(g);
+    const Leaf<NA> leaf = find(u);
     int64_t e0 = 4 * (g - leaf.goff);
     if constexpr (PH >= 0) e0 -= (int64_t)(leaf.p[PH] >> 2 & 31u);
     int64_t w = e0 + 4 <= leaf.numel ? e0 : leaf.numel - 4;
@@ -175,6 +188,17 @@ __device__ __forceinline__ void store4(uint64_t leaf, int64_t i, const f32x4& x)
   *(gptr<loose>)(leaf + 4 * (uint64_t)i) = x;
 }
 
+// Those of four elements whose bits are set.
+__device__ __forceinline__ void store_own(uint64_t to, uint32_t own, const f32x4& y) {
+  if (own == 15u) {
+    store4(to, 0, y);
+  } else if (own) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (own >> i & 1u) gaddr<float>(to)[i] = y[i];
+  }
+}
+
 __device__ __forceinline__ double wave_sum(double x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
@@ -184,32 +208,39 @@ __device__ __forceinline__ double wave_sum(double x) {
 // Partial sums of a b over the operands' elements (b = a with one operand).
 // With two, nothing is read where stats says that the gradient was not clipped:
 // the sum has no weight then.
-template <bool FLAT, int NA>
-__global__ __launch_bounds__(kSumBlock) void clip_sums(Space sp, Operands<NA> ops, const float* stats, double* parts) {
-  __shared__ std::conditional_t<FLAT, char, Window<NA>> windows[kSumWaves];
-  __shared__ double sums[kSumWaves];
+template <bool FLAT, int NA, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, (NA == 1 ? 8 : 4)) void clip_sums(Space sp, Operands<NA> ops, const float* stats, double* parts) {
+  __shared__ std::conditional_t<FLAT, char, Window<NA>> windows[WAVES];
+  __shared__ double sums[WAVES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   double acc[2] = {0.0, 0.0};
+  static_assert(kGroups * 4 == 32, "a lane's elements are the bits of a word");
   const bool skip = NA == 2 && stats[1] >= 1.0f;
   // wave after wave takes a tile, workgroup after workgroup: neighbouring tiles are read together
   if (!skip)
-    for (int64_t b = (int64_t)wave * gridDim.x + blockIdx.x; b < sp.ntiles; b += (int64_t)gridDim.x * kSumWaves) {
+    for (int64_t b = (int64_t)wave * gridDim.x + blockIdx.x; b < sp.ntiles; b += (int64_t)gridDim.x * WAVES) {
       const Tile<FLAT, NA, FLAT ? 0 : -1> tile(sp, ops, reinterpret_cast<Window<NA>&>(windows[FLAT ? 0 : wave]), b, lane);
       f32x4 v[NA][kGroups];
-      int own[kGroups];
+      uint32_t own = 0;  // four bits a group
       const uint64_t dummy = FLAT ? reinterpret_cast<uint64_t>(ops.a[0]) : reinterpret_cast<uint64_t>(sp.seg);  // 16 bytes that are there
       const bool few = tile.groups([&](int u, const Leaf<NA>& leaf, int64_t w, int o) {
-        own[u] = o;
+        own |= (uint32_t)o << (4 * u);
 #pragma unroll
         for (int q = 0; q < NA; ++q) v[q][u] = load4(o ? leaf.p[q] : dummy, o ? w : 0);
       });
+      if (!__all(own == ~0u)) {
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!(own >> (4 * u + i) & 1u))
+#pragma unroll
+              for (int q = 0; q < NA; ++q) v[q][u][i] = 0.0f;
+      }
 #pragma unroll
       for (int u = 0; u < kGroups; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const double x = own[u] >> i & 1 ? (double)v[0][u][i] : 0.0, y = NA == 1 ? x : own[u] >> i & 1 ? (double)v[NA - 1][u][i] : 0.0;
-          acc[i & 1] = __builtin_fma(x, y, acc[i & 1]);
-        }
+        for (int i = 0; i < 4; ++i) acc[i & 1] = __builtin_fma((double)v[0][u][i], (double)v[NA - 1][u][i], acc[i & 1]);
       if (__any(few))
         tile.few([&](const Leaf<NA>& leaf, int64_t i) {
           const double x = gaddr<const float>(leaf.p[0])[i], y = gaddr<const float>(leaf.p[NA - 1])[i];
@@ -222,7 +253,7 @@ __global__ __launch_bounds__(kSumBlock) void clip_sums(Space sp, Operands<NA> op
   __syncthreads();
   if (threadIdx.x == 0) {
     double all = 0.0;
-    for (int w = 0; w < kSumWaves; ++w) all += sums[w];
+    for (int w = 0; w < WAVES; ++w) all += sums[w];
     parts[blockIdx.x] = all;
   }
 }
@@ -279,10 +310,10 @@ __global__ __launch_bounds__(kScaleBlock) void clip_scale(Space sp, Operands<2> 
   const Tile<FLAT, 2, 1> tile(sp, ops, reinterpret_cast<Window<2>&>(windows[FLAT ? 0 : wave]), b, lane);
   f32x4 v[kGroups];
   uint64_t to[kGroups];
-  int own[kGroups];
+  uint32_t own = 0;  // four bits a group
   const uint64_t dummy = FLAT ? reinterpret_cast<uint64_t>(ops.a[0]) : reinterpret_cast<uint64_t>(sp.seg);
   const bool few = tile.groups([&](int u, const Leaf<2>& leaf, int64_t w, int o) {
-    own[u] = o;
+    own |= (uint32_t)o << (4 * u);
     to[u] = leaf.p[1] + 4 * (uint64_t)w;
     v[u] = load4(o ? leaf.p[0] : dummy, o ? w : 0);
   });
@@ -291,13 +322,7 @@ __global__ __launch_bounds__(kScaleBlock) void clip_scale(Space sp, Operands<2> 
 #pragma unroll
   for (int u = 0; u < kGroups; ++u) {
     const f32x4 y = v[u] * c;
-    if (own[u] == 15) {
-      store4(to[u], 0, y);
-    } else if (own[u]) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (own[u] >> i & 1) gaddr<float>(to[u])[i] = y[i];
-    }
+    store_own(to[u], own >> (4 * u) & 15u, y);
   }
   if (__any(few)) tile.few([&](const Leaf<2>& leaf, int64_t i) { gaddr<float>(leaf.p[1])[i] = c * gaddr<const float>(leaf.p[0])[i]; });
 }
@@ -316,10 +341,10 @@ __global__ __launch_bounds__(kScaleBlock) void clip_gradient(Space sp, Operands<
   const Tile<FLAT, NA, 1> tile(sp, ops, reinterpret_cast<Window<NA>&>(windows[FLAT ? 0 : wave]), b, lane);
   f32x4 v[kGroups], d[DOUT ? kGroups : 1];
   uint64_t to[kGroups];
-  int own[kGroups];
+  uint32_t own = 0;  // four bits a group
   const uint64_t dummy = FLAT ? reinterpret_cast<uint64_t>(ops.a[0]) : reinterpret_cast<uint64_t>(sp.seg);
   const bool few = tile.groups([&](int u, const Leaf<NA>& leaf, int64_t w, int o) {
-    own[u] = o;
+    own |= (uint32_t)o << (4 * u);
     to[u] = leaf.p[1] + 4 * (uint64_t)w;
     v[u] = load4(o ? leaf.p[0] : dummy, o ? w : 0);
     if constexpr (DOUT) d[u] = load4(o ? leaf.p[NA - 1] : dummy, o ? w : 0);
@@ -331,13 +356,7 @@ __global__ __launch_bounds__(kScaleBlock) void clip_gradient(Space sp, Operands<
     f32x4 y;
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = value(v[u][i], DOUT ? d[DOUT ? u : 0][i] : 0.0f);
-    if (own[u] == 15) {
-      store4(to[u], 0, y);
-    } else if (own[u]) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (own[u] >> i & 1) gaddr<float>(to[u])[i] = y[i];
-    }
+    store_own(to[u], own >> (4 * u) & 15u, y);
   }
   if (__any(few))
     tile.few([&](const Leaf<NA>& leaf, int64_t i) {
@@ -444,8 +463,10 @@ struct Elements {
   int64_t count() const { return table ? table->elems : n; }
   int64_t tiles() const { return table ? table->ntiles : ((n + 3) / 4 + 8 + kTileGroups - 1) / kTileGroups; }
   bool alone() const { return count() <= kAlone && (!table || table->tiny); }
+  bool many() const { return tiles() >= kManyTiles; }
   int32_t parts() const {
-    const int64_t blocks = (tiles() + kSumWaves - 1) / kSumWaves;
+    if (many()) return kManyParts;
+    const int64_t blocks = (tiles() + kFewWaves - 1) / kFewWaves;
     return (int32_t)(blocks < kMostParts ? blocks : kMostParts);
   }
   int64_t workspace() const { return count() == 0 || alone() ? 0 : (int64_t)parts() * 8; }
@@ -458,6 +479,13 @@ struct Elements {
 
 #define DIFFOPT_LAUNCH(kernel, grid, block, ...) hipLaunchKernelGGL((kernel), dim3((unsigned)(grid)), dim3(block), 0, st, __VA_ARGS__)
 
+// Partial sums of the operands' products.
+template <bool FLAT, int NA>
+void sums(const Elements& e, const Operands<NA>& ops, const float* stats, double* parts, hipStream_t st) {
+  if (e.many()) DIFFOPT_LAUNCH((clip_sums<FLAT, NA, kManyWaves>), e.parts(), 64 * kManyWaves, e.space(), ops, stats, parts);
+  else DIFFOPT_LAUNCH((clip_sums<FLAT, NA, kFewWaves>), e.parts(), 64 * kFewWaves, e.space(), ops, stats, parts);
+}
+
 template <bool FLAT>
 int fwd(const char* who, const Elements& e, const void* grad, double max_norm, double eps, const void* out, float* stats, void* workspace, hipStream_t st) {
   const Operands<2> ops{{grad, out}};
@@ -465,9 +493,9 @@ int fwd(const char* who, const Elements& e, const void* grad, double max_norm, d
     DIFFOPT_LAUNCH((clip_alone<FLAT>), 1, kAloneBlock, FLAT ? TinyTable{} : e.table->small, e.count(), ops, max_norm, eps, stats);
     return launch_status(who);
   }
-  double* parts = static_cast<double*>(workspace);
   const Space sp = e.space();
-  DIFFOPT_LAUNCH((clip_sums<FLAT, 1>), e.parts(), kSumBlock, sp, (Operands<1>{{grad}}), nullptr, parts);
+  double* parts = static_cast<double*>(workspace);
+  sums<FLAT, 1>(e, Operands<1>{{grad}}, nullptr, parts, st);
   DIFFOPT_LAUNCH((clip_scale<FLAT>), out ? e.scale_blocks() : 1u, kScaleBlock, sp, ops, parts, e.parts(), max_norm, eps, stats);
   return launch_status(who);
 }
@@ -483,13 +511,13 @@ int bwd(const char* who, const Elements& e, const void* dout, const float* dnorm
     else DIFFOPT_LAUNCH((clip_gradient_alone<FLAT, false>), 1, kAloneBlock, small, e.count(), two, dnorm, stats, eps);
     return launch_status(who);
   }
-  double* parts = static_cast<double*>(workspace);
   const Space sp = e.space();
   if (dout) {
-    DIFFOPT_LAUNCH((clip_sums<FLAT, 2>), e.parts(), kSumBlock, sp, (Operands<2>{{grad, dout}}), stats, parts);
+    double* parts = static_cast<double*>(workspace);
+    sums<FLAT, 2>(e, Operands<2>{{grad, dout}}, stats, parts, st);
     DIFFOPT_LAUNCH((clip_gradient<FLAT, true>), e.scale_blocks(), kScaleBlock, sp, three, parts, e.parts(), dnorm, stats, eps);
   } else {
-    DIFFOPT_LAUNCH((clip_gradient<FLAT, false>), e.scale_blocks(), kScaleBlock, sp, two, parts, 0, dnorm, stats, eps);
+    DIFFOPT_LAUNCH((clip_gradient<FLAT, false>), e.scale_blocks(), kScaleBlock, sp, two, nullptr, 0, dnorm, stats, eps);
   }
   return launch_status(who);
 }

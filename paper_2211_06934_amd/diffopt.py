@@ -634,6 +634,8 @@ def _stats(stats) -> torch.Tensor:
 def clip_norm_fwd(grad, max_norm: float, out, stats, eps: float = 1e-6, workspace=None, stream=None) -> None:
     """diffopt_clip_norm_fwd: stats [2] = the norm of grad and c = min(1, max_norm / (norm + eps)); out = c grad (out may be
     grad, or None)."""
+    if (stream is None or workspace is not None) and _done(_native.clip_norm_fwd(grad, max_norm, out, stats, eps, workspace, _stream(stream))):
+        return
     if not isinstance(grad, torch.Tensor):
         raise TypeError("grad: expected a torch.Tensor")
     n = grad.numel()
@@ -646,6 +648,8 @@ def clip_norm_fwd(grad, max_norm: float, out, stats, eps: float = 1e-6, workspac
 def clip_norm_bwd(dout, dnorm, grad, stats, dgrad, eps: float = 1e-6, workspace=None, stream=None) -> None:
     """diffopt_clip_norm_bwd: gradient of clip_norm_fwd for cotangents of out and of the norm (either None: zero); dgrad may be
     dout or grad."""
+    if (stream is None or workspace is not None) and _done(_native.clip_norm_bwd(dout, dnorm, grad, stats, dgrad, eps, workspace, _stream(stream))):
+        return
     if not isinstance(grad, torch.Tensor):
         raise TypeError("grad: expected a torch.Tensor")
     n = grad.numel()
@@ -658,6 +662,9 @@ def clip_norm_bwd(dout, dnorm, grad, stats, dgrad, eps: float = 1e-6, workspace=
 def clip_norm_fwd_tree(table: SegTable, grad, max_norm: float, out, stats, eps: float = 1e-6, workspace=None, stream=None) -> None:
     """diffopt_clip_norm_fwd_tree: clip_norm_fwd over the leaves of a tree (out may be grad, or None)."""
     k = len(table.numel)
+    if (stream is None or workspace is not None) and _done(_native.clip_norm_fwd_tree(
+            k, table.handle, grad, max_norm, out, stats, eps, workspace, _stream(stream))):
+        return
     keep, ws, nws = _clip_scratch(workspace, clip_norm_workspace_tree(table), _stats(stats), stream)
     _on_device((grad, "grad"), (out, "out"), (stats, "stats"))
     _check(_lib.diffopt_clip_norm_fwd_tree(table.handle, _leaf_array(grad, "grad", k), float(max_norm), float(eps), _leaf_array(out, "out", k),
@@ -667,6 +674,9 @@ def clip_norm_fwd_tree(table: SegTable, grad, max_norm: float, out, stats, eps: 
 def clip_norm_bwd_tree(table: SegTable, dout, dnorm, grad, stats, dgrad, eps: float = 1e-6, workspace=None, stream=None) -> None:
     """diffopt_clip_norm_bwd_tree: clip_norm_bwd over the leaves of a tree (dgrad may be dout or grad)."""
     k = len(table.numel)
+    if (stream is None or workspace is not None) and _done(_native.clip_norm_bwd_tree(
+            k, table.handle, dout, dnorm, grad, stats, dgrad, eps, workspace, _stream(stream))):
+        return
     keep, ws, nws = _clip_scratch(workspace, clip_norm_workspace_tree(table), _stats(stats), stream)
     _on_device((dout, "dout"), (dnorm, "dnorm"), (grad, "grad"), (stats, "stats"), (dgrad, "dgrad"))
     _check(_lib.diffopt_clip_norm_bwd_tree(table.handle, _leaf_array(dout, "dout", k), _addr(dnorm, "dnorm", n=1), _leaf_array(grad, "grad", k),
