@@ -960,7 +960,7 @@ template <class E_, bool ENT, bool TOP>
 int fwd_rows(const char* who, const Rows& r, int32_t dtype, const Results& o, void* workspace, hipStream_t st) {
   const Cut c = row_cut(r.N, r.V, dtype);
   const Parts p = parts_of(c, TOP ? o.K : 0, workspace);
-  const int64_t bytes = c.per * elem_size(dtype);
+  const int64_t bytes = r.V * elem_size(dtype);  // of a row: slices are for few rows, whose time is latency
   if (bytes <= kShortRow) DIFFOPT_LAUNCH((logprob_row<E_, ENT, TOP, 128>), r.N * c.slices, 128, r, o, p);
   else if (bytes <= kMiddleRow) DIFFOPT_LAUNCH((logprob_row<E_, ENT, TOP, 256>), r.N * c.slices, 256, r, o, p);
   else DIFFOPT_LAUNCH((logprob_row<E_, ENT, TOP, kLB>), r.N * c.slices, kLB, r, o, p);
