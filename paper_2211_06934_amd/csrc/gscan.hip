@@ -80,6 +80,16 @@ __device__ __forceinline__ void store_pack(E* at, const float* v) {
   }
 }
 
+// The wave, as a number that its lanes share: rows' addresses are scalars.
+__device__ __forceinline__ int wave_of() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
+// A barrier for what is in LDS: loads from memory stay on their way.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 __device__ __forceinline__ float gate(float lg) { return __builtin_amdgcn_exp2f(lg * kLog2e); }
 
 // States of VEC channels that pass through a run forwards (h, y) and backwards (e, f).
@@ -106,17 +116,16 @@ __device__ __forceinline__ void pass_bwd(float& e, float& f, const R& run) {
 // Where a workgroup, a wave and a lane work.
 template <int VEC>
 struct Place {
-  int64_t b, seg, c, len;
+  int64_t b, seg, len;
+  uint32_t c;
   bool on;  // the lane has channels; the last one's may be the neighbour's too, with the same values
   __device__ __forceinline__ Place(const Scan& s) {
-    int64_t block = blockIdx.x;
-    const int64_t col = block % s.cols;
-    block /= s.cols;
-    seg = block % s.S;
-    b = block / s.S;
-    c = (col * 64 + (threadIdx.x & 63)) * VEC;
+    const uint32_t row = blockIdx.x / (uint32_t)s.cols, col = blockIdx.x - row * s.cols;
+    b = row / (uint32_t)s.S;
+    seg = row - b * s.S;
+    c = (col * 64 + (threadIdx.x & 63)) * VEC;  // below 2^32: C is at most 2^31
     on = c < s.C;
-    if (c + VEC > s.C) c = s.C - VEC;  // C >= VEC
+    if (c + VEC > s.C) c = (uint32_t)s.C - VEC;  // C >= VEC
     len = s.T;
     if (s.lengths) {
       const int64_t n = s.lengths[b];
@@ -132,11 +141,11 @@ struct Tokens {
   float run[fields(MODE)][VEC];
 
   static __device__ __forceinline__ void rows(const HeadArr& h, const Place<VEC>& at, int64_t t0, float (*v)[VEC]) {
-    const E* p = static_cast<const E*>(h.p) + at.b * h.sb + at.c;
+    const E* row = static_cast<const E*>(h.p) + at.b * h.sb + t0 * h.st;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t t = t0 + u < at.len ? t0 + u : t0;  // a row that is there, for tokens past the end
-      load_pack<E, VEC>(p + t * h.st, v[u]);
+      load_pack<E, VEC>(row + at.c, v[u]);
+      if (t0 + u + 1 < at.len) row += h.st;  // else once more the last one
     }
   }
   static __device__ __forceinline__ void no_rows(float (*v)[VEC]) {
@@ -230,7 +239,7 @@ __global__ __launch_bounds__(64 * kW) void gscan_runs(Scan s) {
   __shared__ Runs<MODE, VEC> R;
   constexpr int NF = fields(MODE);
   const Place<VEC> at(s);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = wave_of();
   const int64_t t0 = (at.seg * kW + wave) * U;
   Tokens<E, MODE, VEC, U> tok;
   tok.load(s, at, t0);
@@ -271,7 +280,7 @@ __global__ __launch_bounds__(64 * kJW) void gscan_join(Scan s) {
   constexpr int NF = fields(MODE);
   __shared__ float v[kJW][NF][64];
   const int64_t cols = (s.C + 63) / 64, b = blockIdx.x / cols;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = wave_of();
   const int64_t c0 = (blockIdx.x - b * cols) * 64 + lane, c = c0 < s.C ? c0 : s.C - 1;
   const int64_t per = (s.S + kJW - 1) / kJW, s0 = wave * per < s.S ? wave * per : s.S, s1 = s0 + per < s.S ? s0 + per : s.S;
   float L = 0.0f, rho = 0.0f, h = 0.0f, y = 0.0f, e = 0.0f, f = 0.0f;
@@ -376,14 +385,15 @@ __device__ __forceinline__ void enter(const Scan& s, const Place<VEC>& at, State
 
 template <class E, int VEC, int U>
 __device__ __forceinline__ void store_rows(const Scan& s, const HeadArr& h, const Place<VEC>& at, int64_t t0, float (*v)[VEC]) {
-  E* p = static_cast<E*>(h.p) + at.b * h.sb + at.c;
+  E* row = static_cast<E*>(h.p) + at.b * h.sb + t0 * h.st;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     if (t0 + u >= at.len) {
 #pragma unroll
       for (int i = 0; i < VEC; ++i) v[u][i] = 0.0f;
     }
-    if (t0 + u < s.T) store_pack<E, VEC>(p + (t0 + u) * h.st, v[u]);
+    if (t0 + u < s.T) store_pack<E, VEC>(row + at.c, v[u]);
+    row += h.st;
   }
 }
 
@@ -394,7 +404,7 @@ __global__ __launch_bounds__(64 * kW, (MODE == kSecond && JOIN ? 4 : 1)) void gs
   __shared__ Runs<MODE, VEC> R;
   __shared__ std::conditional_t<JOIN, Runs<MODE, VEC>, char> J;
   const Place<VEC> at(s);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = wave_of();
   const int64_t t0 = (at.seg * kW + wave) * U;
   Tokens<E, MODE, VEC, U> tok;
   tok.load(s, at, t0);
@@ -495,6 +505,229 @@ __global__ __launch_bounds__(64 * kW, (MODE == kSecond && JOIN ? 4 : 1)) void gs
   }
 }
 
+// ---- sweeps: many channels --------------------------------------------------
+// With enough columns of 64 channels a workgroup takes its column through the
+// whole sequence, kSweepWaves U tokens at a time, the next ones on their way: a
+// forward sweep reads its operands once, where chunks of their own read them
+// twice.  The backward sweep needs the states from before: a forward sweep that
+// stores nothing else leaves one for each chunk.
+
+constexpr int kSweepWaves = 16;
+constexpr int kSweepU = 16, kBackU = 8;              // tokens of a wave
+constexpr int kBackChunk = kSweepWaves * kBackU;     // tokens for which a state is left
+
+struct Sweep {
+  int64_t b, len, T, nk;  // nk: chunks
+  uint32_t c;             // lanes past the last channel take the last one, and write what its own lane writes
+  int lane, wave;
+  __device__ __forceinline__ Sweep(const Scan& s, int tokens) {
+    lane = threadIdx.x & 63;
+    wave = wave_of();
+    b = blockIdx.x / (uint32_t)s.cols;
+    c = (uint32_t)(blockIdx.x - b * s.cols) * 64 + lane;
+    if (c >= s.C) c = (uint32_t)s.C - 1;
+    T = s.T;
+    len = T;
+    if (s.lengths) {
+      const int64_t n = s.lengths[b];
+      len = n < 0 ? 0 : n < len ? n : len;
+    }
+    nk = (T + tokens - 1) / tokens;
+  }
+};
+
+// A wave's tokens of one channel a lane, as memory holds them.  FULL: all of
+// them are there.
+template <class E, int U>
+struct Raw {
+  E v[U];
+  template <bool FULL>
+  __device__ __forceinline__ void load(const HeadArr& h, const Sweep& w, int64_t t0) {
+    const E* row = static_cast<const E*>(h.p) + w.b * h.sb + t0 * h.st;
+    if (FULL || t0 < w.len) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        v[u] = row[w.c];
+        if (FULL || t0 + u + 1 < w.len) row += h.st;  // else once more the last one
+      }
+    }
+  }
+  // tokens past the end are 0
+  template <bool FULL>
+  __device__ __forceinline__ void get(const Sweep& w, int64_t t0, float* to) const {
+#pragma unroll
+    for (int u = 0; u < U; ++u) to[u] = FULL || t0 + u < w.len ? (float)v[u] : 0.0f;
+  }
+};
+
+template <bool FULL, class E, int U>
+__device__ __forceinline__ void put_rows(const HeadArr& h, const Sweep& w, int64_t t0, const float* v) {
+  E* row = static_cast<E*>(h.p) + w.b * h.sb + t0 * h.st;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (FULL || t0 + u < w.T) row[w.c] = (E)(FULL || t0 + u < w.len ? v[u] : 0.0f);
+    row += h.st;
+  }
+}
+
+// Forward: h and the last state, or (STATES) the state before each kBackChunk
+// tokens.  Whole chunks are pipelined: their code has no condition around a load
+// or a store, so that the wait for the next chunk's loads counts the stores after
+// them and does not wait for those too.
+template <class E, bool STATES>
+struct SweepFwd {
+  static constexpr int U = kSweepU, W = kSweepWaves;
+  const Scan& s;
+  const Sweep w;
+  float h;
+  Raw<E, U> lg, x;
+
+  template <bool FULL>
+  __device__ __forceinline__ void load(int64_t k) {
+    const int64_t t0 = (k * W + w.wave) * U;
+    lg.template load<FULL>(s.lg, w, t0);
+    x.template load<FULL>(s.x, w, t0);
+  }
+  template <bool FULL>
+  __device__ __forceinline__ void step(int64_t k, int64_t next, float (*r)[2][64]) {
+    const int64_t t0 = (k * W + w.wave) * U;
+    float a[U], v[U], L = 0.0f, X = 0.0f;
+    lg.template get<FULL>(w, t0, a);
+    x.template get<FULL>(w, t0, v);
+    if (FULL) load<FULL>(next);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      L += a[u];
+      a[u] = gate(a[u]);
+      X = a[u] * X + v[u];
+    }
+    r[w.wave][0][w.lane] = gate(L);
+    r[w.wave][1][w.lane] = X;
+    lds_barrier();  // the other half is written only after the next one
+    float mine = h;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      if (i == w.wave) mine = h;
+      h = r[i][0][w.lane] * h + r[i][1][w.lane];
+    }
+    if constexpr (STATES) {
+      if (w.wave * U % kBackChunk == 0 && t0 < w.T) s.parts[(w.b * s.S + t0 / kBackChunk) * s.C + w.c] = mine;
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = mine = a[u] * mine + v[u];
+      put_rows<FULL, E, U>(s.out[0], w, t0, v);
+    }
+  }
+};
+
+template <class E, bool STATES>
+__global__ __launch_bounds__(64 * kSweepWaves) void gscan_sweep(Scan s) {
+  using F = SweepFwd<E, STATES>;
+  __shared__ float R[2][F::W][2][64];
+  F f{s, Sweep(s, F::W * F::U), 0.0f, {}, {}};
+  const int64_t st = f.w.b * s.C + f.w.c;
+  if (s.state) f.h = s.state[st];
+  const int64_t full = f.w.len / (F::W * F::U);
+  if (full > 0) {
+    f.template load<true>(0);
+    f.template step<true>(0, full > 1 ? 1 : 0, R[0]);
+    for (int64_t k = 1; k < full; ++k) f.template step<true>(k, k + 1 < full ? k + 1 : k, R[k & 1]);
+  }
+  for (int64_t k = full; k < f.w.nk; ++k) {
+    f.template load<false>(k);
+    f.template step<false>(k, k, R[k & 1]);
+  }
+  if (!STATES && s.end && f.w.wave == 0) s.end[st] = f.h;
+}
+
+// Backward, from the last chunk to the first.
+template <class E, bool DLG, bool DX>
+struct SweepBwd {
+  static constexpr int U = kBackU, W = kSweepWaves;
+  const Scan& s;
+  const Sweep w;
+  float e, before;
+  Raw<E, U> lg, x, dh;
+
+  template <bool FULL>
+  __device__ __forceinline__ void load(int64_t k) {
+    const int64_t t0 = (k * W + w.wave) * U;
+    lg.template load<FULL>(s.lg, w, t0);
+    x.template load<FULL>(s.x, w, t0);
+    dh.template load<FULL>(s.dh, w, t0);
+    before = s.parts[(w.b * s.S + k) * s.C + w.c];
+  }
+  template <bool FULL>
+  __device__ __forceinline__ void step(int64_t k, int64_t next, float (*r)[3][64]) {
+    const int64_t t0 = (k * W + w.wave) * U;
+    float a[U], v[U], g[U], L = 0.0f, X = 0.0f, E0 = 0.0f, h = before;
+    lg.template get<FULL>(w, t0, a);
+    x.template get<FULL>(w, t0, v);
+    dh.template get<FULL>(w, t0, g);
+    if (FULL) load<FULL>(next);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      L += a[u];
+      a[u] = gate(a[u]);
+      X = a[u] * X + v[u];
+    }
+#pragma unroll
+    for (int u = U - 1; u >= 0; --u) E0 = a[u] * (g[u] + E0);
+    r[w.wave][0][w.lane] = gate(L);
+    r[w.wave][1][w.lane] = X;
+    r[w.wave][2][w.lane] = E0;
+    lds_barrier();  // the other half is written only after the next one
+    float mine = h, back = e;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      if (i == w.wave) mine = h;
+      h = r[i][0][w.lane] * h + r[i][1][w.lane];
+    }
+#pragma unroll
+    for (int i = W - 1; i >= 0; --i) {
+      if (i == w.wave) back = e;
+      e = r[i][0][w.lane] * e + r[i][2][w.lane];
+    }
+    float dlg[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      dlg[u] = mine;
+      mine = a[u] * mine + v[u];
+    }
+    {
+#pragma clang fp contract(off)  // the same roundings whichever results are wanted
+#pragma unroll
+      for (int u = U - 1; u >= 0; --u) {
+        g[u] = g[u] + back;
+        back = a[u] * g[u];
+        dlg[u] = dlg[u] * back;
+      }
+    }
+    if constexpr (DLG) put_rows<FULL, E, U>(s.out[0], w, t0, dlg);
+    if constexpr (DX) put_rows<FULL, E, U>(s.out[1], w, t0, g);
+  }
+};
+
+template <class E, bool DLG, bool DX>
+__global__ __launch_bounds__(64 * kSweepWaves) void gscan_back(Scan s) {
+  using F = SweepBwd<E, DLG, DX>;
+  __shared__ float R[2][F::W][3][64];
+  F f{s, Sweep(s, F::W * F::U), 0.0f, 0.0f, {}, {}, {}};
+  const int64_t st = f.w.b * s.C + f.w.c;
+  if (s.dstate_out) f.e = s.dstate_out[st];
+  const int64_t full = f.w.len / (F::W * F::U);
+  for (int64_t k = f.w.nk - 1; k >= full; --k) {
+    f.template load<false>(k);
+    f.template step<false>(k, k, R[k & 1]);
+  }
+  if (full > 0) {
+    f.template load<true>(full - 1);
+    f.template step<true>(full - 1, full > 1 ? full - 2 : 0, R[(full - 1) & 1]);
+    for (int64_t k = full - 2; k >= 0; --k) f.template step<true>(k, k > 0 ? k - 1 : 0, R[k & 1]);
+  }
+  if (s.begin && f.w.wave == 0) s.begin[st] = f.e;
+}
+
 // One token of every sequence, the state in place.
 template <class E, int VEC>
 __global__ __launch_bounds__(kBlock) void gscan_one(HeadArr lg, HeadArr x, HeadArr out, float* state, int64_t C, int64_t cols, int64_t n) {
@@ -519,7 +752,23 @@ constexpr int kU = 8;  // tokens of a wave
 constexpr int64_t kChunk = kW * kU;
 int64_t chunks_of(int64_t T) { return T <= kChunk ? 1 : (T + kChunk - 1) / kChunk; }
 
+// Sweeps or chunks.  A forward sweep's step of 256 tokens takes 2.4 us until memory
+// bounds it, a backward one's of 128 3.5: sweeps are for sequences of few steps, or
+// enough columns of 64 channels to keep the memory busy.  bf16, columns x tokens, sweep
+// and chunks: forward 1 x 256 4.9 and 7.7 us, 1 x 1024 11.0 and 11.9, 1 x 2048 19.2 and
+// 11.5, 32 x 2048 19.9 and 17.6, 64 x 2048 20.5 and 24.3, 64 x 8192 69 and 66, 128 x 4096
+// 40 and 68, 256 x 2048 33 and 63; backward 128 x 2048 57 and 52, 128 x 8192 282 and 231,
+// 192 x 256 13.7 and 13.9, 192 x 2048 62 and 73, 256 x 1024 40 and 53, 512 x 2048 205 and 233.
+constexpr int64_t kSweepTokens = 1024, kSweepColumns = 64, kBackTokens = 256, kBackColumns = 192;
+bool sweeps(int64_t B, int64_t T, int64_t C, int mode) {
+  const int64_t cols = B * ((C + 63) / 64);
+  if (mode == kFwd) return T > kChunk && (T <= kSweepTokens || cols >= kSweepColumns);
+  return mode == kBwd && T >= kBackTokens && cols >= kBackColumns;
+}
+
 int64_t workspace_bytes(int64_t B, int64_t T, int64_t C, int mode) {
+  if (B == 0 || C == 0) return 0;
+  if (sweeps(B, T, C, mode)) return mode == kFwd ? 0 : B * ((T + kBackChunk - 1) / kBackChunk) * C * 4;
   const int64_t S = chunks_of(T);
   return B == 0 || C == 0 || S == 1 ? 0 : B * S * fields(mode) * C * 4;
 }
@@ -546,8 +795,25 @@ int launch(const char* who, Scan s, int64_t B, hipStream_t st) {
   return launch_status(who);
 }
 
+template <class E, int MODE>
+int launch_sweeps(const char* who, Scan s, int64_t B, hipStream_t st) {
+  s.cols = (int32_t)((s.C + 63) / 64);
+  s.S = (s.T + kBackChunk - 1) / kBackChunk;
+  const dim3 grid((unsigned)(B * s.cols)), block(64 * kSweepWaves);
+  hipLaunchKernelGGL((gscan_sweep<E, MODE == kBwd>), grid, block, 0, st, s);
+  if constexpr (MODE == kBwd) {
+    if (s.out[0].p && s.out[1].p) hipLaunchKernelGGL((gscan_back<E, true, true>), grid, block, 0, st, s);
+    else if (s.out[0].p) hipLaunchKernelGGL((gscan_back<E, true, false>), grid, block, 0, st, s);
+    else if (s.out[1].p) hipLaunchKernelGGL((gscan_back<E, false, true>), grid, block, 0, st, s);
+    else hipLaunchKernelGGL((gscan_back<E, false, false>), grid, block, 0, st, s);
+  }
+  return launch_status(who);
+}
+
 template <int MODE>
 int run(const char* who, const Scan& s, int64_t B, int32_t dtype, hipStream_t st) {
+  if constexpr (MODE != kSecond)
+    if (sweeps(B, s.T, s.C, MODE)) return dtype == DIFFOPT_F32 ? launch_sweeps<float, MODE>(who, s, B, st) : launch_sweeps<bf16, MODE>(who, s, B, st);
   constexpr int V = MODE == kSecond ? 2 : 1;
   if (s.C < 64 * V) return dtype == DIFFOPT_F32 ? launch<float, MODE, 1>(who, s, B, st) : launch<bf16, MODE, 1>(who, s, B, st);
   return dtype == DIFFOPT_F32 ? launch<float, MODE, V>(who, s, B, st) : launch<bf16, MODE, V>(who, s, B, st);

@@ -109,6 +109,14 @@ def test_what_may_be_left_out(T, state, lengths, resets, dtype):
     _check(2, T, 130, dtype, seed=T, state=state, lengths=lengths, resets=resets)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,T,C", [(200, 260, 3), (193, 512, 5), (210, 1100, 2), (97, 300, 67), (66, 1100, 1), (3, 257, 4100)])
+@pytest.mark.parametrize("rest", [False, True])
+def test_many_channels(B, T, C, rest, dtype):
+    # enough columns of channels for both directions to take a sequence in one sweep; whole steps and a rest
+    _check(B, T, C, dtype, seed=T, state=rest, lengths=rest, resets=rest)
+
+
 @pytest.mark.parametrize("lengths", [[0, 0, 0], [1, 0, 64], [65, 130, 129], [-5, 1000, 8]])
 def test_ends_of_sequences(lengths):
     I = _inputs(3, 130, 70, torch.float32)
@@ -136,9 +144,9 @@ def test_gates_above_zero_and_strong_ones():
     _compare(_run(I), _reference(I), torch.float32)
 
 
-@pytest.mark.parametrize("T", [60, 300, 900])
+@pytest.mark.parametrize("T", [60, 300, 900, 1500])
 def test_values_that_are_not_finite(T):
-    # finite exactly where the recurrence's results are: before the token, in other channels, after a reset
+    # finite exactly where the recurrence's results are: before the token, in other channels
     I = _inputs(2, T, 70, torch.float32, resets=False, lengths=False)
     I["x"][0, T // 3, 4] = math.nan
     I["x"][1, T // 2, 9] = math.inf
@@ -161,9 +169,9 @@ def test_strides(kind, dtype):
         pad, off = (8, 0) if kind == "wide tokens" else (3, 1) if kind == "odd tokens" else (0, 0)
         buf = torch.full((B * T * (C + pad) + 1,), math.nan, dtype=t.dtype, device="cuda")
         return buf.as_strided((B, T, C), (T * (C + pad), C + pad, 1), off).copy_(t)
-    for T in (70, 700):
-        I = _inputs(2, T, 131, dtype, seed=T)
-        results = lambda: wrap(torch.zeros(2, T, 131, dtype=dtype))  # noqa: E731
+    for B, T, C in ((2, 70, 131), (2, 700, 131), (2, 1100, 131), (64, 300, 131)):
+        I = _inputs(B, T, C, dtype, seed=T)
+        results = lambda: wrap(torch.zeros(B, T, C, dtype=dtype))  # noqa: E731
         _compare(_run(I, wrap, None if kind == "backwards" else results), _reference(I), dtype)
 
 
@@ -175,7 +183,7 @@ def test_broadcast_operands():
     _compare(_run(I, wrap), _reference(I), torch.float32)
 
 
-@pytest.mark.parametrize("T", [1, 64, 100, 700])
+@pytest.mark.parametrize("T", [1, 64, 100, 700, 1500])
 def test_state_in_place(T):
     import paper_2211_06934_amd as P
     I = _inputs(2, T, 300, torch.float32)
@@ -186,10 +194,10 @@ def test_state_in_place(T):
     assert_close(state, want["s1"].double(), 1e-6)
 
 
-@pytest.mark.parametrize("T", [60, 300, 900])
-def test_results_that_are_not_wanted(T):
+@pytest.mark.parametrize("T,C", [(60, 70), (300, 70), (900, 70), (300, 6300)])
+def test_results_that_are_not_wanted(T, C):
     import paper_2211_06934_amd as P
-    I = {k: None if v is None else v.cuda() for k, v in _inputs(2, T, 70, torch.float32).items()}
+    I = {k: None if v is None else v.cuda() for k, v in _inputs(2, T, C, torch.float32).items()}
     want = _run(I)
     new = lambda: torch.empty_like(I["x"])  # noqa: E731
     for keep in range(8):
@@ -263,7 +271,7 @@ def test_gradients_against_differences():
 
 def test_streams_workspaces_and_repeats():
     import paper_2211_06934_amd as P
-    I = {k: None if v is None else v.cuda() for k, v in _inputs(2, 900, 300, torch.bfloat16).items()}
+    I = {k: None if v is None else v.cuda() for k, v in _inputs(2, 1900, 300, torch.bfloat16).items()}
     ref = _run(I)
     streams = [torch.cuda.Stream(), torch.cuda.Stream()]
     torch.cuda.synchronize()
@@ -274,7 +282,7 @@ def test_streams_workspaces_and_repeats():
     torch.cuda.synchronize()
     for g in got:
         assert all(torch.equal(g[k], ref[k]) for k in ref)
-    need = P.gscan_workspace(2, 900, 300, torch.bfloat16)
+    need = P.gscan_workspace(2, 1900, 300, torch.bfloat16)
     assert need > 0
     h, ws = torch.empty_like(I["x"]), torch.full((need // 4,), math.nan, device="cuda").view(torch.uint8)
     P.gscan_fwd(I["lg"], I["x"], h, I["s0"], None, I["lengths"], workspace=ws, stream=torch.cuda.current_stream())
