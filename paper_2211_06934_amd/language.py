@@ -185,16 +185,17 @@ class GatedScanFn(torch.autograd.Function):
         if dh is None and ds1 is None:
             return (None,) * 5
         dh = torch.zeros(x.shape, dtype=x.dtype, device=x.device) if dh is None else _dense(dh)
-        return (*GatedScanGradFn.apply(dh, _whole(ds1), log_gate, x, state, lengths), None, None)
+        want = (*ctx.needs_input_grad[:2], ctx.needs_input_grad[2] and state is not None)
+        return (*GatedScanGradFn.apply(dh, _whole(ds1), log_gate, x, state, lengths, want), None, None)
 
 
 class GatedScanGradFn(torch.autograd.Function):
-    """(dh, dstate_out, log_gate, x, state) -> (dlog_gate, dx, dstate)."""
+    """(dh, dstate_out, log_gate, x, state) -> (dlog_gate, dx, dstate), those that `want` names."""
 
     @staticmethod
-    def forward(ctx, dh, ds1, log_gate, x, state, lengths):
-        dg, dx = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for _ in range(2))
-        ds = None if state is None else torch.empty_like(state)
+    def forward(ctx, dh, ds1, log_gate, x, state, lengths, want):
+        dg, dx = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if w else None for w in want[:2])
+        ds = torch.empty_like(state) if want[2] else None
         _o.gscan_bwd(dh, log_gate, x, dg, dx, state, ds1, ds, lengths)
         ctx.save_for_backward(dh, ds1, log_gate, x, state, lengths)
         ctx.set_materialize_grads(False)
@@ -205,13 +206,13 @@ class GatedScanGradFn(torch.autograd.Function):
     def backward(ctx, r, p, s):
         dh, ds1, log_gate, x, state, lengths = ctx.saved_tensors
         if r is None and p is None and s is None:
-            return (None,) * 6
+            return (None,) * 7
         new = lambda like: torch.empty(like.shape, dtype=like.dtype, device=like.device)
         zero = lambda c: torch.zeros(x.shape, dtype=x.dtype, device=x.device) if c is None else _dense(c)
         oh, og, ox = new(x), new(x), new(x)
         o1, o0 = (None if like is None else new(like) for like in (ds1, state))
         _o.gscan_bwd_bwd(zero(r), zero(p), dh, log_gate, x, oh, og, ox, state, ds1, _whole(s), o1, o0, lengths)
-        return oh, o1, og, ox, o0, None
+        return oh, o1, og, ox, o0, None, None
 
 
 def gated_scan(log_gate, x, state=None, lengths=None, return_state: bool = False):

@@ -118,6 +118,13 @@ def test_alternatives(K, ids64):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,V", [(1, 150001), (40, 70003), (2, 17000), (300, 10000), (2, 300001)])
+def test_most_alternatives(N, V, dtype):
+    # cut rows and whole ones, workgroups of each size
+    _check(N, V, 128, dtype, seed=N)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("N", [1, 2, 9, 300, 2000])
 def test_rows(N, dtype):
     _check(N, 501, 5, dtype, seed=N)

@@ -198,6 +198,16 @@ def test_expanded_operands_and_cotangents():
         assert_close(got, want, F32)
     for got, want in zip(second, torch.autograd.grad(sum((g * g).sum() for g in ref), [a, b, c])):
         assert_close(got, want, 3 * F32)
+    # one operand alone
+    for i, (args, want) in enumerate((((a, b.detach()), a), ((a.detach(), b), b))):
+        ours = [t.detach().float().cuda() for t in (a, b)]
+        ours[i].requires_grad_(True)
+        (got,) = torch.autograd.grad(P.gated_scan(ours[0].expand(3, 12, -1), ours[1]).square().sum(), [ours[i]], create_graph=True)
+        (twice,) = torch.autograd.grad(got.square().sum(), [ours[i]])
+        r0 = _scan(args[0].expand(3, 12, -1), args[1], torch.zeros(3, 20, dtype=torch.float64), torch.full((3,), 12))[0]
+        (ref0,) = torch.autograd.grad(r0.square().sum(), [want], create_graph=True)
+        assert_close(got, ref0, 3 * F32)
+        assert_close(twice, torch.autograd.grad(ref0.square().sum(), [want])[0], 9 * F32)
     # the state alone, and nothing but h
     (only,) = torch.autograd.grad(P.gated_scan(lg.expand(3, 12, -1), x, s0.expand(3, -1), return_state=True)[1].sum(), [s0])
     assert_close(only, torch.autograd.grad(_scan(a.expand(3, 12, -1), b, c.expand(3, -1), torch.full((3,), 12))[1].sum(), [c])[0], F32)
