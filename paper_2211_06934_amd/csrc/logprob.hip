@@ -26,6 +26,9 @@ constexpr int kLB = 512;     // threads per workgroup of a streamed row
 constexpr int kJB = 256;     // ... of a row's joined slices
 constexpr int kMaxTop = 128;
 constexpr int kCap = 1024;   // candidates that are ranked
+// Comparisons of a lane from which on the lowest candidates are left out first: 8,000
+// rows of 500 bf16 logits with 64 alternatives 43 us, ranked as they are 246.
+constexpr int kRanking = 640;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLow = -256.0f;  // 2^d is 0 from here on: 0 log 0 = 0, whatever d is
 
@@ -148,6 +151,7 @@ struct Share {
   __device__ __forceinline__ bool has_single(int32_t lane) const { return lane < n - nv * N; }
   __device__ __forceinline__ int64_t single(int32_t lane) const { return c0 + (lane < head ? lane : lane + (int64_t)nv * N); }
   // what a lane has, for the others to look at
+  static constexpr bool kOwn = false;
   __device__ __forceinline__ int32_t items() const { return (nv + B - 1) / B + 1; }
   template <class F>
   __device__ __forceinline__ void item(int32_t lane, int32_t j, F f) const {
@@ -188,6 +192,32 @@ __device__ __forceinline__ void row_sums(const Share<E_, B>& sh, float c, Sums& 
       if (i + a * B < sh.nv) sums.template piece<N, ENT>(e[a], c);
   }
   if (single) sums.template piece<1, ENT>(&one, c);
+}
+
+// A lane's sums over a row that stays in registers.  d is (x - m) c, not x c - m c
+// in one instruction: the largest logit's e is 1, so that no probability is above 1
+// and that of a row's only token is.
+template <bool ENT, class E_, int B, int NV>
+__device__ __forceinline__ void kept_sums(const Kept<E_, B, NV>& kept, float c, Sums& sums) {
+  constexpr int N = Vec<E_>::N;
+  float top = (float)kept.single;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float e[N];
+    kept.get(i, e);
+#pragma unroll
+    for (int k = 0; k < N; k += 2) top = fmaxf(fmaxf(top, e[k]), e[k + 1]);
+  }
+  sums.m = top;
+  const float b = safe_max(top);
+  sums.add<ENT>((float)kept.single, b, c);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    float e[N];
+    kept.get(i, e);
+#pragma unroll
+    for (int k = 0; k < N; ++k) sums.add<ENT>(e[k], b, c);
+  }
 }
 
 // ---- alternatives -----------------------------------------------------------
@@ -235,10 +265,31 @@ __device__ __forceinline__ uint32_t floor_of(const Select& S, int K) {
   return floor << 16;
 }
 
-// The K largest of what a workgroup of B lanes shares: of(lane, j, f) calls
-// f(value, id) for item j < items() of a lane, largest is the largest value of this
-// lane's; emit(rank, value, id) takes the results, (-inf, -1) where fewer values
-// are above -inf.
+// ... that K of the n candidates reach.  Lanes count their own: with a ballot for
+// each number the kernel takes more than 80 scalar registers, and a SIMD has
+// seven waves instead of eight (2,048 rows of 50,021 logits: 46 us instead of 42).
+__device__ __forceinline__ uint32_t floor_of_found(const Select& S, int n, int K) {
+  constexpr int G = kCap / 64;
+  uint32_t k[G], floor = 0;
+#pragma unroll
+  for (int g = 0; g < G; ++g) k[g] = 64 * g + (int)threadIdx.x < n ? (uint32_t)(S.found[64 * g + threadIdx.x] >> 48) : 0;
+#pragma unroll 1
+  for (int bit = 15; bit >= 0; --bit) {
+    const uint32_t more = floor | 1u << bit;
+    int reached = 0;
+#pragma unroll
+    for (int g = 0; g < G; ++g) reached += k[g] >= more;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) reached += __shfl_xor(reached, o, 64);
+    if (reached >= K) floor = more;
+  }
+  return floor;
+}
+
+// The K largest of what a workgroup of B lanes shares: of.item(lane, j, f) calls
+// f(value, id) for item j < items() of a lane, or (kOwn) of.each(f) for all of this
+// lane's; largest is the largest value of this lane's; emit(rank, value, id) takes
+// the results, (-inf, -1) where fewer values are above -inf.
 template <int B, class Of, class Emit>
 __device__ __forceinline__ void select_top(Select& S, int K, float largest, const Of& of, Emit emit) {
   const int tid = threadIdx.x;
@@ -252,7 +303,13 @@ __device__ __forceinline__ void select_top(Select& S, int K, float largest, cons
   }
   __syncthreads();
   const uint32_t floor = S.floor;
-  const int items = of.items();
+  const auto mine = [&](auto f) {
+    if constexpr (Of::kOwn) {
+      of.each(f);
+    } else {
+      for (int j = 0; j < of.items(); ++j) of.item(tid, j, f);
+    }
+  };
   const auto put = [&](uint64_t from) {
     return [&S, from](float v, int64_t id) {
       const uint64_t k = key_of(v, id);
@@ -262,12 +319,25 @@ __device__ __forceinline__ void select_top(Select& S, int K, float largest, cons
       }
     };
   };
-  if (own >= floor) S.lane[atomicAdd(&S.lanes, 1u)] = (uint16_t)tid;
-  __syncthreads();
-  // all lanes share what those lanes have: one round trip to the caches, not one an item
-  for (int i = tid; i < (int)S.lanes * items; i += B) {
-    const int l = i / items;
-    of.item(S.lane[l], i - l * items, put((uint64_t)floor << 32));
+  if constexpr (Of::kOwn) {
+    if (own >= floor) {
+      const float least = floor > key_of(-kInf) ? value_of(floor) : -__FLT_MAX__;
+      of.each([&](float v, int64_t id) {
+        if (v >= least) {
+          const uint32_t i = atomicAdd(&S.count, 1u);
+          if (i < kCap) S.found[i] = key_of(v, id);
+        }
+      });
+    }
+  } else {
+    if (own >= floor) S.lane[atomicAdd(&S.lanes, 1u)] = (uint16_t)tid;
+    __syncthreads();
+    // all lanes share what those lanes have: one round trip to the caches, not one an item
+    const int items = of.items();
+    for (int i = tid; i < (int)S.lanes * items; i += B) {
+      const int l = i / items;
+      of.item(S.lane[l], i - l * items, put((uint64_t)floor << 32));
+    }
   }
   __syncthreads();
   if (S.count > kCap) {  // the same for all lanes; the K-th key digit by digit, until at most kCap keys are not below it
@@ -277,11 +347,10 @@ __device__ __forceinline__ void select_top(Select& S, int K, float largest, cons
       __syncthreads();
       for (int i = tid; i < 256; i += B) S.hist[i] = 0;
       __syncthreads();
-      for (int j = 0; j < items; ++j)
-        of.item(tid, j, [&](float v, int64_t id) {
-          const uint64_t k = key_of(v, id);
-          if (v > -kInf && (shift == 56 || k >> (shift + 8) == prefix >> (shift + 8))) atomicAdd(&S.hist[k >> shift & 255], 1u);
-        });
+      mine([&](float v, int64_t id) {
+        const uint64_t k = key_of(v, id);
+        if (v > -kInf && (shift == 56 || k >> (shift + 8) == prefix >> (shift + 8))) atomicAdd(&S.hist[k >> shift & 255], 1u);
+      });
       __syncthreads();
       if (tid == 0) {
         uint32_t n = left;
@@ -297,13 +366,33 @@ __device__ __forceinline__ void select_top(Select& S, int K, float largest, cons
       left = S.left;
       if (S.enough || shift == 0) break;
     }
-    for (int j = 0; j < items; ++j) of.item(tid, j, put(prefix));
+    mine(put(prefix));
     __syncthreads();
   }
-  const int n = (int)(S.count < kCap ? S.count : kCap);
+  int n = __builtin_amdgcn_readfirstlane((int)(S.count < kCap ? S.count : kCap));
+  if (n > K && n * ((n + B - 1) / B) > kRanking) {  // few groups of lanes for K, or few that hold values: the lowest candidates are left out first
+    uint64_t k[kCap / B];
+#pragma unroll
+    for (int j = 0; j < kCap / B; ++j) k[j] = tid + j * B < n ? S.found[tid + j * B] : 0;
+    if (tid < 64) {
+      const uint32_t cut = floor_of_found(S, n, K);
+      if (tid == 0) {
+        S.floor = cut;
+        S.count = 0;
+      }
+    }
+    __syncthreads();
+    const uint32_t cut = S.floor;
+#pragma unroll
+    for (int j = 0; j < kCap / B; ++j)
+      if (tid + j * B < n && (uint32_t)(k[j] >> 48) >= cut) S.found[atomicAdd(&S.count, 1u)] = k[j];
+    __syncthreads();
+    n = __builtin_amdgcn_readfirstlane((int)S.count);
+  }
   for (int i = tid; i < n; i += B) {
     const uint64_t k = S.found[i];
     int rank = 0;
+#pragma unroll 8
     for (int j = 0; j < n; ++j) rank += S.found[j] > k;
     if (rank < K) emit(rank, value_of((uint32_t)(k >> 32)), (int64_t)(0xffffffffu - (uint32_t)k));
   }
@@ -410,11 +499,53 @@ __global__ __launch_bounds__(B) void logprob_row(Rows r, Results o, Parts parts)
   if constexpr (TOP) finish_top<B>(r, o, S, sl.row, tok, sums, largest, share);
 }
 
+// What a lane has of a row that stays in registers.
+template <class E_, int B, int NV>
+struct OwnPieces {
+  const Kept<E_, B, NV>& kept;
+  static constexpr bool kOwn = true;
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+    if (kept.has_single) f((float)kept.single, (int64_t)kept.at_single);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (kept.has(i)) {
+        float e[Vec<E_>::N];
+        kept.get(i, e);
+#pragma unroll
+        for (int k = 0; k < Vec<E_>::N; ++k) f(e[k], (int64_t)(kept.at(i) + k));
+      }
+  }
+};
+
+// A short row of many, read once.
+template <class E_, bool ENT, bool TOP, int B, int NV>
+__global__ __launch_bounds__(B, kept_waves(B, NV)) void logprob_kept(Rows r, Results o) {
+  __shared__ float R[kMaxWaves][3];
+  __shared__ std::conditional_t<TOP, Select, int> S;
+  const int64_t row = blockIdx.x;
+  const Token tok = token_of(r, row);
+  const E_* x = static_cast<const E_*>(r.logits) + row * r.row_stride;
+  const float c = r.invT * kLog2e;
+  Kept<E_, B, NV> kept;
+  Sums sums;
+  if (tok.live) {
+    kept.place(x, (uint32_t)r.V);
+    kept.load(x, (E_)-kInf);
+    kept_sums<ENT>(kept, c, sums);
+  }
+  const float largest = sums.m;
+  sums.all<ENT>(R, c);
+  if (threadIdx.x == 0) finish(r, o, row, tok, tok.id >= 0 ? (float)x[tok.id] : 0.0f, sums);
+  if constexpr (TOP) finish_top<B>(r, o, S, row, tok, sums, largest, OwnPieces<E_, B, NV>{kept});
+}
+
 // What the slices of a row found, shared by the lanes that join them.
 struct Found {
   const Parts& parts;
   int64_t first;
   int32_t n;
+  static constexpr bool kOwn = false;
   __device__ __forceinline__ int32_t items() const { return (n + kJB - 1) / kJB; }
   template <class F>
   __device__ __forceinline__ void item(int32_t lane, int32_t j, F f) const {
@@ -501,14 +632,6 @@ __device__ __forceinline__ float off(const Shift& sh) {
   return WIDE ? 0.0f : -__builtin_fmaf(sh.b, sh.c, -sh.bc);
 }
 
-// t + s o in two roundings: where one token is left, t is -s o rounded and the
-// entropy 0, not what a multiply-add would leave.
-__device__ __forceinline__ float plus_product(float t, float s, float o) {
-#pragma clang fp contract(off)
-  const float so = s * o;
-  return t + so;
-}
-
 // The dense part of a row's gradient, -(p / T)(G + h (l + H)) with l + H = ln 2 (d
 // + off) - log s + H, as w e (A + B d).
 struct Dense {
@@ -559,40 +682,7 @@ __global__ __launch_bounds__(B, (STATS == kKept ? kept_waves(B, NV) : 1)) void l
     if constexpr (STATS == kRead) row_sums<E_, B, ENT>(Share<E_, B>(x, 0, r.V), c, sums);
     if constexpr (STATS == kParts)
       for (int i = threadIdx.x; i < parts.slices; i += B) sums.join<ENT>(parts.get(row * parts.slices + i), c);
-    if constexpr (STATS == kKept) {
-      float top = (float)kept.single;
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        float e[N];
-        kept.get(i, e);
-#pragma unroll
-        for (int k = 0; k < N; k += 2) top = fmaxf(fmaxf(top, e[k]), e[k + 1]);
-      }
-      sums.m = top;
-      const Shift sh(safe_max(top), c);
-      const auto sum = [&](auto wide) {
-        const auto one = [&](float v) {
-          const float d = depth<wide.value>(sh, v), e = exp2_fast(d);
-          sums.s += e;
-          if (ENT) sums.t = __builtin_fmaf(e, fmaxf(d, kLow), sums.t);
-        };
-        one((float)kept.single);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          float e[N];
-          kept.get(i, e);
-#pragma unroll
-          for (int k = 0; k < N; ++k) one(e[k]);
-        }
-        const float f = sh.factor<wide.value>();
-        if (ENT) sums.t = f * plus_product(sums.t, sums.s, off<wide.value>(sh));
-        sums.s *= f;
-      };
-      if (__any(sh.wide))
-        sum(std::true_type{});
-      else
-        sum(std::false_type{});
-    }
+    if constexpr (STATS == kKept) kept_sums<ENT>(kept, c, sums);
   }
   float H = 0.0f;
   if constexpr (STATS == kGiven) {
@@ -938,6 +1028,12 @@ Cut row_cut(int64_t N, int64_t V, int32_t dtype) { return cut_of(N, V, dtype, 16
 // with 128, 28.5 with 256 and 51.6 with 512; 4,000 of 16,000 31.5, 31.5 and 38.0; 2,048
 // of 50,021 42.0, 41.8 and 41.9 (without alternatives 38 with 512, 43 with 256).
 constexpr int64_t kShortRow = 16384, kMiddleRow = 65536;
+// Many short rows stay in registers: their maximum is known before the sums, and the
+// alternatives are looked for in the lanes that read them.  8,000 rows of 4,000 bf16
+// logits 15.1 us (streamed 19.7), with 5 alternatives 24.0 (26.2); 4,000 of 16,000 without
+// 23.1 (28.5), with 5 50 (31); of more than 64 KiB and of few rows streaming is as fast or
+// faster (300 of 1,000 fp32 logits 4.8 against 5.7, 2,048 of 50,021 39.7 against 41.7).
+constexpr int64_t kKeptRows = 2048;
 
 int64_t parts_bytes(int64_t N, int64_t V, int32_t dtype, int64_t K) {
   const Cut c = row_cut(N, V, dtype);
@@ -961,6 +1057,21 @@ int fwd_rows(const char* who, const Rows& r, int32_t dtype, const Results& o, vo
   const Cut c = row_cut(r.N, r.V, dtype);
   const Parts p = parts_of(c, TOP ? o.K : 0, workspace);
   const int64_t bytes = r.V * elem_size(dtype);  // of a row: slices are for few rows, whose time is latency
+#define DIFFOPT_KEPT(B, NV)                                                    \
+  if (bytes <= (int64_t)B * NV * 16) {                                         \
+    DIFFOPT_LAUNCH((logprob_kept<E_, ENT, TOP, B, NV>), r.N, B, r, o);         \
+    return launch_status(who);                                                 \
+  }
+  if (r.N >= kKeptRows && c.slices == 1) {
+    DIFFOPT_KEPT(128, 2)
+    DIFFOPT_KEPT(128, 4)
+    if constexpr (!TOP) {
+      DIFFOPT_KEPT(128, 8)
+      DIFFOPT_KEPT(256, 8)
+      DIFFOPT_KEPT(256, 16)
+    }
+  }
+#undef DIFFOPT_KEPT
   if (bytes <= kShortRow) DIFFOPT_LAUNCH((logprob_row<E_, ENT, TOP, 128>), r.N * c.slices, 128, r, o, p);
   else if (bytes <= kMiddleRow) DIFFOPT_LAUNCH((logprob_row<E_, ENT, TOP, 256>), r.N * c.slices, 256, r, o, p);
   else DIFFOPT_LAUNCH((logprob_row<E_, ENT, TOP, kLB>), r.N * c.slices, kLB, r, o, p);

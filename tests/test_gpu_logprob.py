@@ -5,6 +5,7 @@ import math
 import pytest
 import torch
 
+import paper_2211_06934_amd as P
 from lm_reference import F32, assert_close, tol
 
 pytestmark = pytest.mark.gpu
@@ -128,6 +129,35 @@ def test_most_alternatives(N, V, dtype):
 @pytest.mark.parametrize("N", [1, 2, 9, 300, 2000])
 def test_rows(N, dtype):
     _check(N, 501, 5, dtype, seed=N)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,V,K", [(2100, 1, 1), (2100, 37, 64), (2100, 500, 0), (2100, 500, 64), (2300, 900, 128), (2100, 2049, 5), (2100, 4090, 20), (2100, 4090, 0),
+                                   (2049, 8193, 0), (2049, 9001, 128), (2100, 16001, 0), (2100, 30011, 0), (2047, 500, 20), (3, 700, 128)])
+@pytest.mark.parametrize("values", ["all", "few", "one"])
+def test_many_rows(N, V, K, values, dtype):
+    # short rows whose results come from registers; values that many tokens share
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    x = 2.5 * torch.randn(N, V + 3, generator=gen, device="cuda")
+    x = (x.round() if values == "few" else torch.ones_like(x) if values == "one" else x).to(dtype)[:, 1 : V + 1]
+    x[5 % N, 1:] = -math.inf
+    ids = torch.randint(0, V, (N,), generator=gen, device="cuda")
+    ids[1], ids[5 % N] = -1, 0
+    lp, en, stats, tops = (torch.full(n, math.nan, device="cuda") for n in ((N,), (N,), (N, 2), (N, K)))
+    tids = torch.full((N, K), 77, dtype=torch.int64, device="cuda")
+    P.logprob_fwd(x, ids, lp, stats, en, tops if K else None, tids if K else None, 0.8)
+    raw = x.double()
+    ref = torch.log_softmax(raw / 0.8, 1)
+    there = ids >= 0
+    assert_close(lp, torch.where(there, ref.gather(1, ids.clamp(min=0)[:, None])[:, 0], 0.0), F32)
+    assert_close(en, torch.where(there, -(ref.exp() * torch.where(raw == -math.inf, 0.0, ref)).sum(1), 0.0), F32)
+    order = torch.sort(raw, dim=1, descending=True, stable=True).indices[:, :K]
+    value = ref.gather(1, order)
+    order = torch.where((value == -math.inf) | ~there[:, None], -1, order)
+    n = order.shape[1]
+    assert torch.equal(tids[:, :n], order) and bool((tids[:, n:] == -1).all())
+    assert torch.equal(tops == -math.inf, tids < 0)
+    assert_close(torch.where(order < 0, 0.0, tops[:, :n].double()), torch.where(order < 0, 0.0, value), F32)
 
 
 @pytest.mark.parametrize("T", [0.25, 1.0, 7.5])
