@@ -274,10 +274,10 @@ __global__ __launch_bounds__(64 * kW) void gscan_runs(Scan s) {
 // Chunks' runs become the states that enter each chunk: kX holds h, kY y, kE e
 // and kF f.  A workgroup has 64 channels of a sequence, its waves share the
 // chunks.
-constexpr int kJW = 16, kBatch = 8;
+constexpr int kJW = 16;
 template <int MODE>
 __global__ __launch_bounds__(64 * kJW) void gscan_join(Scan s) {
-  constexpr int NF = fields(MODE);
+  constexpr int NF = fields(MODE), kBatch = MODE == kFwd ? 16 : 8;
   __shared__ float v[kJW][NF][64];
   const int64_t cols = (s.C + 63) / 64, b = blockIdx.x / cols;
   const int lane = threadIdx.x & 63, wave = wave_of();
@@ -603,7 +603,8 @@ struct SweepFwd {
     }
     r[w.wave][0][w.lane] = gate(L);
     r[w.wave][1][w.lane] = X;
-    lds_barrier();  // the other half is written only after the next one
+    asm volatile("" : "+v"(h));  // the state has arrived: past the barrier its place may be written
+    lds_barrier();               // the other half is written only after the next one
     float mine = h;
 #pragma unroll
     for (int i = 0; i < W; ++i) {
