@@ -4,17 +4,20 @@
 // Two launches: partial sums in fp64, one a workgroup, in an order that the
 // sizes alone decide; then every wave adds the few hundred partial sums while
 // its elements are on their way, and scales them (a launch of its own that makes
-// them one costs more: 20M elements 40.3 us against 38.7, 354M 754 against 745).  fp64 holds a square of any
-// fp32 value and its sum to far below an fp32 rounding, at no cost: two
-// instructions for an element of four bytes.  Bound by memory, the elements
-// being read twice; the second pass goes backwards, so that it begins with
-// what the first one left in the Infinity Cache.
+// them one costs more: 20M elements 40.3 us against 38.7, 354M 754 against 745).
+// fp64 holds a square of any fp32 value and its sum to far below an fp32 rounding,
+// at no cost: two instructions for an element of four bytes.  Bound by memory, the
+// elements being read twice; the second pass goes backwards, so that it begins
+// with what the first one left in the Infinity Cache.  A tree of 354M elements: the
+// sums read 6.0 TB/s, the second pass moves 5.8.
 //
 // A wave takes one tile of the segment table (512 groups of four elements).  A
 // tile inside one leaf reads that leaf's entry with scalar loads; others stage
-// their window of the table in the wave's own LDS and search it, so that waves
-// never wait for one another.  Gradients of up to kAlone elements take one
-// launch of one workgroup, which keeps them in registers.
+// their window of the table in the wave's own LDS and search it, so that
+// waves never wait for one another.  The sums look up a wave's next tile while this
+// one's elements are on their way (20M elements in 3,384 leaves 20.7 us, looked
+// up afterwards 26.9).  Gradients of up to kAlone elements take one launch of one
+// workgroup, which keeps them in registers.
 #include <cmath>
 #include <initializer_list>
 #include <type_traits>
@@ -26,12 +29,10 @@ namespace diffopt {
 namespace {
 
 constexpr int kScaleBlock = 256, kScaleWaves = kScaleBlock / 64;
-// Waves of a workgroup of sums, and how many workgroups there are at most.  One
-// large workgroup a compute unit is best for long runs of tiles (354M elements:
-// 235 us; 2 of 8 waves 243, 4 of 8 250, 8 of 4 257), more and smaller ones where
-// there are few (2M in 338 leaves: 11.8 us, 2 of 8 waves 10.4).
-constexpr int kManyWaves = 16, kManyParts = 256, kFewWaves = 8, kMostParts = 512;
-constexpr int64_t kManyTiles = 16384;
+// Waves of a workgroup of sums, and how many workgroups there are at most: one large
+// one a compute unit (trees of 354M and of 20M elements 236 and 20.8 us; 512 workgroups of
+// 8 waves 256 and 20.7, 256 of them 231 and 23.1).
+constexpr int kSumWaves = 16, kMostParts = 256;
 constexpr int kGroups = (int)(kTileGroups / 64);  // of a lane
 constexpr int kAloneBlock = 1024, kAloneEach = 8;
 constexpr int64_t kAlone = kAloneBlock * kAloneEach;
@@ -72,15 +73,14 @@ __device__ __forceinline__ void wave_sync() {  // LDS written by the wave's lane
 // PH's leaf (PH < 0: from the leaf), so that stores fill lines.
 template <bool FLAT, int NA, int PH>
 struct Tile {
-  const Space& sp;
-  Window<NA>& win;
+  Window<NA>* win;
   Leaf<NA> one;  // of a tile inside one leaf
   int64_t first;
   int W;         // leaves of the window; 0: one leaf
   int mine, lane;  // window place of the leaf that has the lane's eight consecutive groups
 
-  __device__ __forceinline__ Tile(const Space& sp_, const Operands<NA>& ops, Window<NA>& win_, int64_t b, int lane_)
-      : sp(sp_), win(win_), one{0, sp_.n, {}}, first(b * kTileGroups + lane_), W(0), mine(0), lane(lane_) {
+  __device__ __forceinline__ Tile(const Space& sp, const Operands<NA>& ops, Window<NA>& window, int64_t b, int lane_)
+      : win(&window), one{0, sp.n, {}}, first(b * kTileGroups + lane_), W(0), mine(0), lane(lane_) {
     if constexpr (FLAT) {
 #pragma unroll
       for (int q = 0; q < NA; ++q) one.p[q] = reinterpret_cast<uint64_t>(ops.a[q]);
@@ -104,10 +104,10 @@ struct Tile {
       uint64_t v[NA];
 #pragma unroll
       for (int q = 0; q < NA; ++q) v[q] = static_cast<const uint64_t*>(ops.a[q])[decltype(dense)::value ? j0 + t : e.orig];
-      win.goff[t] = e.goff;
-      win.numel[t] = e.numel;
+      win->goff[t] = e.goff;
+      win->numel[t] = e.numel;
 #pragma unroll
-      for (int q = 0; q < NA; ++q) win.p[q][t] = v[q];
+      for (int q = 0; q < NA; ++q) win->p[q][t] = v[q];
     };
     for (int t = lane; t < W; t += 64)
       if (sp.dense_orig) stage(t, std::true_type{});
@@ -119,7 +119,7 @@ struct Tile {
     int hi = W - 1;  // goff[0] <= g
     while (mine < hi) {
       const int mid = (mine + hi + 1) >> 1;
-      if (win.goff[mid] <= g) mine = mid;
+      if (win->goff[mid] <= g) mine = mid;
       else hi = mid - 1;
     }
   }
@@ -127,9 +127,9 @@ struct Tile {
   __device__ __forceinline__ Leaf<NA> find(int u) const {
     if (FLAT || W == 0) return one;
     const int lo = __shfl(mine, u * (64 / (int)kLeafGroupAlign) + lane / (int)kLeafGroupAlign, 64);
-    Leaf<NA> leaf{win.goff[lo], win.numel[lo], {}};
+    Leaf<NA> leaf{win->goff[lo], win->numel[lo], {}};
 #pragma unroll
-    for (int q = 0; q < NA; ++q) leaf.p[q] = win.p[q][lo];
+    for (int q = 0; q < NA; ++q) leaf.p[q] = win->p[q][lo];
     return leaf;
   }
 
@@ -208,18 +208,20 @@ __device__ __forceinline__ double wave_sum(double x) {
 // Partial sums of a b over the operands' elements (b = a with one operand).
 // With two, nothing is read where stats says that the gradient was not clipped:
 // the sum has no weight then.
-template <bool FLAT, int NA, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, (NA == 1 ? 8 : 4)) void clip_sums(Space sp, Operands<NA> ops, const float* stats, double* parts) {
-  __shared__ std::conditional_t<FLAT, char, Window<NA>> windows[WAVES];
-  __shared__ double sums[WAVES];
+template <bool FLAT, int NA>
+__global__ __launch_bounds__(64 * kSumWaves, 4) void clip_sums(Space sp, Operands<NA> ops, const float* stats, double* parts) {
+  __shared__ std::conditional_t<FLAT, char, Window<NA>> windows[kSumWaves][2];
+  __shared__ double sums[kSumWaves];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   double acc[2] = {0.0, 0.0};
   static_assert(kGroups * 4 == 32, "a lane's elements are the bits of a word");
   const bool skip = NA == 2 && stats[1] >= 1.0f;
+  using T = Tile<FLAT, NA, FLAT ? 0 : -1>;
+  const auto tile_at = [&](int64_t b, int half) { return T(sp, ops, reinterpret_cast<Window<NA>&>(windows[FLAT ? 0 : wave][FLAT ? 0 : half]), b, lane); };
   // wave after wave takes a tile, workgroup after workgroup: neighbouring tiles are read together
-  if (!skip)
-    for (int64_t b = (int64_t)wave * gridDim.x + blockIdx.x; b < sp.ntiles; b += (int64_t)gridDim.x * WAVES) {
-      const Tile<FLAT, NA, FLAT ? 0 : -1> tile(sp, ops, reinterpret_cast<Window<NA>&>(windows[FLAT ? 0 : wave]), b, lane);
+  int64_t b = (int64_t)wave * gridDim.x + blockIdx.x;
+  if (!skip && b < sp.ntiles)
+    for (T tile = tile_at(b, 0), next = tile;; tile = next) {
       f32x4 v[NA][kGroups];
       uint32_t own = 0;  // four bits a group
       const uint64_t dummy = FLAT ? reinterpret_cast<uint64_t>(ops.a[0]) : reinterpret_cast<uint64_t>(sp.seg);  // 16 bytes that are there
@@ -228,6 +230,9 @@ __global__ __launch_bounds__(64 * WAVES, (NA == 1 ? 8 : 4)) void clip_sums(Space
 #pragma unroll
         for (int q = 0; q < NA; ++q) v[q][u] = load4(o ? leaf.p[q] : dummy, o ? w : 0);
       });
+      b += (int64_t)gridDim.x * kSumWaves;
+      const bool more = b < sp.ntiles;
+      if (more) next = tile_at(b, tile.win == reinterpret_cast<Window<NA>*>(&windows[FLAT ? 0 : wave][0]));  // its leaves are found while the elements are on their way
       if (!__all(own == ~0u)) {
 #pragma unroll
         for (int u = 0; u < kGroups; ++u)
@@ -246,14 +251,15 @@ __global__ __launch_bounds__(64 * WAVES, (NA == 1 ? 8 : 4)) void clip_sums(Space
           const double x = gaddr<const float>(leaf.p[0])[i], y = gaddr<const float>(leaf.p[NA - 1])[i];
           acc[0] += x * y;
         });
-      if constexpr (!FLAT) wave_sync();  // before the next tile's window
+      if (!more) break;
+      if constexpr (!FLAT) wave_sync();  // this tile's window is the one after the next's
     }
   const double sum = wave_sum(acc[0] + acc[1]);
   if (lane == 0) sums[wave] = sum;
   __syncthreads();
   if (threadIdx.x == 0) {
     double all = 0.0;
-    for (int w = 0; w < WAVES; ++w) all += sums[w];
+    for (int w = 0; w < kSumWaves; ++w) all += sums[w];
     parts[blockIdx.x] = all;
   }
 }
@@ -463,10 +469,8 @@ struct Elements {
   int64_t count() const { return table ? table->elems : n; }
   int64_t tiles() const { return table ? table->ntiles : ((n + 3) / 4 + 8 + kTileGroups - 1) / kTileGroups; }
   bool alone() const { return count() <= kAlone && (!table || table->tiny); }
-  bool many() const { return tiles() >= kManyTiles; }
   int32_t parts() const {
-    if (many()) return kManyParts;
-    const int64_t blocks = (tiles() + kFewWaves - 1) / kFewWaves;
+    const int64_t blocks = (tiles() + kSumWaves - 1) / kSumWaves;
     return (int32_t)(blocks < kMostParts ? blocks : kMostParts);
   }
   int64_t workspace() const { return count() == 0 || alone() ? 0 : (int64_t)parts() * 8; }
@@ -479,13 +483,6 @@ struct Elements {
 
 #define DIFFOPT_LAUNCH(kernel, grid, block, ...) hipLaunchKernelGGL((kernel), dim3((unsigned)(grid)), dim3(block), 0, st, __VA_ARGS__)
 
-// Partial sums of the operands' products.
-template <bool FLAT, int NA>
-void sums(const Elements& e, const Operands<NA>& ops, const float* stats, double* parts, hipStream_t st) {
-  if (e.many()) DIFFOPT_LAUNCH((clip_sums<FLAT, NA, kManyWaves>), e.parts(), 64 * kManyWaves, e.space(), ops, stats, parts);
-  else DIFFOPT_LAUNCH((clip_sums<FLAT, NA, kFewWaves>), e.parts(), 64 * kFewWaves, e.space(), ops, stats, parts);
-}
-
 template <bool FLAT>
 int fwd(const char* who, const Elements& e, const void* grad, double max_norm, double eps, const void* out, float* stats, void* workspace, hipStream_t st) {
   const Operands<2> ops{{grad, out}};
@@ -495,7 +492,9 @@ int fwd(const char* who, const Elements& e, const void* grad, double max_norm, d
   }
   const Space sp = e.space();
   double* parts = static_cast<double*>(workspace);
-  sums<FLAT, 1>(e, Operands<1>{{grad}}, nullptr, parts, st);
+  const Operands<1> one{{grad}};
+  const float* none = nullptr;
+  DIFFOPT_LAUNCH((clip_sums<FLAT, 1>), e.parts(), 64 * kSumWaves, sp, one, none, parts);
   DIFFOPT_LAUNCH((clip_scale<FLAT>), out ? e.scale_blocks() : 1u, kScaleBlock, sp, ops, parts, e.parts(), max_norm, eps, stats);
   return launch_status(who);
 }
@@ -514,7 +513,8 @@ int bwd(const char* who, const Elements& e, const void* dout, const float* dnorm
   const Space sp = e.space();
   if (dout) {
     double* parts = static_cast<double*>(workspace);
-    sums<FLAT, 2>(e, Operands<2>{{grad, dout}}, stats, parts, st);
+    const Operands<2> product{{grad, dout}};
+    DIFFOPT_LAUNCH((clip_sums<FLAT, 2>), e.parts(), 64 * kSumWaves, sp, product, stats, parts);
     DIFFOPT_LAUNCH((clip_gradient<FLAT, true>), e.scale_blocks(), kScaleBlock, sp, three, parts, e.parts(), dnorm, stats, eps);
   } else {
     DIFFOPT_LAUNCH((clip_gradient<FLAT, false>), e.scale_blocks(), kScaleBlock, sp, two, nullptr, 0, dnorm, stats, eps);

@@ -15,7 +15,15 @@
 // sequences are cut into one chunk a workgroup: a first launch writes each
 // chunk's run, a small one turns runs into the states that enter each chunk, a
 // third walks the chunks.  A token past its sequence's end maps every state to
-// itself.
+// itself.  With enough columns of 64 channels, or in short sequences, a workgroup
+// takes its column through the whole sequence instead (sweeps, below).
+//
+// An element costs an exponential, a few multiply-adds and its share of a run:
+// memory bounds it, and that chunks read their operands twice, which they could
+// only avoid by waiting for one another.  4 x 4,096 tokens of 2,048 bf16 channels: the
+// sweep 62 us (201 MB, 3.2 TB/s), backward runs 35 (201 MB, 5.8 TB/s), join 8, walk
+// 58 (336 MB, 5.8 TB/s).  16,384 tokens in one sequence: runs 28 (134 MB, 4.8 TB/s),
+// join 8, walk 38 (201 MB, 5.3 TB/s).
 #include <initializer_list>
 #include <type_traits>
 
@@ -273,7 +281,7 @@ __global__ __launch_bounds__(64 * kW) void gscan_runs(Scan s) {
 
 // Chunks' runs become the states that enter each chunk: kX holds h, kY y, kE e
 // and kF f.  A workgroup has 64 channels of a sequence, its waves share the
-// chunks.
+// chunks, and hold 16 of them forwards (256 chunks 8.2 us, in two batches of 8 9.5).
 constexpr int kJW = 16;
 template <int MODE>
 __global__ __launch_bounds__(64 * kJW) void gscan_join(Scan s) {
@@ -511,6 +519,9 @@ __global__ __launch_bounds__(64 * kW, (MODE == kSecond && JOIN ? 4 : 1)) void gs
 // forward sweep reads its operands once, where chunks of their own read them
 // twice.  The backward sweep needs the states from before: a forward sweep that
 // stores nothing else leaves one for each chunk.
+// 128 columns occupy half of the compute units, and 16 waves each with 32 loads a lane
+// on their way bring 3.2 TB/s of operands that lie in no cache (a plain copy of the same
+// columns by the same workgroups is no faster); 256 columns of 2,048 tokens 6.1 TB/s.
 
 constexpr int kSweepWaves = 16;
 constexpr int kSweepU = 16, kBackU = 8;              // tokens of a wave
@@ -729,7 +740,8 @@ __global__ __launch_bounds__(64 * kSweepWaves) void gscan_back(Scan s) {
   if (s.begin && f.w.wave == 0) s.begin[st] = f.e;
 }
 
-// One token of every sequence, the state in place.
+// One token of every sequence, the state in place: the state's traffic (512 sequences of
+// 4,096 channels 5.2 us, 29 MB), or the launch (2,048 channels 1.6 us).
 template <class E, int VEC>
 __global__ __launch_bounds__(kBlock) void gscan_one(HeadArr lg, HeadArr x, HeadArr out, float* state, int64_t C, int64_t cols, int64_t n) {
   const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
@@ -760,6 +772,7 @@ int64_t chunks_of(int64_t T) { return T <= kChunk ? 1 : (T + kChunk - 1) / kChun
 // 11.5, 32 x 2048 19.9 and 17.6, 64 x 2048 20.5 and 24.3, 64 x 8192 69 and 66, 128 x 4096
 // 40 and 68, 256 x 2048 33 and 63; backward 128 x 2048 57 and 52, 128 x 8192 282 and 231,
 // 192 x 256 13.7 and 13.9, 192 x 2048 62 and 73, 256 x 1024 40 and 53, 512 x 2048 205 and 233.
+// With operands that lie in no cache 128 x 4096 forward takes 62 and 71.
 constexpr int64_t kSweepTokens = 1024, kSweepColumns = 64, kBackTokens = 256, kBackColumns = 192;
 bool sweeps(int64_t B, int64_t T, int64_t C, int mode) {
   const int64_t cols = B * ((C + 63) / 64);
