@@ -199,20 +199,49 @@ __device__ __forceinline__ void row_sums(const Share<E_, B>& sh, float c, Sums& 
   if (single) sums.template piece<1, ENT>(&one, c);
 }
 
+// The largest value of a row that stays in registers.  Pairs of bf16 values stay
+// packed: as signed numbers their order is right where one of them is not negative,
+// and else the least unsigned number is the largest value.  A NaN is the largest
+// value or shows in the sums.  4,096 rows of 50,021 with their gradient, bound by
+// vector instructions: 162.6 us, unpacked for the maximum too 166.3.
+template <class E_, int B, int NV>
+__device__ __forceinline__ float kept_max(const Kept<E_, B, NV>& kept) {
+  constexpr int N = Vec<E_>::N;
+  float top = (float)kept.single;
+  if constexpr (sizeof(E_) == 2) {
+    typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    i16x2 most = (int16_t)-32768;
+    u16x2 least = (uint16_t)65535;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        most = __builtin_elementwise_max(most, __builtin_bit_cast(i16x2, kept.v[i][k]));
+        least = __builtin_elementwise_min(least, __builtin_bit_cast(u16x2, kept.v[i][k]));
+      }
+    const int16_t high = most[0] > most[1] ? most[0] : most[1];
+    const uint16_t low = least[0] < least[1] ? least[0] : least[1];
+    return fmaxf(top, __builtin_bit_cast(float, (uint32_t)(high >= 0 ? (uint16_t)high : low) << 16));
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float e[N];
+      kept.get(i, e);
+#pragma unroll
+      for (int k = 0; k < N; k += 2) top = fmaxf(fmaxf(top, e[k]), e[k + 1]);
+    }
+    return top;
+  }
+}
+
 // A lane's sums over a row that stays in registers.  d is (x - m) c, not x c - m c
 // in one instruction: the largest logit's e is 1, so that no probability is above 1
 // and that of a row's only token is.
 template <bool ENT, class E_, int B, int NV>
 __device__ __forceinline__ void kept_sums(const Kept<E_, B, NV>& kept, float c, Sums& sums) {
   constexpr int N = Vec<E_>::N;
-  float top = (float)kept.single;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    float e[N];
-    kept.get(i, e);
-#pragma unroll
-    for (int k = 0; k < N; k += 2) top = fmaxf(fmaxf(top, e[k]), e[k + 1]);
-  }
+  const float top = kept_max(kept);
   sums.m = top;
   const float b = safe_max(top);
   sums.add<ENT>((float)kept.single, b, c);

@@ -166,6 +166,50 @@ def test_temperatures(T):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shift", [-40.0, 40.0])
+@pytest.mark.parametrize("N,V", [(4, 1), (4, 9), (300, 700), (40, 33000), (6, 50021)])
+def test_values_of_one_sign(N, V, shift, dtype):
+    # logits of 8 bits about the shift; the other results have 1 and no token at 0
+    I = _inputs(N, V, min(V, 5), dtype, seed=V)
+    I["x"] = (I["x"].float() + shift).to(dtype)
+    if V > 2:
+        I["x"][0, : V // 2] = -math.inf
+        I["ids"][0] = V - 1
+    o, both = _run(I, 1.0)
+    ref = _reference(I, 1.0)
+    alone = _reference(dict(I, c=torch.zeros(N, 0)), 1.0)
+    for k in ("logprob", "entropy", "top", "dx"):
+        if V > 1:
+            assert_close(o[k], ref[k], tol(dtype) if k == "dx" else F32, k)
+    for k in both:
+        if V > 1:
+            assert_close(both[k], alone[k], tol(dtype) if k == "dx" else F32, "at once " + k)
+    if V == 1:
+        assert not both["logprob"].any() and not both["entropy"].any() and not o["logprob"].any()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_nan_shows(dtype):
+    # of either sign, among values of either sign, in a lane's packed pieces and beside them
+    for V in (300, 9001):
+        x = torch.randn(8, V, generator=torch.Generator().manual_seed(V)).to(dtype).cuda()
+        bits = x.view(torch.int16 if dtype == torch.bfloat16 else torch.int32)
+        quiet = 0x7FC0 if dtype == torch.bfloat16 else 0x7FC00000
+        low = -0x8000 if dtype == torch.bfloat16 else -0x80000000
+        x[2:4] = x[2:4].abs().neg()
+        for row, at in ((0, 17), (2, 17), (4, V - 1)):
+            bits[row, at], bits[row + 1, at] = quiet, quiet + low
+        ids = torch.zeros(8, dtype=torch.int64, device="cuda")
+        new = lambda *n: torch.zeros(n, device="cuda")  # noqa: E731
+        lp, en, dx = new(8), new(8), torch.zeros_like(x)
+        P.logprob_fwd_bwd(new(8) + 1.0, x, ids, lp, new(8, 2), dx, new(8), en)
+        for t in (lp, en, dx.float().sum(1)):
+            assert torch.isnan(t).tolist() == [True] * 6 + [False] * 2
+        P.logprob_fwd(x, ids, lp, new(8, 2), en)
+        assert torch.isnan(lp).tolist() == torch.isnan(en).tolist() == [True] * 6 + [False] * 2
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("V", [40, 700, 33000, 140001])
 def test_masked_vocabularies(V, dtype):
     # from a single token on; fewer than K are left in some rows
