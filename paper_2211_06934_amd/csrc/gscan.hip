@@ -23,7 +23,7 @@
 // only avoid by waiting for one another.  4 x 4,096 tokens of 2,048 bf16 channels: the
 // sweep 62 us (201 MB, 3.2 TB/s), backward runs 35 (201 MB, 5.8 TB/s), join 8, walk
 // 58 (336 MB, 5.8 TB/s).  16,384 tokens in one sequence: runs 28 (134 MB, 4.8 TB/s),
-// join 8, walk 38 (201 MB, 5.3 TB/s).
+// join 7, walk 34 (201 MB, 6.0 TB/s).
 #include <initializer_list>
 #include <type_traits>
 
@@ -51,7 +51,6 @@ struct Scan {
   float* parts;                             // [B][S][fields][C]: chunks' runs, then the states that enter them
   int64_t T, C, S;
   int32_t cols;
-  bool in_place;  // chunks after the first must not read the state, which the last one overwrites
 };
 
 template <class E, int VEC>
@@ -281,7 +280,8 @@ __global__ __launch_bounds__(64 * kW) void gscan_runs(Scan s) {
 
 // Chunks' runs become the states that enter each chunk: kX holds h, kY y, kE e
 // and kF f.  A workgroup has 64 channels of a sequence, its waves share the
-// chunks, and hold 16 of them forwards (256 chunks 8.2 us, in two batches of 8 9.5).
+// chunks, and hold 16 of them forwards (256 chunks 8.2 us, in two batches of 8 9.5; 128
+// chunks 7.1).
 constexpr int kJW = 16;
 template <int MODE>
 __global__ __launch_bounds__(64 * kJW) void gscan_join(Scan s) {
@@ -761,9 +761,16 @@ __global__ __launch_bounds__(kBlock) void gscan_one(HeadArr lg, HeadArr x, HeadA
 
 // ---- host -------------------------------------------------------------------
 
-constexpr int kU = 8;  // tokens of a wave
+// Tokens of a wave in sequences of one chunk, and in longer ones.  Forward in bf16 a
+// lane has more of its two operands on their way: 16,384 x 2,048 channels 69.5 us, with
+// 8 tokens 74.0, 12 70.8, 24 70.7 (in fp32 131.1 and 128.6; 64 tokens 5.5 and 5.2).
+constexpr int kU = 8;
+constexpr int long_tokens(int mode, int32_t dtype) { return mode == kFwd && dtype == DIFFOPT_BF16 ? 16 : kU; }
 constexpr int64_t kChunk = kW * kU;
-int64_t chunks_of(int64_t T) { return T <= kChunk ? 1 : (T + kChunk - 1) / kChunk; }
+int64_t chunks_of(int64_t T, int mode, int32_t dtype) {
+  const int64_t chunk = kW * long_tokens(mode, dtype);
+  return T <= kChunk ? 1 : (T + chunk - 1) / chunk;
+}
 
 // Sweeps or chunks.  A forward sweep's step of 256 tokens takes 2.4 us until memory
 // bounds it, a backward one's of 128 3.5: sweeps are for sequences of few steps, or
@@ -780,18 +787,18 @@ bool sweeps(int64_t B, int64_t T, int64_t C, int mode) {
   return mode == kBwd && T >= kBackTokens && cols >= kBackColumns;
 }
 
-int64_t workspace_bytes(int64_t B, int64_t T, int64_t C, int mode) {
+int64_t workspace_bytes(int64_t B, int64_t T, int64_t C, int32_t dtype, int mode) {
   if (B == 0 || C == 0) return 0;
   if (sweeps(B, T, C, mode)) return mode == kFwd ? 0 : B * ((T + kBackChunk - 1) / kBackChunk) * C * 4;
-  const int64_t S = chunks_of(T);
-  return B == 0 || C == 0 || S == 1 ? 0 : B * S * fields(mode) * C * 4;
+  const int64_t S = chunks_of(T, mode, dtype);
+  return S == 1 ? 0 : B * S * fields(mode) * C * 4;
 }
 
 bool sizes_ok(int64_t B, int64_t T, int64_t C) {
   if (B < 0 || T < 0 || C < 0) return false;
   if (B == 0 || C == 0) return true;
   if (T > (int64_t(1) << 35) || C > (int64_t(1) << 31) || B > (int64_t(1) << 31)) return false;
-  const int64_t cols = (C + 63) / 64, S = chunks_of(T);  // at most 2^25, 2^29
+  const int64_t cols = (C + 63) / 64, S = chunks_of(T, kBwd, DIFFOPT_F32);  // the most: at most 2^25, 2^29
   return cols <= kMostGroups / S && B <= kMostGroups / (cols * S);
 }
 
@@ -799,12 +806,15 @@ template <class E, int MODE, int VEC>
 int launch(const char* who, Scan s, int64_t B, hipStream_t st) {
   s.cols = (int32_t)((s.C + 64 * VEC - 1) / (64 * VEC));
   const dim3 grid((unsigned)(B * s.S * s.cols)), block(64 * kW);
-  if (s.S > 1) hipLaunchKernelGGL((gscan_runs<E, MODE, VEC, kU>), grid, block, 0, st, s);
-  if (s.S <= kW && !s.in_place) {
+  if (s.S == 1 || (MODE != kFwd && s.S <= kW)) {  // forward, sweeps take what has two to eight chunks
+    if constexpr (MODE != kFwd)
+      if (s.S > 1) hipLaunchKernelGGL((gscan_runs<E, MODE, VEC, kU>), grid, block, 0, st, s);
     hipLaunchKernelGGL((gscan_walk<E, MODE, VEC, kU, true>), grid, block, 0, st, s);
   } else {
-    if (s.S > 1) hipLaunchKernelGGL((gscan_join<MODE>), dim3((unsigned)(B * ((s.C + 63) / 64))), dim3(64 * kJW), 0, st, s);
-    hipLaunchKernelGGL((gscan_walk<E, MODE, VEC, kU, false>), grid, block, 0, st, s);
+    constexpr int U = long_tokens(MODE, sizeof(E) == 2 ? DIFFOPT_BF16 : DIFFOPT_F32);
+    hipLaunchKernelGGL((gscan_runs<E, MODE, VEC, U>), grid, block, 0, st, s);
+    hipLaunchKernelGGL((gscan_join<MODE>), dim3((unsigned)(B * ((s.C + 63) / 64))), dim3(64 * kJW), 0, st, s);
+    hipLaunchKernelGGL((gscan_walk<E, MODE, VEC, U, false>), grid, block, 0, st, s);
   }
   return launch_status(who);
 }
@@ -884,8 +894,8 @@ int check_call(const char* who, const int32_t* lengths, int64_t B, int64_t T, in
   return DIFFOPT_OK;
 }
 
-int check_workspace(const char* who, int64_t B, int64_t T, int64_t C, int mode, const void* workspace, int64_t bytes) {
-  const int64_t need = workspace_bytes(B, T, C, mode);
+int check_workspace(const char* who, int64_t B, int64_t T, int64_t C, int32_t dtype, int mode, const void* workspace, int64_t bytes) {
+  const int64_t need = workspace_bytes(B, T, C, dtype, mode);
   if (need > 0 && (!workspace || bytes < need))
     return fail(DIFFOPT_EINVAL, "%s: the workspace has %lld bytes of %lld", who, (long long)(workspace ? bytes : 0), (long long)need);
   if (!aligned_to(workspace, 4)) return fail(DIFFOPT_EINVAL, "%s: the workspace is not 4-byte aligned", who);
@@ -899,7 +909,7 @@ using namespace diffopt;
 
 extern "C" int64_t diffopt_gscan_workspace(int64_t B, int64_t T, int64_t C, int32_t dtype, int32_t order) {
   if (!sizes_ok(B, T, C) || !dtype_ok(dtype) || order < 0 || order > 2) return -1;
-  return workspace_bytes(B, T, C, order);
+  return workspace_bytes(B, T, C, dtype, order);
 }
 
 extern "C" int diffopt_gscan_fwd(const diffopt_heads* log_gate, const diffopt_heads* x, const int32_t* lengths, const float* state, int64_t B,
@@ -913,7 +923,7 @@ extern "C" int diffopt_gscan_fwd(const diffopt_heads* log_gate, const diffopt_he
   if (T > 0) rc = check_arrays(who, dtype, {{"log_gate", log_gate, &s.lg}, {"x", x, &s.x}}, {{"h", h, &s.out[0]}});
   const bool in_place = state && state_out == state;
   if (!rc) rc = check_states(who, 4 * B * C, {{"state", in_place ? nullptr : state}}, {{"state_out", state_out}});
-  if (!rc) rc = check_workspace(who, B, T, C, kFwd, workspace, workspace_bytes);
+  if (!rc) rc = check_workspace(who, B, T, C, dtype, kFwd, workspace, workspace_bytes);
   if (rc || (T == 0 && !state_out)) return rc;
   s.lengths = lengths;
   s.state = state;
@@ -921,8 +931,7 @@ extern "C" int diffopt_gscan_fwd(const diffopt_heads* log_gate, const diffopt_he
   s.parts = static_cast<float*>(workspace);
   s.T = T;
   s.C = C;
-  s.S = chunks_of(T);
-  s.in_place = in_place && s.S > 1;
+  s.S = chunks_of(T, kFwd, dtype);
   return run<kFwd>(who, s, B, dtype, as_stream(stream));
 }
 
@@ -939,7 +948,7 @@ extern "C" int diffopt_gscan_bwd(const diffopt_heads* dh, const float* dstate_ou
     rc = check_arrays(who, dtype, {{"log_gate", log_gate, &s.lg}, {"x", x, &s.x}, {"dh", dh, &s.dh}},
                       {{"dlog_gate", dlog_gate, &s.out[0], true}, {"dx", dx, &s.out[1], true}});
   if (!rc) rc = check_states(who, 4 * B * C, {{"state", state}, {"dstate_out", dstate_out}}, {{"dstate", dstate}});
-  if (!rc) rc = check_workspace(who, B, T, C, kBwd, workspace, workspace_bytes);
+  if (!rc) rc = check_workspace(who, B, T, C, dtype, kBwd, workspace, workspace_bytes);
   if (rc || ((T == 0 || (!dlog_gate && !dx)) && !dstate)) return rc;
   s.lengths = lengths;
   s.state = state;
@@ -948,7 +957,7 @@ extern "C" int diffopt_gscan_bwd(const diffopt_heads* dh, const float* dstate_ou
   s.parts = static_cast<float*>(workspace);
   s.T = T;
   s.C = C;
-  s.S = chunks_of(T);
+  s.S = chunks_of(T, kBwd, dtype);
   return run<kBwd>(who, s, B, dtype, as_stream(stream));
 }
 
@@ -969,7 +978,7 @@ extern "C" int diffopt_gscan_bwd_bwd(const diffopt_heads* ddlog_gate, const diff
   if (!rc)
     rc = check_states(who, 4 * B * C, {{"state", state}, {"dstate_out", dstate_out}, {"ddstate", ddstate}},
                       {{"out_dstate_out", out_dstate_out}, {"out_state", out_state}});
-  if (!rc) rc = check_workspace(who, B, T, C, kSecond, workspace, workspace_bytes);
+  if (!rc) rc = check_workspace(who, B, T, C, dtype, kSecond, workspace, workspace_bytes);
   if (rc || (T == 0 && !out_dstate_out && !out_state)) return rc;
   s.lengths = lengths;
   s.state = state;
@@ -980,7 +989,7 @@ extern "C" int diffopt_gscan_bwd_bwd(const diffopt_heads* ddlog_gate, const diff
   s.parts = static_cast<float*>(workspace);
   s.T = T;
   s.C = C;
-  s.S = chunks_of(T);
+  s.S = chunks_of(T, kSecond, dtype);
   return run<kSecond>(who, s, B, dtype, as_stream(stream));
 }
 
