@@ -221,6 +221,9 @@ def gated_scan(log_gate, x, state=None, lengths=None, return_state: bool = False
     state: fp32 [B, C] before the first token (None: zeros).  lengths: int32 [B]; tokens from there on give zeros.  A gate
     of -inf forgets what came before (where another document begins).  Returns h [B, T, C], with return_state also the
     state after the last token.  Differentiable twice in log_gate, x and state."""
+    _o._axes(3, (log_gate, "log_gate"), (x, "x"))
+    if state is not None:
+        _o._axes(2, (state, "state"))
     h, s1 = GatedScanFn.apply(_dense(log_gate), _dense(x), _whole(state), lengths, bool(return_state))
     return (h, s1) if return_state else h
 
@@ -228,6 +231,7 @@ def gated_scan(log_gate, x, state=None, lengths=None, return_state: bool = False
 def gated_scan_step(log_gate, x, state) -> torch.Tensor:
     """One token of every sequence for generation: log_gate, x [B, C] -> h [B, C]; `state` is updated in place.  Not
     differentiable: an operand that asks for a gradient is refused, but under torch.no_grad()."""
+    _o._axes(2, (log_gate, "log_gate"), (x, "x"), (state, "state"))
     if torch.is_grad_enabled():
         for t, what in ((log_gate, "log_gate"), (x, "x"), (state, "state")):
             if isinstance(t, torch.Tensor) and t.requires_grad:
@@ -422,6 +426,9 @@ def token_logprobs(logits, ids=None, temperature: float = 1.0, entropy: bool = F
     [N, top], falling, the lowest id first among equals (-inf and -1 where the logits leave fewer).  A negative id is a row
     of padding: zeros.  Without ids (generation) logprob is None.  The alternatives are ids and a teacher's logits as
     distillation_loss takes them.  Differentiable twice in logits."""
+    _o._axes(2, (logits, "logits"))
+    if ids is not None:
+        _o._axes(1, (ids, "ids"))
     if int(top) < 0:
         raise ValueError("token_logprobs: top must be >= 0")
     return TokenLogprobs(*TokenLogprobsFn.apply(_dense(logits), _whole(ids), float(temperature), bool(entropy), int(top)))

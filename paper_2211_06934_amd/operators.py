@@ -163,10 +163,14 @@ def _scratch(given, need: int, device, stream):
 # ---- linear attention -------------------------------------------------------
 
 
-def _dims(q, k, v, axes: int):
-    for x, what in ((q, "q"), (k, "k"), (v, "v")):
+def _axes(axes: int, *named) -> None:
+    for x, what in named:
         if not isinstance(x, torch.Tensor) or x.dim() != axes:
             raise ValueError("%s: expected a tensor of %d axes" % (what, axes))
+
+
+def _dims(q, k, v, axes: int):
+    _axes(axes, (q, "q"), (k, "k"), (v, "v"))
     return q.shape[-2], k.shape[-2], q.shape[-1], v.shape[-1]
 
 

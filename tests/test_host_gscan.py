@@ -94,3 +94,20 @@ def test_workspaces():
                 _refused(_call(name, T=T, C=C, ws=f, nws=need - 1), "the workspace has")
                 _refused(_call(name, T=T, C=C, ws=odd, nws=need), "not 4-byte aligned")
     assert size(2, -1, 100, F32, 0) == size(2, 9, 100, 7, 0) == size(2, 9, 100, F32, 3) == size(1 << 40, 9, 100, F32, 0) == -1
+
+
+@pytest.mark.parametrize("bad", [None, (8,), (2, 3, 4, 5), ()])
+def test_operands_of_other_axes_are_named(bad):
+    import torch
+
+    import paper_2211_06934_amd as P
+    wrong = None if bad is None else torch.zeros(bad)
+    seq, row = torch.zeros(2, 3, 8), torch.zeros(2, 8)
+    for name, args in (("log_gate", (wrong, seq)), ("x", (seq, wrong)), ("state", (seq, seq, wrong))):
+        if name == "state" and bad is None:
+            continue
+        with pytest.raises(ValueError, match="%s: expected a tensor of" % name):
+            P.gated_scan(*args, return_state=True)
+    for name, args in (("log_gate", (wrong, row, row)), ("x", (row, wrong, row)), ("state", (row, row, wrong))):
+        with pytest.raises(ValueError, match="%s: expected a tensor of 2 axes" % name):
+            P.gated_scan_step(*args)

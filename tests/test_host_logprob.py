@@ -104,3 +104,16 @@ def test_workspaces():
         _refused(_call(name, **big), "the workspace has 0 bytes")
         _refused(_call(name, **big, ws=at(20), nws=n - 1), "the workspace has")
         _refused(_call(name, **big, ws=odd, nws=n), "not 4-byte aligned")
+
+
+@pytest.mark.parametrize("bad", [(), (8,), (2, 3, 4)])
+def test_operands_of_other_axes_are_named(bad):
+    import torch
+
+    import paper_2211_06934_amd as P
+    for logits in (None, torch.zeros(bad)):
+        with pytest.raises(ValueError, match="logits: expected a tensor of 2 axes"):
+            P.token_logprobs(logits, top=2)
+    for ids in ([1, 2], torch.zeros(2, 1, dtype=torch.int64), torch.zeros((), dtype=torch.int64)):
+        with pytest.raises(ValueError, match="ids: expected a tensor of 1 axes"):
+            P.token_logprobs(torch.zeros(2, 9), ids)
