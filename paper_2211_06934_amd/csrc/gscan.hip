@@ -834,13 +834,20 @@ int launch_sweeps(const char* who, Scan s, int64_t B, hipStream_t st) {
   return launch_status(who);
 }
 
+// Two channels a lane for the second derivative in bf16, where workgroups for all compute
+// units are left: 4 x 2,048 x 1,024 channels 57.9 us against 62.0, 16 x 128 x 1,024 14.8
+// against 15.4, but 1 x 509 x 1,000 13.5 against 12.0; in fp32 one is as fast or faster
+// (8 x 509 x 1,034 57.5 against 56.4, 2 x 300 x 512 14.3 against 11.1).
+constexpr int64_t kPairGroups = 256;
+
 template <int MODE>
 int run(const char* who, const Scan& s, int64_t B, int32_t dtype, hipStream_t st) {
   if constexpr (MODE != kSecond)
     if (sweeps(B, s.T, s.C, MODE)) return dtype == DIFFOPT_F32 ? launch_sweeps<float, MODE>(who, s, B, st) : launch_sweeps<bf16, MODE>(who, s, B, st);
-  constexpr int V = MODE == kSecond ? 2 : 1;
-  if (s.C < 64 * V) return dtype == DIFFOPT_F32 ? launch<float, MODE, 1>(who, s, B, st) : launch<bf16, MODE, 1>(who, s, B, st);
-  return dtype == DIFFOPT_F32 ? launch<float, MODE, V>(who, s, B, st) : launch<bf16, MODE, V>(who, s, B, st);
+  if (dtype == DIFFOPT_F32) return launch<float, MODE, 1>(who, s, B, st);
+  if constexpr (MODE == kSecond)
+    if (s.C >= 128 && B * s.S * ((s.C + 127) / 128) >= kPairGroups) return launch<bf16, MODE, 2>(who, s, B, st);
+  return launch<bf16, MODE, 1>(who, s, B, st);
 }
 
 struct Operand {

@@ -110,7 +110,7 @@ def test_what_may_be_left_out(T, state, lengths, resets, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("B,T,C", [(200, 260, 3), (193, 512, 5), (210, 1100, 2), (97, 300, 67), (66, 1100, 1), (3, 257, 4100)])
+@pytest.mark.parametrize("B,T,C", [(200, 260, 3), (193, 512, 5), (210, 1100, 2), (97, 300, 67), (66, 1100, 1), (3, 257, 4100), (4, 1030, 517), (130, 60, 129)])
 @pytest.mark.parametrize("rest", [False, True])
 def test_many_channels(B, T, C, rest, dtype):
     # enough columns of channels for both directions to take a sequence in one sweep; whole steps and a rest
