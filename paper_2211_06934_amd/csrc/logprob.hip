@@ -11,7 +11,7 @@
 // logits 24 for K = 20 and 64 groups, 177 for K = 128 and 256).  They are ranked by value and lowest
 // id in LDS.  A row of so many equal logits that they do not fit there takes
 // eight counting passes over the digits of (value, id) instead.  Eight rows of
-// 131,072 fp32 logits with 20: slices 6.1 us, join 5.7, both latency.
+// 131,072 fp32 logits with 20: slices 6.1 us, join 5.1, both latency.
 // The gradient's dense part takes the row from registers where the same call
 // has read it (rows of up to 256 KiB), else from memory; the tokens that are
 // named are written once more after a barrier.  A few exponentials per element:
@@ -32,7 +32,7 @@ constexpr int kJB = 256;     // ... of a row's joined slices
 constexpr int kMaxTop = 128;
 constexpr int kCap = 1024;   // candidates that are ranked
 // Comparisons of a lane from which on the lowest candidates are left out first: 8,000
-// rows of 500 bf16 logits with 64 alternatives 43 us, ranked as they are 246.
+// rows of 500 bf16 logits with 64 alternatives 39 us, ranked as they are 246.
 constexpr int kRanking = 640;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLow = -256.0f;  // 2^d is 0 from here on: 0 log 0 = 0, whatever d is
@@ -302,20 +302,21 @@ __device__ __forceinline__ uint32_t floor_of(const Select& S, int K) {
 // ... that K of the n candidates reach.  Lanes count their own: with a ballot for
 // each number the kernel takes more than 80 scalar registers, and a SIMD has
 // seven waves instead of eight (2,048 rows of 50,021 logits: 46 us instead of 42).
-__device__ __forceinline__ uint32_t floor_of_found(const Select& S, int n, int K) {
+__device__ __forceinline__ uint32_t floor_of_found(const Select& S, int count, int K) {
   constexpr int G = kCap / 64;
   uint32_t k[G], floor = 0;
 #pragma unroll
-  for (int g = 0; g < G; ++g) k[g] = 64 * g + (int)threadIdx.x < n ? (uint32_t)(S.found[64 * g + threadIdx.x] >> 48) : 0;
+  for (int g = 0; g < G; ++g) k[g] = 64 * g + (int)threadIdx.x < count ? (uint32_t)(S.found[64 * g + threadIdx.x] >> 48) : 0;
 #pragma unroll 1
   for (int bit = 15; bit >= 0; --bit) {
     const uint32_t more = floor | 1u << bit;
     int reached = 0;
 #pragma unroll
     for (int g = 0; g < G; ++g) reached += k[g] >= more;
+    int n = 0;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) reached += __shfl_xor(reached, o, 64);
-    if (reached >= K) floor = more;
+    for (int b = 0; 1 << b <= G; ++b) n += __popcll(__ballot(reached >> b & 1)) << b;
+    if (n >= K) floor = more;
   }
   return floor;
 }
@@ -590,6 +591,31 @@ struct Found {
   }
 };
 
+// ... by a lane, where there are few enough to hold: eight rows of 131,072 with 20
+// alternatives 11.3 us, read again for those above the floor 11.9.
+constexpr int kHeld = 4;
+struct Held {
+  float v[kHeld];
+  int32_t id[kHeld];
+  static constexpr bool kOwn = true;
+  __device__ __forceinline__ explicit Held(const Found& found) {
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+      v[j] = -kInf;
+      id[j] = -1;
+      found.item(threadIdx.x, j, [&](float x, int64_t i) {
+        v[j] = x;
+        id[j] = (int32_t)i;
+      });
+    }
+  }
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) f(v[j], (int64_t)id[j]);
+  }
+};
+
 // A row from its slices' sums and largest logits.
 template <class E_, bool ENT, bool TOP>
 __global__ __launch_bounds__(kJB) void logprob_join(Rows r, Results o, Parts parts) {
@@ -602,8 +628,22 @@ __global__ __launch_bounds__(kJB) void logprob_join(Rows r, Results o, Parts par
   Sums sums;
   float largest = -kInf;
   const Found found{parts, first, parts.slices * parts.K};
-  if (tok.live) {
+  const auto join = [&] {
     for (int i = threadIdx.x; i < parts.slices; i += kJB) sums.join<ENT>(parts.get(first + i), c);
+  };
+  if constexpr (TOP)
+    if (tok.live && found.n <= kHeld * kJB) {
+      const Held held(found);
+      join();
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j) largest = fmaxf(largest, held.v[j]);
+      sums.all<ENT>(R, c);
+      if (threadIdx.x == 0) finish(r, o, row, tok, tok.id >= 0 ? (float)x[tok.id] : 0.0f, sums);
+      finish_top<kJB>(r, o, S, row, tok, sums, largest, held);
+      return;
+    }
+  if (tok.live) {
+    join();
     if constexpr (TOP)
       for (int j = 0; j < found.items(); ++j) found.item(threadIdx.x, j, [&](float v, int64_t) { largest = fmaxf(largest, v); });
   }
