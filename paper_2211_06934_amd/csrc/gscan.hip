@@ -22,8 +22,8 @@
 // memory bounds it, and that chunks read their operands twice, which they could
 // only avoid by waiting for one another.  4 x 4,096 tokens of 2,048 bf16 channels: the
 // sweep 62 us (201 MB, 3.2 TB/s), backward runs 35 (201 MB, 5.8 TB/s), join 8, walk
-// 58 (336 MB, 5.8 TB/s).  16,384 tokens in one sequence: runs 28 (134 MB, 4.8 TB/s),
-// join 7, walk 34 (201 MB, 6.0 TB/s).
+// 58 (336 MB, 5.8 TB/s).  16,384 tokens in one sequence: runs 27 (134 MB, 5.0 TB/s),
+// join 7, walk 33 (201 MB, 6.1 TB/s).
 #include <initializer_list>
 #include <type_traits>
 

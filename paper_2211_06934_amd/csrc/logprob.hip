@@ -16,7 +16,7 @@
 // has read it (rows of up to 256 KiB), else from memory; the tokens that are
 // named are written once more after a barrier.  A few exponentials per element:
 // bound by memory.  4,096 rows of 50,021 bf16 logits, a tenth of them padding: results
-// and gradient at once 158 us (779 MB, 4.9 TB/s).  2,048 rows with 5 alternatives: 42 us
+// and gradient at once 157 us (779 MB, 5.0 TB/s).  2,048 rows with 5 alternatives: 42 us
 // (205 MB, 4.9 TB/s).  1,024 rows of 32,000 fp32 logits with 8: forward 37 us where
 // earlier results are still on their way to memory, else 25 (131 MB, 5.2 TB/s), gradient
 // 43 (262 MB, 6.1 TB/s), its backward 80 (393 MB, 4.9 TB/s).
