@@ -575,39 +575,33 @@ __global__ __launch_bounds__(B, kept_waves(B, NV)) void logprob_kept(Rows r, Res
   if constexpr (TOP) finish_top<B>(r, o, S, row, tok, sums, largest, OwnPieces<E_, B, NV>{kept});
 }
 
-// What the slices of a row found, shared by the lanes that join them.
-struct Found {
-  const Parts& parts;
-  int64_t first;
-  int32_t n;
-  static constexpr bool kOwn = false;
-  __device__ __forceinline__ int32_t items() const { return (n + kJB - 1) / kJB; }
-  template <class F>
-  __device__ __forceinline__ void item(int32_t lane, int32_t j, F f) const {
-    const int32_t i = lane + j * kJB;
-    if (i >= n) return;
-    const int32_t slice = i / parts.K, k = i - slice * parts.K;
-    f(parts.values(first + slice)[k], (int64_t)parts.ids(first + slice)[k]);
-  }
-};
-
-// ... by a lane, where there are few enough to hold: eight rows of 131,072 with 20
-// alternatives 11.3 us, read again for those above the floor 11.9.
-constexpr int kHeld = 4;
+// What the slices of a row found, kHeld values a lane.  A slice's values fall: each
+// slice is turned a little further than the one before it, so that the largest ones of
+// all slices lie in different lanes (2 rows of 151,722 fp32 logits with 128 alternatives
+// 29 us, unturned 55).
+constexpr int kHeld = 8, kTurn = 37;
 struct Held {
   float v[kHeld];
   int32_t id[kHeld];
   static constexpr bool kOwn = true;
-  __device__ __forceinline__ explicit Held(const Found& found) {
+  __device__ __forceinline__ Held(const Parts& parts, int64_t first, bool live) {
+    const int32_t n = live ? parts.slices * parts.K : 0;
 #pragma unroll
     for (int j = 0; j < kHeld; ++j) {
+      const int32_t i = threadIdx.x + j * kJB;
       v[j] = -kInf;
       id[j] = -1;
-      found.item(threadIdx.x, j, [&](float x, int64_t i) {
-        v[j] = x;
-        id[j] = (int32_t)i;
-      });
+      if (i >= n) continue;
+      const int32_t slice = i / parts.K, k = (i - slice * parts.K + slice * kTurn) % parts.K;
+      v[j] = parts.values(first + slice)[k];
+      id[j] = parts.ids(first + slice)[k];
     }
+  }
+  __device__ __forceinline__ float largest() const {
+    float x = v[0];
+#pragma unroll
+    for (int j = 1; j < kHeld; ++j) x = fmaxf(x, v[j]);
+    return x;
   }
   template <class F>
   __device__ __forceinline__ void each(F f) const {
@@ -625,31 +619,13 @@ __global__ __launch_bounds__(kJB) void logprob_join(Rows r, Results o, Parts par
   const Token tok = token_of(r, row);
   const E_* x = static_cast<const E_*>(r.logits) + row * r.row_stride;
   const float c = r.invT * kLog2e;
+  const Held held(parts, first, TOP && tok.live);
   Sums sums;
-  float largest = -kInf;
-  const Found found{parts, first, parts.slices * parts.K};
-  const auto join = [&] {
+  if (tok.live)
     for (int i = threadIdx.x; i < parts.slices; i += kJB) sums.join<ENT>(parts.get(first + i), c);
-  };
-  if constexpr (TOP)
-    if (tok.live && found.n <= kHeld * kJB) {
-      const Held held(found);
-      join();
-#pragma unroll
-      for (int j = 0; j < kHeld; ++j) largest = fmaxf(largest, held.v[j]);
-      sums.all<ENT>(R, c);
-      if (threadIdx.x == 0) finish(r, o, row, tok, tok.id >= 0 ? (float)x[tok.id] : 0.0f, sums);
-      finish_top<kJB>(r, o, S, row, tok, sums, largest, held);
-      return;
-    }
-  if (tok.live) {
-    join();
-    if constexpr (TOP)
-      for (int j = 0; j < found.items(); ++j) found.item(threadIdx.x, j, [&](float v, int64_t) { largest = fmaxf(largest, v); });
-  }
   sums.all<ENT>(R, c);
   if (threadIdx.x == 0) finish(r, o, row, tok, tok.id >= 0 ? (float)x[tok.id] : 0.0f, sums);
-  if constexpr (TOP) finish_top<kJB>(r, o, S, row, tok, sums, largest, found);
+  if constexpr (TOP) finish_top<kJB>(r, o, S, row, tok, sums, held.largest(), held);
 }
 
 // ---- gradient ---------------------------------------------------------------
@@ -1095,8 +1071,13 @@ int check_cotangents(const char* who, const Rows& r, const Cotangents& t) {
 }
 
 // Slices are longer than distillation's, whose join has no alternatives to rank: 8
-// rows of 512 KiB with 20 of them 13.3 us in slices of 8 KiB, 11.8 of 16, 11.6 of 32.
-Cut row_cut(int64_t N, int64_t V, int32_t dtype) { return cut_of(N, V, dtype, 16384); }
+// rows of 512 KiB with 20 of them 13.3 us in slices of 8 KiB, 11.8 of 16, 11.6 of 32.  With
+// many alternatives they are as long as it takes for the join to hold what they find: one
+// row of 600,000 fp32 logits with 20 12.5 us, in slices of 16 KiB 15.8, with 128 23.6 and 64.
+Cut row_cut(int64_t N, int64_t V, int32_t dtype, int64_t K) {
+  const int64_t fewest = (V * elem_size(dtype) * K + kHeld * kJB - 1) / (kHeld * kJB);
+  return cut_of(N, V, dtype, fewest > 16384 ? fewest : 16384);
+}
 
 // Lanes of a row: 8,000 rows of 4,000 bf16 logits with 5 alternatives take 27.5 us
 // with 128, 28.5 with 256 and 51.6 with 512; 4,000 of 16,000 31.5, 31.5 and 38.0; 2,048
@@ -1110,7 +1091,7 @@ constexpr int64_t kShortRow = 16384, kMiddleRow = 65536;
 constexpr int64_t kKeptRows = 2048;
 
 int64_t parts_bytes(int64_t N, int64_t V, int32_t dtype, int64_t K) {
-  const Cut c = row_cut(N, V, dtype);
+  const Cut c = row_cut(N, V, dtype, K);
   return c.slices > 1 ? N * c.slices * (4 + 2 * K) * 4 : 0;
 }
 
@@ -1128,7 +1109,7 @@ Parts parts_of(const Cut& c, int64_t K, void* workspace) { return Parts{static_c
 
 template <class E_, bool ENT, bool TOP>
 int fwd_rows(const char* who, const Rows& r, int32_t dtype, const Results& o, void* workspace, hipStream_t st) {
-  const Cut c = row_cut(r.N, r.V, dtype);
+  const Cut c = row_cut(r.N, r.V, dtype, TOP ? o.K : 0);
   const Parts p = parts_of(c, TOP ? o.K : 0, workspace);
   const int64_t bytes = r.V * elem_size(dtype);  // of a row: slices are for few rows, whose time is latency
 #define DIFFOPT_KEPT(B, NV)                                                    \
@@ -1156,7 +1137,7 @@ int fwd_rows(const char* who, const Rows& r, int32_t dtype, const Results& o, vo
 template <class E_, bool ENT>
 int bwd_rows(const char* who, const Rows& r, int32_t dtype, const Cotangents& t, const float* stats, void* dx, int64_t dstride, hipStream_t st) {
   // over the logits in place, a row's workgroups would overwrite one another's named tokens
-  const Cut c = dx == r.logits ? Cut{1, r.V} : row_cut(r.N, r.V, dtype);
+  const Cut c = dx == r.logits ? Cut{1, r.V} : row_cut(r.N, r.V, dtype, 0);
   DIFFOPT_LAUNCH((logprob_grad<E_, kGiven, ENT>), r.N * c.slices, kLB, r, Results{}, t, stats, static_cast<E_*>(dx), dstride, parts_of(c, 0, nullptr));
   return launch_status(who);
 }
@@ -1164,7 +1145,7 @@ int bwd_rows(const char* who, const Rows& r, int32_t dtype, const Cotangents& t,
 template <class E_, bool ENT>
 int both_rows(const char* who, const Rows& r, int32_t dtype, const Results& o, const Cotangents& t, void* dlogits, int64_t dstride, void* workspace,
               hipStream_t st) {
-  const Cut c = row_cut(r.N, r.V, dtype);
+  const Cut c = row_cut(r.N, r.V, dtype, 0);
   const Parts p = parts_of(c, 0, workspace);
   E_* dx = static_cast<E_*>(dlogits);
   const float* none = nullptr;
@@ -1193,7 +1174,7 @@ int both_rows(const char* who, const Rows& r, int32_t dtype, const Results& o, c
 
 template <class E_, bool ENT>
 int second_rows(const char* who, const Rows& r, int32_t dtype, const Cotangents& t, const Second& q, void* workspace, hipStream_t st) {
-  const Cut c = row_cut(r.N, r.V, dtype);
+  const Cut c = row_cut(r.N, r.V, dtype, 0);
   const Parts p = parts_of(c, 0, workspace);
   if (c.slices > 1) {
     DIFFOPT_LAUNCH((logprob_second_parts<E_, ENT>), r.N * c.slices, kLB, r, t, q, p);
