@@ -1082,7 +1082,11 @@ Cut row_cut(int64_t N, int64_t V, int32_t dtype, int64_t K) {
 // Lanes of a row: 8,000 rows of 4,000 bf16 logits with 5 alternatives take 27.5 us
 // with 128, 28.5 with 256 and 51.6 with 512; 4,000 of 16,000 31.5, 31.5 and 38.0; 2,048
 // of 50,021 42.0, 41.8 and 41.9 (without alternatives 38 with 512, 43 with 256).
-constexpr int64_t kShortRow = 16384, kMiddleRow = 65536;
+// With more than kFewTop alternatives 128 lanes say too little about where they are, once
+// 256 have a piece or nearly: 300 rows of 4,000 with 128 of them 11.3 us, with 128 lanes
+// 30.5; 4,000 rows 35.0 and 50.3, with 64 of them 22.4 and 25.2; but 4,000 rows of 500 fp32
+// logits with 128 33.9 and 28.9.
+constexpr int64_t kShortRow = 16384, kMiddleRow = 65536, kWideRow = 3200;
 // Many short rows stay in registers: their maximum is known before the sums, and the
 // alternatives are looked for in the lanes that read them.  8,000 rows of 4,000 bf16
 // logits 15.1 us (streamed 19.7), with 5 alternatives 24.0 (26.2); 4,000 of 16,000 without
@@ -1117,7 +1121,8 @@ int fwd_rows(const char* who, const Rows& r, int32_t dtype, const Results& o, vo
     DIFFOPT_LAUNCH((logprob_kept<E_, ENT, TOP, B, NV>), r.N, B, r, o);         \
     return launch_status(who);                                                 \
   }
-  if (r.N >= kKeptRows && c.slices == 1) {
+  const bool wide = TOP && o.K > kFewTop && bytes >= kWideRow;
+  if (r.N >= kKeptRows && c.slices == 1 && !wide) {
     DIFFOPT_KEPT(128, 2)
     DIFFOPT_KEPT(128, 4)
     if constexpr (!TOP) {
@@ -1127,7 +1132,7 @@ int fwd_rows(const char* who, const Rows& r, int32_t dtype, const Results& o, vo
     }
   }
 #undef DIFFOPT_KEPT
-  if (bytes <= kShortRow) DIFFOPT_LAUNCH((logprob_row<E_, ENT, TOP, 128>), r.N * c.slices, 128, r, o, p);
+  if (bytes <= kShortRow && !wide) DIFFOPT_LAUNCH((logprob_row<E_, ENT, TOP, 128>), r.N * c.slices, 128, r, o, p);
   else if (bytes <= kMiddleRow) DIFFOPT_LAUNCH((logprob_row<E_, ENT, TOP, 256>), r.N * c.slices, 256, r, o, p);
   else DIFFOPT_LAUNCH((logprob_row<E_, ENT, TOP, kLB>), r.N * c.slices, kLB, r, o, p);
   if (c.slices > 1) DIFFOPT_LAUNCH((logprob_join<E_, ENT, TOP>), r.N, kJB, r, o, p);

@@ -133,7 +133,8 @@ def test_rows(N, dtype):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("N,V,K", [(2100, 1, 1), (2100, 37, 64), (2100, 500, 0), (2100, 500, 64), (2300, 900, 128), (2100, 2049, 5), (2100, 4090, 20), (2100, 4090, 0),
-                                   (2049, 8193, 0), (2049, 9001, 128), (2100, 16001, 0), (2100, 30011, 0), (2047, 500, 20), (3, 700, 128)])
+                                   (2049, 8193, 0), (2049, 9001, 128), (2100, 16001, 0), (2100, 30011, 0), (2047, 500, 20), (3, 700, 128),
+                                   (300, 1999, 128), (2100, 4090, 128), (2050, 4001, 49)])
 @pytest.mark.parametrize("values", ["all", "few", "one"])
 def test_many_rows(N, V, K, values, dtype):
     # short rows whose results come from registers; values that many tokens share
