@@ -268,7 +268,7 @@ __device__ __forceinline__ uint64_t key_of(float x, int64_t id) { return (uint64
 
 struct Select {
   uint64_t found[kCap], prefix;
-  uint32_t lane_key[kLB], hist[256], count, lanes, floor, left, enough;
+  uint32_t lane_key[kLB], hist[256], count, left_over, lanes, floor, left, enough;
   uint16_t lane[kLB];
 };
 
@@ -330,7 +330,7 @@ __device__ __forceinline__ void select_top(Select& S, int K, float largest, cons
   const int tid = threadIdx.x;
   const uint32_t own = key_of(largest);
   S.lane_key[tid] = own;
-  if (tid == 0) S.count = S.lanes = 0;
+  if (tid == 0) S.count = S.left_over = S.lanes = 0;
   __syncthreads();
   if (tid < 64) {
     const uint32_t floor = K <= kFewTop ? floor_of<B, 1>(S, K) : floor_of<B, (B < 256 ? B / 64 : 4)>(S, K);
@@ -411,18 +411,15 @@ __device__ __forceinline__ void select_top(Select& S, int K, float largest, cons
     for (int j = 0; j < kCap / B; ++j) k[j] = tid + j * B < n ? S.found[tid + j * B] : 0;
     if (tid < 64) {
       const uint32_t cut = floor_of_found(S, n, K);
-      if (tid == 0) {
-        S.floor = cut;
-        S.count = 0;
-      }
+      if (tid == 0) S.floor = cut;  // not count: others may still read it
     }
     __syncthreads();
     const uint32_t cut = S.floor;
 #pragma unroll
     for (int j = 0; j < kCap / B; ++j)
-      if (tid + j * B < n && (uint32_t)(k[j] >> 48) >= cut) S.found[atomicAdd(&S.count, 1u)] = k[j];
+      if (tid + j * B < n && (uint32_t)(k[j] >> 48) >= cut) S.found[atomicAdd(&S.left_over, 1u)] = k[j];
     __syncthreads();
-    n = __builtin_amdgcn_readfirstlane((int)S.count);
+    n = __builtin_amdgcn_readfirstlane((int)S.left_over);
   }
   for (int i = tid; i < n; i += B) {
     const uint64_t k = S.found[i];

@@ -161,6 +161,18 @@ def test_many_rows(N, V, K, values, dtype):
     assert_close(torch.where(order < 0, 0.0, tops[:, :n].double()), torch.where(order < 0, 0.0, value), F32)
 
 
+@pytest.mark.parametrize("V,K", [(900, 128), (500, 64), (230, 100)])
+def test_ranks_of_many_equal_values(V, K):
+    # the candidates are counted twice: no wave takes the second count for the first, however late it is
+    x, ids = torch.ones(6000, V, device="cuda"), torch.zeros(6000, dtype=torch.int64, device="cuda")
+    lp, stats, tops = torch.empty(6000, device="cuda"), torch.empty(6000, 2, device="cuda"), torch.empty(6000, K, device="cuda")
+    want = torch.arange(K, device="cuda").expand(6000, K)
+    for _ in range(30):
+        tids = torch.full((6000, K), -7, dtype=torch.int64, device="cuda")
+        P.logprob_fwd(x, ids, lp, stats, None, tops, tids)
+        assert torch.equal(tids, want)
+
+
 @pytest.mark.parametrize("T", [0.25, 1.0, 7.5])
 def test_temperatures(T):
     _check(6, 3001, 12, torch.float32, T=T)
