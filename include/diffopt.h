@@ -869,10 +869,12 @@ int diffopt_gscan_step(const diffopt_heads* log_gate, const diffopt_heads* x,
  *   top_logprob fp32 [N][K], top_ids [N][K] int32 or int64 (by top_id_bytes);
  *            0 <= K <= 128, and NULL for K = 0;  N < 2^22
  *   workspace  diffopt_logprob_workspace() bytes, or NULL if that is 0
- * Log probabilities and entropies near 0 are right to 2^-22 absolutely.  A row
- * that is no distribution (a NaN or +inf, or -inf alone) has NaN for its
- * results and -1 for its top_ids.  Results must not overlap operands or one
- * another where an entry point does not say that they may.                  */
+ * Where one logit has nearly all of the probability, its log probability and the
+ * entropy are right to 2^-22 absolutely, and to what 2^-21 of the other logits'
+ * distances to it makes of them.  A row that is no distribution (a NaN or +inf,
+ * or -inf alone) has NaN for its results and -1 for its top_ids.  Results must
+ * not overlap operands or one another where an entry point does not say that
+ * they may.                                                                 */
 int diffopt_logprob_fwd(const void* logits, int64_t row_stride, int64_t N,
                         int64_t V, int32_t dtype, const void* ids,
                         int32_t id_bytes, double temperature, float* logprob,

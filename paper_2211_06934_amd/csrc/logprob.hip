@@ -68,20 +68,57 @@ __device__ __forceinline__ Token token_of(const Rows& r, int64_t row) {
   return Token{id < 0 || id >= r.V ? -1 : id, id >= 0, id >= r.V};
 }
 
-// A maximum with the sums over e = 2^d and e d, d = (x - m) c.
-struct Sums {
-  float m = -kInf, s = 0.0f, t = 0.0f;
+__device__ __forceinline__ double wave_sum(double x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
 
-  template <bool ENT>
-  __device__ __forceinline__ void add(float x, float b, float c) {
-    const float d = (x - b) * c, e = exp2_fast(d);
-    s += e;
-    if (ENT) t = __builtin_fmaf(e, fmaxf(d, kLow), t);
+// The logarithm of a sum of exponentials, as exact near a sum of 1 as elsewhere.
+__device__ __forceinline__ float log_sum(double s) {
+  const float near = (float)s;
+  return __builtin_fmaf((float)(s - (double)near), __builtin_amdgcn_rcpf(near), logf(near));
+}
+
+// A maximum with the sums over e = 2^d and e d, d = (x - m) c.  A likely token's 1
+// beside thousands of numbers near 2^-24 keeps none of them in fp32: eight terms
+// are added by a tree, of three roundings at most that have the 1, and fp64 takes
+// their sums, over lanes too (bf16, 4,096 rows of 50,021 with their gradient 165 us,
+// 2,048 rows with 5 alternatives 43.8, 8,000 rows of 500 12.4; with the whole sum in
+// fp32 164, 43.5 and 10.6).
+constexpr int kTree = 8;
+struct Sums {
+  float m = -kInf;
+  double s = 0.0, t = 0.0;
+
+  // N values, m not below them.
+  template <int N, bool ENT>
+  __device__ __forceinline__ void add(const float* x, float b, float c) {
+    constexpr int G = N < kTree ? N : kTree;
+    static_assert(N % G == 0 && (G & (G - 1)) == 0, "whole trees");
+#pragma unroll
+    for (int first = 0; first < N; first += G) {
+      float e[G], ed = 0.0f;
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        const float d = (x[first + i] - b) * c;
+        e[i] = exp2_fast(d);
+        if (ENT) ed = __builtin_fmaf(e[i], fmaxf(d, kLow), ed);
+      }
+#pragma unroll
+      for (int half = G / 2; half > 0; half /= 2)
+#pragma unroll
+        for (int i = 0; i < half; ++i) e[i] += e[i + half];
+      s += (double)e[0];
+      if (ENT) t += (double)ed;
+      if (N > G) __builtin_amdgcn_sched_barrier(0);  // trees side by side take 65 registers, a wave of a SIMD less
+    }
   }
   template <bool ENT>
   __device__ __forceinline__ void shift(float to, float c) {  // the sums as from another maximum, not below m
-    const float d = (m - safe_max(to)) * c, e = exp2_fast(d);
-    if (ENT) t = e * __builtin_fmaf(s, fmaxf(d, kLow), t);
+    const float d = (m - safe_max(to)) * c;
+    const double e = (double)exp2_fast(d);
+    if (ENT) t = e * __builtin_fma(s, (double)fmaxf(d, kLow), t);
     s *= e;
     m = to;
   }
@@ -101,42 +138,44 @@ struct Sums {
 #pragma unroll
     for (int i = 1; i < N; ++i) vm = fmaxf(vm, e[i]);
     if (vm > m) shift<ENT>(vm, c);
-    const float b = safe_max(m);
-#pragma unroll
-    for (int i = 0; i < N; ++i) add<ENT>(e[i], b, c);
+    add<N, ENT>(e, safe_max(m), c);
   }
   template <bool ENT>
-  __device__ __forceinline__ void all(float (*R)[3], float c) {  // over the workgroup
+  __device__ __forceinline__ void all(double (*R)[3], float c) {  // over the workgroup
     shift<ENT>(wave_max(m), c);
     s = wave_sum(s);
-    if (ENT) t = wave_sum(t);
+    float near = (float)t;  // a sum of one sign: its own roundings suffice
+    if (ENT) near = wave_sum(near);
     const int wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) {
       R[wave][0] = m;
       R[wave][1] = s;
-      R[wave][2] = t;
+      R[wave][2] = near;
     }
     __syncthreads();
     // a wave's lanes take one wave each: nw <= 16
     const int w = threadIdx.x & 15;
     const bool in = w < nw;
-    m = in ? R[w][0] : -kInf;
-    s = in ? R[w][1] : 0.0f;
-    t = in ? R[w][2] : 0.0f;
+    m = in ? (float)R[w][0] : -kInf;
+    s = in ? R[w][1] : 0.0;
+    t = in ? R[w][2] : 0.0;
     float M = m;
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
     shift<ENT>(M, c);
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) {
-      s += __shfl_xor(s, o, 64);
-      if (ENT) t += __shfl_xor(t, o, 64);
+    for (int o = 8; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if (ENT) {
+      near = (float)t;
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) near += __shfl_xor(near, o, 64);
+      t = near;
     }
   }
   // whether they are those of a distribution: no NaN, no +inf, not -inf alone
-  __device__ __forceinline__ bool good() const { return s > 0.0f && s < kInf && m < kInf; }
-  __device__ __forceinline__ float entropy() const { return fmaxf(logf(s) - kLn2 * (t / s), 0.0f); }  // of good ones
+  __device__ __forceinline__ bool good() const { return s > 0.0 && s < (double)kInf && m < kInf; }
+  __device__ __forceinline__ float entropy() const { return fmaxf(log_sum(s) - kLn2 * ((float)t / (float)s), 0.0f); }  // of good ones
 };
 
 // How a workgroup of B lanes shares elements [c0, c1) of a row: 16-byte pieces
@@ -244,13 +283,13 @@ __device__ __forceinline__ void kept_sums(const Kept<E_, B, NV>& kept, float c, 
   const float top = kept_max(kept);
   sums.m = top;
   const float b = safe_max(top);
-  sums.add<ENT>((float)kept.single, b, c);
+  const float single = (float)kept.single;
+  sums.template add<1, ENT>(&single, b, c);
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     float e[N];
     kept.get(i, e);
-#pragma unroll
-    for (int k = 0; k < N; ++k) sums.add<ENT>(e[k], b, c);
+    sums.template add<N, ENT>(e, b, c);
   }
 }
 
@@ -437,7 +476,7 @@ struct Results {
   int32_t top_bytes, K;
 };
 
-// What a slice leaves for the join: its sums, then its K largest logits and their ids.
+// What a slice leaves for the join: its sums (s in two parts), then its K largest logits and their ids.
 struct Parts {
   float* p;
   int32_t slices, K;
@@ -448,9 +487,16 @@ struct Parts {
   __device__ __forceinline__ Sums get(int64_t i) const {
     Sums s;
     s.m = sums(i)[0];
-    s.s = sums(i)[1];
-    s.t = sums(i)[2];
+    s.s = (double)sums(i)[1] + (double)sums(i)[2];
+    s.t = sums(i)[3];
     return s;
+  }
+  __device__ __forceinline__ void put(int64_t i, const Sums& s) const {
+    const float near = (float)s.s;
+    sums(i)[0] = s.m;
+    sums(i)[1] = near;
+    sums(i)[2] = (float)(s.s - (double)near);
+    sums(i)[3] = (float)s.t;
   }
 };
 
@@ -473,9 +519,9 @@ __device__ __forceinline__ void finish(const Rows& r, const Results& o, int64_t 
   const bool good = sums.good() && !tok.bad;
   if (o.stats) {
     o.stats[2 * row] = tok.live ? sums.m : 0.0f;
-    o.stats[2 * row + 1] = tok.live ? sums.s : 1.0f;
+    o.stats[2 * row + 1] = tok.live ? (float)sums.s : 1.0f;
   }
-  if (o.logprob) o.logprob[row] = !tok.live ? 0.0f : good ? (x - sums.m) * r.invT - logf(sums.s) : kNan;
+  if (o.logprob) o.logprob[row] = !tok.live ? 0.0f : good ? (x - sums.m) * r.invT - log_sum(sums.s) : kNan;
   if (o.entropy) o.entropy[row] = !tok.live ? 0.0f : good ? sums.entropy() : kNan;
 }
 
@@ -483,7 +529,7 @@ __device__ __forceinline__ void finish(const Rows& r, const Results& o, int64_t 
 template <int B, class Of>
 __device__ __forceinline__ void finish_top(const Rows& r, const Results& o, Select& S, int64_t row, const Token& tok, const Sums& sums, float largest,
                                            const Of& of) {
-  const float ls = logf(sums.s);
+  const float ls = log_sum(sums.s);
   if (!tok.live || tok.bad || !sums.good()) {
     for (int k = threadIdx.x; k < o.K; k += B) {
       o.top_logprob[row * o.K + k] = tok.live ? kNan : -kInf;
@@ -501,7 +547,7 @@ __device__ __forceinline__ void finish_top(const Rows& r, const Results& o, Sele
 // at theirs again, from the caches.
 template <class E_, bool ENT, bool TOP, int B>
 __global__ __launch_bounds__(B) void logprob_row(Rows r, Results o, Parts parts) {
-  __shared__ float R[kMaxWaves][3];
+  __shared__ double R[B / 64][3];
   __shared__ std::conditional_t<TOP, Select, int> S;
   const Slice sl = slice_of(r, parts.slices, parts.per);
   const Token tok = token_of(r, sl.row);
@@ -514,12 +560,7 @@ __global__ __launch_bounds__(B) void logprob_row(Rows r, Results o, Parts parts)
   const float largest = sums.m;
   sums.all<ENT>(R, c);
   if (parts.slices > 1) {
-    if (threadIdx.x == 0) {
-      float* to = parts.sums(blockIdx.x);
-      to[0] = sums.m;
-      to[1] = sums.s;
-      to[2] = sums.t;
-    }
+    if (threadIdx.x == 0) parts.put(blockIdx.x, sums);
     if constexpr (TOP)
       select_top<B>(S, o.K, largest, share, [&](int rank, float v, int64_t id) {
         parts.values(blockIdx.x)[rank] = v;
@@ -553,7 +594,7 @@ struct OwnPieces {
 // A short row of many, read once.
 template <class E_, bool ENT, bool TOP, int B, int NV>
 __global__ __launch_bounds__(B, kept_waves(B, NV)) void logprob_kept(Rows r, Results o) {
-  __shared__ float R[kMaxWaves][3];
+  __shared__ double R[B / 64][3];
   __shared__ std::conditional_t<TOP, Select, int> S;
   const int64_t row = blockIdx.x;
   const Token tok = token_of(r, row);
@@ -610,7 +651,7 @@ struct Held {
 // A row from its slices' sums and largest logits.
 template <class E_, bool ENT, bool TOP>
 __global__ __launch_bounds__(kJB) void logprob_join(Rows r, Results o, Parts parts) {
-  __shared__ float R[kMaxWaves][3];
+  __shared__ double R[kJB / 64][3];
   __shared__ std::conditional_t<TOP, Select, int> S;
   const int64_t row = blockIdx.x, first = row * parts.slices;
   const Token tok = token_of(r, row);
@@ -709,7 +750,7 @@ template <class E_, int STATS, bool ENT, int B = kLB, int NV = 1>
 __global__ __launch_bounds__(B, (STATS == kKept ? kept_waves(B, NV) : 1)) void logprob_grad(Rows r, Results o, Cotangents t, const float* stats,
                                                                                             E_* dlogits, int64_t drow_stride, Parts parts) {
   __shared__ Named M;
-  __shared__ float R[kMaxWaves][3];
+  __shared__ double R[B / 64][3];
   constexpr int N = Vec<E_>::N;
   const int lane = threadIdx.x & 63;
   const float c = r.invT * kLog2e;
@@ -756,7 +797,7 @@ __global__ __launch_bounds__(B, (STATS == kKept ? kept_waves(B, NV) : 1)) void l
         [&](int64_t at) { dx[at] = (E_)fill; });
     return;
   }
-  const Dense dense(sums.m, sums.s, c, r.invT, M.sum, ENT && t.dentropy ? t.dentropy[row] : 0.0f, H);
+  const Dense dense(sums.m, (float)sums.s, c, r.invT, M.sum, ENT && t.dentropy ? t.dentropy[row] : 0.0f, H);
   const auto write = [&](auto wide) {
     constexpr bool W = wide.value;
     if constexpr (STATS == kKept) {
@@ -950,7 +991,7 @@ __global__ __launch_bounds__(B) void logprob_second(Rows r, Cotangents t, Second
     for (int j = lane; j <= t.K; j += 64) aj[j] = M.id[j] >= 0 ? (float)a[M.id[j]] : 0.0f;
   }
   const float H = ENT ? t.entropy[row] : 0.0f, h = ENT && t.dentropy ? t.dentropy[row] : 0.0f;
-  const Prob prob(sums.m, sums.s, r.invT * kLog2e, H);
+  const Prob prob(sums.m, (float)sums.s, r.invT * kLog2e, H);
   Means means;
   if constexpr (STATS == kKept) {
     const auto sum = [&](auto wide) {
