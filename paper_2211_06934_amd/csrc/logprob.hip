@@ -476,12 +476,15 @@ struct Results {
   int32_t top_bytes, K;
 };
 
+constexpr int kMeans = 8;  // floats of a slice's averages
+
 // What a slice leaves for the join: its sums (s in two parts), then its K largest logits and their ids.
 struct Parts {
   float* p;
   int32_t slices, K;
   int64_t per;
   __device__ __forceinline__ float* sums(int64_t i) const { return p + i * (4 + 2 * K); }
+  __device__ __forceinline__ float* means(int64_t i) const { return p + i * kMeans; }  // of the second derivative, in their place
   __device__ __forceinline__ float* values(int64_t i) const { return sums(i) + 4; }
   __device__ __forceinline__ int32_t* ids(int64_t i) const { return reinterpret_cast<int32_t*>(sums(i) + 4 + K); }
   __device__ __forceinline__ Sums get(int64_t i) const {
@@ -846,39 +849,65 @@ struct Second {
   int64_t out_stride;
 };
 
-// The averages under p of a, of a (l + H) and of l + H itself, which is 0 but for
-// roundings that a's mean would carry into the covariance.
+// What a and l + H average to under p, and how they vary together, from sums that
+// have no rounding of a in them: weights of fp32, products and sums of fp64, divided
+// by the weights' own sum.  Sums in fp32 carry a value common to all of a into the
+// covariance, with its rounding: at 100 beside deviations of 0.1 4e-4 of it.  2,048 rows
+// of 50,021 bf16 logits 185 us, 1,024 of 32,000 fp32 logits 96, with fp32 sums 162 and 88;
+// fp32 sums about a at a lane's likeliest token 186 and 97.
 struct Means {
-  float a = 0.0f, al = 0.0f, l = 0.0f;
+  double w = 0.0, a = 0.0, l = 0.0, al = 0.0;
   template <bool ENT>
   __device__ __forceinline__ void add(float e, float lH, float v) {
-    a = __builtin_fmaf(e, v, a);
+    const double p = (double)e, u = (double)v;
+    w += p;
+    a = __builtin_fma(p, u, a);
     if (ENT) {
-      const float el = e * lH;
-      l += el;
-      al = __builtin_fmaf(el, v, al);
+      const double pl = (double)(e * lH);
+      l += pl;
+      al = __builtin_fma(pl, u, al);
     }
   }
   template <bool ENT>
-  __device__ __forceinline__ void all(float (*R)[3]) {  // over the workgroup
+  __device__ __forceinline__ void all(double (*R)[4]) {  // over the workgroup
+    w = wave_sum(w);
     a = wave_sum(a);
     if (ENT) {
-      al = wave_sum(al);
       l = wave_sum(l);
+      al = wave_sum(al);
     }
     __syncthreads();
     if ((threadIdx.x & 63) == 0) {
-      R[threadIdx.x >> 6][0] = a;
-      R[threadIdx.x >> 6][1] = al;
-      R[threadIdx.x >> 6][2] = l;
+      double* to = R[threadIdx.x >> 6];
+      to[0] = w;
+      to[1] = a;
+      to[2] = l;
+      to[3] = al;
     }
     __syncthreads();
-    a = al = l = 0.0f;
-    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) {
-      a += R[w][0];
-      al += R[w][1];
-      l += R[w][2];
+    w = a = l = al = 0.0;
+#pragma unroll 4
+    for (int i = 0; i < (int)(blockDim.x >> 6); ++i) {
+      w += R[i][0];
+      a += R[i][1];
+      l += R[i][2];
+      al += R[i][3];
     }
+  }
+  // of a slice: each sum in two parts
+  __device__ __forceinline__ void put(float* to) const {
+    const double v[4] = {w, a, l, al};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      to[2 * i] = (float)v[i];
+      to[2 * i + 1] = (float)(v[i] - (double)to[2 * i]);
+    }
+  }
+  __device__ __forceinline__ void take(const float* from) {
+    w += (double)from[0] + (double)from[1];
+    a += (double)from[2] + (double)from[3];
+    l += (double)from[4] + (double)from[5];
+    al += (double)from[6] + (double)from[7];
   }
 };
 
@@ -924,7 +953,7 @@ __device__ __forceinline__ void row_means(const E_* x, const E_* a, int64_t c0, 
 // A slice's averages, for rows that several workgroups share.
 template <class E_, bool ENT>
 __global__ __launch_bounds__(kLB) void logprob_second_parts(Rows r, Cotangents t, Second q, Parts parts) {
-  __shared__ float R[kMaxWaves][3];
+  __shared__ double R[kLB / 64][4];
   const Slice sl = slice_of(r, parts.slices, parts.per);
   if (!token_of(r, sl.row).live) return;
   const Prob prob(q.stats[2 * sl.row], q.stats[2 * sl.row + 1], r.invT * kLog2e, ENT ? t.entropy[sl.row] : 0.0f);
@@ -932,19 +961,15 @@ __global__ __launch_bounds__(kLB) void logprob_second_parts(Rows r, Cotangents t
   row_means<E_, ENT>(static_cast<const E_*>(r.logits) + sl.row * r.row_stride, static_cast<const E_*>(q.a) + sl.row * q.a_stride, sl.c0, sl.c1, prob,
                      means);
   means.all<ENT>(R);
-  if (threadIdx.x == 0) {
-    float* to = parts.sums(blockIdx.x);
-    to[0] = means.a;
-    to[1] = means.al;
-    to[2] = means.l;
-  }
+  if (threadIdx.x == 0) means.put(parts.means(blockIdx.x));
 }
 
 // Logits and a read once where they stay in registers, a result written.
 template <class E_, int STATS, bool ENT, int B = kLB, int NV = 1>
 __global__ __launch_bounds__(B) void logprob_second(Rows r, Cotangents t, Second q, Parts parts) {
   __shared__ Named M;
-  __shared__ float R[kMaxWaves][3], aj[kMaxTop + 1];
+  __shared__ double R[B / 64][4];
+  __shared__ float aj[kMaxTop + 1];
   constexpr int N = Vec<E_>::N;
   const int lane = threadIdx.x & 63;
   const Slice sl = slice_of(r, parts.slices, parts.per);
@@ -1003,6 +1028,7 @@ __global__ __launch_bounds__(B) void logprob_second(Rows r, Cotangents t, Second
       one((float)kx.single, (float)ka.single);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
+        if (!kx.has(i)) continue;  // short rows: whole waves have nothing (8,000 of 500 bf16 logits 30.3 us, all pieces summed 46)
         float e[N], u[N];
         kx.get(i, e);
         ka.get(i, u);
@@ -1017,29 +1043,26 @@ __global__ __launch_bounds__(B) void logprob_second(Rows r, Cotangents t, Second
   } else if constexpr (STATS == kRead) {
     row_means<E_, ENT>(x, a, 0, r.V, prob, means);
   } else {
-    for (int i = threadIdx.x; i < parts.slices; i += B) {
-      const float* from = parts.sums(row * parts.slices + i);
-      means.a += from[0];
-      means.al += from[1];
-      means.l += from[2];
-    }
+    for (int i = threadIdx.x; i < parts.slices; i += B) means.take(parts.means(row * parts.slices + i));
   }
   means.all<ENT>(R);  // also: the named tokens are there
-  const float mean = means.a, kappa = means.al - mean * means.l, G = M.sum;
+  const double mean = means.a / means.w;
+  const float kappa = ENT ? (float)((means.al - mean * means.l) / means.w) : 0.0f, G = M.sum;
+  const float near = (float)mean, rest = (float)(mean - (double)near);  // a's distance to the mean is a - near, exact where they are close, less the rest
   if (first) {
     if (threadIdx.x == 0) {
-      if (q.out_dlogprob) q.out_dlogprob[row] = M.id[t.K] >= 0 ? r.invT * (aj[t.K] - mean) : 0.0f;
+      if (q.out_dlogprob) q.out_dlogprob[row] = M.id[t.K] >= 0 ? r.invT * (aj[t.K] - near - rest) : 0.0f;
       if (q.out_dentropy) q.out_dentropy[row] = ENT ? -r.invT * kappa : 0.0f;
     }
     if (q.out_dtop)
-      for (int k = threadIdx.x; k < t.K; k += B) q.out_dtop[row * t.K + k] = M.id[k] >= 0 ? r.invT * (aj[k] - mean) : 0.0f;
+      for (int k = threadIdx.x; k < t.K; k += B) q.out_dtop[row * t.K + k] = M.id[k] >= 0 ? r.invT * (aj[k] - near - rest) : 0.0f;
   }
   const float w = -r.invT * r.invT;
   const auto write = [&](auto wide) {
     const auto value = [&](float v, float u) {
       float e, l;
       prob.at<ENT, wide.value>(v, e, l);
-      const float du = u - mean;
+      const float du = u - near - rest;
       return w * e * (ENT ? __builtin_fmaf(du, __builtin_fmaf(h, l + 1.0f, G), -h * kappa) : du * G);
     };
     if constexpr (STATS == kKept) {
@@ -1134,7 +1157,7 @@ constexpr int64_t kKeptRows = 2048;
 
 int64_t parts_bytes(int64_t N, int64_t V, int32_t dtype, int64_t K) {
   const Cut c = row_cut(N, V, dtype, K);
-  return c.slices > 1 ? N * c.slices * (4 + 2 * K) * 4 : 0;
+  return c.slices > 1 ? N * c.slices * (K ? 4 + 2 * K : kMeans) * 4 : 0;  // K = 0: the second derivative's too
 }
 
 int check_workspace(const char* who, const Rows& r, int32_t dtype, int64_t K, void* workspace, int64_t bytes) {
