@@ -444,8 +444,10 @@ int diffopt_clip_norm_fwd_tree(const diffopt_segtable* table,
 /* Their vector-Jacobian product, for cotangents dout and dnorm (a DEVICE fp32
  * scalar; either NULL: 0):
  *   dgrad = c dout + grad (dnorm - [c < 1] c <dout, grad> / (norm + eps)) / norm
- * and 0 in place of the second term for a norm of 0.  dgrad may be dout or
- * grad.                                                                     */
+ * and 0 in place of the second term for a norm of 0.  c and the norm are those
+ * of stats: where c is rounded to 1, nothing was clipped; a norm of finite
+ * elements that is above fp32 is infinite there, and has no second term.
+ * dgrad may be dout or grad.                                                */
 int diffopt_clip_norm_bwd(const float* dout, const float* dnorm,
                           const float* grad, const float* stats, int64_t n,
                           double eps, float* dgrad, void* workspace,

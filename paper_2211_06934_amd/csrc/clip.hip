@@ -285,12 +285,32 @@ __device__ __forceinline__ float scale_of(double norm, double max_norm, double e
 }
 
 // The factor of the gradient in its own gradient: d norm / d g = g / norm, d c / d
-// norm = -c / (norm + eps) where c < 1.
-__device__ __forceinline__ float slope_of(double dot, const float* dnorm, float norm, float c, double eps) {
-  if (norm == 0.0f) return 0.0f;
+// norm = -c / (norm + eps) where c < 1.  A norm below 3e-39 has a factor above any fp32
+// number, a large one may have one below, though the product is an ordinary number: the
+// factor is rounded to 24 bits and keeps its power of two apart, which goes to the
+// element before the product where it is large and after it where it is small.
+struct Factor {
+  float part;
+  int32_t before, after;
+  __device__ __forceinline__ explicit Factor(double x) : part((float)x), before(0), after(0) {
+    if (x == 0.0 || !__builtin_isfinite(x)) return;
+    const int32_t e = __builtin_amdgcn_frexp_exp(x);
+    part = (float)__builtin_amdgcn_frexp_mant(x);  // in [1/2, 1]
+    if (e > 0) {
+      part *= 2.0f;
+      before = e - 1;
+    } else {
+      after = e;
+    }
+  }
+  __device__ __forceinline__ float times(float g) const { return __builtin_ldexpf(__builtin_ldexpf(g, before) * part, after); }
+};
+
+__device__ __forceinline__ Factor slope_of(double dot, const float* dnorm, float norm, float c, double eps) {
+  if (norm == 0.0f) return Factor(0.0);
   double x = dnorm ? (double)*dnorm : 0.0;
   if (!(c >= 1.0f)) x -= (double)c * dot / ((double)norm + eps);
-  return (float)(x / (double)norm);
+  return Factor(x / (double)norm);
 }
 
 // out = c grad (operands 0 grad, 1 out); workgroup 0 writes the norm and c.
@@ -355,8 +375,8 @@ __global__ __launch_bounds__(kScaleBlock) void clip_gradient(Space sp, Operands<
     v[u] = load4(o ? leaf.p[0] : dummy, o ? w : 0);
     if constexpr (DOUT) d[u] = load4(o ? leaf.p[NA - 1] : dummy, o ? w : 0);
   });
-  const float slope = slope_of(parts.sum(), dnorm, norm, c, eps);
-  const auto value = [&](float g, float dy) { return DOUT ? __builtin_fmaf(c, dy, slope * g) : slope * g; };
+  const Factor slope = slope_of(parts.sum(), dnorm, norm, c, eps);
+  const auto value = [&](float g, float dy) { return DOUT ? __builtin_fmaf(c, dy, slope.times(g)) : slope.times(g); };
 #pragma unroll
   for (int u = 0; u < kGroups; ++u) {
     f32x4 y;
@@ -453,10 +473,10 @@ __global__ __launch_bounds__(kAloneBlock) void clip_gradient_alone(TinyTable tt,
   }
 #pragma unroll
   for (int k = 0; k < kAloneEach; ++k) acc = __builtin_fma((double)v[k], (double)d[k], acc);
-  const float slope = slope_of(DOUT ? alone_sum(acc) : 0.0, dnorm, norm, c, eps);
+  const Factor slope = slope_of(DOUT ? alone_sum(acc) : 0.0, dnorm, norm, c, eps);
 #pragma unroll
   for (int k = 0; k < kAloneEach; ++k)
-    if (to[k]) *to[k] = DOUT ? __builtin_fmaf(c, d[k], slope * v[k]) : slope * v[k];
+    if (to[k]) *to[k] = DOUT ? __builtin_fmaf(c, d[k], slope.times(v[k])) : slope.times(v[k]);
 }
 
 // ---- host -------------------------------------------------------------------
