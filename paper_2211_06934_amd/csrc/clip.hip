@@ -216,7 +216,7 @@ __global__ __launch_bounds__(64 * kSumWaves, 4) void clip_sums(Space sp, Operand
   double acc[2] = {0.0, 0.0};
   static_assert(kGroups * 4 == 32, "a lane's elements are the bits of a word");
   const bool skip = NA == 2 && stats[1] >= 1.0f;
-  using T = Tile<FLAT, NA, FLAT ? 0 : -1>;
+  using T = Tile<FLAT, NA, -1>;  // groups counted from the first element: an order that goes by no address
   const auto tile_at = [&](int64_t b, int half) { return T(sp, ops, reinterpret_cast<Window<NA>&>(windows[FLAT ? 0 : wave][FLAT ? 0 : half]), b, lane); };
   // wave after wave takes a tile, workgroup after workgroup: neighbouring tiles are read together
   int64_t b = (int64_t)wave * gridDim.x + blockIdx.x;
