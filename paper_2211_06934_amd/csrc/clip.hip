@@ -481,6 +481,8 @@ __global__ __launch_bounds__(kAloneBlock) void clip_gradient_alone(TinyTable tt,
 
 // ---- host -------------------------------------------------------------------
 
+constexpr int64_t kMostElements = int64_t(1) << 36;
+
 // A call's elements: a table's, or n of a buffer.
 struct Elements {
   const diffopt_segtable* table;
@@ -498,7 +500,9 @@ struct Elements {
     return table ? Space{table->d_seg, table->d_tile_first, table->ntiles, table->ngroups, 0, table->dense_orig}
                  : Space{nullptr, nullptr, tiles(), tiles() * kTileGroups, n, 0};
   }
-  unsigned scale_blocks() const { return (unsigned)((tiles() + kScaleWaves - 1) / kScaleWaves); }
+  int64_t scale_blocks() const { return (tiles() + kScaleWaves - 1) / kScaleWaves; }
+  // what a call takes: a launch has fewer than 2^32 threads (a tree's leaves begin tiles of their own)
+  bool fits() const { return count() >= 0 && count() < kMostElements && scale_blocks() < (int64_t(1) << 32) / kScaleBlock; }
 };
 
 #define DIFFOPT_LAUNCH(kernel, grid, block, ...) hipLaunchKernelGGL((kernel), dim3((unsigned)(grid)), dim3(block), 0, st, __VA_ARGS__)
@@ -515,7 +519,7 @@ int fwd(const char* who, const Elements& e, const void* grad, double max_norm, d
   const Operands<1> one{{grad}};
   const float* none = nullptr;
   DIFFOPT_LAUNCH((clip_sums<FLAT, 1>), e.parts(), 64 * kSumWaves, sp, one, none, parts);
-  DIFFOPT_LAUNCH((clip_scale<FLAT>), out ? e.scale_blocks() : 1u, kScaleBlock, sp, ops, parts, e.parts(), max_norm, eps, stats);
+  DIFFOPT_LAUNCH((clip_scale<FLAT>), out ? e.scale_blocks() : 1, kScaleBlock, sp, ops, parts, e.parts(), max_norm, eps, stats);
   return launch_status(who);
 }
 
@@ -549,7 +553,7 @@ int check_numbers(const char* who, double max_norm, double eps) {
 }
 
 int check_elements(const char* who, const Elements& e, void* workspace, int64_t bytes) {
-  if (e.scale_blocks() >= (uint64_t(1) << 32) / kScaleBlock) return fail(DIFFOPT_EINVAL, "%s: too many elements", who);
+  if (!e.fits()) return fail(DIFFOPT_EINVAL, "%s: too many elements", who);
   const int64_t need = e.workspace();
   if (need > 0 && (!workspace || bytes < need))
     return fail(DIFFOPT_EINVAL, "%s: the workspace has %lld bytes of %lld", who, (long long)(workspace ? bytes : 0), (long long)need);
@@ -579,20 +583,19 @@ int check_buffers(const char* who, const char* what, const float* result, std::i
   return DIFFOPT_OK;
 }
 
-constexpr int64_t kMostElements = int64_t(1) << 40;  // before anything is computed of it
-
 }  // namespace
 }  // namespace diffopt
 
 using namespace diffopt;
 
 extern "C" int64_t diffopt_clip_norm_workspace(int64_t n) {
-  if (n < 0 || n > kMostElements) return -1;
-  return Elements{nullptr, n}.workspace();
+  const Elements e{nullptr, n};
+  return e.fits() ? e.workspace() : -1;
 }
 
 extern "C" int64_t diffopt_clip_norm_workspace_tree(const diffopt_segtable* table) {
-  return table ? Elements{table, 0}.workspace() : -1;
+  const Elements e{table, 0};
+  return table && e.fits() ? e.workspace() : -1;
 }
 
 extern "C" int diffopt_clip_norm_fwd(const float* grad, int64_t n, double max_norm, double eps, float* out, float* stats, void* workspace,
@@ -600,7 +603,6 @@ extern "C" int diffopt_clip_norm_fwd(const float* grad, int64_t n, double max_no
   clear_error();
   static const char* who = "diffopt_clip_norm_fwd";
   if (n < 0) return fail(DIFFOPT_EINVAL, "%s: n must be >= 0", who);
-  if (n > kMostElements) return fail(DIFFOPT_EINVAL, "%s: too many elements", who);
   int rc = check_numbers(who, max_norm, eps);
   if (rc) return rc;
   if (!stats || (n > 0 && !grad)) return fail(DIFFOPT_EINVAL, "%s: null grad or stats", who);
@@ -634,7 +636,6 @@ extern "C" int diffopt_clip_norm_bwd(const float* dout, const float* dnorm, cons
   clear_error();
   static const char* who = "diffopt_clip_norm_bwd";
   if (n < 0) return fail(DIFFOPT_EINVAL, "%s: n must be >= 0", who);
-  if (n > kMostElements) return fail(DIFFOPT_EINVAL, "%s: too many elements", who);
   int rc = check_numbers(who, 0.0, eps);
   if (rc || n == 0) return rc;
   if (!grad || !stats || !dgrad) return fail(DIFFOPT_EINVAL, "%s: null grad, stats or dgrad", who);

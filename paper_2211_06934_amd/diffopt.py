@@ -595,7 +595,10 @@ def clip_norm_workspace(n: int) -> int:
 
 def clip_norm_workspace_tree(table: SegTable) -> int:
     """diffopt_clip_norm_workspace_tree: bytes that clip_norm_fwd_tree and clip_norm_bwd_tree need for this table."""
-    return int(_lib.diffopt_clip_norm_workspace_tree(table.handle))
+    need = int(_lib.diffopt_clip_norm_workspace_tree(table.handle))
+    if need < 0:
+        raise ValueError("clip_norm: a size that the operator refuses")
+    return need
 
 
 def _clip_scratch(given, need: int, like: torch.Tensor, stream):
