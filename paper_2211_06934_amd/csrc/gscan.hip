@@ -907,6 +907,59 @@ int check_arrays(const char* who, int32_t dtype, std::initializer_list<Operand> 
   return DIFFOPT_OK;
 }
 
+// An array of a call: B x T rows of `bytes` bytes, or one piece (B and T 1).
+struct Extent {
+  const char* name;
+  const void* p;
+  int64_t bytes, B = 1, T = 1, sb = 0, st = 0;  // strides in bytes
+  int64_t low() const { return (sb < 0 ? sb * (B - 1) : 0) + (st < 0 ? st * (T - 1) : 0); }
+  int64_t high() const { return (sb > 0 ? sb * (B - 1) : 0) + (st > 0 ? st * (T - 1) : 0) + bytes; }
+  bool piece() const { return B == 1 && T == 1; }
+};
+
+Extent rows_of(const char* name, const HeadArr& h, int64_t B, int64_t T, int64_t C, int64_t size) {
+  return Extent{name, T > 0 ? h.p : nullptr, C * size, B, T, B > 1 ? h.sb * size : 0, T > 1 ? h.st * size : 0};
+}
+
+// Whether from + j step lies in (-below, above) for a j of [first, last].
+bool lands(int64_t from, int64_t step, int64_t first, int64_t last, int64_t below, int64_t above) {
+  int64_t j = first;
+  if (step < 0) {
+    step = -step;
+    j = -last;
+    last = -first;
+  }
+  if (step > 0 && from + j * step <= -below) j += (-below - (from + j * step)) / step + 1;  // the first that is above -below
+  return j <= last && from + j * step > -below && from + j * step < above;
+}
+
+// Whether two arrays share bytes: exact for a piece, and for rows at the same strides;
+// rows at other strides meet where their spans do.
+bool meet(const Extent& a, const Extent& b) {
+  if (!a.p || !b.p) return false;
+  const int64_t from = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p));
+  if (from + b.low() >= a.high() || from + b.high() <= a.low()) return false;
+  if (!a.piece() && !b.piece() && (a.sb != b.sb || a.st != b.st)) return true;
+  // one of b's rows begins less than a's bytes after one of a's, or less than b's before it: the shorter axis step by step
+  const Extent& r = a.piece() ? b : a;
+  const bool by_b = r.B <= r.T;
+  for (int64_t i = by_b ? 1 - a.B : 1 - a.T; i < (by_b ? b.B : b.T); ++i)
+    if (by_b ? lands(from + i * r.sb, r.st, 1 - a.T, b.T - 1, b.bytes, a.bytes) : lands(from + i * r.st, r.sb, 1 - a.B, b.B - 1, b.bytes, a.bytes)) return true;
+  return false;
+}
+
+// No result shares bytes with an operand or with another result.  Strides can let rows
+// of two arrays lie beside one another, so that their first addresses say little.
+int check_apart(const char* who, std::initializer_list<Extent> operands, std::initializer_list<Extent> results) {
+  for (auto r = results.begin(); r != results.end(); ++r) {
+    for (const Extent& o : operands)
+      if (meet(*r, o)) return fail(DIFFOPT_EINVAL, "%s: %s must lie apart from %s", who, r->name, o.name);
+    for (auto t = results.begin(); t != r; ++t)
+      if (meet(*r, *t)) return fail(DIFFOPT_EINVAL, "%s: %s must lie apart from %s", who, r->name, t->name);
+  }
+  return DIFFOPT_OK;
+}
+
 struct States32 {
   const char* name;
   const float* p;
@@ -964,6 +1017,9 @@ extern "C" int diffopt_gscan_fwd(const diffopt_heads* log_gate, const diffopt_he
   const bool in_place = state && state_out == state;
   if (!rc) rc = check_states(who, 4 * B * C, {{"state", in_place ? nullptr : state}}, {{"state_out", state_out}});
   if (!rc) rc = check_workspace(who, B, T, C, dtype, kFwd, workspace, workspace_bytes);
+  const auto rows = [&](const char* name, const HeadArr& h) { return rows_of(name, h, B, T, C, elem_size(dtype)); };
+  const Extent ends{"lengths", lengths, 4 * B}, begin{"state", in_place ? nullptr : state, 4 * B * C};
+  if (!rc) rc = check_apart(who, {rows("log_gate", s.lg), rows("x", s.x), ends, begin}, {rows("h", s.out[0]), {"state_out", state_out, 4 * B * C}});
   if (rc || (T == 0 && !state_out)) return rc;
   s.lengths = lengths;
   s.state = state;
@@ -989,6 +1045,11 @@ extern "C" int diffopt_gscan_bwd(const diffopt_heads* dh, const float* dstate_ou
                       {{"dlog_gate", dlog_gate, &s.out[0], true}, {"dx", dx, &s.out[1], true}});
   if (!rc) rc = check_states(who, 4 * B * C, {{"state", state}, {"dstate_out", dstate_out}}, {{"dstate", dstate}});
   if (!rc) rc = check_workspace(who, B, T, C, dtype, kBwd, workspace, workspace_bytes);
+  const auto rows = [&](const char* name, const HeadArr& h) { return rows_of(name, h, B, T, C, elem_size(dtype)); };
+  const auto states = [&](const char* name, const float* p) { return Extent{name, p, 4 * B * C}; };
+  if (!rc)
+    rc = check_apart(who, {rows("log_gate", s.lg), rows("x", s.x), rows("dh", s.dh), {"lengths", lengths, 4 * B}, states("state", state), states("dstate_out", dstate_out)},
+                     {rows("dlog_gate", s.out[0]), rows("dx", s.out[1]), states("dstate", dstate)});
   if (rc || ((T == 0 || (!dlog_gate && !dx)) && !dstate)) return rc;
   s.lengths = lengths;
   s.state = state;
@@ -1019,6 +1080,14 @@ extern "C" int diffopt_gscan_bwd_bwd(const diffopt_heads* ddlog_gate, const diff
     rc = check_states(who, 4 * B * C, {{"state", state}, {"dstate_out", dstate_out}, {"ddstate", ddstate}},
                       {{"out_dstate_out", out_dstate_out}, {"out_state", out_state}});
   if (!rc) rc = check_workspace(who, B, T, C, dtype, kSecond, workspace, workspace_bytes);
+  const auto rows = [&](const char* name, const HeadArr& h) { return rows_of(name, h, B, T, C, elem_size(dtype)); };
+  const auto states = [&](const char* name, const float* p) { return Extent{name, p, 4 * B * C}; };
+  if (!rc)
+    rc = check_apart(who,
+                     {rows("ddlog_gate", s.r), rows("ddx", s.p), rows("dh", s.dh), rows("log_gate", s.lg), rows("x", s.x), {"lengths", lengths, 4 * B},
+                      states("state", state), states("dstate_out", dstate_out), states("ddstate", ddstate)},
+                     {rows("out_dh", s.out[0]), rows("out_log_gate", s.out[1]), rows("out_x", s.out[2]), states("out_dstate_out", out_dstate_out),
+                      states("out_state", out_state)});
   if (rc || (T == 0 && !out_dstate_out && !out_state)) return rc;
   s.lengths = lengths;
   s.state = state;
@@ -1044,7 +1113,12 @@ extern "C" int diffopt_gscan_step(const diffopt_heads* log_gate, const diffopt_h
   if (rc) return rc;
   if (!state) return fail(DIFFOPT_EINVAL, "%s: null state", who);
   if (!aligned_to(state, 4)) return fail(DIFFOPT_EINVAL, "%s: state is not 4-byte aligned", who);
-  if (state == lg.p || state == xs.p || state == o.p) return fail(DIFFOPT_EINVAL, "%s: state must lie apart from the operands and out", who);
+  const auto rows = [&](const char* name, const HeadArr& h) { return rows_of(name, h, B, 1, C, elem_size(dtype)); };
+  const Extent in_place{"state", state, 4 * B * C};
+  for (const Extent& e : {rows("log_gate", lg), rows("x", xs), rows("out", o)})
+    if (meet(in_place, e)) return fail(DIFFOPT_EINVAL, "%s: state must lie apart from the operands and out", who);
+  rc = check_apart(who, {rows("log_gate", lg), rows("x", xs)}, {rows("out", o)});
+  if (rc) return rc;
   const hipStream_t st = as_stream(stream);
   const auto go = [&](auto kernel, int vec) {
     const int64_t cols = C / vec, n = B * cols;
