@@ -789,8 +789,9 @@ int64_t diffopt_distill_workspace(int64_t N, int64_t V, int32_t dtype,
  *   h_t = a_t h_{t-1} + x_t,  a_t = exp(log_gate_t)   t = 0 .. lengths[b] - 1
  *   state_out = h_{lengths[b]-1}                      (h_{-1} = state)
  * Tokens from lengths[b] on are not read and get h = 0.  A gate of -inf
- * forgets what came before.  Gates above 0 are taken too; where the product of
- * a run of them leaves fp32, results do.  Results must not overlap operands or
+ * multiplies the state by 0: it forgets what came before if that is finite, and
+ * an infinite state or a NaN is a NaN from there on.  Gates above 0 are taken
+ * too; where the product of a run of them leaves fp32, results do.  Results must not overlap operands or
  * one another where an entry point does not say that they may (rows may lie
  * between another array's rows of the same strides).
  *   log_gate, x, h  [B][T][C]: diffopt_heads whose heads are not used
