@@ -421,7 +421,7 @@ __device__ __forceinline__ void store_rows(const Scan& s, const HeadArr& h, cons
 // A chunk's results.  JOIN: the sequence has at most kW chunks, whose runs the
 // workgroup joins itself.
 template <class E, int MODE, int VEC, int U, bool JOIN>
-__global__ __launch_bounds__(64 * kW, (MODE == kSecond && JOIN ? 4 : 1)) void gscan_walk(Scan s) {
+__global__ __launch_bounds__(64 * kW) void gscan_walk(Scan s) {
   __shared__ Runs<MODE, VEC> R;
   __shared__ std::conditional_t<JOIN, Runs<MODE, VEC>, char> J;
   const Place<VEC> at(s, s.from_end);

@@ -219,8 +219,8 @@ def gated_scan(log_gate, x, state=None, lengths=None, return_state: bool = False
     """h_t = exp(log_gate_t) h_{t-1} + x_t for each channel, over sequences: log_gate and x [B, T, C], both fp32 or both bf16.
 
     state: fp32 [B, C] before the first token (None: zeros).  lengths: int32 [B]; tokens from there on give zeros.  A gate
-    of -inf forgets a finite state (where another document begins); infinities and NaN go on as NaN.  Returns h [B, T, C], with return_state also the
-    state after the last token.  Differentiable twice in log_gate, x and state."""
+    of -inf forgets a finite state (where another document begins); an infinite one or a NaN goes on as NaN.  Returns h
+    [B, T, C], with return_state also the state after the last token.  Differentiable twice in log_gate, x and state."""
     _o._axes(3, (log_gate, "log_gate"), (x, "x"))
     if state is not None:
         _o._axes(2, (state, "state"))
