@@ -9,15 +9,16 @@
 // at no cost: two instructions for an element of four bytes.  Bound by memory, the
 // elements being read twice; the second pass goes backwards, so that it begins
 // with what the first one left in the Infinity Cache.  A tree of 354M elements: the
-// sums read 6.0 TB/s, the second pass moves 5.8.
+// sums read 6.0 TB/s by themselves (236 us), 5.3 (269) where the results of a pass before
+// are still on their way to memory; the second pass moves 5.8 (490).
 //
 // A wave takes one tile of the segment table (512 groups of four elements).  A
 // tile inside one leaf reads that leaf's entry with scalar loads; others stage
 // their window of the table in the wave's own LDS and search it, so that
-// waves never wait for one another.  The sums look up a wave's next tile while this
-// one's elements are on their way (20M elements in 3,384 leaves 20.7 us, looked
-// up afterwards 26.9).  Gradients of up to kAlone elements take one launch of one
-// workgroup, which keeps them in registers.
+// waves never wait for one another (looking a wave's next tile up while this one's
+// elements are on their way takes as long or longer: 20M elements in 3,384 leaves 19.1
+// and 19.8 us, in 200,000 24.7 and 25.6).  Gradients of up to kAlone elements take one
+// launch of one workgroup, which keeps them in registers.
 #include <cmath>
 #include <initializer_list>
 #include <type_traits>
@@ -30,8 +31,8 @@ namespace {
 
 constexpr int kScaleBlock = 256, kScaleWaves = kScaleBlock / 64;
 // Waves of a workgroup of sums, and how many workgroups there are at most: one large
-// one a compute unit (trees of 354M and of 20M elements 236 and 20.8 us; 512 workgroups of
-// 8 waves 256 and 20.7, 256 of them 231 and 23.1).
+// one a compute unit (trees of 354M and of 20M elements, behind other passes' results, 269
+// and 20.3 us; 512 workgroups of 8 waves 277 and 18.9, 256 of them 264 and 22.8).
 constexpr int kSumWaves = 16, kMostParts = 256;
 constexpr int kGroups = (int)(kTileGroups / 64);  // of a lane
 constexpr int kAloneBlock = 1024, kAloneEach = 8;
@@ -210,18 +211,17 @@ __device__ __forceinline__ double wave_sum(double x) {
 // the sum has no weight then.
 template <bool FLAT, int NA>
 __global__ __launch_bounds__(64 * kSumWaves, 4) void clip_sums(Space sp, Operands<NA> ops, const float* stats, double* parts) {
-  __shared__ std::conditional_t<FLAT, char, Window<NA>> windows[kSumWaves][2];
+  __shared__ std::conditional_t<FLAT, char, Window<NA>> windows[kSumWaves];
   __shared__ double sums[kSumWaves];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   double acc[2] = {0.0, 0.0};
   static_assert(kGroups * 4 == 32, "a lane's elements are the bits of a word");
   const bool skip = NA == 2 && stats[1] >= 1.0f;
   using T = Tile<FLAT, NA, -1>;  // groups counted from the first element: an order that goes by no address
-  const auto tile_at = [&](int64_t b, int half) { return T(sp, ops, reinterpret_cast<Window<NA>&>(windows[FLAT ? 0 : wave][FLAT ? 0 : half]), b, lane); };
   // wave after wave takes a tile, workgroup after workgroup: neighbouring tiles are read together
-  int64_t b = (int64_t)wave * gridDim.x + blockIdx.x;
-  if (!skip && b < sp.ntiles)
-    for (T tile = tile_at(b, 0), next = tile;; tile = next) {
+  if (!skip)
+    for (int64_t b = (int64_t)wave * gridDim.x + blockIdx.x; b < sp.ntiles; b += (int64_t)gridDim.x * kSumWaves) {
+      const T tile(sp, ops, reinterpret_cast<Window<NA>&>(windows[FLAT ? 0 : wave]), b, lane);
       f32x4 v[NA][kGroups];
       uint32_t own = 0;  // four bits a group
       const uint64_t dummy = FLAT ? reinterpret_cast<uint64_t>(ops.a[0]) : reinterpret_cast<uint64_t>(sp.seg);  // 16 bytes that are there
@@ -230,9 +230,6 @@ __global__ __launch_bounds__(64 * kSumWaves, 4) void clip_sums(Space sp, Operand
 #pragma unroll
         for (int q = 0; q < NA; ++q) v[q][u] = load4(o ? leaf.p[q] : dummy, o ? w : 0);
       });
-      b += (int64_t)gridDim.x * kSumWaves;
-      const bool more = b < sp.ntiles;
-      if (more) next = tile_at(b, tile.win == reinterpret_cast<Window<NA>*>(&windows[FLAT ? 0 : wave][0]));  // its leaves are found while the elements are on their way
       if (!__all(own == ~0u)) {
 #pragma unroll
         for (int u = 0; u < kGroups; ++u)
@@ -251,8 +248,7 @@ __global__ __launch_bounds__(64 * kSumWaves, 4) void clip_sums(Space sp, Operand
           const double x = gaddr<const float>(leaf.p[0])[i], y = gaddr<const float>(leaf.p[NA - 1])[i];
           acc[0] += x * y;
         });
-      if (!more) break;
-      if constexpr (!FLAT) wave_sync();  // this tile's window is the one after the next's
+      if constexpr (!FLAT) wave_sync();  // the next tile's window takes this one's place
     }
   const double sum = wave_sum(acc[0] + acc[1]);
   if (lane == 0) sums[wave] = sum;
