@@ -11,15 +11,15 @@
 // logits 24 for K = 20 and 64 groups, 177 for K = 128 and 256).  They are ranked by value and lowest
 // id in LDS.  A row of so many equal logits that they do not fit there takes
 // eight counting passes over the digits of (value, id) instead.  Eight rows of
-// 131,072 fp32 logits with 20: slices 6.1 us, join 5.1, both latency.
+// 131,072 fp32 logits with 20: slices 7.0 us, join 5.1, both latency.
 // The gradient's dense part takes the row from registers where the same call
 // has read it (rows of up to 256 KiB), else from memory; the tokens that are
 // named are written once more after a barrier.  A few exponentials per element:
 // bound by memory.  4,096 rows of 50,021 bf16 logits, a tenth of them padding: results
-// and gradient at once 157 us (779 MB, 5.0 TB/s).  2,048 rows with 5 alternatives: 42 us
-// (205 MB, 4.9 TB/s).  1,024 rows of 32,000 fp32 logits with 8: forward 37 us where
-// earlier results are still on their way to memory, else 25 (131 MB, 5.2 TB/s), gradient
-// 43 (262 MB, 6.1 TB/s), its backward 80 (393 MB, 4.9 TB/s).
+// and gradient at once 158 us (779 MB, 4.9 TB/s).  2,048 rows with 5 alternatives: 43 us
+// (205 MB, 4.8 TB/s).  1,024 rows of 32,000 fp32 logits with 8: forward 38 us where
+// earlier results are still on their way to memory, else 28 with its launch (131 MB),
+// gradient 43 (262 MB, 6.1 TB/s), its backward 91 (393 MB, 4.3 TB/s).
 #include <type_traits>
 
 #include "lm_rows.hpp"
@@ -32,7 +32,7 @@ constexpr int kJB = 256;     // ... of a row's joined slices
 constexpr int kMaxTop = 128;
 constexpr int kCap = 1024;   // candidates that are ranked
 // Comparisons of a lane from which on the lowest candidates are left out first: 8,000
-// rows of 500 bf16 logits with 64 alternatives 39 us, ranked as they are 246.
+// rows of 500 bf16 logits with 64 alternatives 41 us, ranked as they are 247.
 constexpr int kRanking = 640;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLow = -256.0f;  // 2^d is 0 from here on: 0 log 0 = 0, whatever d is
@@ -212,7 +212,7 @@ struct Share {
 };
 
 // A lane's sums over its share, kAhead pieces on their way at once (2,048 rows of
-// 50,021 bf16 logits: 39.5 us, with two 41.7, with six 43.3, with eight 44.2).
+// 50,021 bf16 logits: 40.6 us, with two 43.3, with six 45.0, with eight 48.0).
 constexpr int kAhead = 4;
 template <class E_, int B, bool ENT>
 __device__ __forceinline__ void row_sums(const Share<E_, B>& sh, float c, Sums& sums) {
@@ -242,7 +242,7 @@ __device__ __forceinline__ void row_sums(const Share<E_, B>& sh, float c, Sums& 
 // packed: as signed numbers their order is right where one of them is not negative,
 // and else the least unsigned number is the largest value.  A NaN is the largest
 // value or shows in the sums.  4,096 rows of 50,021 with their gradient, bound by
-// vector instructions: 162.6 us, unpacked for the maximum too 166.3.
+// vector instructions: 166.8 us, unpacked for the maximum too 167.7.
 template <class E_, int B, int NV>
 __device__ __forceinline__ float kept_max(const Kept<E_, B, NV>& kept) {
   constexpr int N = Vec<E_>::N;
@@ -619,7 +619,7 @@ __global__ __launch_bounds__(B, kept_waves(B, NV)) void logprob_kept(Rows r, Res
 // What the slices of a row found, kHeld values a lane.  A slice's values fall: each
 // slice is turned a little further than the one before it, so that the largest ones of
 // all slices lie in different lanes (2 rows of 151,722 fp32 logits with 128 alternatives
-// 29 us, unturned 55).
+// 19 us, unturned 23).
 constexpr int kHeld = 8, kTurn = 37;
 struct Held {
   float v[kHeld];
@@ -1132,27 +1132,28 @@ int check_cotangents(const char* who, const Rows& r, const Cotangents& t) {
 }
 
 // Slices are longer than distillation's, whose join has no alternatives to rank: 8
-// rows of 512 KiB with 20 of them 13.3 us in slices of 8 KiB, 11.8 of 16, 11.6 of 32.  With
+// rows of 512 KiB with 20 of them 13.8 us in slices of 8 KiB, 12.3 of 16, 12.3 of 32.  With
 // many alternatives they are as long as it takes for the join to hold what they find: one
-// row of 600,000 fp32 logits with 20 12.5 us, in slices of 16 KiB 15.8, with 128 23.6 and 64.
+// row of 600,000 fp32 logits with 20 13.3 us, with 128 24.0; a join that reads what slices
+// of 16 KiB found again took 15.8 and 64.
 Cut row_cut(int64_t N, int64_t V, int32_t dtype, int64_t K) {
   const int64_t fewest = (V * elem_size(dtype) * K + kHeld * kJB - 1) / (kHeld * kJB);
   return cut_of(N, V, dtype, fewest > 16384 ? fewest : 16384);
 }
 
-// Lanes of a row: 8,000 rows of 4,000 bf16 logits with 5 alternatives take 27.5 us
-// with 128, 28.5 with 256 and 51.6 with 512; 4,000 of 16,000 31.5, 31.5 and 38.0; 2,048
-// of 50,021 42.0, 41.8 and 41.9 (without alternatives 38 with 512, 43 with 256).
+// Lanes of a row: 8,000 rows of 4,000 bf16 logits with 5 alternatives take 28.1 us
+// with 128, 30.8 with 256 and 52.2 with 512; 4,000 of 16,000 36.3, 36.9 and 43.2; 2,048
+// of 50,021 48.1, 48.3 and 43.6 (without alternatives 42.9, 44.2 and 39.2).
 // With more than kFewTop alternatives 128 lanes say too little about where they are, once
-// 256 have a piece or nearly: 300 rows of 4,000 with 128 of them 11.3 us, with 128 lanes
-// 30.5; 4,000 rows 35.0 and 50.3, with 64 of them 22.4 and 25.2; but 4,000 rows of 500 fp32
-// logits with 128 33.9 and 28.9.
+// 256 have a piece or nearly: 300 rows of 4,000 with 128 of them 11.7 us, with 128 lanes
+// 29.4; 4,000 rows 38.2 and 51.7, with 64 of them 24.3 and 25.6; but 4,000 rows of 500 fp32
+// logits with 128 35.8 and 30.3.
 constexpr int64_t kShortRow = 16384, kMiddleRow = 65536, kWideRow = 3200;
 // Many short rows stay in registers: their maximum is known before the sums, and the
 // alternatives are looked for in the lanes that read them.  8,000 rows of 4,000 bf16
-// logits 15.1 us (streamed 19.7), with 5 alternatives 24.0 (26.2); 4,000 of 16,000 without
-// 23.1 (28.5), with 5 50 (31); of more than 64 KiB and of few rows streaming is as fast or
-// faster (300 of 1,000 fp32 logits 4.8 against 5.7, 2,048 of 50,021 39.7 against 41.7).
+// logits 17.2 us (streamed 20.6), with 5 alternatives 25.8 (28.1); 4,000 of 16,000 without
+// 28.5 (33.4), with 5 50 (31); of more than 64 KiB and of few rows streaming is as fast or
+// faster (300 of 1,000 fp32 logits 4.9 against 5.3, 2,048 of 50,021 39.7 against 41.7).
 constexpr int64_t kKeptRows = 2048;
 
 int64_t parts_bytes(int64_t N, int64_t V, int32_t dtype, int64_t K) {
