@@ -791,9 +791,10 @@ int64_t diffopt_distill_workspace(int64_t N, int64_t V, int32_t dtype,
  * Tokens from lengths[b] on are not read and get h = 0.  A gate of -inf
  * multiplies the state by 0: it forgets what came before if that is finite, and
  * an infinite state or a NaN is a NaN from there on.  Gates above 0 are taken
- * too; where the product of a run of them leaves fp32, results do.  Results must not overlap operands or
- * one another where an entry point does not say that they may (rows may lie
- * between another array's rows of the same strides).
+ * too; where the product of a run of them leaves fp32, results do.
+ * Results must not overlap operands or one another where an entry point does
+ * not say that they may: such calls are refused.  Rows may lie between another
+ * array's rows of the same strides; at other strides the spans lie apart.
  *   log_gate, x, h  [B][T][C]: diffopt_heads whose heads are not used
  *   lengths    DEVICE int32 [B] in [0, T] (clamped), or NULL for T
  *   state, state_out  fp32 [B][C], or NULL (zeros / not wanted); state_out
